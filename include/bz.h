@@ -487,6 +487,134 @@ int bz_last_path(void);
 /* Number of kernels this library has launched from the calling process since it was loaded. */
 uint64_t bz_kernel_launch_count(void);
 
+/*
+ * ---- A worker's step ---------------------------------------------------------------------------
+ * Operators of a language model's training step for the workers whose file gradients the calls above
+ * aggregate.  The vote is exact, so the r honest copies of a file's gradient have to agree bit for bit:
+ * every sum below is taken in an order fixed by the sizes and by how the rows sit relative to 16-byte
+ * boundaries (no floating-point atomics, nothing that depends on load or on the stream), so two GPUs of
+ * this kind given the same inputs, laid out alike, return the same bits.
+ *
+ * Types: BZ_F32, BZ_F16, BZ_BF16 name IEEE binary32, binary16 and bfloat16 elements.  Sums, softmax
+ * statistics and losses are binary32; a result is rounded once, to its own type, when it is stored.
+ * Any base alignment and leading dimension that the element type allows is accepted; rows whose addresses
+ * are equal modulo 16 in every tensor of a call (for bz_glu: bases and leading dimensions that are
+ * multiples of 16 bytes) take the wide loads, the others a slower path with the same results.
+ */
+#define BZ_F32 0
+#define BZ_F16 1
+#define BZ_BF16 2
+
+#define BZ_ACT_SILU 0      /* g / (1 + exp(-g))                                             */
+#define BZ_ACT_GELU_TANH 1 /* g/2 * (1 + tanh(sqrt(2/pi) * (g + 0.044715 g^3)))             */
+#define BZ_ACT_GELU 2      /* g/2 * (1 + erf(g / sqrt(2)))                                  */
+#define BZ_ACT_RELU 3      /* max(g, 0); derivative 0 at 0                                  */
+
+/*
+ * Gated feed-forward block: g = x w_gate^T, u = x w_up^T, h = act(g) * u, both projections, the
+ * activation and the product in one kernel on the tensor cores.
+ *   x device [m][k] with ld_x;  w_gate, w_up device [n][k], both with ld_w;  h device [m][n] with ld_h.
+ *   dtype   BZ_F16 or BZ_BF16 (x, weights, h);  act  BZ_ACT_*.
+ *   preact  device binary32 [2][m][n], 16-byte aligned, or NULL: receives g and then u for the backward
+ *           call.  A caller short of memory passes NULL here and repeats the call with one shared buffer
+ *           before the backward call.
+ *   k == 0 gives h = 0 (empty sums); m == 0 or n == 0 is a successful no-op.
+ *   workspace  device, bz_glu_workspace_bytes(m, n, k, dtype, 0) bytes, 256-byte aligned; the bytes are 0
+ *           and NULL will do where x and the weights are 16-byte aligned with leading dimensions that are
+ *           multiples of 8 (other operands are laid out there first).
+ * m, n, k up to 2^31 - 1 each.  The tensor-core kernels bound every wait; one that runs out stops the
+ * kernel early with incomplete outputs and counts in bz_pipeline_timeouts().
+ */
+int bz_glu(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w, int64_t m, int64_t n, int64_t k,
+           int dtype, int act, void* h, int64_t ld_h, float* preact, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradient, with preact as bz_glu left it: dg = dh * u * act'(g) and du = dh * act(g), rounded to
+ * dtype (the operands of the products below are 16-bit), then
+ *   dx = dg w_gate + du w_up,   dw_gate = dg^T x,   dw_up = du^T x.
+ *   dh device [m][n] with ld_dh;  dx device [m][k] with ld_dx, or NULL;  dw_gate, dw_up device [n][k], both
+ *   with ld_dw, or both NULL.  grad_dtype is the type of dw_gate and dw_up: dtype, or BZ_F32 to keep the
+ *   32-bit sums - then they may lie in a binary32 gradient row as the aggregation calls read it.
+ *   m == 0 writes dw_gate = dw_up = 0; n == 0 writes dx = 0.
+ *   workspace  device, bz_glu_workspace_bytes(m, n, k, dtype, 1) bytes, 256-byte aligned.
+ */
+int bz_glu_backward(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w, const float* preact,
+                    const void* dh, int64_t ld_dh, int64_t m, int64_t n, int64_t k, int dtype, int act, void* dx, int64_t ld_dx,
+                    void* dw_gate, void* dw_up, int64_t ld_dw, int grad_dtype, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/* Device scratch of bz_glu (backward == 0) or bz_glu_backward for any alignment; 0 for arguments they refuse. */
+size_t bz_glu_workspace_bytes(int64_t m, int64_t n, int64_t k, int dtype, int backward);
+
+/*
+ * Softmax of attention scores with a learned relative position bias, applied on the way.
+ *   z[b][h][i][j] = scale * scores[b][h][i][j] + table[bucket(j - p)][h],   p = i + q_start[b],
+ * over the keys j that query i sees: j < k_len[b], and j <= p when causal.  probs gets the softmax of z
+ * over them and 0 elsewhere; a query that sees no key, or none with z > -inf, gets a row of zeros.  Scores
+ * that are not seen are not read into any sum (they may be infinite or NaN).
+ * bucket(rel): with both directions (bidirectional != 0) nb = buckets / 2, n = |rel|, and nb is added
+ * where rel > 0; otherwise nb = buckets, n = max(-rel, 0).  Distances n < e = nb / 2 have a bucket each;
+ * from there bucket e + t, t = 0 .. nb - e - 1, begins at the smallest n >= e * (max_distance / e)^(t / (nb - e)).
+ *   scores, probs  device [b][h][tq][tk], unit stride along tk; strides of b, h, tq in elements in host
+ *           arrays of three (any sign-free layout; probs may be scores itself).  dtype: BZ_F32, _F16, _BF16.
+ *   table   device binary32 [buckets][h], contiguous;  2 <= buckets <= 256 (4 <= buckets, even, when
+ *           bidirectional), nb / 2 < max_distance <= BZ_MAX_DISTANCE.
+ *   k_len   device int32 [b], values taken into [0, tk], or NULL: all tk.
+ *   q_start device int32 [b], or NULL: all 0.  A single query behind its cache: q_start[b] = k_len[b] - 1.
+ *   stats   device binary32 [b][h][tq][2] for the backward call, or NULL: the row's largest z (-inf for an
+ *           empty row) and the sum of exp(z - that) (0).  Kept apart, since their logarithmic sum would lose
+ *           the last digits where z is large.
+ * b, h <= 65535, tq, tk < 2^31; any of them 0 is a successful no-op.
+ */
+#define BZ_MAX_DISTANCE 2048
+int bz_bias_softmax(const void* scores, const int64_t* strides_scores, int dtype, int64_t b, int64_t h, int64_t tq, int64_t tk,
+                    const float* table, int buckets, int max_distance, int bidirectional, int causal, float scale,
+                    const int32_t* k_len, const int32_t* q_start, void* probs, const int64_t* strides_probs, float* stats, void* stream);
+
+/*
+ * Its gradient.  With p the probabilities (recomputed in binary32 from scores and stats), dp = dprobs and
+ * D = sum over j of p dp:   dz = p (dp - D),  dscores = scale * dz,
+ * dtable[c][h] = sum of dz over all b, i, j whose bucket is c.
+ *   dprobs, dscores  like scores (dscores may be dprobs or scores itself), dscores may be NULL.
+ *   dtable  device binary32 [buckets][h], overwritten, or NULL.
+ *   workspace  device, bz_bias_softmax_workspace_bytes(b, h, tq, tk, buckets) bytes, 256-byte aligned (needed
+ *           with dtable only).
+ */
+int bz_bias_softmax_backward(const void* scores, const int64_t* strides_scores, int dtype, int64_t b, int64_t h, int64_t tq,
+                             int64_t tk, const float* table, int buckets, int max_distance, int bidirectional, int causal,
+                             float scale, const int32_t* k_len, const int32_t* q_start, const float* stats, const void* dprobs,
+                             const int64_t* strides_dprobs, void* dscores, const int64_t* strides_dscores, float* dtable,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+size_t bz_bias_softmax_workspace_bytes(int64_t b, int64_t h, int64_t tq, int64_t tk, int buckets);
+
+/*
+ * Distillation from a teacher's t largest logits per position, temperature T:
+ *   p = softmax over the kept entries of teacher / T,   q = softmax over all v of logits / T,
+ *   loss = T^2 * sum over the kept entries e of p_e (log p_e - log q[index_e]),
+ *   dlogits[c] = dloss * T * (q[c] - sum of p_e with index_e = c).
+ * An entry is kept if 0 <= index < v and its teacher logit is not -inf; a position that keeps none
+ * has loss 0 and dlogits 0.  Two kept entries may name the same c.  Student logits may be -inf (a masked
+ * vocabulary): q is 0 there, and a kept entry that names such a c makes the loss +inf; in a position whose
+ * logits are all -inf every q counts as 0.
+ *   logits  device [m][v] with ld, dtype BZ_F32, _F16, _BF16;  teacher device binary32 [m][t], index device
+ *           int32 [m][t], both contiguous, 1 <= t <= BZ_MAX_TOP;  temperature > 0, finite.
+ *   loss    device binary32 [m];  stats  device binary32 [m][2]: the row's largest logits / T and the sum of
+ *           exp(logits / T - that), for the backward call; either may be NULL.
+ *   dloss   device binary32 [m], the upstream gradient of each position's loss, or NULL: all 1.
+ *   dlogits device [m][v] with ld_d, dtype's elements, or NULL: the loss alone.  With it the logits are
+ *           read once for loss and gradient together.  It may be logits itself (ld_d == ld).
+ * v < 2^31; m == 0 is a successful no-op; v == 0 writes loss 0, stats (-inf, 0).
+ */
+#define BZ_MAX_TOP 1024
+int bz_distill(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const float* teacher, const int32_t* index, int t,
+               float temperature, const float* dloss, float* loss, float* stats, void* dlogits, int64_t ld_d, void* stream);
+
+/* The gradient alone, with stats as bz_distill left it, for a dloss that is known only after the loss.  dlogits may be
+ * logits itself. */
+int bz_distill_backward(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const float* teacher, const int32_t* index,
+                        int t, float temperature, const float* stats, const float* dloss, void* dlogits, int64_t ld_d, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

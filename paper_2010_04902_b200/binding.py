@@ -21,6 +21,9 @@ ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_PRECONDITION, ERR_WORKSPACE, ERR_BUDGET, E
 OP_PAIRDIST, OP_MULTIKRUM, OP_BULYAN, OP_WORST_CASE, OP_VOTE_MEDIAN_HOST, OP_WORST_CASE_MOLS, OP_VOTE_VECTORWISE = 1, 2, 3, 4, 5, 6, 7
 MAX_R, MAX_F = 15, 128
 STATUS_RECOMPUTED, STATUS_STOPPED_EARLY = 1, 2
+F32, F16, BF16 = 0, 1, 2
+ACT_SILU, ACT_GELU_TANH, ACT_GELU, ACT_RELU = range(4)
+MAX_DISTANCE, MAX_TOP = 2048, 1024
 PATH_NONE, PATH_STAGED, PATH_REGISTERS, PATH_GENERIC, PATH_TENSOR, PATH_FP32, PATH_FP32_FUSED, PATH_FP64 = range(8)
 
 
@@ -36,6 +39,7 @@ class BzError(RuntimeError):
 _lib = None
 
 _c_int, _c_i64, _c_sz, _c_vp, _c_u64 = ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_uint64
+_c_f = ctypes.c_float
 
 _SIGNATURES = {
     "bz_assign_mols": (_c_int, [_c_int, _c_int, _c_vp, _c_vp, _c_vp]),
@@ -79,6 +83,18 @@ _SIGNATURES = {
     "bz_debug_stall_pipeline": (_c_int, [_c_int]),
     "bz_last_path": (_c_int, []),
     "bz_stream_probe": (_c_int, [_c_vp, _c_sz, _c_int, _c_vp, _c_vp]),
+    "bz_glu": (_c_int, [_c_vp, _c_i64, _c_vp, _c_vp, _c_i64, _c_i64, _c_i64, _c_i64, _c_int, _c_int, _c_vp, _c_i64, _c_vp, _c_vp, _c_sz,
+                        _c_vp]),
+    "bz_glu_backward": (_c_int, [_c_vp, _c_i64, _c_vp, _c_vp, _c_i64, _c_vp, _c_vp, _c_i64, _c_i64, _c_i64, _c_i64, _c_int, _c_int, _c_vp,
+                                 _c_i64, _c_vp, _c_vp, _c_i64, _c_int, _c_vp, _c_sz, _c_vp]),
+    "bz_glu_workspace_bytes": (_c_sz, [_c_i64, _c_i64, _c_i64, _c_int, _c_int]),
+    "bz_bias_softmax": (_c_int, [_c_vp, _c_vp, _c_int, _c_i64, _c_i64, _c_i64, _c_i64, _c_vp, _c_int, _c_int, _c_int, _c_int, _c_f, _c_vp,
+                                 _c_vp, _c_vp, _c_vp, _c_vp, _c_vp]),
+    "bz_bias_softmax_backward": (_c_int, [_c_vp, _c_vp, _c_int, _c_i64, _c_i64, _c_i64, _c_i64, _c_vp, _c_int, _c_int, _c_int, _c_int, _c_f,
+                                          _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_sz, _c_vp]),
+    "bz_bias_softmax_workspace_bytes": (_c_sz, [_c_i64, _c_i64, _c_i64, _c_i64, _c_int]),
+    "bz_distill": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_vp, _c_int, _c_f, _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]),
+    "bz_distill_backward": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_vp, _c_int, _c_f, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]),
 }
 
 EXPORTS = sorted(_SIGNATURES)
@@ -585,3 +601,223 @@ def vote_bulyan(replicas: torch.Tensor, c: int, voted: torch.Tensor | None = Non
                               sel.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
     _check(st, "bz_vote_bulyan")
     return out, sel[:max(theta, 0)], voted
+
+
+# ------------------------------------------------------------------------------------- a worker's step
+
+_DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+_ACTS = {"silu": ACT_SILU, "gelu_tanh": ACT_GELU_TANH, "gelu": ACT_GELU, "relu": ACT_RELU}
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda or t.dtype not in _DTYPES:
+        raise TypeError("%s must be a CUDA tensor of float32, float16 or bfloat16" % name)
+    return _DTYPES[t.dtype]
+
+
+def _matrix(t: torch.Tensor, name: str):
+    """_matrix(), and rows that overlap (an expanded tensor's) are refused: there is no leading dimension for them."""
+    f, d, ld = _rows(t, name)
+    if f > 1 and t.stride(0) < d:
+        raise ValueError("%s has rows that overlap: make it contiguous" % name)
+    return f, d, ld
+
+
+def _shaped(t: torch.Tensor, shape, dtype, name: str) -> int:
+    """Address of a tensor of exactly this shape and type (strides are the caller's business)."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s" % (name, "".join("[%d]" % n for n in shape)))
+    return _dev(t, dtype, name)
+
+
+def _packed(t, shape, dtype, name: str):
+    """Address of a contiguous tensor of this shape and type, or None."""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return _shaped(t, shape, dtype, name)
+
+
+def _act(name: str) -> int:
+    if name not in _ACTS:
+        raise ValueError("act must be one of %s" % ", ".join(sorted(_ACTS)))
+    return _ACTS[name]
+
+
+def _like_matrix(t: torch.Tensor) -> torch.Tensor:
+    """A new tensor of t's shape whose rows are as far apart as t's: the kernels' wide loads and stores need rows that
+    sit alike relative to 16-byte boundaries."""
+    ld = t.stride(-2) if t.dim() > 1 and t.shape[-2] > 1 else t.shape[-1]
+    if ld <= t.shape[-1] or ld > 2 * t.shape[-1]:
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return torch.empty(t.shape[:-1] + (ld,), dtype=t.dtype, device=t.device)[..., :t.shape[-1]]
+
+
+def _glu_operands(x, w_gate, w_up):
+    m, k, ld_x = _matrix(x, "x")
+    n, k2, ld_w = _matrix(w_gate, "w_gate")
+    if k2 != k or tuple(w_up.shape) != (n, k):
+        raise ValueError("w_gate and w_up must both be [n][%d]" % k)
+    if _matrix(w_up, "w_up")[2] != ld_w:
+        raise ValueError("w_gate and w_up must have the same leading dimension")
+    return m, n, k, ld_x, ld_w
+
+
+def _glu_workspace(m, n, k, dtype, backward, operands, lds, workspace, device):
+    if workspace is not None:
+        return workspace.data_ptr(), workspace.numel()
+    if not backward and not any(ld % 8 for ld in lds) and not any(p % 16 for p in operands):
+        return None, 0
+    ws = torch.empty(max(256, lib().bz_glu_workspace_bytes(m, n, k, dtype, backward)), dtype=torch.uint8, device=device)
+    return ws.data_ptr(), ws.numel()
+
+
+def glu_workspace_bytes(m: int, n: int, k: int, dtype=torch.bfloat16, backward: bool = False) -> int:
+    return int(lib().bz_glu_workspace_bytes(m, n, k, _DTYPES[dtype], 1 if backward else 0))
+
+
+def glu(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "silu", h: torch.Tensor | None = None,
+        preact: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """bz_glu: act(x w_gate^T) * (x w_up^T) for x [m][k], weights [n][k] (float16 or bfloat16).  `preact`, binary32
+    [2][m][n], receives both projections for glu_backward."""
+    m, n, k, ld_x, ld_w = _glu_operands(x, w_gate, w_up)
+    dt = _dtype(x, "x")
+    if h is None:
+        h = torch.empty((m, n), dtype=x.dtype, device=x.device)
+    px, pg, pu = _dev(x, x.dtype, "x"), _dev(w_gate, x.dtype, "w_gate"), _dev(w_up, x.dtype, "w_up")
+    ws, ws_bytes = _glu_workspace(m, n, k, dt, 0, (px, pg, pu), (ld_x, ld_w), workspace, x.device)
+    st = lib().bz_glu(px, ld_x, pg, pu, ld_w, m, n, k, dt, _act(act), _shaped(h, (m, n), x.dtype, "h"), _matrix(h, "h")[2],
+                      _packed(preact, (2, m, n), torch.float32, "preact"), ws, ws_bytes, _stream())
+    _check(st, "bz_glu")
+    return h
+
+
+def glu_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, preact: torch.Tensor, dh: torch.Tensor,
+                 act: str = "silu", dx: torch.Tensor | None = None, dw_gate: torch.Tensor | None = None,
+                 dw_up: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """bz_glu_backward: returns (dx, dw_gate, dw_up).  dw_gate and dw_up may be given as float32 tensors (views of a
+    gradient row, for instance) to keep the 32-bit sums; new ones have the weights' type."""
+    m, n, k, ld_x, ld_w = _glu_operands(x, w_gate, w_up)
+    dt = _dtype(x, "x")
+    if dx is None:
+        dx = torch.empty((m, k), dtype=x.dtype, device=x.device)
+    if (dw_gate is None) != (dw_up is None):
+        raise ValueError("give both dw_gate and dw_up, or neither")
+    if dw_gate is None:
+        dw_gate = torch.empty((n, k), dtype=x.dtype, device=x.device)
+        dw_up = torch.empty((n, k), dtype=x.dtype, device=x.device)
+    px, pg, pu = _dev(x, x.dtype, "x"), _dev(w_gate, x.dtype, "w_gate"), _dev(w_up, x.dtype, "w_up")
+    pdg, pdu = _shaped(dw_gate, (n, k), dw_gate.dtype, "dw_gate"), _shaped(dw_up, (n, k), dw_gate.dtype, "dw_up")
+    ld_dw = _matrix(dw_gate, "dw_gate")[2]
+    if _matrix(dw_up, "dw_up")[2] != ld_dw:
+        raise ValueError("dw_gate and dw_up must have the same leading dimension")
+    ws, ws_bytes = _glu_workspace(m, n, k, dt, 1, (), (), workspace, x.device)
+    st = lib().bz_glu_backward(px, ld_x, pg, pu, ld_w, _packed(preact, (2, m, n), torch.float32, "preact"),
+                               _shaped(dh, (m, n), x.dtype, "dh"), _matrix(dh, "dh")[2], m, n, k, dt, _act(act),
+                               _shaped(dx, (m, k), x.dtype, "dx"), _matrix(dx, "dx")[2], pdg, pdu, ld_dw, _dtype(dw_gate, "dw_gate"),
+                               ws, ws_bytes, _stream())
+    _check(st, "bz_glu_backward")
+    return dx, dw_gate, dw_up
+
+
+def _strides(t: torch.Tensor, name: str):
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError("%s must be [b][h][tq][tk] with unit stride along tk" % name)
+    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+
+
+def _bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start):
+    b, h, tq, tk = scores.shape
+    if table.dim() != 2 or table.shape[1] != h:
+        raise ValueError("table must be [buckets][%d]" % h)
+    return [_packed(table, table.shape, torch.float32, "table"), table.shape[0], max_distance, 1 if bidirectional else 0,
+            1 if causal else 0, float(scale), _packed(k_len, (b,), torch.int32, "k_len"), _packed(q_start, (b,), torch.int32, "q_start")]
+
+
+def bias_softmax(scores: torch.Tensor, table: torch.Tensor, max_distance: int = 128, bidirectional: bool = True,
+                 causal: bool = False, scale: float = 1.0, k_len: torch.Tensor | None = None,
+                 q_start: torch.Tensor | None = None, probs: torch.Tensor | None = None, stats: torch.Tensor | None = None):
+    """bz_bias_softmax: softmax over keys of scale * scores [b][h][tq][tk] + table[bucket(key - query)][h].  Returns
+    (probs, stats)."""
+    strides = _strides(scores, "scores")
+    if probs is None:
+        probs = _like_matrix(scores)
+    if stats is None:
+        stats = torch.empty(scores.shape[:3] + (2,), dtype=torch.float32, device=scores.device)
+    st = lib().bz_bias_softmax(scores.data_ptr(), strides, _dtype(scores, "scores"), *scores.shape,
+                               *_bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start),
+                               _shaped(probs, scores.shape, scores.dtype, "probs"), _strides(probs, "probs"),
+                               _packed(stats, tuple(scores.shape[:3]) + (2,), torch.float32, "stats"), _stream())
+    _check(st, "bz_bias_softmax")
+    return probs, stats
+
+
+def bias_softmax_backward(scores: torch.Tensor, table: torch.Tensor, stats: torch.Tensor, dprobs: torch.Tensor,
+                          max_distance: int = 128, bidirectional: bool = True, causal: bool = False, scale: float = 1.0,
+                          k_len: torch.Tensor | None = None, q_start: torch.Tensor | None = None,
+                          dscores: torch.Tensor | None = None, dtable: torch.Tensor | None = None,
+                          workspace: torch.Tensor | None = None):
+    """bz_bias_softmax_backward: returns (dscores, dtable)."""
+    strides = _strides(scores, "scores")
+    if dscores is None:
+        dscores = _like_matrix(scores)
+    if dtable is None:
+        dtable = torch.empty_like(table)
+    form = _bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start)
+    ws = workspace
+    if ws is None:
+        ws = torch.empty(max(256, lib().bz_bias_softmax_workspace_bytes(*scores.shape, table.shape[0])), dtype=torch.uint8,
+                         device=scores.device)
+    st = lib().bz_bias_softmax_backward(scores.data_ptr(), strides, _dtype(scores, "scores"), *scores.shape, *form,
+                                        _packed(stats, tuple(scores.shape[:3]) + (2,), torch.float32, "stats"),
+                                        _shaped(dprobs, scores.shape, scores.dtype, "dprobs"), _strides(dprobs, "dprobs"),
+                                        _shaped(dscores, scores.shape, scores.dtype, "dscores"), _strides(dscores, "dscores"),
+                                        _packed(dtable, table.shape, torch.float32, "dtable"), ws.data_ptr(), ws.numel(), _stream())
+    _check(st, "bz_bias_softmax_backward")
+    return dscores, dtable
+
+
+def _teacher(logits, teacher, index):
+    m = logits.shape[0]
+    if teacher.dim() != 2 or teacher.shape[0] != m:
+        raise ValueError("teacher must be [%d][t]" % m)
+    return [_packed(teacher, teacher.shape, torch.float32, "teacher"), _packed(index, teacher.shape, torch.int32, "index"), teacher.shape[1]]
+
+
+def distill(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, temperature: float = 1.0,
+            dloss: torch.Tensor | None = None, loss: torch.Tensor | None = None, stats: torch.Tensor | None = None,
+            dlogits: torch.Tensor | None = None):
+    """bz_distill: the loss of each position against the teacher's top logits.  Returns (loss, stats); with `dloss`
+    (float32 [m]) or `dlogits` given also the gradient, from the same pass: (loss, stats, dlogits)."""
+    m, v, ld = _matrix(logits, "logits")
+    dt = _dtype(logits, "logits")
+    grad = dloss is not None or dlogits is not None
+    if loss is None:
+        loss = torch.empty(m, dtype=torch.float32, device=logits.device)
+    if stats is None:
+        stats = torch.empty((m, 2), dtype=torch.float32, device=logits.device)
+    if grad and dlogits is None:
+        dlogits = _like_matrix(logits)
+    st = lib().bz_distill(logits.data_ptr(), ld, dt, m, v, *_teacher(logits, teacher, index), float(temperature),
+                          _packed(dloss, (m,), torch.float32, "dloss"), _packed(loss, (m,), torch.float32, "loss"),
+                          _packed(stats, (m, 2), torch.float32, "stats"),
+                          _shaped(dlogits, (m, v), logits.dtype, "dlogits") if grad else None,
+                          _matrix(dlogits, "dlogits")[2] if grad else 0, _stream())
+    _check(st, "bz_distill")
+    return (loss, stats, dlogits) if grad else (loss, stats)
+
+
+def distill_backward(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, stats: torch.Tensor,
+                     dloss: torch.Tensor | None = None, temperature: float = 1.0,
+                     dlogits: torch.Tensor | None = None) -> torch.Tensor:
+    """bz_distill_backward: the gradient alone, with stats as distill() returned it."""
+    m, v, ld = _matrix(logits, "logits")
+    if dlogits is None:
+        dlogits = _like_matrix(logits)
+    st = lib().bz_distill_backward(logits.data_ptr(), ld, _dtype(logits, "logits"), m, v, *_teacher(logits, teacher, index),
+                                   float(temperature), _packed(stats, (m, 2), torch.float32, "stats"),
+                                   _packed(dloss, (m,), torch.float32, "dloss"),
+                                   _shaped(dlogits, (m, v), logits.dtype, "dlogits"), _matrix(dlogits, "dlogits")[2], _stream())
+    _check(st, "bz_distill_backward")
+    return dlogits

@@ -1,0 +1,573 @@
+// Softmax of attention scores with a learned relative position bias, and its gradient.
+//
+// Forward: z = scale*s + bias[bucket(j - p)], P = e^(z - M) / S.  One read of the scores, one
+// write of P: bound by memory.  A row is held in registers by G threads (32 elements each), so that the maximum, the
+// sum and the result need no second read; rows longer than the largest group loop twice.  Every thread forms its
+// exponentials relative to its own maximum and one joint reduction of (maximum, sum) pairs follows, instead of one
+// reduction for each.
+// The bias depends on j - p alone and is constant from max_distance on, so a CTA keeps the head's values for the
+// 2*max_distance + 1 distances in shared memory (with one word of padding every eight: a lane's eight neighbours
+// and the next lane's eight would otherwise share banks), and slots that lie beyond take one of the two end values.
+//
+// Backward: p from the kept maximum and sum, D = sum p dp, dz = p (dp - D).  The table's gradient needs the sum of dz over
+// each diagonal of the scores inside the window and one sum for either side beyond it.  A warp owns a private array
+// of diagonals: a row meets each diagonal once, so its lanes add without conflict, row after row, in a fixed order;
+// the far sums stay in registers.  CTAs leave one value a bucket and a last kernel adds those in order.
+#include "worker_common.cuh"
+
+namespace bz {
+
+namespace {
+
+constexpr int kMaxStarts = 128;  // nb - nb/2 with nb up to 256
+
+struct BiasForm {
+    const float* table;
+    const int32_t *k_len, *q_start;
+    float scale;
+    int buckets, nb, exact, distance, bidirectional, causal;
+    int h;
+    int64_t tq, tk;
+    int rows_per_cta;
+    uint16_t starts[kMaxStarts];  // starts[t]: smallest distance of bucket exact + t
+};
+
+template <typename T> struct Rows4 {  // a [b][h][tq][tk] tensor
+    T* p;
+    int64_t b, h, q;
+    __device__ T* row(int64_t ib, int64_t ih, int64_t iq) const { return p + ib * b + ih * h + iq * q; }
+};
+
+__device__ __forceinline__ int bucket_of(const BiasForm& f, int rel) {
+    const int n = f.bidirectional ? abs(rel) : max(-rel, 0);
+    int c = n;
+    if (n >= f.exact) {
+        c = f.exact;
+        for (int t = 1; t < f.nb - f.exact; ++t) c += n >= f.starts[t];
+    }
+    return f.bidirectional && rel > 0 ? c + f.nb : c;
+}
+
+__device__ __forceinline__ int padded(int i) { return i + (i >> 3); }
+
+// bias[padded(rel + distance)]
+__device__ __forceinline__ void build_bias(const BiasForm& f, int head, float* bias) {
+    for (int d = threadIdx.x; d <= 2 * f.distance; d += blockDim.x)
+        bias[padded(d)] = f.table[bucket_of(f, d - f.distance) * f.h + head];
+}
+
+struct RowRange {
+    int64_t p, end;  // position of the query among the keys; keys [0, end) are seen
+};
+__device__ __forceinline__ RowRange row_range(const BiasForm& f, int ib, int64_t iq) {
+    int64_t end = f.tk;
+    if (f.k_len != nullptr) end = min(end, static_cast<int64_t>(max(f.k_len[ib], 0)));
+    const int64_t p = iq + (f.q_start != nullptr ? f.q_start[ib] : 0);
+    if (f.causal) end = min(end, max(p + 1, int64_t(0)));
+    return {p, end};
+}
+
+// z[i] = scale*s[i] + bias for the keys j0 + i that are seen, -inf for the others.
+template <int VEC>
+__device__ __forceinline__ void add_bias(const BiasForm& f, const float* bias, const RowRange& r, int64_t j0, float (&z)[VEC]) {
+    const int64_t rel = j0 - r.p;
+    if (rel >= f.distance || rel + VEC - 1 <= -f.distance) {
+        const float c = bias[padded(rel > 0 ? 2 * f.distance : 0)];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) z[i] = fmaf(z[i], f.scale, c);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const int d = max(-f.distance, min(f.distance, static_cast<int>(rel) + i)) + f.distance;
+            z[i] = fmaf(z[i], f.scale, bias[padded(d)]);
+        }
+    }
+    if (j0 < 0 || j0 + VEC > r.end) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (j0 + i < 0 || j0 + i >= r.end) z[i] = -INFINITY;
+    }
+}
+
+// Joins one value per thread over the G threads of a row.  G > 32: the CTA is the group; `part` holds two sets of
+// warp results used in turn, so one barrier a call suffices.
+template <int G> __device__ __forceinline__ MaxSum group_join(MaxSum v, MaxSum (*part)[16], int turn) {
+    v = warp_join(v);
+    if constexpr (G > 32) {
+        if ((threadIdx.x & 31) == 0) part[turn & 1][threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = part[turn & 1][0];
+#pragma unroll
+        for (int w = 1; w < G / 32; ++w) v = join(v, part[turn & 1][w]);
+    }
+    return v;
+}
+template <int G> __device__ __forceinline__ float group_sum(float v, float (*part)[16], int turn) {
+    v = warp_sum(v);
+    if constexpr (G > 32) {
+        if ((threadIdx.x & 31) == 0) part[turn & 1][threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = part[turn & 1][0];
+#pragma unroll
+        for (int w = 1; w < G / 32; ++w) v += part[turn & 1][w];
+    }
+    return v;
+}
+
+template <int G> struct Cta {
+    static constexpr int kThreads = G > 32 ? G : 256;
+    static constexpr int kRows = kThreads / G;  // rows in hand at a time
+};
+
+// E elements a thread are held in registers; E == 0: the row is read twice.
+template <typename T, int VEC, int G, int E>
+__global__ void __launch_bounds__(Cta<G>::kThreads)
+    bias_softmax_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<T> probs, MaxSum* stats) {
+    extern __shared__ float bias[];
+    __shared__ MaxSum part[2][16];
+    constexpr int kSlots = E / VEC;
+    const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y;
+    build_bias(f, ih, bias);
+    __syncthreads();
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta;
+    for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
+        const int64_t iq = first + it + threadIdx.x / G;
+        if (G > 32 && first + it >= f.tq) break;
+        if (G == 32 && iq >= f.tq) break;
+        const RowRange r = row_range(f, ib, iq);
+        const T* in = scores.row(ib, ih, iq);
+        T* out = probs.row(ib, ih, iq);
+        const int lead = row_lead<T, VEC>(in);
+        MaxSum v{-INFINITY, 0.f};
+        if constexpr (E > 0) {
+            float z[kSlots][VEC];
+#pragma unroll
+            for (int c = 0; c < kSlots; ++c) {
+                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) z[c][i] = -INFINITY;
+                if (j0 < r.end) load_slot<T, VEC>(in, j0, f.tk, 0.f, z[c]);
+            }
+#pragma unroll
+            for (int c = 0; c < kSlots; ++c) {
+                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
+                if (j0 < r.end) add_bias<VEC>(f, bias, r, j0, z[c]);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v.m = fmaxf(v.m, z[c][i]);
+            }
+            const float own = finite_or_zero(v.m);
+#pragma unroll
+            for (int c = 0; c < kSlots; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    z[c][i] = exp_below(z[c][i] - own);
+                    v.s += z[c][i];
+                }
+            const MaxSum all = group_join<G>(v, part, it);
+            const float norm = all.s == 0.f ? 0.f : exp_below(v.m - finite_or_zero(all.m)) / all.s;
+#pragma unroll
+            for (int c = 0; c < kSlots; ++c) {
+                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
+                if (j0 < f.tk) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) z[c][i] = j0 < r.end && norm != 0.f ? z[c][i] * norm : 0.f;
+                    store_slot<T, VEC>(out, j0, f.tk, z[c]);
+                }
+            }
+            if (t == 0 && stats != nullptr) stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq] = all;
+        } else {
+            for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < r.end; j0 += G * VEC) {
+                float z[VEC];
+                load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
+                add_bias<VEC>(f, bias, r, j0, z);
+                MaxSum w{-INFINITY, 0.f};
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) w.m = fmaxf(w.m, z[i]);
+                const float own = finite_or_zero(w.m);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) w.s += exp_below(z[i] - own);
+                v = join(v, w);
+            }
+            const MaxSum all = group_join<G>(v, part, it);
+            const float top = finite_or_zero(all.m), norm = all.s == 0.f ? 0.f : 1.f / all.s;
+            for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < f.tk; j0 += G * VEC) {
+                float z[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) z[i] = 0.f;
+                if (j0 < r.end && norm != 0.f) {
+                    load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
+                    add_bias<VEC>(f, bias, r, j0, z);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) z[i] = exp_below(z[i] - top) * norm;
+                }
+                store_slot<T, VEC>(out, j0, f.tk, z);
+            }
+            if (t == 0 && stats != nullptr) stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq] = all;
+        }
+    }
+}
+
+// One slot of the table's gradient: dz of the keys j0 .. j0 + VEC - 1 (0 where a key is not seen).
+template <int VEC>
+__device__ __forceinline__ void add_diagonals(const BiasForm& f, float* diag, int64_t rel, const float (&dz)[VEC], float& left, float& right) {
+    if (rel >= f.distance || rel + VEC - 1 <= -f.distance) {
+        float s = dz[0];
+#pragma unroll
+        for (int i = 1; i < VEC; ++i) s += dz[i];
+        if (rel > 0)
+            right += s;
+        else
+            left += s;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const int r = static_cast<int>(rel) + i;
+            if (r >= f.distance)
+                right += dz[i];
+            else if (r <= -f.distance)
+                left += dz[i];
+            else
+                diag[padded(r + f.distance)] += dz[i];
+        }
+    }
+}
+
+template <typename T, int VEC, int G, int E>
+__global__ void __launch_bounds__(Cta<G>::kThreads)
+    bias_softmax_backward_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<const T> dprobs,
+                                 const Rows4<T> dscores, const MaxSum* __restrict__ stats, float* __restrict__ partial) {
+    extern __shared__ float bias[];
+    __shared__ float part[2][16];
+    constexpr int kWarps = Cta<G>::kThreads / 32, kSlots = E / VEC;
+    const int span = padded(2 * f.distance) + 1;
+    float* diags = bias + span;
+    float* diag = diags + (threadIdx.x >> 5) * span;
+    const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y;
+    build_bias(f, ih, bias);
+    if (partial != nullptr)
+        for (int i = threadIdx.x; i < kWarps * span; i += blockDim.x) diags[i] = 0.f;
+    __syncthreads();
+    float left = 0.f, right = 0.f;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta;
+    for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
+        const int64_t iq = first + it + threadIdx.x / G;
+        if (G > 32 && first + it >= f.tq) break;
+        if (G == 32 && iq >= f.tq) break;
+        const RowRange r = row_range(f, ib, iq);
+        const T* in = scores.row(ib, ih, iq);
+        const T* up = dprobs.row(ib, ih, iq);
+        T* out = dscores.p != nullptr ? dscores.row(ib, ih, iq) : nullptr;
+        const int lead = row_lead<T, VEC>(in);
+        const MaxSum all = stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq];
+        const bool empty = all.s == 0.f;
+        const float norm = 1.f / all.s;
+        float dot = 0.f;
+        if constexpr (E > 0) {
+            float p[kSlots][VEC], dp[kSlots][VEC];
+#pragma unroll
+            for (int c = 0; c < kSlots; ++c) {
+                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) p[c][i] = dp[c][i] = 0.f;
+                if (j0 < r.end && !empty) {
+                    load_slot<T, VEC>(in, j0, f.tk, 0.f, p[c]);
+                    load_slot<T, VEC>(up, j0, r.end, 0.f, dp[c]);
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kSlots; ++c) {
+                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
+                if (j0 < r.end && !empty) {
+                    add_bias<VEC>(f, bias, r, j0, p[c]);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        p[c][i] = exp_below(p[c][i] - all.m) * norm;
+                        dot = fmaf(p[c][i], dp[c][i], dot);
+                    }
+                }
+            }
+            dot = group_sum<G>(dot, part, it);
+#pragma unroll
+            for (int c = 0; c < kSlots; ++c) {
+                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
+                if (j0 < f.tk) {
+                    float dz[VEC];
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) dz[i] = j0 + i >= 0 && j0 + i < r.end && !empty ? p[c][i] * (dp[c][i] - dot) : 0.f;
+                    if (partial != nullptr && j0 < r.end) add_diagonals<VEC>(f, diag, j0 - r.p, dz, left, right);
+                    if (out != nullptr) {
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) dz[i] *= f.scale;
+                        store_slot<T, VEC>(out, j0, f.tk, dz);
+                    }
+                }
+            }
+        } else {
+            for (int pass = 0; pass < 2; ++pass) {
+                for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < f.tk; j0 += G * VEC) {
+                    float p[VEC], dp[VEC];
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) p[i] = dp[i] = 0.f;
+                    if (j0 < r.end && !empty) {
+                        load_slot<T, VEC>(in, j0, f.tk, 0.f, p);
+                        load_slot<T, VEC>(up, j0, r.end, 0.f, dp);
+                        add_bias<VEC>(f, bias, r, j0, p);
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) p[i] = exp_below(p[i] - all.m) * norm;
+                    }
+                    if (pass == 0) {
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) dot = fmaf(p[i], dp[i], dot);
+                        continue;
+                    }
+                    float dz[VEC];
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) dz[i] = j0 + i >= 0 && j0 + i < r.end && !empty ? p[i] * (dp[i] - dot) : 0.f;
+                    if (partial != nullptr && j0 < r.end) add_diagonals<VEC>(f, diag, j0 - r.p, dz, left, right);
+                    if (out != nullptr) {
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) dz[i] *= f.scale;
+                        store_slot<T, VEC>(out, j0, f.tk, dz);
+                    }
+                }
+                if (pass == 0) dot = group_sum<G>(dot, part, it);
+            }
+        }
+        __syncwarp();  // the next row meets this row's diagonals through other lanes
+    }
+    if (partial == nullptr) return;
+    // the two ends of the warp's array take the far sums, then warps join diagonal by diagonal and diagonals by bucket
+    left = warp_sum(left);
+    right = warp_sum(right);
+    if ((threadIdx.x & 31) == 0) {
+        diag[padded(0)] = left;
+        diag[padded(2 * f.distance)] = right;
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d <= 2 * f.distance; d += blockDim.x) {
+        float s = diags[padded(d)];
+        for (int w = 1; w < kWarps; ++w) s += diags[w * span + padded(d)];
+        diags[padded(d)] = s;
+    }
+    __syncthreads();
+    float* mine = partial + ((static_cast<int64_t>(ih) * gridDim.z + ib) * gridDim.x + blockIdx.x) * f.buckets;
+    for (int c = threadIdx.x; c < f.buckets; c += blockDim.x) {
+        const int k = f.bidirectional && c >= f.nb ? c - f.nb : c;
+        const int lo = k < f.exact ? k : f.starts[k - f.exact];
+        const int hi = k < f.exact ? k + 1 : (k == f.nb - 1 ? f.distance + 1 : f.starts[k - f.exact + 1]);
+        float s = 0.f;
+        if (c != k) {
+            for (int n = max(lo, 1); n < hi; ++n) s += diags[padded(f.distance + n)];
+        } else {
+            for (int n = lo; n < hi; ++n) s += diags[padded(f.distance - n)];
+            if (!f.bidirectional && c == 0)
+                for (int n = 1; n <= f.distance; ++n) s += diags[padded(f.distance + n)];
+        }
+        mine[c] = s;
+    }
+}
+
+// dtable[c][head]: the parts of one head added by 32 lanes, then the lanes; one warp a value.
+__global__ void __launch_bounds__(256) bias_table_kernel(const float* __restrict__ partial, int64_t parts, int h, int buckets, float* __restrict__ dtable) {
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    if (id >= static_cast<int64_t>(h) * buckets) return;
+    const int head = static_cast<int>(id / buckets), c = static_cast<int>(id % buckets);
+    float s = 0.f;
+    for (int64_t i = threadIdx.x & 31; i < parts; i += 32) s += partial[(head * parts + i) * buckets + c];
+    s = warp_sum(s);
+    if ((threadIdx.x & 31) == 0) dtable[static_cast<int64_t>(c) * h + head] = s;
+}
+
+// ---- host side ----------------------------------------------------------------------------------
+
+// Boundaries of the logarithmic buckets: the smallest n >= e*(d/e)^(t/steps); a bound that is a whole number counts as
+// reached (it differs from the rounded power by far less than one part in 10^9).
+void fill_starts(BiasForm& f) {
+    const int steps = f.nb - f.exact;
+    f.starts[0] = static_cast<uint16_t>(f.exact);
+    for (int t = 1; t < steps; ++t) {
+        const double x = f.exact * pow(static_cast<double>(f.distance) / f.exact, static_cast<double>(t) / steps);
+        f.starts[t] = static_cast<uint16_t>(ceil(x * (1.0 - 1e-9)));
+    }
+}
+
+// Query rows a CTA of the backward kernel takes: enough of them that the CTA's last step (one value a bucket) is a small
+// part of its work, few enough that the grid fills the GPU.
+int backward_rows(int64_t b, int64_t h, int64_t tq) {
+    int rows = 64;
+    while (rows > 8 && b * h * ((tq + rows - 1) / rows) < 8 * kNumSMs) rows >>= 1;
+    return rows;
+}
+
+int check_form(int dtype, int64_t b, int64_t h, int64_t tq, int64_t tk, const float* table, int buckets, int max_distance,
+               int bidirectional, float scale) {
+    if (element_bytes(dtype) == 0 || b < 0 || h < 0 || tq < 0 || tk < 0) return BZ_ERR_INVALID_ARG;
+    if (table == nullptr || buckets < 2 || (bidirectional && (buckets < 4 || buckets % 2)) || !(scale == scale)) return BZ_ERR_INVALID_ARG;
+    const int nb = bidirectional ? buckets / 2 : buckets;
+    if (max_distance <= nb / 2) return BZ_ERR_INVALID_ARG;
+    if (buckets > 256 || max_distance > BZ_MAX_DISTANCE || b > 65535 || h > 65535 || tq >= (int64_t(1) << 31) || tk >= (int64_t(1) << 31))
+        return BZ_ERR_UNSUPPORTED;
+    return BZ_OK;
+}
+
+int check_tensor(const void* p, const int64_t* strides, int dtype) {
+    if (p == nullptr || strides == nullptr || reinterpret_cast<uintptr_t>(p) % element_bytes(dtype)) return BZ_ERR_INVALID_ARG;
+    return BZ_OK;
+}
+
+// Whether two tensors' rows all sit alike relative to 16-byte boundaries.
+bool alike(const void* p, const int64_t* sp, const void* q, const int64_t* sq, int64_t b, int64_t h, int64_t tq, int bytes) {
+    if ((reinterpret_cast<uintptr_t>(p) - reinterpret_cast<uintptr_t>(q)) & 15) return false;
+    const int64_t n[3] = {b, h, tq};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && ((sp[i] - sq[i]) * bytes) & 15) return false;
+    return true;
+}
+
+BiasForm make_form(int64_t h, int64_t tq, int64_t tk, const float* table, int buckets, int max_distance, int bidirectional, int causal,
+                   float scale, const int32_t* k_len, const int32_t* q_start) {
+    BiasForm f{};
+    f.table = table, f.k_len = k_len, f.q_start = q_start, f.scale = scale;
+    f.buckets = buckets, f.nb = bidirectional ? buckets / 2 : buckets, f.exact = f.nb / 2, f.distance = max_distance;
+    f.bidirectional = bidirectional != 0, f.causal = causal != 0, f.h = static_cast<int>(h), f.tq = tq, f.tk = tk;
+    fill_starts(f);
+    return f;
+}
+
+template <typename K> int allow_smem(K kern, size_t bytes) {
+    if (bytes <= 48 * 1024) return BZ_OK;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    return e == cudaSuccess ? BZ_OK : cuda_failed(e);
+}
+
+template <typename T> Rows4<T> rows4(T* p, const int64_t* s) { return {p, p ? s[0] : 0, p ? s[1] : 0, p ? s[2] : 0}; }
+
+template <typename T, int VEC, int G, int E>
+int launch_forward(BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<T>& out, MaxSum* stats, cudaStream_t s) {
+    f.rows_per_cta = Cta<G>::kRows * 8;
+    while (f.rows_per_cta > Cta<G>::kRows && b * f.h * ((f.tq + f.rows_per_cta - 1) / f.rows_per_cta) < 8 * kNumSMs) f.rows_per_cta /= 2;
+    const size_t smem = (2 * f.distance + 2 * f.distance / 8 + 1) * sizeof(float);
+    const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
+    bias_softmax_kernel<T, VEC, G, E><<<grid, Cta<G>::kThreads, smem, s>>>(f, in, out, stats);
+    note_launch();
+    return check_launch();
+}
+
+template <typename T, int VEC>
+int dispatch_forward(BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<T>& out, MaxSum* stats, cudaStream_t s) {
+    const int64_t n = f.tk + (VEC > 1 ? VEC - 1 : 0);  // the first slot may begin before the row
+    if (n <= 8 * 32) return launch_forward<T, VEC, 32, 8>(f, b, in, out, stats, s);
+    if (n <= 32 * 32) return launch_forward<T, VEC, 32, 32>(f, b, in, out, stats, s);
+    if (n <= 32 * 128) return launch_forward<T, VEC, 128, 32>(f, b, in, out, stats, s);
+    if (n <= 32 * 512) return launch_forward<T, VEC, 512, 32>(f, b, in, out, stats, s);
+    return launch_forward<T, VEC, 512, 0>(f, b, in, out, stats, s);
+}
+
+template <typename T, int VEC, int G, int E>
+int launch_backward(const BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out, const MaxSum* stats,
+                    float* partial, cudaStream_t s) {
+    const size_t span = 2 * f.distance + 2 * f.distance / 8 + 1;
+    const size_t smem = span * sizeof(float) * (1 + (partial != nullptr ? Cta<G>::kThreads / 32 : 0));
+    auto kern = bias_softmax_backward_kernel<T, VEC, G, E>;
+    const int st = allow_smem(kern, smem);
+    if (st != BZ_OK) return st;
+    const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
+    kern<<<grid, Cta<G>::kThreads, smem, s>>>(f, in, up, out, stats, partial);
+    note_launch();
+    return check_launch();
+}
+
+template <typename T, int VEC>
+int dispatch_backward(const BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out,
+                      const MaxSum* stats, float* partial, cudaStream_t s) {
+    const int64_t n = f.tk + (VEC > 1 ? VEC - 1 : 0);
+    if (n <= 8 * 32) return launch_backward<T, VEC, 32, 8>(f, b, in, up, out, stats, partial, s);
+    if (n <= 16 * 32) return launch_backward<T, VEC, 32, 16>(f, b, in, up, out, stats, partial, s);
+    if (n <= 16 * 128) return launch_backward<T, VEC, 128, 16>(f, b, in, up, out, stats, partial, s);
+    if (n <= 16 * 256) return launch_backward<T, VEC, 256, 16>(f, b, in, up, out, stats, partial, s);
+    return launch_backward<T, VEC, 256, 0>(f, b, in, up, out, stats, partial, s);
+}
+
+template <typename T>
+int forward(BiasForm& f, int64_t b, const void* scores, const int64_t* ss, void* probs, const int64_t* sp, MaxSum* stats, cudaStream_t s) {
+    const auto in = rows4(static_cast<const T*>(scores), ss);
+    const auto out = rows4(static_cast<T*>(probs), sp);
+    if (alike(scores, ss, probs, sp, b, f.h, f.tq, sizeof(T))) return dispatch_forward<T, Word<T>::kN>(f, b, in, out, stats, s);
+    return dispatch_forward<T, 1>(f, b, in, out, stats, s);
+}
+
+template <typename T>
+int backward(const BiasForm& f, int64_t b, const void* scores, const int64_t* ss, const void* dprobs, const int64_t* sd, void* dscores,
+             const int64_t* so, const MaxSum* stats, float* partial, cudaStream_t s) {
+    const auto in = rows4(static_cast<const T*>(scores), ss);
+    const auto up = rows4(static_cast<const T*>(dprobs), sd);
+    const auto out = rows4(static_cast<T*>(dscores), so);
+    if (alike(scores, ss, dprobs, sd, b, f.h, f.tq, sizeof(T)) && (dscores == nullptr || alike(scores, ss, dscores, so, b, f.h, f.tq, sizeof(T))))
+        return dispatch_backward<T, Word<T>::kN>(f, b, in, up, out, stats, partial, s);
+    return dispatch_backward<T, 1>(f, b, in, up, out, stats, partial, s);
+}
+
+}  // namespace
+
+}  // namespace bz
+
+using namespace bz;
+
+extern "C" size_t bz_bias_softmax_workspace_bytes(int64_t b, int64_t h, int64_t tq, int64_t tk, int buckets) {
+    if (b < 1 || h < 1 || tq < 1 || tk < 1 || buckets < 2 || buckets > 256 || b > 65535 || h > 65535 || tq >= (int64_t(1) << 31)) return 0;
+    const int rows = backward_rows(b, h, tq);
+    return round_up(static_cast<size_t>(b) * h * ((tq + rows - 1) / rows) * buckets * sizeof(float), 256);
+}
+
+extern "C" int bz_bias_softmax(const void* scores, const int64_t* strides_scores, int dtype, int64_t b, int64_t h, int64_t tq, int64_t tk,
+                               const float* table, int buckets, int max_distance, int bidirectional, int causal, float scale,
+                               const int32_t* k_len, const int32_t* q_start, void* probs, const int64_t* strides_probs, float* stats,
+                               void* stream) {
+    int st = check_form(dtype, b, h, tq, tk, table, buckets, max_distance, bidirectional, scale);
+    if (st != BZ_OK) return st;
+    if (b == 0 || h == 0 || tq == 0 || tk == 0) return BZ_OK;
+    if ((st = check_tensor(scores, strides_scores, dtype)) != BZ_OK || (st = check_tensor(probs, strides_probs, dtype)) != BZ_OK) return st;
+    if (!aligned8(stats)) return BZ_ERR_INVALID_ARG;
+    BiasForm f = make_form(h, tq, tk, table, buckets, max_distance, bidirectional, causal, scale, k_len, q_start);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (dtype == BZ_F32) return forward<float>(f, b, scores, strides_scores, probs, strides_probs, reinterpret_cast<MaxSum*>(stats), s);
+    if (dtype == BZ_F16) return forward<__half>(f, b, scores, strides_scores, probs, strides_probs, reinterpret_cast<MaxSum*>(stats), s);
+    return forward<__nv_bfloat16>(f, b, scores, strides_scores, probs, strides_probs, reinterpret_cast<MaxSum*>(stats), s);
+}
+
+extern "C" int bz_bias_softmax_backward(const void* scores, const int64_t* strides_scores, int dtype, int64_t b, int64_t h, int64_t tq,
+                                        int64_t tk, const float* table, int buckets, int max_distance, int bidirectional, int causal,
+                                        float scale, const int32_t* k_len, const int32_t* q_start, const float* stats, const void* dprobs,
+                                        const int64_t* strides_dprobs, void* dscores, const int64_t* strides_dscores, float* dtable,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+    int st = check_form(dtype, b, h, tq, tk, table, buckets, max_distance, bidirectional, scale);
+    if (st != BZ_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (dscores == nullptr && dtable == nullptr) return BZ_ERR_INVALID_ARG;
+    if (b == 0 || h == 0 || tq == 0 || tk == 0) {
+        if (dtable == nullptr || h == 0) return BZ_OK;
+        const cudaError_t e = cudaMemsetAsync(dtable, 0, sizeof(float) * buckets * h, s);
+        return e == cudaSuccess ? BZ_OK : cuda_failed(e);
+    }
+    if (stats == nullptr || !aligned8(stats)) return BZ_ERR_INVALID_ARG;
+    if ((st = check_tensor(scores, strides_scores, dtype)) != BZ_OK || (st = check_tensor(dprobs, strides_dprobs, dtype)) != BZ_OK) return st;
+    if (dscores != nullptr && (st = check_tensor(dscores, strides_dscores, dtype)) != BZ_OK) return st;
+    if (dtable != nullptr &&
+        (workspace == nullptr || !aligned256(workspace) || workspace_bytes < bz_bias_softmax_workspace_bytes(b, h, tq, tk, buckets)))
+        return BZ_ERR_WORKSPACE;
+    BiasForm f = make_form(h, tq, tk, table, buckets, max_distance, bidirectional, causal, scale, k_len, q_start);
+    f.rows_per_cta = backward_rows(b, h, tq);
+    float* partial = dtable != nullptr ? static_cast<float*>(workspace) : nullptr;
+    if (dtype == BZ_F32)
+        st = backward<float>(f, b, scores, strides_scores, dprobs, strides_dprobs, dscores, strides_dscores, reinterpret_cast<const MaxSum*>(stats), partial, s);
+    else if (dtype == BZ_F16)
+        st = backward<__half>(f, b, scores, strides_scores, dprobs, strides_dprobs, dscores, strides_dscores, reinterpret_cast<const MaxSum*>(stats), partial, s);
+    else
+        st = backward<__nv_bfloat16>(f, b, scores, strides_scores, dprobs, strides_dprobs, dscores, strides_dscores, reinterpret_cast<const MaxSum*>(stats), partial, s);
+    if (st != BZ_OK || dtable == nullptr) return st;
+    const int64_t parts = b * ((tq + f.rows_per_cta - 1) / f.rows_per_cta);
+    const int64_t values = h * buckets;
+    bias_table_kernel<<<static_cast<unsigned>((values + 7) / 8), 256, 0, s>>>(partial, parts, static_cast<int>(h), buckets, dtable);
+    note_launch();
+    return check_launch();
+}

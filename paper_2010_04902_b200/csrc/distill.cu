@@ -1,0 +1,368 @@
+// Distillation loss against a teacher's top logits, and its gradient.
+//
+// q = softmax(s/T) runs over the whole vocabulary, the teacher's p over t entries.  Loss and gradient need the same
+// maximum and sum of a row, so the fused call reads the row once, keeps its exponentials in registers (32 elements a
+// thread) and writes the gradient from there: two transfers a logit, bound by memory.  A row that one CTA cannot hold
+// is split over a cluster of up to eight; the CTAs exchange their (maximum, sum) pair through distributed shared
+// memory, one barrier a row.  Beyond that (more than 262 144 logits) the cluster reads the row twice.
+// The t entries: one warp forms p while the row's loads are in flight; after the dense part dlogits = dloss*T*q is
+// stored, the threads overwrite the named places, adding up entries that name the same one in their order.  No atomics:
+// the same inputs give the same bits.
+#include <cooperative_groups.h>
+
+#include "worker_common.cuh"
+
+namespace bz {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kHeld = 32;        // logits a thread keeps in registers
+constexpr int kMaxThreads = 1024;
+constexpr int kMaxCluster = 8;   // portable cluster size
+
+struct DistillArgs {
+    int64_t ld, v, ld_d;
+    const float* teacher;
+    const int32_t* index;
+    int t;
+    float temperature, scale;    // scale = 1 / T
+    const float* dloss;
+    float* loss;
+    MaxSum* stats;
+};
+
+struct Entries {  // dynamic shared memory: the teacher's entries of one row
+    float *p, *log_p, *s;  // probability, its logarithm, student logit / T
+    int* at;               // -1: not kept
+};
+__device__ __forceinline__ Entries entries(float* smem, int t) {
+    return {smem, smem + t, smem + 2 * t, reinterpret_cast<int*>(smem + 3 * t)};
+}
+
+// One warp: p of the row's kept entries; the student's logit at each that lies in [lo, hi).  Returns whether any is kept.
+template <typename T>
+__device__ __forceinline__ bool teacher_row(const DistillArgs& a, const T* row, int64_t i, const Entries& e, int64_t lo, int64_t hi) {
+    const int lane = threadIdx.x & 31;
+    float top = -INFINITY;
+    for (int k = lane; k < a.t; k += 32) {
+        const int at = a.index[i * a.t + k];
+        const float z = a.teacher[i * a.t + k] * a.scale;
+        const bool kept = at >= 0 && at < a.v && z != -INFINITY;
+        e.at[k] = kept ? at : -1;
+        e.log_p[k] = z;
+        e.s[k] = kept && at >= lo && at < hi ? to_f32(row[at]) * a.scale : 0.f;
+        if (kept) top = fmaxf(top, z);
+    }
+    top = finite_or_zero(warp_max(top));
+    float sum = 0.f;
+    bool any = false;
+    for (int k = lane; k < a.t; k += 32)
+        if (e.at[k] >= 0) {
+            any = true;
+            sum += exp_below(e.log_p[k] - top);
+        }
+    sum = warp_sum(sum);
+    any = __any_sync(~0u, any);
+    const float log_sum = logf(sum), norm = 1.f / sum;
+    for (int k = lane; k < a.t; k += 32) {
+        e.log_p[k] = e.log_p[k] - top;
+        e.p[k] = e.at[k] >= 0 ? exp_below(e.log_p[k]) * norm : 0.f;
+        e.log_p[k] -= log_sum;
+    }
+    __syncwarp();
+    return any;
+}
+
+// One warp: the loss of the row from its maximum and sum.
+__device__ __forceinline__ float row_loss(const DistillArgs& a, const Entries& e, const MaxSum& all) {
+    const float top = finite_or_zero(all.m), log_sum = logf(all.s);
+    float sum = 0.f;
+    for (int k = threadIdx.x & 31; k < a.t; k += 32) {
+        const float p = e.p[k];
+        if (p != 0.f) {  // an entry without weight adds nothing, whatever its q
+            const float log_q = e.s[k] == -INFINITY ? -INFINITY : e.s[k] - top - log_sum;
+            sum += p * (e.log_p[k] - log_q);
+        }
+    }
+    return warp_sum(sum) * (a.temperature * a.temperature);
+}
+
+// All threads: the places of [lo, hi) that the teacher names.
+template <typename T>
+__device__ __forceinline__ void write_entries(const DistillArgs& a, const Entries& e, const MaxSum& all, float g, int64_t lo, int64_t hi, T* out) {
+    for (int k = threadIdx.x; k < a.t; k += blockDim.x) {
+        const int at = e.at[k];
+        if (at < 0 || at < lo || at >= hi) continue;   // lo may lie before the row (its first slot's lead)
+        float p = 0.f;
+        for (int o = 0; o < a.t; ++o) p += e.at[o] == at ? e.p[o] : 0.f;
+        const float q = e.s[k] == -INFINITY ? 0.f : exp_below(e.s[k] - all.m) / all.s;
+        out[at] = from_f32<T>(g * (q - p));
+    }
+}
+
+// Joins one pair per thread over the CTA.
+__device__ __forceinline__ MaxSum cta_join(MaxSum v, MaxSum* part) {
+    v = warp_join(v);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    return warp_join(lane < (blockDim.x >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f});
+}
+
+// One cluster a row.  HELD: the row's exponentials stay in registers; otherwise the row is read twice.
+template <typename T, int VEC, bool HELD>
+__global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_constant__ DistillArgs a, const T* logits, T* dlogits) {
+    extern __shared__ float smem[];
+    __shared__ MaxSum part[32], peers[kMaxCluster];
+    __shared__ int s_any;
+    constexpr int kSlots = kHeld / VEC;
+    const Entries e = entries(smem, a.t);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = cluster.block_rank(), ranks = cluster.num_blocks();
+    const int64_t i = blockIdx.x / ranks;
+    const T* row = logits + i * a.ld;
+    const int lead = row_lead<T, VEC>(row);
+    const int64_t per_cta = static_cast<int64_t>(blockDim.x) * kHeld;          // HELD: elements of one CTA's share
+    const int64_t base = (HELD ? rank * per_cta : static_cast<int64_t>(rank) * blockDim.x * VEC) - lead;
+    const int64_t step = static_cast<int64_t>(blockDim.x) * VEC * (HELD ? 1 : ranks);
+    if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // every CTA of the cluster has started
+    float x[HELD ? kSlots : 1][VEC];
+    MaxSum mine{-INFINITY, 0.f};
+    if constexpr (HELD) {
+#pragma unroll
+        for (int c = 0; c < kSlots; ++c) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) x[c][k] = -INFINITY;
+            const int64_t j0 = base + c * step + static_cast<int64_t>(threadIdx.x) * VEC;
+            if (j0 < a.v) load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[c]);
+        }
+    }
+    if (threadIdx.x < 32) {
+        const bool any = teacher_row(a, row, i, e, 0, a.v);
+        if (threadIdx.x == 0) s_any = any;
+    }
+    if constexpr (HELD) {
+#pragma unroll
+        for (int c = 0; c < kSlots; ++c)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                x[c][k] *= a.scale;
+                mine.m = fmaxf(mine.m, x[c][k]);
+            }
+        const float own = finite_or_zero(mine.m);
+#pragma unroll
+        for (int c = 0; c < kSlots; ++c)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                x[c][k] = exp_below(x[c][k] - own);
+                mine.s += x[c][k];
+            }
+    } else {
+        for (int64_t j0 = base + static_cast<int64_t>(threadIdx.x) * VEC; j0 < a.v; j0 += step) {
+            load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[0]);
+            MaxSum w{-INFINITY, 0.f};
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                x[0][k] *= a.scale;
+                w.m = fmaxf(w.m, x[0][k]);
+            }
+            const float own = finite_or_zero(w.m);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) w.s += exp_below(x[0][k] - own);
+            mine = join(mine, w);
+        }
+    }
+    MaxSum all = cta_join(mine, part);
+    if (ranks > 1) {
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (threadIdx.x < ranks) *cluster.map_shared_rank(&peers[rank], threadIdx.x) = all;
+        cluster.sync();
+        all = peers[0];
+        for (int c = 1; c < ranks; ++c) all = join(all, peers[c]);
+    }
+    const bool any = s_any != 0;
+    if (rank == 0 && threadIdx.x < 32) {
+        const float loss = row_loss(a, e, all);
+        if (threadIdx.x == 0) {
+            if (a.loss != nullptr) a.loss[i] = any ? loss : 0.f;
+            if (a.stats != nullptr) a.stats[i] = all;
+        }
+    }
+    if (dlogits == nullptr) return;
+    T* out = dlogits + i * a.ld_d;
+    const float g = any ? (a.dloss != nullptr ? a.dloss[i] : 1.f) * a.temperature : 0.f;
+    const float top = finite_or_zero(all.m);
+    const float factor = all.s == 0.f || !any ? 0.f : g * (HELD ? exp_below(mine.m - top) : 1.f) / all.s;
+    if constexpr (HELD) {
+#pragma unroll
+        for (int c = 0; c < kSlots; ++c) {
+            const int64_t j0 = base + c * step + static_cast<int64_t>(threadIdx.x) * VEC;
+            if (j0 < a.v) {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) x[c][k] = any ? x[c][k] * factor : 0.f;
+                store_slot<T, VEC>(out, j0, a.v, x[c]);
+            }
+        }
+        __syncthreads();
+        if (any) write_entries(a, e, all, g, base, base + per_cta, out);
+    } else {
+        for (int64_t j0 = base + static_cast<int64_t>(threadIdx.x) * VEC; j0 < a.v; j0 += step) {
+            load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[0]);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) x[0][k] = any ? exp_below(x[0][k] * a.scale - top) * factor : 0.f;
+            store_slot<T, VEC>(out, j0, a.v, x[0]);
+        }
+        // the cluster's CTAs share the row slot by slot: the named places wait for all of them
+        if (ranks > 1)
+            cluster.sync();
+        else
+            __syncthreads();
+        if (any && rank == 0) write_entries(a, e, all, g, 0, a.v, out);
+    }
+}
+
+// The gradient from a given maximum and sum: CTA (x, y) takes share x of row y's columns.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) distill_backward_kernel(const __grid_constant__ DistillArgs a, const T* logits, T* dlogits, int shares) {
+    extern __shared__ float smem[];
+    __shared__ int s_any;
+    constexpr int kSlots = kHeld / VEC;
+    const Entries e = entries(smem, a.t);
+    const int64_t i = blockIdx.x / shares, share = blockIdx.x % shares;
+    const T* row = logits + i * a.ld;
+    T* out = dlogits + i * a.ld_d;
+    const int64_t base = share * (256 * kHeld) - row_lead<T, VEC>(row);
+    float x[kSlots][VEC];
+#pragma unroll
+    for (int c = 0; c < kSlots; ++c) {
+        const int64_t j0 = base + (c * 256 + static_cast<int64_t>(threadIdx.x)) * VEC;
+        if (j0 < a.v) load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[c]);
+    }
+    if (threadIdx.x < 32) {
+        const bool any = teacher_row(a, row, i, e, base, base + 256 * kHeld);
+        if (threadIdx.x == 0) s_any = any;
+    }
+    __syncthreads();
+    const bool any = s_any != 0;
+    const MaxSum all = a.stats[i];
+    const float g = any ? (a.dloss != nullptr ? a.dloss[i] : 1.f) * a.temperature : 0.f;
+    const float factor = all.s == 0.f ? 0.f : g / all.s, top = finite_or_zero(all.m);
+#pragma unroll
+    for (int c = 0; c < kSlots; ++c) {
+        const int64_t j0 = base + (c * 256 + static_cast<int64_t>(threadIdx.x)) * VEC;
+        if (j0 < a.v) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) x[c][k] = any ? exp_below(x[c][k] * a.scale - top) * factor : 0.f;
+            store_slot<T, VEC>(out, j0, a.v, x[c]);
+        }
+    }
+    __syncthreads();
+    if (any) write_entries(a, e, all, g, base, base + 256 * kHeld, out);
+}
+
+// v == 0: no logits at all.
+__global__ void distill_empty_kernel(int64_t m, float* loss, MaxSum* stats) {
+    for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < m; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        if (loss != nullptr) loss[i] = 0.f;
+        if (stats != nullptr) stats[i] = {-INFINITY, 0.f};
+    }
+}
+
+// ---- host side ----------------------------------------------------------------------------------
+
+template <typename T, int VEC> int launch(const DistillArgs& a, int64_t m, const T* logits, T* dlogits, cudaStream_t s) {
+    const int64_t slots = (a.v + (VEC > 1 ? VEC - 1 : 0) + VEC - 1) / VEC, per_thread = kHeld / VEC;
+    int ranks = 1;
+    while (ranks < kMaxCluster && (slots + ranks * per_thread - 1) / (ranks * per_thread) > kMaxThreads) ranks *= 2;
+    int64_t threads = ((slots + ranks * per_thread - 1) / (ranks * per_thread) + 31) / 32 * 32;
+    const bool held = threads <= kMaxThreads;
+    if (!held) threads = kMaxThreads;
+    if (m * ranks >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(m * ranks));
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = static_cast<size_t>(a.t) * 16;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {static_cast<unsigned>(ranks), 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = held ? cudaLaunchKernelEx(&cfg, distill_kernel<T, VEC, true>, a, logits, dlogits)
+                               : cudaLaunchKernelEx(&cfg, distill_kernel<T, VEC, false>, a, logits, dlogits);
+    if (e != cudaSuccess) return cuda_failed(e);
+    note_launch();
+    return check_launch();
+}
+
+template <typename T, int VEC> int launch_backward(const DistillArgs& a, int64_t m, const T* logits, T* dlogits, cudaStream_t s) {
+    const int64_t shares = (a.v + (VEC > 1 ? VEC - 1 : 0) + 256 * kHeld - 1) / (256 * kHeld);
+    if (m * shares >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
+    distill_backward_kernel<T, VEC><<<static_cast<unsigned>(m * shares), 256, static_cast<size_t>(a.t) * 16, s>>>(
+        a, logits, dlogits, static_cast<int>(shares));
+    note_launch();
+    return check_launch();
+}
+
+template <typename T> int dispatch(const DistillArgs& a, int64_t m, const void* logits, void* dlogits, bool backward, cudaStream_t s) {
+    const T* in = static_cast<const T*>(logits);
+    T* out = static_cast<T*>(dlogits);
+    const uintptr_t apart = reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(dlogits);
+    const bool alike = out == nullptr || ((apart & 15) == 0 && (m == 1 || ((a.ld - a.ld_d) * static_cast<int64_t>(sizeof(T))) % 16 == 0));
+    if (backward)
+        return alike ? launch_backward<T, Word<T>::kN>(a, m, in, out, s) : launch_backward<T, 1>(a, m, in, out, s);
+    return alike ? launch<T, Word<T>::kN>(a, m, in, out, s) : launch<T, 1>(a, m, in, out, s);
+}
+
+int check(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const float* teacher, const int32_t* index, int t,
+          float temperature, const void* dlogits, int64_t ld_d) {
+    const int bytes = element_bytes(dtype);
+    if (bytes == 0 || m < 0 || v < 0 || t < 1 || !(temperature > 0.f) || temperature > 3.4e38f) return BZ_ERR_INVALID_ARG;
+    if (v >= (int64_t(1) << 31) || t > BZ_MAX_TOP) return BZ_ERR_UNSUPPORTED;
+    if (m == 0) return BZ_OK;
+    if (teacher == nullptr || index == nullptr) return BZ_ERR_INVALID_ARG;
+    if (v == 0) return BZ_OK;
+    if (logits == nullptr || (m > 1 && ld < v) || reinterpret_cast<uintptr_t>(logits) % bytes) return BZ_ERR_INVALID_ARG;
+    if (dlogits != nullptr && ((m > 1 && ld_d < v) || reinterpret_cast<uintptr_t>(dlogits) % bytes)) return BZ_ERR_INVALID_ARG;
+    return BZ_OK;
+}
+
+}  // namespace
+
+}  // namespace bz
+
+using namespace bz;
+
+extern "C" int bz_distill(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const float* teacher, const int32_t* index,
+                          int t, float temperature, const float* dloss, float* loss, float* stats, void* dlogits, int64_t ld_d, void* stream) {
+    const int st = check(logits, ld, dtype, m, v, teacher, index, t, temperature, dlogits, ld_d);
+    if (st != BZ_OK) return st;
+    if (m == 0) return BZ_OK;
+    if ((loss == nullptr && stats == nullptr && dlogits == nullptr) || !aligned8(stats)) return BZ_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (v == 0) {
+        distill_empty_kernel<<<kNumSMs, 256, 0, s>>>(m, loss, reinterpret_cast<MaxSum*>(stats));
+        note_launch();
+        return check_launch();
+    }
+    const DistillArgs a{ld, v, ld_d, teacher, index, t, temperature, 1.f / temperature, dloss, loss, reinterpret_cast<MaxSum*>(stats)};
+    if (dtype == BZ_F32) return dispatch<float>(a, m, logits, dlogits, false, s);
+    if (dtype == BZ_F16) return dispatch<__half>(a, m, logits, dlogits, false, s);
+    return dispatch<__nv_bfloat16>(a, m, logits, dlogits, false, s);
+}
+
+extern "C" int bz_distill_backward(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const float* teacher,
+                                   const int32_t* index, int t, float temperature, const float* stats, const float* dloss, void* dlogits,
+                                   int64_t ld_d, void* stream) {
+    const int st = check(logits, ld, dtype, m, v, teacher, index, t, temperature, dlogits, ld_d);
+    if (st != BZ_OK) return st;
+    if (m == 0 || v == 0) return BZ_OK;
+    if (stats == nullptr || !aligned8(stats) || dlogits == nullptr) return BZ_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const DistillArgs a{ld, v, ld_d, teacher, index, t, temperature, 1.f / temperature, dloss, nullptr, reinterpret_cast<MaxSum*>(const_cast<float*>(stats))};
+    if (dtype == BZ_F32) return dispatch<float>(a, m, logits, dlogits, true, s);
+    if (dtype == BZ_F16) return dispatch<__half>(a, m, logits, dlogits, true, s);
+    return dispatch<__nv_bfloat16>(a, m, logits, dlogits, true, s);
+}

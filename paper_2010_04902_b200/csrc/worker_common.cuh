@@ -1,0 +1,130 @@
+// Element types and row access shared by the operators of a worker's step (glu, bias_softmax, distill).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "bz_common.cuh"
+
+namespace bz {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+inline int element_bytes(int dtype) { return dtype == BZ_F32 ? 4 : (dtype == BZ_F16 || dtype == BZ_BF16 ? 2 : 0); }
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// Elements of one 16-byte word as binary32, and back.
+template <typename T> struct Word;
+template <> struct Word<float> {
+    static constexpr int kN = 4;
+    __device__ static __forceinline__ void unpack(const uint4& w, float* x) {
+        x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y), x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
+    }
+    __device__ static __forceinline__ uint4 pack(const float* x) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+};
+__device__ __forceinline__ float2 unpack2(__nv_bfloat16, uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ float2 unpack2(__half, uint32_t w) {
+    __half2 h;
+    memcpy(&h, &w, 4);
+    return __half22float2(h);
+}
+__device__ __forceinline__ uint32_t pack2(__nv_bfloat16, float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    uint32_t w;
+    memcpy(&w, &h, 4);
+    return w;
+}
+__device__ __forceinline__ uint32_t pack2(__half, float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    uint32_t w;
+    memcpy(&w, &h, 4);
+    return w;
+}
+template <typename T> struct Word16 {
+    static constexpr int kN = 8;
+    __device__ static __forceinline__ void unpack(const uint4& w, float* x) {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2(T(), u[i]);
+            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        }
+    }
+    __device__ static __forceinline__ uint4 pack(const float* x) {
+        return make_uint4(pack2(T(), x[0], x[1]), pack2(T(), x[2], x[3]), pack2(T(), x[4], x[5]), pack2(T(), x[6], x[7]));
+    }
+};
+template <> struct Word<__half> : Word16<__half> {};
+template <> struct Word<__nv_bfloat16> : Word16<__nv_bfloat16> {};
+
+// A row of `n` elements cut into slots of VEC.  VEC = the elements of a 16-byte word: slots lie on 16-byte boundaries,
+// so the first one begins `lead` elements before the row; slots that reach over an end are read and written element by
+// element.  VEC = 1: a slot is an element, for tensors whose rows do not sit alike relative to 16-byte boundaries.
+template <typename T, int VEC> __device__ __forceinline__ int row_lead(const T* row) {
+    return VEC == 1 ? 0 : static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
+}
+// x[i] = element j0 + i of the row where that lies in [0, n); the others keep `fill`.
+template <typename T, int VEC> __device__ __forceinline__ void load_slot(const T* row, int64_t j0, int64_t n, float fill, float (&x)[VEC]) {
+    if constexpr (VEC == 1) {
+        x[0] = j0 < n ? to_f32(row[j0]) : fill;
+    } else if (j0 >= 0 && j0 + VEC <= n) {
+        Word<T>::unpack(*reinterpret_cast<const uint4*>(row + j0), x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) x[i] = j0 + i >= 0 && j0 + i < n ? to_f32(row[j0 + i]) : fill;
+    }
+}
+template <typename T, int VEC> __device__ __forceinline__ void store_slot(T* row, int64_t j0, int64_t n, const float (&x)[VEC]) {
+    if constexpr (VEC == 1) {
+        if (j0 < n) row[j0] = from_f32<T>(x[0]);
+    } else if (j0 >= 0 && j0 + VEC <= n) {
+        *reinterpret_cast<uint4*>(row + j0) = Word<T>::pack(x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (j0 + i >= 0 && j0 + i < n) row[j0 + i] = from_f32<T>(x[i]);
+    }
+}
+
+// e^x for x = z - maximum <= 0.  The difference is taken before the factor log2(e), so that a row of the type's lowest
+// values neither overflows nor loses its differences.
+__device__ __forceinline__ float exp_below(float x) { return exp2f(x * kLog2e); }
+
+// (maximum, sum of e^(z - maximum)) of a part of a row.  An empty part has maximum -inf and sum 0.
+struct MaxSum {
+    float m, s;
+};
+__device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ MaxSum join(const MaxSum& a, const MaxSum& b) {
+    const float m = fmaxf(a.m, b.m), r = finite_or_zero(m);
+    return {m, a.s * exp_below(a.m - r) + b.s * exp_below(b.m - r)};
+}
+__device__ __forceinline__ MaxSum warp_join(MaxSum v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const MaxSum w{__shfl_xor_sync(~0u, v.m, o), __shfl_xor_sync(~0u, v.s, o)};
+        v = (threadIdx.x & o) ? join(w, v) : join(v, w);   // both lanes of a pair add in the same order
+    }
+    return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
+    return v;
+}
+
+}  // namespace bz

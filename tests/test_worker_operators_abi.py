@@ -1,0 +1,118 @@
+"""Refusals of the worker's operators: every call here returns from the host's checks, before anything is launched."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2010_04902_b200 import binding as bz
+from paper_2010_04902_b200 import build as bz_build
+
+BIG = 1 << 40
+F = ctypes.c_void_p(256)      # never dereferenced
+ODD = ctypes.c_void_p(257)
+S = (ctypes.c_int64 * 3)(80, 40, 10)
+
+
+@pytest.fixture(scope="module")
+def L():
+    bz_build.build()
+    return bz.lib()
+
+
+def test_glu(L):
+    def call(x=F, ld_x=8, wg=F, wu=F, ld_w=8, m=4, n=6, k=8, dtype=bz.BF16, act=0, h=F, ld_h=6, preact=None, ws=None, size=0):
+        return L.bz_glu(x, ld_x, wg, wu, ld_w, m, n, k, dtype, act, h, ld_h, preact, ws, size, None)
+
+    n0 = bz.kernel_launch_count()
+    for bad in (dict(x=None), dict(wg=None), dict(wu=None), dict(h=None), dict(ld_x=7), dict(ld_w=7), dict(ld_h=5), dict(m=-1), dict(n=-1),
+                dict(k=-1), dict(dtype=3), dict(dtype=-1), dict(act=4), dict(act=-1), dict(x=ODD), dict(wu=ODD), dict(h=ODD),
+                dict(preact=ctypes.c_void_p(264))):
+        assert call(**bad) == bz.ERR_INVALID_ARG, bad
+    for bad in (dict(dtype=bz.F32), dict(m=BIG), dict(n=BIG, ld_h=BIG), dict(k=BIG, ld_x=BIG, ld_w=BIG)):
+        assert call(**bad) == bz.ERR_UNSUPPORTED, bad
+    need = L.bz_glu_workspace_bytes(4, 6, 9, bz.BF16, 0)
+    for ws, size in ((None, BIG), (F, need - 1), (ctypes.c_void_p(264), BIG)):      # operands that have to be laid out first
+        assert call(k=9, ld_x=9, ld_w=9, ws=ws, size=size) == bz.ERR_WORKSPACE
+    assert call(m=0) == bz.OK and call(n=0, wg=None, wu=None) == bz.OK
+    assert bz.kernel_launch_count() == n0
+
+
+def test_glu_backward(L):
+    def call(x=F, ld_x=8, wg=F, wu=F, ld_w=8, preact=F, dh=F, ld_dh=6, m=4, n=6, k=8, dtype=bz.F16, act=0, dx=F, ld_dx=8, dwg=F, dwu=F, ld_dw=8,
+             grad=bz.F16, ws=F, size=BIG):
+        return L.bz_glu_backward(x, ld_x, wg, wu, ld_w, preact, dh, ld_dh, m, n, k, dtype, act, dx, ld_dx, dwg, dwu, ld_dw, grad, ws, size, None)
+
+    n0 = bz.kernel_launch_count()
+    for bad in (dict(x=None), dict(wg=None), dict(wu=None), dict(preact=None), dict(dh=None), dict(dwg=None), dict(dwu=None), dict(ld_dh=5),
+                dict(ld_dx=7), dict(ld_dw=7), dict(ld_x=7), dict(ld_w=7), dict(grad=bz.BF16), dict(grad=9), dict(act=7), dict(m=-1),
+                dict(dh=ODD), dict(dx=ODD), dict(dwg=ODD), dict(dx=None, dwg=None, dwu=None), dict(preact=ctypes.c_void_p(264)),
+                dict(grad=bz.F32, dwg=ctypes.c_void_p(258))):
+        assert call(**bad) == bz.ERR_INVALID_ARG, bad
+    assert call(dtype=bz.F32, grad=bz.F32) == bz.ERR_UNSUPPORTED and call(m=BIG) == bz.ERR_UNSUPPORTED
+    need = L.bz_glu_workspace_bytes(4, 6, 8, bz.F16, 1)
+    for ws, size in ((None, BIG), (F, need - 1), (ctypes.c_void_p(264), BIG)):
+        assert call(ws=ws, size=size) == bz.ERR_WORKSPACE
+    assert call(m=0, n=0) == bz.OK and call(k=0) == bz.OK
+    assert bz.kernel_launch_count() == n0
+    assert need > 0 and need % 256 == 0
+    for args in ((-1, 6, 8, bz.F16, 1), (4, -1, 8, bz.F16, 1), (4, 6, -1, bz.F16, 1), (4, 6, 8, bz.F32, 1), (4, 6, 8, 5, 1)):
+        assert L.bz_glu_workspace_bytes(*args) == 0
+
+
+def test_bias_softmax(L):
+    def both(scores=F, ss=S, dtype=bz.F16, b=1, h=2, tq=4, tk=10, table=F, buckets=32, distance=128, bi=1, causal=0, scale=1.0, probs=F, sp=S,
+             stats=F, dprobs=F, sd=S, ds=F, so=S, dt=F, ws=F, size=BIG):
+        head = (scores, ss, dtype, b, h, tq, tk, table, buckets, distance, bi, causal, scale, None, None)
+        return (L.bz_bias_softmax(*head, probs, sp, stats, None),
+                L.bz_bias_softmax_backward(*head, stats, dprobs, sd, ds, so, dt, ws, size, None))
+
+    n0 = bz.kernel_launch_count()
+    for bad in (dict(scores=None), dict(ss=None), dict(dtype=7), dict(b=-1), dict(h=-1), dict(tq=-1), dict(tk=-1), dict(table=None),
+                dict(buckets=1), dict(buckets=33), dict(buckets=2), dict(distance=8), dict(scale=float("nan")), dict(scores=ODD),
+                dict(stats=ctypes.c_void_p(260))):
+        assert both(**bad) == (bz.ERR_INVALID_ARG, bz.ERR_INVALID_ARG), bad
+    for bad in (dict(buckets=258), dict(distance=2049), dict(b=65536), dict(h=65536), dict(tq=1 << 31), dict(tk=1 << 31)):
+        assert both(**bad) == (bz.ERR_UNSUPPORTED, bz.ERR_UNSUPPORTED), bad
+    for bad in (dict(probs=None, stats=None), dict(sp=None, dprobs=None), dict(probs=ODD, sd=None), dict(probs=None, ds=None, dt=None),
+                dict(probs=None, so=None), dict(probs=None, ds=ODD)):
+        assert both(**bad) == (bz.ERR_INVALID_ARG, bz.ERR_INVALID_ARG), bad
+    for bad in (dict(ws=None), dict(ws=ctypes.c_void_p(264)), dict(size=8)):
+        assert both(probs=None, **bad)[1] == bz.ERR_WORKSPACE
+    for none in (dict(b=0), dict(h=0), dict(tq=0), dict(tk=0)):
+        assert both(dt=None, **none) == (bz.OK, bz.OK)
+    assert bz.kernel_launch_count() == n0
+    assert L.bz_bias_softmax_workspace_bytes(2, 3, 100, 100, 32) >= 2 * 3 * 32 * 4
+    assert L.bz_bias_softmax_workspace_bytes(0, 3, 100, 100, 32) == 0 and L.bz_bias_softmax_workspace_bytes(2, 3, 100, 100, 1000) == 0
+
+
+def test_distill(L):
+    def both(logits=F, ld=10, dtype=bz.F16, m=4, v=10, teacher=F, index=F, t=3, T=1.0, dloss=None, loss=F, stats=F, d=F, ld_d=10):
+        return (L.bz_distill(logits, ld, dtype, m, v, teacher, index, t, T, dloss, loss, stats, d, ld_d, None),
+                L.bz_distill_backward(logits, ld, dtype, m, v, teacher, index, t, T, stats, dloss, d, ld_d, None))
+
+    n0 = bz.kernel_launch_count()
+    for bad in (dict(logits=None), dict(ld=9), dict(dtype=3), dict(m=-1), dict(v=-1), dict(teacher=None), dict(index=None), dict(t=0), dict(T=0.0),
+                dict(T=-1.0), dict(T=float("inf")), dict(T=float("nan")), dict(ld_d=9), dict(logits=ODD), dict(d=ODD),
+                dict(stats=ctypes.c_void_p(260)), dict(loss=None, stats=None, d=None)):
+        assert both(**bad) == (bz.ERR_INVALID_ARG, bz.ERR_INVALID_ARG), bad
+    assert L.bz_distill_backward(F, 10, bz.F16, 4, 10, F, F, 3, 1.0, None, None, F, 10, None) == bz.ERR_INVALID_ARG      # no stats
+    for bad in (dict(v=1 << 31, ld=1 << 31, ld_d=1 << 31), dict(t=1025)):
+        assert both(**bad) == (bz.ERR_UNSUPPORTED, bz.ERR_UNSUPPORTED), bad
+    assert both(m=0, teacher=None, index=None, loss=None, stats=None, d=None) == (bz.OK, bz.OK)
+    assert bz.kernel_launch_count() == n0
+
+
+def test_python_side():
+    x = torch.zeros(4, 8)
+    with pytest.raises(TypeError):
+        bz.glu(x.half(), x.half(), x.half())                      # not on the GPU
+    with pytest.raises(ValueError):
+        bz.glu(x, torch.zeros(3, 7), torch.zeros(3, 7))
+    with pytest.raises(ValueError):
+        bz.glu(x.expand(2, 4, 8), x, x)
+    with pytest.raises(ValueError):
+        bz.glu(torch.zeros(1, 8).expand(4, 8), x, x)              # rows that repeat have no leading dimension
+    with pytest.raises(ValueError):
+        bz.bias_softmax(torch.zeros(2, 3, 4), torch.zeros(32, 3))
+    with pytest.raises(TypeError):
+        bz.distill(torch.zeros(3, 9), torch.zeros(3, 2), torch.zeros(3, 2, dtype=torch.int32))
