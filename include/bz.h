@@ -14,7 +14,7 @@
  *     are ordinary process memory.  The caller owns every buffer.  The library never allocates
  *     or frees device memory; scratch space is a caller-provided device workspace whose size
  *     bz_workspace_bytes() reports.  Device state that outlives a call is limited to what is part
- *     of the library image: four counters of expired waits (bz_pipeline_timeouts), the switch of
+ *     of the library image: five counters of expired waits (bz_pipeline_timeouts), the switch of
  *     bz_debug_stall_pipeline and the built-in array of bz_pairdist_static.  None of it
  *     influences a result.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream).  Calls with
@@ -522,7 +522,7 @@ uint64_t bz_kernel_launch_count(void);
  *   workspace  device, bz_glu_workspace_bytes(m, n, k, dtype, 0) bytes, 256-byte aligned; the bytes are 0
  *           and NULL will do where x and the weights are 16-byte aligned with leading dimensions that are
  *           multiples of 8 (other operands are laid out there first).
- * m, n, k up to 2^31 - 1 each.  The tensor-core kernels bound every wait; one that runs out stops the
+ * m, n, k up to 2^31 - 512 each.  The tensor-core kernels bound every wait; one that runs out stops the
  * kernel early with incomplete outputs and counts in bz_pipeline_timeouts().
  */
 int bz_glu(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w, int64_t m, int64_t n, int64_t k,

@@ -1,158 +1,251 @@
-// Gated feed-forward block and its gradient.
-#include "worker_common.cuh"
+// Gated feed-forward block and its gradient: host side, the pass between the products, and operands laid out on the way in.
+#include "glu_product.cuh"
 
 namespace bz {
 
 namespace {
 
-template <int ACT> __device__ __forceinline__ float act(float g) {
-    if constexpr (ACT == BZ_ACT_SILU) return g / (1.f + __expf(-g));
-    if constexpr (ACT == BZ_ACT_GELU_TANH) return g / (1.f + __expf(-1.5957691216f * (g + 0.044715f * g * g * g)));
-    if constexpr (ACT == BZ_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678f));
-    return fmaxf(g, 0.f);
-}
-template <int ACT> __device__ __forceinline__ float act_slope(float g) {
-    if constexpr (ACT == BZ_ACT_SILU) {
-        const float s = 1.f / (1.f + __expf(-g));
-        return s * (1.f + g * (1.f - s));
-    }
-    if constexpr (ACT == BZ_ACT_GELU_TANH) {  // (1 + tanh y)/2 = 1/(1 + exp(-2y))
-        const float s = 1.f / (1.f + __expf(-1.5957691216f * (g + 0.044715f * g * g * g)));
-        return s + g * s * (1.f - s) * 1.5957691216f * (1.f + 0.134145f * g * g);
-    }
-    if constexpr (ACT == BZ_ACT_GELU) return 0.5f * (1.f + erff(g * 0.70710678f)) + g * 0.39894228f * __expf(-0.5f * g * g);
-    return g > 0.f ? 1.f : 0.f;
-}
+__device__ unsigned int g_timeouts = 0;
 
-// acc[r][c] = sum over l of A(i0 + 4 ty + r, l) * B(j0 + 4 tx + c, l), A(i, l) = a[i*ai + l*al] for i < ni, l < nl.
-template <typename T>
-__device__ __forceinline__ void tile_product(const T* a, int64_t ai, int64_t al, const T* b, int64_t bj, int64_t bl, int64_t i0, int64_t ni,
-                                             int64_t j0, int64_t nj, int64_t nl, float (&acc)[4][4], float (*sa)[65], float (*sb)[65]) {
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    for (int64_t l0 = 0; l0 < nl; l0 += 16) {
-        for (int e = threadIdx.x; e < 1024; e += 256) {
-            const int l = al == 1 ? e % 16 : e / 64, i = al == 1 ? e / 16 : e % 64;
-            sa[l][i] = i0 + i < ni && l0 + l < nl ? to_f32(a[(i0 + i) * ai + (l0 + l) * al]) : 0.f;
-            const int l2 = bl == 1 ? e % 16 : e / 64, j = bl == 1 ? e / 16 : e % 64;
-            sb[l2][j] = j0 + j < nj && l0 + l2 < nl ? to_f32(b[(j0 + j) * bj + (l0 + l2) * bl]) : 0.f;
+constexpr int kClusters = kNumSMs / 2;
+constexpr size_t kPartialBytes = static_cast<size_t>(kClusters) * kRowTile * 256 * sizeof(float);  // one tile a cluster
+
+// dgu[0] = dh * u * act'(g), dgu[1] = dh * act(g), each [m][ld], rounded to the operands' type.  14 bytes a hidden unit
+// (8 of them preact): bound by memory.  V columns a thread.
+template <typename T, int ACT, int V>
+__global__ void __launch_bounds__(256) glu_dgu_kernel(const float* __restrict__ preact, const T* __restrict__ dh, int64_t ld_dh, int64_t m, int64_t n,
+                                                      T* __restrict__ dgu, int64_t ld) {
+    const int64_t c = (blockIdx.x * int64_t(256) + threadIdx.x) * V;
+    if (c >= n) return;
+    for (int64_t r = blockIdx.y; r < m; r += gridDim.y) {
+        float g[V], u[V], d[V], a[V], b[V];
+        if constexpr (V == 8) {
+            const uint4* pg = reinterpret_cast<const uint4*>(preact + r * n + c);
+            const uint4* pu = reinterpret_cast<const uint4*>(preact + (m + r) * n + c);
+            const uint4 g0 = ld_stream(pg), g1 = ld_stream(pg + 1), u0 = ld_stream(pu), u1 = ld_stream(pu + 1);
+            Word<T>::unpack(*reinterpret_cast<const uint4*>(dh + r * ld_dh + c), d);
+            Word<float>::unpack(g0, g), Word<float>::unpack(g1, g + 4), Word<float>::unpack(u0, u), Word<float>::unpack(u1, u + 4);
+        } else {
+            g[0] = preact[r * n + c], u[0] = preact[(m + r) * n + c], d[0] = to_f32(dh[r * ld_dh + c]);
         }
-        __syncthreads();
-        for (int l = 0; l < 16; ++l)
-            for (int r = 0; r < 4; ++r)
-                for (int c = 0; c < 4; ++c) acc[r][c] = fmaf(sa[l][4 * ty + r], sb[l][4 * tx + c], acc[r][c]);
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < V; ++i) a[i] = d[i] * u[i] * act_slope<ACT>(g[i]), b[i] = d[i] * act<ACT>(g[i]);
+        if constexpr (V == 8) {
+            *reinterpret_cast<uint4*>(dgu + r * ld + c) = Word<T>::pack(a);
+            *reinterpret_cast<uint4*>(dgu + (m + r) * ld + c) = Word<T>::pack(b);
+        } else {
+            dgu[r * ld + c] = from_f32<T>(a[0]), dgu[(m + r) * ld + c] = from_f32<T>(b[0]);
+        }
     }
 }
 
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) glu_kernel(const T* x, int64_t ld_x, const T* wg, const T* wu, int64_t ld_w, int64_t m, int64_t n,
-                                                  int64_t k, T* h, int64_t ld_h, float* preact) {
-    __shared__ float sa[16][65], sb[16][65];
-    const int64_t i0 = static_cast<int64_t>(blockIdx.x) * 64, j0 = static_cast<int64_t>(blockIdx.y) * 64;
-    float g[4][4] = {}, u[4][4] = {};
-    tile_product(x, ld_x, int64_t(1), wg, ld_w, int64_t(1), i0, m, j0, n, k, g, sa, sb);
-    tile_product(x, ld_x, int64_t(1), wu, ld_w, int64_t(1), i0, m, j0, n, k, u, sa, sb);
-    for (int r = 0; r < 4; ++r)
-        for (int c = 0; c < 4; ++c) {
-            const int64_t i = i0 + threadIdx.x / 16 * 4 + r, j = j0 + threadIdx.x % 16 * 4 + c;
-            if (i >= m || j >= n) continue;
-            h[i * ld_h + j] = from_f32<T>(act<ACT>(g[r][c]) * u[r][c]);
-            if (preact != nullptr) preact[i * n + j] = g[r][c], preact[(m + i) * n + j] = u[r][c];
-        }
+// Rows of 16-bit elements copied to rows that begin on 16-byte boundaries.
+__global__ void __launch_bounds__(256) glu_lay_out_kernel(const uint16_t* __restrict__ from, int64_t ld_from, int64_t rows, int64_t n,
+                                                          uint16_t* __restrict__ to, int64_t ld_to) {
+    const int64_t c = blockIdx.x * int64_t(256) + threadIdx.x;
+    if (c >= n) return;
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) to[r * ld_to + c] = from[r * ld_from + c];
 }
 
-// dgu[0] = dh * u * act'(g), dgu[1] = dh * act(g), each [m][n].
-template <typename T, int ACT>
-__global__ void __launch_bounds__(256) glu_dgu_kernel(const float* preact, const T* dh, int64_t ld_dh, int64_t m, int64_t n, T* dgu) {
-    for (int64_t e = blockIdx.x * int64_t(256) + threadIdx.x; e < m * n; e += gridDim.x * int64_t(256)) {
-        const float g = preact[e], u = preact[m * n + e], d = to_f32(dh[e / n * ld_dh + e % n]);
-        dgu[e] = from_f32<T>(d * u * act_slope<ACT>(g));
-        dgu[m * n + e] = from_f32<T>(d * act<ACT>(g));
+dim3 row_grid(int64_t rows, int64_t columns_of_threads) {
+    const int64_t x = (columns_of_threads + 255) / 256;
+    int64_t y = (32 * kNumSMs + x - 1) / x;
+    if (y > rows) y = rows;
+    if (y > 65535) y = 65535;
+    return dim3(static_cast<unsigned>(x), static_cast<unsigned>(y));
+}
+
+// Whether a tensor map can describe rows like these.
+bool laid_out(const void* p, int64_t ld, int64_t rows) { return aligned16(p) && (rows <= 1 || ld % 8 == 0); }
+
+struct Operand {
+    const void* p;
+    int64_t ld;
+};
+// The operand itself, or a copy of it in `room`.
+int lay_out(const void* p, int64_t ld, int64_t rows, int64_t n, char*& room, Operand& o, cudaStream_t s) {
+    const int64_t ld_to = (n + 7) / 8 * 8;
+    if (laid_out(p, ld, rows)) {
+        o = {p, rows > 1 ? ld : ld_to};
+        return BZ_OK;
     }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(256) glu_dx_kernel(const T* dgu, const T* wg, const T* wu, int64_t ld_w, int64_t m, int64_t n, int64_t k, T* dx, int64_t ld_dx) {
-    __shared__ float sa[16][65], sb[16][65];
-    const int64_t i0 = static_cast<int64_t>(blockIdx.x) * 64, j0 = static_cast<int64_t>(blockIdx.y) * 64;
-    float acc[4][4] = {};
-    tile_product(dgu, n, int64_t(1), wg, int64_t(1), ld_w, i0, m, j0, k, n, acc, sa, sb);
-    tile_product(dgu + m * n, n, int64_t(1), wu, int64_t(1), ld_w, i0, m, j0, k, n, acc, sa, sb);
-    for (int r = 0; r < 4; ++r)
-        for (int c = 0; c < 4; ++c) {
-            const int64_t i = i0 + threadIdx.x / 16 * 4 + r, j = j0 + threadIdx.x % 16 * 4 + c;
-            if (i < m && j < k) dx[i * ld_dx + j] = from_f32<T>(acc[r][c]);
-        }
-}
-
-template <typename T, typename G>
-__global__ void __launch_bounds__(256) glu_dw_kernel(const T* dgu, const T* x, int64_t ld_x, int64_t m, int64_t n, int64_t k, G* dwg, G* dwu, int64_t ld_dw) {
-    __shared__ float sa[16][65], sb[16][65];
-    const int64_t i0 = static_cast<int64_t>(blockIdx.x) * 64, j0 = static_cast<int64_t>(blockIdx.y) * 64;
-    float acc[4][4] = {};
-    tile_product(dgu + blockIdx.z * m * n, int64_t(1), n, x, int64_t(1), ld_x, i0, n, j0, k, m, acc, sa, sb);
-    G* out = blockIdx.z ? dwu : dwg;
-    for (int r = 0; r < 4; ++r)
-        for (int c = 0; c < 4; ++c) {
-            const int64_t i = i0 + threadIdx.x / 16 * 4 + r, j = j0 + threadIdx.x % 16 * 4 + c;
-            if (i < n && j < k) out[i * ld_dw + j] = from_f32<G>(acc[r][c]);
-        }
-}
-
-unsigned tiles(int64_t n) { return static_cast<unsigned>((n + 63) / 64); }
-
-template <typename T, int ACT>
-int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, int64_t m, int64_t n, int64_t k, void* h, int64_t ld_h,
-            float* preact, cudaStream_t s) {
-    glu_kernel<T, ACT><<<dim3(tiles(m), tiles(n)), 256, 0, s>>>(static_cast<const T*>(x), ld_x, static_cast<const T*>(wg),
-                                                                 static_cast<const T*>(wu), ld_w, m, n, k, static_cast<T*>(h), ld_h, preact);
+    o = {room, ld_to};
+    glu_lay_out_kernel<<<row_grid(rows, n), 256, 0, s>>>(static_cast<const uint16_t*>(p), ld, rows, n, reinterpret_cast<uint16_t*>(room), ld_to);
+    room += round_up(static_cast<size_t>(rows) * ld_to * 2, 256);
     note_launch();
     return check_launch();
 }
 
+// Tensor map of [z][rows][n] 16-bit elements, boxes of 64 x box_rows, 128-byte swizzle, zeros outside.
+template <typename T> bool make_map(CUtensorMap* map, const void* p, int64_t n, int64_t rows, int64_t ld, int box_rows, int64_t ld_z) {
+    EncodeTiledFn enc = encode_tiled();
+    if (enc == nullptr) return false;
+    const cuuint32_t rank = ld_z ? 3 : 2;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(n), static_cast<cuuint64_t>(rows), 2};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld_z) * 2};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1}, elem[3] = {1, 1, 1};
+    return enc(map, __is_same(T, __half) ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(p), dims,
+               strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Width of the tiles and shares of the contraction.
+struct Plan {
+    int bn, splits;
+};
+Plan plan(GluProduct kind, int64_t rows, int64_t cols, int64_t blocks) {
+    const int64_t row_tiles = (kind == kWeight ? 2 : 1) * ceil_div(rows, kRowTile);
+    Plan best{256, 1};
+    double least = 0;
+    for (int bn = 256; bn >= (kind == kForward ? 64 : 128); bn /= 2) {
+        const int64_t tiles = row_tiles * ceil_div(cols, kind == kForward ? bn / 2 : bn);
+        int splits = 1;
+        if (kind != kForward)
+            while (splits < 16 && tiles * (splits + 1) <= kClusters && blocks / (splits + 1) >= 8) ++splits;
+        const double cost = static_cast<double>(ceil_div(tiles * splits, kClusters)) *
+                            (static_cast<double>(ceil_div(blocks, splits)) * (bn == 256 ? 520 : (bn == 128 ? 380 : 320)) + 1500);
+        if (least == 0 || cost < least) least = cost, best = {bn, splits};
+    }
+    return best;
+}
+
+template <typename T, GluProduct P, int BN>
+int launch_product(const CUtensorMap& a, const CUtensorMap& b0, const CUtensorMap& b1, const ProductParams& p, cudaStream_t s) {
+    auto kern = glu_product_kernel<T, P, BN>;
+    constexpr int smem = ProductShape<BN>::kSmem;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return cuda_failed(e);
+    unsigned int* timeouts = nullptr;
+    if ((e = cudaGetSymbolAddress(reinterpret_cast<void**>(&timeouts), g_timeouts)) != cudaSuccess) return cuda_failed(e);
+    const int64_t tiles = p.row_tiles * p.col_tiles * p.splits;
+    kern<<<static_cast<unsigned>(2 * (tiles < kClusters ? tiles : kClusters)), kProductThreads, smem, s>>>(a, b0, b1, p, timeouts);
+    note_launch();
+    const int st = check_launch();
+    if (st != BZ_OK || p.splits == 1) return st;
+    glu_shares_kernel<T, BN><<<4 * kNumSMs, 256, 0, s>>>(p, P == kWeight);
+    note_launch();
+    return check_launch();
+}
+
+template <typename T, GluProduct P>
+int product(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b0, const CUtensorMap& b1, const ProductParams& p, cudaStream_t s) {
+    if (pl.bn == 256) return launch_product<T, P, 256>(a, b0, b1, p, s);
+    if constexpr (P == kForward)
+        if (pl.bn == 64) return launch_product<T, P, 64>(a, b0, b1, p, s);
+    return launch_product<T, P, 128>(a, b0, b1, p, s);
+}
+
+int zero(void* p, int64_t ld, int64_t rows, int64_t n, int bytes, cudaStream_t s) {
+    if (p == nullptr || rows == 0 || n == 0) return BZ_OK;
+    const cudaError_t e = cudaMemset2DAsync(p, static_cast<size_t>(rows > 1 ? ld : n) * bytes, 0, static_cast<size_t>(n) * bytes, rows, s);
+    return e == cudaSuccess ? BZ_OK : cuda_failed(e);
+}
+
+bool wide_rows(const void* p, int64_t ld, int64_t rows, int bytes) { return aligned16(p) && (rows <= 1 || ld * bytes % 16 == 0); }
+
+template <typename T>
+int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, int64_t m, int64_t n, int64_t k, int act, void* h,
+            int64_t ld_h, float* preact, char* ws, cudaStream_t s) {
+    int st;
+    if (k == 0) {
+        if (preact != nullptr && (st = zero(preact, n, 2 * m, n, 4, s)) != BZ_OK) return st;
+        return zero(h, ld_h, m, n, 2, s);
+    }
+    Operand ox, og, ou;
+    if ((st = lay_out(x, ld_x, m, k, ws, ox, s)) != BZ_OK || (st = lay_out(wg, ld_w, n, k, ws, og, s)) != BZ_OK ||
+        (st = lay_out(wu, ld_w, n, k, ws, ou, s)) != BZ_OK)
+        return st;
+    ProductParams p{};
+    p.rows = m, p.cols = n, p.blocks = ceil_div(k, kBlockK);
+    const Plan pl = plan(kForward, m, n, p.blocks);
+    p.row_tiles = ceil_div(m, kRowTile), p.col_tiles = ceil_div(n, pl.bn / 2), p.splits = 1;
+    p.act = act, p.out = h, p.ld_out = ld_h, p.wide = wide_rows(h, ld_h, m, 2);
+    p.preact = preact, p.preact_wide = n % 4 == 0;
+    CUtensorMap a, b0, b1;
+    if (!make_map<T>(&a, ox.p, k, m, ox.ld, 128, 0) || !make_map<T>(&b0, og.p, k, n, og.ld, pl.bn / 2, 0) ||
+        !make_map<T>(&b1, ou.p, k, n, ou.ld, pl.bn / 2, 0))
+        return BZ_ERR_UNSUPPORTED;
+    return product<T, kForward>(pl, a, b0, b1, p, s);
+}
+
 template <typename T, int ACT>
+int launch_dgu(const float* preact, const T* dh, int64_t ld_dh, int64_t m, int64_t n, T* dgu, int64_t ld, cudaStream_t s) {
+    if (n % 8 == 0 && laid_out(dh, ld_dh, m))
+        glu_dgu_kernel<T, ACT, 8><<<row_grid(m, n / 8), 256, 0, s>>>(preact, dh, ld_dh, m, n, dgu, ld);
+    else
+        glu_dgu_kernel<T, ACT, 1><<<row_grid(m, n), 256, 0, s>>>(preact, dh, ld_dh, m, n, dgu, ld);
+    note_launch();
+    return check_launch();
+}
+
+template <typename T>
 int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, const float* preact, const void* dh, int64_t ld_dh,
-             int64_t m, int64_t n, int64_t k, void* dx, int64_t ld_dx, void* dwg, void* dwu, int64_t ld_dw, int grad_dtype, void* ws, cudaStream_t s) {
-    T* dgu = static_cast<T*>(ws);
-    glu_dgu_kernel<T, ACT><<<8 * kNumSMs, 256, 0, s>>>(preact, static_cast<const T*>(dh), ld_dh, m, n, dgu);
-    note_launch();
-    if (dx != nullptr && m > 0 && k > 0) {
-        glu_dx_kernel<T><<<dim3(tiles(m), tiles(k)), 256, 0, s>>>(dgu, static_cast<const T*>(wg), static_cast<const T*>(wu), ld_w, m, n, k, static_cast<T*>(dx), ld_dx);
-        note_launch();
+             int64_t m, int64_t n, int64_t k, int act, void* dx, int64_t ld_dx, void* dwg, void* dwu, int64_t ld_dw, int grad_f32, char* ws,
+             cudaStream_t s) {
+    int st;
+    if (m == 0 || n == 0) {
+        if ((st = zero(dx, ld_dx, m, k, 2, s)) != BZ_OK || (st = zero(dwg, ld_dw, n, k, grad_f32 ? 4 : 2, s)) != BZ_OK) return st;
+        return zero(dwu, ld_dw, n, k, grad_f32 ? 4 : 2, s);
     }
-    if (dwg != nullptr && n > 0 && k > 0) {
-        const dim3 grid(tiles(n), tiles(k), 2);
-        if (grad_dtype == BZ_F32)
-            glu_dw_kernel<T, float><<<grid, 256, 0, s>>>(dgu, static_cast<const T*>(x), ld_x, m, n, k, static_cast<float*>(dwg), static_cast<float*>(dwu), ld_dw);
-        else
-            glu_dw_kernel<T, T><<<grid, 256, 0, s>>>(dgu, static_cast<const T*>(x), ld_x, m, n, k, static_cast<T*>(dwg), static_cast<T*>(dwu), ld_dw);
-        note_launch();
+    const int64_t ld = (n + 7) / 8 * 8;
+    T* dgu = reinterpret_cast<T*>(ws);
+    float* partial = reinterpret_cast<float*>(ws + round_up(static_cast<size_t>(4) * m * ld, 256));
+    char* room = reinterpret_cast<char*>(partial) + kPartialBytes;
+    const T* d = static_cast<const T*>(dh);
+    switch (act) {
+        case BZ_ACT_SILU: st = launch_dgu<T, BZ_ACT_SILU>(preact, d, ld_dh, m, n, dgu, ld, s); break;
+        case BZ_ACT_GELU_TANH: st = launch_dgu<T, BZ_ACT_GELU_TANH>(preact, d, ld_dh, m, n, dgu, ld, s); break;
+        case BZ_ACT_GELU: st = launch_dgu<T, BZ_ACT_GELU>(preact, d, ld_dh, m, n, dgu, ld, s); break;
+        default: st = launch_dgu<T, BZ_ACT_RELU>(preact, d, ld_dh, m, n, dgu, ld, s); break;
     }
-    return check_launch();
+    if (st != BZ_OK) return st;
+    CUtensorMap a, b0, b1;
+    ProductParams p{};
+    p.cols = k, p.partial = partial;
+    if (dx != nullptr) {
+        Operand og, ou;
+        if ((st = lay_out(wg, ld_w, n, k, room, og, s)) != BZ_OK || (st = lay_out(wu, ld_w, n, k, room, ou, s)) != BZ_OK) return st;
+        p.rows = m, p.blocks = ceil_div(n, kBlockK);
+        const Plan pl = plan(kInput, m, k, 2 * p.blocks);
+        p.row_tiles = ceil_div(m, kRowTile), p.col_tiles = ceil_div(k, pl.bn), p.splits = pl.splits;
+        p.out = dx, p.ld_out = ld_dx, p.wide = wide_rows(dx, ld_dx, m, 2);
+        if (!make_map<T>(&a, dgu, n, m, ld, 128, m * ld) || !make_map<T>(&b0, og.p, k, n, og.ld, kBlockK, 0) ||
+            !make_map<T>(&b1, ou.p, k, n, ou.ld, kBlockK, 0))
+            return BZ_ERR_UNSUPPORTED;
+        if ((st = product<T, kInput>(pl, a, b0, b1, p, s)) != BZ_OK) return st;
+    }
+    if (dwg != nullptr) {
+        Operand ox;
+        if ((st = lay_out(x, ld_x, m, k, room, ox, s)) != BZ_OK) return st;
+        p.rows = n, p.blocks = ceil_div(m, kBlockK);
+        const Plan pl = plan(kWeight, n, k, p.blocks);
+        p.row_tiles = 2 * ceil_div(n, kRowTile), p.col_tiles = ceil_div(k, pl.bn), p.splits = pl.splits;
+        p.out = dwg, p.out2 = dwu, p.ld_out = ld_dw, p.out_f32 = grad_f32;
+        p.wide = wide_rows(dwg, ld_dw, n, grad_f32 ? 4 : 2) && aligned16(dwu);
+        if (!make_map<T>(&a, dgu, n, m, ld, kBlockK, m * ld) || !make_map<T>(&b0, ox.p, k, m, ox.ld, kBlockK, 0)) return BZ_ERR_UNSUPPORTED;
+        if ((st = product<T, kWeight>(pl, a, b0, b0, p, s)) != BZ_OK) return st;
+    }
+    return BZ_OK;
 }
-
-#define BZ_GLU_SWITCH(CALL)                                                   \
-    switch (act) {                                                            \
-        case BZ_ACT_SILU: return dtype == BZ_F16 ? CALL(__half, BZ_ACT_SILU) : CALL(__nv_bfloat16, BZ_ACT_SILU);                \
-        case BZ_ACT_GELU_TANH: return dtype == BZ_F16 ? CALL(__half, BZ_ACT_GELU_TANH) : CALL(__nv_bfloat16, BZ_ACT_GELU_TANH); \
-        case BZ_ACT_GELU: return dtype == BZ_F16 ? CALL(__half, BZ_ACT_GELU) : CALL(__nv_bfloat16, BZ_ACT_GELU);                \
-        default: return dtype == BZ_F16 ? CALL(__half, BZ_ACT_RELU) : CALL(__nv_bfloat16, BZ_ACT_RELU);                         \
-    }
 
 int check(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, int64_t m, int64_t n, int64_t k, int dtype, int act) {
     if (m < 0 || n < 0 || k < 0 || element_bytes(dtype) == 0 || act < BZ_ACT_SILU || act > BZ_ACT_RELU) return BZ_ERR_INVALID_ARG;
-    const int64_t most = (int64_t(1) << 31) - 1;
-    if (m > most || n > most || k > most || dtype == BZ_F32) return BZ_ERR_UNSUPPORTED;
+    const int64_t most = (int64_t(1) << 31) - 512;  // tile coordinates are 32-bit
+    if (m > most || n > most || k > most || dtype == BZ_F32 || ld_x >= int64_t(1) << 38 || ld_w >= int64_t(1) << 38) return BZ_ERR_UNSUPPORTED;
     if ((m > 1 && ld_x < k) || (n > 1 && ld_w < k)) return BZ_ERR_INVALID_ARG;
     if ((m > 0 && k > 0 && x == nullptr) || (n > 0 && k > 0 && (wg == nullptr || wu == nullptr))) return BZ_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(wg) | reinterpret_cast<uintptr_t>(wu)) & 1) return BZ_ERR_INVALID_ARG;
     return BZ_OK;
 }
 
-// Whether a tensor map can describe rows like these.
-bool laid_out(const void* p, int64_t ld, int64_t rows) { return aligned16(p) && (rows <= 1 || ld % 8 == 0); }
-
 }  // namespace
+
+int glu_timeouts(unsigned int* count) {
+    const cudaError_t e = cudaMemcpyFromSymbol(count, g_timeouts, sizeof(unsigned int));
+    return e == cudaSuccess ? BZ_OK : cuda_failed(e);
+}
 
 }  // namespace bz
 
@@ -160,7 +253,9 @@ using namespace bz;
 
 extern "C" size_t bz_glu_workspace_bytes(int64_t m, int64_t n, int64_t k, int dtype, int backward) {
     if (m < 0 || n < 0 || k < 0 || (dtype != BZ_F16 && dtype != BZ_BF16)) return 0;
-    return backward ? round_up(static_cast<size_t>(4) * m * n, 256) + 256 : 256;
+    const size_t kp = round_up(k, 8), np = round_up(n, 8);
+    const size_t operands = round_up(2 * m * kp, 256) + 2 * round_up(2 * n * kp, 256);
+    return backward ? round_up(4 * m * np, 256) + kPartialBytes + operands : operands;
 }
 
 extern "C" int bz_glu(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w, int64_t m, int64_t n, int64_t k,
@@ -173,9 +268,9 @@ extern "C" int bz_glu(const void* x, int64_t ld_x, const void* w_gate, const voi
         (workspace == nullptr || !aligned256(workspace) || workspace_bytes < bz_glu_workspace_bytes(m, n, k, dtype, 0)))
         return BZ_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-#define BZ_CALL(T, A) forward<T, A>(x, ld_x, w_gate, w_up, ld_w, m, n, k, h, ld_h, preact, s)
-    BZ_GLU_SWITCH(BZ_CALL)
-#undef BZ_CALL
+    char* ws = static_cast<char*>(workspace);
+    return dtype == BZ_F16 ? forward<__half>(x, ld_x, w_gate, w_up, ld_w, m, n, k, act, h, ld_h, preact, ws, s)
+                           : forward<__nv_bfloat16>(x, ld_x, w_gate, w_up, ld_w, m, n, k, act, h, ld_h, preact, ws, s);
 }
 
 extern "C" int bz_glu_backward(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w, const float* preact,
@@ -194,8 +289,9 @@ extern "C" int bz_glu_backward(const void* x, int64_t ld_x, const void* w_gate, 
         return BZ_ERR_INVALID_ARG;
     if (workspace == nullptr || !aligned256(workspace) || workspace_bytes < bz_glu_workspace_bytes(m, n, k, dtype, 1)) return BZ_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-#define BZ_CALL(T, A) \
-    backward<T, A>(x, ld_x, w_gate, w_up, ld_w, preact, dh, ld_dh, m, n, k, dx, ld_dx, dw_gate, dw_up, ld_dw, grad_dtype, workspace, s)
-    BZ_GLU_SWITCH(BZ_CALL)
-#undef BZ_CALL
+    char* ws = static_cast<char*>(workspace);
+    const int f32 = grad_dtype == BZ_F32;
+    return dtype == BZ_F16
+               ? backward<__half>(x, ld_x, w_gate, w_up, ld_w, preact, dh, ld_dh, m, n, k, act, dx, ld_dx, dw_gate, dw_up, ld_dw, f32, ws, s)
+               : backward<__nv_bfloat16>(x, ld_x, w_gate, w_up, ld_w, preact, dh, ld_dh, m, n, k, act, dx, ld_dx, dw_gate, dw_up, ld_dw, f32, ws, s);
 }

@@ -1,0 +1,332 @@
+// The three products of the gated feed-forward block on the tensor cores, one kernel template.
+//
+//   kForward   [g | u] = x [w_gate | w_up]^T      rows m, columns n (gate and up side by side), contraction k
+//   kInput     dx = dg w_gate + du w_up           rows m, columns k, contraction over both halves of n
+//   kWeight    dw_gate | dw_up = (dg | du)^T x    rows n (gate tiles, then up tiles), columns k, contraction m
+//
+// A pair of CTAs (one cluster) computes a 256 x BN tile with tcgen05.mma.cta_group::2, K = 16 an instruction: a pair
+// reads half as much of B from shared memory per flop as two single CTAs would.  Operands arrive by TMA in blocks of 64
+// along the contraction, 128-byte swizzle, a ring of stages; the layouts of x, weights and dgu in memory are taken as
+// they are: where the contraction index is not the contiguous one (the weights in kInput, both operands in kWeight) the
+// MMA reads the block across rows.  For the forward product CTA 0 brings gate columns and CTA 1 up columns of the same
+// BN/2 hidden units, so g and u of a unit meet in one thread of the epilogue and h = act(g)*u leaves without another pass.
+// Accumulators: two sets of BN tensor-memory columns in turn, so a tile's epilogue runs under the next tile's MMAs.
+//
+// Persistent: at most one cluster per pair of SMs; tiles in groups of eight row tiles, columns inside a group in turn, so
+// that the operands of the tiles in flight stay in the L2.  kInput and kWeight may be cut along the contraction when there
+// are fewer tiles than clusters; each share then leaves binary32 sums in the workspace and a last kernel adds the
+// shares in order.
+//
+// Every wait is bounded: a thread whose wait runs out sets its CTA's `dead` word, all roles leave their loops, the leader
+// waits (bounded again) for the loads in flight, and both CTAs meet at the cluster barrier before tensor memory is freed.
+#pragma once
+
+#include "umma_pair.cuh"
+#include "worker_common.cuh"
+
+namespace bz {
+
+enum GluProduct { kForward, kInput, kWeight };
+
+constexpr int kRowTile = 256, kBlockK = 64, kEpilogueWarps = 4, kProductThreads = 128 + 32 * kEpilogueWarps;
+
+struct ProductParams {
+    int64_t rows, cols;          // extents of the result (kWeight: rows of one half; kForward: hidden units)
+    int64_t row_tiles, col_tiles;
+    int64_t blocks;              // of kBlockK along the contraction (kInput: of one half)
+    int splits;                  // shares of the contraction
+    int act;
+    void* out;                   // h / dx / dw_gate
+    void* out2;                  // dw_up
+    int64_t ld_out;
+    int out_f32, wide;           // binary32 output; 16-byte stores possible
+    float* preact;               // kForward: [2][rows][cols] or null
+    int preact_wide;
+    float* partial;              // splits > 1: [split][tile][256][BN]
+};
+
+template <int BN> struct ProductShape {
+    static constexpr int kABytes = 128 * kBlockK * 2, kBBytes = BN / 2 * kBlockK * 2, kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = BN == 256 ? 6 : (BN == 128 ? 8 : 10);
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + (2 * kStages + 4) * 8 + 16;
+};
+
+// ---- activations --------------------------------------------------------------------------------
+
+__device__ __forceinline__ float logistic(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+template <int ACT> __device__ __forceinline__ float act(float g) {
+    if constexpr (ACT == BZ_ACT_SILU) return g * logistic(g);
+    // (1 + tanh y)/2 = 1/(1 + exp(-2y))
+    if constexpr (ACT == BZ_ACT_GELU_TANH) return g * logistic(1.5957691216f * (g + 0.044715f * g * g * g));
+    if constexpr (ACT == BZ_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678f));
+    return g > 0.f ? g : (g == g ? 0.f : g);
+}
+template <int ACT> __device__ __forceinline__ float act_slope(float g) {
+    if constexpr (ACT == BZ_ACT_SILU) {
+        const float s = logistic(g);
+        return s * (1.f + g * (1.f - s));
+    }
+    if constexpr (ACT == BZ_ACT_GELU_TANH) {
+        const float s = logistic(1.5957691216f * (g + 0.044715f * g * g * g));
+        return s + g * s * (1.f - s) * 1.5957691216f * (1.f + 0.134145f * g * g);
+    }
+    if constexpr (ACT == BZ_ACT_GELU) return 0.5f * (1.f + erff(g * 0.70710678f)) + g * 0.39894228f * __expf(-0.5f * g * g);
+    return g > 0.f ? 1.f : 0.f;
+}
+template <int ACT> __device__ __forceinline__ void gate32(float (&g)[32], const float (&u)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) g[i] = act<ACT>(g[i]) * u[i];
+}
+
+// ---- stores -------------------------------------------------------------------------------------
+
+// 32 values of one row from column c0 on; `n` columns exist.
+template <typename T> __device__ __forceinline__ void store32(T* row, int64_t c0, int64_t n, bool wide, const float (&x)[32]) {
+    constexpr int V = Word<T>::kN;
+    if (wide && c0 + 32 <= n) {
+#pragma unroll
+        for (int i = 0; i < 32 / V; ++i) reinterpret_cast<uint4*>(row + c0)[i] = Word<T>::pack(x + i * V);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (c0 + i < n) row[c0 + i] = from_f32<T>(x[i]);
+    }
+}
+
+struct ProductTile {
+    int64_t row, col;  // in tiles
+    int split;
+};
+__device__ __forceinline__ ProductTile tile_at(const ProductParams& p, int64_t i) {
+    constexpr int64_t G = 8;
+    ProductTile t;
+    const int64_t per = p.row_tiles * p.col_tiles;
+    t.split = static_cast<int>(i / per);
+    i -= t.split * per;
+    const int64_t g = i / (G * p.col_tiles), first = g * G;
+    const int64_t n = min(G, p.row_tiles - first);
+    i -= g * G * p.col_tiles;
+    t.row = first + i % n;
+    t.col = i / n;
+    return t;
+}
+// Contraction blocks [from, to) of a share.
+__device__ __forceinline__ void share_of(const ProductParams& p, int64_t all, int split, int64_t& from, int64_t& to) {
+    from = all * split / p.splits;
+    to = all * (split + 1) / p.splits;
+}
+
+// b0 / b1: the B operands of the two halves (kForward: CTA 0's and CTA 1's; kInput: of the first and second half of the
+// contraction; kWeight: b0 alone).
+template <typename T, GluProduct P, int BN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
+    glu_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b0_map,
+                       const __grid_constant__ CUtensorMap b1_map, const __grid_constant__ ProductParams p, unsigned int* timeouts) {
+    using S = ProductShape<BN>;
+    constexpr bool kAcrossA = P == kWeight, kAcrossB = P != kForward;
+    constexpr uint32_t kIdesc = idesc_16bit(256, BN, sizeof(T) == 2 && !__is_same(T, __half), kAcrossA, kAcrossB);
+    constexpr int kBlockBytes = 64 * kBlockK * 2;   // 64 rows of 128 bytes
+    extern __shared__ unsigned char raw[];
+    unsigned char* smem = raw + (1024 - smem_u32(raw) % 1024) % 1024;
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStageBytes);
+    uint64_t* empty = full + S::kStages;
+    uint64_t* acc_full = empty + S::kStages;   // [2]
+    uint64_t* acc_empty = acc_full + 2;        // [2], the leader's are used
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+    volatile int* dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int64_t cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
+    const int64_t tiles = p.row_tiles * p.col_tiles * p.splits;
+    const int64_t blocks = P == kInput ? 2 * p.blocks : p.blocks;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
+        for (int s = 0; s < 2; ++s) mbar_init(&acc_full[s], 1), mbar_init(&acc_empty[s], 2 * kEpilogueWarps);
+        *dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) tmem_alloc_pair(tmem_slot, 512);
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    int64_t it = 0;   // blocks loaded (thread 0), multiplied (the issuing thread)
+
+    if (warp == 0 && lane == 0) {
+        // ---------------------------------------------------------------- loads
+        bool alive = true;
+        for (int64_t i = cluster; i < tiles && alive; i += clusters) {
+            const ProductTile t = tile_at(p, i);
+            int64_t from, to;
+            share_of(p, blocks, t.split, from, to);
+            for (int64_t kb = from; kb < to; ++kb, ++it) {
+                const int s = static_cast<int>(it % S::kStages);
+                const uint32_t round = static_cast<uint32_t>(it / S::kStages);
+                if (round > 0 && !mbar_wait_live(&empty[s], (round - 1) & 1, dead)) {
+                    alive = false;
+                    break;
+                }
+                const uint32_t bar = leader_addr(&full[s]);
+                if (rank == 0) mbar_expect_tx(&full[s], 2 * S::kStageBytes);
+                const uint32_t a = smem_u32(smem + s * S::kStageBytes), b = a + S::kABytes;
+                if constexpr (P == kForward) {
+                    const int x = static_cast<int>(kb * kBlockK);
+                    tma_load_pair(a, &a_map, bar, x, static_cast<int>(t.row * 256 + rank * 128));
+                    tma_load_pair(b, rank == 0 ? &b0_map : &b1_map, bar, x, static_cast<int>(t.col * (BN / 2)));
+                } else if constexpr (P == kInput) {
+                    const int half = kb >= p.blocks, x = static_cast<int>((kb - half * p.blocks) * kBlockK);
+                    tma_load_pair(a, &a_map, bar, x, static_cast<int>(t.row * 256 + rank * 128), half);
+#pragma unroll
+                    for (int c = 0; c < BN / 128; ++c)
+                        tma_load_pair(b + c * kBlockBytes, half ? &b1_map : &b0_map, bar, static_cast<int>(t.col * BN + rank * (BN / 2) + c * 64), x);
+                } else {
+                    const int y = static_cast<int>(kb * kBlockK);
+                    const int64_t half_tiles = p.row_tiles / 2;
+                    const int half = t.row >= half_tiles;
+                    const int x = static_cast<int>((t.row - half * half_tiles) * 256 + rank * 128);
+                    tma_load_pair(a, &a_map, bar, x, y, half);
+                    tma_load_pair(a + kBlockBytes, &a_map, bar, x + 64, y, half);
+#pragma unroll
+                    for (int c = 0; c < BN / 128; ++c)
+                        tma_load_pair(b + c * kBlockBytes, &b0_map, bar, static_cast<int>(t.col * BN + rank * (BN / 2) + c * 64), y);
+                }
+            }
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        // ---------------------------------------------------------------- MMA issue
+        int64_t n = 0;
+        bool alive = true;
+        for (int64_t i = cluster; i < tiles && alive; i += clusters, ++n) {
+            const ProductTile t = tile_at(p, i);
+            int64_t from, to;
+            share_of(p, blocks, t.split, from, to);
+            const int acc = static_cast<int>(n & 1);
+            if (n >= 2 && !mbar_wait_live(&acc_empty[acc], static_cast<uint32_t>((n >> 1) - 1) & 1, dead)) break;
+            tc_fence_after_sync();
+            for (int64_t kb = from; kb < to; ++kb, ++it) {
+                const int s = static_cast<int>(it % S::kStages);
+                if (!mbar_wait_live(&full[s], static_cast<uint32_t>(it / S::kStages) & 1, dead)) {
+                    alive = false;
+                    break;
+                }
+                tc_fence_after_sync();
+                const uint32_t a = smem_u32(smem + s * S::kStageBytes), b = a + S::kABytes;
+#pragma unroll
+                for (int k = 0; k < kBlockK / 16; ++k) {
+                    const uint64_t da = kAcrossA ? smem_desc_mn128(a + k * 2048, kBlockBytes) : smem_desc_k128(a + k * 32);
+                    const uint64_t db = kAcrossB ? smem_desc_mn128(b + k * 2048, kBlockBytes) : smem_desc_k128(b + k * 32);
+                    mma_16bit_pair(tmem + acc * 256, da, db, kIdesc, kb > from || k > 0);
+                }
+                mma_commit_pair(&empty[s]);
+            }
+            if (alive) mma_commit_pair(&acc_full[acc]);
+        }
+    } else if (warp >= 4) {
+        // ---------------------------------------------------------------- epilogue: one row a thread
+        const int quarter = warp & 3;
+        int64_t n = 0;
+        for (int64_t i = cluster; i < tiles; i += clusters, ++n) {
+            const ProductTile t = tile_at(p, i);
+            const int acc = static_cast<int>(n & 1);
+            if (!__all_sync(~0u, mbar_wait_live(&acc_full[acc], static_cast<uint32_t>(n >> 1) & 1, dead))) break;  // a warp leaves as one
+            tc_fence_after_sync();
+            const uint32_t base = tmem + acc * 256 + (static_cast<uint32_t>(quarter * 32) << 16);
+            const int in_tile = static_cast<int>(rank) * 128 + quarter * 32 + lane;
+            if constexpr (P == kForward) {
+                const int64_t r = t.row * 256 + in_tile;
+#pragma unroll 1
+                for (int c = 0; c < BN / 2; c += 32) {
+                    float g[32], u[32];
+                    tmem_ld32(base + c, g);
+                    tmem_ld32(base + BN / 2 + c, u);
+                    tmem_ld32_wait(g);
+                    tmem_ld32_wait(u);
+                    const int64_t c0 = t.col * (BN / 2) + c;
+                    if (r < p.rows && c0 < p.cols) {
+                        if (p.preact != nullptr) {
+                            store32<float>(p.preact + r * p.cols, c0, p.cols, p.preact_wide, g);
+                            store32<float>(p.preact + (p.rows + r) * p.cols, c0, p.cols, p.preact_wide, u);
+                        }
+                        switch (p.act) {
+                            case BZ_ACT_SILU: gate32<BZ_ACT_SILU>(g, u); break;
+                            case BZ_ACT_GELU_TANH: gate32<BZ_ACT_GELU_TANH>(g, u); break;
+                            case BZ_ACT_GELU: gate32<BZ_ACT_GELU>(g, u); break;
+                            default: gate32<BZ_ACT_RELU>(g, u); break;
+                        }
+                        store32<T>(static_cast<T*>(p.out) + r * p.ld_out, c0, p.cols, p.wide, g);
+                    }
+                }
+            } else {
+                const int64_t half_tiles = P == kWeight ? p.row_tiles / 2 : 0;
+                const int half = P == kWeight && t.row >= half_tiles;
+                const int64_t r = (t.row - half * half_tiles) * 256 + in_tile;
+                void* out = half ? p.out2 : p.out;
+#pragma unroll 1
+                for (int c = 0; c < BN; c += 32) {
+                    float x[32];
+                    tmem_ld32(base + c, x);
+                    tmem_ld32_wait(x);
+                    const int64_t c0 = t.col * BN + c;
+                    if (p.splits > 1) {
+                        float* dst = p.partial + (i * 256 + in_tile) * BN + c;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) reinterpret_cast<uint4*>(dst)[e] = Word<float>::pack(x + 4 * e);
+                    } else if (r < p.rows && c0 < p.cols) {
+                        if (p.out_f32)
+                            store32<float>(static_cast<float*>(out) + r * p.ld_out, c0, p.cols, p.wide, x);
+                        else
+                            store32<T>(static_cast<T*>(out) + r * p.ld_out, c0, p.cols, p.wide, x);
+                    }
+                }
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) arrive_cluster(leader_addr(&acc_empty[acc]));
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (threadIdx.x == 0 && *dead) {
+        atomicAdd(timeouts, 1u);
+        if (rank == 0)  // shared memory has to outlive the loads in flight, the other CTA's among them
+            for (int64_t j = it > S::kStages ? it - S::kStages : 0; j < it; ++j)
+                mbar_wait(&full[j % S::kStages], static_cast<uint32_t>(j / S::kStages) & 1);
+    }
+    tc_fence_before_sync();
+    cluster_sync();
+    tc_fence_after_sync();
+    if (warp == 2) tmem_dealloc_pair(tmem, 512);
+}
+
+// The shares' sums of one product, in order: one thread a group of four columns.
+template <typename T, int BN>
+__global__ void __launch_bounds__(256) glu_shares_kernel(const __grid_constant__ ProductParams p, int weight) {
+    const int64_t per = p.row_tiles * p.col_tiles, groups = per * 256 * (BN / 4);
+    const int64_t half_tiles = weight ? p.row_tiles / 2 : 0;
+    for (int64_t e = blockIdx.x * int64_t(256) + threadIdx.x; e < groups; e += gridDim.x * int64_t(256)) {
+        const int64_t i = e / (256 * (BN / 4));
+        const int in = static_cast<int>(e % (256 * (BN / 4))), in_row = in / (BN / 4), c = in % (BN / 4) * 4;
+        const ProductTile t = tile_at(p, i);
+        const int half = weight && t.row >= half_tiles;
+        const int64_t r = (t.row - half * half_tiles) * 256 + in_row, c0 = t.col * BN + c;
+        if (r >= p.rows || c0 >= p.cols) continue;
+        float4 s = *reinterpret_cast<const float4*>(p.partial + (i * 256 + in_row) * BN + c);
+        for (int k = 1; k < p.splits; ++k) {
+            const float4 v = *reinterpret_cast<const float4*>(p.partial + ((k * per + i) * 256 + in_row) * BN + c);
+            s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+        }
+        const float x[4] = {s.x, s.y, s.z, s.w};
+        void* out = half ? p.out2 : p.out;
+        for (int k = 0; k < 4; ++k)
+            if (c0 + k < p.cols) {
+                if (p.out_f32)
+                    static_cast<float*>(out)[r * p.ld_out + c0 + k] = x[k];
+                else
+                    static_cast<T*>(out)[r * p.ld_out + c0 + k] = from_f32<T>(x[k]);
+            }
+    }
+}
+
+}  // namespace bz
