@@ -143,6 +143,7 @@ int zero(void* p, int64_t ld, int64_t rows, int64_t n, int bytes, cudaStream_t s
     return e == cudaSuccess ? BZ_OK : cuda_failed(e);
 }
 
+bool pair_rows(const void* p, int64_t ld, int64_t rows) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0 && (rows <= 1 || ld % 2 == 0); }
 bool wide_rows(const void* p, int64_t ld, int64_t rows, int bytes) { return aligned16(p) && (rows <= 1 || ld * bytes % 16 == 0); }
 
 template <typename T>
@@ -161,7 +162,7 @@ int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t
     p.rows = m, p.cols = n, p.blocks = ceil_div(k, kBlockK);
     const Plan pl = plan(kForward, m, n, p.blocks);
     p.row_tiles = ceil_div(m, kRowTile), p.col_tiles = ceil_div(n, pl.bn / 2), p.splits = 1;
-    p.act = act, p.out = h, p.ld_out = ld_h, p.wide = wide_rows(h, ld_h, m, 2);
+    p.act = act, p.out = h, p.ld_out = ld_h, p.wide = wide_rows(h, ld_h, m, 2), p.pairs = pair_rows(h, ld_h, m);
     p.preact = preact, p.preact_wide = n % 4 == 0;
     CUtensorMap a, b0, b1;
     if (!make_map<T>(&a, ox.p, k, m, ox.ld, 128, 0) || !make_map<T>(&b0, og.p, k, n, og.ld, pl.bn / 2, 0) ||
@@ -210,7 +211,7 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
         p.rows = m, p.blocks = ceil_div(n, kBlockK);
         const Plan pl = plan(kInput, m, k, 2 * p.blocks);
         p.row_tiles = ceil_div(m, kRowTile), p.col_tiles = ceil_div(k, pl.bn), p.splits = pl.splits;
-        p.out = dx, p.ld_out = ld_dx, p.wide = wide_rows(dx, ld_dx, m, 2);
+        p.out = dx, p.ld_out = ld_dx, p.wide = wide_rows(dx, ld_dx, m, 2), p.pairs = pair_rows(dx, ld_dx, m);
         if (!make_map<T>(&a, dgu, n, m, ld, 128, m * ld) || !make_map<T>(&b0, og.p, k, n, og.ld, kBlockK, 0) ||
             !make_map<T>(&b1, ou.p, k, n, ou.ld, kBlockK, 0))
             return BZ_ERR_UNSUPPORTED;
@@ -224,6 +225,7 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
         p.row_tiles = 2 * ceil_div(n, kRowTile), p.col_tiles = ceil_div(k, pl.bn), p.splits = pl.splits;
         p.out = dwg, p.out2 = dwu, p.ld_out = ld_dw, p.out_f32 = grad_f32;
         p.wide = wide_rows(dwg, ld_dw, n, grad_f32 ? 4 : 2) && aligned16(dwu);
+        p.pairs = pair_rows(dwg, ld_dw, n) && pair_rows(dwu, ld_dw, n);
         if (!make_map<T>(&a, dgu, n, m, ld, kBlockK, m * ld) || !make_map<T>(&b0, ox.p, k, m, ox.ld, kBlockK, 0)) return BZ_ERR_UNSUPPORTED;
         if ((st = product<T, kWeight>(pl, a, b0, b0, p, s)) != BZ_OK) return st;
     }

@@ -39,16 +39,53 @@ struct ProductParams {
     void* out;                   // h / dx / dw_gate
     void* out2;                  // dw_up
     int64_t ld_out;
-    int out_f32, wide;           // binary32 output; 16-byte stores possible
+    int out_f32, wide, pairs;    // binary32 output; 16-byte stores possible; 4-byte stores possible
     float* preact;               // kForward: [2][rows][cols] or null
     int preact_wide;
     float* partial;              // splits > 1: [split][tile][256][BN]
 };
 
+// ---- stores -------------------------------------------------------------------------------------
+// The accumulator gives a thread one row; memory wants a warp on one row.  A warp turns 32 rows x 32 words (128 bytes of
+// each row) through shared memory: rows 36 words apart, so that both the 16-byte writes (eight rows) and the 16-byte
+// reads (one row) of a quarter warp meet every bank once.
+
+constexpr int kTurnWords = 36, kTurnBytes = 32 * kTurnWords * 4;
+
+__device__ __forceinline__ void turn_in(float* turn, int word, const uint4& w) {
+    *reinterpret_cast<uint4*>(turn + (threadIdx.x & 31) * kTurnWords + word) = w;
+}
+// Writes elements [c0, c0 + 128 / sizeof(E)) of rows r0 .. r0 + 31 of `out`; `rows`, `cols` exist.  wide: 16-byte stores
+// possible; pairs: 4-byte stores of two 16-bit elements possible.
+template <typename E>
+__device__ __forceinline__ void turn_out(const float* turn, E* out, int64_t ld, int64_t r0, int64_t rows, int64_t c0, int64_t cols, bool wide, bool pairs) {
+    constexpr int kEach = 128 / static_cast<int>(sizeof(E)), kPer = 4 / static_cast<int>(sizeof(E));
+    const int lane = threadIdx.x & 31;
+    const int n_rows = static_cast<int>(min(int64_t(32), rows - r0)), n = static_cast<int>(min(int64_t(kEach), cols - c0));
+    if (n_rows <= 0 || n <= 0) return;
+    E* base = out + r0 * ld + c0;
+    if (wide && n == kEach) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + lane / 8, w = lane % 8 * 4;
+            if (r < n_rows) *reinterpret_cast<uint4*>(base + r * ld + w * kPer) = *reinterpret_cast<const uint4*>(turn + r * kTurnWords + w);
+        }
+    } else if (kPer == 1 || (pairs && n % 2 == 0)) {
+        if (lane * kPer < n)
+            for (int r = 0; r < n_rows; ++r) *reinterpret_cast<float*>(base + r * ld + lane * kPer) = turn[r * kTurnWords + lane];
+    } else {
+        for (int r = 0; r < n_rows; ++r) {
+            const E* from = reinterpret_cast<const E*>(turn + r * kTurnWords);
+            if (lane < n) base[r * ld + lane] = from[lane];
+            if (lane + 32 < n) base[r * ld + lane + 32] = from[lane + 32];
+        }
+    }
+}
+
 template <int BN> struct ProductShape {
     static constexpr int kABytes = 128 * kBlockK * 2, kBBytes = BN / 2 * kBlockK * 2, kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = BN == 256 ? 6 : (BN == 128 ? 8 : 10);
-    static constexpr int kSmem = 1024 + kStages * kStageBytes + (2 * kStages + 4) * 8 + 16;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpilogueWarps * kTurnBytes + (2 * kStages + 4) * 8 + 16;
 };
 
 // ---- activations --------------------------------------------------------------------------------
@@ -76,21 +113,6 @@ template <int ACT> __device__ __forceinline__ float act_slope(float g) {
 template <int ACT> __device__ __forceinline__ void gate32(float (&g)[32], const float (&u)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) g[i] = act<ACT>(g[i]) * u[i];
-}
-
-// ---- stores -------------------------------------------------------------------------------------
-
-// 32 values of one row from column c0 on; `n` columns exist.
-template <typename T> __device__ __forceinline__ void store32(T* row, int64_t c0, int64_t n, bool wide, const float (&x)[32]) {
-    constexpr int V = Word<T>::kN;
-    if (wide && c0 + 32 <= n) {
-#pragma unroll
-        for (int i = 0; i < 32 / V; ++i) reinterpret_cast<uint4*>(row + c0)[i] = Word<T>::pack(x + i * V);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (c0 + i < n) row[c0 + i] = from_f32<T>(x[i]);
-    }
 }
 
 struct ProductTile {
@@ -128,7 +150,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     constexpr int kBlockBytes = 64 * kBlockK * 2;   // 64 rows of 128 bytes
     extern __shared__ unsigned char raw[];
     unsigned char* smem = raw + (1024 - smem_u32(raw) % 1024) % 1024;
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStageBytes);
+    float* turns = reinterpret_cast<float*>(smem + S::kStages * S::kStageBytes);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStageBytes + kEpilogueWarps * kTurnBytes);
     uint64_t* empty = full + S::kStages;
     uint64_t* acc_full = empty + S::kStages;   // [2]
     uint64_t* acc_empty = acc_full + 2;        // [2], the leader's are used
@@ -226,6 +249,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     } else if (warp >= 4) {
         // ---------------------------------------------------------------- epilogue: one row a thread
         const int quarter = warp & 3;
+        float* turn = turns + (warp - 4) * (kTurnBytes / 4);
         int64_t n = 0;
         for (int64_t i = cluster; i < tiles; i += clusters, ++n) {
             const ProductTile t = tile_at(p, i);
@@ -233,21 +257,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
             if (!__all_sync(~0u, mbar_wait_live(&acc_full[acc], static_cast<uint32_t>(n >> 1) & 1, dead))) break;  // a warp leaves as one
             tc_fence_after_sync();
             const uint32_t base = tmem + acc * 256 + (static_cast<uint32_t>(quarter * 32) << 16);
-            const int in_tile = static_cast<int>(rank) * 128 + quarter * 32 + lane;
+            const int in_tile = static_cast<int>(rank) * 128 + quarter * 32;   // first row of this warp
             if constexpr (P == kForward) {
-                const int64_t r = t.row * 256 + in_tile;
+                const int64_t r0 = t.row * 256 + in_tile;
+                constexpr int kStep = BN / 2 < 64 ? BN / 2 : 64;
 #pragma unroll 1
-                for (int c = 0; c < BN / 2; c += 32) {
-                    float g[32], u[32];
-                    tmem_ld32(base + c, g);
-                    tmem_ld32(base + BN / 2 + c, u);
-                    tmem_ld32_wait(g);
-                    tmem_ld32_wait(u);
-                    const int64_t c0 = t.col * (BN / 2) + c;
-                    if (r < p.rows && c0 < p.cols) {
+                for (int c = 0; c < BN / 2; c += kStep) {
+                    uint4 h[kStep / 8];
+#pragma unroll
+                    for (int half = 0; half < kStep / 32; ++half) {
+                        float g[32], u[32];
+                        tmem_ld32(base + c + half * 32, g);
+                        tmem_ld32(base + BN / 2 + c + half * 32, u);
+                        tmem_ld32_wait(g);
+                        tmem_ld32_wait(u);
                         if (p.preact != nullptr) {
-                            store32<float>(p.preact + r * p.cols, c0, p.cols, p.preact_wide, g);
-                            store32<float>(p.preact + (p.rows + r) * p.cols, c0, p.cols, p.preact_wide, u);
+                            const int64_t c0 = t.col * (BN / 2) + c + half * 32;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<float>::pack(g + 4 * e));
+                            __syncwarp();
+                            turn_out<float>(turn, p.preact, p.cols, r0, p.rows, c0, p.cols, p.preact_wide, false);
+                            __syncwarp();
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<float>::pack(u + 4 * e));
+                            __syncwarp();
+                            turn_out<float>(turn, p.preact + p.rows * p.cols, p.cols, r0, p.rows, c0, p.cols, p.preact_wide, false);
+                            __syncwarp();
                         }
                         switch (p.act) {
                             case BZ_ACT_SILU: gate32<BZ_ACT_SILU>(g, u); break;
@@ -255,29 +290,47 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
                             case BZ_ACT_GELU: gate32<BZ_ACT_GELU>(g, u); break;
                             default: gate32<BZ_ACT_RELU>(g, u); break;
                         }
-                        store32<T>(static_cast<T*>(p.out) + r * p.ld_out, c0, p.cols, p.wide, g);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) h[half * 4 + e] = Word<T>::pack(g + 8 * e);
                     }
+#pragma unroll
+                    for (int e = 0; e < kStep / 8; ++e) turn_in(turn, 4 * e, h[e]);
+                    __syncwarp();
+                    const int64_t c0 = t.col * (BN / 2) + c;
+                    turn_out<T>(turn, static_cast<T*>(p.out), p.ld_out, r0, p.rows, c0, min(p.cols, c0 + kStep), p.wide, p.pairs);
+                    __syncwarp();
                 }
             } else {
                 const int64_t half_tiles = P == kWeight ? p.row_tiles / 2 : 0;
                 const int half = P == kWeight && t.row >= half_tiles;
-                const int64_t r = (t.row - half * half_tiles) * 256 + in_tile;
+                const int64_t r0 = (t.row - half * half_tiles) * 256 + in_tile;
                 void* out = half ? p.out2 : p.out;
+                const bool f32 = p.out_f32 || p.splits > 1;
 #pragma unroll 1
-                for (int c = 0; c < BN; c += 32) {
-                    float x[32];
-                    tmem_ld32(base + c, x);
-                    tmem_ld32_wait(x);
-                    const int64_t c0 = t.col * BN + c;
-                    if (p.splits > 1) {
-                        float* dst = p.partial + (i * 256 + in_tile) * BN + c;
+                for (int c = 0; c < BN; c += 64) {
+                    float x[2][32];
+                    tmem_ld32(base + c, x[0]);
+                    tmem_ld32(base + c + 32, x[1]);
+                    tmem_ld32_wait(x[0]);
+                    tmem_ld32_wait(x[1]);
+                    if (f32) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) reinterpret_cast<uint4*>(dst)[e] = Word<float>::pack(x + 4 * e);
-                    } else if (r < p.rows && c0 < p.cols) {
-                        if (p.out_f32)
-                            store32<float>(static_cast<float*>(out) + r * p.ld_out, c0, p.cols, p.wide, x);
-                        else
-                            store32<T>(static_cast<T*>(out) + r * p.ld_out, c0, p.cols, p.wide, x);
+                        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<float>::pack(x[k] + 4 * e));
+                            __syncwarp();
+                            if (p.splits > 1)
+                                turn_out<float>(turn, p.partial + i * 256 * BN, BN, in_tile, 256, c + k * 32, BN, true, false);
+                            else
+                                turn_out<float>(turn, static_cast<float*>(out), p.ld_out, r0, p.rows, t.col * BN + c + k * 32, p.cols, p.wide, false);
+                            __syncwarp();
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<T>::pack(x[e / 4] + e % 4 * 8));
+                        __syncwarp();
+                        turn_out<T>(turn, static_cast<T*>(out), p.ld_out, r0, p.rows, t.col * BN + c, p.cols, p.wide, p.pairs);
+                        __syncwarp();
                     }
                 }
             }
