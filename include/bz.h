@@ -521,7 +521,7 @@ uint64_t bz_kernel_launch_count(void);
  *   k == 0 gives h = 0 (empty sums); m == 0 or n == 0 is a successful no-op.
  *   workspace  device, bz_glu_workspace_bytes(m, n, k, dtype, 0) bytes, 256-byte aligned; the bytes are 0
  *           and NULL will do where x and the weights are 16-byte aligned with leading dimensions that are
- *           multiples of 8 (other operands are laid out there first).
+ *           multiples of 8 (other operands are laid out there first), and up to 32 rows.
  * m, n, k up to 2^31 - 512 each.  The tensor-core kernels bound every wait; one that runs out stops the
  * kernel early with incomplete outputs and counts in bz_pipeline_timeouts().
  */

@@ -24,6 +24,7 @@ STATUS_RECOMPUTED, STATUS_STOPPED_EARLY = 1, 2
 F32, F16, BF16 = 0, 1, 2
 ACT_SILU, ACT_GELU_TANH, ACT_GELU, ACT_RELU = range(4)
 MAX_DISTANCE, MAX_TOP = 2048, 1024
+GLU_FEW = 32                # up to so many rows bz_glu needs no workspace
 PATH_NONE, PATH_STAGED, PATH_REGISTERS, PATH_GENERIC, PATH_TENSOR, PATH_FP32, PATH_FP32_FUSED, PATH_FP64 = range(8)
 
 
@@ -171,7 +172,8 @@ def _check(status: int, what: str):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # torch.cuda.current_stream().cuda_stream without building the stream object (3.2 -> 0.3 us a call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dev(t: torch.Tensor, dtype, name: str) -> int:
@@ -606,6 +608,7 @@ def vote_bulyan(replicas: torch.Tensor, c: int, voted: torch.Tensor | None = Non
 # ------------------------------------------------------------------------------------- a worker's step
 
 _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+_Strides = ctypes.c_int64 * 3
 _ACTS = {"silu": ACT_SILU, "gelu_tanh": ACT_GELU_TANH, "gelu": ACT_GELU, "relu": ACT_RELU}
 
 
@@ -616,16 +619,22 @@ def _dtype(t: torch.Tensor, name: str) -> int:
 
 
 def _matrix(t: torch.Tensor, name: str):
-    """_matrix(), and rows that overlap (an expanded tensor's) are refused: there is no leading dimension for them."""
-    f, d, ld = _rows(t, name)
-    if f > 1 and t.stride(0) < d:
+    """_rows(), and rows that overlap (an expanded tensor's) are refused: there is no leading dimension for them."""
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix" % name)
+    (f, d), (ld, one) = t.shape, t.stride()
+    if d > 1 and one != 1:
+        raise ValueError("%s must have unit stride along its rows" % name)
+    if f <= 1:
+        return f, d, d
+    if ld < d:
         raise ValueError("%s has rows that overlap: make it contiguous" % name)
     return f, d, ld
 
 
 def _shaped(t: torch.Tensor, shape, dtype, name: str) -> int:
     """Address of a tensor of exactly this shape and type (strides are the caller's business)."""
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s must be %s" % (name, "".join("[%d]" % n for n in shape)))
     return _dev(t, dtype, name)
 
@@ -648,29 +657,22 @@ def _act(name: str) -> int:
 def _like_matrix(t: torch.Tensor) -> torch.Tensor:
     """A new tensor of t's shape whose rows are as far apart as t's: the kernels' wide loads and stores need rows that
     sit alike relative to 16-byte boundaries."""
-    ld = t.stride(-2) if t.dim() > 1 and t.shape[-2] > 1 else t.shape[-1]
-    if ld <= t.shape[-1] or ld > 2 * t.shape[-1]:
-        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
-    return torch.empty(t.shape[:-1] + (ld,), dtype=t.dtype, device=t.device)[..., :t.shape[-1]]
+    if t.is_contiguous():
+        return torch.empty_like(t)
+    n, ld = t.shape[-1], t.stride(-2)
+    if t.shape[-2] <= 1 or ld <= n or ld > 2 * n:
+        return t.new_empty(t.shape)
+    return t.new_empty(t.shape[:-1] + (ld,))[..., :n]
 
 
 def _glu_operands(x, w_gate, w_up):
     m, k, ld_x = _matrix(x, "x")
     n, k2, ld_w = _matrix(w_gate, "w_gate")
-    if k2 != k or tuple(w_up.shape) != (n, k):
+    if k2 != k or w_up.shape != w_gate.shape:
         raise ValueError("w_gate and w_up must both be [n][%d]" % k)
-    if _matrix(w_up, "w_up")[2] != ld_w:
+    if w_up.stride() != w_gate.stride() and _matrix(w_up, "w_up")[2] != ld_w:
         raise ValueError("w_gate and w_up must have the same leading dimension")
     return m, n, k, ld_x, ld_w
-
-
-def _glu_workspace(m, n, k, dtype, backward, operands, lds, workspace, device):
-    if workspace is not None:
-        return workspace.data_ptr(), workspace.numel()
-    if not backward and not any(ld % 8 for ld in lds) and not any(p % 16 for p in operands):
-        return None, 0
-    ws = torch.empty(max(256, lib().bz_glu_workspace_bytes(m, n, k, dtype, backward)), dtype=torch.uint8, device=device)
-    return ws.data_ptr(), ws.numel()
 
 
 def glu_workspace_bytes(m: int, n: int, k: int, dtype=torch.bfloat16, backward: bool = False) -> int:
@@ -684,11 +686,18 @@ def glu(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "s
     m, n, k, ld_x, ld_w = _glu_operands(x, w_gate, w_up)
     dt = _dtype(x, "x")
     if h is None:
-        h = torch.empty((m, n), dtype=x.dtype, device=x.device)
-    px, pg, pu = _dev(x, x.dtype, "x"), _dev(w_gate, x.dtype, "w_gate"), _dev(w_up, x.dtype, "w_up")
-    ws, ws_bytes = _glu_workspace(m, n, k, dt, 0, (px, pg, pu), (ld_x, ld_w), workspace, x.device)
-    st = lib().bz_glu(px, ld_x, pg, pu, ld_w, m, n, k, dt, _act(act), _shaped(h, (m, n), x.dtype, "h"), _matrix(h, "h")[2],
-                      _packed(preact, (2, m, n), torch.float32, "preact"), ws, ws_bytes, _stream())
+        h, ld_h = x.new_empty((m, n)), n
+        ph = h.data_ptr()
+    else:
+        ph, ld_h = _shaped(h, (m, n), x.dtype, "h"), _matrix(h, "h")[2]
+    px, pg, pu = x.data_ptr(), _dev(w_gate, x.dtype, "w_gate"), _dev(w_up, x.dtype, "w_up")
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+    elif m > GLU_FEW and ((ld_x | ld_w) & 7 or (px | pg | pu) & 15):
+        workspace = torch.empty(max(256, lib().bz_glu_workspace_bytes(m, n, k, dt, 0)), dtype=torch.uint8, device=x.device)
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+    st = lib().bz_glu(px, ld_x, pg, pu, ld_w, m, n, k, dt, _act(act), ph, ld_h, _packed(preact, (2, m, n), torch.float32, "preact"), ws, ws_bytes, _stream())
     _check(st, "bz_glu")
     return h
 
@@ -701,22 +710,22 @@ def glu_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, prea
     m, n, k, ld_x, ld_w = _glu_operands(x, w_gate, w_up)
     dt = _dtype(x, "x")
     if dx is None:
-        dx = torch.empty((m, k), dtype=x.dtype, device=x.device)
+        dx = x.new_empty((m, k))
     if (dw_gate is None) != (dw_up is None):
         raise ValueError("give both dw_gate and dw_up, or neither")
     if dw_gate is None:
-        dw_gate = torch.empty((n, k), dtype=x.dtype, device=x.device)
-        dw_up = torch.empty((n, k), dtype=x.dtype, device=x.device)
+        dw_gate, dw_up = x.new_empty((n, k)), x.new_empty((n, k))
     px, pg, pu = _dev(x, x.dtype, "x"), _dev(w_gate, x.dtype, "w_gate"), _dev(w_up, x.dtype, "w_up")
     pdg, pdu = _shaped(dw_gate, (n, k), dw_gate.dtype, "dw_gate"), _shaped(dw_up, (n, k), dw_gate.dtype, "dw_up")
     ld_dw = _matrix(dw_gate, "dw_gate")[2]
     if _matrix(dw_up, "dw_up")[2] != ld_dw:
         raise ValueError("dw_gate and dw_up must have the same leading dimension")
-    ws, ws_bytes = _glu_workspace(m, n, k, dt, 1, (), (), workspace, x.device)
+    if workspace is None:
+        workspace = torch.empty(lib().bz_glu_workspace_bytes(m, n, k, dt, 1), dtype=torch.uint8, device=x.device)
     st = lib().bz_glu_backward(px, ld_x, pg, pu, ld_w, _packed(preact, (2, m, n), torch.float32, "preact"),
                                _shaped(dh, (m, n), x.dtype, "dh"), _matrix(dh, "dh")[2], m, n, k, dt, _act(act),
                                _shaped(dx, (m, k), x.dtype, "dx"), _matrix(dx, "dx")[2], pdg, pdu, ld_dw, _dtype(dw_gate, "dw_gate"),
-                               ws, ws_bytes, _stream())
+                               workspace.data_ptr(), workspace.numel(), _stream())
     _check(st, "bz_glu_backward")
     return dx, dw_gate, dw_up
 
@@ -724,7 +733,7 @@ def glu_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, prea
 def _strides(t: torch.Tensor, name: str):
     if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
         raise ValueError("%s must be [b][h][tq][tk] with unit stride along tk" % name)
-    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+    return _Strides(*t.stride()[:3])
 
 
 def _bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start):
@@ -744,7 +753,7 @@ def bias_softmax(scores: torch.Tensor, table: torch.Tensor, max_distance: int = 
     if probs is None:
         probs = _like_matrix(scores)
     if stats is None:
-        stats = torch.empty(scores.shape[:3] + (2,), dtype=torch.float32, device=scores.device)
+        stats = table.new_empty(scores.shape[:3] + (2,))
     st = lib().bz_bias_softmax(scores.data_ptr(), strides, _dtype(scores, "scores"), *scores.shape,
                                *_bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start),
                                _shaped(probs, scores.shape, scores.dtype, "probs"), _strides(probs, "probs"),
@@ -794,9 +803,9 @@ def distill(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, te
     dt = _dtype(logits, "logits")
     grad = dloss is not None or dlogits is not None
     if loss is None:
-        loss = torch.empty(m, dtype=torch.float32, device=logits.device)
+        loss = teacher.new_empty(m)
     if stats is None:
-        stats = torch.empty((m, 2), dtype=torch.float32, device=logits.device)
+        stats = teacher.new_empty((m, 2))
     if grad and dlogits is None:
         dlogits = _like_matrix(logits)
     st = lib().bz_distill(logits.data_ptr(), ld, dt, m, v, *_teacher(logits, teacher, index), float(temperature),

@@ -1,11 +1,11 @@
 // Gated feed-forward block and its gradient: host side, the pass between the products, and operands laid out on the way in.
-#include "glu_product.cuh"
+#include <atomic>
+
+#include "glu_few.cuh"
 
 namespace bz {
 
 namespace {
-
-__device__ unsigned int g_timeouts = 0;
 
 constexpr int kClusters = kNumSMs / 2;
 constexpr size_t kPartialBytes = static_cast<size_t>(kClusters) * kRowTile * 256 * sizeof(float);  // one tile a cluster
@@ -115,12 +115,18 @@ template <typename T, GluProduct P, int BN>
 int launch_product(const CUtensorMap& a, const CUtensorMap& b0, const CUtensorMap& b1, const ProductParams& p, cudaStream_t s) {
     auto kern = glu_product_kernel<T, P, BN>;
     constexpr int smem = ProductShape<BN>::kSmem;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    // the attribute stays with the kernel: set once per device (bits of the first 64 devices)
+    static std::atomic<uint64_t> set{0};
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return cuda_failed(e);
-    unsigned int* timeouts = nullptr;
-    if ((e = cudaGetSymbolAddress(reinterpret_cast<void**>(&timeouts), g_timeouts)) != cudaSuccess) return cuda_failed(e);
+    const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+    if (!(set.load(std::memory_order_relaxed) & bit)) {
+        if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return cuda_failed(e);
+        set.fetch_or(bit, std::memory_order_relaxed);
+    }
     const int64_t tiles = p.row_tiles * p.col_tiles * p.splits;
-    kern<<<static_cast<unsigned>(2 * (tiles < kClusters ? tiles : kClusters)), kProductThreads, smem, s>>>(a, b0, b1, p, timeouts);
+    kern<<<static_cast<unsigned>(2 * (tiles < kClusters ? tiles : kClusters)), kProductThreads, smem, s>>>(a, b0, b1, p);
     note_launch();
     const int st = check_launch();
     if (st != BZ_OK || p.splits == 1) return st;
@@ -146,6 +152,21 @@ int zero(void* p, int64_t ld, int64_t rows, int64_t n, int bytes, cudaStream_t s
 bool pair_rows(const void* p, int64_t ld, int64_t rows) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0 && (rows <= 1 || ld % 2 == 0); }
 bool wide_rows(const void* p, int64_t ld, int64_t rows, int bytes) { return aligned16(p) && (rows <= 1 || ld * bytes % 16 == 0); }
 
+template <typename T, int NT> int launch_few(const FewParams& p, bool wide, cudaStream_t s) {
+    const unsigned grid = static_cast<unsigned>(ceil_div(p.n, kFewUnits));
+    if (wide)
+        glu_few_kernel<T, NT, true><<<grid, 32 * kFewWarps, 0, s>>>(p);
+    else
+        glu_few_kernel<T, NT, false><<<grid, 32 * kFewWarps, 0, s>>>(p);
+    note_launch();
+    return check_launch();
+}
+template <typename T> int few(const FewParams& p, bool wide, cudaStream_t s) {
+    if (p.m <= 8) return launch_few<T, 1>(p, wide, s);
+    if (p.m <= 16) return launch_few<T, 2>(p, wide, s);
+    return launch_few<T, 4>(p, wide, s);
+}
+
 template <typename T>
 int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, int64_t m, int64_t n, int64_t k, int act, void* h,
             int64_t ld_h, float* preact, char* ws, cudaStream_t s) {
@@ -153,6 +174,11 @@ int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t
     if (k == 0) {
         if (preact != nullptr && (st = zero(preact, n, 2 * m, n, 4, s)) != BZ_OK) return st;
         return zero(h, ld_h, m, n, 2, s);
+    }
+    if (m <= kFewMost) {
+        const FewParams p{x, wg, wu, ld_x, ld_w, n, k, static_cast<int>(m), act, h, ld_h, preact};
+        const bool wide = laid_out(x, ld_x, m) && laid_out(wg, ld_w, n) && laid_out(wu, ld_w, n);
+        return few<T>(p, wide, s);
     }
     Operand ox, og, ou;
     if ((st = lay_out(x, ld_x, m, k, ws, ox, s)) != BZ_OK || (st = lay_out(wg, ld_w, n, k, ws, og, s)) != BZ_OK ||
@@ -245,7 +271,7 @@ int check(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t l
 }  // namespace
 
 int glu_timeouts(unsigned int* count) {
-    const cudaError_t e = cudaMemcpyFromSymbol(count, g_timeouts, sizeof(unsigned int));
+    const cudaError_t e = cudaMemcpyFromSymbol(count, g_glu_timeouts, sizeof(unsigned int));
     return e == cudaSuccess ? BZ_OK : cuda_failed(e);
 }
 
@@ -266,7 +292,7 @@ extern "C" int bz_glu(const void* x, int64_t ld_x, const void* w_gate, const voi
     if (st != BZ_OK) return st;
     if (m == 0 || n == 0) return BZ_OK;
     if (h == nullptr || (m > 1 && ld_h < n) || (reinterpret_cast<uintptr_t>(h) & 1) || !aligned16(preact)) return BZ_ERR_INVALID_ARG;
-    if (!(laid_out(x, ld_x, m) && laid_out(w_gate, ld_w, n) && laid_out(w_up, ld_w, n)) && k > 0 &&
+    if (m > kFewMost && !(laid_out(x, ld_x, m) && laid_out(w_gate, ld_w, n) && laid_out(w_up, ld_w, n)) && k > 0 &&
         (workspace == nullptr || !aligned256(workspace) || workspace_bytes < bz_glu_workspace_bytes(m, n, k, dtype, 0)))
         return BZ_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -26,6 +26,8 @@
 
 namespace bz {
 
+static __device__ unsigned int g_glu_timeouts = 0;
+
 enum GluProduct { kForward, kInput, kWeight };
 
 constexpr int kRowTile = 256, kBlockK = 64, kEpilogueWarps = 4, kProductThreads = 128 + 32 * kEpilogueWarps;
@@ -71,10 +73,15 @@ __device__ __forceinline__ void turn_out(const float* turn, E* out, int64_t ld, 
             if (r < n_rows) *reinterpret_cast<uint4*>(base + r * ld + w * kPer) = *reinterpret_cast<const uint4*>(turn + r * kTurnWords + w);
         }
     } else if (kPer == 1 || (pairs && n % 2 == 0)) {
-        if (lane * kPer < n)
-            for (int r = 0; r < n_rows; ++r) *reinterpret_cast<float*>(base + r * ld + lane * kPer) = turn[r * kTurnWords + lane];
+        if (lane * kPer < n) {
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r)
+                if (r < n_rows) *reinterpret_cast<float*>(base + r * ld + lane * kPer) = turn[r * kTurnWords + lane];
+        }
     } else {
-        for (int r = 0; r < n_rows; ++r) {
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r) {
+            if (r >= n_rows) break;
             const E* from = reinterpret_cast<const E*>(turn + r * kTurnWords);
             if (lane < n) base[r * ld + lane] = from[lane];
             if (lane + 32 < n) base[r * ld + lane + 32] = from[lane + 32];
@@ -143,7 +150,7 @@ __device__ __forceinline__ void share_of(const ProductParams& p, int64_t all, in
 template <typename T, GluProduct P, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     glu_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b0_map,
-                       const __grid_constant__ CUtensorMap b1_map, const __grid_constant__ ProductParams p, unsigned int* timeouts) {
+                       const __grid_constant__ CUtensorMap b1_map, const __grid_constant__ ProductParams p) {
     using S = ProductShape<BN>;
     constexpr bool kAcrossA = P == kWeight, kAcrossB = P != kForward;
     constexpr uint32_t kIdesc = idesc_16bit(256, BN, sizeof(T) == 2 && !__is_same(T, __half), kAcrossA, kAcrossB);
@@ -342,7 +349,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     __syncwarp();
     __syncthreads();
     if (threadIdx.x == 0 && *dead) {
-        atomicAdd(timeouts, 1u);
+        atomicAdd(&g_glu_timeouts, 1u);
         if (rank == 0)  // shared memory has to outlive the loads in flight, the other CTA's among them
             for (int64_t j = it > S::kStages ? it - S::kStages : 0; j < it; ++j)
                 mbar_wait(&full[j % S::kStages], static_cast<uint32_t>(j / S::kStages) & 1);

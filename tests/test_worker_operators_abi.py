@@ -30,9 +30,9 @@ def test_glu(L):
         assert call(**bad) == bz.ERR_INVALID_ARG, bad
     for bad in (dict(dtype=bz.F32), dict(m=BIG), dict(n=BIG, ld_h=BIG), dict(k=BIG, ld_x=BIG, ld_w=BIG)):
         assert call(**bad) == bz.ERR_UNSUPPORTED, bad
-    need = L.bz_glu_workspace_bytes(4, 6, 9, bz.BF16, 0)
+    need = L.bz_glu_workspace_bytes(40, 6, 9, bz.BF16, 0)
     for ws, size in ((None, BIG), (F, need - 1), (ctypes.c_void_p(264), BIG)):      # operands that have to be laid out first
-        assert call(k=9, ld_x=9, ld_w=9, ws=ws, size=size) == bz.ERR_WORKSPACE
+        assert call(m=40, k=9, ld_x=9, ld_w=9, ws=ws, size=size) == bz.ERR_WORKSPACE
     assert call(m=0) == bz.OK and call(n=0, wg=None, wu=None) == bz.OK
     assert bz.kernel_launch_count() == n0
 
