@@ -1,10 +1,10 @@
 // Softmax of attention scores with a learned relative position bias, and its gradient.
 //
-// Forward: z = scale*s + bias[bucket(j - p)], P = e^(z - M) / S.  One read of the scores, one
-// write of P: bound by memory.  A row is held in registers by G threads (32 elements each), so that the maximum, the
-// sum and the result need no second read; rows longer than the largest group loop twice.  Every thread forms its
-// exponentials relative to its own maximum and one joint reduction of (maximum, sum) pairs follows, instead of one
-// reduction for each.
+// Forward: z = scale*s + bias[bucket(j - p)], P = e^(z - M) / S.  One read of the scores, one write of P: bound by memory.
+// A row lies in the registers of G threads (a warp up to 1024 keys, a CTA of 128 or 512 beyond; 32 elements each), the
+// next row's loads are on their way while this one is worked on, and a warp takes its exponentials relative to its own
+// maximum, so that one exchange of (maximum, sum) pairs a row is all that a CTA's warps need.  Rows beyond 16 384 keys
+// are read twice.
 // The bias depends on j - p alone and is constant from max_distance on, so a CTA keeps the head's values for the
 // 2*max_distance + 1 distances in shared memory (with one word of padding every eight: a lane's eight neighbours
 // and the next lane's eight would otherwise share banks), and slots that lie beyond take one of the two end values.
@@ -56,49 +56,47 @@ __device__ __forceinline__ void build_bias(const BiasForm& f, int head, float* b
         bias[padded(d)] = f.table[bucket_of(f, d - f.distance) * f.h + head];
 }
 
-struct RowRange {
-    int64_t p, end;  // position of the query among the keys; keys [0, end) are seen
+// Keys [0, end) are seen by the query at position p.
+struct Queries {
+    int64_t keys, start;   // this batch entry's
+    __device__ Queries(const BiasForm& f, int ib)
+        : keys(f.k_len != nullptr ? min(f.tk, static_cast<int64_t>(max(f.k_len[ib], 0))) : f.tk), start(f.q_start != nullptr ? f.q_start[ib] : 0) {}
+    __device__ int64_t position(int64_t iq) const { return iq + start; }
+    __device__ int64_t end(const BiasForm& f, int64_t iq) const { return f.causal ? min(keys, max(position(iq) + 1, int64_t(0))) : keys; }
 };
-__device__ __forceinline__ RowRange row_range(const BiasForm& f, int ib, int64_t iq) {
-    int64_t end = f.tk;
-    if (f.k_len != nullptr) end = min(end, static_cast<int64_t>(max(f.k_len[ib], 0)));
-    const int64_t p = iq + (f.q_start != nullptr ? f.q_start[ib] : 0);
-    if (f.causal) end = min(end, max(p + 1, int64_t(0)));
-    return {p, end};
-}
 
-// z[i] = scale*s[i] + bias for the keys j0 + i that are seen, -inf for the others.
+// z[i] = scale*s[i] + bias for the keys j0 + i that are seen, -inf for the others.  rel = j0 - p.
 template <int VEC>
-__device__ __forceinline__ void add_bias(const BiasForm& f, const float* bias, const RowRange& r, int64_t j0, float (&z)[VEC]) {
-    const int64_t rel = j0 - r.p;
+__device__ __forceinline__ void add_bias(const BiasForm& f, const float* bias, int64_t j0, int64_t end, int64_t rel, float (&z)[VEC]) {
     if (rel >= f.distance || rel + VEC - 1 <= -f.distance) {
         const float c = bias[padded(rel > 0 ? 2 * f.distance : 0)];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) z[i] = fmaf(z[i], f.scale, c);
     } else {
+        const int first = static_cast<int>(rel) + f.distance;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const int d = max(-f.distance, min(f.distance, static_cast<int>(rel) + i)) + f.distance;
-            z[i] = fmaf(z[i], f.scale, bias[padded(d)]);
-        }
+        for (int i = 0; i < VEC; ++i) z[i] = fmaf(z[i], f.scale, bias[padded(max(0, min(2 * f.distance, first + i)))]);
     }
-    if (j0 < 0 || j0 + VEC > r.end) {
+    if (j0 < 0 || j0 + VEC > end) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
-            if (j0 + i < 0 || j0 + i >= r.end) z[i] = -INFINITY;
+            if (j0 + i < 0 || j0 + i >= end) z[i] = -INFINITY;
     }
 }
 
-// Joins one value per thread over the G threads of a row.  G > 32: the CTA is the group; `part` holds two sets of
-// warp results used in turn, so one barrier a call suffices.
-template <int G> __device__ __forceinline__ MaxSum group_join(MaxSum v, MaxSum (*part)[16], int turn) {
-    v = warp_join(v);
+template <int G> struct Cta {
+    static constexpr int kThreads = G > 32 ? G : 128;
+    static constexpr int kRows = kThreads / G;    // rows in hand at a time
+};
+
+// Joins one part per warp over the G threads of a row (a CTA when G > 32); every lane passes its warp's part.  `part`
+// holds two sets of warp results used in turn, so one barrier a call suffices.
+template <int G> __device__ __forceinline__ MaxSum group_join(MaxSum v, float c, MaxSum (*part)[16], int turn) {
     if constexpr (G > 32) {
         if ((threadIdx.x & 31) == 0) part[turn & 1][threadIdx.x >> 5] = v;
         __syncthreads();
-        v = part[turn & 1][0];
-#pragma unroll
-        for (int w = 1; w < G / 32; ++w) v = join(v, part[turn & 1][w]);
+        const int lane = threadIdx.x & 31;
+        v = warp_join(lane < G / 32 ? part[turn & 1][lane] : MaxSum{-INFINITY, 0.f}, c);
     }
     return v;
 }
@@ -107,107 +105,160 @@ template <int G> __device__ __forceinline__ float group_sum(float v, float (*par
     if constexpr (G > 32) {
         if ((threadIdx.x & 31) == 0) part[turn & 1][threadIdx.x >> 5] = v;
         __syncthreads();
-        v = part[turn & 1][0];
-#pragma unroll
-        for (int w = 1; w < G / 32; ++w) v += part[turn & 1][w];
+        const int lane = threadIdx.x & 31;
+        v = warp_sum(lane < G / 32 ? part[turn & 1][lane] : 0.f);
     }
     return v;
 }
 
-template <int G> struct Cta {
-    static constexpr int kThreads = G > 32 ? G : 256;
-    static constexpr int kRows = kThreads / G;  // rows in hand at a time
+// A slot as it was loaded: 16 bytes, or one element.
+template <typename T, int VEC> struct Raw {
+    uint4 w;
+    __device__ __forceinline__ void load(const T* row, int64_t j0, int64_t n) {
+        if (j0 >= 0 && j0 + VEC <= n) {
+            w = ld_stream(reinterpret_cast<const uint4*>(row + j0));
+        } else {
+            float x[VEC];
+            load_slot<T, VEC>(row, j0, n, 0.f, x);
+            w = Word<T>::pack(x);
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[VEC]) const { Word<T>::unpack(w, x); }
+};
+template <typename T> struct Raw<T, 1> {
+    T e;
+    __device__ __forceinline__ void load(const T* row, int64_t j0, int64_t n) { e = j0 < n ? row[j0] : from_f32<T>(0.f); }
+    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = to_f32(e); }
 };
 
-// E elements a thread are held in registers; E == 0: the row is read twice.
-template <typename T, int VEC, int G, int E>
-__global__ void __launch_bounds__(Cta<G>::kThreads)
+// SLOTS slots a thread are held in registers, and the next row's are loaded before this row's are used.
+template <typename T, int VEC, int G, int SLOTS>
+__global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
     bias_softmax_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<T> probs, MaxSum* stats) {
     extern __shared__ float bias[];
     __shared__ MaxSum part[2][16];
-    constexpr int kSlots = E / VEC;
     const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta + threadIdx.x / G;
+    const Queries q(f, ib);
+    Raw<T, VEC> raw[SLOTS];
+    auto fetch = [&](int64_t iq) {
+        const T* in = scores.row(ib, ih, iq);
+        const int lead = row_lead<T, VEC>(in), end = static_cast<int>(q.end(f, iq));
+#pragma unroll
+        for (int c = 0; c < SLOTS; ++c) {
+            const int j0 = (c * G + t) * VEC - lead;
+            if (j0 < end) raw[c].load(in, j0, f.tk);
+        }
+    };
+    if (first < f.tq) fetch(first);
+    build_bias(f, ih, bias);
+    __syncthreads();
+    for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
+        const int64_t iq = first + it;
+        if (iq >= f.tq) break;   // G > 32: the whole CTA; otherwise this warp
+        const int64_t p = q.position(iq);
+        const int end = static_cast<int>(q.end(f, iq)), lead = row_lead<T, VEC>(scores.row(ib, ih, iq));
+        float z[SLOTS][VEC];
+        float top = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < SLOTS; ++c) {
+            const int j0 = (c * G + t) * VEC - lead;
+            if (j0 < end) {
+                raw[c].get(z[c]);
+                add_bias<VEC>(f, bias, j0, end, j0 - p, z[c]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) z[c][i] = -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) top = fmaxf(top, z[c][i]);
+        }
+        if (it + Cta<G>::kRows < f.rows_per_cta && iq + Cta<G>::kRows < f.tq) fetch(iq + Cta<G>::kRows);
+        MaxSum v{warp_max(top), 0.f};
+        const Reference own(v.m, kLog2e);
+        if (!own.apart) {
+#pragma unroll
+            for (int c = 0; c < SLOTS; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) z[c][i] = exp2_fast(fmaf(z[c][i], kLog2e, -own.mc));
+        } else {
+#pragma unroll
+            for (int c = 0; c < SLOTS; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) z[c][i] = exp2_fast((z[c][i] - own.m) * kLog2e);
+        }
+#pragma unroll
+        for (int c = 0; c < SLOTS; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v.s += z[c][i];
+        v.s = warp_sum(v.s);
+        const MaxSum all = group_join<G>(v, kLog2e, part, it / Cta<G>::kRows);
+        float norm = all.s == 0.f ? 0.f : 1.f / all.s;
+        if (G > 32 && v.s != 0.f) norm *= exp2_fast(Reference(all.m, kLog2e).of_part(v.m, kLog2e));
+        T* out = probs.row(ib, ih, iq);
+#pragma unroll
+        for (int c = 0; c < SLOTS; ++c) {
+            const int j0 = (c * G + t) * VEC - lead;
+            if (j0 < f.tk) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) z[c][i] *= norm;
+                store_slot<T, VEC>(out, j0, f.tk, z[c]);
+            }
+        }
+        if (t == 0 && stats != nullptr) stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq] = {all.m, all.s / Reference(all.m, kLog2e).left_out(kLog2e)};
+    }
+}
+
+// Rows of any length, read twice.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(512) bias_softmax_long_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<T> probs, MaxSum* stats) {
+    constexpr int G = 512;
+    extern __shared__ float bias[];
+    __shared__ MaxSum part[2][16];
+    const int t = threadIdx.x, ib = blockIdx.z, ih = blockIdx.y;
+    const Queries q(f, ib);
     build_bias(f, ih, bias);
     __syncthreads();
     const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta;
-    for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
-        const int64_t iq = first + it + threadIdx.x / G;
-        if (G > 32 && first + it >= f.tq) break;
-        if (G == 32 && iq >= f.tq) break;
-        const RowRange r = row_range(f, ib, iq);
+    for (int it = 0; it < f.rows_per_cta && first + it < f.tq; ++it) {
+        const int64_t iq = first + it, p = q.position(iq), end = q.end(f, iq);
         const T* in = scores.row(ib, ih, iq);
         T* out = probs.row(ib, ih, iq);
         const int lead = row_lead<T, VEC>(in);
         MaxSum v{-INFINITY, 0.f};
-        if constexpr (E > 0) {
-            float z[kSlots][VEC];
+        for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < end; j0 += G * VEC) {
+            float z[VEC];
+            load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
+            add_bias<VEC>(f, bias, j0, end, j0 - p, z);
+            float m = v.m;
 #pragma unroll
-            for (int c = 0; c < kSlots; ++c) {
-                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
+            for (int i = 0; i < VEC; ++i) m = fmaxf(m, z[i]);
+            const Reference r(m, kLog2e);
+            if (v.s != 0.f) v.s *= exp2_fast(r.of_part(v.m, kLog2e));
+            v.m = m;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) z[c][i] = -INFINITY;
-                if (j0 < r.end) load_slot<T, VEC>(in, j0, f.tk, 0.f, z[c]);
-            }
-#pragma unroll
-            for (int c = 0; c < kSlots; ++c) {
-                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
-                if (j0 < r.end) add_bias<VEC>(f, bias, r, j0, z[c]);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v.m = fmaxf(v.m, z[c][i]);
-            }
-            const float own = finite_or_zero(v.m);
-#pragma unroll
-            for (int c = 0; c < kSlots; ++c)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    z[c][i] = exp_below(z[c][i] - own);
-                    v.s += z[c][i];
-                }
-            const MaxSum all = group_join<G>(v, part, it);
-            const float norm = all.s == 0.f ? 0.f : exp_below(v.m - finite_or_zero(all.m)) / all.s;
-#pragma unroll
-            for (int c = 0; c < kSlots; ++c) {
-                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
-                if (j0 < f.tk) {
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) z[c][i] = j0 < r.end && norm != 0.f ? z[c][i] * norm : 0.f;
-                    store_slot<T, VEC>(out, j0, f.tk, z[c]);
-                }
-            }
-            if (t == 0 && stats != nullptr) stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq] = all;
-        } else {
-            for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < r.end; j0 += G * VEC) {
-                float z[VEC];
-                load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
-                add_bias<VEC>(f, bias, r, j0, z);
-                MaxSum w{-INFINITY, 0.f};
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) w.m = fmaxf(w.m, z[i]);
-                const float own = finite_or_zero(w.m);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) w.s += exp_below(z[i] - own);
-                v = join(v, w);
-            }
-            const MaxSum all = group_join<G>(v, part, it);
-            const float top = finite_or_zero(all.m), norm = all.s == 0.f ? 0.f : 1.f / all.s;
-            for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < f.tk; j0 += G * VEC) {
-                float z[VEC];
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) z[i] = 0.f;
-                if (j0 < r.end && norm != 0.f) {
-                    load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
-                    add_bias<VEC>(f, bias, r, j0, z);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) z[i] = exp_below(z[i] - top) * norm;
-                }
-                store_slot<T, VEC>(out, j0, f.tk, z);
-            }
-            if (t == 0 && stats != nullptr) stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq] = all;
+            for (int i = 0; i < VEC; ++i) v.s += exp2_fast(r.of(z[i], kLog2e));
         }
+        const MaxSum all = group_join<G>(warp_join(v, kLog2e), kLog2e, part, it);
+        const Reference r(all.m, kLog2e);
+        const float norm = all.s == 0.f ? 0.f : 1.f / all.s;
+        for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < f.tk; j0 += G * VEC) {
+            float z[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) z[i] = 0.f;
+            if (j0 < end) {
+                load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
+                add_bias<VEC>(f, bias, j0, end, j0 - p, z);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) z[i] = exp2_fast(r.of(z[i], kLog2e)) * norm;
+            }
+            store_slot<T, VEC>(out, j0, f.tk, z);
+        }
+        if (t == 0 && stats != nullptr) stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq] = {all.m, all.s / Reference(all.m, kLog2e).left_out(kLog2e)};
     }
 }
 
-// One slot of the table's gradient: dz of the keys j0 .. j0 + VEC - 1 (0 where a key is not seen).
+// One slot of the table's gradient: dz of the keys at distances rel .. rel + VEC - 1 (0 where a key is not seen).
 template <int VEC>
 __device__ __forceinline__ void add_diagonals(const BiasForm& f, float* diag, int64_t rel, const float (&dz)[VEC], float& left, float& right) {
     if (rel >= f.distance || rel + VEC - 1 <= -f.distance) {
@@ -219,124 +270,24 @@ __device__ __forceinline__ void add_diagonals(const BiasForm& f, float* diag, in
         else
             left += s;
     } else {
+        const int first = static_cast<int>(rel) + f.distance;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int r = static_cast<int>(rel) + i;
-            if (r >= f.distance)
+            if (first + i >= 2 * f.distance)
                 right += dz[i];
-            else if (r <= -f.distance)
+            else if (first + i <= 0)
                 left += dz[i];
             else
-                diag[padded(r + f.distance)] += dz[i];
+                diag[padded(first + i)] += dz[i];
         }
     }
 }
 
-template <typename T, int VEC, int G, int E>
-__global__ void __launch_bounds__(Cta<G>::kThreads)
-    bias_softmax_backward_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<const T> dprobs,
-                                 const Rows4<T> dscores, const MaxSum* __restrict__ stats, float* __restrict__ partial) {
-    extern __shared__ float bias[];
-    __shared__ float part[2][16];
-    constexpr int kWarps = Cta<G>::kThreads / 32, kSlots = E / VEC;
+// What the rows of a CTA leave for the table.  The two ends of each warp's array take its far sums, then warps join
+// diagonal by diagonal and diagonals by bucket.
+__device__ __forceinline__ void leave_buckets(const BiasForm& f, float* diags, int warps, float left, float right, float* mine) {
     const int span = padded(2 * f.distance) + 1;
-    float* diags = bias + span;
     float* diag = diags + (threadIdx.x >> 5) * span;
-    const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y;
-    build_bias(f, ih, bias);
-    if (partial != nullptr)
-        for (int i = threadIdx.x; i < kWarps * span; i += blockDim.x) diags[i] = 0.f;
-    __syncthreads();
-    float left = 0.f, right = 0.f;
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta;
-    for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
-        const int64_t iq = first + it + threadIdx.x / G;
-        if (G > 32 && first + it >= f.tq) break;
-        if (G == 32 && iq >= f.tq) break;
-        const RowRange r = row_range(f, ib, iq);
-        const T* in = scores.row(ib, ih, iq);
-        const T* up = dprobs.row(ib, ih, iq);
-        T* out = dscores.p != nullptr ? dscores.row(ib, ih, iq) : nullptr;
-        const int lead = row_lead<T, VEC>(in);
-        const MaxSum all = stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq];
-        const bool empty = all.s == 0.f;
-        const float norm = 1.f / all.s;
-        float dot = 0.f;
-        if constexpr (E > 0) {
-            float p[kSlots][VEC], dp[kSlots][VEC];
-#pragma unroll
-            for (int c = 0; c < kSlots; ++c) {
-                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) p[c][i] = dp[c][i] = 0.f;
-                if (j0 < r.end && !empty) {
-                    load_slot<T, VEC>(in, j0, f.tk, 0.f, p[c]);
-                    load_slot<T, VEC>(up, j0, r.end, 0.f, dp[c]);
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < kSlots; ++c) {
-                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
-                if (j0 < r.end && !empty) {
-                    add_bias<VEC>(f, bias, r, j0, p[c]);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        p[c][i] = exp_below(p[c][i] - all.m) * norm;
-                        dot = fmaf(p[c][i], dp[c][i], dot);
-                    }
-                }
-            }
-            dot = group_sum<G>(dot, part, it);
-#pragma unroll
-            for (int c = 0; c < kSlots; ++c) {
-                const int64_t j0 = static_cast<int64_t>(c * G + t) * VEC - lead;
-                if (j0 < f.tk) {
-                    float dz[VEC];
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) dz[i] = j0 + i >= 0 && j0 + i < r.end && !empty ? p[c][i] * (dp[c][i] - dot) : 0.f;
-                    if (partial != nullptr && j0 < r.end) add_diagonals<VEC>(f, diag, j0 - r.p, dz, left, right);
-                    if (out != nullptr) {
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) dz[i] *= f.scale;
-                        store_slot<T, VEC>(out, j0, f.tk, dz);
-                    }
-                }
-            }
-        } else {
-            for (int pass = 0; pass < 2; ++pass) {
-                for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < f.tk; j0 += G * VEC) {
-                    float p[VEC], dp[VEC];
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) p[i] = dp[i] = 0.f;
-                    if (j0 < r.end && !empty) {
-                        load_slot<T, VEC>(in, j0, f.tk, 0.f, p);
-                        load_slot<T, VEC>(up, j0, r.end, 0.f, dp);
-                        add_bias<VEC>(f, bias, r, j0, p);
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) p[i] = exp_below(p[i] - all.m) * norm;
-                    }
-                    if (pass == 0) {
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) dot = fmaf(p[i], dp[i], dot);
-                        continue;
-                    }
-                    float dz[VEC];
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) dz[i] = j0 + i >= 0 && j0 + i < r.end && !empty ? p[i] * (dp[i] - dot) : 0.f;
-                    if (partial != nullptr && j0 < r.end) add_diagonals<VEC>(f, diag, j0 - r.p, dz, left, right);
-                    if (out != nullptr) {
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i) dz[i] *= f.scale;
-                        store_slot<T, VEC>(out, j0, f.tk, dz);
-                    }
-                }
-                if (pass == 0) dot = group_sum<G>(dot, part, it);
-            }
-        }
-        __syncwarp();  // the next row meets this row's diagonals through other lanes
-    }
-    if (partial == nullptr) return;
-    // the two ends of the warp's array take the far sums, then warps join diagonal by diagonal and diagonals by bucket
     left = warp_sum(left);
     right = warp_sum(right);
     if ((threadIdx.x & 31) == 0) {
@@ -346,11 +297,10 @@ __global__ void __launch_bounds__(Cta<G>::kThreads)
     __syncthreads();
     for (int d = threadIdx.x; d <= 2 * f.distance; d += blockDim.x) {
         float s = diags[padded(d)];
-        for (int w = 1; w < kWarps; ++w) s += diags[w * span + padded(d)];
+        for (int w = 1; w < warps; ++w) s += diags[w * span + padded(d)];
         diags[padded(d)] = s;
     }
     __syncthreads();
-    float* mine = partial + ((static_cast<int64_t>(ih) * gridDim.z + ib) * gridDim.x + blockIdx.x) * f.buckets;
     for (int c = threadIdx.x; c < f.buckets; c += blockDim.x) {
         const int k = f.bidirectional && c >= f.nb ? c - f.nb : c;
         const int lo = k < f.exact ? k : f.starts[k - f.exact];
@@ -365,6 +315,158 @@ __global__ void __launch_bounds__(Cta<G>::kThreads)
         }
         mine[c] = s;
     }
+}
+
+// SLOTS slots of scores and of dprobs a thread are held: p in binary32, dprobs as loaded.
+template <typename T, int VEC, int G, int SLOTS>
+__global__ void __launch_bounds__(Cta<G>::kThreads, 640 / Cta<G>::kThreads)
+    bias_softmax_backward_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<const T> dprobs,
+                                 const Rows4<T> dscores, const MaxSum* __restrict__ stats, float* __restrict__ partial) {
+    extern __shared__ float bias[];
+    __shared__ float part[2][16];
+    constexpr int kWarps = Cta<G>::kThreads / 32;
+    const int span = padded(2 * f.distance) + 1;
+    float* diags = bias + span;
+    float* diag = diags + (threadIdx.x >> 5) * span;
+    const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y;
+    const Queries q(f, ib);
+    build_bias(f, ih, bias);
+    if (partial != nullptr)
+        for (int i = threadIdx.x; i < kWarps * span; i += blockDim.x) diags[i] = 0.f;
+    __syncthreads();
+    float left = 0.f, right = 0.f;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta + threadIdx.x / G;
+    for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
+        const int64_t iq = first + it;
+        if (iq >= f.tq) break;
+        const int64_t p0 = q.position(iq);
+        const T* in = scores.row(ib, ih, iq);
+        const T* up = dprobs.row(ib, ih, iq);
+        const int lead = row_lead<T, VEC>(in);
+        const MaxSum all = stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq];
+        const int end = all.s == 0.f ? 0 : static_cast<int>(q.end(f, iq));   // a row without keys: all 0
+        Raw<T, VEC> s[SLOTS], dp[SLOTS];
+#pragma unroll
+        for (int c = 0; c < SLOTS; ++c) {
+            const int j0 = (c * G + t) * VEC - lead;
+            if (j0 < end) {
+                s[c].load(in, j0, f.tk);
+                dp[c].load(up, j0, end);
+            }
+        }
+        const Reference r(all.m, kLog2e);
+        const float norm = 1.f / (all.s * r.left_out(kLog2e));
+        float p[SLOTS][VEC], dot = 0.f;
+#pragma unroll
+        for (int c = 0; c < SLOTS; ++c) {
+            const int j0 = (c * G + t) * VEC - lead;
+            if (j0 < end) {
+                float d[VEC];
+                s[c].get(p[c]);
+                dp[c].get(d);
+                add_bias<VEC>(f, bias, j0, end, j0 - p0, p[c]);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    p[c][i] = exp2_fast(r.of(p[c][i], kLog2e)) * norm;
+                    dot = fmaf(p[c][i], d[i], dot);
+                }
+            }
+        }
+        dot = group_sum<G>(dot, part, it / Cta<G>::kRows);
+        T* out = dscores.p != nullptr ? dscores.row(ib, ih, iq) : nullptr;
+#pragma unroll
+        for (int c = 0; c < SLOTS; ++c) {
+            const int j0 = (c * G + t) * VEC - lead;
+            if (j0 < f.tk) {
+                float dz[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) dz[i] = 0.f;
+                if (j0 < end) {
+                    dp[c].get(dz);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) dz[i] = p[c][i] * (dz[i] - dot);
+                    if (j0 < 0 || j0 + VEC > end) {
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i)
+                            if (j0 + i < 0 || j0 + i >= end) dz[i] = 0.f;   // whatever dot is
+                    }
+                    if (partial != nullptr) add_diagonals<VEC>(f, diag, j0 - p0, dz, left, right);
+                }
+                if (out != nullptr) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) dz[i] *= f.scale;
+                    store_slot<T, VEC>(out, j0, f.tk, dz);
+                }
+            }
+        }
+        __syncwarp();  // the next row meets this row's diagonals through other lanes
+    }
+    if (partial == nullptr) return;
+    leave_buckets(f, diags, kWarps, left, right, partial + ((static_cast<int64_t>(ih) * gridDim.z + ib) * gridDim.x + blockIdx.x) * f.buckets);
+}
+
+// Rows of any length, read twice.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256)
+    bias_softmax_backward_long_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<const T> dprobs,
+                                      const Rows4<T> dscores, const MaxSum* __restrict__ stats, float* __restrict__ partial) {
+    constexpr int G = 256, kWarps = G / 32;
+    extern __shared__ float bias[];
+    __shared__ float part[2][16];
+    const int span = padded(2 * f.distance) + 1;
+    float* diags = bias + span;
+    float* diag = diags + (threadIdx.x >> 5) * span;
+    const int t = threadIdx.x, ib = blockIdx.z, ih = blockIdx.y;
+    const Queries q(f, ib);
+    build_bias(f, ih, bias);
+    if (partial != nullptr)
+        for (int i = threadIdx.x; i < kWarps * span; i += blockDim.x) diags[i] = 0.f;
+    __syncthreads();
+    float left = 0.f, right = 0.f;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta;
+    for (int it = 0; it < f.rows_per_cta && first + it < f.tq; ++it) {
+        const int64_t iq = first + it, p0 = q.position(iq);
+        const T* in = scores.row(ib, ih, iq);
+        const T* up = dprobs.row(ib, ih, iq);
+        T* out = dscores.p != nullptr ? dscores.row(ib, ih, iq) : nullptr;
+        const int lead = row_lead<T, VEC>(in);
+        const MaxSum all = stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq];
+        const int64_t end = all.s == 0.f ? 0 : q.end(f, iq);
+        const Reference r(all.m, kLog2e);
+        const float norm = 1.f / (all.s * r.left_out(kLog2e));
+        float dot = 0.f;
+        for (int pass = 0; pass < 2; ++pass) {
+            for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < (pass ? f.tk : end); j0 += G * VEC) {
+                float p[VEC], dp[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) p[i] = dp[i] = 0.f;
+                if (j0 < end) {
+                    load_slot<T, VEC>(in, j0, f.tk, 0.f, p);
+                    load_slot<T, VEC>(up, j0, end, 0.f, dp);
+                    add_bias<VEC>(f, bias, j0, end, j0 - p0, p);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) p[i] = exp2_fast(r.of(p[i], kLog2e)) * norm;
+                }
+                if (pass == 0) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) dot = fmaf(p[i], dp[i], dot);
+                    continue;
+                }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) p[i] = j0 + i >= 0 && j0 + i < end ? p[i] * (dp[i] - dot) : 0.f;
+                if (partial != nullptr && j0 < end) add_diagonals<VEC>(f, diag, j0 - p0, p, left, right);
+                if (out != nullptr) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) p[i] *= f.scale;
+                    store_slot<T, VEC>(out, j0, f.tk, p);
+                }
+            }
+            if (pass == 0) dot = group_sum<G>(dot, part, it);
+        }
+        __syncwarp();
+    }
+    if (partial == nullptr) return;
+    leave_buckets(f, diags, kWarps, left, right, partial + ((static_cast<int64_t>(ih) * gridDim.z + ib) * gridDim.x + blockIdx.x) * f.buckets);
 }
 
 // dtable[c][head]: the parts of one head added by 32 lanes, then the lanes; one warp a value.
@@ -442,58 +544,78 @@ template <typename K> int allow_smem(K kern, size_t bytes) {
 
 template <typename T> Rows4<T> rows4(T* p, const int64_t* s) { return {p, p ? s[0] : 0, p ? s[1] : 0, p ? s[2] : 0}; }
 
-template <typename T, int VEC, int G, int E>
+template <typename T, int VEC, int G, int SLOTS>
 int launch_forward(BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<T>& out, MaxSum* stats, cudaStream_t s) {
-    f.rows_per_cta = Cta<G>::kRows * 8;
-    while (f.rows_per_cta > Cta<G>::kRows && b * f.h * ((f.tq + f.rows_per_cta - 1) / f.rows_per_cta) < 8 * kNumSMs) f.rows_per_cta /= 2;
+    constexpr bool kLong = SLOTS == 0;
+    constexpr int kRows = Cta<G>::kRows;
+    f.rows_per_cta = kRows * 8;
+    while (f.rows_per_cta > kRows && b * f.h * ((f.tq + f.rows_per_cta - 1) / f.rows_per_cta) < 16 * kNumSMs) f.rows_per_cta /= 2;
     const size_t smem = (2 * f.distance + 2 * f.distance / 8 + 1) * sizeof(float);
     const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
-    bias_softmax_kernel<T, VEC, G, E><<<grid, Cta<G>::kThreads, smem, s>>>(f, in, out, stats);
+    if constexpr (kLong)
+        bias_softmax_long_kernel<T, VEC><<<grid, 512, smem, s>>>(f, in, out, stats);
+    else
+        bias_softmax_kernel<T, VEC, G, SLOTS><<<grid, Cta<G>::kThreads, smem, s>>>(f, in, out, stats);
     note_launch();
     return check_launch();
 }
 
+// `n`: elements from the first slot's begin to the row's end.
 template <typename T, int VEC>
-int dispatch_forward(BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<T>& out, MaxSum* stats, cudaStream_t s) {
-    const int64_t n = f.tk + (VEC > 1 ? VEC - 1 : 0);  // the first slot may begin before the row
-    if (n <= 8 * 32) return launch_forward<T, VEC, 32, 8>(f, b, in, out, stats, s);
-    if (n <= 32 * 32) return launch_forward<T, VEC, 32, 32>(f, b, in, out, stats, s);
-    if (n <= 32 * 128) return launch_forward<T, VEC, 128, 32>(f, b, in, out, stats, s);
-    if (n <= 32 * 512) return launch_forward<T, VEC, 512, 32>(f, b, in, out, stats, s);
+int dispatch_forward(BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in, const Rows4<T>& out, MaxSum* stats, cudaStream_t s) {
+    constexpr int kFew = VEC == 1 ? 8 : 1, kFull = VEC == 1 ? 16 : 4, kMost = kFull * VEC;   // 64 bytes a thread
+    if (n <= kFew * VEC * 32) return launch_forward<T, VEC, 32, kFew>(f, b, in, out, stats, s);
+    if (n <= kMost * 32) return launch_forward<T, VEC, 32, kFull>(f, b, in, out, stats, s);
+    if (n <= kMost * 64) return launch_forward<T, VEC, 64, kFull>(f, b, in, out, stats, s);
+    if (n <= kMost * 128) return launch_forward<T, VEC, 128, kFull>(f, b, in, out, stats, s);
+    if (n <= kMost * 256) return launch_forward<T, VEC, 256, kFull>(f, b, in, out, stats, s);
+    if (n <= kMost * 512) return launch_forward<T, VEC, 512, kFull>(f, b, in, out, stats, s);
     return launch_forward<T, VEC, 512, 0>(f, b, in, out, stats, s);
 }
 
-template <typename T, int VEC, int G, int E>
+template <typename T, int VEC, int G, int SLOTS>
 int launch_backward(const BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out, const MaxSum* stats,
                     float* partial, cudaStream_t s) {
     const size_t span = 2 * f.distance + 2 * f.distance / 8 + 1;
     const size_t smem = span * sizeof(float) * (1 + (partial != nullptr ? Cta<G>::kThreads / 32 : 0));
-    auto kern = bias_softmax_backward_kernel<T, VEC, G, E>;
-    const int st = allow_smem(kern, smem);
-    if (st != BZ_OK) return st;
     const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
-    kern<<<grid, Cta<G>::kThreads, smem, s>>>(f, in, up, out, stats, partial);
+    int st;
+    if constexpr (SLOTS == 0) {
+        if ((st = allow_smem(bias_softmax_backward_long_kernel<T, VEC>, smem)) != BZ_OK) return st;
+        bias_softmax_backward_long_kernel<T, VEC><<<grid, 256, smem, s>>>(f, in, up, out, stats, partial);
+    } else {
+        if ((st = allow_smem(bias_softmax_backward_kernel<T, VEC, G, SLOTS>, smem)) != BZ_OK) return st;
+        bias_softmax_backward_kernel<T, VEC, G, SLOTS><<<grid, Cta<G>::kThreads, smem, s>>>(f, in, up, out, stats, partial);
+    }
     note_launch();
     return check_launch();
 }
 
 template <typename T, int VEC>
-int dispatch_backward(const BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out,
+int dispatch_backward(const BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out,
                       const MaxSum* stats, float* partial, cudaStream_t s) {
-    const int64_t n = f.tk + (VEC > 1 ? VEC - 1 : 0);
-    if (n <= 8 * 32) return launch_backward<T, VEC, 32, 8>(f, b, in, up, out, stats, partial, s);
-    if (n <= 16 * 32) return launch_backward<T, VEC, 32, 16>(f, b, in, up, out, stats, partial, s);
-    if (n <= 16 * 128) return launch_backward<T, VEC, 128, 16>(f, b, in, up, out, stats, partial, s);
-    if (n <= 16 * 256) return launch_backward<T, VEC, 256, 16>(f, b, in, up, out, stats, partial, s);
+    constexpr int kFew = VEC == 1 ? 8 : 1, kFull = VEC == 1 ? 16 : 4, kMost = kFull * VEC;
+    if (n <= kFew * VEC * 32) return launch_backward<T, VEC, 32, kFew>(f, b, in, up, out, stats, partial, s);
+    if (n <= kMost * 32) return launch_backward<T, VEC, 32, kFull>(f, b, in, up, out, stats, partial, s);
+    if (n <= kMost * 64) return launch_backward<T, VEC, 64, kFull>(f, b, in, up, out, stats, partial, s);
+    if (n <= kMost * 128) return launch_backward<T, VEC, 128, kFull>(f, b, in, up, out, stats, partial, s);
+    if (n <= kMost * 256) return launch_backward<T, VEC, 256, kFull>(f, b, in, up, out, stats, partial, s);
     return launch_backward<T, VEC, 256, 0>(f, b, in, up, out, stats, partial, s);
+}
+
+// Elements a row takes up from its first slot on: none before it if every row begins on a 16-byte boundary.
+int64_t row_span(const void* p, const int64_t* strides, int64_t b, int64_t h, int64_t tq, int64_t tk, int bytes) {
+    const int64_t zero[3] = {0, 0, 0};
+    return alike(p, strides, nullptr, zero, b, h, tq, bytes) ? tk : tk + 16 / bytes - 1;
 }
 
 template <typename T>
 int forward(BiasForm& f, int64_t b, const void* scores, const int64_t* ss, void* probs, const int64_t* sp, MaxSum* stats, cudaStream_t s) {
     const auto in = rows4(static_cast<const T*>(scores), ss);
     const auto out = rows4(static_cast<T*>(probs), sp);
-    if (alike(scores, ss, probs, sp, b, f.h, f.tq, sizeof(T))) return dispatch_forward<T, Word<T>::kN>(f, b, in, out, stats, s);
-    return dispatch_forward<T, 1>(f, b, in, out, stats, s);
+    if (alike(scores, ss, probs, sp, b, f.h, f.tq, sizeof(T)))
+        return dispatch_forward<T, Word<T>::kN>(f, row_span(scores, ss, b, f.h, f.tq, f.tk, sizeof(T)), b, in, out, stats, s);
+    return dispatch_forward<T, 1>(f, f.tk, b, in, out, stats, s);
 }
 
 template <typename T>
@@ -503,8 +625,8 @@ int backward(const BiasForm& f, int64_t b, const void* scores, const int64_t* ss
     const auto up = rows4(static_cast<const T*>(dprobs), sd);
     const auto out = rows4(static_cast<T*>(dscores), so);
     if (alike(scores, ss, dprobs, sd, b, f.h, f.tq, sizeof(T)) && (dscores == nullptr || alike(scores, ss, dscores, so, b, f.h, f.tq, sizeof(T))))
-        return dispatch_backward<T, Word<T>::kN>(f, b, in, up, out, stats, partial, s);
-    return dispatch_backward<T, 1>(f, b, in, up, out, stats, partial, s);
+        return dispatch_backward<T, Word<T>::kN>(f, row_span(scores, ss, b, f.h, f.tq, f.tk, sizeof(T)), b, in, up, out, stats, partial, s);
+    return dispatch_backward<T, 1>(f, f.tk, b, in, up, out, stats, partial, s);
 }
 
 }  // namespace

@@ -4,7 +4,7 @@
 // maximum and sum of a row, so the fused call reads the row once, keeps its exponentials in registers (32 elements a
 // thread) and writes the gradient from there: two transfers a logit, bound by memory.  A row that one CTA cannot hold
 // is split over a cluster of up to eight; the CTAs exchange their (maximum, sum) pair through distributed shared
-// memory, one barrier a row.  Beyond that (more than 262 144 logits) the cluster reads the row twice.
+// memory, one barrier a row.  Beyond that (more than 131 072 logits) the cluster reads the row twice.
 // The t entries: one warp forms p while the row's loads are in flight; after the dense part dlogits = dloss*T*q is
 // stored, the threads overwrite the named places, adding up entries that name the same one in their order.  No atomics:
 // the same inputs give the same bits.
@@ -19,7 +19,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kHeld = 32;        // logits a thread keeps in registers
-constexpr int kMaxThreads = 1024;
+constexpr int kMaxThreads = 512, kBestThreads = 256;
 constexpr int kMaxCluster = 8;   // portable cluster size
 
 struct DistillArgs {
@@ -27,14 +27,14 @@ struct DistillArgs {
     const float* teacher;
     const int32_t* index;
     int t;
-    float temperature, scale;    // scale = 1 / T
+    float temperature, c;        // c = log2(e) / T
     const float* dloss;
     float* loss;
-    MaxSum* stats;
+    MaxSum* stats;               // largest logit and the sum of e^((s - that)/T)
 };
 
 struct Entries {  // dynamic shared memory: the teacher's entries of one row
-    float *p, *log_p, *s;  // probability, its logarithm, student logit / T
+    float *p, *log_p, *s;  // probability, its logarithm, student logit
     int* at;               // -1: not kept
 };
 __device__ __forceinline__ Entries entries(float* smem, int t) {
@@ -48,28 +48,28 @@ __device__ __forceinline__ bool teacher_row(const DistillArgs& a, const T* row, 
     float top = -INFINITY;
     for (int k = lane; k < a.t; k += 32) {
         const int at = a.index[i * a.t + k];
-        const float z = a.teacher[i * a.t + k] * a.scale;
+        const float z = a.teacher[i * a.t + k];
         const bool kept = at >= 0 && at < a.v && z != -INFINITY;
         e.at[k] = kept ? at : -1;
         e.log_p[k] = z;
-        e.s[k] = kept && at >= lo && at < hi ? to_f32(row[at]) * a.scale : 0.f;
+        e.s[k] = kept && at >= lo && at < hi ? to_f32(row[at]) : 0.f;
         if (kept) top = fmaxf(top, z);
     }
-    top = finite_or_zero(warp_max(top));
+    const Reference r(warp_max(top), a.c);
     float sum = 0.f;
     bool any = false;
     for (int k = lane; k < a.t; k += 32)
         if (e.at[k] >= 0) {
             any = true;
-            sum += exp_below(e.log_p[k] - top);
+            sum += exp2_fast(r.of(e.log_p[k], a.c));
         }
     sum = warp_sum(sum);
     any = __any_sync(~0u, any);
     const float log_sum = logf(sum), norm = 1.f / sum;
     for (int k = lane; k < a.t; k += 32) {
-        e.log_p[k] = e.log_p[k] - top;
-        e.p[k] = e.at[k] >= 0 ? exp_below(e.log_p[k]) * norm : 0.f;
-        e.log_p[k] -= log_sum;
+        const float y = r.of(e.log_p[k], a.c);
+        e.p[k] = e.at[k] >= 0 ? exp2_fast(y) * norm : 0.f;
+        e.log_p[k] = y * kLn2 - log_sum;
     }
     __syncwarp();
     return any;
@@ -77,12 +77,13 @@ __device__ __forceinline__ bool teacher_row(const DistillArgs& a, const T* row, 
 
 // One warp: the loss of the row from its maximum and sum.
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const Entries& e, const MaxSum& all) {
-    const float top = finite_or_zero(all.m), log_sum = logf(all.s);
+    const Reference r(all.m, a.c);
+    const float log_sum = logf(all.s);
     float sum = 0.f;
     for (int k = threadIdx.x & 31; k < a.t; k += 32) {
         const float p = e.p[k];
         if (p != 0.f) {  // an entry without weight adds nothing, whatever its q
-            const float log_q = e.s[k] == -INFINITY ? -INFINITY : e.s[k] - top - log_sum;
+            const float log_q = e.s[k] == -INFINITY ? -INFINITY : r.of(e.s[k], a.c) * kLn2 - log_sum;
             sum += p * (e.log_p[k] - log_q);
         }
     }
@@ -92,23 +93,34 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const Entries& e
 // All threads: the places of [lo, hi) that the teacher names.
 template <typename T>
 __device__ __forceinline__ void write_entries(const DistillArgs& a, const Entries& e, const MaxSum& all, float g, int64_t lo, int64_t hi, T* out) {
+    const Reference r(all.m, a.c);
     for (int k = threadIdx.x; k < a.t; k += blockDim.x) {
         const int at = e.at[k];
         if (at < 0 || at < lo || at >= hi) continue;   // lo may lie before the row (its first slot's lead)
         float p = 0.f;
         for (int o = 0; o < a.t; ++o) p += e.at[o] == at ? e.p[o] : 0.f;
-        const float q = e.s[k] == -INFINITY ? 0.f : exp_below(e.s[k] - all.m) / all.s;
+        const float q = e.s[k] == -INFINITY ? 0.f : exp2_fast(r.of(e.s[k], a.c)) / all.s;
         out[at] = from_f32<T>(g * (q - p));
     }
 }
 
-// Joins one pair per thread over the CTA.
-__device__ __forceinline__ MaxSum cta_join(MaxSum v, MaxSum* part) {
-    v = warp_join(v);
+// Joins one part per warp (each lane passes its warp's) over the CTA.
+__device__ __forceinline__ MaxSum cta_join(const MaxSum& v, float c, MaxSum* part) {
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
     __syncthreads();
     const int lane = threadIdx.x & 31;
-    return warp_join(lane < (blockDim.x >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f});
+    return warp_join(lane < (blockDim.x >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f}, c);
+}
+
+// x[i] = 2^(exponent of x[i]) relative to r.
+template <int N> __device__ __forceinline__ void exponentials(float (&x)[N], const Reference& r, float c) {
+    if (!r.apart) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = exp2_fast(fmaf(x[k], c, -r.mc));
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = exp2_fast((x[k] - r.m) * c);
+    }
 }
 
 // One cluster a row.  HELD: the row's exponentials stay in registers; otherwise the row is read twice.
@@ -123,20 +135,20 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_const
     const int rank = cluster.block_rank(), ranks = cluster.num_blocks();
     const int64_t i = blockIdx.x / ranks;
     const T* row = logits + i * a.ld;
-    const int lead = row_lead<T, VEC>(row);
-    const int64_t per_cta = static_cast<int64_t>(blockDim.x) * kHeld;          // HELD: elements of one CTA's share
-    const int64_t base = (HELD ? rank * per_cta : static_cast<int64_t>(rank) * blockDim.x * VEC) - lead;
-    const int64_t step = static_cast<int64_t>(blockDim.x) * VEC * (HELD ? 1 : ranks);
+    const int lead = row_lead<T, VEC>(row), n = static_cast<int>(a.v);
+    const int per_cta = blockDim.x * kHeld;          // HELD: elements of one CTA's share
+    const int64_t base = (HELD ? static_cast<int64_t>(rank) * per_cta : static_cast<int64_t>(rank) * blockDim.x * VEC) - lead;
+    const int step = blockDim.x * VEC * (HELD ? 1 : ranks);
     if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // every CTA of the cluster has started
     float x[HELD ? kSlots : 1][VEC];
     MaxSum mine{-INFINITY, 0.f};
+    const int at0 = static_cast<int>(base) + threadIdx.x * VEC;   // HELD: at most 8 * 512 * 32
     if constexpr (HELD) {
 #pragma unroll
         for (int c = 0; c < kSlots; ++c) {
 #pragma unroll
             for (int k = 0; k < VEC; ++k) x[c][k] = -INFINITY;
-            const int64_t j0 = base + c * step + static_cast<int64_t>(threadIdx.x) * VEC;
-            if (j0 < a.v) load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[c]);
+            if (at0 + c * step < n) load_slot<T, VEC>(row, at0 + c * step, n, -INFINITY, x[c]);
         }
     }
     if (threadIdx.x < 32) {
@@ -147,71 +159,69 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_const
 #pragma unroll
         for (int c = 0; c < kSlots; ++c)
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                x[c][k] *= a.scale;
-                mine.m = fmaxf(mine.m, x[c][k]);
-            }
-        const float own = finite_or_zero(mine.m);
+            for (int k = 0; k < VEC; ++k) mine.m = fmaxf(mine.m, x[c][k]);
+        mine.m = warp_max(mine.m);
+        const Reference own(mine.m, a.c);
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c)
+        for (int c = 0; c < kSlots; ++c) {
+            exponentials(x[c], own, a.c);
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                x[c][k] = exp_below(x[c][k] - own);
-                mine.s += x[c][k];
-            }
+            for (int k = 0; k < VEC; ++k) mine.s += x[c][k];
+        }
+        mine.s = warp_sum(mine.s);
     } else {
         for (int64_t j0 = base + static_cast<int64_t>(threadIdx.x) * VEC; j0 < a.v; j0 += step) {
             load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[0]);
-            MaxSum w{-INFINITY, 0.f};
+            float m = mine.m;
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                x[0][k] *= a.scale;
-                w.m = fmaxf(w.m, x[0][k]);
-            }
-            const float own = finite_or_zero(w.m);
+            for (int k = 0; k < VEC; ++k) m = fmaxf(m, x[0][k]);
+            const Reference r(m, a.c);
+            if (mine.s != 0.f) mine.s *= exp2_fast(r.of_part(mine.m, a.c));
+            mine.m = m;
+            exponentials(x[0], r, a.c);
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) w.s += exp_below(x[0][k] - own);
-            mine = join(mine, w);
+            for (int k = 0; k < VEC; ++k) mine.s += x[0][k];
         }
+        mine = warp_join(mine, a.c);
     }
-    MaxSum all = cta_join(mine, part);
+    MaxSum all = cta_join(mine, a.c, part);
     if (ranks > 1) {
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (threadIdx.x < ranks) *cluster.map_shared_rank(&peers[rank], threadIdx.x) = all;
         cluster.sync();
-        all = peers[0];
-        for (int c = 1; c < ranks; ++c) all = join(all, peers[c]);
+        const int lane = threadIdx.x & 31;
+        all = warp_join(lane < ranks ? peers[lane] : MaxSum{-INFINITY, 0.f}, a.c);
     }
     const bool any = s_any != 0;
     if (rank == 0 && threadIdx.x < 32) {
         const float loss = row_loss(a, e, all);
         if (threadIdx.x == 0) {
             if (a.loss != nullptr) a.loss[i] = any ? loss : 0.f;
-            if (a.stats != nullptr) a.stats[i] = all;
+            if (a.stats != nullptr) a.stats[i] = {all.m, all.s / Reference(all.m, a.c).left_out(a.c)};
         }
     }
     if (dlogits == nullptr) return;
     T* out = dlogits + i * a.ld_d;
     const float g = any ? (a.dloss != nullptr ? a.dloss[i] : 1.f) * a.temperature : 0.f;
-    const float top = finite_or_zero(all.m);
-    const float factor = all.s == 0.f || !any ? 0.f : g * (HELD ? exp_below(mine.m - top) : 1.f) / all.s;
+    const Reference r(all.m, a.c);
+    float factor = all.s == 0.f || !any ? 0.f : g / all.s;
     if constexpr (HELD) {
+        factor = mine.s == 0.f ? 0.f : factor * exp2_fast(r.of_part(mine.m, a.c));
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c) {
-            const int64_t j0 = base + c * step + static_cast<int64_t>(threadIdx.x) * VEC;
-            if (j0 < a.v) {
+        for (int c = 0; c < kSlots; ++c)
+            if (at0 + c * step < n) {
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) x[c][k] = any ? x[c][k] * factor : 0.f;
-                store_slot<T, VEC>(out, j0, a.v, x[c]);
+                store_slot<T, VEC>(out, at0 + c * step, n, x[c]);
             }
-        }
         __syncthreads();
         if (any) write_entries(a, e, all, g, base, base + per_cta, out);
     } else {
         for (int64_t j0 = base + static_cast<int64_t>(threadIdx.x) * VEC; j0 < a.v; j0 += step) {
             load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[0]);
+            exponentials(x[0], r, a.c);
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) x[0][k] = any ? exp_below(x[0][k] * a.scale - top) * factor : 0.f;
+            for (int k = 0; k < VEC; ++k) x[0][k] = any ? x[0][k] * factor : 0.f;
             store_slot<T, VEC>(out, j0, a.v, x[0]);
         }
         // the cluster's CTAs share the row slot by slot: the named places wait for all of them
@@ -246,15 +256,18 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(const __grid_cons
     }
     __syncthreads();
     const bool any = s_any != 0;
-    const MaxSum all = a.stats[i];
+    MaxSum all = a.stats[i];
+    const Reference r(all.m, a.c);
+    all.s *= r.left_out(a.c);
     const float g = any ? (a.dloss != nullptr ? a.dloss[i] : 1.f) * a.temperature : 0.f;
-    const float factor = all.s == 0.f ? 0.f : g / all.s, top = finite_or_zero(all.m);
+    const float factor = all.s == 0.f ? 0.f : g / all.s;
 #pragma unroll
     for (int c = 0; c < kSlots; ++c) {
         const int64_t j0 = base + (c * 256 + static_cast<int64_t>(threadIdx.x)) * VEC;
         if (j0 < a.v) {
+            exponentials(x[c], r, a.c);
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) x[c][k] = any ? exp_below(x[c][k] * a.scale - top) * factor : 0.f;
+            for (int k = 0; k < VEC; ++k) x[c][k] = any ? x[c][k] * factor : 0.f;
             store_slot<T, VEC>(out, j0, a.v, x[c]);
         }
     }
@@ -275,7 +288,7 @@ __global__ void distill_empty_kernel(int64_t m, float* loss, MaxSum* stats) {
 template <typename T, int VEC> int launch(const DistillArgs& a, int64_t m, const T* logits, T* dlogits, cudaStream_t s) {
     const int64_t slots = (a.v + (VEC > 1 ? VEC - 1 : 0) + VEC - 1) / VEC, per_thread = kHeld / VEC;
     int ranks = 1;
-    while (ranks < kMaxCluster && (slots + ranks * per_thread - 1) / (ranks * per_thread) > kMaxThreads) ranks *= 2;
+    while (ranks < kMaxCluster && (slots + ranks * per_thread - 1) / (ranks * per_thread) > kBestThreads) ranks *= 2;
     int64_t threads = ((slots + ranks * per_thread - 1) / (ranks * per_thread) + 31) / 32 * 32;
     const bool held = threads <= kMaxThreads;
     if (!held) threads = kMaxThreads;
@@ -347,7 +360,7 @@ extern "C" int bz_distill(const void* logits, int64_t ld, int dtype, int64_t m, 
         note_launch();
         return check_launch();
     }
-    const DistillArgs a{ld, v, ld_d, teacher, index, t, temperature, 1.f / temperature, dloss, loss, reinterpret_cast<MaxSum*>(stats)};
+    const DistillArgs a{ld, v, ld_d, teacher, index, t, temperature, kLog2e / temperature, dloss, loss, reinterpret_cast<MaxSum*>(stats)};
     if (dtype == BZ_F32) return dispatch<float>(a, m, logits, dlogits, false, s);
     if (dtype == BZ_F16) return dispatch<__half>(a, m, logits, dlogits, false, s);
     return dispatch<__nv_bfloat16>(a, m, logits, dlogits, false, s);
@@ -361,7 +374,7 @@ extern "C" int bz_distill_backward(const void* logits, int64_t ld, int dtype, in
     if (m == 0 || v == 0) return BZ_OK;
     if (stats == nullptr || !aligned8(stats) || dlogits == nullptr) return BZ_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const DistillArgs a{ld, v, ld_d, teacher, index, t, temperature, 1.f / temperature, dloss, nullptr, reinterpret_cast<MaxSum*>(const_cast<float*>(stats))};
+    const DistillArgs a{ld, v, ld_d, teacher, index, t, temperature, kLog2e / temperature, dloss, nullptr, reinterpret_cast<MaxSum*>(const_cast<float*>(stats))};
     if (dtype == BZ_F32) return dispatch<float>(a, m, logits, dlogits, true, s);
     if (dtype == BZ_F16) return dispatch<__half>(a, m, logits, dlogits, true, s);
     return dispatch<__nv_bfloat16>(a, m, logits, dlogits, true, s);

@@ -95,26 +95,45 @@ template <typename T, int VEC> __device__ __forceinline__ void store_slot(T* row
     }
 }
 
-// e^x for x = z - maximum <= 0.  The difference is taken before the factor log2(e), so that a row of the type's lowest
-// values neither overflows nor loses its differences.
-__device__ __forceinline__ float exp_below(float x) { return exp2f(x * kLog2e); }
+// 2^x in one instruction (ex2.approx: at most two units in the last place; results below 2^-126 become 0).
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
-// (maximum, sum of e^(z - maximum)) of a part of a row.  An empty part has maximum -inf and sum 0.
+// A part of a row of softmax arguments: (largest z, sum of e^((z - that)/T)).  An empty part is (-inf, 0).
+//
+// With c = log2(e)/T an exponent is one multiply-add, z*c - m*c.  The product m*c is rounded, but everything that is
+// compared or joined uses the same rounded number, so its error cancels.  Where m*c leaves binary32's range although m
+// does not (a row of the type's lowest values), exponents are (z - m)*c instead.
 struct MaxSum {
     float m, s;
 };
-__device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ MaxSum join(const MaxSum& a, const MaxSum& b) {
-    const float m = fmaxf(a.m, b.m), r = finite_or_zero(m);
-    return {m, a.s * exp_below(a.m - r) + b.s * exp_below(b.m - r)};
+// A product that no multiply-add takes in.
+__device__ __forceinline__ float rounded_product(float a, float b) {
+    float y;
+    asm("mul.rn.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
 }
-__device__ __forceinline__ MaxSum warp_join(MaxSum v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const MaxSum w{__shfl_xor_sync(~0u, v.m, o), __shfl_xor_sync(~0u, v.s, o)};
-        v = (threadIdx.x & o) ? join(w, v) : join(v, w);   // both lanes of a pair add in the same order
-    }
-    return v;
+struct Reference {
+    float m, mc;   // a part's largest z (0 for an empty part) and its rounded product with c
+    bool apart;
+    __device__ __forceinline__ Reference(float largest, float c) : m(largest == -INFINITY ? 0.f : largest), mc(rounded_product(m, c)), apart(isinf(mc) && !isinf(m)) {}
+    // exponent of z, which is at most m; z may be -inf
+    __device__ __forceinline__ float of(float z, float c) const { return apart ? (z - m) * c : fmaf(z, c, -mc); }
+    // 2^(what the rounding of m*c left out): sums are kept relative to mc inside a kernel and to m itself outside
+    __device__ __forceinline__ float left_out(float c) const { return apart || isinf(m) ? 1.f : exp2_fast(fmaf(m, c, -mc)); }
+    // exponent of another part's reference: between the two rounded products
+    __device__ __forceinline__ float of_part(float other, float c) const { return apart ? (other - m) * c : rounded_product(other, c) - mc; }
+};
+__device__ __forceinline__ float warp_sum(float v);
+__device__ __forceinline__ float warp_max(float v);
+// The parts of a warp's lanes as one.
+__device__ __forceinline__ MaxSum warp_join(const MaxSum& v, float c) {
+    const float m = warp_max(v.m);
+    const Reference r(m, c);
+    return {m, warp_sum(v.s == 0.f ? 0.f : v.s * exp2_fast(r.of_part(v.m, c)))};
 }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -122,9 +141,9 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 __device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
-    return v;
+    float m;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
 }
 
 }  // namespace bz

@@ -64,7 +64,7 @@ def check(logits, teacher, index, T, dloss, dlogits=None):
     loss, stats, d = bz.distill(logits, teacher, index, T, dloss=dloss, dlogits=dlogits)
     near = lambda got, want, tol: bool(((got.cpu().double() == want) | ((got.cpu().double() - want).abs() <= tol)).all())  # noqa: E731
     assert near(loss, want_loss, TOL * T * T + TOL * want_loss.abs())
-    lse = stats[:, 0].double() + torch.log(stats[:, 1].double())
+    lse = stats[:, 0].double() / T + torch.log(stats[:, 1].double())
     assert near(lse, want_lse, TOL)
     bound = 2 * TOL * size + HALF_UNIT[d.dtype] * want_d.abs() + TINY[d.dtype]
     assert near(d, want_d, bound)
