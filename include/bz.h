@@ -14,7 +14,7 @@
  *     are ordinary process memory.  The caller owns every buffer.  The library never allocates
  *     or frees device memory; scratch space is a caller-provided device workspace whose size
  *     bz_workspace_bytes() reports.  Device state that outlives a call is limited to what is part
- *     of the library image: five counters of expired waits (bz_pipeline_timeouts), the switch of
+ *     of the library image: six counters of expired waits (bz_pipeline_timeouts), the switch of
  *     bz_debug_stall_pipeline and the built-in array of bz_pairdist_static.  None of it
  *     influences a result.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream).  Calls with

@@ -10,6 +10,7 @@
 // the same inputs give the same bits.
 #include <cooperative_groups.h>
 
+#include "umma.cuh"
 #include "worker_common.cuh"
 
 namespace bz {
@@ -17,6 +18,8 @@ namespace bz {
 namespace {
 
 namespace cg = cooperative_groups;
+
+__device__ unsigned int g_timeouts = 0;
 
 constexpr int kHeld = 32;        // logits a thread keeps in registers
 constexpr int kMaxThreads = 512, kBestThreads = 256;
@@ -44,16 +47,29 @@ __device__ __forceinline__ Entries entries(float* smem, int t) {
 // One warp: p of the row's kept entries; the student's logit at each that lies in [lo, hi).  Returns whether any is kept.
 template <typename T>
 __device__ __forceinline__ bool teacher_row(const DistillArgs& a, const T* row, int64_t i, const Entries& e, int64_t lo, int64_t hi) {
+    constexpr int B = 4;   // entries a lane has on their way at a time
     const int lane = threadIdx.x & 31;
     float top = -INFINITY;
-    for (int k = lane; k < a.t; k += 32) {
-        const int at = a.index[i * a.t + k];
-        const float z = a.teacher[i * a.t + k];
-        const bool kept = at >= 0 && at < a.v && z != -INFINITY;
-        e.at[k] = kept ? at : -1;
-        e.log_p[k] = z;
-        e.s[k] = kept && at >= lo && at < hi ? to_f32(row[at]) : 0.f;
-        if (kept) top = fmaxf(top, z);
+    for (int k0 = lane; k0 < a.t; k0 += 32 * B) {
+        int at[B];
+        float z[B], x[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const int k = k0 + 32 * b;
+            at[b] = k < a.t ? __ldg(a.index + i * a.t + k) : -1;
+            z[b] = k < a.t ? __ldg(a.teacher + i * a.t + k) : -INFINITY;
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            if (at[b] < 0 || at[b] >= a.v || z[b] == -INFINITY) at[b] = -1;
+            x[b] = at[b] >= 0 && at[b] >= lo && at[b] < hi ? to_f32(row[at[b]]) : 0.f;
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const int k = k0 + 32 * b;
+            if (k < a.t) e.at[k] = at[b], e.log_p[k] = z[b], e.s[k] = x[b];
+            if (at[b] >= 0) top = fmaxf(top, z[b]);
+        }
     }
     const Reference r(warp_max(top), a.c);
     float sum = 0.f;
@@ -90,18 +106,22 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const Entries& e
     return warp_sum(sum) * (a.temperature * a.temperature);
 }
 
+// The gradient at the place that entry k names.
+__device__ __forceinline__ float entry_value(const DistillArgs& a, const Entries& e, const Reference& r, const MaxSum& all, float g, int k) {
+    const int at = e.at[k];
+    float p = 0.f;
+#pragma unroll 8
+    for (int o = 0; o < a.t; ++o) p += e.at[o] == at ? e.p[o] : 0.f;
+    const float q = e.s[k] == -INFINITY ? 0.f : exp2_fast(r.of(e.s[k], a.c)) / all.s;
+    return g * (q - p);
+}
 // All threads: the places of [lo, hi) that the teacher names.
 template <typename T>
 __device__ __forceinline__ void write_entries(const DistillArgs& a, const Entries& e, const MaxSum& all, float g, int64_t lo, int64_t hi, T* out) {
     const Reference r(all.m, a.c);
-    for (int k = threadIdx.x; k < a.t; k += blockDim.x) {
-        const int at = e.at[k];
-        if (at < 0 || at < lo || at >= hi) continue;   // lo may lie before the row (its first slot's lead)
-        float p = 0.f;
-        for (int o = 0; o < a.t; ++o) p += e.at[o] == at ? e.p[o] : 0.f;
-        const float q = e.s[k] == -INFINITY ? 0.f : exp2_fast(r.of(e.s[k], a.c)) / all.s;
-        out[at] = from_f32<T>(g * (q - p));
-    }
+    for (int k = threadIdx.x; k < a.t; k += blockDim.x)
+        if (e.at[k] >= 0 && e.at[k] >= lo && e.at[k] < hi)   // lo may lie before the row (its first slot's lead)
+            out[e.at[k]] = from_f32<T>(entry_value(a, e, r, all, g, k));
 }
 
 // Joins one part per warp (each lane passes its warp's) over the CTA.
@@ -233,6 +253,199 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_const
     }
 }
 
+// ---- many long rows: one CTA an SM, rows streamed through a ring ---------------------------------
+//
+// A producer thread copies a row's 16-byte words in chunks of 32 KB (cp.async.bulk) into a ring of six, running ahead
+// over rows; 16 warps read a chunk from shared memory, four words a thread.  First pass: each thread's largest logit and
+// sum.  Second pass (gradient): exponentials again from shared memory if the row is at most three chunks long, so that the
+// next row still has half of the ring; longer rows come a second time, out of the L2.  Two further warps take the
+// teacher's side of every other row: p while the row before is worked on, the loss once the CTA has joined its sums,
+// the named places once every warp has stored its part of the gradient - the 16 warps wait for neither.
+// Words that reach over an end of the row are read by the thread that owns them, element by element.
+
+constexpr int kChunkBytes = 32768, kChunkWords = kChunkBytes / 16, kRing = 6, kHoldChunks = kRing / 2;
+constexpr int kWorkers = 512, kTeachers = 2, kStreamThreads = kWorkers + 32 * kTeachers + 32;
+
+__device__ __forceinline__ void named_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kWorkers + 32) : "memory"); }
+__device__ __forceinline__ void named_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kWorkers + 32) : "memory"); }
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes),
+                 "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// The row's words: [begin, end) whole ones, counted from the 16-byte boundary at or before the row.
+template <typename T> struct RowWords {
+    int lead, begin, end, chunks;
+    __device__ __forceinline__ RowWords(const T* row, int64_t v) {
+        constexpr int N = Word<T>::kN;
+        lead = row_lead<T, N>(row);
+        begin = lead != 0;
+        end = static_cast<int>((lead + v) / N);
+        chunks = static_cast<int>(((lead + v + N - 1) / N + kChunkWords - 1) / kChunkWords);
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kStreamThreads, 1) distill_stream_kernel(const __grid_constant__ DistillArgs a, int64_t m, const T* logits, T* dlogits, int hold) {
+    constexpr int N = Word<T>::kN, kMine = kChunkWords / kWorkers;
+    extern __shared__ __align__(128) unsigned char ring[];
+    uint64_t* full = reinterpret_cast<uint64_t*>(ring + kRing * kChunkBytes);
+    uint64_t* empty = full + kRing;
+    // four sets of warp results in turn: a set is written again only after the teacher that read it has met the workers
+    MaxSum(*part)[32] = reinterpret_cast<MaxSum(*)[32]>(empty + kRing);
+    float* entry_room = reinterpret_cast<float*>(part + 4);
+    __shared__ int dead_word, some[4];   // some: whether the row's teacher keeps an entry
+    volatile int* dead = &dead_word;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        dead_word = 0;
+        for (int s = 0; s < kRing; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], kWorkers / 32);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    const bool grad = dlogits != nullptr;
+    const int passes = grad && !hold ? 2 : 1;
+    int64_t seq = 0;   // chunks so far
+    if (warp == kWorkers / 32 + kTeachers) {
+        // ---------------------------------------------------------------- loads
+        if (lane == 0) {
+            bool alive = true;
+            for (int64_t i = blockIdx.x; i < m && alive; i += gridDim.x) {
+                const T* row = logits + i * a.ld;
+                const RowWords<T> w(row, a.v);
+                for (int c = 0; c < passes * w.chunks; ++c, ++seq) {
+                    const int s = static_cast<int>(seq % kRing);
+                    if (seq >= kRing && !mbar_wait_live(&empty[s], static_cast<uint32_t>(seq / kRing - 1) & 1, dead)) {
+                        alive = false;
+                        break;
+                    }
+                    const int base = (c < w.chunks ? c : c - w.chunks) * kChunkWords;
+                    const int from = max(base, w.begin), to = min(base + kChunkWords, w.end);
+                    if (from < to) {
+                        const uint32_t bytes = static_cast<uint32_t>(to - from) * 16;
+                        mbar_expect_tx(&full[s], bytes);
+                        bulk_load(ring + s * kChunkBytes + (from - base) * 16, row - w.lead + static_cast<int64_t>(from) * N, bytes, &full[s]);
+                    } else {
+                        mbar_arrive(&full[s]);
+                    }
+                }
+            }
+        }
+    } else if (warp >= kWorkers / 32) {
+        // ---------------------------------------------------------------- the teacher's side of every other row
+        const int which = warp - kWorkers / 32;
+        const Entries e = entries(entry_room + which * 4 * a.t, a.t);
+        int64_t r = which;
+        for (int64_t i = blockIdx.x + which * static_cast<int64_t>(gridDim.x); i < m; i += kTeachers * static_cast<int64_t>(gridDim.x), r += kTeachers) {
+            const T* row = logits + i * a.ld;
+            const bool any = teacher_row(a, row, i, e, 0, a.v);
+            const float d = grad && a.dloss != nullptr ? a.dloss[i] : 1.f;
+            if (lane == 0) some[r & 3] = any;
+            named_sync(1 + which);
+            const MaxSum all = warp_join(lane < kWorkers / 32 ? part[r & 3][lane] : MaxSum{-INFINITY, 0.f}, a.c);
+            const float loss = row_loss(a, e, all);
+            if (lane == 0) {
+                if (a.loss != nullptr) a.loss[i] = any ? loss : 0.f;
+                if (a.stats != nullptr) a.stats[i] = {all.m, all.s / Reference(all.m, a.c).left_out(a.c)};
+            }
+            if (grad) {
+                // what the named places get is formed before the stores are waited for; it takes the place of log_p
+                const Reference ref(all.m, a.c);
+                __syncwarp();
+                for (int k = lane; k < a.t; k += 32) e.log_p[k] = e.at[k] >= 0 ? entry_value(a, e, ref, all, d * a.temperature, k) : 0.f;
+                named_sync(3 + which);
+                T* out = dlogits + i * a.ld_d;
+                for (int k = lane; k < a.t; k += 32)
+                    if (e.at[k] >= 0) out[e.at[k]] = from_f32<T>(e.log_p[k]);
+                __syncwarp();
+            }
+        }
+    } else {
+        // ---------------------------------------------------------------- the row
+        int64_t r = 0;
+        for (int64_t i = blockIdx.x; i < m; i += gridDim.x, ++r) {
+            const T* row = logits + i * a.ld;
+            const RowWords<T> w(row, a.v);
+            const int n = static_cast<int>(a.v);
+            const int64_t row_seq = seq;
+            MaxSum mine{-INFINITY, 0.f};
+            float x[kMine][N];
+            // this thread's words of a chunk, from shared memory or, where they reach over an end, from the row
+            auto take = [&](int c, int s) {
+#pragma unroll
+                for (int k = 0; k < kMine; ++k) {
+                    const int in = k * kWorkers + static_cast<int>(threadIdx.x), word = c * kChunkWords + in;
+                    if (word >= w.begin && word < w.end) {
+                        Word<T>::unpack(*reinterpret_cast<const uint4*>(ring + s * kChunkBytes + in * 16), x[k]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < N; ++e) x[k][e] = -INFINITY;
+                        if (word * N - w.lead < n) load_slot<T, N>(row, word * N - w.lead, n, -INFINITY, x[k]);
+                    }
+                }
+            };
+            for (int c = 0; c < w.chunks; ++c, ++seq) {
+                const int s = static_cast<int>(seq % kRing);
+                mbar_wait_live(&full[s], static_cast<uint32_t>(seq / kRing) & 1, dead);   // expired: go on with what is there
+                take(c, s);
+                if (!(grad && hold)) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&empty[s]);
+                }
+                float top = mine.m;
+#pragma unroll
+                for (int k = 0; k < kMine; ++k)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) top = fmaxf(top, x[k][e]);
+                const Reference own(top, a.c);
+                if (mine.s != 0.f) mine.s *= exp2_fast(own.of_part(mine.m, a.c));
+                mine.m = top;
+#pragma unroll
+                for (int k = 0; k < kMine; ++k) {
+                    exponentials(x[k], own, a.c);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) mine.s += x[k][e];
+                }
+            }
+            mine = warp_join(mine, a.c);
+            if (lane == 0) part[r & 3][warp] = mine;
+            named_sync(1 + static_cast<int>(r & 1));
+            if (!grad) continue;
+            const MaxSum all = warp_join(lane < kWorkers / 32 ? part[r & 3][lane] : MaxSum{-INFINITY, 0.f}, a.c);
+            const Reference ref(all.m, a.c);
+            const float g = (a.dloss != nullptr ? a.dloss[i] : 1.f) * a.temperature;
+            const float factor = all.s == 0.f ? 0.f : g / all.s;
+            const bool any = some[r & 3] != 0;
+            T* out = dlogits + i * a.ld_d;
+            for (int c = 0; c < w.chunks; ++c) {
+                const int64_t at = hold ? row_seq + c : seq++;
+                const int s = static_cast<int>(at % kRing);
+                if (!hold) mbar_wait_live(&full[s], static_cast<uint32_t>(at / kRing) & 1, dead);
+                take(c, s);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&empty[s]);
+#pragma unroll
+                for (int k = 0; k < kMine; ++k) {
+                    const int j0 = (c * kChunkWords + k * kWorkers + static_cast<int>(threadIdx.x)) * N - w.lead;
+                    if (j0 >= n) break;
+                    exponentials(x[k], ref, a.c);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[k][e] = any ? x[k][e] * factor : 0.f;
+                    store_slot<T, N>(out, j0, n, x[k]);
+                }
+            }
+            named_arrive(3 + static_cast<int>(r & 1));
+        }
+    }
+    __syncthreads();
+    if (*dead && warp == kWorkers / 32 + kTeachers && lane == 0) {
+        atomicAdd(&g_timeouts, 1u);
+        for (int64_t j = seq > kRing ? seq - kRing : 0; j < seq; ++j) mbar_wait(&full[j % kRing], static_cast<uint32_t>(j / kRing) & 1);  // loads in flight
+    }
+}
+
 // The gradient from a given maximum and sum: CTA (x, y) takes share x of row y's columns.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) distill_backward_kernel(const __grid_constant__ DistillArgs a, const T* logits, T* dlogits, int shares) {
@@ -310,6 +523,20 @@ template <typename T, int VEC> int launch(const DistillArgs& a, int64_t m, const
     return check_launch();
 }
 
+// Rows from which the ring pays, and their length (see stream()).
+constexpr int64_t kStreamRows = 2 * kNumSMs, kStreamBytes = 16384;
+
+template <typename T> int stream(const DistillArgs& a, int64_t m, const T* logits, T* dlogits, cudaStream_t s) {
+    const int smem = kRing * kChunkBytes + 2 * kRing * 8 + 4 * 32 * static_cast<int>(sizeof(MaxSum)) + kTeachers * 16 * a.t;
+    auto kern = distill_stream_kernel<T>;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return cuda_failed(e);
+    const int hold = a.v + 2 * (Word<T>::kN - 1) <= static_cast<int64_t>(kHoldChunks) * kChunkWords * Word<T>::kN;
+    kern<<<static_cast<unsigned>(m < kNumSMs ? m : kNumSMs), kStreamThreads, smem, s>>>(a, m, logits, dlogits, hold);
+    note_launch();
+    return check_launch();
+}
+
 template <typename T, int VEC> int launch_backward(const DistillArgs& a, int64_t m, const T* logits, T* dlogits, cudaStream_t s) {
     const int64_t shares = (a.v + (VEC > 1 ? VEC - 1 : 0) + 256 * kHeld - 1) / (256 * kHeld);
     if (m * shares >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
@@ -326,6 +553,7 @@ template <typename T> int dispatch(const DistillArgs& a, int64_t m, const void* 
     const bool alike = out == nullptr || ((apart & 15) == 0 && (m == 1 || ((a.ld - a.ld_d) * static_cast<int64_t>(sizeof(T))) % 16 == 0));
     if (backward)
         return alike ? launch_backward<T, Word<T>::kN>(a, m, in, out, s) : launch_backward<T, 1>(a, m, in, out, s);
+    if (alike && m >= kStreamRows && a.v * static_cast<int64_t>(sizeof(T)) >= kStreamBytes && a.v < (int64_t(1) << 30)) return stream<T>(a, m, in, out, s);
     return alike ? launch<T, Word<T>::kN>(a, m, in, out, s) : launch<T, 1>(a, m, in, out, s);
 }
 
@@ -343,6 +571,11 @@ int check(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const
 }
 
 }  // namespace
+
+int distill_timeouts(unsigned int* count) {
+    const cudaError_t e = cudaMemcpyFromSymbol(count, g_timeouts, sizeof(unsigned int));
+    return e == cudaSuccess ? BZ_OK : cuda_failed(e);
+}
 
 }  // namespace bz
 

@@ -105,8 +105,10 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // A part of a row of softmax arguments: (largest z, sum of e^((z - that)/T)).  An empty part is (-inf, 0).
 //
 // With c = log2(e)/T an exponent is one multiply-add, z*c - m*c.  The product m*c is rounded, but everything that is
-// compared or joined uses the same rounded number, so its error cancels.  Where m*c leaves binary32's range although m
-// does not (a row of the type's lowest values), exponents are (z - m)*c instead.
+// compared or joined uses the same rounded number, so its error (up to 2^-25 of the product) cancels.  Where the product is
+// beyond 128 - up to a row of the type's lowest values, whose product may not even be finite - that error is no longer
+// small, and exponents are (z - m)*c, one operation more.  Parts of either kind may be joined: they differ by less than
+// 128 * 2^-25 in the exponent.
 struct MaxSum {
     float m, s;
 };
@@ -119,7 +121,7 @@ __device__ __forceinline__ float rounded_product(float a, float b) {
 struct Reference {
     float m, mc;   // a part's largest z (0 for an empty part) and its rounded product with c
     bool apart;
-    __device__ __forceinline__ Reference(float largest, float c) : m(largest == -INFINITY ? 0.f : largest), mc(rounded_product(m, c)), apart(isinf(mc) && !isinf(m)) {}
+    __device__ __forceinline__ Reference(float largest, float c) : m(largest == -INFINITY ? 0.f : largest), mc(rounded_product(m, c)), apart(fabsf(mc) > 128.f && !isinf(m)) {}
     // exponent of z, which is at most m; z may be -inf
     __device__ __forceinline__ float of(float z, float c) const { return apart ? (z - m) * c : fmaf(z, c, -mc); }
     // 2^(what the rounding of m*c left out): sums are kept relative to mc inside a kernel and to m itself outside

@@ -162,6 +162,42 @@ def test_gradient_against_differences():
         assert abs(float(diff) * float(dloss[i]) - float(d[i, c])) < 5e-6
 
 
+@pytest.mark.parametrize("dtype,v,pad,t", [(torch.bfloat16, 8200, 0, 5), (torch.bfloat16, 8201, 0, 40), (torch.float32, 4111, 1, 3), (torch.float16, 49140, 0, 33),
+                                           (torch.float16, 49153, 3, 64), (torch.float32, 30011, 0, 300), (torch.bfloat16, 150001, 0, 8)])
+def test_many_rows(dtype, v, pad, t):
+    """Rows enough for the ring: shorter than one chunk, several chunks, longer than what is held."""
+    m = 300 if v > 100000 else 500
+    logits, teacher, index, dloss = make(m, v, t, dtype, seed=v + t, pad=pad)
+    index[3] = -1
+    index[m - 1, 1:] = index[m - 1, 0]
+    logits[7] = -math.inf
+    logits[9, 5:] = torch.finfo(dtype).min
+    some = [0, 1, 2, 3, 7, 9, 147, 148, 149, 295, 296, 297, m - 2, m - 1]
+    out = torch.empty_like(logits) if pad == 0 else torch.empty(m, v + pad, dtype=dtype, device="cuda")[:, :v]
+    loss, stats, d = bz.distill(logits, teacher, index, 2.0, dloss=dloss, dlogits=out)
+    want_loss, want_lse, want_d, size = reference(logits[some], teacher[some], index[some], 2.0, dloss[some])
+    want_loss = want_loss.float().double()    # row 9's is beyond binary32: an infinity there
+    near = lambda got, want, tol: bool(((got.cpu().double() == want) | ((got.cpu().double() - want).abs() <= tol)).all())  # noqa: E731
+    assert near(loss[some], want_loss, 4 * TOL + TOL * want_loss.abs())
+    assert near(d[some], want_d, 2 * TOL * size + HALF_UNIT[dtype] * want_d.abs() + TINY[dtype])
+    # every row against the two other kernels: a few rows at a time, and the gradient alone
+    for lo in range(0, m, 100):
+        part = slice(lo, lo + 100)
+        few, few_stats, few_d = bz.distill(logits[part], teacher[part].contiguous(), index[part].contiguous(), 2.0, dloss=dloss[part].contiguous())
+        assert near(loss[part], few.cpu().double(), 8 * TOL + 2 * TOL * few.cpu().double().abs().clamp(max=1e30))
+        same = (d[part].float() - few_d.float()).abs() <= (2 * HALF_UNIT[dtype] + 4 * TOL) * few_d.float().abs() + 4 * TOL * dloss[part][:, None] + TINY[dtype]
+        assert same.all() and torch.equal(stats[part][:, 0], few_stats[:, 0])
+        assert torch.allclose(stats[part][:, 1], few_stats[:, 1], rtol=TOL)
+    for _ in range(5):
+        loss2, stats2, d2 = bz.distill(logits, teacher, index, 2.0, dloss=dloss, dlogits=torch.empty_like(logits) if pad == 0 else torch.empty(m, v + pad, dtype=dtype, device="cuda")[:, :v])
+        assert torch.equal(loss, loss2) and torch.equal(stats, stats2) and torch.equal(d, d2)
+    only, stats2 = bz.distill(logits, teacher, index, 2.0)
+    assert torch.equal(only, loss) and torch.equal(stats2, stats)
+    if pad == 0:
+        bz.distill(logits, teacher, index, 2.0, dloss=dloss, dlogits=logits)
+        assert torch.equal(logits, d)
+
+
 def test_many_entries():
     logits, teacher, index, dloss = make(2, 5000, 1024, torch.float32, seed=5)
     check(logits, teacher, index, 1.0, dloss)
