@@ -6,8 +6,7 @@
 // maximum, so that one exchange of (maximum, sum) pairs a row is all that a CTA's warps need.  Rows beyond 16 384 keys
 // are read twice.
 // The bias depends on j - p alone and is constant from max_distance on, so a CTA keeps the head's values for the
-// 2*max_distance + 1 distances in shared memory (with one word of padding every eight: a lane's eight neighbours
-// and the next lane's eight would otherwise share banks), and slots that lie beyond take one of the two end values.
+// 2*max_distance + 1 distances in shared memory, in copies that make a slot's values whole words (struct Window).
 //
 // Backward: p from the kept maximum and sum, D = sum p dp, dz = p (dp - D).  The table's gradient needs the sum of dz over
 // each diagonal of the scores inside the window and one sum for either side beyond it.  A warp owns a private array
@@ -48,12 +47,45 @@ __device__ __forceinline__ int bucket_of(const BiasForm& f, int rel) {
     return f.bidirectional && rel > 0 ? c + f.nb : c;
 }
 
-__device__ __forceinline__ int padded(int i) { return i + (i >> 3); }
-
-// bias[padded(rel + distance)]
-__device__ __forceinline__ void build_bias(const BiasForm& f, int head, float* bias) {
-    for (int d = threadIdx.x; d <= 2 * f.distance; d += blockDim.x)
-        bias[padded(d)] = f.table[bucket_of(f, d - f.distance) * f.h + head];
+// The head's bias by distance in shared memory, for slots of VEC keys.  A slot that begins at relative position rel needs
+// the values of distances rel .. rel + VEC - 1; with rel + max_distance = VEC*b + a (0 <= a < VEC) these are VEC consecutive
+// values from VEC*b + a on, ends repeated outside.  Copy a of the table is laid out so that they are whole 16-byte words:
+// b runs from -2 to `last`, where all VEC values are an end's, so a slot beyond the window is clamped to one of those and
+// nothing branches.  The four-value groups of a slot lie in different halves: neighbouring lanes read neighbouring words.
+template <int VEC> struct Window {
+    static constexpr int kGroups = VEC / 4 > 0 ? VEC / 4 : 1, kIn = VEC / kGroups;
+    int slots;   // per copy
+    __host__ __device__ explicit Window(int distance) : slots((2 * distance + VEC - 1) / VEC + 3) {}
+    __host__ __device__ int floats() const { return VEC * slots * VEC; }
+    __device__ __forceinline__ int at(int a, int slot, int group) const { return ((a * kGroups + group) * slots + slot) * kIn; }
+    // copy and slot of relative position rel
+    __device__ __forceinline__ void place(int rel, int distance, int& a, int& slot) const {
+        const int first = rel + distance;
+        a = first & (VEC - 1);
+        slot = max(0, min(slots - 1, (first - a) / VEC + 2));
+    }
+    // value index (a distance plus max_distance, maybe outside [0, 2*max_distance]) of element i
+    __device__ __forceinline__ int index(int a, int slot, int i) const { return VEC * (slot - 2) + a + i; }
+};
+template <int VEC> __device__ __forceinline__ void build_bias(const BiasForm& f, int head, const Window<VEC>& w, float* plain, float* bias) {
+    for (int d = threadIdx.x; d <= 2 * f.distance; d += blockDim.x) plain[d] = f.table[bucket_of(f, d - f.distance) * f.h + head];
+    __syncthreads();
+    for (int e = threadIdx.x; e < VEC * w.slots * Window<VEC>::kGroups; e += blockDim.x) {
+        const int slot = e % w.slots, group = e / w.slots % Window<VEC>::kGroups, a = e / w.slots / Window<VEC>::kGroups;
+        for (int i = 0; i < Window<VEC>::kIn; ++i)
+            bias[w.at(a, slot, group) + i] = plain[max(0, min(2 * f.distance, w.index(a, slot, group * Window<VEC>::kIn + i)))];
+    }
+}
+template <int VEC> __device__ __forceinline__ void window_load(const float* table, const Window<VEC>& w, int a, int slot, float (&x)[VEC]) {
+    if constexpr (VEC == 1) {
+        x[0] = table[w.at(a, slot, 0)];
+    } else {
+#pragma unroll
+        for (int g = 0; g < VEC / 4; ++g) {
+            const float4 v = *reinterpret_cast<const float4*>(table + w.at(a, slot, g));
+            x[4 * g] = v.x, x[4 * g + 1] = v.y, x[4 * g + 2] = v.z, x[4 * g + 3] = v.w;
+        }
+    }
 }
 
 // Keys [0, end) are seen by the query at position p.
@@ -65,18 +97,17 @@ struct Queries {
     __device__ int64_t end(const BiasForm& f, int64_t iq) const { return f.causal ? min(keys, max(position(iq) + 1, int64_t(0))) : keys; }
 };
 
+// A position as the held kernels use it: rows of at most 2^14 keys, so everything beyond +-2^28 is alike.
+__device__ __forceinline__ int near_position(int64_t p) { return static_cast<int>(max(int64_t(-1) << 28, min(int64_t(1) << 28, p))); }
+
 // z[i] = scale*s[i] + bias for the keys j0 + i that are seen, -inf for the others.  rel = j0 - p.
-template <int VEC>
-__device__ __forceinline__ void add_bias(const BiasForm& f, const float* bias, int64_t j0, int64_t end, int64_t rel, float (&z)[VEC]) {
-    if (rel >= f.distance || rel + VEC - 1 <= -f.distance) {
-        const float c = bias[padded(rel > 0 ? 2 * f.distance : 0)];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) z[i] = fmaf(z[i], f.scale, c);
-    } else {
-        const int first = static_cast<int>(rel) + f.distance;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) z[i] = fmaf(z[i], f.scale, bias[padded(max(0, min(2 * f.distance, first + i)))]);
-    }
+template <int VEC, typename I>
+__device__ __forceinline__ void add_bias(const BiasForm& f, const float* bias, const Window<VEC>& w, I j0, I end, int rel, float (&z)[VEC]) {
+    float b[VEC];
+    int a, slot;
+    w.place(rel, f.distance, a, slot);
+    window_load<VEC>(bias, w, a, slot, b);
+    multiply_add(z, f.scale, b);
     if (j0 < 0 || j0 + VEC > end) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
@@ -135,74 +166,65 @@ template <typename T> struct Raw<T, 1> {
 template <typename T, int VEC, int G, int SLOTS>
 __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
     bias_softmax_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<T> probs, MaxSum* stats) {
-    extern __shared__ float bias[];
+    extern __shared__ __align__(16) float bias[];
     __shared__ MaxSum part[2][16];
-    const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y;
+    const Window<VEC> w(f.distance);
+    const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y, n = static_cast<int>(f.tk);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta + threadIdx.x / G;
     const Queries q(f, ib);
     Raw<T, VEC> raw[SLOTS];
     auto fetch = [&](int64_t iq) {
         const T* in = scores.row(ib, ih, iq);
-        const int lead = row_lead<T, VEC>(in), end = static_cast<int>(q.end(f, iq));
+        const int j = t * VEC - row_lead<T, VEC>(in), end = static_cast<int>(q.end(f, iq));
 #pragma unroll
-        for (int c = 0; c < SLOTS; ++c) {
-            const int j0 = (c * G + t) * VEC - lead;
-            if (j0 < end) raw[c].load(in, j0, f.tk);
-        }
+        for (int c = 0; c < SLOTS; ++c)
+            if (j + c * G * VEC < end) raw[c].load(in, j + c * G * VEC, n);
     };
     if (first < f.tq) fetch(first);
-    build_bias(f, ih, bias);
+    build_bias<VEC>(f, ih, w, bias + w.floats(), bias);
     __syncthreads();
     for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
         const int64_t iq = first + it;
         if (iq >= f.tq) break;   // G > 32: the whole CTA; otherwise this warp
-        const int64_t p = q.position(iq);
-        const int end = static_cast<int>(q.end(f, iq)), lead = row_lead<T, VEC>(scores.row(ib, ih, iq));
+        const int p = near_position(q.position(iq)), end = static_cast<int>(q.end(f, iq));
+        const int j = t * VEC - row_lead<T, VEC>(scores.row(ib, ih, iq));
         float z[SLOTS][VEC];
         float top = -INFINITY;
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
-            const int j0 = (c * G + t) * VEC - lead;
+            const int j0 = j + c * G * VEC;
             if (j0 < end) {
                 raw[c].get(z[c]);
-                add_bias<VEC>(f, bias, j0, end, j0 - p, z[c]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) z[c][i] = -INFINITY;
+                add_bias<VEC>(f, bias, w, j0, end, j0 - p, z[c]);
+                top = largest(top, z[c]);
             }
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) top = fmaxf(top, z[c][i]);
         }
         if (it + Cta<G>::kRows < f.rows_per_cta && iq + Cta<G>::kRows < f.tq) fetch(iq + Cta<G>::kRows);
         MaxSum v{warp_max(top), 0.f};
         const Reference own(v.m, kLog2e);
-        if (!own.apart) {
-#pragma unroll
-            for (int c = 0; c < SLOTS; ++c)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) z[c][i] = exp2_fast(fmaf(z[c][i], kLog2e, -own.mc));
-        } else {
-#pragma unroll
-            for (int c = 0; c < SLOTS; ++c)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) z[c][i] = exp2_fast((z[c][i] - own.m) * kLog2e);
-        }
+        float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) v.s += z[c][i];
-        v.s = warp_sum(v.s);
+            if (j + c * G * VEC < end) {
+                exponentials(z[c], own, kLog2e);
+                add_up(sum, z[c]);
+            }
+        v.s = warp_sum(sum.x + sum.y);
         const MaxSum all = group_join<G>(v, kLog2e, part, it / Cta<G>::kRows);
         float norm = all.s == 0.f ? 0.f : 1.f / all.s;
         if (G > 32 && v.s != 0.f) norm *= exp2_fast(Reference(all.m, kLog2e).of_part(v.m, kLog2e));
         T* out = probs.row(ib, ih, iq);
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
-            const int j0 = (c * G + t) * VEC - lead;
-            if (j0 < f.tk) {
+            const int j0 = j + c * G * VEC;
+            if (j0 < n) {
+                if (j0 < end) {
+                    multiply(z[c], norm);
+                } else {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) z[c][i] *= norm;
-                store_slot<T, VEC>(out, j0, f.tk, z[c]);
+                    for (int i = 0; i < VEC; ++i) z[c][i] = 0.f;
+                }
+                store_slot<T, VEC>(out, j0, n, z[c]);
             }
         }
         if (t == 0 && stats != nullptr) stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq] = {all.m, all.s / Reference(all.m, kLog2e).left_out(kLog2e)};
@@ -213,11 +235,12 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
 template <typename T, int VEC>
 __global__ void __launch_bounds__(512) bias_softmax_long_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<T> probs, MaxSum* stats) {
     constexpr int G = 512;
-    extern __shared__ float bias[];
+    extern __shared__ __align__(16) float bias[];
     __shared__ MaxSum part[2][16];
+    const Window<VEC> w(f.distance);
     const int t = threadIdx.x, ib = blockIdx.z, ih = blockIdx.y;
     const Queries q(f, ib);
-    build_bias(f, ih, bias);
+    build_bias<VEC>(f, ih, w, bias + w.floats(), bias);
     __syncthreads();
     const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta;
     for (int it = 0; it < f.rows_per_cta && first + it < f.tq; ++it) {
@@ -229,7 +252,7 @@ __global__ void __launch_bounds__(512) bias_softmax_long_kernel(const __grid_con
         for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < end; j0 += G * VEC) {
             float z[VEC];
             load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
-            add_bias<VEC>(f, bias, j0, end, j0 - p, z);
+            add_bias<VEC>(f, bias, w, j0, end, near_position(j0 - p), z);
             float m = v.m;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) m = fmaxf(m, z[i]);
@@ -248,7 +271,7 @@ __global__ void __launch_bounds__(512) bias_softmax_long_kernel(const __grid_con
             for (int i = 0; i < VEC; ++i) z[i] = 0.f;
             if (j0 < end) {
                 load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
-                add_bias<VEC>(f, bias, j0, end, j0 - p, z);
+                add_bias<VEC>(f, bias, w, j0, end, near_position(j0 - p), z);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) z[i] = exp2_fast(r.of(z[i], kLog2e)) * norm;
             }
@@ -258,47 +281,60 @@ __global__ void __launch_bounds__(512) bias_softmax_long_kernel(const __grid_con
     }
 }
 
-// One slot of the table's gradient: dz of the keys at distances rel .. rel + VEC - 1 (0 where a key is not seen).
+// One slot of the table's gradient: dz of the keys at distances rel .. rel + VEC - 1 (0 where a key is not seen).  `sums`:
+// the warp's window, laid out as the bias.  Lanes whose slot touches the window have slots of their own in it; the first
+// and the last slot of a copy stand for either side beyond it and stay in registers.
 template <int VEC>
-__device__ __forceinline__ void add_diagonals(const BiasForm& f, float* diag, int64_t rel, const float (&dz)[VEC], float& left, float& right) {
-    if (rel >= f.distance || rel + VEC - 1 <= -f.distance) {
-        float s = dz[0];
-#pragma unroll
-        for (int i = 1; i < VEC; ++i) s += dz[i];
-        if (rel > 0)
-            right += s;
-        else
-            left += s;
+__device__ __forceinline__ void add_diagonals(const BiasForm& f, float* sums, const Window<VEC>& w, int rel, const float (&dz)[VEC], float2& left, float2& right) {
+    int a, slot;
+    w.place(rel, f.distance, a, slot);
+    if (slot == 0) {
+        add_up(left, dz);
+    } else if (slot == w.slots - 1) {
+        add_up(right, dz);
     } else {
-        const int first = static_cast<int>(rel) + f.distance;
+        float x[VEC];
+        window_load<VEC>(sums, w, a, slot, x);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            if (first + i >= 2 * f.distance)
-                right += dz[i];
-            else if (first + i <= 0)
-                left += dz[i];
-            else
-                diag[padded(first + i)] += dz[i];
+        for (int i = 0; i < VEC; ++i) x[i] += dz[i];
+        if constexpr (VEC == 1) {
+            sums[w.at(a, slot, 0)] = x[0];
+        } else {
+#pragma unroll
+            for (int g = 0; g < VEC / 4; ++g)
+                *reinterpret_cast<float4*>(sums + w.at(a, slot, g)) = make_float4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]);
         }
     }
 }
 
-// What the rows of a CTA leave for the table.  The two ends of each warp's array take its far sums, then warps join
-// diagonal by diagonal and diagonals by bucket.
-__device__ __forceinline__ void leave_buckets(const BiasForm& f, float* diags, int warps, float left, float right, float* mine) {
-    const int span = padded(2 * f.distance) + 1;
-    float* diag = diags + (threadIdx.x >> 5) * span;
-    left = warp_sum(left);
-    right = warp_sum(right);
+// What the rows of a CTA leave for the table.  Each warp's far sums take the first and last slot of its copy 0 (both ends
+// of the table's values); then, distance by distance, warps and copies are added in order, and distances by bucket.
+template <int VEC>
+__device__ __forceinline__ void leave_buckets(const BiasForm& f, float* all_sums, const Window<VEC>& w, int warps, float2 left2, float2 right2, float* by_distance, float* mine) {
+    const float left = warp_sum(left2.x + left2.y), right = warp_sum(right2.x + right2.y);
     if ((threadIdx.x & 31) == 0) {
-        diag[padded(0)] = left;
-        diag[padded(2 * f.distance)] = right;
+        float* sums = all_sums + (threadIdx.x >> 5) * w.floats();
+        sums[w.at(0, 0, 0)] = left;
+        sums[w.at(0, w.slots - 1, 0)] = right;
     }
     __syncthreads();
-    for (int d = threadIdx.x; d <= 2 * f.distance; d += blockDim.x) {
-        float s = diags[padded(d)];
-        for (int w = 1; w < warps; ++w) s += diags[w * span + padded(d)];
-        diags[padded(d)] = s;
+    const int ends = 2 * f.distance;
+    for (int d = threadIdx.x; d <= ends; d += blockDim.x) {
+        // elements (a, slot, i) with value index d; indices outside belong to the ends
+        float s = 0.f;
+        for (int k = 0; k < warps; ++k) {
+            const float* sums = all_sums + k * w.floats();
+            for (int a = 0; a < VEC; ++a) {
+                if (d > 0 && d < ends) {
+                    const int e = d - a + 2 * VEC;   // VEC*slot + i
+                    s += sums[w.at(a, e / VEC, e % VEC / Window<VEC>::kIn) + e % VEC % Window<VEC>::kIn];
+                } else {
+                    const int from = d == 0 ? 0 : max(0, ends - a + 2 * VEC), to = d == 0 ? 2 * VEC - a : VEC * w.slots - 1;
+                    for (int e = from; e <= to; ++e) s += sums[w.at(a, e / VEC, e % VEC / Window<VEC>::kIn) + e % VEC % Window<VEC>::kIn];
+                }
+            }
+        }
+        by_distance[d] = s;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < f.buckets; c += blockDim.x) {
@@ -307,11 +343,11 @@ __device__ __forceinline__ void leave_buckets(const BiasForm& f, float* diags, i
         const int hi = k < f.exact ? k + 1 : (k == f.nb - 1 ? f.distance + 1 : f.starts[k - f.exact + 1]);
         float s = 0.f;
         if (c != k) {
-            for (int n = max(lo, 1); n < hi; ++n) s += diags[padded(f.distance + n)];
+            for (int n = max(lo, 1); n < hi; ++n) s += by_distance[f.distance + n];
         } else {
-            for (int n = lo; n < hi; ++n) s += diags[padded(f.distance - n)];
+            for (int n = lo; n < hi; ++n) s += by_distance[f.distance - n];
             if (!f.bidirectional && c == 0)
-                for (int n = 1; n <= f.distance; ++n) s += diags[padded(f.distance + n)];
+                for (int n = 1; n <= f.distance; ++n) s += by_distance[f.distance + n];
         }
         mine[c] = s;
     }
@@ -322,66 +358,63 @@ template <typename T, int VEC, int G, int SLOTS>
 __global__ void __launch_bounds__(Cta<G>::kThreads, 640 / Cta<G>::kThreads)
     bias_softmax_backward_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<const T> dprobs,
                                  const Rows4<T> dscores, const MaxSum* __restrict__ stats, float* __restrict__ partial) {
-    extern __shared__ float bias[];
+    extern __shared__ __align__(16) float bias[];
     __shared__ float part[2][16];
     constexpr int kWarps = Cta<G>::kThreads / 32;
-    const int span = padded(2 * f.distance) + 1;
-    float* diags = bias + span;
-    float* diag = diags + (threadIdx.x >> 5) * span;
-    const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y;
+    const Window<VEC> w(f.distance);
+    float* all_sums = bias + w.floats();
+    float* sums = all_sums + (threadIdx.x >> 5) * w.floats();
+    float* plain = all_sums + (partial != nullptr ? kWarps * w.floats() : 0);
+    const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y, n = static_cast<int>(f.tk);
     const Queries q(f, ib);
-    build_bias(f, ih, bias);
+    build_bias<VEC>(f, ih, w, plain, bias);
     if (partial != nullptr)
-        for (int i = threadIdx.x; i < kWarps * span; i += blockDim.x) diags[i] = 0.f;
+        for (int i = threadIdx.x; i < kWarps * w.floats(); i += blockDim.x) all_sums[i] = 0.f;
     __syncthreads();
-    float left = 0.f, right = 0.f;
+    float2 left = make_float2(0.f, 0.f), right = left;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta + threadIdx.x / G;
     for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
         const int64_t iq = first + it;
         if (iq >= f.tq) break;
-        const int64_t p0 = q.position(iq);
+        const int p0 = near_position(q.position(iq));
         const T* in = scores.row(ib, ih, iq);
         const T* up = dprobs.row(ib, ih, iq);
-        const int lead = row_lead<T, VEC>(in);
-        const MaxSum all = stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq];
-        const int end = all.s == 0.f ? 0 : static_cast<int>(q.end(f, iq));   // a row without keys: all 0
+        const int j = t * VEC - row_lead<T, VEC>(in);
+        MaxSum all = stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq];
+        const int end = static_cast<int>(q.end(f, iq));
         Raw<T, VEC> s[SLOTS], dp[SLOTS];
 #pragma unroll
-        for (int c = 0; c < SLOTS; ++c) {
-            const int j0 = (c * G + t) * VEC - lead;
-            if (j0 < end) {
-                s[c].load(in, j0, f.tk);
-                dp[c].load(up, j0, end);
+        for (int c = 0; c < SLOTS; ++c)
+            if (j + c * G * VEC < end) {
+                s[c].load(in, j + c * G * VEC, n);
+                dp[c].load(up, j + c * G * VEC, end);
             }
-        }
         const Reference r(all.m, kLog2e);
-        const float norm = 1.f / (all.s * r.left_out(kLog2e));
+        const bool empty = all.s == 0.f;   // a row without keys, or none above -inf: all 0
+        const float norm = empty ? 0.f : 1.f / (all.s * r.left_out(kLog2e));
         float p[SLOTS][VEC], dot = 0.f;
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
-            const int j0 = (c * G + t) * VEC - lead;
+            const int j0 = j + c * G * VEC;
             if (j0 < end) {
                 float d[VEC];
                 s[c].get(p[c]);
                 dp[c].get(d);
-                add_bias<VEC>(f, bias, j0, end, j0 - p0, p[c]);
+                add_bias<VEC>(f, bias, w, j0, end, j0 - p0, p[c]);
+                exponentials(p[c], r, kLog2e);
+                multiply(p[c], norm);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    p[c][i] = exp2_fast(r.of(p[c][i], kLog2e)) * norm;
-                    dot = fmaf(p[c][i], d[i], dot);
-                }
+                for (int i = 0; i < VEC; ++i) dot = fmaf(p[c][i], d[i], dot);
             }
         }
         dot = group_sum<G>(dot, part, it / Cta<G>::kRows);
         T* out = dscores.p != nullptr ? dscores.row(ib, ih, iq) : nullptr;
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
-            const int j0 = (c * G + t) * VEC - lead;
-            if (j0 < f.tk) {
+            const int j0 = j + c * G * VEC;
+            if (j0 < n) {
                 float dz[VEC];
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) dz[i] = 0.f;
-                if (j0 < end) {
+                if (j0 < end && !empty) {
                     dp[c].get(dz);
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) dz[i] = p[c][i] * (dz[i] - dot);
@@ -390,19 +423,21 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 640 / Cta<G>::kThreads)
                         for (int i = 0; i < VEC; ++i)
                             if (j0 + i < 0 || j0 + i >= end) dz[i] = 0.f;   // whatever dot is
                     }
-                    if (partial != nullptr) add_diagonals<VEC>(f, diag, j0 - p0, dz, left, right);
+                    if (partial != nullptr) add_diagonals<VEC>(f, sums, w, j0 - p0, dz, left, right);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) dz[i] = 0.f;
                 }
                 if (out != nullptr) {
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) dz[i] *= f.scale;
-                    store_slot<T, VEC>(out, j0, f.tk, dz);
+                    multiply(dz, f.scale);
+                    store_slot<T, VEC>(out, j0, n, dz);
                 }
             }
         }
         __syncwarp();  // the next row meets this row's diagonals through other lanes
     }
     if (partial == nullptr) return;
-    leave_buckets(f, diags, kWarps, left, right, partial + ((static_cast<int64_t>(ih) * gridDim.z + ib) * gridDim.x + blockIdx.x) * f.buckets);
+    leave_buckets<VEC>(f, all_sums, w, kWarps, left, right, plain, partial + ((static_cast<int64_t>(ih) * gridDim.z + ib) * gridDim.x + blockIdx.x) * f.buckets);
 }
 
 // Rows of any length, read twice.
@@ -411,18 +446,19 @@ __global__ void __launch_bounds__(256)
     bias_softmax_backward_long_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<const T> dprobs,
                                       const Rows4<T> dscores, const MaxSum* __restrict__ stats, float* __restrict__ partial) {
     constexpr int G = 256, kWarps = G / 32;
-    extern __shared__ float bias[];
+    extern __shared__ __align__(16) float bias[];
     __shared__ float part[2][16];
-    const int span = padded(2 * f.distance) + 1;
-    float* diags = bias + span;
-    float* diag = diags + (threadIdx.x >> 5) * span;
+    const Window<VEC> w(f.distance);
+    float* all_sums = bias + w.floats();
+    float* sums = all_sums + (threadIdx.x >> 5) * w.floats();
+    float* plain = all_sums + (partial != nullptr ? kWarps * w.floats() : 0);
     const int t = threadIdx.x, ib = blockIdx.z, ih = blockIdx.y;
     const Queries q(f, ib);
-    build_bias(f, ih, bias);
+    build_bias<VEC>(f, ih, w, plain, bias);
     if (partial != nullptr)
-        for (int i = threadIdx.x; i < kWarps * span; i += blockDim.x) diags[i] = 0.f;
+        for (int i = threadIdx.x; i < kWarps * w.floats(); i += blockDim.x) all_sums[i] = 0.f;
     __syncthreads();
-    float left = 0.f, right = 0.f;
+    float2 left = make_float2(0.f, 0.f), right = left;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta;
     for (int it = 0; it < f.rows_per_cta && first + it < f.tq; ++it) {
         const int64_t iq = first + it, p0 = q.position(iq);
@@ -443,7 +479,7 @@ __global__ void __launch_bounds__(256)
                 if (j0 < end) {
                     load_slot<T, VEC>(in, j0, f.tk, 0.f, p);
                     load_slot<T, VEC>(up, j0, end, 0.f, dp);
-                    add_bias<VEC>(f, bias, j0, end, j0 - p0, p);
+                    add_bias<VEC>(f, bias, w, j0, end, near_position(j0 - p0), p);
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) p[i] = exp2_fast(r.of(p[i], kLog2e)) * norm;
                 }
@@ -454,7 +490,7 @@ __global__ void __launch_bounds__(256)
                 }
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) p[i] = j0 + i >= 0 && j0 + i < end ? p[i] * (dp[i] - dot) : 0.f;
-                if (partial != nullptr && j0 < end) add_diagonals<VEC>(f, diag, j0 - p0, p, left, right);
+                if (partial != nullptr && j0 < end) add_diagonals<VEC>(f, sums, w, near_position(j0 - p0), p, left, right);
                 if (out != nullptr) {
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) p[i] *= f.scale;
@@ -466,7 +502,7 @@ __global__ void __launch_bounds__(256)
         __syncwarp();
     }
     if (partial == nullptr) return;
-    leave_buckets(f, diags, kWarps, left, right, partial + ((static_cast<int64_t>(ih) * gridDim.z + ib) * gridDim.x + blockIdx.x) * f.buckets);
+    leave_buckets<VEC>(f, all_sums, w, kWarps, left, right, plain, partial + ((static_cast<int64_t>(ih) * gridDim.z + ib) * gridDim.x + blockIdx.x) * f.buckets);
 }
 
 // dtable[c][head]: the parts of one head added by 32 lanes, then the lanes; one warp a value.
@@ -550,7 +586,7 @@ int launch_forward(BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4
     constexpr int kRows = Cta<G>::kRows;
     f.rows_per_cta = kRows * 8;
     while (f.rows_per_cta > kRows && b * f.h * ((f.tq + f.rows_per_cta - 1) / f.rows_per_cta) < 16 * kNumSMs) f.rows_per_cta /= 2;
-    const size_t smem = (2 * f.distance + 2 * f.distance / 8 + 1) * sizeof(float);
+    const size_t smem = (Window<VEC>(f.distance).floats() + 2 * f.distance + 1) * sizeof(float);
     const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
     if constexpr (kLong)
         bias_softmax_long_kernel<T, VEC><<<grid, 512, smem, s>>>(f, in, out, stats);
@@ -576,8 +612,7 @@ int dispatch_forward(BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in
 template <typename T, int VEC, int G, int SLOTS>
 int launch_backward(const BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out, const MaxSum* stats,
                     float* partial, cudaStream_t s) {
-    const size_t span = 2 * f.distance + 2 * f.distance / 8 + 1;
-    const size_t smem = span * sizeof(float) * (1 + (partial != nullptr ? Cta<G>::kThreads / 32 : 0));
+    const size_t smem = (Window<VEC>(f.distance).floats() * (1 + (partial != nullptr ? Cta<G>::kThreads / 32 : 0)) + 2 * f.distance + 1) * sizeof(float);
     const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
     int st;
     if constexpr (SLOTS == 0) {
@@ -603,6 +638,9 @@ int dispatch_backward(const BiasForm& f, int64_t n, int64_t b, const Rows4<const
     return launch_backward<T, VEC, 256, 0>(f, b, in, up, out, stats, partial, s);
 }
 
+// The wide kernels keep eight (or four) copies of the window; beyond this distance they would leave one CTA an SM.
+constexpr int kWideDistance = 256;
+
 // Elements a row takes up from its first slot on: none before it if every row begins on a 16-byte boundary.
 int64_t row_span(const void* p, const int64_t* strides, int64_t b, int64_t h, int64_t tq, int64_t tk, int bytes) {
     const int64_t zero[3] = {0, 0, 0};
@@ -613,7 +651,7 @@ template <typename T>
 int forward(BiasForm& f, int64_t b, const void* scores, const int64_t* ss, void* probs, const int64_t* sp, MaxSum* stats, cudaStream_t s) {
     const auto in = rows4(static_cast<const T*>(scores), ss);
     const auto out = rows4(static_cast<T*>(probs), sp);
-    if (alike(scores, ss, probs, sp, b, f.h, f.tq, sizeof(T)))
+    if (f.distance <= kWideDistance && alike(scores, ss, probs, sp, b, f.h, f.tq, sizeof(T)))
         return dispatch_forward<T, Word<T>::kN>(f, row_span(scores, ss, b, f.h, f.tq, f.tk, sizeof(T)), b, in, out, stats, s);
     return dispatch_forward<T, 1>(f, f.tk, b, in, out, stats, s);
 }
@@ -624,7 +662,7 @@ int backward(const BiasForm& f, int64_t b, const void* scores, const int64_t* ss
     const auto in = rows4(static_cast<const T*>(scores), ss);
     const auto up = rows4(static_cast<const T*>(dprobs), sd);
     const auto out = rows4(static_cast<T*>(dscores), so);
-    if (alike(scores, ss, dprobs, sd, b, f.h, f.tq, sizeof(T)) && (dscores == nullptr || alike(scores, ss, dscores, so, b, f.h, f.tq, sizeof(T))))
+    if (f.distance <= kWideDistance && alike(scores, ss, dprobs, sd, b, f.h, f.tq, sizeof(T)) && (dscores == nullptr || alike(scores, ss, dscores, so, b, f.h, f.tq, sizeof(T))))
         return dispatch_backward<T, Word<T>::kN>(f, row_span(scores, ss, b, f.h, f.tq, f.tk, sizeof(T)), b, in, up, out, stats, partial, s);
     return dispatch_backward<T, 1>(f, f.tk, b, in, up, out, stats, partial, s);
 }

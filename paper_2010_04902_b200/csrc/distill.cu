@@ -132,17 +132,6 @@ __device__ __forceinline__ MaxSum cta_join(const MaxSum& v, float c, MaxSum* par
     return warp_join(lane < (blockDim.x >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f}, c);
 }
 
-// x[i] = 2^(exponent of x[i]) relative to r.
-template <int N> __device__ __forceinline__ void exponentials(float (&x)[N], const Reference& r, float c) {
-    if (!r.apart) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) x[k] = exp2_fast(fmaf(x[k], c, -r.mc));
-    } else {
-#pragma unroll
-        for (int k = 0; k < N; ++k) x[k] = exp2_fast((x[k] - r.m) * c);
-    }
-}
-
 // One cluster a row.  HELD: the row's exponentials stay in registers; otherwise the row is read twice.
 template <typename T, int VEC, bool HELD>
 __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_constant__ DistillArgs a, const T* logits, T* dlogits) {
@@ -372,10 +361,13 @@ __global__ void __launch_bounds__(kStreamThreads, 1) distill_stream_kernel(const
             const int64_t row_seq = seq;
             MaxSum mine{-INFINITY, 0.f};
             float x[kMine][N];
+            // whether the 512 words of step k of a chunk hold any of the row
+            auto there = [&](int c, int k) { return (c * kChunkWords + k * kWorkers) * N - w.lead < n; };
             // this thread's words of a chunk, from shared memory or, where they reach over an end, from the row
             auto take = [&](int c, int s) {
 #pragma unroll
                 for (int k = 0; k < kMine; ++k) {
+                    if (!there(c, k)) break;
                     const int in = k * kWorkers + static_cast<int>(threadIdx.x), word = c * kChunkWords + in;
                     if (word >= w.begin && word < w.end) {
                         Word<T>::unpack(*reinterpret_cast<const uint4*>(ring + s * kChunkBytes + in * 16), x[k]);
@@ -397,17 +389,18 @@ __global__ void __launch_bounds__(kStreamThreads, 1) distill_stream_kernel(const
                 float top = mine.m;
 #pragma unroll
                 for (int k = 0; k < kMine; ++k)
-#pragma unroll
-                    for (int e = 0; e < N; ++e) top = fmaxf(top, x[k][e]);
+                    if (there(c, k)) top = largest(top, x[k]);
                 const Reference own(top, a.c);
                 if (mine.s != 0.f) mine.s *= exp2_fast(own.of_part(mine.m, a.c));
                 mine.m = top;
+                float2 sum = make_float2(mine.s, 0.f);
 #pragma unroll
-                for (int k = 0; k < kMine; ++k) {
-                    exponentials(x[k], own, a.c);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) mine.s += x[k][e];
-                }
+                for (int k = 0; k < kMine; ++k)
+                    if (there(c, k)) {
+                        exponentials(x[k], own, a.c);
+                        add_up(sum, x[k]);
+                    }
+                mine.s = sum.x + sum.y;
             }
             mine = warp_join(mine, a.c);
             if (lane == 0) part[r & 3][warp] = mine;
@@ -431,8 +424,11 @@ __global__ void __launch_bounds__(kStreamThreads, 1) distill_stream_kernel(const
                     const int j0 = (c * kChunkWords + k * kWorkers + static_cast<int>(threadIdx.x)) * N - w.lead;
                     if (j0 >= n) break;
                     exponentials(x[k], ref, a.c);
+                    multiply(x[k], factor);
+                    if (!any) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) x[k][e] = any ? x[k][e] * factor : 0.f;
+                        for (int e = 0; e < N; ++e) x[k][e] = 0.f;
+                    }
                     store_slot<T, N>(out, j0, n, x[k]);
                 }
             }

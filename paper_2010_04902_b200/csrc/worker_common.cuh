@@ -148,4 +148,67 @@ __device__ __forceinline__ float warp_max(float v) {
     return m;
 }
 
+// ---- arrays in registers, two elements an instruction where there are two -------------------------
+
+// x[i] = x[i]*a + b[i]
+template <int N> __device__ __forceinline__ void multiply_add(float (&x)[N], float a, const float (&b)[N]) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 y = __ffma2_rn(make_float2(x[i], x[i + 1]), make_float2(a, a), make_float2(b[i], b[i + 1]));
+            x[i] = y.x, x[i + 1] = y.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = fmaf(x[i], a, b[i]);
+    }
+}
+template <int N> __device__ __forceinline__ void multiply(float (&x)[N], float a) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 y = __fmul2_rn(make_float2(x[i], x[i + 1]), make_float2(a, a));
+            x[i] = y.x, x[i + 1] = y.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] *= a;
+    }
+}
+// Largest of m and x (NaNs do not count).
+template <int N> __device__ __forceinline__ float largest(float m, const float (&x)[N]) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(x[i]), "f"(x[i + 1]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+    }
+    return m;
+}
+// s += x, element by element in two partial sums.
+template <int N> __device__ __forceinline__ void add_up(float2& s, const float (&x)[N]) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) s = __fadd2_rn(s, make_float2(x[i], x[i + 1]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s.x += x[i];
+    }
+}
+// x[i] = 2^(exponent of x[i]) relative to r.
+template <int N> __device__ __forceinline__ void exponentials(float (&x)[N], const Reference& r, float c) {
+    if (!r.apart) {
+        float b[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) b[i] = -r.mc;
+        multiply_add(x, c, b);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = (x[i] - r.m) * c;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = exp2_fast(x[i]);
+}
+
 }  // namespace bz
