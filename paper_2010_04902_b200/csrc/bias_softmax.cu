@@ -34,6 +34,7 @@ struct BiasForm {
 template <typename T> struct Rows4 {  // a [b][h][tq][tk] tensor
     T* p;
     int64_t b, h, q;
+    Extent extent;
     __device__ T* row(int64_t ib, int64_t ih, int64_t iq) const { return p + ib * b + ih * h + iq * q; }
 };
 
@@ -100,20 +101,29 @@ struct Queries {
 // A position as the held kernels use it: rows of at most 2^14 keys, so everything beyond +-2^28 is alike.
 __device__ __forceinline__ int near_position(int64_t p) { return static_cast<int>(max(int64_t(-1) << 28, min(int64_t(1) << 28, p))); }
 
-// z[i] = scale*s[i] + bias for the keys j0 + i that are seen, -inf for the others.  rel = j0 - p.
-template <int VEC, typename I>
-__device__ __forceinline__ void add_bias(const BiasForm& f, const float* bias, const Window<VEC>& w, I j0, I end, int rel, float (&z)[VEC]) {
+// z[i] = scale*s[i] + bias.  rel = j0 - p.
+template <int VEC> __device__ __forceinline__ void add_bias(const BiasForm& f, const float* bias, const Window<VEC>& w, int rel, float (&z)[VEC]) {
     float b[VEC];
     int a, slot;
     w.place(rel, f.distance, a, slot);
     window_load<VEC>(bias, w, a, slot, b);
     multiply_add(z, f.scale, b);
+}
+// `gone` in the place of the keys j0 + i that are not seen.
+template <int VEC, typename I> __device__ __forceinline__ void mask(I j0, I end, float gone, float (&z)[VEC]) {
     if (j0 < 0 || j0 + VEC > end) {
+        rare();
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
-            if (j0 + i < 0 || j0 + i >= end) z[i] = -INFINITY;
+            if (j0 + i < 0 || j0 + i >= end) z[i] = gone;
     }
 }
+// Of a row's SLOTS steps (G slots of VEC keys each): the first `whole` hold seen keys only, those from `some` on hold none.
+// Both are the same for all threads of a row, so the common steps run without a test of their own.
+template <int VEC, int G> struct Steps {
+    int whole, some;
+    __device__ __forceinline__ Steps(int lead, int end) : whole(lead == 0 ? end / (G * VEC) : 0), some((lead + end + G * VEC - 1) / (G * VEC)) {}
+};
 
 template <int G> struct Cta {
     static constexpr int kThreads = G > 32 ? G : 128;
@@ -142,26 +152,6 @@ template <int G> __device__ __forceinline__ float group_sum(float v, float (*par
     return v;
 }
 
-// A slot as it was loaded: 16 bytes, or one element.
-template <typename T, int VEC> struct Raw {
-    uint4 w;
-    __device__ __forceinline__ void load(const T* row, int64_t j0, int64_t n) {
-        if (j0 >= 0 && j0 + VEC <= n) {
-            w = ld_stream(reinterpret_cast<const uint4*>(row + j0));
-        } else {
-            float x[VEC];
-            load_slot<T, VEC>(row, j0, n, 0.f, x);
-            w = Word<T>::pack(x);
-        }
-    }
-    __device__ __forceinline__ void get(float (&x)[VEC]) const { Word<T>::unpack(w, x); }
-};
-template <typename T> struct Raw<T, 1> {
-    T e;
-    __device__ __forceinline__ void load(const T* row, int64_t j0, int64_t n) { e = j0 < n ? row[j0] : from_f32<T>(0.f); }
-    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = to_f32(e); }
-};
-
 // SLOTS slots a thread are held in registers, and the next row's are loaded before this row's are used.
 template <typename T, int VEC, int G, int SLOTS>
 __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
@@ -177,8 +167,7 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
         const T* in = scores.row(ib, ih, iq);
         const int j = t * VEC - row_lead<T, VEC>(in), end = static_cast<int>(q.end(f, iq));
 #pragma unroll
-        for (int c = 0; c < SLOTS; ++c)
-            if (j + c * G * VEC < end) raw[c].load(in, j + c * G * VEC, n);
+        for (int c = 0; c < SLOTS; ++c) raw[c].fetch(in, j + c * G * VEC, j + c * G * VEC < end, scores.extent);
     };
     if (first < f.tq) fetch(first);
     build_bias<VEC>(f, ih, w, bias + w.floats(), bias);
@@ -187,25 +176,30 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
         const int64_t iq = first + it;
         if (iq >= f.tq) break;   // G > 32: the whole CTA; otherwise this warp
         const int p = near_position(q.position(iq)), end = static_cast<int>(q.end(f, iq));
-        const int j = t * VEC - row_lead<T, VEC>(scores.row(ib, ih, iq));
+        const T* in = scores.row(ib, ih, iq);
+        const int lead = row_lead<T, VEC>(in), j = t * VEC - lead;
+        const Steps<VEC, G> steps(lead, end);
         float z[SLOTS][VEC];
         float top = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < SLOTS; ++c) {
-            const int j0 = j + c * G * VEC;
-            if (j0 < end) {
-                raw[c].get(z[c]);
-                add_bias<VEC>(f, bias, w, j0, end, j0 - p, z[c]);
+        for (int c = 0; c < SLOTS; ++c)
+            if (c < steps.some) {
+                const int j0 = j + c * G * VEC;
+                if (c < steps.whole)
+                    raw[c].get(z[c]);
+                else
+                    raw[c].get(in, j0, n, scores.extent, z[c]);
+                add_bias<VEC>(f, bias, w, j0 - p, z[c]);
+                if (c >= steps.whole) mask<VEC>(j0, end, -INFINITY, z[c]);
                 top = largest(top, z[c]);
             }
-        }
         if (it + Cta<G>::kRows < f.rows_per_cta && iq + Cta<G>::kRows < f.tq) fetch(iq + Cta<G>::kRows);
         MaxSum v{warp_max(top), 0.f};
         const Reference own(v.m, kLog2e);
         float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c)
-            if (j + c * G * VEC < end) {
+            if (c < steps.some) {
                 exponentials(z[c], own, kLog2e);
                 add_up(sum, z[c]);
             }
@@ -217,15 +211,16 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
             const int j0 = j + c * G * VEC;
-            if (j0 < n) {
-                if (j0 < end) {
-                    multiply(z[c], norm);
-                } else {
+            if (c < steps.some) {
+                multiply(z[c], norm);
+            } else {
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) z[c][i] = 0.f;
-                }
-                store_slot<T, VEC>(out, j0, n, z[c]);
+                for (int i = 0; i < VEC; ++i) z[c][i] = 0.f;
             }
+            if (c < steps.whole)
+                store_whole<T, VEC>(out + j0, z[c]);
+            else if (j0 < n)
+                store_slot<T, VEC>(out, j0, n, z[c]);
         }
         if (t == 0 && stats != nullptr) stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq] = {all.m, all.s / Reference(all.m, kLog2e).left_out(kLog2e)};
     }
@@ -252,7 +247,8 @@ __global__ void __launch_bounds__(512) bias_softmax_long_kernel(const __grid_con
         for (int64_t j0 = static_cast<int64_t>(t) * VEC - lead; j0 < end; j0 += G * VEC) {
             float z[VEC];
             load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
-            add_bias<VEC>(f, bias, w, j0, end, near_position(j0 - p), z);
+            add_bias<VEC>(f, bias, w, near_position(j0 - p), z);
+            mask<VEC>(j0, end, -INFINITY, z);
             float m = v.m;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) m = fmaxf(m, z[i]);
@@ -271,7 +267,8 @@ __global__ void __launch_bounds__(512) bias_softmax_long_kernel(const __grid_con
             for (int i = 0; i < VEC; ++i) z[i] = 0.f;
             if (j0 < end) {
                 load_slot<T, VEC>(in, j0, f.tk, 0.f, z);
-                add_bias<VEC>(f, bias, w, j0, end, near_position(j0 - p), z);
+                add_bias<VEC>(f, bias, w, near_position(j0 - p), z);
+            mask<VEC>(j0, end, -INFINITY, z);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) z[i] = exp2_fast(r.of(z[i], kLog2e)) * norm;
             }
@@ -379,59 +376,78 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 640 / Cta<G>::kThreads)
         const int p0 = near_position(q.position(iq));
         const T* in = scores.row(ib, ih, iq);
         const T* up = dprobs.row(ib, ih, iq);
-        const int j = t * VEC - row_lead<T, VEC>(in);
-        MaxSum all = stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq];
+        const int lead = row_lead<T, VEC>(in), j = t * VEC - lead;
         const int end = static_cast<int>(q.end(f, iq));
+        const Steps<VEC, G> steps(lead, end);
         Raw<T, VEC> s[SLOTS], dp[SLOTS];
 #pragma unroll
-        for (int c = 0; c < SLOTS; ++c)
-            if (j + c * G * VEC < end) {
-                s[c].load(in, j + c * G * VEC, n);
-                dp[c].load(up, j + c * G * VEC, end);
-            }
+        for (int c = 0; c < SLOTS; ++c) {
+            s[c].fetch(in, j + c * G * VEC, j + c * G * VEC < end, scores.extent);
+            dp[c].fetch(up, j + c * G * VEC, j + c * G * VEC < end, dprobs.extent);
+        }
+        const MaxSum all = stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq];
         const Reference r(all.m, kLog2e);
         const bool empty = all.s == 0.f;   // a row without keys, or none above -inf: all 0
         const float norm = empty ? 0.f : 1.f / (all.s * r.left_out(kLog2e));
-        float p[SLOTS][VEC], dot = 0.f;
+        float p[SLOTS][VEC];
+        float2 dot2 = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int c = 0; c < SLOTS; ++c) {
-            const int j0 = j + c * G * VEC;
-            if (j0 < end) {
+        for (int c = 0; c < SLOTS; ++c)
+            if (c < steps.some) {
+                const int j0 = j + c * G * VEC;
                 float d[VEC];
-                s[c].get(p[c]);
-                dp[c].get(d);
-                add_bias<VEC>(f, bias, w, j0, end, j0 - p0, p[c]);
+                if (c < steps.whole) {
+                    s[c].get(p[c]);
+                    dp[c].get(d);
+                } else {
+                    s[c].get(in, j0, n, scores.extent, p[c]);
+                    dp[c].get(up, j0, n, dprobs.extent, d);
+                }
+                add_bias<VEC>(f, bias, w, j0 - p0, p[c]);
                 exponentials(p[c], r, kLog2e);
                 multiply(p[c], norm);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) dot = fmaf(p[c][i], d[i], dot);
+                if (c >= steps.whole) {
+                    mask<VEC>(j0, end, 0.f, p[c]);
+                    mask<VEC>(j0, end, 0.f, d);
+                }
+                add_products(dot2, p[c], d);
             }
-        }
-        dot = group_sum<G>(dot, part, it / Cta<G>::kRows);
+        const float dot = group_sum<G>(dot2.x + dot2.y, part, it / Cta<G>::kRows);
         T* out = dscores.p != nullptr ? dscores.row(ib, ih, iq) : nullptr;
+        // steps [near, far) of this warp meet the window; those before lie left of it, those behind right
+        const int warp_j = j - (t & 31) * VEC - p0;
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
             const int j0 = j + c * G * VEC;
-            if (j0 < n) {
-                float dz[VEC];
-                if (j0 < end && !empty) {
+            float dz[VEC];
+            if (c < steps.some && !empty) {
+                if (c < steps.whole)
                     dp[c].get(dz);
+                else
+                    dp[c].get(up, j0, n, dprobs.extent, dz);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) dz[i] = p[c][i] * (dz[i] - dot);
-                    if (j0 < 0 || j0 + VEC > end) {
-#pragma unroll
-                        for (int i = 0; i < VEC; ++i)
-                            if (j0 + i < 0 || j0 + i >= end) dz[i] = 0.f;   // whatever dot is
-                    }
-                    if (partial != nullptr) add_diagonals<VEC>(f, sums, w, j0 - p0, dz, left, right);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) dz[i] = 0.f;
+                for (int i = 0; i < VEC; ++i) dz[i] -= dot;
+                multiply_by(dz, p[c]);
+                if (c >= steps.whole) mask<VEC>(j0, end, 0.f, dz);   // whatever dot is
+                if (partial != nullptr) {
+                    const int at = warp_j + c * G * VEC;   // of the warp's first key
+                    if (at + 32 * VEC <= -f.distance)
+                        add_up(left, dz);
+                    else if (at >= f.distance)
+                        add_up(right, dz);
+                    else
+                        add_diagonals<VEC>(f, sums, w, j0 - p0, dz, left, right);
                 }
-                if (out != nullptr) {
-                    multiply(dz, f.scale);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) dz[i] = 0.f;
+            }
+            if (out != nullptr) {
+                multiply(dz, f.scale);
+                if (c < steps.whole)
+                    store_whole<T, VEC>(out + j0, dz);
+                else if (j0 < n)
                     store_slot<T, VEC>(out, j0, n, dz);
-                }
             }
         }
         __syncwarp();  // the next row meets this row's diagonals through other lanes
@@ -479,7 +495,8 @@ __global__ void __launch_bounds__(256)
                 if (j0 < end) {
                     load_slot<T, VEC>(in, j0, f.tk, 0.f, p);
                     load_slot<T, VEC>(up, j0, end, 0.f, dp);
-                    add_bias<VEC>(f, bias, w, j0, end, near_position(j0 - p0), p);
+                    add_bias<VEC>(f, bias, w, near_position(j0 - p0), p);
+                    mask<VEC>(j0, end, -INFINITY, p);
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) p[i] = exp2_fast(r.of(p[i], kLog2e)) * norm;
                 }
@@ -578,7 +595,11 @@ template <typename K> int allow_smem(K kern, size_t bytes) {
     return e == cudaSuccess ? BZ_OK : cuda_failed(e);
 }
 
-template <typename T> Rows4<T> rows4(T* p, const int64_t* s) { return {p, p ? s[0] : 0, p ? s[1] : 0, p ? s[2] : 0}; }
+template <typename T> Rows4<T> rows4(T* p, const int64_t* s, int64_t b, const BiasForm& f) {
+    if (p == nullptr) return {};
+    return {p, s[0], s[1], s[2],
+            {reinterpret_cast<const char*>(p), reinterpret_cast<const char*>(p + (b - 1) * s[0] + (f.h - 1) * s[1] + (f.tq - 1) * s[2] + f.tk)}};
+}
 
 template <typename T, int VEC, int G, int SLOTS>
 int launch_forward(BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<T>& out, MaxSum* stats, cudaStream_t s) {
@@ -649,8 +670,8 @@ int64_t row_span(const void* p, const int64_t* strides, int64_t b, int64_t h, in
 
 template <typename T>
 int forward(BiasForm& f, int64_t b, const void* scores, const int64_t* ss, void* probs, const int64_t* sp, MaxSum* stats, cudaStream_t s) {
-    const auto in = rows4(static_cast<const T*>(scores), ss);
-    const auto out = rows4(static_cast<T*>(probs), sp);
+    const auto in = rows4(static_cast<const T*>(scores), ss, b, f);
+    const auto out = rows4(static_cast<T*>(probs), sp, b, f);
     if (f.distance <= kWideDistance && alike(scores, ss, probs, sp, b, f.h, f.tq, sizeof(T)))
         return dispatch_forward<T, Word<T>::kN>(f, row_span(scores, ss, b, f.h, f.tq, f.tk, sizeof(T)), b, in, out, stats, s);
     return dispatch_forward<T, 1>(f, f.tk, b, in, out, stats, s);
@@ -659,9 +680,9 @@ int forward(BiasForm& f, int64_t b, const void* scores, const int64_t* ss, void*
 template <typename T>
 int backward(const BiasForm& f, int64_t b, const void* scores, const int64_t* ss, const void* dprobs, const int64_t* sd, void* dscores,
              const int64_t* so, const MaxSum* stats, float* partial, cudaStream_t s) {
-    const auto in = rows4(static_cast<const T*>(scores), ss);
-    const auto up = rows4(static_cast<const T*>(dprobs), sd);
-    const auto out = rows4(static_cast<T*>(dscores), so);
+    const auto in = rows4(static_cast<const T*>(scores), ss, b, f);
+    const auto up = rows4(static_cast<const T*>(dprobs), sd, b, f);
+    const auto out = rows4(static_cast<T*>(dscores), so, b, f);
     if (f.distance <= kWideDistance && alike(scores, ss, dprobs, sd, b, f.h, f.tq, sizeof(T)) && (dscores == nullptr || alike(scores, ss, dscores, so, b, f.h, f.tq, sizeof(T))))
         return dispatch_backward<T, Word<T>::kN>(f, row_span(scores, ss, b, f.h, f.tq, f.tk, sizeof(T)), b, in, up, out, stats, partial, s);
     return dispatch_backward<T, 1>(f, f.tk, b, in, up, out, stats, partial, s);

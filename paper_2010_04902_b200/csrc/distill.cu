@@ -29,6 +29,7 @@ struct DistillArgs {
     int64_t ld, v, ld_d;
     const float* teacher;
     const int32_t* index;
+    Extent extent;               // of the logits
     int t;
     float temperature, c;        // c = log2(e) / T
     const float* dloss;
@@ -132,6 +133,16 @@ __device__ __forceinline__ MaxSum cta_join(const MaxSum& v, float c, MaxSum* par
     return warp_join(lane < (blockDim.x >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f}, c);
 }
 
+// -inf in the place of what is not the row's.
+template <int VEC> __device__ __forceinline__ void outside(int64_t j0, int64_t n, float (&x)[VEC]) {
+    if (j0 < 0 || j0 + VEC > n) {
+        rare();
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+            if (j0 + k < 0 || j0 + k >= n) x[k] = -INFINITY;
+    }
+}
+
 // One cluster a row.  HELD: the row's exponentials stay in registers; otherwise the row is read twice.
 template <typename T, int VEC, bool HELD>
 __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_constant__ DistillArgs a, const T* logits, T* dlogits) {
@@ -150,15 +161,12 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_const
     const int step = blockDim.x * VEC * (HELD ? 1 : ranks);
     if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // every CTA of the cluster has started
     float x[HELD ? kSlots : 1][VEC];
+    Raw<T, VEC> raw[HELD ? kSlots : 1];
     MaxSum mine{-INFINITY, 0.f};
     const int at0 = static_cast<int>(base) + threadIdx.x * VEC;   // HELD: at most 8 * 512 * 32
     if constexpr (HELD) {
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c) {
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) x[c][k] = -INFINITY;
-            if (at0 + c * step < n) load_slot<T, VEC>(row, at0 + c * step, n, -INFINITY, x[c]);
-        }
+        for (int c = 0; c < kSlots; ++c) raw[c].fetch(row, at0 + c * step, at0 + c * step < n, a.extent);
     }
     if (threadIdx.x < 32) {
         const bool any = teacher_row(a, row, i, e, 0, a.v);
@@ -166,18 +174,20 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_const
     }
     if constexpr (HELD) {
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c)
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) mine.m = fmaxf(mine.m, x[c][k]);
+        for (int c = 0; c < kSlots; ++c) {
+            raw[c].get(row, at0 + c * step, n, a.extent, x[c]);
+            outside<VEC>(at0 + c * step, n, x[c]);
+            mine.m = largest(mine.m, x[c]);
+        }
         mine.m = warp_max(mine.m);
         const Reference own(mine.m, a.c);
+        float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < kSlots; ++c) {
             exponentials(x[c], own, a.c);
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) mine.s += x[c][k];
+            add_up(sum, x[c]);
         }
-        mine.s = warp_sum(mine.s);
+        mine.s = warp_sum(sum.x + sum.y);
     } else {
         for (int64_t j0 = base + static_cast<int64_t>(threadIdx.x) * VEC; j0 < a.v; j0 += step) {
             load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[0]);
@@ -367,14 +377,18 @@ __global__ void __launch_bounds__(kStreamThreads, 1) distill_stream_kernel(const
             auto take = [&](int c, int s) {
 #pragma unroll
                 for (int k = 0; k < kMine; ++k) {
-                    if (!there(c, k)) break;
-                    const int in = k * kWorkers + static_cast<int>(threadIdx.x), word = c * kChunkWords + in;
-                    if (word >= w.begin && word < w.end) {
+                    const int in = k * kWorkers + static_cast<int>(threadIdx.x), first = c * kChunkWords + k * kWorkers, word = c * kChunkWords + in;
+                    if (first >= w.begin && first + kWorkers <= w.end) {   // all 512 of them whole
                         Word<T>::unpack(*reinterpret_cast<const uint4*>(ring + s * kChunkBytes + in * 16), x[k]);
-                    } else {
+                    } else if (there(c, k)) {
+                        if (word >= w.begin && word < w.end) {
+                            Word<T>::unpack(*reinterpret_cast<const uint4*>(ring + s * kChunkBytes + in * 16), x[k]);
+                        } else {
+                            rare();
 #pragma unroll
-                        for (int e = 0; e < N; ++e) x[k][e] = -INFINITY;
-                        if (word * N - w.lead < n) load_slot<T, N>(row, word * N - w.lead, n, -INFINITY, x[k]);
+                            for (int e = 0; e < N; ++e) x[k][e] = -INFINITY;
+                            if (word * N - w.lead < n) load_slot<T, N>(row, word * N - w.lead, n, -INFINITY, x[k]);
+                        }
                     }
                 }
             };
@@ -421,15 +435,19 @@ __global__ void __launch_bounds__(kStreamThreads, 1) distill_stream_kernel(const
                 if (lane == 0) mbar_arrive(&empty[s]);
 #pragma unroll
                 for (int k = 0; k < kMine; ++k) {
-                    const int j0 = (c * kChunkWords + k * kWorkers + static_cast<int>(threadIdx.x)) * N - w.lead;
-                    if (j0 >= n) break;
+                    const int first = c * kChunkWords + k * kWorkers, j0 = (first + static_cast<int>(threadIdx.x)) * N - w.lead;
+                    if (!there(c, k)) break;
                     exponentials(x[k], ref, a.c);
                     multiply(x[k], factor);
                     if (!any) {
+                        rare();
 #pragma unroll
                         for (int e = 0; e < N; ++e) x[k][e] = 0.f;
                     }
-                    store_slot<T, N>(out, j0, n, x[k]);
+                    if (first >= w.begin && first + kWorkers <= w.end)
+                        *reinterpret_cast<uint4*>(out + j0) = Word<T>::pack(x[k]);
+                    else if (j0 < n)
+                        store_slot<T, N>(out, j0, n, x[k]);
                 }
             }
             named_arrive(3 + static_cast<int>(r & 1));
@@ -453,11 +471,11 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(const __grid_cons
     const T* row = logits + i * a.ld;
     T* out = dlogits + i * a.ld_d;
     const int64_t base = share * (256 * kHeld) - row_lead<T, VEC>(row);
-    float x[kSlots][VEC];
+    Raw<T, VEC> raw[kSlots];
 #pragma unroll
     for (int c = 0; c < kSlots; ++c) {
         const int64_t j0 = base + (c * 256 + static_cast<int64_t>(threadIdx.x)) * VEC;
-        if (j0 < a.v) load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[c]);
+        raw[c].fetch(row, j0, j0 < a.v, a.extent);
     }
     if (threadIdx.x < 32) {
         const bool any = teacher_row(a, row, i, e, base, base + 256 * kHeld);
@@ -474,10 +492,16 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(const __grid_cons
     for (int c = 0; c < kSlots; ++c) {
         const int64_t j0 = base + (c * 256 + static_cast<int64_t>(threadIdx.x)) * VEC;
         if (j0 < a.v) {
-            exponentials(x[c], r, a.c);
+            float x[VEC];
+            raw[c].get(row, j0, a.v, a.extent, x);
+            exponentials(x, r, a.c);
+            multiply(x, factor);
+            if (!any) {
+                rare();
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) x[c][k] = any ? x[c][k] * factor : 0.f;
-            store_slot<T, VEC>(out, j0, a.v, x[c]);
+                for (int k = 0; k < VEC; ++k) x[k] = 0.f;
+            }
+            store_slot<T, VEC>(out, j0, a.v, x);
         }
     }
     __syncthreads();
@@ -566,6 +590,11 @@ int check(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const
     return BZ_OK;
 }
 
+Extent extent_of(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v) {
+    const char* p = static_cast<const char*>(logits);
+    return {p, p + ((m - 1) * ld + v) * element_bytes(dtype)};
+}
+
 }  // namespace
 
 int distill_timeouts(unsigned int* count) {
@@ -589,7 +618,7 @@ extern "C" int bz_distill(const void* logits, int64_t ld, int dtype, int64_t m, 
         note_launch();
         return check_launch();
     }
-    const DistillArgs a{ld, v, ld_d, teacher, index, t, temperature, kLog2e / temperature, dloss, loss, reinterpret_cast<MaxSum*>(stats)};
+    const DistillArgs a{ld, v, ld_d, teacher, index, extent_of(logits, ld, dtype, m, v), t, temperature, kLog2e / temperature, dloss, loss, reinterpret_cast<MaxSum*>(stats)};
     if (dtype == BZ_F32) return dispatch<float>(a, m, logits, dlogits, false, s);
     if (dtype == BZ_F16) return dispatch<__half>(a, m, logits, dlogits, false, s);
     return dispatch<__nv_bfloat16>(a, m, logits, dlogits, false, s);
@@ -603,7 +632,7 @@ extern "C" int bz_distill_backward(const void* logits, int64_t ld, int dtype, in
     if (m == 0 || v == 0) return BZ_OK;
     if (stats == nullptr || !aligned8(stats) || dlogits == nullptr) return BZ_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const DistillArgs a{ld, v, ld_d, teacher, index, t, temperature, kLog2e / temperature, dloss, nullptr, reinterpret_cast<MaxSum*>(const_cast<float*>(stats))};
+    const DistillArgs a{ld, v, ld_d, teacher, index, extent_of(logits, ld, dtype, m, v), t, temperature, kLog2e / temperature, dloss, nullptr, reinterpret_cast<MaxSum*>(const_cast<float*>(stats))};
     if (dtype == BZ_F32) return dispatch<float>(a, m, logits, dlogits, true, s);
     if (dtype == BZ_F16) return dispatch<__half>(a, m, logits, dlogits, true, s);
     return dispatch<__nv_bfloat16>(a, m, logits, dlogits, true, s);

@@ -36,14 +36,20 @@ template <typename T> __device__ __forceinline__ void mma_few(float (&c)[4], uin
 }
 
 // Eight 16-bit elements from `p`, of which `n` exist (n <= 0: none); the others are zero.  WIDE: p on a 16-byte boundary.
+// The load is one instruction under a predicate: one under a branch would end in a copy that waits for it.
 template <bool WIDE> __device__ __forceinline__ uint4 load_eight(const uint16_t* p, int64_t n) {
-    if (WIDE && n >= 8) return __ldg(reinterpret_cast<const uint4*>(p));
     uint32_t w[4] = {0, 0, 0, 0};
-    if (n > 0) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) w[i / 2] |= static_cast<uint32_t>(__ldg(p + i)) << (i % 2 * 16);
+    if constexpr (WIDE) {
+        const int go = n >= 8;
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n@p ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%5];\n}\n"
+                     : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])
+                     : "r"(go), "l"(p));
+        if (n <= 0 || n >= 8) return make_uint4(w[0], w[1], w[2], w[3]);
+        asm volatile("");   // rare: the last elements of a row whose length is no multiple of eight
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) w[i / 2] |= static_cast<uint32_t>(__ldg(p + i)) << (i % 2 * 16);
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 

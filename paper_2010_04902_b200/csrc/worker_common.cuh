@@ -148,6 +148,73 @@ __device__ __forceinline__ float warp_max(float v) {
     return m;
 }
 
+// ---- loads that stay in flight -------------------------------------------------------------------
+
+// Bounds of a tensor's memory: from its first element to behind its last.
+struct Extent {
+    const char *begin, *end;
+};
+// A slot as it was loaded.  A load under a branch ends in a copy of its registers, and a copy waits for the load; so the load
+// is one instruction under a predicate, into registers that keep what they held.  A slot that reaches over an end of its
+// row is read whole as long as its 16 bytes lie in the tensor (what is not the row's is masked later); the few that would
+// leave the tensor are read element by element when they are used.
+template <typename T, int VEC> struct Raw {
+    uint32_t w[4] = {0, 0, 0, 0};
+    __device__ __forceinline__ void fetch(const T* row, int64_t j0, bool wanted, const Extent& x) {
+        const char* p = reinterpret_cast<const char*>(row + j0);
+        const int go = wanted && p >= x.begin && p + 16 <= x.end;
+        asm volatile(
+            "{\n"
+            ".reg .pred p;\n"
+            "setp.ne.b32 p, %4, 0;\n"
+            "@p ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%5];\n"
+            "}\n"
+            : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])
+            : "r"(go), "l"(p));
+    }
+    __device__ __forceinline__ void get(float (&x)[VEC]) const { Word<T>::unpack(make_uint4(w[0], w[1], w[2], w[3]), x); }
+    // whatever was fetched: elements [0, n) of the row, the others undefined
+    __device__ __forceinline__ void get(const T* row, int64_t j0, int64_t n, const Extent& b, float (&x)[VEC]) const {
+        get(x);
+        const char* p = reinterpret_cast<const char*>(row + j0);
+        if (p < b.begin || p + 16 > b.end) {
+            asm volatile("");   // rare: keep it a branch
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[i] = j0 + i >= 0 && j0 + i < n ? to_f32(row[j0 + i]) : 0.f;
+        }
+    }
+};
+template <typename T> struct Raw<T, 1> {
+    uint32_t w = 0;
+    __device__ __forceinline__ void fetch(const T* row, int64_t j0, bool wanted, const Extent&) {
+        const int go = wanted;
+        if constexpr (sizeof(T) == 4) {
+            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.cs.u32 %0, [%2];\n}\n" : "+r"(w) : "r"(go), "l"(row + j0));
+        } else {
+            uint16_t h = static_cast<uint16_t>(w);
+            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.cs.u16 %0, [%2];\n}\n" : "+h"(h) : "r"(go), "l"(row + j0));
+            w = h;
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[1]) const {
+        if constexpr (sizeof(T) == 4) {
+            x[0] = __uint_as_float(w);
+        } else {
+            T e;
+            const uint16_t h = static_cast<uint16_t>(w);
+            memcpy(&e, &h, 2);
+            x[0] = to_f32(e);
+        }
+    }
+    __device__ __forceinline__ void get(const T*, int64_t, int64_t, const Extent&, float (&x)[1]) const { get(x); }
+};
+template <typename T, int VEC> __device__ __forceinline__ void store_whole(T* p, const float (&x)[VEC]) {
+    if constexpr (VEC == 1)
+        *p = from_f32<T>(x[0]);
+    else
+        *reinterpret_cast<uint4*>(p) = Word<T>::pack(x);
+}
+
 // ---- arrays in registers, two elements an instruction where there are two -------------------------
 
 // x[i] = x[i]*a + b[i]
@@ -175,6 +242,29 @@ template <int N> __device__ __forceinline__ void multiply(float (&x)[N], float a
         for (int i = 0; i < N; ++i) x[i] *= a;
     }
 }
+// x[i] *= a[i]
+template <int N> __device__ __forceinline__ void multiply_by(float (&x)[N], const float (&a)[N]) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 y = __fmul2_rn(make_float2(x[i], x[i + 1]), make_float2(a[i], a[i + 1]));
+            x[i] = y.x, x[i + 1] = y.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] *= a[i];
+    }
+}
+// s += x*y in two partial sums.
+template <int N> __device__ __forceinline__ void add_products(float2& s, const float (&x)[N], const float (&y)[N]) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) s = __ffma2_rn(make_float2(x[i], x[i + 1]), make_float2(y[i], y[i + 1]), s);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s.x = fmaf(x[i], y[i], s.x);
+    }
+}
 // Largest of m and x (NaNs do not count).
 template <int N> __device__ __forceinline__ float largest(float m, const float (&x)[N]) {
     if constexpr (N % 2 == 0) {
@@ -196,17 +286,19 @@ template <int N> __device__ __forceinline__ void add_up(float2& s, const float (
         for (int i = 0; i < N; ++i) s.x += x[i];
     }
 }
+// Keeps what follows in a branch of its own: not worth executing under a predicate.
+__device__ __forceinline__ void rare() { asm volatile(""); }
 // x[i] = 2^(exponent of x[i]) relative to r.
 template <int N> __device__ __forceinline__ void exponentials(float (&x)[N], const Reference& r, float c) {
-    if (!r.apart) {
-        float b[N];
+    if (r.apart) {
+        rare();
 #pragma unroll
-        for (int i = 0; i < N; ++i) b[i] = -r.mc;
-        multiply_add(x, c, b);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = (x[i] - r.m) * c;
+        for (int i = 0; i < N; ++i) x[i] -= r.m;
     }
+    float b[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) b[i] = r.apart ? 0.f : -r.mc;
+    multiply_add(x, c, b);
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = exp2_fast(x[i]);
 }
