@@ -58,6 +58,8 @@ template <int VEC> struct Window {
     int slots;   // per copy
     __host__ __device__ explicit Window(int distance) : slots((2 * distance + VEC - 1) / VEC + 3) {}
     __host__ __device__ int floats() const { return VEC * slots * VEC; }
+    // value indices run over [-2*VEC, values() - 2*VEC)
+    __host__ __device__ int values() const { return VEC * (slots + 1); }
     __device__ __forceinline__ int at(int a, int slot, int group) const { return ((a * kGroups + group) * slots + slot) * kIn; }
     // copy and slot of relative position rel
     __device__ __forceinline__ void place(int rel, int distance, int& a, int& slot) const {
@@ -71,10 +73,12 @@ template <int VEC> struct Window {
 template <int VEC> __device__ __forceinline__ void build_bias(const BiasForm& f, int head, const Window<VEC>& w, float* plain, float* bias) {
     for (int d = threadIdx.x; d <= 2 * f.distance; d += blockDim.x) plain[d] = f.table[bucket_of(f, d - f.distance) * f.h + head];
     __syncthreads();
-    for (int e = threadIdx.x; e < VEC * w.slots * Window<VEC>::kGroups; e += blockDim.x) {
-        const int slot = e % w.slots, group = e / w.slots % Window<VEC>::kGroups, a = e / w.slots / Window<VEC>::kGroups;
-        for (int i = 0; i < Window<VEC>::kIn; ++i)
-            bias[w.at(a, slot, group) + i] = plain[max(0, min(2 * f.distance, w.index(a, slot, group * Window<VEC>::kIn + i)))];
+    constexpr int kGroups = Window<VEC>::kGroups, kIn = Window<VEC>::kIn;
+    for (int o = threadIdx.x >> 5; o < VEC * kGroups; o += blockDim.x >> 5) {   // a warp one copy's half
+        const int a = o / kGroups, group = o % kGroups;
+        for (int slot = threadIdx.x & 31; slot < w.slots; slot += 32)
+#pragma unroll
+            for (int i = 0; i < kIn; ++i) bias[w.at(a, slot, group) + i] = plain[max(0, min(2 * f.distance, w.index(a, slot, group * kIn + i)))];
     }
 }
 template <int VEC> __device__ __forceinline__ void window_load(const float* table, const Window<VEC>& w, int a, int slot, float (&x)[VEC]) {
@@ -162,21 +166,26 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
     const int t = threadIdx.x % G, ib = blockIdx.z, ih = blockIdx.y, n = static_cast<int>(f.tk);
     const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta + threadIdx.x / G;
     const Queries q(f, ib);
+    const int rows = static_cast<int>(min(static_cast<int64_t>(f.rows_per_cta), f.tq - first));   // it < rows: this group's (may be <= 0)
+    const T* in = scores.row(ib, ih, first);
+    T* out = probs.row(ib, ih, first);
+    const int64_t in_step = Cta<G>::kRows * scores.q, out_step = Cta<G>::kRows * probs.q;
     Raw<T, VEC> raw[SLOTS];
-    auto fetch = [&](int64_t iq) {
-        const T* in = scores.row(ib, ih, iq);
-        const int j = t * VEC - row_lead<T, VEC>(in), end = static_cast<int>(q.end(f, iq));
+    auto fetch = [&](const T* row, int64_t iq) {
+        const int lead = row_lead<T, VEC>(row), j = t * VEC - lead, end = static_cast<int>(q.end(f, iq));
+        const bool safe = scores.extent.around(row, n);
 #pragma unroll
-        for (int c = 0; c < SLOTS; ++c) raw[c].fetch(in, j + c * G * VEC, j + c * G * VEC < end, scores.extent);
+        for (int c = 0; c < SLOTS; ++c) {
+            const int j0 = j + c * G * VEC;
+            raw[c].fetch(row + j0, j0 < end && (safe || VEC == 1 || (j0 >= 0 && j0 + VEC <= n)));
+        }
     };
-    if (first < f.tq) fetch(first);
+    if (rows > 0) fetch(in, first);
     build_bias<VEC>(f, ih, w, bias + w.floats(), bias);
     __syncthreads();
-    for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
+    for (int it = 0; it < rows; it += Cta<G>::kRows, in += in_step, out += out_step) {   // G > 32: the whole CTA alike
         const int64_t iq = first + it;
-        if (iq >= f.tq) break;   // G > 32: the whole CTA; otherwise this warp
         const int p = near_position(q.position(iq)), end = static_cast<int>(q.end(f, iq));
-        const T* in = scores.row(ib, ih, iq);
         const int lead = row_lead<T, VEC>(in), j = t * VEC - lead;
         const Steps<VEC, G> steps(lead, end);
         float z[SLOTS][VEC];
@@ -185,15 +194,13 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
         for (int c = 0; c < SLOTS; ++c)
             if (c < steps.some) {
                 const int j0 = j + c * G * VEC;
-                if (c < steps.whole)
-                    raw[c].get(z[c]);
-                else
-                    raw[c].get(in, j0, n, scores.extent, z[c]);
+                raw[c].get(z[c]);
+                if (VEC > 1 && c >= steps.whole && (j0 < 0 || j0 + VEC > n) && !scores.extent.around(in, n)) read_apart<T, VEC>(in, j0, n, z[c]);
                 add_bias<VEC>(f, bias, w, j0 - p, z[c]);
                 if (c >= steps.whole) mask<VEC>(j0, end, -INFINITY, z[c]);
                 top = largest(top, z[c]);
             }
-        if (it + Cta<G>::kRows < f.rows_per_cta && iq + Cta<G>::kRows < f.tq) fetch(iq + Cta<G>::kRows);
+        if (it + Cta<G>::kRows < rows) fetch(in + in_step, iq + Cta<G>::kRows);
         MaxSum v{warp_max(top), 0.f};
         const Reference own(v.m, kLog2e);
         float2 sum = make_float2(0.f, 0.f);
@@ -207,7 +214,6 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
         const MaxSum all = group_join<G>(v, kLog2e, part, it / Cta<G>::kRows);
         float norm = all.s == 0.f ? 0.f : 1.f / all.s;
         if (G > 32 && v.s != 0.f) norm *= exp2_fast(Reference(all.m, kLog2e).of_part(v.m, kLog2e));
-        T* out = probs.row(ib, ih, iq);
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
             const int j0 = j + c * G * VEC;
@@ -304,55 +310,54 @@ __device__ __forceinline__ void add_diagonals(const BiasForm& f, float* sums, co
     }
 }
 
-// What the rows of a CTA leave for the table.  Each warp's far sums take the first and last slot of its copy 0 (both ends
-// of the table's values); then, distance by distance, warps and copies are added in order, and distances by bucket.
+// What the rows of a CTA leave for the table.  Each warp's far sums take the first and last slot of its copy 0; then warps
+// and copies are added in order, value index by value index, and a warp a bucket adds its distances (those beyond the
+// window belong to the last bucket of their side).
 template <int VEC>
-__device__ __forceinline__ void leave_buckets(const BiasForm& f, float* all_sums, const Window<VEC>& w, int warps, float2 left2, float2 right2, float* by_distance, float* mine) {
+__device__ __forceinline__ void leave_buckets(const BiasForm& f, float* all_sums, const Window<VEC>& w, int warps, float2 left2, float2 right2, float* by_value, float* mine) {
     const float left = warp_sum(left2.x + left2.y), right = warp_sum(right2.x + right2.y);
-    if ((threadIdx.x & 31) == 0) {
-        float* sums = all_sums + (threadIdx.x >> 5) * w.floats();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, values = w.values();
+    if (lane == 0) {
+        float* sums = all_sums + warp * w.floats();
         sums[w.at(0, 0, 0)] = left;
         sums[w.at(0, w.slots - 1, 0)] = right;
     }
     __syncthreads();
-    const int ends = 2 * f.distance;
-    for (int d = threadIdx.x; d <= ends; d += blockDim.x) {
-        // elements (a, slot, i) with value index d; indices outside belong to the ends
+    for (int v = threadIdx.x; v < values; v += blockDim.x) {
         float s = 0.f;
         for (int k = 0; k < warps; ++k) {
             const float* sums = all_sums + k * w.floats();
+#pragma unroll
             for (int a = 0; a < VEC; ++a) {
-                if (d > 0 && d < ends) {
-                    const int e = d - a + 2 * VEC;   // VEC*slot + i
-                    s += sums[w.at(a, e / VEC, e % VEC / Window<VEC>::kIn) + e % VEC % Window<VEC>::kIn];
-                } else {
-                    const int from = d == 0 ? 0 : max(0, ends - a + 2 * VEC), to = d == 0 ? 2 * VEC - a : VEC * w.slots - 1;
-                    for (int e = from; e <= to; ++e) s += sums[w.at(a, e / VEC, e % VEC / Window<VEC>::kIn) + e % VEC % Window<VEC>::kIn];
-                }
+                const int e = v - a;   // VEC*slot + i
+                if (e >= 0 && e < VEC * w.slots) s += sums[w.at(a, e / VEC, e % VEC / Window<VEC>::kIn) + e % VEC % Window<VEC>::kIn];
             }
         }
-        by_distance[d] = s;
+        by_value[v] = s;
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < f.buckets; c += blockDim.x) {
+    const float* at = by_value + 2 * VEC + f.distance;   // at[rel]
+    for (int c = warp; c < f.buckets; c += warps) {
         const int k = f.bidirectional && c >= f.nb ? c - f.nb : c;
-        const int lo = k < f.exact ? k : f.starts[k - f.exact];
-        const int hi = k < f.exact ? k + 1 : (k == f.nb - 1 ? f.distance + 1 : f.starts[k - f.exact + 1]);
+        const bool last = k == f.nb - 1;
+        const int lo = k < f.exact ? k : f.starts[k - f.exact], hi = k < f.exact && !last ? k + 1 : (last ? values : f.starts[k - f.exact + 1]);
+        const int most_left = f.distance + 2 * VEC, most_right = values - 1 - most_left;   // largest distances there are
         float s = 0.f;
         if (c != k) {
-            for (int n = max(lo, 1); n < hi; ++n) s += by_distance[f.distance + n];
+            for (int n = max(lo, 1) + lane; n < hi && n <= most_right; n += 32) s += at[n];
         } else {
-            for (int n = lo; n < hi; ++n) s += by_distance[f.distance - n];
+            for (int n = lo + lane; n < hi && n <= most_left; n += 32) s += at[-n];
             if (!f.bidirectional && c == 0)
-                for (int n = 1; n <= f.distance; ++n) s += by_distance[f.distance + n];
+                for (int n = 1 + lane; n <= most_right; n += 32) s += at[n];
         }
-        mine[c] = s;
+        s = warp_sum(s);
+        if (lane == 0) mine[c] = s;
     }
 }
 
 // SLOTS slots of scores and of dprobs a thread are held: p in binary32, dprobs as loaded.
 template <typename T, int VEC, int G, int SLOTS>
-__global__ void __launch_bounds__(Cta<G>::kThreads, 640 / Cta<G>::kThreads)
+__global__ void __launch_bounds__(Cta<G>::kThreads, 512 / Cta<G>::kThreads)
     bias_softmax_backward_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<const T> dprobs,
                                  const Rows4<T> dscores, const MaxSum* __restrict__ stats, float* __restrict__ partial) {
     extern __shared__ __align__(16) float bias[];
@@ -370,22 +375,28 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 640 / Cta<G>::kThreads)
     __syncthreads();
     float2 left = make_float2(0.f, 0.f), right = left;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta + threadIdx.x / G;
-    for (int it = 0; it < f.rows_per_cta; it += Cta<G>::kRows) {
+    const int rows = static_cast<int>(min(static_cast<int64_t>(f.rows_per_cta), f.tq - first));   // it < rows: this group's
+    const T* in = scores.row(ib, ih, first);
+    const T* up = dprobs.row(ib, ih, first);
+    T* out = dscores.p != nullptr ? dscores.row(ib, ih, first) : nullptr;
+    const MaxSum* stat = stats + (static_cast<int64_t>(ib) * f.h + ih) * f.tq + first;
+    constexpr int kRows = Cta<G>::kRows;
+    Raw<T, VEC> s[SLOTS], dp[SLOTS];
+    for (int it = 0; it < rows; it += kRows, in += kRows * scores.q, up += kRows * dprobs.q, out += kRows * dscores.q, stat += kRows) {
         const int64_t iq = first + it;
-        if (iq >= f.tq) break;
         const int p0 = near_position(q.position(iq));
-        const T* in = scores.row(ib, ih, iq);
-        const T* up = dprobs.row(ib, ih, iq);
         const int lead = row_lead<T, VEC>(in), j = t * VEC - lead;
         const int end = static_cast<int>(q.end(f, iq));
         const Steps<VEC, G> steps(lead, end);
-        Raw<T, VEC> s[SLOTS], dp[SLOTS];
+        const bool safe = VEC == 1 || (scores.extent.around(in, n) && dprobs.extent.around(up, n));
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
-            s[c].fetch(in, j + c * G * VEC, j + c * G * VEC < end, scores.extent);
-            dp[c].fetch(up, j + c * G * VEC, j + c * G * VEC < end, dprobs.extent);
+            const int j0 = j + c * G * VEC;
+            const bool go = j0 < end && (safe || (j0 >= 0 && j0 + VEC <= n));
+            s[c].fetch(in + j0, go);
+            dp[c].fetch(up + j0, go);
         }
-        const MaxSum all = stats[(static_cast<int64_t>(ib) * f.h + ih) * f.tq + iq];
+        const MaxSum all = *stat;
         const Reference r(all.m, kLog2e);
         const bool empty = all.s == 0.f;   // a row without keys, or none above -inf: all 0
         const float norm = empty ? 0.f : 1.f / (all.s * r.left_out(kLog2e));
@@ -396,12 +407,11 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 640 / Cta<G>::kThreads)
             if (c < steps.some) {
                 const int j0 = j + c * G * VEC;
                 float d[VEC];
-                if (c < steps.whole) {
-                    s[c].get(p[c]);
-                    dp[c].get(d);
-                } else {
-                    s[c].get(in, j0, n, scores.extent, p[c]);
-                    dp[c].get(up, j0, n, dprobs.extent, d);
+                s[c].get(p[c]);
+                dp[c].get(d);
+                if (c >= steps.whole && !safe && (j0 < 0 || j0 + VEC > n)) {
+                    read_apart<T, VEC>(in, j0, n, p[c]);
+                    read_apart<T, VEC>(up, j0, n, d);
                 }
                 add_bias<VEC>(f, bias, w, j0 - p0, p[c]);
                 exponentials(p[c], r, kLog2e);
@@ -413,18 +423,15 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 640 / Cta<G>::kThreads)
                 add_products(dot2, p[c], d);
             }
         const float dot = group_sum<G>(dot2.x + dot2.y, part, it / Cta<G>::kRows);
-        T* out = dscores.p != nullptr ? dscores.row(ib, ih, iq) : nullptr;
-        // steps [near, far) of this warp meet the window; those before lie left of it, those behind right
+        // a warp's step may meet the window, lie left of it or right
         const int warp_j = j - (t & 31) * VEC - p0;
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
             const int j0 = j + c * G * VEC;
             float dz[VEC];
             if (c < steps.some && !empty) {
-                if (c < steps.whole)
-                    dp[c].get(dz);
-                else
-                    dp[c].get(up, j0, n, dprobs.extent, dz);
+                dp[c].get(dz);
+                if (c >= steps.whole && !safe && (j0 < 0 || j0 + VEC > n)) read_apart<T, VEC>(up, j0, n, dz);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) dz[i] -= dot;
                 multiply_by(dz, p[c]);
@@ -633,7 +640,8 @@ int dispatch_forward(BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in
 template <typename T, int VEC, int G, int SLOTS>
 int launch_backward(const BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out, const MaxSum* stats,
                     float* partial, cudaStream_t s) {
-    const size_t smem = (Window<VEC>(f.distance).floats() * (1 + (partial != nullptr ? Cta<G>::kThreads / 32 : 0)) + 2 * f.distance + 1) * sizeof(float);
+    const Window<VEC> w(f.distance);
+    const size_t smem = (w.floats() * (1 + (partial != nullptr ? Cta<G>::kThreads / 32 : 0)) + w.values()) * sizeof(float);
     const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
     int st;
     if constexpr (SLOTS == 0) {

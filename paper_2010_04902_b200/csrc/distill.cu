@@ -143,6 +143,11 @@ template <int VEC> __device__ __forceinline__ void outside(int64_t j0, int64_t n
     }
 }
 
+// Whether a slot of the row can be read whole.
+template <int VEC> __device__ __forceinline__ bool fetchable(int64_t j0, int64_t n, bool safe) {
+    return j0 < n && (safe || (j0 >= 0 && j0 + VEC <= n));
+}
+
 // One cluster a row.  HELD: the row's exponentials stay in registers; otherwise the row is read twice.
 template <typename T, int VEC, bool HELD>
 __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_constant__ DistillArgs a, const T* logits, T* dlogits) {
@@ -162,11 +167,12 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_const
     if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // every CTA of the cluster has started
     float x[HELD ? kSlots : 1][VEC];
     Raw<T, VEC> raw[HELD ? kSlots : 1];
+    const bool safe = a.extent.around(row, a.v);
     MaxSum mine{-INFINITY, 0.f};
     const int at0 = static_cast<int>(base) + threadIdx.x * VEC;   // HELD: at most 8 * 512 * 32
     if constexpr (HELD) {
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c) raw[c].fetch(row, at0 + c * step, at0 + c * step < n, a.extent);
+        for (int c = 0; c < kSlots; ++c) raw[c].fetch(row + at0 + c * step, fetchable<VEC>(at0 + c * step, n, safe));
     }
     if (threadIdx.x < 32) {
         const bool any = teacher_row(a, row, i, e, 0, a.v);
@@ -175,7 +181,8 @@ __global__ void __launch_bounds__(kMaxThreads) distill_kernel(const __grid_const
     if constexpr (HELD) {
 #pragma unroll
         for (int c = 0; c < kSlots; ++c) {
-            raw[c].get(row, at0 + c * step, n, a.extent, x[c]);
+            raw[c].get(x[c]);
+            if (at0 + c * step < n && !fetchable<VEC>(at0 + c * step, n, safe)) read_apart<T, VEC>(row, at0 + c * step, n, x[c]);
             outside<VEC>(at0 + c * step, n, x[c]);
             mine.m = largest(mine.m, x[c]);
         }
@@ -472,10 +479,11 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(const __grid_cons
     T* out = dlogits + i * a.ld_d;
     const int64_t base = share * (256 * kHeld) - row_lead<T, VEC>(row);
     Raw<T, VEC> raw[kSlots];
+    const bool safe = a.extent.around(row, a.v);
 #pragma unroll
     for (int c = 0; c < kSlots; ++c) {
         const int64_t j0 = base + (c * 256 + static_cast<int64_t>(threadIdx.x)) * VEC;
-        raw[c].fetch(row, j0, j0 < a.v, a.extent);
+        raw[c].fetch(row + j0, fetchable<VEC>(j0, a.v, safe));
     }
     if (threadIdx.x < 32) {
         const bool any = teacher_row(a, row, i, e, base, base + 256 * kHeld);
@@ -493,7 +501,8 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(const __grid_cons
         const int64_t j0 = base + (c * 256 + static_cast<int64_t>(threadIdx.x)) * VEC;
         if (j0 < a.v) {
             float x[VEC];
-            raw[c].get(row, j0, a.v, a.extent, x);
+            raw[c].get(x);
+            if (!fetchable<VEC>(j0, a.v, safe)) read_apart<T, VEC>(row, j0, a.v, x);
             exponentials(x, r, a.c);
             multiply(x, factor);
             if (!any) {

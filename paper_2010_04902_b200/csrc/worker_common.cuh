@@ -153,16 +153,18 @@ __device__ __forceinline__ float warp_max(float v) {
 // Bounds of a tensor's memory: from its first element to behind its last.
 struct Extent {
     const char *begin, *end;
+    // whether every 16-byte word that a row of n elements touches lies in the tensor
+    template <typename T> __device__ __forceinline__ bool around(const T* row, int64_t n) const {
+        return reinterpret_cast<const char*>(row) - 16 >= begin && reinterpret_cast<const char*>(row + n) + 16 <= end;
+    }
 };
 // A slot as it was loaded.  A load under a branch ends in a copy of its registers, and a copy waits for the load; so the load
 // is one instruction under a predicate, into registers that keep what they held.  A slot that reaches over an end of its
-// row is read whole as long as its 16 bytes lie in the tensor (what is not the row's is masked later); the few that would
-// leave the tensor are read element by element when they are used.
+// row is read whole where the tensor goes on (what is not the row's is masked later); in the few rows at the tensor's ends
+// it is read element by element when it is used.
 template <typename T, int VEC> struct Raw {
     uint32_t w[4] = {0, 0, 0, 0};
-    __device__ __forceinline__ void fetch(const T* row, int64_t j0, bool wanted, const Extent& x) {
-        const char* p = reinterpret_cast<const char*>(row + j0);
-        const int go = wanted && p >= x.begin && p + 16 <= x.end;
+    __device__ __forceinline__ void fetch(const T* p, bool go) {
         asm volatile(
             "{\n"
             ".reg .pred p;\n"
@@ -170,29 +172,18 @@ template <typename T, int VEC> struct Raw {
             "@p ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%5];\n"
             "}\n"
             : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])
-            : "r"(go), "l"(p));
+            : "r"(static_cast<int>(go)), "l"(p));
     }
     __device__ __forceinline__ void get(float (&x)[VEC]) const { Word<T>::unpack(make_uint4(w[0], w[1], w[2], w[3]), x); }
-    // whatever was fetched: elements [0, n) of the row, the others undefined
-    __device__ __forceinline__ void get(const T* row, int64_t j0, int64_t n, const Extent& b, float (&x)[VEC]) const {
-        get(x);
-        const char* p = reinterpret_cast<const char*>(row + j0);
-        if (p < b.begin || p + 16 > b.end) {
-            asm volatile("");   // rare: keep it a branch
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) x[i] = j0 + i >= 0 && j0 + i < n ? to_f32(row[j0 + i]) : 0.f;
-        }
-    }
 };
 template <typename T> struct Raw<T, 1> {
     uint32_t w = 0;
-    __device__ __forceinline__ void fetch(const T* row, int64_t j0, bool wanted, const Extent&) {
-        const int go = wanted;
+    __device__ __forceinline__ void fetch(const T* p, bool go) {
         if constexpr (sizeof(T) == 4) {
-            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.cs.u32 %0, [%2];\n}\n" : "+r"(w) : "r"(go), "l"(row + j0));
+            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.cs.u32 %0, [%2];\n}\n" : "+r"(w) : "r"(static_cast<int>(go)), "l"(p));
         } else {
             uint16_t h = static_cast<uint16_t>(w);
-            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.cs.u16 %0, [%2];\n}\n" : "+h"(h) : "r"(go), "l"(row + j0));
+            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.cs.u16 %0, [%2];\n}\n" : "+h"(h) : "r"(static_cast<int>(go)), "l"(p));
             w = h;
         }
     }
@@ -206,8 +197,15 @@ template <typename T> struct Raw<T, 1> {
             x[0] = to_f32(e);
         }
     }
-    __device__ __forceinline__ void get(const T*, int64_t, int64_t, const Extent&, float (&x)[1]) const { get(x); }
 };
+// Keeps what follows in a branch of its own: not worth executing under a predicate.
+__device__ __forceinline__ void rare() { asm volatile(""); }
+// For a slot that was not fetched because it reaches over an end of a tensor.
+template <typename T, int VEC> __device__ __forceinline__ void read_apart(const T* row, int64_t j0, int64_t n, float (&x)[VEC]) {
+    rare();
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x[i] = j0 + i >= 0 && j0 + i < n ? to_f32(row[j0 + i]) : 0.f;
+}
 template <typename T, int VEC> __device__ __forceinline__ void store_whole(T* p, const float (&x)[VEC]) {
     if constexpr (VEC == 1)
         *p = from_f32<T>(x[0]);
@@ -286,8 +284,6 @@ template <int N> __device__ __forceinline__ void add_up(float2& s, const float (
         for (int i = 0; i < N; ++i) s.x += x[i];
     }
 }
-// Keeps what follows in a branch of its own: not worth executing under a predicate.
-__device__ __forceinline__ void rare() { asm volatile(""); }
 // x[i] = 2^(exponent of x[i]) relative to r.
 template <int N> __device__ __forceinline__ void exponentials(float (&x)[N], const Reference& r, float c) {
     if (r.apart) {
