@@ -56,7 +56,8 @@ __device__ __forceinline__ int bucket_of(const BiasForm& f, int rel) {
 template <int VEC> struct Window {
     static constexpr int kGroups = VEC / 4 > 0 ? VEC / 4 : 1, kIn = VEC / kGroups;
     int slots;   // per copy
-    __host__ __device__ explicit Window(int distance) : slots((2 * distance + VEC - 1) / VEC + 3) {}
+    // VEC == 1: rounded up to whole 16-byte words
+    __host__ __device__ explicit Window(int distance) : slots(VEC == 1 ? (2 * distance + 6) / 4 * 4 : (2 * distance + VEC - 1) / VEC + 3) {}
     __host__ __device__ int floats() const { return VEC * slots * VEC; }
     // value indices run over [-2*VEC, values() - 2*VEC)
     __host__ __device__ int values() const { return VEC * (slots + 1); }
@@ -157,7 +158,8 @@ template <int G> __device__ __forceinline__ float group_sum(float v, float (*par
 }
 
 // SLOTS slots a thread are held in registers, and the next row's are loaded before this row's are used.
-template <typename T, int VEC, int G, int SLOTS>
+// WHOLE: every slot of every row holds seen keys only - no test, no mask.
+template <typename T, int VEC, int G, int SLOTS, bool WHOLE>
 __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
     bias_softmax_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<T> probs, MaxSum* stats) {
     extern __shared__ __align__(16) float bias[];
@@ -172,12 +174,12 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
     const int64_t in_step = Cta<G>::kRows * scores.q, out_step = Cta<G>::kRows * probs.q;
     Raw<T, VEC> raw[SLOTS];
     auto fetch = [&](const T* row, int64_t iq) {
-        const int lead = row_lead<T, VEC>(row), j = t * VEC - lead, end = static_cast<int>(q.end(f, iq));
-        const bool safe = scores.extent.around(row, n);
+        const int lead = WHOLE ? 0 : row_lead<T, VEC>(row), j = t * VEC - lead, end = WHOLE ? n : static_cast<int>(q.end(f, iq));
+        const bool safe = WHOLE || scores.extent.around(row, n);
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
             const int j0 = j + c * G * VEC;
-            raw[c].fetch(row + j0, j0 < end && (safe || VEC == 1 || (j0 >= 0 && j0 + VEC <= n)));
+            raw[c].fetch(row + j0, WHOLE || (j0 < end && (safe || VEC == 1 || (j0 >= 0 && j0 + VEC <= n))));
         }
     };
     if (rows > 0) fetch(in, first);
@@ -185,19 +187,19 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
     __syncthreads();
     for (int it = 0; it < rows; it += Cta<G>::kRows, in += in_step, out += out_step) {   // G > 32: the whole CTA alike
         const int64_t iq = first + it;
-        const int p = near_position(q.position(iq)), end = static_cast<int>(q.end(f, iq));
-        const int lead = row_lead<T, VEC>(in), j = t * VEC - lead;
+        const int lead = WHOLE ? 0 : row_lead<T, VEC>(in), end = WHOLE ? n : static_cast<int>(q.end(f, iq));
         const Steps<VEC, G> steps(lead, end);
+        const int p = near_position(q.position(iq)), j = t * VEC - lead;
         float z[SLOTS][VEC];
         float top = -INFINITY;
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c)
-            if (c < steps.some) {
+            if (WHOLE || c < steps.some) {
                 const int j0 = j + c * G * VEC;
                 raw[c].get(z[c]);
-                if (VEC > 1 && c >= steps.whole && (j0 < 0 || j0 + VEC > n) && !scores.extent.around(in, n)) read_apart<T, VEC>(in, j0, n, z[c]);
+                if (!WHOLE && VEC > 1 && c >= steps.whole && (j0 < 0 || j0 + VEC > n) && !scores.extent.around(in, n)) read_apart<T, VEC>(in, j0, n, z[c]);
                 add_bias<VEC>(f, bias, w, j0 - p, z[c]);
-                if (c >= steps.whole) mask<VEC>(j0, end, -INFINITY, z[c]);
+                if (!WHOLE && c >= steps.whole) mask<VEC>(j0, end, -INFINITY, z[c]);
                 top = largest(top, z[c]);
             }
         if (it + Cta<G>::kRows < rows) fetch(in + in_step, iq + Cta<G>::kRows);
@@ -206,7 +208,7 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
         float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c)
-            if (c < steps.some) {
+            if (WHOLE || c < steps.some) {
                 exponentials(z[c], own, kLog2e);
                 add_up(sum, z[c]);
             }
@@ -217,13 +219,13 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 768 / Cta<G>::kThreads)
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
             const int j0 = j + c * G * VEC;
-            if (c < steps.some) {
+            if (WHOLE || c < steps.some) {
                 multiply(z[c], norm);
             } else {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) z[c][i] = 0.f;
             }
-            if (c < steps.whole)
+            if (WHOLE || c < steps.whole)
                 store_whole<T, VEC>(out + j0, z[c]);
             else if (j0 < n)
                 store_slot<T, VEC>(out, j0, n, z[c]);
@@ -291,15 +293,14 @@ template <int VEC>
 __device__ __forceinline__ void add_diagonals(const BiasForm& f, float* sums, const Window<VEC>& w, int rel, const float (&dz)[VEC], float2& left, float2& right) {
     int a, slot;
     w.place(rel, f.distance, a, slot);
-    if (slot == 0) {
-        add_up(left, dz);
-    } else if (slot == w.slots - 1) {
-        add_up(right, dz);
-    } else {
+    float2 sum = make_float2(0.f, 0.f);
+    add_up(sum, dz);
+    left.x += slot == 0 ? sum.x + sum.y : 0.f;
+    right.x += slot == w.slots - 1 ? sum.x + sum.y : 0.f;
+    if (slot > 0 && slot < w.slots - 1) {
         float x[VEC];
         window_load<VEC>(sums, w, a, slot, x);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) x[i] += dz[i];
+        multiply_add(x, 1.f, dz);
         if constexpr (VEC == 1) {
             sums[w.at(a, slot, 0)] = x[0];
         } else {
@@ -325,13 +326,12 @@ __device__ __forceinline__ void leave_buckets(const BiasForm& f, float* all_sums
     __syncthreads();
     for (int v = threadIdx.x; v < values; v += blockDim.x) {
         float s = 0.f;
-        for (int k = 0; k < warps; ++k) {
-            const float* sums = all_sums + k * w.floats();
 #pragma unroll
-            for (int a = 0; a < VEC; ++a) {
-                const int e = v - a;   // VEC*slot + i
-                if (e >= 0 && e < VEC * w.slots) s += sums[w.at(a, e / VEC, e % VEC / Window<VEC>::kIn) + e % VEC % Window<VEC>::kIn];
-            }
+        for (int a = 0; a < VEC; ++a) {
+            const int e = v - a;   // VEC*slot + i
+            if (e < 0 || e >= VEC * w.slots) continue;
+            const float* sums = all_sums + w.at(a, e / VEC, e % VEC / Window<VEC>::kIn) + e % VEC % Window<VEC>::kIn;
+            for (int k = 0; k < warps; ++k) s += sums[k * w.floats()];
         }
         by_value[v] = s;
     }
@@ -356,7 +356,7 @@ __device__ __forceinline__ void leave_buckets(const BiasForm& f, float* all_sums
 }
 
 // SLOTS slots of scores and of dprobs a thread are held: p in binary32, dprobs as loaded.
-template <typename T, int VEC, int G, int SLOTS>
+template <typename T, int VEC, int G, int SLOTS, bool WHOLE>
 __global__ void __launch_bounds__(Cta<G>::kThreads, 512 / Cta<G>::kThreads)
     bias_softmax_backward_kernel(const __grid_constant__ BiasForm f, const Rows4<const T> scores, const Rows4<const T> dprobs,
                                  const Rows4<T> dscores, const MaxSum* __restrict__ stats, float* __restrict__ partial) {
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 512 / Cta<G>::kThreads)
     const Queries q(f, ib);
     build_bias<VEC>(f, ih, w, plain, bias);
     if (partial != nullptr)
-        for (int i = threadIdx.x; i < kWarps * w.floats(); i += blockDim.x) all_sums[i] = 0.f;
+        for (int i = threadIdx.x; i < kWarps * w.floats() / 4; i += blockDim.x) reinterpret_cast<float4*>(all_sums)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     __syncthreads();
     float2 left = make_float2(0.f, 0.f), right = left;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta + threadIdx.x / G;
@@ -383,16 +383,14 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 512 / Cta<G>::kThreads)
     constexpr int kRows = Cta<G>::kRows;
     Raw<T, VEC> s[SLOTS], dp[SLOTS];
     for (int it = 0; it < rows; it += kRows, in += kRows * scores.q, up += kRows * dprobs.q, out += kRows * dscores.q, stat += kRows) {
-        const int64_t iq = first + it;
-        const int p0 = near_position(q.position(iq));
-        const int lead = row_lead<T, VEC>(in), j = t * VEC - lead;
-        const int end = static_cast<int>(q.end(f, iq));
+        const int lead = WHOLE ? 0 : row_lead<T, VEC>(in), end = WHOLE ? n : static_cast<int>(q.end(f, first + it));
         const Steps<VEC, G> steps(lead, end);
-        const bool safe = VEC == 1 || (scores.extent.around(in, n) && dprobs.extent.around(up, n));
+        const int p0 = near_position(q.position(first + it)), j = t * VEC - lead;
+        const bool safe = WHOLE || VEC == 1 || (scores.extent.around(in, n) && dprobs.extent.around(up, n));
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c) {
             const int j0 = j + c * G * VEC;
-            const bool go = j0 < end && (safe || (j0 >= 0 && j0 + VEC <= n));
+            const bool go = WHOLE || (j0 < end && (safe || (j0 >= 0 && j0 + VEC <= n)));
             s[c].fetch(in + j0, go);
             dp[c].fetch(up + j0, go);
         }
@@ -404,19 +402,19 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 512 / Cta<G>::kThreads)
         float2 dot2 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < SLOTS; ++c)
-            if (c < steps.some) {
+            if (WHOLE || c < steps.some) {
                 const int j0 = j + c * G * VEC;
                 float d[VEC];
                 s[c].get(p[c]);
                 dp[c].get(d);
-                if (c >= steps.whole && !safe && (j0 < 0 || j0 + VEC > n)) {
+                if (!WHOLE && c >= steps.whole && !safe && (j0 < 0 || j0 + VEC > n)) {
                     read_apart<T, VEC>(in, j0, n, p[c]);
                     read_apart<T, VEC>(up, j0, n, d);
                 }
                 add_bias<VEC>(f, bias, w, j0 - p0, p[c]);
                 exponentials(p[c], r, kLog2e);
                 multiply(p[c], norm);
-                if (c >= steps.whole) {
+                if (!WHOLE && c >= steps.whole) {
                     mask<VEC>(j0, end, 0.f, p[c]);
                     mask<VEC>(j0, end, 0.f, d);
                 }
@@ -429,13 +427,15 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 512 / Cta<G>::kThreads)
         for (int c = 0; c < SLOTS; ++c) {
             const int j0 = j + c * G * VEC;
             float dz[VEC];
-            if (c < steps.some && !empty) {
+            if ((WHOLE || c < steps.some) && !empty) {
                 dp[c].get(dz);
-                if (c >= steps.whole && !safe && (j0 < 0 || j0 + VEC > n)) read_apart<T, VEC>(up, j0, n, dz);
+                if (!WHOLE && c >= steps.whole && !safe && (j0 < 0 || j0 + VEC > n)) read_apart<T, VEC>(up, j0, n, dz);
+                float less[VEC];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) dz[i] -= dot;
+                for (int i = 0; i < VEC; ++i) less[i] = -dot;
+                multiply_add(dz, 1.f, less);
                 multiply_by(dz, p[c]);
-                if (c >= steps.whole) mask<VEC>(j0, end, 0.f, dz);   // whatever dot is
+                if (!WHOLE && c >= steps.whole) mask<VEC>(j0, end, 0.f, dz);   // whatever dot is
                 if (partial != nullptr) {
                     const int at = warp_j + c * G * VEC;   // of the warp's first key
                     if (at + 32 * VEC <= -f.distance)
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(Cta<G>::kThreads, 512 / Cta<G>::kThreads)
             }
             if (out != nullptr) {
                 multiply(dz, f.scale);
-                if (c < steps.whole)
+                if (WHOLE || c < steps.whole)
                     store_whole<T, VEC>(out + j0, dz);
                 else if (j0 < n)
                     store_slot<T, VEC>(out, j0, n, dz);
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(256)
     const Queries q(f, ib);
     build_bias<VEC>(f, ih, w, plain, bias);
     if (partial != nullptr)
-        for (int i = threadIdx.x; i < kWarps * w.floats(); i += blockDim.x) all_sums[i] = 0.f;
+        for (int i = threadIdx.x; i < kWarps * w.floats() / 4; i += blockDim.x) reinterpret_cast<float4*>(all_sums)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     __syncthreads();
     float2 left = make_float2(0.f, 0.f), right = left;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * f.rows_per_cta;
@@ -553,12 +553,22 @@ void fill_starts(BiasForm& f) {
     }
 }
 
-// Query rows a CTA of the backward kernel takes: enough of them that the CTA's last step (one value a bucket) is a small
-// part of its work, few enough that the grid fills the GPU.
-int backward_rows(int64_t b, int64_t h, int64_t tq) {
-    int rows = 64;
-    while (rows > 8 && b * h * ((tq + rows - 1) / rows) < 8 * kNumSMs) rows >>= 1;
-    return rows;
+// Query rows a CTA takes.  Building the window (and leaving the buckets) costs a CTA what some rows do, so it takes up to
+// `most` of them; `resident` CTAs run at a time, and of the counts that fill whole rounds of those the smallest one is taken
+// (a part-filled last round leaves the GPU idle).  Small problems spread over one round.
+int rows_for(int64_t heads, int64_t tq, int64_t resident, int at_a_time, int most) {
+    for (int64_t rounds = 1;; ++rounds) {
+        int64_t chunks = rounds * resident / heads;
+        if (chunks < 1) chunks = 1;
+        const int64_t rows = ((tq + chunks - 1) / chunks + at_a_time - 1) / at_a_time * at_a_time;
+        if (rows <= most) return static_cast<int>(rows);
+    }
+}
+// The backward kernels run 512 threads an SM; the smallest groups (64 threads, one row) make the most CTAs.
+constexpr int kBackwardMost = 64;
+int64_t most_chunks(int64_t heads, int64_t tq) {
+    const int rows = rows_for(heads, tq, 8 * kNumSMs, 1, kBackwardMost);
+    return (tq + rows - 1) / rows;
 }
 
 int check_form(int dtype, int64_t b, int64_t h, int64_t tq, int64_t tk, const float* table, int buckets, int max_distance,
@@ -608,18 +618,27 @@ template <typename T> Rows4<T> rows4(T* p, const int64_t* s, int64_t b, const Bi
             {reinterpret_cast<const char*>(p), reinterpret_cast<const char*>(p + (b - 1) * s[0] + (f.h - 1) * s[1] + (f.tq - 1) * s[2] + f.tk)}};
 }
 
+// Whether every query sees every key and the rows fill the group's registers.
+template <typename T, int VEC, int G, int SLOTS> bool whole_rows(const BiasForm& f, int64_t n) {
+    return VEC > 1 && !f.causal && f.k_len == nullptr && n == f.tk && f.tk == static_cast<int64_t>(G) * SLOTS * VEC;
+}
+
 template <typename T, int VEC, int G, int SLOTS>
-int launch_forward(BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<T>& out, MaxSum* stats, cudaStream_t s) {
-    constexpr bool kLong = SLOTS == 0;
+int launch_forward(BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in, const Rows4<T>& out, MaxSum* stats, cudaStream_t s) {
     constexpr int kRows = Cta<G>::kRows;
-    f.rows_per_cta = kRows * 8;
-    while (f.rows_per_cta > kRows && b * f.h * ((f.tq + f.rows_per_cta - 1) / f.rows_per_cta) < 16 * kNumSMs) f.rows_per_cta /= 2;
+    // causal rows differ in length, so their CTAs are kept small enough for the last ones to even out
+    f.rows_per_cta = f.causal ? rows_for(b * f.h, f.tq, 16 * kNumSMs, kRows, kRows * 8)
+                              : rows_for(b * f.h, f.tq, SLOTS == 0 ? 4 * kNumSMs : 768 / Cta<G>::kThreads * kNumSMs, kRows, kRows * 16);
     const size_t smem = (Window<VEC>(f.distance).floats() + 2 * f.distance + 1) * sizeof(float);
     const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
-    if constexpr (kLong)
+    if constexpr (SLOTS == 0) {
         bias_softmax_long_kernel<T, VEC><<<grid, 512, smem, s>>>(f, in, out, stats);
-    else
-        bias_softmax_kernel<T, VEC, G, SLOTS><<<grid, Cta<G>::kThreads, smem, s>>>(f, in, out, stats);
+    } else {
+        if (VEC > 1 && whole_rows<T, VEC, G, SLOTS>(f, n))
+            bias_softmax_kernel<T, VEC, G, SLOTS, (VEC > 1)><<<grid, Cta<G>::kThreads, smem, s>>>(f, in, out, stats);
+        else
+            bias_softmax_kernel<T, VEC, G, SLOTS, false><<<grid, Cta<G>::kThreads, smem, s>>>(f, in, out, stats);
+    }
     note_launch();
     return check_launch();
 }
@@ -628,18 +647,19 @@ int launch_forward(BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4
 template <typename T, int VEC>
 int dispatch_forward(BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in, const Rows4<T>& out, MaxSum* stats, cudaStream_t s) {
     constexpr int kFew = VEC == 1 ? 8 : 1, kFull = VEC == 1 ? 16 : 4, kMost = kFull * VEC;   // 64 bytes a thread
-    if (n <= kFew * VEC * 32) return launch_forward<T, VEC, 32, kFew>(f, b, in, out, stats, s);
-    if (n <= kMost * 32) return launch_forward<T, VEC, 32, kFull>(f, b, in, out, stats, s);
-    if (n <= kMost * 64) return launch_forward<T, VEC, 64, kFull>(f, b, in, out, stats, s);
-    if (n <= kMost * 128) return launch_forward<T, VEC, 128, kFull>(f, b, in, out, stats, s);
-    if (n <= kMost * 256) return launch_forward<T, VEC, 256, kFull>(f, b, in, out, stats, s);
-    if (n <= kMost * 512) return launch_forward<T, VEC, 512, kFull>(f, b, in, out, stats, s);
-    return launch_forward<T, VEC, 512, 0>(f, b, in, out, stats, s);
+    if (n <= kFew * VEC * 32) return launch_forward<T, VEC, 32, kFew>(f, n, b, in, out, stats, s);
+    if (n <= kMost * 32) return launch_forward<T, VEC, 32, kFull>(f, n, b, in, out, stats, s);
+    if (n <= kMost * 64) return launch_forward<T, VEC, 64, kFull>(f, n, b, in, out, stats, s);
+    if (n <= kMost * 128) return launch_forward<T, VEC, 128, kFull>(f, n, b, in, out, stats, s);
+    if (n <= kMost * 256) return launch_forward<T, VEC, 256, kFull>(f, n, b, in, out, stats, s);
+    if (n <= kMost * 512) return launch_forward<T, VEC, 512, kFull>(f, n, b, in, out, stats, s);
+    return launch_forward<T, VEC, 512, 0>(f, n, b, in, out, stats, s);
 }
 
 template <typename T, int VEC, int G, int SLOTS>
-int launch_backward(const BiasForm& f, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out, const MaxSum* stats,
+int launch_backward(BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out, const MaxSum* stats,
                     float* partial, cudaStream_t s) {
+    f.rows_per_cta = rows_for(b * f.h, f.tq, 512 / Cta<G>::kThreads * kNumSMs, Cta<G>::kRows, kBackwardMost);
     const Window<VEC> w(f.distance);
     const size_t smem = (w.floats() * (1 + (partial != nullptr ? Cta<G>::kThreads / 32 : 0)) + w.values()) * sizeof(float);
     const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
@@ -648,23 +668,25 @@ int launch_backward(const BiasForm& f, int64_t b, const Rows4<const T>& in, cons
         if ((st = allow_smem(bias_softmax_backward_long_kernel<T, VEC>, smem)) != BZ_OK) return st;
         bias_softmax_backward_long_kernel<T, VEC><<<grid, 256, smem, s>>>(f, in, up, out, stats, partial);
     } else {
-        if ((st = allow_smem(bias_softmax_backward_kernel<T, VEC, G, SLOTS>, smem)) != BZ_OK) return st;
-        bias_softmax_backward_kernel<T, VEC, G, SLOTS><<<grid, Cta<G>::kThreads, smem, s>>>(f, in, up, out, stats, partial);
+        auto kern = VEC > 1 && whole_rows<T, VEC, G, SLOTS>(f, n) ? bias_softmax_backward_kernel<T, VEC, G, SLOTS, (VEC > 1)>
+                                                                  : bias_softmax_backward_kernel<T, VEC, G, SLOTS, false>;
+        if ((st = allow_smem(kern, smem)) != BZ_OK) return st;
+        kern<<<grid, Cta<G>::kThreads, smem, s>>>(f, in, up, out, stats, partial);
     }
     note_launch();
     return check_launch();
 }
 
 template <typename T, int VEC>
-int dispatch_backward(const BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out,
+int dispatch_backward(BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out,
                       const MaxSum* stats, float* partial, cudaStream_t s) {
     constexpr int kFew = VEC == 1 ? 8 : 1, kFull = VEC == 1 ? 16 : 4, kMost = kFull * VEC;
-    if (n <= kFew * VEC * 32) return launch_backward<T, VEC, 32, kFew>(f, b, in, up, out, stats, partial, s);
-    if (n <= kMost * 32) return launch_backward<T, VEC, 32, kFull>(f, b, in, up, out, stats, partial, s);
-    if (n <= kMost * 64) return launch_backward<T, VEC, 64, kFull>(f, b, in, up, out, stats, partial, s);
-    if (n <= kMost * 128) return launch_backward<T, VEC, 128, kFull>(f, b, in, up, out, stats, partial, s);
-    if (n <= kMost * 256) return launch_backward<T, VEC, 256, kFull>(f, b, in, up, out, stats, partial, s);
-    return launch_backward<T, VEC, 256, 0>(f, b, in, up, out, stats, partial, s);
+    if (n <= kFew * VEC * 32) return launch_backward<T, VEC, 32, kFew>(f, n, b, in, up, out, stats, partial, s);
+    if (n <= kMost * 32) return launch_backward<T, VEC, 32, kFull>(f, n, b, in, up, out, stats, partial, s);
+    if (n <= kMost * 64) return launch_backward<T, VEC, 64, kFull>(f, n, b, in, up, out, stats, partial, s);
+    if (n <= kMost * 128) return launch_backward<T, VEC, 128, kFull>(f, n, b, in, up, out, stats, partial, s);
+    if (n <= kMost * 256) return launch_backward<T, VEC, 256, kFull>(f, n, b, in, up, out, stats, partial, s);
+    return launch_backward<T, VEC, 256, 0>(f, n, b, in, up, out, stats, partial, s);
 }
 
 // The wide kernels keep eight (or four) copies of the window; beyond this distance they would leave one CTA an SM.
@@ -686,7 +708,7 @@ int forward(BiasForm& f, int64_t b, const void* scores, const int64_t* ss, void*
 }
 
 template <typename T>
-int backward(const BiasForm& f, int64_t b, const void* scores, const int64_t* ss, const void* dprobs, const int64_t* sd, void* dscores,
+int backward(BiasForm& f, int64_t b, const void* scores, const int64_t* ss, const void* dprobs, const int64_t* sd, void* dscores,
              const int64_t* so, const MaxSum* stats, float* partial, cudaStream_t s) {
     const auto in = rows4(static_cast<const T*>(scores), ss, b, f);
     const auto up = rows4(static_cast<const T*>(dprobs), sd, b, f);
@@ -704,8 +726,7 @@ using namespace bz;
 
 extern "C" size_t bz_bias_softmax_workspace_bytes(int64_t b, int64_t h, int64_t tq, int64_t tk, int buckets) {
     if (b < 1 || h < 1 || tq < 1 || tk < 1 || buckets < 2 || buckets > 256 || b > 65535 || h > 65535 || tq >= (int64_t(1) << 31)) return 0;
-    const int rows = backward_rows(b, h, tq);
-    return round_up(static_cast<size_t>(b) * h * ((tq + rows - 1) / rows) * buckets * sizeof(float), 256);
+    return round_up(static_cast<size_t>(b) * h * most_chunks(b * h, tq) * buckets * sizeof(float), 256);
 }
 
 extern "C" int bz_bias_softmax(const void* scores, const int64_t* strides_scores, int dtype, int64_t b, int64_t h, int64_t tq, int64_t tk,
@@ -745,7 +766,6 @@ extern "C" int bz_bias_softmax_backward(const void* scores, const int64_t* strid
         (workspace == nullptr || !aligned256(workspace) || workspace_bytes < bz_bias_softmax_workspace_bytes(b, h, tq, tk, buckets)))
         return BZ_ERR_WORKSPACE;
     BiasForm f = make_form(h, tq, tk, table, buckets, max_distance, bidirectional, causal, scale, k_len, q_start);
-    f.rows_per_cta = backward_rows(b, h, tq);
     float* partial = dtable != nullptr ? static_cast<float*>(workspace) : nullptr;
     if (dtype == BZ_F32)
         st = backward<float>(f, b, scores, strides_scores, dprobs, strides_dprobs, dscores, strides_dscores, reinterpret_cast<const MaxSum*>(stats), partial, s);
