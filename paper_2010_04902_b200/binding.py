@@ -173,7 +173,7 @@ def _check(status: int, what: str):
 
 def _stream() -> int:
     # torch.cuda.current_stream().cuda_stream without building the stream object (3.2 -> 0.3 us a call)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _dev(t: torch.Tensor, dtype, name: str) -> int:
@@ -643,15 +643,29 @@ def _packed(t, shape, dtype, name: str):
     """Address of a contiguous tensor of this shape and type, or None."""
     if t is None:
         return None
+    if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
     return _shaped(t, shape, dtype, name)
 
 
+def _like_rows(t: torch.Tensor) -> torch.Tensor:
+    """A new tensor of t's shape whose rows are as far apart as t's: the kernels' wide loads and stores need rows that
+    sit alike relative to 16-byte boundaries."""
+    if t.is_contiguous():
+        return torch.empty_like(t)
+    n, ld = t.shape[-1], t.stride(-2)
+    if t.shape[-2] <= 1 or ld <= n or ld > 2 * n:
+        return t.new_empty(t.shape)
+    return t.new_empty(t.shape[:-1] + (ld,))[..., :n]
+
+
 def _act(name: str) -> int:
-    if name not in _ACTS:
-        raise ValueError("act must be one of %s" % ", ".join(sorted(_ACTS)))
-    return _ACTS[name]
+    try:
+        return _ACTS[name]
+    except KeyError:
+        raise ValueError("act must be one of %s" % ", ".join(sorted(_ACTS))) from None
 
 
 def _like_matrix(t: torch.Tensor) -> torch.Tensor:
@@ -731,17 +745,34 @@ def glu_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, prea
 
 
 def _strides(t: torch.Tensor, name: str):
-    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
-        raise ValueError("%s must be [b][h][tq][tk] with unit stride along tk" % name)
-    return _Strides(*t.stride()[:3])
+    if t.dim() != 4:
+        raise ValueError("%s must be [b][h][tq][tk]" % name)
+    a, b, c, one = t.stride()
+    if one != 1 and t.shape[3] > 1:
+        raise ValueError("%s must have unit stride along tk" % name)
+    return _Strides(a, b, c)
 
 
 def _bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start):
+    """The arguments from scores to q_start of both calls."""
+    strides = _strides(scores, "scores")
     b, h, tq, tk = scores.shape
     if table.dim() != 2 or table.shape[1] != h:
         raise ValueError("table must be [buckets][%d]" % h)
-    return [_packed(table, table.shape, torch.float32, "table"), table.shape[0], max_distance, 1 if bidirectional else 0,
-            1 if causal else 0, float(scale), _packed(k_len, (b,), torch.int32, "k_len"), _packed(q_start, (b,), torch.int32, "q_start")]
+    return strides, (scores.data_ptr(), strides, _dtype(scores, "scores"), b, h, tq, tk, _packed(table, table.shape, torch.float32, "table"),
+                     table.shape[0], max_distance, 1 if bidirectional else 0, 1 if causal else 0, scale,
+                     _packed(k_len, (b,), torch.int32, "k_len"), _packed(q_start, (b,), torch.int32, "q_start"))
+
+
+def _rows_out(t, like, like_strides, name):
+    """(tensor, address, strides) of an output shaped like scores; a new one if t is None."""
+    if t is None:
+        if like.is_contiguous():
+            t = torch.empty_like(like)
+            return t, t.data_ptr(), like_strides
+        t = _like_rows(like)
+        return t, t.data_ptr(), _strides(t, name)
+    return t, _shaped(t, like.shape, like.dtype, name), _strides(t, name)
 
 
 def bias_softmax(scores: torch.Tensor, table: torch.Tensor, max_distance: int = 128, bidirectional: bool = True,
@@ -749,16 +780,16 @@ def bias_softmax(scores: torch.Tensor, table: torch.Tensor, max_distance: int = 
                  q_start: torch.Tensor | None = None, probs: torch.Tensor | None = None, stats: torch.Tensor | None = None):
     """bz_bias_softmax: softmax over keys of scale * scores [b][h][tq][tk] + table[bucket(key - query)][h].  Returns
     (probs, stats)."""
-    strides = _strides(scores, "scores")
-    if probs is None:
-        probs = _like_matrix(scores)
+    strides, form = _bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start)
+    probs, p_probs, s_probs = _rows_out(probs, scores, strides, "probs")
     if stats is None:
-        stats = table.new_empty(scores.shape[:3] + (2,))
-    st = lib().bz_bias_softmax(scores.data_ptr(), strides, _dtype(scores, "scores"), *scores.shape,
-                               *_bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start),
-                               _shaped(probs, scores.shape, scores.dtype, "probs"), _strides(probs, "probs"),
-                               _packed(stats, tuple(scores.shape[:3]) + (2,), torch.float32, "stats"), _stream())
-    _check(st, "bz_bias_softmax")
+        stats = table.new_empty((*scores.shape[:3], 2))
+        p_stats = stats.data_ptr()
+    else:
+        p_stats = _packed(stats, (*scores.shape[:3], 2), torch.float32, "stats")
+    st = lib().bz_bias_softmax(*form, p_probs, s_probs, p_stats, _stream())
+    if st:
+        _check(st, "bz_bias_softmax")
     return probs, stats
 
 
@@ -768,22 +799,19 @@ def bias_softmax_backward(scores: torch.Tensor, table: torch.Tensor, stats: torc
                           dscores: torch.Tensor | None = None, dtable: torch.Tensor | None = None,
                           workspace: torch.Tensor | None = None):
     """bz_bias_softmax_backward: returns (dscores, dtable)."""
-    strides = _strides(scores, "scores")
-    if dscores is None:
-        dscores = _like_matrix(scores)
+    strides, form = _bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start)
+    dscores, p_ds, s_ds = _rows_out(dscores, scores, strides, "dscores")
     if dtable is None:
         dtable = torch.empty_like(table)
-    form = _bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start)
-    ws = workspace
-    if ws is None:
-        ws = torch.empty(max(256, lib().bz_bias_softmax_workspace_bytes(*scores.shape, table.shape[0])), dtype=torch.uint8,
-                         device=scores.device)
-    st = lib().bz_bias_softmax_backward(scores.data_ptr(), strides, _dtype(scores, "scores"), *scores.shape, *form,
-                                        _packed(stats, tuple(scores.shape[:3]) + (2,), torch.float32, "stats"),
-                                        _shaped(dprobs, scores.shape, scores.dtype, "dprobs"), _strides(dprobs, "dprobs"),
-                                        _shaped(dscores, scores.shape, scores.dtype, "dscores"), _strides(dscores, "dscores"),
-                                        _packed(dtable, table.shape, torch.float32, "dtable"), ws.data_ptr(), ws.numel(), _stream())
-    _check(st, "bz_bias_softmax_backward")
+    if workspace is None:
+        size = lib().bz_bias_softmax_workspace_bytes(*scores.shape, table.shape[0])
+        workspace = torch.empty(max(256, size), dtype=torch.uint8, device=scores.device)
+    st = lib().bz_bias_softmax_backward(*form, _packed(stats, (*scores.shape[:3], 2), torch.float32, "stats"),
+                                        _shaped(dprobs, scores.shape, scores.dtype, "dprobs"), _strides(dprobs, "dprobs"), p_ds, s_ds,
+                                        _packed(dtable, table.shape, torch.float32, "dtable"), workspace.data_ptr(), workspace.numel(),
+                                        _stream())
+    if st:
+        _check(st, "bz_bias_softmax_backward")
     return dscores, dtable
 
 
@@ -791,7 +819,7 @@ def _teacher(logits, teacher, index):
     m = logits.shape[0]
     if teacher.dim() != 2 or teacher.shape[0] != m:
         raise ValueError("teacher must be [%d][t]" % m)
-    return [_packed(teacher, teacher.shape, torch.float32, "teacher"), _packed(index, teacher.shape, torch.int32, "index"), teacher.shape[1]]
+    return _packed(teacher, teacher.shape, torch.float32, "teacher"), _packed(index, teacher.shape, torch.int32, "index"), teacher.shape[1]
 
 
 def distill(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, temperature: float = 1.0,
@@ -801,32 +829,38 @@ def distill(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, te
     (float32 [m]) or `dlogits` given also the gradient, from the same pass: (loss, stats, dlogits)."""
     m, v, ld = _matrix(logits, "logits")
     dt = _dtype(logits, "logits")
+    p_teacher, p_index, top = _teacher(logits, teacher, index)
     grad = dloss is not None or dlogits is not None
     if loss is None:
         loss = teacher.new_empty(m)
     if stats is None:
         stats = teacher.new_empty((m, 2))
-    if grad and dlogits is None:
-        dlogits = _like_matrix(logits)
-    st = lib().bz_distill(logits.data_ptr(), ld, dt, m, v, *_teacher(logits, teacher, index), float(temperature),
+    p_d, ld_d = None, 0
+    if grad:
+        if dlogits is None:
+            dlogits = _like_rows(logits)
+            p_d, ld_d = dlogits.data_ptr(), dlogits.stride(0) if m > 1 else v
+        else:
+            p_d, ld_d = _shaped(dlogits, (m, v), logits.dtype, "dlogits"), _matrix(dlogits, "dlogits")[2]
+    st = lib().bz_distill(logits.data_ptr(), ld, dt, m, v, p_teacher, p_index, top, temperature,
                           _packed(dloss, (m,), torch.float32, "dloss"), _packed(loss, (m,), torch.float32, "loss"),
-                          _packed(stats, (m, 2), torch.float32, "stats"),
-                          _shaped(dlogits, (m, v), logits.dtype, "dlogits") if grad else None,
-                          _matrix(dlogits, "dlogits")[2] if grad else 0, _stream())
-    _check(st, "bz_distill")
+                          _packed(stats, (m, 2), torch.float32, "stats"), p_d, ld_d, _stream())
+    if st:
+        _check(st, "bz_distill")
     return (loss, stats, dlogits) if grad else (loss, stats)
 
 
 def distill_backward(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, stats: torch.Tensor,
                      dloss: torch.Tensor | None = None, temperature: float = 1.0,
                      dlogits: torch.Tensor | None = None) -> torch.Tensor:
-    """bz_distill_backward: the gradient alone, with stats as distill() returned it."""
+    """bz_distill_backward: the gradient alone, with stats as distill() returned them."""
     m, v, ld = _matrix(logits, "logits")
     if dlogits is None:
-        dlogits = _like_matrix(logits)
+        dlogits = _like_rows(logits)
     st = lib().bz_distill_backward(logits.data_ptr(), ld, _dtype(logits, "logits"), m, v, *_teacher(logits, teacher, index),
-                                   float(temperature), _packed(stats, (m, 2), torch.float32, "stats"),
+                                   temperature, _packed(stats, (m, 2), torch.float32, "stats"),
                                    _packed(dloss, (m,), torch.float32, "dloss"),
                                    _shaped(dlogits, (m, v), logits.dtype, "dlogits"), _matrix(dlogits, "dlogits")[2], _stream())
-    _check(st, "bz_distill_backward")
+    if st:
+        _check(st, "bz_distill_backward")
     return dlogits

@@ -543,14 +543,13 @@ __global__ void __launch_bounds__(256) bias_table_kernel(const float* __restrict
 // ---- host side ----------------------------------------------------------------------------------
 
 // Boundaries of the logarithmic buckets: the smallest n >= e*(d/e)^(t/steps); a bound that is a whole number counts as
-// reached (it differs from the rounded power by far less than one part in 10^9).
+// reached (it differs from the rounded products by far less than one part in 10^9).
 void fill_starts(BiasForm& f) {
     const int steps = f.nb - f.exact;
+    const double ratio = pow(static_cast<double>(f.distance) / f.exact, 1.0 / steps);
+    double x = f.exact;
     f.starts[0] = static_cast<uint16_t>(f.exact);
-    for (int t = 1; t < steps; ++t) {
-        const double x = f.exact * pow(static_cast<double>(f.distance) / f.exact, static_cast<double>(t) / steps);
-        f.starts[t] = static_cast<uint16_t>(ceil(x * (1.0 - 1e-9)));
-    }
+    for (int t = 1; t < steps; ++t) f.starts[t] = static_cast<uint16_t>(ceil((x *= ratio) * (1.0 - 1e-9)));
 }
 
 // Query rows a CTA takes.  Building the window (and leaving the buckets) costs a CTA what some rows do, so it takes up to

@@ -164,6 +164,7 @@ template <typename T, int NT> int launch_few(const FewParams& p, bool wide, cuda
 template <typename T> int few(const FewParams& p, bool wide, cudaStream_t s) {
     if (p.m <= 8) return launch_few<T, 1>(p, wide, s);
     if (p.m <= 16) return launch_few<T, 2>(p, wide, s);
+    if (p.m <= 24) return launch_few<T, 3>(p, wide, s);
     return launch_few<T, 4>(p, wide, s);
 }
 
