@@ -19,7 +19,11 @@ __global__ void __launch_bounds__(256) glu_dgu_kernel(const float* __restrict__ 
     if (c >= n) return;
     for (int64_t r = blockIdx.y; r < m; r += gridDim.y) {
         float g[V], u[V], d[V], a[V], b[V];
-        if constexpr (V == 8) {
+        if constexpr (V == 2) {
+            const float2 g2 = *reinterpret_cast<const float2*>(preact + r * n + c), u2 = *reinterpret_cast<const float2*>(preact + (m + r) * n + c);
+            const float2 d2 = unpack2(T(), *reinterpret_cast<const uint32_t*>(dh + r * ld_dh + c));
+            g[0] = g2.x, g[1] = g2.y, u[0] = u2.x, u[1] = u2.y, d[0] = d2.x, d[1] = d2.y;
+        } else if constexpr (V == 8) {
             const uint4* pg = reinterpret_cast<const uint4*>(preact + r * n + c);
             const uint4* pu = reinterpret_cast<const uint4*>(preact + (m + r) * n + c);
             const uint4 g0 = ld_stream(pg), g1 = ld_stream(pg + 1), u0 = ld_stream(pu), u1 = ld_stream(pu + 1);
@@ -30,7 +34,10 @@ __global__ void __launch_bounds__(256) glu_dgu_kernel(const float* __restrict__ 
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) a[i] = d[i] * u[i] * act_slope<ACT>(g[i]), b[i] = d[i] * act<ACT>(g[i]);
-        if constexpr (V == 8) {
+        if constexpr (V == 2) {
+            *reinterpret_cast<uint32_t*>(dgu + r * ld + c) = pack2(T(), a[0], a[1]);
+            *reinterpret_cast<uint32_t*>(dgu + (m + r) * ld + c) = pack2(T(), b[0], b[1]);
+        } else if constexpr (V == 8) {
             *reinterpret_cast<uint4*>(dgu + r * ld + c) = Word<T>::pack(a);
             *reinterpret_cast<uint4*>(dgu + (m + r) * ld + c) = Word<T>::pack(b);
         } else {
@@ -130,7 +137,8 @@ int launch_product(const CUtensorMap& a, const CUtensorMap& b0, const CUtensorMa
     note_launch();
     const int st = check_launch();
     if (st != BZ_OK || p.splits == 1) return st;
-    glu_shares_kernel<T, BN><<<4 * kNumSMs, 256, 0, s>>>(p, P == kWeight);
+    const int64_t groups = p.row_tiles * p.col_tiles * (256 * BN / 4 / 256);
+    glu_shares_kernel<T, BN><<<static_cast<unsigned>(groups < 16 * kNumSMs ? groups : 16 * kNumSMs), 256, 0, s>>>(p, P == kWeight);
     note_launch();
     return check_launch();
 }
@@ -149,7 +157,7 @@ int zero(void* p, int64_t ld, int64_t rows, int64_t n, int bytes, cudaStream_t s
     return e == cudaSuccess ? BZ_OK : cuda_failed(e);
 }
 
-bool pair_rows(const void* p, int64_t ld, int64_t rows) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0 && (rows <= 1 || ld % 2 == 0); }
+bool pair_rows(const void* p, int64_t ld, int64_t rows, int bytes) { return reinterpret_cast<uintptr_t>(p) % (2 * bytes) == 0 && (rows <= 1 || ld % 2 == 0); }
 bool wide_rows(const void* p, int64_t ld, int64_t rows, int bytes) { return aligned16(p) && (rows <= 1 || ld * bytes % 16 == 0); }
 
 template <typename T, int NT> int launch_few(const FewParams& p, bool wide, cudaStream_t s) {
@@ -189,8 +197,8 @@ int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t
     p.rows = m, p.cols = n, p.blocks = ceil_div(k, kBlockK);
     const Plan pl = plan(kForward, m, n, p.blocks);
     p.row_tiles = ceil_div(m, kRowTile), p.col_tiles = ceil_div(n, pl.bn / 2), p.splits = 1;
-    p.act = act, p.out = h, p.ld_out = ld_h, p.wide = wide_rows(h, ld_h, m, 2), p.pairs = pair_rows(h, ld_h, m);
-    p.preact = preact, p.preact_wide = n % 4 == 0;
+    p.act = act, p.out = h, p.ld_out = ld_h, p.wide = wide_rows(h, ld_h, m, 2), p.pairs = pair_rows(h, ld_h, m, 2);
+    p.preact = preact, p.preact_wide = n % 4 == 0, p.preact_pairs = n % 2 == 0;
     CUtensorMap a, b0, b1;
     if (!make_map<T>(&a, ox.p, k, m, ox.ld, 128, 0) || !make_map<T>(&b0, og.p, k, n, og.ld, pl.bn / 2, 0) ||
         !make_map<T>(&b1, ou.p, k, n, ou.ld, pl.bn / 2, 0))
@@ -202,6 +210,8 @@ template <typename T, int ACT>
 int launch_dgu(const float* preact, const T* dh, int64_t ld_dh, int64_t m, int64_t n, T* dgu, int64_t ld, cudaStream_t s) {
     if (n % 8 == 0 && laid_out(dh, ld_dh, m))
         glu_dgu_kernel<T, ACT, 8><<<row_grid(m, n / 8), 256, 0, s>>>(preact, dh, ld_dh, m, n, dgu, ld);
+    else if (n % 2 == 0 && pair_rows(dh, ld_dh, m, 2))
+        glu_dgu_kernel<T, ACT, 2><<<row_grid(m, n / 2), 256, 0, s>>>(preact, dh, ld_dh, m, n, dgu, ld);
     else
         glu_dgu_kernel<T, ACT, 1><<<row_grid(m, n), 256, 0, s>>>(preact, dh, ld_dh, m, n, dgu, ld);
     note_launch();
@@ -238,7 +248,7 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
         p.rows = m, p.blocks = ceil_div(n, kBlockK);
         const Plan pl = plan(kInput, m, k, 2 * p.blocks);
         p.row_tiles = ceil_div(m, kRowTile), p.col_tiles = ceil_div(k, pl.bn), p.splits = pl.splits;
-        p.out = dx, p.ld_out = ld_dx, p.wide = wide_rows(dx, ld_dx, m, 2), p.pairs = pair_rows(dx, ld_dx, m);
+        p.out = dx, p.ld_out = ld_dx, p.wide = wide_rows(dx, ld_dx, m, 2), p.pairs = pair_rows(dx, ld_dx, m, 2);
         if (!make_map<T>(&a, dgu, n, m, ld, 128, m * ld) || !make_map<T>(&b0, og.p, k, n, og.ld, kBlockK, 0) ||
             !make_map<T>(&b1, ou.p, k, n, ou.ld, kBlockK, 0))
             return BZ_ERR_UNSUPPORTED;
@@ -252,7 +262,7 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
         p.row_tiles = 2 * ceil_div(n, kRowTile), p.col_tiles = ceil_div(k, pl.bn), p.splits = pl.splits;
         p.out = dwg, p.out2 = dwu, p.ld_out = ld_dw, p.out_f32 = grad_f32;
         p.wide = wide_rows(dwg, ld_dw, n, grad_f32 ? 4 : 2) && aligned16(dwu);
-        p.pairs = pair_rows(dwg, ld_dw, n) && pair_rows(dwu, ld_dw, n);
+        p.pairs = pair_rows(dwg, ld_dw, n, grad_f32 ? 4 : 2) && pair_rows(dwu, ld_dw, n, grad_f32 ? 4 : 2);
         if (!make_map<T>(&a, dgu, n, m, ld, kBlockK, m * ld) || !make_map<T>(&b0, ox.p, k, m, ox.ld, kBlockK, 0)) return BZ_ERR_UNSUPPORTED;
         if ((st = product<T, kWeight>(pl, a, b0, b0, p, s)) != BZ_OK) return st;
     }

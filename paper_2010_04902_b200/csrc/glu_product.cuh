@@ -30,7 +30,7 @@ static __device__ unsigned int g_glu_timeouts = 0;
 
 enum GluProduct { kForward, kInput, kWeight };
 
-constexpr int kRowTile = 256, kBlockK = 64, kEpilogueWarps = 4, kProductThreads = 128 + 32 * kEpilogueWarps;
+constexpr int kRowTile = 256, kBlockK = 64, kEpilogueWarps = 8, kProductThreads = 128 + 32 * kEpilogueWarps;
 
 struct ProductParams {
     int64_t rows, cols;          // extents of the result (kWeight: rows of one half; kForward: hidden units)
@@ -41,9 +41,9 @@ struct ProductParams {
     void* out;                   // h / dx / dw_gate
     void* out2;                  // dw_up
     int64_t ld_out;
-    int out_f32, wide, pairs;    // binary32 output; 16-byte stores possible; 4-byte stores possible
+    int out_f32, wide, pairs;    // binary32 output; 16-byte stores possible; stores of two elements possible
     float* preact;               // kForward: [2][rows][cols] or null
-    int preact_wide;
+    int preact_wide, preact_pairs;
     float* partial;              // splits > 1: [split][tile][256][BN]
 };
 
@@ -58,7 +58,7 @@ __device__ __forceinline__ void turn_in(float* turn, int word, const uint4& w) {
     *reinterpret_cast<uint4*>(turn + (threadIdx.x & 31) * kTurnWords + word) = w;
 }
 // Writes elements [c0, c0 + 128 / sizeof(E)) of rows r0 .. r0 + 31 of `out`; `rows`, `cols` exist.  wide: 16-byte stores
-// possible; pairs: 4-byte stores of two 16-bit elements possible.
+// possible; pairs: stores of two elements possible.
 template <typename E>
 __device__ __forceinline__ void turn_out(const float* turn, E* out, int64_t ld, int64_t r0, int64_t rows, int64_t c0, int64_t cols, bool wide, bool pairs) {
     constexpr int kEach = 128 / static_cast<int>(sizeof(E)), kPer = 4 / static_cast<int>(sizeof(E));
@@ -71,6 +71,12 @@ __device__ __forceinline__ void turn_out(const float* turn, E* out, int64_t ld, 
         for (int i = 0; i < 8; ++i) {
             const int r = i * 4 + lane / 8, w = lane % 8 * 4;
             if (r < n_rows) *reinterpret_cast<uint4*>(base + r * ld + w * kPer) = *reinterpret_cast<const uint4*>(turn + r * kTurnWords + w);
+        }
+    } else if (kPer == 1 && pairs && n == kEach) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = i * 2 + lane / 16, w = lane % 16 * 2;
+            if (r < n_rows) *reinterpret_cast<float2*>(base + r * ld + w) = *reinterpret_cast<const float2*>(turn + r * kTurnWords + w);
         }
     } else if (kPer == 1 || (pairs && n % 2 == 0)) {
         if (lane * kPer < n) {
@@ -91,7 +97,7 @@ __device__ __forceinline__ void turn_out(const float* turn, E* out, int64_t ld, 
 
 template <int BN> struct ProductShape {
     static constexpr int kABytes = 128 * kBlockK * 2, kBBytes = BN / 2 * kBlockK * 2, kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = BN == 256 ? 6 : (BN == 128 ? 8 : 10);
+    static constexpr int kStages = BN == 256 ? 5 : (BN == 128 ? 7 : 9);
     static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpilogueWarps * kTurnBytes + (2 * kStages + 4) * 8 + 16;
 };
 
@@ -170,6 +176,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     const int64_t cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
     const int64_t tiles = p.row_tiles * p.col_tiles * p.splits;
     const int64_t blocks = P == kInput ? 2 * p.blocks : p.blocks;
+    if (warp == 3 && lane < 3) {
+        const CUtensorMap* map = lane == 0 ? &a_map : (lane == 1 ? &b0_map : &b1_map);
+        asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
         for (int s = 0; s < 2; ++s) mbar_init(&acc_full[s], 1), mbar_init(&acc_empty[s], 2 * kEpilogueWarps);
@@ -254,8 +264,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
             if (alive) mma_commit_pair(&acc_full[acc]);
         }
     } else if (warp >= 4) {
-        // ---------------------------------------------------------------- epilogue: one row a thread
-        const int quarter = warp & 3;
+        // ---------------------------------------------------------------- epilogue: one row and half of the columns a thread
+        const int quarter = warp & 3, half_of_columns = (warp - 4) >> 2;
         float* turn = turns + (warp - 4) * (kTurnBytes / 4);
         int64_t n = 0;
         for (int64_t i = cluster; i < tiles; i += clusters, ++n) {
@@ -267,9 +277,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
             const int in_tile = static_cast<int>(rank) * 128 + quarter * 32;   // first row of this warp
             if constexpr (P == kForward) {
                 const int64_t r0 = t.row * 256 + in_tile;
-                constexpr int kStep = BN / 2 < 64 ? BN / 2 : 64;
+                constexpr int kStep = BN / 2 < 128 ? 32 : 64;   // a warp takes every other step
 #pragma unroll 1
-                for (int c = 0; c < BN / 2; c += kStep) {
+                for (int c = half_of_columns * kStep; c < BN / 2; c += 2 * kStep) {
                     uint4 h[kStep / 8];
 #pragma unroll
                     for (int half = 0; half < kStep / 32; ++half) {
@@ -283,12 +293,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 #pragma unroll
                             for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<float>::pack(g + 4 * e));
                             __syncwarp();
-                            turn_out<float>(turn, p.preact, p.cols, r0, p.rows, c0, p.cols, p.preact_wide, false);
+                            turn_out<float>(turn, p.preact, p.cols, r0, p.rows, c0, p.cols, p.preact_wide, p.preact_pairs);
                             __syncwarp();
 #pragma unroll
                             for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<float>::pack(u + 4 * e));
                             __syncwarp();
-                            turn_out<float>(turn, p.preact + p.rows * p.cols, p.cols, r0, p.rows, c0, p.cols, p.preact_wide, false);
+                            turn_out<float>(turn, p.preact + p.rows * p.cols, p.cols, r0, p.rows, c0, p.cols, p.preact_wide, p.preact_pairs);
                             __syncwarp();
                         }
                         switch (p.act) {
@@ -314,7 +324,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
                 void* out = half ? p.out2 : p.out;
                 const bool f32 = p.out_f32 || p.splits > 1;
 #pragma unroll 1
-                for (int c = 0; c < BN; c += 64) {
+                for (int c = half_of_columns * 64; c < BN; c += 128) {
                     float x[2][32];
                     tmem_ld32(base + c, x[0]);
                     tmem_ld32(base + c + 32, x[1]);
@@ -329,7 +339,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
                             if (p.splits > 1)
                                 turn_out<float>(turn, p.partial + i * 256 * BN, BN, in_tile, 256, c + k * 32, BN, true, false);
                             else
-                                turn_out<float>(turn, static_cast<float*>(out), p.ld_out, r0, p.rows, t.col * BN + c + k * 32, p.cols, p.wide, false);
+                                turn_out<float>(turn, static_cast<float*>(out), p.ld_out, r0, p.rows, t.col * BN + c + k * 32, p.cols, p.wide, p.pairs);
                             __syncwarp();
                         }
                     } else {
