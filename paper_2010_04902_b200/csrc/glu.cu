@@ -1,4 +1,5 @@
 // Gated feed-forward block and its gradient: host side, the pass between the products, and operands laid out on the way in.
+#include <algorithm>
 #include <atomic>
 
 #include "glu_few.cuh"
@@ -8,7 +9,7 @@ namespace bz {
 namespace {
 
 constexpr int kClusters = kNumSMs / 2;
-constexpr size_t kPartialBytes = static_cast<size_t>(kClusters) * kRowTile * 256 * sizeof(float);  // one tile a cluster
+constexpr size_t kPartialBytes = static_cast<size_t>(2 * kClusters) * kRowTile * 256 * sizeof(float);  // see plan_backward()
 
 // dgu[0] = dh * u * act'(g), dgu[1] = dh * act(g), each [m][ld], rounded to the operands' type.  14 bytes a hidden unit
 // (8 of them preact): bound by memory.  V columns a thread.
@@ -98,28 +99,57 @@ template <typename T> bool make_map(CUtensorMap* map, const void* p, int64_t n, 
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Width of the tiles and shares of the contraction.
-struct Plan {
-    int bn, splits;
-};
-Plan plan(GluProduct kind, int64_t rows, int64_t cols, int64_t blocks) {
-    const int64_t row_tiles = (kind == kWeight ? 2 : 1) * ceil_div(rows, kRowTile);
-    Plan best{256, 1};
+// Cycles of a block of the contraction and of a tile's ends, for choosing the width of the tiles: 256 columns a tile fill the
+// tensor cores (520 cycles a block), narrower tiles are bound by the loads of A but part the work more evenly.
+double block_cycles(int bn) { return bn == 256 ? 520 : (bn == 128 ? 380 : 320); }
+constexpr double kTileCycles = 1500, kSharesCycles = 4000;
+
+int plan_forward(int64_t rows, int64_t cols, int64_t blocks) {
+    int best = 256;
     double least = 0;
-    for (int bn = 256; bn >= (kind == kForward ? 64 : 128); bn /= 2) {
-        const int64_t tiles = row_tiles * ceil_div(cols, kind == kForward ? bn / 2 : bn);
-        int splits = 1;
-        if (kind != kForward)
-            while (splits < 16 && tiles * (splits + 1) <= kClusters && blocks / (splits + 1) >= 8) ++splits;
-        const double cost = static_cast<double>(ceil_div(tiles * splits, kClusters)) *
-                            (static_cast<double>(ceil_div(blocks, splits)) * (bn == 256 ? 520 : (bn == 128 ? 380 : 320)) + 1500);
-        if (least == 0 || cost < least) least = cost, best = {bn, splits};
+    for (int bn = 256; bn >= 64; bn /= 2) {
+        const int64_t tiles = ceil_div(rows, kRowTile) * ceil_div(cols, bn / 2);
+        const double cost = static_cast<double>(ceil_div(tiles, kClusters)) * (blocks * block_cycles(bn) + kTileCycles);
+        if (bn == 256 || cost < least) least = cost, best = bn;
     }
     return best;
 }
 
-template <typename T, GluProduct P, int BN>
-int launch_product(const CUtensorMap& a, const CUtensorMap& b0, const CUtensorMap& b1, const ProductParams& p, cudaStream_t s) {
+// Sets the two parts' tiles and shares for tiles of bn columns and returns the cycles that it should take.  A contraction
+// longer than a cluster's part of the whole work (and than eight blocks) is cut into pieces no longer than that.  Only parts
+// of fewer than kClusters tiles can be that long, so there are fewer than 2 * kClusters pieces with sums to keep.
+double plan_backward(ProductParams& p, int bn) {
+    int64_t work = 0;
+    for (ProductPart& o : p.part) {
+        if (o.out == nullptr) continue;
+        o.row_tiles = (&o == &p.part[kWeight] ? 2 : 1) * ceil_div(o.rows, kRowTile);
+        o.col_tiles = ceil_div(o.cols, bn);
+        work += o.row_tiles * o.col_tiles * o.blocks;
+    }
+    const int64_t piece = std::max<int64_t>(8, ceil_div(work, kClusters));
+    double cost = 0;
+    for (ProductPart& o : p.part)
+        if (o.out != nullptr) {
+            o.splits = static_cast<int>(ceil_div(o.blocks, piece));
+            if (o.splits > 1) cost = kSharesCycles;
+        }
+    p.weight_first = p.part[kWeight].out != nullptr &&
+                     (p.part[kInput].out == nullptr || p.part[kWeight].blocks / p.part[kWeight].splits > p.part[kInput].blocks / p.part[kInput].splits);
+    // pieces go round the clusters, longer ones first
+    double longest = 0;
+    int64_t at = 0, rounds = 0;
+    for (int k = 0; k < 2; ++k) {
+        const ProductPart& o = p.part[p.weight_first ? 1 - k : k];
+        if (o.out == nullptr) continue;
+        at += o.tiles();
+        const int64_t more = ceil_div(at, kClusters) - rounds;
+        longest += more * (static_cast<double>(ceil_div(o.blocks, o.splits)) * block_cycles(bn) + kTileCycles);
+        rounds += more;
+    }
+    return cost + longest;
+}
+
+template <typename T, GluProduct P, int BN> int launch_product(const ProductMaps& maps, const ProductParams& p, cudaStream_t s) {
     auto kern = glu_product_kernel<T, P, BN>;
     constexpr int smem = ProductShape<BN>::kSmem;
     // the attribute stays with the kernel: set once per device (bits of the first 64 devices)
@@ -132,23 +162,17 @@ int launch_product(const CUtensorMap& a, const CUtensorMap& b0, const CUtensorMa
         if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return cuda_failed(e);
         set.fetch_or(bit, std::memory_order_relaxed);
     }
-    const int64_t tiles = p.row_tiles * p.col_tiles * p.splits;
-    kern<<<static_cast<unsigned>(2 * (tiles < kClusters ? tiles : kClusters)), kProductThreads, smem, s>>>(a, b0, b1, p);
+    const int64_t tiles = p.part[0].tiles() + p.part[1].tiles();
+    kern<<<static_cast<unsigned>(2 * (tiles < kClusters ? tiles : kClusters)), kProductThreads, smem, s>>>(maps, p);
     note_launch();
     const int st = check_launch();
-    if (st != BZ_OK || p.splits == 1) return st;
-    const int64_t groups = p.row_tiles * p.col_tiles * (256 * BN / 4 / 256);
-    glu_shares_kernel<T, BN><<<static_cast<unsigned>(groups < 16 * kNumSMs ? groups : 16 * kNumSMs), 256, 0, s>>>(p, P == kWeight);
+    if (P == kForward || st != BZ_OK || (p.part[0].splits < 2 && p.part[1].splits < 2)) return st;
+    int64_t groups = 0;
+    for (const ProductPart& o : p.part)
+        if (o.splits > 1) groups = std::max(groups, o.row_tiles * o.col_tiles * (256 * BN / 4 / 256));
+    glu_shares_kernel<T, BN><<<static_cast<unsigned>(std::min<int64_t>(groups, 16 * kNumSMs)), 256, 0, s>>>(p);
     note_launch();
     return check_launch();
-}
-
-template <typename T, GluProduct P>
-int product(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b0, const CUtensorMap& b1, const ProductParams& p, cudaStream_t s) {
-    if (pl.bn == 256) return launch_product<T, P, 256>(a, b0, b1, p, s);
-    if constexpr (P == kForward)
-        if (pl.bn == 64) return launch_product<T, P, 64>(a, b0, b1, p, s);
-    return launch_product<T, P, 128>(a, b0, b1, p, s);
 }
 
 int zero(void* p, int64_t ld, int64_t rows, int64_t n, int bytes, cudaStream_t s) {
@@ -194,16 +218,18 @@ int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t
         (st = lay_out(wu, ld_w, n, k, ws, ou, s)) != BZ_OK)
         return st;
     ProductParams p{};
-    p.rows = m, p.cols = n, p.blocks = ceil_div(k, kBlockK);
-    const Plan pl = plan(kForward, m, n, p.blocks);
-    p.row_tiles = ceil_div(m, kRowTile), p.col_tiles = ceil_div(n, pl.bn / 2), p.splits = 1;
-    p.act = act, p.out = h, p.ld_out = ld_h, p.wide = wide_rows(h, ld_h, m, 2), p.pairs = pair_rows(h, ld_h, m, 2);
-    p.preact = preact, p.preact_wide = n % 4 == 0, p.preact_pairs = n % 2 == 0;
-    CUtensorMap a, b0, b1;
-    if (!make_map<T>(&a, ox.p, k, m, ox.ld, 128, 0) || !make_map<T>(&b0, og.p, k, n, og.ld, pl.bn / 2, 0) ||
-        !make_map<T>(&b1, ou.p, k, n, ou.ld, pl.bn / 2, 0))
+    ProductPart& o = p.part[0];
+    o.rows = m, o.cols = n, o.blocks = ceil_div(k, kBlockK);
+    const int bn = plan_forward(m, n, o.blocks);
+    o.row_tiles = ceil_div(m, kRowTile), o.col_tiles = ceil_div(n, bn / 2), o.splits = 1;
+    o.out = h, o.ld_out = ld_h, o.wide = wide_rows(h, ld_h, m, 2), o.pairs = pair_rows(h, ld_h, m, 2);
+    p.act = act, p.preact = preact, p.preact_wide = n % 4 == 0, p.preact_pairs = n % 2 == 0;
+    ProductMaps maps;
+    if (!make_map<T>(&maps.map[0], ox.p, k, m, ox.ld, 128, 0) || !make_map<T>(&maps.map[1], og.p, k, n, og.ld, bn / 2, 0) ||
+        !make_map<T>(&maps.map[2], ou.p, k, n, ou.ld, bn / 2, 0))
         return BZ_ERR_UNSUPPORTED;
-    return product<T, kForward>(pl, a, b0, b1, p, s);
+    if (bn == 256) return launch_product<T, kForward, 256>(maps, p, s);
+    return bn == 128 ? launch_product<T, kForward, 128>(maps, p, s) : launch_product<T, kForward, 64>(maps, p, s);
 }
 
 template <typename T, int ACT>
@@ -239,34 +265,40 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
         default: st = launch_dgu<T, BZ_ACT_RELU>(preact, d, ld_dh, m, n, dgu, ld, s); break;
     }
     if (st != BZ_OK) return st;
-    CUtensorMap a, b0, b1;
     ProductParams p{};
-    p.cols = k, p.partial = partial;
+    ProductMaps maps;
     if (dx != nullptr) {
         Operand og, ou;
         if ((st = lay_out(wg, ld_w, n, k, room, og, s)) != BZ_OK || (st = lay_out(wu, ld_w, n, k, room, ou, s)) != BZ_OK) return st;
-        p.rows = m, p.blocks = ceil_div(n, kBlockK);
-        const Plan pl = plan(kInput, m, k, 2 * p.blocks);
-        p.row_tiles = ceil_div(m, kRowTile), p.col_tiles = ceil_div(k, pl.bn), p.splits = pl.splits;
-        p.out = dx, p.ld_out = ld_dx, p.wide = wide_rows(dx, ld_dx, m, 2), p.pairs = pair_rows(dx, ld_dx, m, 2);
-        if (!make_map<T>(&a, dgu, n, m, ld, 128, m * ld) || !make_map<T>(&b0, og.p, k, n, og.ld, kBlockK, 0) ||
-            !make_map<T>(&b1, ou.p, k, n, ou.ld, kBlockK, 0))
+        ProductPart& o = p.part[kInput];
+        o.rows = m, o.cols = k, o.half_blocks = ceil_div(n, kBlockK), o.blocks = 2 * o.half_blocks;
+        o.out = dx, o.ld_out = ld_dx, o.wide = wide_rows(dx, ld_dx, m, 2), o.pairs = pair_rows(dx, ld_dx, m, 2);
+        if (!make_map<T>(&maps.map[0], dgu, n, m, ld, 128, m * ld) || !make_map<T>(&maps.map[1], og.p, k, n, og.ld, kBlockK, 0) ||
+            !make_map<T>(&maps.map[2], ou.p, k, n, ou.ld, kBlockK, 0))
             return BZ_ERR_UNSUPPORTED;
-        if ((st = product<T, kInput>(pl, a, b0, b1, p, s)) != BZ_OK) return st;
     }
     if (dwg != nullptr) {
         Operand ox;
         if ((st = lay_out(x, ld_x, m, k, room, ox, s)) != BZ_OK) return st;
-        p.rows = n, p.blocks = ceil_div(m, kBlockK);
-        const Plan pl = plan(kWeight, n, k, p.blocks);
-        p.row_tiles = 2 * ceil_div(n, kRowTile), p.col_tiles = ceil_div(k, pl.bn), p.splits = pl.splits;
-        p.out = dwg, p.out2 = dwu, p.ld_out = ld_dw, p.out_f32 = grad_f32;
-        p.wide = wide_rows(dwg, ld_dw, n, grad_f32 ? 4 : 2) && aligned16(dwu);
-        p.pairs = pair_rows(dwg, ld_dw, n, grad_f32 ? 4 : 2) && pair_rows(dwu, ld_dw, n, grad_f32 ? 4 : 2);
-        if (!make_map<T>(&a, dgu, n, m, ld, kBlockK, m * ld) || !make_map<T>(&b0, ox.p, k, m, ox.ld, kBlockK, 0)) return BZ_ERR_UNSUPPORTED;
-        if ((st = product<T, kWeight>(pl, a, b0, b0, p, s)) != BZ_OK) return st;
+        const int bytes = grad_f32 ? 4 : 2;
+        ProductPart& o = p.part[kWeight];
+        o.rows = n, o.cols = k, o.blocks = ceil_div(m, kBlockK);
+        o.out = dwg, o.out2 = dwu, o.ld_out = ld_dw, o.out_f32 = grad_f32;
+        o.wide = wide_rows(dwg, ld_dw, n, bytes) && aligned16(dwu);
+        o.pairs = pair_rows(dwg, ld_dw, n, bytes) && pair_rows(dwu, ld_dw, n, bytes);
+        if (!make_map<T>(&maps.map[3], dgu, n, m, ld, kBlockK, m * ld) || !make_map<T>(&maps.map[4], ox.p, k, m, ox.ld, kBlockK, 0))
+            return BZ_ERR_UNSUPPORTED;
     }
-    return BZ_OK;
+    if (dx == nullptr) maps.map[0] = maps.map[1] = maps.map[2] = maps.map[3];   // prefetched, not used
+    if (dwg == nullptr) maps.map[3] = maps.map[4] = maps.map[0];
+    const double narrow = plan_backward(p, 128);
+    const bool wide = plan_backward(p, 256) <= narrow;
+    if (!wide) plan_backward(p, 128);
+    const int bn = wide ? 256 : 128;
+    float* at = partial;
+    for (ProductPart& o : p.part)
+        if (o.splits > 1) o.partial = at, at += o.tiles() * kRowTile * bn;
+    return wide ? launch_product<T, kBackward, 256>(maps, p, s) : launch_product<T, kBackward, 128>(maps, p, s);
 }
 
 int check(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, int64_t m, int64_t n, int64_t k, int dtype, int act) {

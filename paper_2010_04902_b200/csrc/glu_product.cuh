@@ -1,8 +1,10 @@
-// The three products of the gated feed-forward block on the tensor cores, one kernel template.
+// The products of the gated feed-forward block on the tensor cores, one kernel template.
 //
 //   kForward   [g | u] = x [w_gate | w_up]^T      rows m, columns n (gate and up side by side), contraction k
-//   kInput     dx = dg w_gate + du w_up           rows m, columns k, contraction over both halves of n
-//   kWeight    dw_gate | dw_up = (dg | du)^T x    rows n (gate tiles, then up tiles), columns k, contraction m
+//   kBackward  both gradients in one launch, tiles of either kind in one list (a launch of its own for each would cost
+//              seven microseconds more, which is most of a small step):
+//              kInput   dx = dg w_gate + du w_up           rows m, columns k, contraction over both halves of n
+//              kWeight  dw_gate | dw_up = (dg | du)^T x    rows n (gate tiles, then up tiles), columns k, contraction m
 //
 // A pair of CTAs (one cluster) computes a 256 x BN tile with tcgen05.mma.cta_group::2, K = 16 an instruction: a pair
 // reads half as much of B from shared memory per flop as two single CTAs would.  Operands arrive by TMA in blocks of 64
@@ -11,11 +13,13 @@
 // MMA reads the block across rows.  For the forward product CTA 0 brings gate columns and CTA 1 up columns of the same
 // BN/2 hidden units, so g and u of a unit meet in one thread of the epilogue and h = act(g)*u leaves without another pass.
 // Accumulators: two sets of BN tensor-memory columns in turn, so a tile's epilogue runs under the next tile's MMAs.
+// Eight epilogue warps: two to each quarter of the lanes, steps of columns in turn.
 //
-// Persistent: at most one cluster per pair of SMs; tiles in groups of eight row tiles, columns inside a group in turn, so
-// that the operands of the tiles in flight stay in the L2.  kInput and kWeight may be cut along the contraction when there
-// are fewer tiles than clusters; each share then leaves binary32 sums in the workspace and a last kernel adds the
-// shares in order.
+// Persistent: at most one cluster per pair of SMs; tiles in groups of sixteen row tiles, columns inside a group in turn, so
+// that the operands of the tiles in flight stay in the L2 (8192 x 4096 x 8192 forward: 934 us with groups of four, 900
+// with eight, 880 with sixteen, sustained).  Tiles of the backward products may be cut along the contraction when there are
+// fewer of them than clusters; each share then leaves binary32 sums in the workspace and a last kernel adds the shares in
+// order.
 //
 // Every wait is bounded: a thread whose wait runs out sets its CTA's `dead` word, all roles leave their loops, the leader
 // waits (bounded again) for the loads in flight, and both CTAs meet at the cluster barrier before tensor memory is freed.
@@ -28,23 +32,35 @@ namespace bz {
 
 static __device__ unsigned int g_glu_timeouts = 0;
 
-enum GluProduct { kForward, kInput, kWeight };
+enum GluProduct { kForward, kBackward };
+enum GluKind { kInput, kWeight };
 
 constexpr int kRowTile = 256, kBlockK = 64, kEpilogueWarps = 8, kProductThreads = 128 + 32 * kEpilogueWarps;
 
-struct ProductParams {
-    int64_t rows, cols;          // extents of the result (kWeight: rows of one half; kForward: hidden units)
+// One result: h, or dx, or both weights' gradients.
+struct ProductPart {
+    int64_t rows, cols;          // extents (kWeight: rows of one half; kForward: hidden units)
     int64_t row_tiles, col_tiles;
-    int64_t blocks;              // of kBlockK along the contraction (kInput: of one half)
+    int64_t blocks;              // of kBlockK along the contraction
+    int64_t half_blocks;         // kInput: of one half of it
     int splits;                  // shares of the contraction
-    int act;
     void* out;                   // h / dx / dw_gate
     void* out2;                  // dw_up
     int64_t ld_out;
     int out_f32, wide, pairs;    // binary32 output; 16-byte stores possible; stores of two elements possible
+    float* partial;              // splits > 1: [split][tile][256][BN]
+    __host__ __device__ int64_t tiles() const { return row_tiles * col_tiles * splits; }
+};
+struct ProductParams {
+    ProductPart part[2];         // kForward: the first; kBackward: by GluKind
+    int weight_first;            // the order of the two in the list of tiles: longer contractions first
+    int act;
     float* preact;               // kForward: [2][rows][cols] or null
     int preact_wide, preact_pairs;
-    float* partial;              // splits > 1: [split][tile][256][BN]
+};
+// kForward: x, w_gate, w_up.  kBackward: dgu by rows, w_gate, w_up, dgu across rows, x.
+struct ProductMaps {
+    CUtensorMap map[5];
 };
 
 // ---- stores -------------------------------------------------------------------------------------
@@ -129,37 +145,40 @@ template <int ACT> __device__ __forceinline__ void gate32(float (&g)[32], const 
 }
 
 struct ProductTile {
+    int kind;          // GluKind
+    int64_t index;     // in its part
     int64_t row, col;  // in tiles
-    int split;
+    int64_t from, to;  // contraction blocks
 };
-__device__ __forceinline__ ProductTile tile_at(const ProductParams& p, int64_t i) {
-    constexpr int64_t G = 8;
-    ProductTile t;
-    const int64_t per = p.row_tiles * p.col_tiles;
-    t.split = static_cast<int>(i / per);
-    i -= t.split * per;
-    const int64_t g = i / (G * p.col_tiles), first = g * G;
-    const int64_t n = min(G, p.row_tiles - first);
+__device__ __forceinline__ void place_tile(const ProductPart& p, int64_t i, ProductTile& t) {
+    constexpr int64_t G = 16;
+    const int64_t per = p.row_tiles * p.col_tiles, split = i / per;
+    t.index = i;
+    i -= split * per;
+    const int64_t g = i / (G * p.col_tiles), first = g * G, n = min(G, p.row_tiles - first);
     i -= g * G * p.col_tiles;
     t.row = first + i % n;
     t.col = i / n;
+    t.from = p.blocks * split / p.splits;
+    t.to = p.blocks * (split + 1) / p.splits;
+}
+template <GluProduct P> __device__ __forceinline__ ProductTile tile_at(const ProductParams& p, int64_t i) {
+    ProductTile t;
+    t.kind = kInput;
+    if (P == kBackward) {
+        t.kind = p.weight_first ? kWeight : kInput;
+        const int64_t n = p.part[t.kind].tiles();
+        if (i >= n) i -= n, t.kind ^= 1;
+    }
+    place_tile(p.part[t.kind], i, t);
     return t;
 }
-// Contraction blocks [from, to) of a share.
-__device__ __forceinline__ void share_of(const ProductParams& p, int64_t all, int split, int64_t& from, int64_t& to) {
-    from = all * split / p.splits;
-    to = all * (split + 1) / p.splits;
-}
 
-// b0 / b1: the B operands of the two halves (kForward: CTA 0's and CTA 1's; kInput: of the first and second half of the
-// contraction; kWeight: b0 alone).
 template <typename T, GluProduct P, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
-    glu_product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b0_map,
-                       const __grid_constant__ CUtensorMap b1_map, const __grid_constant__ ProductParams p) {
+    glu_product_kernel(const __grid_constant__ ProductMaps maps, const __grid_constant__ ProductParams p) {
     using S = ProductShape<BN>;
-    constexpr bool kAcrossA = P == kWeight, kAcrossB = P != kForward;
-    constexpr uint32_t kIdesc = idesc_16bit(256, BN, sizeof(T) == 2 && !__is_same(T, __half), kAcrossA, kAcrossB);
+    constexpr int kBf16 = !__is_same(T, __half);
     constexpr int kBlockBytes = 64 * kBlockK * 2;   // 64 rows of 128 bytes
     extern __shared__ unsigned char raw[];
     unsigned char* smem = raw + (1024 - smem_u32(raw) % 1024) % 1024;
@@ -174,12 +193,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int64_t cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
-    const int64_t tiles = p.row_tiles * p.col_tiles * p.splits;
-    const int64_t blocks = P == kInput ? 2 * p.blocks : p.blocks;
-    if (warp == 3 && lane < 3) {
-        const CUtensorMap* map = lane == 0 ? &a_map : (lane == 1 ? &b0_map : &b1_map);
-        asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
-    }
+    const int64_t tiles = p.part[0].tiles() + (P == kBackward ? p.part[1].tiles() : 0);
+    if (warp == 3 && lane < (P == kForward ? 3 : 5)) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.map[lane]) : "memory");
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
         for (int s = 0; s < 2; ++s) mbar_init(&acc_full[s], 1), mbar_init(&acc_empty[s], 2 * kEpilogueWarps);
@@ -198,10 +213,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
         // ---------------------------------------------------------------- loads
         bool alive = true;
         for (int64_t i = cluster; i < tiles && alive; i += clusters) {
-            const ProductTile t = tile_at(p, i);
-            int64_t from, to;
-            share_of(p, blocks, t.split, from, to);
-            for (int64_t kb = from; kb < to; ++kb, ++it) {
+            const ProductTile t = tile_at<P>(p, i);
+            for (int64_t kb = t.from; kb < t.to; ++kb, ++it) {
                 const int s = static_cast<int>(it % S::kStages);
                 const uint32_t round = static_cast<uint32_t>(it / S::kStages);
                 if (round > 0 && !mbar_wait_live(&empty[s], (round - 1) & 1, dead)) {
@@ -213,24 +226,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
                 const uint32_t a = smem_u32(smem + s * S::kStageBytes), b = a + S::kABytes;
                 if constexpr (P == kForward) {
                     const int x = static_cast<int>(kb * kBlockK);
-                    tma_load_pair(a, &a_map, bar, x, static_cast<int>(t.row * 256 + rank * 128));
-                    tma_load_pair(b, rank == 0 ? &b0_map : &b1_map, bar, x, static_cast<int>(t.col * (BN / 2)));
-                } else if constexpr (P == kInput) {
-                    const int half = kb >= p.blocks, x = static_cast<int>((kb - half * p.blocks) * kBlockK);
-                    tma_load_pair(a, &a_map, bar, x, static_cast<int>(t.row * 256 + rank * 128), half);
-#pragma unroll
-                    for (int c = 0; c < BN / 128; ++c)
-                        tma_load_pair(b + c * kBlockBytes, half ? &b1_map : &b0_map, bar, static_cast<int>(t.col * BN + rank * (BN / 2) + c * 64), x);
+                    tma_load_pair(a, &maps.map[0], bar, x, static_cast<int>(t.row * 256 + rank * 128));
+                    tma_load_pair(b, &maps.map[1 + rank], bar, x, static_cast<int>(t.col * (BN / 2)));
                 } else {
-                    const int y = static_cast<int>(kb * kBlockK);
-                    const int64_t half_tiles = p.row_tiles / 2;
-                    const int half = t.row >= half_tiles;
-                    const int x = static_cast<int>((t.row - half * half_tiles) * 256 + rank * 128);
-                    tma_load_pair(a, &a_map, bar, x, y, half);
-                    tma_load_pair(a + kBlockBytes, &a_map, bar, x + 64, y, half);
+                    const int columns = static_cast<int>(t.col * BN + rank * (BN / 2));
+                    if (t.kind == kInput) {
+                        const int half = kb >= p.part[kInput].half_blocks, x = static_cast<int>((kb - half * p.part[kInput].half_blocks) * kBlockK);
+                        tma_load_pair(a, &maps.map[0], bar, x, static_cast<int>(t.row * 256 + rank * 128), half);
 #pragma unroll
-                    for (int c = 0; c < BN / 128; ++c)
-                        tma_load_pair(b + c * kBlockBytes, &b0_map, bar, static_cast<int>(t.col * BN + rank * (BN / 2) + c * 64), y);
+                        for (int c = 0; c < BN / 128; ++c) tma_load_pair(b + c * kBlockBytes, &maps.map[1 + half], bar, columns + c * 64, x);
+                    } else {
+                        const int y = static_cast<int>(kb * kBlockK);
+                        const int64_t half_tiles = p.part[kWeight].row_tiles / 2;
+                        const int half = t.row >= half_tiles, x = static_cast<int>((t.row - half * half_tiles) * 256 + rank * 128);
+                        tma_load_pair(a, &maps.map[3], bar, x, y, half);
+                        tma_load_pair(a + kBlockBytes, &maps.map[3], bar, x + 64, y, half);
+#pragma unroll
+                        for (int c = 0; c < BN / 128; ++c) tma_load_pair(b + c * kBlockBytes, &maps.map[4], bar, columns + c * 64, y);
+                    }
                 }
             }
         }
@@ -239,13 +252,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
         int64_t n = 0;
         bool alive = true;
         for (int64_t i = cluster; i < tiles && alive; i += clusters, ++n) {
-            const ProductTile t = tile_at(p, i);
-            int64_t from, to;
-            share_of(p, blocks, t.split, from, to);
+            const ProductTile t = tile_at<P>(p, i);
+            const bool across_a = P == kBackward && t.kind == kWeight;
+            constexpr bool kAcrossB = P == kBackward;
+            const uint32_t idesc = across_a ? idesc_16bit(256, BN, kBf16, 1, kAcrossB) : idesc_16bit(256, BN, kBf16, 0, kAcrossB);
             const int acc = static_cast<int>(n & 1);
             if (n >= 2 && !mbar_wait_live(&acc_empty[acc], static_cast<uint32_t>((n >> 1) - 1) & 1, dead)) break;
             tc_fence_after_sync();
-            for (int64_t kb = from; kb < to; ++kb, ++it) {
+            for (int64_t kb = t.from; kb < t.to; ++kb, ++it) {
                 const int s = static_cast<int>(it % S::kStages);
                 if (!mbar_wait_live(&full[s], static_cast<uint32_t>(it / S::kStages) & 1, dead)) {
                     alive = false;
@@ -255,9 +269,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
                 const uint32_t a = smem_u32(smem + s * S::kStageBytes), b = a + S::kABytes;
 #pragma unroll
                 for (int k = 0; k < kBlockK / 16; ++k) {
-                    const uint64_t da = kAcrossA ? smem_desc_mn128(a + k * 2048, kBlockBytes) : smem_desc_k128(a + k * 32);
+                    const uint64_t da = across_a ? smem_desc_mn128(a + k * 2048, kBlockBytes) : smem_desc_k128(a + k * 32);
                     const uint64_t db = kAcrossB ? smem_desc_mn128(b + k * 2048, kBlockBytes) : smem_desc_k128(b + k * 32);
-                    mma_16bit_pair(tmem + acc * 256, da, db, kIdesc, kb > from || k > 0);
+                    mma_16bit_pair(tmem + acc * 256, da, db, idesc, kb > t.from || k > 0);
                 }
                 mma_commit_pair(&empty[s]);
             }
@@ -269,7 +283,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
         float* turn = turns + (warp - 4) * (kTurnBytes / 4);
         int64_t n = 0;
         for (int64_t i = cluster; i < tiles; i += clusters, ++n) {
-            const ProductTile t = tile_at(p, i);
+            const ProductTile t = tile_at<P>(p, i);
+            const ProductPart& o = p.part[t.kind];
             const int acc = static_cast<int>(n & 1);
             if (!__all_sync(~0u, mbar_wait_live(&acc_full[acc], static_cast<uint32_t>(n >> 1) & 1, dead))) break;  // a warp leaves as one
             tc_fence_after_sync();
@@ -293,12 +308,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 #pragma unroll
                             for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<float>::pack(g + 4 * e));
                             __syncwarp();
-                            turn_out<float>(turn, p.preact, p.cols, r0, p.rows, c0, p.cols, p.preact_wide, p.preact_pairs);
+                            turn_out<float>(turn, p.preact, o.cols, r0, o.rows, c0, o.cols, p.preact_wide, p.preact_pairs);
                             __syncwarp();
 #pragma unroll
                             for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<float>::pack(u + 4 * e));
                             __syncwarp();
-                            turn_out<float>(turn, p.preact + p.rows * p.cols, p.cols, r0, p.rows, c0, p.cols, p.preact_wide, p.preact_pairs);
+                            turn_out<float>(turn, p.preact + o.rows * o.cols, o.cols, r0, o.rows, c0, o.cols, p.preact_wide, p.preact_pairs);
                             __syncwarp();
                         }
                         switch (p.act) {
@@ -314,15 +329,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
                     for (int e = 0; e < kStep / 8; ++e) turn_in(turn, 4 * e, h[e]);
                     __syncwarp();
                     const int64_t c0 = t.col * (BN / 2) + c;
-                    turn_out<T>(turn, static_cast<T*>(p.out), p.ld_out, r0, p.rows, c0, min(p.cols, c0 + kStep), p.wide, p.pairs);
+                    turn_out<T>(turn, static_cast<T*>(o.out), o.ld_out, r0, o.rows, c0, min(o.cols, c0 + kStep), o.wide, o.pairs);
                     __syncwarp();
                 }
             } else {
-                const int64_t half_tiles = P == kWeight ? p.row_tiles / 2 : 0;
-                const int half = P == kWeight && t.row >= half_tiles;
+                const int64_t half_tiles = t.kind == kWeight ? o.row_tiles / 2 : 0;
+                const int half = t.kind == kWeight && t.row >= half_tiles;
                 const int64_t r0 = (t.row - half * half_tiles) * 256 + in_tile;
-                void* out = half ? p.out2 : p.out;
-                const bool f32 = p.out_f32 || p.splits > 1;
+                void* out = half ? o.out2 : o.out;
+                const bool f32 = o.out_f32 || o.splits > 1;
 #pragma unroll 1
                 for (int c = half_of_columns * 64; c < BN; c += 128) {
                     float x[2][32];
@@ -336,17 +351,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 #pragma unroll
                             for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<float>::pack(x[k] + 4 * e));
                             __syncwarp();
-                            if (p.splits > 1)
-                                turn_out<float>(turn, p.partial + i * 256 * BN, BN, in_tile, 256, c + k * 32, BN, true, false);
+                            if (o.splits > 1)
+                                turn_out<float>(turn, o.partial + t.index * 256 * BN, BN, in_tile, 256, c + k * 32, BN, true, false);
                             else
-                                turn_out<float>(turn, static_cast<float*>(out), p.ld_out, r0, p.rows, t.col * BN + c + k * 32, p.cols, p.wide, p.pairs);
+                                turn_out<float>(turn, static_cast<float*>(out), o.ld_out, r0, o.rows, t.col * BN + c + k * 32, o.cols, o.wide, o.pairs);
                             __syncwarp();
                         }
                     } else {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) turn_in(turn, 4 * e, Word<T>::pack(x[e / 4] + e % 4 * 8));
                         __syncwarp();
-                        turn_out<T>(turn, static_cast<T*>(out), p.ld_out, r0, p.rows, t.col * BN + c, p.cols, p.wide, p.pairs);
+                        turn_out<T>(turn, static_cast<T*>(out), o.ld_out, r0, o.rows, t.col * BN + c, o.cols, o.wide, o.pairs);
                         __syncwarp();
                     }
                 }
@@ -370,15 +385,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     if (warp == 2) tmem_dealloc_pair(tmem, 512);
 }
 
-// The shares' sums of one product, in order: one thread a group of four columns.
-template <typename T, int BN>
-__global__ void __launch_bounds__(256) glu_shares_kernel(const __grid_constant__ ProductParams p, int weight) {
+// The shares' sums of a part, in order: one thread a group of four columns.
+template <typename T, int BN> __device__ __forceinline__ void add_shares(const ProductPart& p, bool weight) {
+    if (p.splits < 2) return;
     const int64_t per = p.row_tiles * p.col_tiles, groups = per * 256 * (BN / 4);
     const int64_t half_tiles = weight ? p.row_tiles / 2 : 0;
     for (int64_t e = blockIdx.x * int64_t(256) + threadIdx.x; e < groups; e += gridDim.x * int64_t(256)) {
         const int64_t i = e / (256 * (BN / 4));
         const int in = static_cast<int>(e % (256 * (BN / 4))), in_row = in / (BN / 4), c = in % (BN / 4) * 4;
-        const ProductTile t = tile_at(p, i);
+        ProductTile t;
+        place_tile(p, i, t);
         const int half = weight && t.row >= half_tiles;
         const int64_t r = (t.row - half * half_tiles) * 256 + in_row, c0 = t.col * BN + c;
         if (r >= p.rows || c0 >= p.cols) continue;
@@ -397,6 +413,10 @@ __global__ void __launch_bounds__(256) glu_shares_kernel(const __grid_constant__
                     static_cast<T*>(out)[r * p.ld_out + c0 + k] = from_f32<T>(x[k]);
             }
     }
+}
+template <typename T, int BN> __global__ void __launch_bounds__(256) glu_shares_kernel(const __grid_constant__ ProductParams p) {
+    add_shares<T, BN>(p.part[kInput], false);
+    add_shares<T, BN>(p.part[kWeight], true);
 }
 
 }  // namespace bz
