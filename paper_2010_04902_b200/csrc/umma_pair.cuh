@@ -104,4 +104,17 @@ __device__ __forceinline__ void tmem_ld32_wait(float (&x)[32]) {
                  : "memory");
 }
 
+// The same for eight columns.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&x)[8]) {
+    uint32_t* u = reinterpret_cast<uint32_t*>(x);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+                 : "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_ld8_wait(float (&x)[8]) {
+    uint32_t* u = reinterpret_cast<uint32_t*>(x);
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]) : : "memory");
+}
+
 }  // namespace bz
