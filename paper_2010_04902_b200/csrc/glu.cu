@@ -100,7 +100,8 @@ template <typename T> bool make_map(CUtensorMap* map, const void* p, int64_t n, 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Cycles of a block of the contraction and of a tile's ends, for choosing the width of the tiles: 256 columns a tile fill the
-// tensor cores (520 cycles a block), narrower tiles are bound by the loads of A but part the work more evenly.
+// tensor cores (512 cycles a block); narrower ones are bound by their loads out of the L2, which a block of A shares among
+// fewer columns, but part the work more evenly.
 double block_cycles(int bn) { return bn == 256 ? 520 : (bn == 128 ? 380 : 320); }
 constexpr double kTileCycles = 1500, kSharesCycles = 4000;
 
@@ -166,13 +167,16 @@ template <typename T, GluProduct P, int BN> int launch_product(const ProductMaps
     kern<<<static_cast<unsigned>(2 * (tiles < kClusters ? tiles : kClusters)), kProductThreads, smem, s>>>(maps, p);
     note_launch();
     const int st = check_launch();
-    if (P == kForward || st != BZ_OK || (p.part[0].splits < 2 && p.part[1].splits < 2)) return st;
-    int64_t groups = 0;
-    for (const ProductPart& o : p.part)
-        if (o.splits > 1) groups = std::max(groups, o.row_tiles * o.col_tiles * (256 * BN / 4 / 256));
-    glu_shares_kernel<T, BN><<<static_cast<unsigned>(std::min<int64_t>(groups, 16 * kNumSMs)), 256, 0, s>>>(p);
-    note_launch();
-    return check_launch();
+    if constexpr (P == kBackward) {
+        int64_t groups = 0;
+        for (const ProductPart& o : p.part)
+            if (o.splits > 1) groups = std::max(groups, o.row_tiles * o.col_tiles * (256 * BN / 4 / 256));
+        if (st != BZ_OK || groups == 0) return st;
+        glu_shares_kernel<T, BN><<<static_cast<unsigned>(std::min<int64_t>(groups, 16 * kNumSMs)), 256, 0, s>>>(p);
+        note_launch();
+        return check_launch();
+    }
+    return st;
 }
 
 int zero(void* p, int64_t ld, int64_t rows, int64_t n, int bytes, cudaStream_t s) {
@@ -292,13 +296,12 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
     if (dx == nullptr) maps.map[0] = maps.map[1] = maps.map[2] = maps.map[3];   // prefetched, not used
     if (dwg == nullptr) maps.map[3] = maps.map[4] = maps.map[0];
     const double narrow = plan_backward(p, 128);
-    const bool wide = plan_backward(p, 256) <= narrow;
-    if (!wide) plan_backward(p, 128);
-    const int bn = wide ? 256 : 128;
+    const int bn = plan_backward(p, 256) <= narrow ? 256 : 128;
+    if (bn == 128) plan_backward(p, 128);
     float* at = partial;
     for (ProductPart& o : p.part)
         if (o.splits > 1) o.partial = at, at += o.tiles() * kRowTile * bn;
-    return wide ? launch_product<T, kBackward, 256>(maps, p, s) : launch_product<T, kBackward, 128>(maps, p, s);
+    return bn == 256 ? launch_product<T, kBackward, 256>(maps, p, s) : launch_product<T, kBackward, 128>(maps, p, s);
 }
 
 int check(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, int64_t m, int64_t n, int64_t k, int dtype, int act) {

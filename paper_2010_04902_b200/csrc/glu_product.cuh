@@ -13,11 +13,12 @@
 // MMA reads the block across rows.  For the forward product CTA 0 brings gate columns and CTA 1 up columns of the same
 // BN/2 hidden units, so g and u of a unit meet in one thread of the epilogue and h = act(g)*u leaves without another pass.
 // Accumulators: two sets of BN tensor-memory columns in turn, so a tile's epilogue runs under the next tile's MMAs.
+// (Tiles of 512 columns over both sets, one ahead of the other, were tried: 842 us against 725 below.)
 // Eight epilogue warps: two to each quarter of the lanes, steps of columns in turn.
 //
 // Persistent: at most one cluster per pair of SMs; tiles in groups of sixteen row tiles, columns inside a group in turn, so
 // that the operands of the tiles in flight stay in the L2 (8192 x 4096 x 8192 forward: 934 us with groups of four, 900
-// with eight, 880 with sixteen, sustained).  Tiles of the backward products may be cut along the contraction when there are
+// with eight, 880 with sixteen, sustained, before the issue loop counted its stages; 800 since: 1374 TFLOP/s).  Tiles of the backward products may be cut along the contraction when there are
 // fewer of them than clusters; each share then leaves binary32 sums in the workspace and a last kernel adds the shares in
 // order.
 //
@@ -65,13 +66,14 @@ struct ProductMaps {
 
 // ---- stores -------------------------------------------------------------------------------------
 // The accumulator gives a thread one row; memory wants a warp on one row.  A warp turns 32 rows x 32 words (128 bytes of
-// each row) through shared memory: rows 36 words apart, so that both the 16-byte writes (eight rows) and the 16-byte
-// reads (one row) of a quarter warp meet every bank once.
+// each row) through shared memory, the 16-byte groups of row r exchanged by r mod 8, so that both the writes (eight rows)
+// and the reads (one row) of a quarter warp meet every bank once.
 
-constexpr int kTurnWords = 36, kTurnBytes = 32 * kTurnWords * 4;
+constexpr int kTurnBytes = 32 * 128;
 
+__device__ __forceinline__ int turned(int row, int word) { return row * 32 + (word ^ ((row & 7) << 2)); }
 __device__ __forceinline__ void turn_in(float* turn, int word, const uint4& w) {
-    *reinterpret_cast<uint4*>(turn + (threadIdx.x & 31) * kTurnWords + word) = w;
+    *reinterpret_cast<uint4*>(turn + turned(threadIdx.x & 31, word)) = w;
 }
 // Writes elements [c0, c0 + 128 / sizeof(E)) of rows r0 .. r0 + 31 of `out`; `rows`, `cols` exist.  wide: 16-byte stores
 // possible; pairs: stores of two elements possible.
@@ -86,27 +88,27 @@ __device__ __forceinline__ void turn_out(const float* turn, E* out, int64_t ld, 
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = i * 4 + lane / 8, w = lane % 8 * 4;
-            if (r < n_rows) *reinterpret_cast<uint4*>(base + r * ld + w * kPer) = *reinterpret_cast<const uint4*>(turn + r * kTurnWords + w);
+            if (r < n_rows) *reinterpret_cast<uint4*>(base + r * ld + w * kPer) = *reinterpret_cast<const uint4*>(turn + turned(r, w));
         }
     } else if (kPer == 1 && pairs && n == kEach) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int r = i * 2 + lane / 16, w = lane % 16 * 2;
-            if (r < n_rows) *reinterpret_cast<float2*>(base + r * ld + w) = *reinterpret_cast<const float2*>(turn + r * kTurnWords + w);
+            if (r < n_rows) *reinterpret_cast<float2*>(base + r * ld + w) = *reinterpret_cast<const float2*>(turn + turned(r, w));
         }
     } else if (kPer == 1 || (pairs && n % 2 == 0)) {
         if (lane * kPer < n) {
 #pragma unroll 8
             for (int r = 0; r < 32; ++r)
-                if (r < n_rows) *reinterpret_cast<float*>(base + r * ld + lane * kPer) = turn[r * kTurnWords + lane];
+                if (r < n_rows) *reinterpret_cast<float*>(base + r * ld + lane * kPer) = turn[turned(r, lane)];
         }
     } else {
 #pragma unroll 8
         for (int r = 0; r < 32; ++r) {
             if (r >= n_rows) break;
-            const E* from = reinterpret_cast<const E*>(turn + r * kTurnWords);
-            if (lane < n) base[r * ld + lane] = from[lane];
-            if (lane + 32 < n) base[r * ld + lane + 32] = from[lane + 32];
+            const E* from = reinterpret_cast<const E*>(turn);
+            if (lane < n) base[r * ld + lane] = from[turned(r, lane / kPer) * kPer + lane % kPer];
+            if (lane + 32 < n) base[r * ld + lane + 32] = from[turned(r, (lane + 32) / kPer) * kPer + lane % kPer];
         }
     }
 }
@@ -143,6 +145,17 @@ template <int ACT> __device__ __forceinline__ void gate(float (&g)[8], const flo
 #pragma unroll
     for (int i = 0; i < 8; ++i) g[i] = act<ACT>(g[i]) * u[i];
 }
+
+// Position in the ring: the stage and the parity of its current round.  Counted, not divided out: the threads that load and
+// issue run one instruction after another, and 64-bit remainders between
+// two MMAs cost a seventh of the rate (8192 x 4096 x 8192 forward: 825 against 725 us).
+template <int STAGES> struct RingAt {
+    int stage = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++stage == STAGES) stage = 0, parity ^= 1;
+    }
+};
 
 struct ProductTile {
     int kind;          // GluKind
@@ -207,42 +220,50 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     cluster_sync();
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
-    int64_t it = 0;   // blocks loaded (thread 0), multiplied (the issuing thread)
+    RingAt<S::kStages> at;          // of the loads (thread 0), of the MMAs (the issuing thread)
+    int filled = 0;                 // stages that have been loaded at least once (thread 0)
 
     if (warp == 0 && lane == 0) {
         // ---------------------------------------------------------------- loads
         bool alive = true;
+        const uint32_t smem_addr = smem_u32(smem), leader_full = leader_addr(full);
         for (int64_t i = cluster; i < tiles && alive; i += clusters) {
             const ProductTile t = tile_at<P>(p, i);
-            for (int64_t kb = t.from; kb < t.to; ++kb, ++it) {
-                const int s = static_cast<int>(it % S::kStages);
-                const uint32_t round = static_cast<uint32_t>(it / S::kStages);
-                if (round > 0 && !mbar_wait_live(&empty[s], (round - 1) & 1, dead)) {
-                    alive = false;
-                    break;
-                }
-                const uint32_t bar = leader_addr(&full[s]);
-                if (rank == 0) mbar_expect_tx(&full[s], 2 * S::kStageBytes);
-                const uint32_t a = smem_u32(smem + s * S::kStageBytes), b = a + S::kABytes;
-                if constexpr (P == kForward) {
-                    const int x = static_cast<int>(kb * kBlockK);
-                    tma_load_pair(a, &maps.map[0], bar, x, static_cast<int>(t.row * 256 + rank * 128));
-                    tma_load_pair(b, &maps.map[1 + rank], bar, x, static_cast<int>(t.col * (BN / 2)));
+            const int row = static_cast<int>(t.row * 256 + rank * 128), half_blocks = static_cast<int>(p.part[kInput].half_blocks);
+            const int column0 = static_cast<int>(P == kForward ? t.col * (BN / 2) : t.col * BN + rank * (BN / 2));
+            const int64_t half_tiles = p.part[kWeight].row_tiles / 2;
+            const int weight_half = t.row >= half_tiles, weight_x = static_cast<int>((t.row - weight_half * half_tiles) * 256 + rank * 128);
+            for (int kb = static_cast<int>(t.from); kb < static_cast<int>(t.to); ++kb, at.next()) {
+                const int s = at.stage;
+                if (filled == S::kStages) {
+                    if (!mbar_wait_live(&empty[s], at.parity ^ 1, dead)) {
+                        alive = false;
+                        break;
+                    }
                 } else {
-                    const int columns = static_cast<int>(t.col * BN + rank * (BN / 2));
+                    ++filled;
+                }
+                const uint32_t bar = leader_full + s * 8;
+                if (rank == 0) mbar_expect_tx(&full[s], 2 * S::kStageBytes);
+                const uint32_t a = smem_addr + s * S::kStageBytes, b = a + S::kABytes;
+                if constexpr (P == kForward) {
+                    const int x = kb * kBlockK;
+                    tma_load_pair(a, &maps.map[0], bar, x, row);
+                    tma_load_pair(b, &maps.map[1 + rank], bar, x, column0);
+                } else {
+                    // this CTA's half of the columns, in blocks of 64
+                    auto column = [&](int c) { return column0 + c * 64; };
                     if (t.kind == kInput) {
-                        const int half = kb >= p.part[kInput].half_blocks, x = static_cast<int>((kb - half * p.part[kInput].half_blocks) * kBlockK);
-                        tma_load_pair(a, &maps.map[0], bar, x, static_cast<int>(t.row * 256 + rank * 128), half);
+                        const int half = kb >= half_blocks, x = (kb - half * half_blocks) * kBlockK;
+                        tma_load_pair(a, &maps.map[0], bar, x, row, half);
 #pragma unroll
-                        for (int c = 0; c < BN / 128; ++c) tma_load_pair(b + c * kBlockBytes, &maps.map[1 + half], bar, columns + c * 64, x);
+                        for (int c = 0; c < BN / 128; ++c) tma_load_pair(b + c * kBlockBytes, &maps.map[1 + half], bar, column(c), x);
                     } else {
-                        const int y = static_cast<int>(kb * kBlockK);
-                        const int64_t half_tiles = p.part[kWeight].row_tiles / 2;
-                        const int half = t.row >= half_tiles, x = static_cast<int>((t.row - half * half_tiles) * 256 + rank * 128);
-                        tma_load_pair(a, &maps.map[3], bar, x, y, half);
-                        tma_load_pair(a + kBlockBytes, &maps.map[3], bar, x + 64, y, half);
+                        const int y = kb * kBlockK;
+                        tma_load_pair(a, &maps.map[3], bar, weight_x, y, weight_half);
+                        tma_load_pair(a + kBlockBytes, &maps.map[3], bar, weight_x + 64, y, weight_half);
 #pragma unroll
-                        for (int c = 0; c < BN / 128; ++c) tma_load_pair(b + c * kBlockBytes, &maps.map[4], bar, columns + c * 64, y);
+                        for (int c = 0; c < BN / 128; ++c) tma_load_pair(b + c * kBlockBytes, &maps.map[4], bar, column(c), y);
                     }
                 }
             }
@@ -256,24 +277,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
             const bool across_a = P == kBackward && t.kind == kWeight;
             constexpr bool kAcrossB = P == kBackward;
             const uint32_t idesc = across_a ? idesc_16bit(256, BN, kBf16, 1, kAcrossB) : idesc_16bit(256, BN, kBf16, 0, kAcrossB);
+            // descriptors of stage 0; a stage and a step of 16 along the contraction add to their address fields
+            constexpr uint32_t kStepA = 32 >> 4, kAcrossStep = 2048 >> 4, kStageStep = S::kStageBytes >> 4;
+            const uint64_t a0 = across_a ? smem_desc_mn128(smem_u32(smem), kBlockBytes) : smem_desc_k128(smem_u32(smem));
+            const uint64_t b0 = kAcrossB ? smem_desc_mn128(smem_u32(smem) + S::kABytes, kBlockBytes) : smem_desc_k128(smem_u32(smem) + S::kABytes);
+            const uint32_t step_a = across_a ? kAcrossStep : kStepA;
+            auto multiply = [&](int stage, uint32_t acc, bool first) {
+                const uint64_t da = a0 + stage * kStageStep, db = b0 + stage * kStageStep;
+#pragma unroll
+                for (int k = 0; k < kBlockK / 16; ++k)
+                    mma_16bit_pair(tmem + acc * 256, da + k * step_a, db + k * (kAcrossB ? kAcrossStep : kStepA), idesc, !first || k > 0);
+            };
             const int acc = static_cast<int>(n & 1);
             if (n >= 2 && !mbar_wait_live(&acc_empty[acc], static_cast<uint32_t>((n >> 1) - 1) & 1, dead)) break;
             tc_fence_after_sync();
-            for (int64_t kb = t.from; kb < t.to; ++kb, ++it) {
-                const int s = static_cast<int>(it % S::kStages);
-                if (!mbar_wait_live(&full[s], static_cast<uint32_t>(it / S::kStages) & 1, dead)) {
+            const int blocks = static_cast<int>(t.to - t.from);
+            for (int kb = 0; kb < blocks; ++kb, at.next()) {
+                if (!mbar_wait_live(&full[at.stage], at.parity, dead)) {
                     alive = false;
                     break;
                 }
                 tc_fence_after_sync();
-                const uint32_t a = smem_u32(smem + s * S::kStageBytes), b = a + S::kABytes;
-#pragma unroll
-                for (int k = 0; k < kBlockK / 16; ++k) {
-                    const uint64_t da = across_a ? smem_desc_mn128(a + k * 2048, kBlockBytes) : smem_desc_k128(a + k * 32);
-                    const uint64_t db = kAcrossB ? smem_desc_mn128(b + k * 2048, kBlockBytes) : smem_desc_k128(b + k * 32);
-                    mma_16bit_pair(tmem + acc * 256, da, db, idesc, kb > t.from || k > 0);
-                }
-                mma_commit_pair(&empty[s]);
+                multiply(at.stage, acc, kb == 0);
+                mma_commit_pair(&empty[at.stage]);
             }
             if (alive) mma_commit_pair(&acc_full[acc]);
         }
@@ -375,8 +401,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     if (threadIdx.x == 0 && *dead) {
         atomicAdd(&g_glu_timeouts, 1u);
         if (rank == 0)  // shared memory has to outlive the loads in flight, the other CTA's among them
-            for (int64_t j = it > S::kStages ? it - S::kStages : 0; j < it; ++j)
-                mbar_wait(&full[j % S::kStages], static_cast<uint32_t>(j / S::kStages) & 1);
+            for (int j = 0; j < filled; ++j, at.next()) mbar_wait(&full[filled < S::kStages ? j : at.stage], filled < S::kStages ? 0 : at.parity ^ 1);
     }
     tc_fence_before_sync();
     cluster_sync();

@@ -95,6 +95,14 @@ def test_matches(shape, dtype):
     check(*make(m, n, k, dtype, seed=m + n + k), ACTS[(m + n + k) % 4])
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(2048, 4100, 136), (2050, 4104, 1032), (4096, 2048, 1024), (9000, 600, 520)])
+def test_more_tiles_than_clusters(shape, dtype):
+    """The widest tiles and several rounds of them, whole and ragged."""
+    m, n, k = shape
+    check(*make(m, n, k, dtype, seed=m + n + k), ACTS[(m + n) % 4])
+
+
 @pytest.mark.parametrize("name", ACTS)
 @pytest.mark.parametrize("m", [2, 200])
 def test_activations(name, m):
