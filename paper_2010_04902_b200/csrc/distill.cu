@@ -315,7 +315,8 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
     __syncthreads();
     const bool grad = dlogits != nullptr;
     const int passes = grad && !hold ? 2 : 1;
-    int64_t seq = 0;   // chunks so far
+    RingAt<kRing> at;      // of the loads (producer), of the chunk in hand (workers)
+    int filled = 0;        // stages loaded at least once (producer)
     if (warp == kWorkers / 32 + kTeachers) {
         // ---------------------------------------------------------------- loads
         if (lane == 0) {
@@ -323,9 +324,11 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
             for (int64_t i = blockIdx.x; i < m && alive; i += gridDim.x) {
                 const T* row = logits + i * a.ld;
                 const RowWords<T> w(row, a.v);
-                for (int c = 0; c < passes * w.chunks; ++c, ++seq) {
-                    const int s = static_cast<int>(seq % kRing);
-                    if (seq >= kRing && !mbar_wait_live(&empty[s], static_cast<uint32_t>(seq / kRing - 1) & 1, dead)) {
+                for (int c = 0; c < passes * w.chunks; ++c, at.next()) {
+                    const int s = at.stage;
+                    if (filled < kRing) {
+                        ++filled;
+                    } else if (!mbar_wait_live(&empty[s], at.parity ^ 1, dead)) {
                         alive = false;
                         break;
                     }
@@ -377,7 +380,7 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
             const T* row = logits + i * a.ld;
             const RowWords<T> w(row, a.v);
             const int n = static_cast<int>(a.v);
-            const int64_t row_seq = seq;
+            RingAt<kRing> again = at;   // the row's first chunk
             MaxSum mine{-INFINITY, 0.f};
             // A chunk of whole words takes the straight path, four words a thread (a first word that begins before the row is
             // mended by the thread that owns it); a row's last chunk takes its steps one by one.
@@ -401,9 +404,9 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
                 mine = {top, sum.x + sum.y};
             };
             const int tid = static_cast<int>(threadIdx.x);
-            for (int c = 0; c < w.chunks; ++c, ++seq) {
-                const int s = static_cast<int>(seq % kRing);
-                mbar_wait_live(&full[s], static_cast<uint32_t>(seq / kRing) & 1, dead);   // expired: go on with what is there
+            for (int c = 0; c < w.chunks; ++c, at.next()) {
+                const int s = at.stage;
+                mbar_wait_live(&full[s], at.parity, dead);   // expired: go on with what is there
                 if (whole(c)) {
                     float x[kMine][N];
 #pragma unroll
@@ -438,10 +441,10 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
             const float factor = all.s == 0.f ? 0.f : g / all.s;
             const bool any = some[r & 3] != 0;
             T* out = dlogits + i * a.ld_d;
-            for (int c = 0; c < w.chunks; ++c) {
-                const int64_t at = hold ? row_seq + c : seq++;
-                const int s = static_cast<int>(at % kRing);
-                if (!hold) mbar_wait_live(&full[s], static_cast<uint32_t>(at / kRing) & 1, dead);
+            if (!hold) again = at;
+            for (int c = 0; c < w.chunks; ++c, again.next()) {
+                const int s = again.stage;
+                if (!hold) mbar_wait_live(&full[s], again.parity, dead);
                 auto finish = [&](float (&x)[N]) {
                     exponentials(x, ref, a.c);
                     multiply(x, factor);
@@ -484,13 +487,14 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
                     if (lane == 0) mbar_arrive(&empty[s]);
                 }
             }
+            if (!hold) at = again;
             named_arrive(3 + static_cast<int>(r & 1));
         }
     }
     __syncthreads();
     if (*dead && warp == kWorkers / 32 + kTeachers && lane == 0) {
         atomicAdd(&g_timeouts, 1u);
-        for (int64_t j = seq > kRing ? seq - kRing : 0; j < seq; ++j) mbar_wait(&full[j % kRing], static_cast<uint32_t>(j / kRing) & 1);  // loads in flight
+        for (int j = 0; j < filled; ++j, at.next()) mbar_wait(&full[filled < kRing ? j : at.stage], filled < kRing ? 0 : at.parity ^ 1);  // loads in flight
     }
 }
 

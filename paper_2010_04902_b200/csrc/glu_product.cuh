@@ -146,17 +146,6 @@ template <int ACT> __device__ __forceinline__ void gate(float (&g)[8], const flo
     for (int i = 0; i < 8; ++i) g[i] = act<ACT>(g[i]) * u[i];
 }
 
-// Position in the ring: the stage and the parity of its current round.  Counted, not divided out: the threads that load and
-// issue run one instruction after another, and 64-bit remainders between
-// two MMAs cost a seventh of the rate (8192 x 4096 x 8192 forward: 825 against 725 us).
-template <int STAGES> struct RingAt {
-    int stage = 0;
-    uint32_t parity = 0;
-    __device__ __forceinline__ void next() {
-        if (++stage == STAGES) stage = 0, parity ^= 1;
-    }
-};
-
 struct ProductTile {
     int kind;          // GluKind
     int64_t index;     // in its part

@@ -148,6 +148,19 @@ __device__ __forceinline__ float warp_max(float v) {
     return m;
 }
 
+// ---- rings of stages in shared memory -------------------------------------------------------------
+
+// Position in a ring: the stage and the parity of its current round.  Counted, not divided out: the threads that load and
+// issue run one instruction after another, and 64-bit remainders between
+// two MMAs cost a seventh of the rate (8192 x 4096 x 8192 forward: 825 against 725 us).
+template <int STAGES> struct RingAt {
+    int stage = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++stage == STAGES) stage = 0, parity ^= 1;
+    }
+};
+
 // ---- loads that stay in flight -------------------------------------------------------------------
 
 // Bounds of a tensor's memory: from its first element to behind its last.
