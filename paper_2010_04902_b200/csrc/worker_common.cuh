@@ -182,7 +182,7 @@ template <typename T, int VEC> struct Raw {
             "{\n"
             ".reg .pred p;\n"
             "setp.ne.b32 p, %4, 0;\n"
-            "@p ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%5];\n"
+            "@p ld.global.v4.u32 {%0, %1, %2, %3}, [%5];\n"
             "}\n"
             : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])
             : "r"(static_cast<int>(go)), "l"(p));
@@ -193,10 +193,10 @@ template <typename T> struct Raw<T, 1> {
     uint32_t w = 0;
     __device__ __forceinline__ void fetch(const T* p, bool go) {
         if constexpr (sizeof(T) == 4) {
-            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.cs.u32 %0, [%2];\n}\n" : "+r"(w) : "r"(static_cast<int>(go)), "l"(p));
+            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.u32 %0, [%2];\n}\n" : "+r"(w) : "r"(static_cast<int>(go)), "l"(p));
         } else {
             uint16_t h = static_cast<uint16_t>(w);
-            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.cs.u16 %0, [%2];\n}\n" : "+h"(h) : "r"(static_cast<int>(go)), "l"(p));
+            asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p ld.global.u16 %0, [%2];\n}\n" : "+h"(h) : "r"(static_cast<int>(go)), "l"(p));
             w = h;
         }
     }
