@@ -459,8 +459,6 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
 #pragma unroll
                     for (int k = 0; k < kMine; ++k) word_of(s, k * kWorkers + tid, x[k]);
                     if (c == 0 && tid == 0 && w.begin) partial(0, x[0]);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&empty[s]);
                     T* to = out + (static_cast<int64_t>(c) * kChunkWords + tid) * N - w.lead;
 #pragma unroll
                     for (int k = 0; k < kMine; ++k) {
@@ -470,6 +468,10 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
                         else
                             *reinterpret_cast<uint4*>(to + k * kWorkers * N) = Word<T>::pack(x[k]);
                     }
+                    // after the stores, which need the values: the copy that refills the stage goes by another proxy, which an
+                    // arrival alone does not order behind loads still on their way
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&empty[s]);
                 } else {
 #pragma unroll 1
                     for (int in = tid; (c * kChunkWords + in - tid) * N - w.lead < n; in += kWorkers) {

@@ -81,16 +81,19 @@ int lay_out(const void* p, int64_t ld, int64_t rows, int64_t n, char*& room, Ope
     return check_launch();
 }
 
-// Tensor map of [z][rows][n] 16-bit elements, boxes of 64 x box_rows, 128-byte swizzle, zeros outside.
-template <typename T> bool make_map(CUtensorMap* map, const void* p, int64_t n, int64_t rows, int64_t ld, int box_rows, int64_t ld_z) {
+// Tensor map of [z][rows][n] 16-bit elements, boxes of box_columns x box_rows, zeros outside; 128-byte swizzle for the boxes
+// of 64 columns that the tensor cores read.
+template <typename T>
+bool make_map(CUtensorMap* map, const void* p, int64_t n, int64_t rows, int64_t ld, int box_rows, int64_t ld_z, int box_columns = 64) {
     EncodeTiledFn enc = encode_tiled();
     if (enc == nullptr) return false;
     const cuuint32_t rank = ld_z ? 3 : 2;
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(n), static_cast<cuuint64_t>(rows), 2};
     const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld_z) * 2};
-    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1}, elem[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_columns), static_cast<cuuint32_t>(box_rows), 1}, elem[3] = {1, 1, 1};
     return enc(map, __is_same(T, __half) ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(p), dims,
-               strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               box_columns == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -185,7 +188,25 @@ int zero(void* p, int64_t ld, int64_t rows, int64_t n, int bytes, cudaStream_t s
 bool pair_rows(const void* p, int64_t ld, int64_t rows, int bytes) { return reinterpret_cast<uintptr_t>(p) % (2 * bytes) == 0 && (rows <= 1 || ld % 2 == 0); }
 bool wide_rows(const void* p, int64_t ld, int64_t rows, int bytes) { return aligned16(p) && (rows <= 1 || ld * bytes % 16 == 0); }
 
+// The ring pays from nine rows on, and for eight and fewer from 16 MB of weights on (out of memory, ring against registers:
+// 24 rows, 512 x 2048 4.7 against 5.7 us; one row, 1024 x 2816 7.1 against 5.9; one row, 2048 x 5461 14.2 against 17.6;
+// one row, 4096 x 10922 42 against 53; 32 rows of that 70 against 90: there the rows' own traffic out of the L2 is the bound).
+constexpr int64_t kFewStreamRows = 9, kFewStreamBytes = int64_t(16) << 20;
+
 template <typename T, int NT> int launch_few(const FewParams& p, bool wide, cudaStream_t s) {
+    if (wide && (p.m >= kFewStreamRows || 4 * p.n * p.k >= kFewStreamBytes)) {
+        constexpr int smem = few_stream_smem<NT>();
+        const cudaError_t e = cudaFuncSetAttribute(glu_few_stream_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return cuda_failed(e);
+        CUtensorMap gate, up;
+        if (!make_map<T>(&gate, p.wg, p.k, p.n, p.n > 1 ? p.ld_w : (p.k + 7) / 8 * 8, kFewUnits, 0, kFewChunk) ||
+            !make_map<T>(&up, p.wu, p.k, p.n, p.n > 1 ? p.ld_w : (p.k + 7) / 8 * 8, kFewUnits, 0, kFewChunk))
+            return BZ_ERR_UNSUPPORTED;
+        const int64_t groups = ceil_div(p.n, kFewUnits);
+        glu_few_stream_kernel<T, NT><<<static_cast<unsigned>(std::min<int64_t>(groups, 2 * kNumSMs)), kFewStreamThreads, smem, s>>>(gate, up, p);
+        note_launch();
+        return check_launch();
+    }
     const unsigned grid = static_cast<unsigned>(ceil_div(p.n, kFewUnits));
     if (wide)
         glu_few_kernel<T, NT, true><<<grid, 32 * kFewWarps, 0, s>>>(p);

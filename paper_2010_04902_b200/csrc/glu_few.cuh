@@ -27,11 +27,11 @@ struct FewParams {
 
 template <typename T> __device__ __forceinline__ void mma_few(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     if constexpr (__is_same(T, __half))
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -52,6 +52,15 @@ __device__ __forceinline__ uint4 gather_eight(const uint16_t* p, int64_t n) {
     for (int i = 0; i < 8; ++i)
         if (i < n) w[i / 2] |= static_cast<uint32_t>(__ldg(p + i)) << (i % 2 * 16);
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ float few_gate(int which, float g) {
+    switch (which) {
+        case BZ_ACT_SILU: return act<BZ_ACT_SILU>(g);
+        case BZ_ACT_GELU_TANH: return act<BZ_ACT_GELU_TANH>(g);
+        case BZ_ACT_GELU: return act<BZ_ACT_GELU>(g);
+        default: return act<BZ_ACT_RELU>(g);
+    }
 }
 
 // NT: groups of eight tokens.
@@ -117,14 +126,142 @@ __global__ void __launch_bounds__(32 * kFewWarps) glu_few_kernel(const __grid_co
             p.preact[token * p.n + unit + u] = gate;
             p.preact[(p.m + token) * p.n + unit + u] = up;
         }
-        float a;
-        switch (p.act) {
-            case BZ_ACT_SILU: a = act<BZ_ACT_SILU>(gate); break;
-            case BZ_ACT_GELU_TANH: a = act<BZ_ACT_GELU_TANH>(gate); break;
-            case BZ_ACT_GELU: a = act<BZ_ACT_GELU>(gate); break;
-            default: a = act<BZ_ACT_RELU>(gate); break;
+        static_cast<T*>(p.h)[token * p.ld_h + unit + u] = from_f32<T>(few_gate(p.act, gate) * up);
+    }
+}
+
+// ---- many weights: the same products fed through a ring -------------------------------------------
+//
+// What the registers of the kernel above can keep in flight ends with every CTA; here two CTAs an SM go from group to
+// group of eight units while one thread brings the units' rows by TMA (boxes of eight rows x 256 elements, gate and up, a
+// stage) eight stages ahead.  Warp w multiplies elements 32w .. 32w + 31 of a stage.  Rows lie 512 bytes apart, so that the
+// two rows of a quarter warp's 16-byte read share banks; padded rows would need a copy a row, and those were slower to
+// issue than to arrive (one token, 5461 units of 2048: 18.6 us against 14.2).
+
+constexpr int kFewChunk = 32 * kFewWarps, kFewBox = kFewUnits * kFewChunk * 2, kFewStage = 2 * kFewBox, kFewStages = 8;
+constexpr int kFewStreamThreads = 32 * kFewWarps + 32;
+
+__device__ __forceinline__ void tma_load_2d(void* smem_dst, const CUtensorMap* map, uint64_t* bar, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(smem_dst)),
+                 "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y)
+                 : "memory");
+}
+
+// The warp's arrival, behind the products that used the stage.
+template <int NT> __device__ __forceinline__ void release_stage(uint64_t* empty, float (&acc)[NT][4]) {
+    asm volatile("" : "+f"(acc[0][0]), "+f"(acc[NT - 1][3])::"memory");
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(empty);
+}
+
+template <int NT> struct FewSums {
+    float v[kFewWarps][2][kFewUnits][8 * NT + 1];
+};
+template <int NT> constexpr int few_stream_smem() { return kFewStages * kFewStage + 2 * static_cast<int>(sizeof(FewSums<NT>)) + 2 * kFewStages * 8 + 16; }
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(kFewStreamThreads, 2)
+    glu_few_stream_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_constant__ CUtensorMap up_map, const __grid_constant__ FewParams p) {
+    extern __shared__ __align__(128) unsigned char ring[];
+    FewSums<NT>* sums = reinterpret_cast<FewSums<NT>*>(ring + kFewStages * kFewStage);   // two, in turn
+    uint64_t* full = reinterpret_cast<uint64_t*>(sums + 2);
+    uint64_t* empty = full + kFewStages;
+    __shared__ int dead_word;
+    volatile int* dead = &dead_word;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    if (threadIdx.x == 0) {
+        dead_word = 0;
+        for (int s = 0; s < kFewStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], kFewWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    const int64_t groups = (p.n + kFewUnits - 1) / kFewUnits;
+    const int k = static_cast<int>(p.k), chunks = (k + kFewChunk - 1) / kFewChunk;
+    RingAt<kFewStages> at;
+    int filled = 0;
+    if (warp == kFewWarps) {
+        // ---------------------------------------------------------------- loads; zeros outside the weights
+        if (lane == 0) {
+            bool alive = true;
+            for (int64_t i = blockIdx.x; i < groups && alive; i += gridDim.x)
+                for (int c = 0; c < chunks; ++c, at.next()) {
+                    if (filled < kFewStages) {
+                        ++filled;
+                    } else if (!mbar_wait_live(&empty[at.stage], at.parity ^ 1, dead)) {
+                        alive = false;
+                        break;
+                    }
+                    unsigned char* to = ring + at.stage * kFewStage;
+                    mbar_expect_tx(&full[at.stage], kFewStage);
+                    tma_load_2d(to, &gate_map, &full[at.stage], c * kFewChunk, static_cast<int>(i * kFewUnits));
+                    tma_load_2d(to + kFewBox, &up_map, &full[at.stage], c * kFewChunk, static_cast<int>(i * kFewUnits));
+                }
         }
-        static_cast<T*>(p.h)[token * p.ld_h + unit + u] = from_f32<T>(a * up);
+    } else {
+        // ---------------------------------------------------------------- products
+        const uint16_t* token[NT];
+        bool asked[NT];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            asked[c] = c * 8 + g < p.m;
+            token[c] = static_cast<const uint16_t*>(p.x) + (asked[c] ? (c * 8 + g) * p.ld_x : 0);
+        }
+        int turn = 0;
+        for (int64_t i = blockIdx.x; i < groups; i += gridDim.x, turn ^= 1) {
+            const int64_t unit = i * kFewUnits;
+            float acc[NT][4] = {};
+            uint4 x[NT];
+            int k0 = warp * 32 + t * 8;
+#pragma unroll
+            for (int c = 0; c < NT; ++c) x[c] = load_eight(token[c] + k0, asked[c] && k0 + 8 <= k);
+            for (int chunk = 0; chunk < chunks; ++chunk, at.next()) {
+                const int next = k0 + kFewChunk;
+                uint4 ahead[NT];
+#pragma unroll
+                for (int c = 0; c < NT; ++c) ahead[c] = load_eight(token[c] + next, asked[c] && next + 8 <= k);
+                if (k0 < k && k0 + 8 > k) {   // a row's last elements, fewer than eight
+                    asm volatile("");
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) x[c] = gather_eight(token[c] + k0, asked[c] ? k - k0 : 0);
+                }
+                mbar_wait_live(&full[at.stage], at.parity, dead);   // expired: go on with what is there
+                const unsigned char* from = ring + at.stage * kFewStage + g * (kFewChunk * 2) + warp * 64 + t * 16;
+                const uint4 a = *reinterpret_cast<const uint4*>(from), b = *reinterpret_cast<const uint4*>(from + kFewBox);
+#pragma unroll
+                for (int c = 0; c < NT; ++c) {
+                    mma_few<T>(acc[c], a.x, b.x, a.y, b.y, x[c].x, x[c].y);
+                    mma_few<T>(acc[c], a.z, b.z, a.w, b.w, x[c].z, x[c].w);
+                    x[c] = ahead[c];
+                }
+                // only now: the loads have ended once their values are used, and the copy that refills the stage goes by
+                // another proxy, which an arrival alone does not order behind loads still on their way
+                release_stage(&empty[at.stage], acc);
+                k0 = next;
+            }
+            FewSums<NT>& part = sums[turn];
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part.v[warp][e >> 1][g][c * 8 + 2 * t + (e & 1)] = acc[c][e];
+            // one barrier a group: the other set of sums is written before the next
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kFewWarps) : "memory");
+            const int e = threadIdx.x, u = e % kFewUnits, tk = e / kFewUnits;
+            if (tk < p.m && unit + u < p.n) {
+                float gate = part.v[0][0][u][tk], up = part.v[0][1][u][tk];
+#pragma unroll
+                for (int w = 1; w < kFewWarps; ++w) gate += part.v[w][0][u][tk], up += part.v[w][1][u][tk];
+                if (p.preact != nullptr) {
+                    p.preact[tk * p.n + unit + u] = gate;
+                    p.preact[(p.m + tk) * p.n + unit + u] = up;
+                }
+                static_cast<T*>(p.h)[tk * p.ld_h + unit + u] = from_f32<T>(few_gate(p.act, gate) * up);
+            }
+        }
+    }
+    __syncthreads();
+    if (*dead && warp == kFewWarps && lane == 0) {
+        atomicAdd(&g_glu_timeouts, 1u);
+        for (int j = 0; j < filled; ++j, at.next()) mbar_wait(&full[filled < kFewStages ? j : at.stage], filled < kFewStages ? 0 : at.parity ^ 1);  // copies in flight
     }
 }
 

@@ -188,7 +188,7 @@ def test_many_rows(dtype, v, pad, t):
         same = (d[part].float() - few_d.float()).abs() <= (2 * HALF_UNIT[dtype] + 4 * TOL) * few_d.float().abs() + 4 * TOL * dloss[part][:, None] + TINY[dtype]
         assert same.all() and torch.equal(stats[part][:, 0], few_stats[:, 0])
         assert torch.allclose(stats[part][:, 1], few_stats[:, 1], rtol=TOL)
-    for _ in range(5):
+    for _ in range(30):
         loss2, stats2, d2 = bz.distill(logits, teacher, index, 2.0, dloss=dloss, dlogits=torch.empty_like(logits) if pad == 0 else torch.empty(m, v + pad, dtype=dtype, device="cuda")[:, :v])
         assert torch.equal(loss, loss2) and torch.equal(stats, stats2) and torch.equal(d, d2)
     only, stats2 = bz.distill(logits, teacher, index, 2.0)
