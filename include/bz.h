@@ -7,7 +7,8 @@
  * file gradient (Eq. 3, Algorithm 1), the robust aggregation of the f winners (coordinate-wise
  * median in ByzShield, Sec. 2 and Sec. 6.1; Multi-Krum and Bulyan as the alternatives named in
  * Sec. 6.1 and Sec. 7), the task assignment that decides which r workers hold a file
- * (Algorithm 2, Sec. 4.2.1) and the exhaustive worst-case count c_max^(q) (Sec. 5.3.2).
+ * (Algorithm 2, Sec. 4.2.1) and the exhaustive worst-case count c_max^(q) (Sec. 5.3.2).  A last part
+ * holds operators for the workers' side of a language model's step (see "A worker's step").
  *
  * Conventions
  *   - "device" pointers are CUDA global-memory addresses of the current device; "host" pointers
