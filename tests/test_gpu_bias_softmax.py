@@ -134,7 +134,7 @@ def test_rows_that_sit_differently(dtype, pad):
 
 
 @pytest.mark.parametrize("both,buckets,distance", [(True, 4, 2), (True, 32, 128), (True, 64, 200), (False, 2, 2), (False, 3, 9), (False, 32, 128),
-                                                   (False, 16, 2048), (True, 256, 2048)])
+                                                   (True, 32, 336), (False, 32, 400), (True, 48, 512), (False, 16, 2048), (True, 256, 2048)])
 def test_bucket_rules(both, buckets, distance):
     tk = 300 if distance < 2048 else 2500
     shape = (1, 2, 6, tk)
