@@ -523,7 +523,7 @@ uint64_t bz_kernel_launch_count(void);
  *   workspace  device, bz_glu_workspace_bytes(m, n, k, dtype, 0) bytes, 256-byte aligned; the bytes are 0
  *           and NULL will do where x and the weights are 16-byte aligned with leading dimensions that are
  *           multiples of 8 (other operands are laid out there first), and up to 32 rows.
- * m, n, k up to 2^31 - 512 each.  The tensor-core kernels bound every wait; one that runs out stops the
+ * m, n, k up to 2^31 - 512 each, leading dimensions below 2^38; m * n below 2^39 in the backward call.  The tensor-core kernels bound every wait; one that runs out stops the
  * kernel early with incomplete outputs and counts in bz_pipeline_timeouts().
  */
 int bz_glu(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, int64_t ld_w, int64_t m, int64_t n, int64_t k,
@@ -557,7 +557,7 @@ size_t bz_glu_workspace_bytes(int64_t m, int64_t n, int64_t k, int dtype, int ba
  * where rel > 0; otherwise nb = buckets, n = max(-rel, 0).  Distances n < e = nb / 2 have a bucket each;
  * from there bucket e + t, t = 0 .. nb - e - 1, begins at the smallest n >= e * (max_distance / e)^(t / (nb - e)).
  *   scores, probs  device [b][h][tq][tk], unit stride along tk; strides of b, h, tq in elements in host
- *           arrays of three (any sign-free layout; probs may be scores itself).  dtype: BZ_F32, _F16, _BF16.
+ *           arrays of three (any order, none negative; probs may be scores itself).  dtype: BZ_F32, _F16, _BF16.
  *   table   device binary32 [buckets][h], contiguous;  2 <= buckets <= 256 (4 <= buckets, even, when
  *           bidirectional), nb / 2 < max_distance <= BZ_MAX_DISTANCE.
  *   k_len   device int32 [b], values taken into [0, tk], or NULL: all tk.

@@ -585,7 +585,7 @@ int check_form(int dtype, int64_t b, int64_t h, int64_t tq, int64_t tk, const fl
 
 int check_tensor(const void* p, const int64_t* strides, int dtype) {
     if (p == nullptr || strides == nullptr || reinterpret_cast<uintptr_t>(p) % element_bytes(dtype)) return BZ_ERR_INVALID_ARG;
-    return BZ_OK;
+    return strides[0] < 0 || strides[1] < 0 || strides[2] < 0 ? BZ_ERR_INVALID_ARG : BZ_OK;
 }
 
 // Whether two tensors' rows all sit alike relative to 16-byte boundaries.

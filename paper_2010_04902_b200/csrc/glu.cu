@@ -372,6 +372,7 @@ extern "C" int bz_glu_backward(const void* x, int64_t ld_x, const void* w_gate, 
     const int st = check(x, ld_x, w_gate, w_up, ld_w, m, n, k, dtype, act);
     if (st != BZ_OK) return st;
     if ((grad_dtype != dtype && grad_dtype != BZ_F32) || (dw_gate == nullptr) != (dw_up == nullptr)) return BZ_ERR_INVALID_ARG;
+    if (m > 0 && static_cast<int64_t>(round_up(n, 8)) >= (int64_t(1) << 39) / m) return BZ_ERR_UNSUPPORTED;  // a tensor map's stride from dg to du
     if (k == 0 || (m == 0 && n == 0)) return BZ_OK;
     const uintptr_t grads = reinterpret_cast<uintptr_t>(dw_gate) | reinterpret_cast<uintptr_t>(dw_up);
     if (dx == nullptr && dw_gate == nullptr) return BZ_ERR_INVALID_ARG;

@@ -84,17 +84,17 @@ __device__ __forceinline__ void turn_out(const float* turn, E* out, int64_t ld, 
     const int n_rows = static_cast<int>(min(int64_t(32), rows - r0)), n = static_cast<int>(min(int64_t(kEach), cols - c0));
     if (n_rows <= 0 || n <= 0) return;
     E* base = out + r0 * ld + c0;
-    if (wide && n == kEach) {
+    if (wide && n % (16 / static_cast<int>(sizeof(E))) == 0) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = i * 4 + lane / 8, w = lane % 8 * 4;
-            if (r < n_rows) *reinterpret_cast<uint4*>(base + r * ld + w * kPer) = *reinterpret_cast<const uint4*>(turn + turned(r, w));
+            if (r < n_rows && w * kPer < n) *reinterpret_cast<uint4*>(base + r * ld + w * kPer) = *reinterpret_cast<const uint4*>(turn + turned(r, w));
         }
-    } else if (kPer == 1 && pairs && n == kEach) {
+    } else if (kPer == 1 && pairs && n % 2 == 0) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int r = i * 2 + lane / 16, w = lane % 16 * 2;
-            if (r < n_rows) *reinterpret_cast<float2*>(base + r * ld + w) = *reinterpret_cast<const float2*>(turn + turned(r, w));
+            if (r < n_rows && w < n) *reinterpret_cast<float2*>(base + r * ld + w) = *reinterpret_cast<const float2*>(turn + turned(r, w));
         }
     } else if (kPer == 1 || (pairs && n % 2 == 0)) {
         if (lane * kPer < n) {

@@ -49,6 +49,7 @@ def test_glu_backward(L):
                 dict(grad=bz.F32, dwg=ctypes.c_void_p(258))):
         assert call(**bad) == bz.ERR_INVALID_ARG, bad
     assert call(dtype=bz.F32, grad=bz.F32) == bz.ERR_UNSUPPORTED and call(m=BIG) == bz.ERR_UNSUPPORTED
+    assert call(m=1 << 30, n=1 << 30, ld_dh=1 << 30) == bz.ERR_UNSUPPORTED
     need = L.bz_glu_workspace_bytes(4, 6, 8, bz.F16, 1)
     for ws, size in ((None, BIG), (F, need - 1), (ctypes.c_void_p(264), BIG)):
         assert call(ws=ws, size=size) == bz.ERR_WORKSPACE
@@ -76,6 +77,8 @@ def test_bias_softmax(L):
     for bad in (dict(probs=None, stats=None), dict(sp=None, dprobs=None), dict(probs=ODD, sd=None), dict(probs=None, ds=None, dt=None),
                 dict(probs=None, so=None), dict(probs=None, ds=ODD)):
         assert both(**bad) == (bz.ERR_INVALID_ARG, bz.ERR_INVALID_ARG), bad
+    back = (ctypes.c_int64 * 3)(80, -40, 10)
+    assert both(ss=back) == (bz.ERR_INVALID_ARG, bz.ERR_INVALID_ARG) and both(sp=back, sd=back) == (bz.ERR_INVALID_ARG, bz.ERR_INVALID_ARG)
     for bad in (dict(ws=None), dict(ws=ctypes.c_void_p(264)), dict(size=8)):
         assert both(probs=None, **bad)[1] == bz.ERR_WORKSPACE
     for none in (dict(b=0), dict(h=0), dict(tq=0), dict(tk=0)):
