@@ -711,8 +711,10 @@ def glu(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "s
     elif m > GLU_FEW and ((ld_x | ld_w) & 7 or (px | pg | pu) & 15):
         workspace = torch.empty(max(256, lib().bz_glu_workspace_bytes(m, n, k, dt, 0)), dtype=torch.uint8, device=x.device)
         ws, ws_bytes = workspace.data_ptr(), workspace.numel()
-    st = lib().bz_glu(px, ld_x, pg, pu, ld_w, m, n, k, dt, _act(act), ph, ld_h, _packed(preact, (2, m, n), torch.float32, "preact"), ws, ws_bytes, _stream())
-    _check(st, "bz_glu")
+    st = lib().bz_glu(px, ld_x, pg, pu, ld_w, m, n, k, dt, _act(act), ph, ld_h, _packed(preact, (2, m, n), torch.float32, "preact"),
+                      ws, ws_bytes, _stream())
+    if st:
+        _check(st, "bz_glu")
     return h
 
 
@@ -724,23 +726,29 @@ def glu_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, prea
     m, n, k, ld_x, ld_w = _glu_operands(x, w_gate, w_up)
     dt = _dtype(x, "x")
     if dx is None:
-        dx = x.new_empty((m, k))
+        dx, ld_dx = x.new_empty((m, k)), k
+        p_dx = dx.data_ptr()
+    else:
+        p_dx, ld_dx = _shaped(dx, (m, k), x.dtype, "dx"), _matrix(dx, "dx")[2]
     if (dw_gate is None) != (dw_up is None):
         raise ValueError("give both dw_gate and dw_up, or neither")
     if dw_gate is None:
-        dw_gate, dw_up = x.new_empty((n, k)), x.new_empty((n, k))
-    px, pg, pu = _dev(x, x.dtype, "x"), _dev(w_gate, x.dtype, "w_gate"), _dev(w_up, x.dtype, "w_up")
-    pdg, pdu = _shaped(dw_gate, (n, k), dw_gate.dtype, "dw_gate"), _shaped(dw_up, (n, k), dw_gate.dtype, "dw_up")
-    ld_dw = _matrix(dw_gate, "dw_gate")[2]
-    if _matrix(dw_up, "dw_up")[2] != ld_dw:
-        raise ValueError("dw_gate and dw_up must have the same leading dimension")
+        whole = w_gate.is_contiguous()
+        dw_gate, dw_up = (torch.empty_like(w_gate), torch.empty_like(w_gate)) if whole else (x.new_empty((n, k)), x.new_empty((n, k)))
+        p_dg, p_du, ld_dw, grad = dw_gate.data_ptr(), dw_up.data_ptr(), k, dt
+    else:
+        p_dg, p_du = _shaped(dw_gate, (n, k), dw_gate.dtype, "dw_gate"), _shaped(dw_up, (n, k), dw_gate.dtype, "dw_up")
+        ld_dw, grad = _matrix(dw_gate, "dw_gate")[2], _dtype(dw_gate, "dw_gate")
+        if _matrix(dw_up, "dw_up")[2] != ld_dw:
+            raise ValueError("dw_gate and dw_up must have the same leading dimension")
     if workspace is None:
         workspace = torch.empty(lib().bz_glu_workspace_bytes(m, n, k, dt, 1), dtype=torch.uint8, device=x.device)
-    st = lib().bz_glu_backward(px, ld_x, pg, pu, ld_w, _packed(preact, (2, m, n), torch.float32, "preact"),
-                               _shaped(dh, (m, n), x.dtype, "dh"), _matrix(dh, "dh")[2], m, n, k, dt, _act(act),
-                               _shaped(dx, (m, k), x.dtype, "dx"), _matrix(dx, "dx")[2], pdg, pdu, ld_dw, _dtype(dw_gate, "dw_gate"),
+    st = lib().bz_glu_backward(_dev(x, x.dtype, "x"), ld_x, _dev(w_gate, x.dtype, "w_gate"), _dev(w_up, x.dtype, "w_up"), ld_w,
+                               _packed(preact, (2, m, n), torch.float32, "preact"), _shaped(dh, (m, n), x.dtype, "dh"),
+                               _matrix(dh, "dh")[2], m, n, k, dt, _act(act), p_dx, ld_dx, p_dg, p_du, ld_dw, grad,
                                workspace.data_ptr(), workspace.numel(), _stream())
-    _check(st, "bz_glu_backward")
+    if st:
+        _check(st, "bz_glu_backward")
     return dx, dw_gate, dw_up
 
 
