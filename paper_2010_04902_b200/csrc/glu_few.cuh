@@ -149,13 +149,6 @@ __device__ __forceinline__ void tma_load_2d(void* smem_dst, const CUtensorMap* m
                  : "memory");
 }
 
-// The warp's arrival, behind the products that used the stage.
-template <int NT> __device__ __forceinline__ void release_stage(uint64_t* empty, float (&acc)[NT][4]) {
-    asm volatile("" : "+f"(acc[0][0]), "+f"(acc[NT - 1][3])::"memory");
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) mbar_arrive(empty);
-}
-
 template <int NT> struct FewSums {
     float v[kFewWarps][2][kFewUnits][8 * NT + 1];
 };
@@ -235,9 +228,7 @@ __global__ void __launch_bounds__(kFewStreamThreads, 2)
                     mma_few<T>(acc[c], a.z, b.z, a.w, b.w, x[c].z, x[c].w);
                     x[c] = ahead[c];
                 }
-                // only now: the loads have ended once their values are used, and the copy that refills the stage goes by
-                // another proxy, which an arrival alone does not order behind loads still on their way
-                release_stage(&empty[at.stage], acc);
+                release_stage(&empty[at.stage]);
                 k0 = next;
             }
             FewSums<NT>& part = sums[turn];

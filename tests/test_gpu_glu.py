@@ -247,3 +247,23 @@ def test_only_what_is_asked_for():
     assert bz.lib().bz_glu_backward(*head, None, 0, dg2.data_ptr(), du2.data_ptr(), 56, *tail) == bz.OK
     torch.cuda.synchronize()
     assert torch.equal(dx, dx2) and torch.equal(dg, dg2) and torch.equal(du, du2)
+
+
+def test_stages_of_the_ring_are_not_refilled_under_their_readers():
+    """Weights that are one number for each group of eight units (gate +, up -, exact in every sum) and tokens that mark parts
+    of the contraction: a product that took a later group's weights shows in whichever call it happens (one in a million
+    before the readers fenced, at these sizes)."""
+    n, k = 5461, 2048
+    group = torch.arange(n, device="cuda") // 8
+    code = (128 + group % 128).float() * 2.0 ** (group // 128).float()
+    wg = code[:, None].expand(n, k).to(torch.bfloat16).contiguous()
+    wu = -wg
+    at = torch.arange(k, device="cuda")
+    x = torch.stack([at // 256 == i for i in range(8)] + [at % 256 // 32 == i for i in range(8)] + [at % 8 == i for i in range(8)]).to(torch.bfloat16)
+    want = torch.stack([x.float().sum(1)[:, None] * code, -x.float().sum(1)[:, None] * code])
+    preact, h = torch.empty(2, 24, n, device="cuda"), torch.empty(24, n, dtype=torch.bfloat16, device="cuda")
+    differs = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(20000):
+        bz.glu(x, wg, wu, h=h, preact=preact)
+        differs += (preact != want).any()
+    assert int(differs) == 0
