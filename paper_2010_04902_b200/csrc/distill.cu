@@ -427,10 +427,7 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
                         absorb(x);
                     }
                 }
-                if (!(grad && hold)) {
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&empty[s]);
-                }
+                if (!(grad && hold)) release_stage(&empty[s]);
             }
             mine = warp_join(mine, a.c);
             if (lane == 0) part[r & 3][warp] = mine;
@@ -469,10 +466,6 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
                         else
                             *reinterpret_cast<uint4*>(to + k * kWorkers * N) = Word<T>::pack(x[k]);
                     }
-                    // after the stores, which need the values: the copy that refills the stage goes by another proxy, which an
-                    // arrival alone does not order behind loads still on their way
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&empty[s]);
                 } else {
 #pragma unroll 1
                     for (int in = tid; (c * kChunkWords + in - tid) * N - w.lead < n; in += kWorkers) {
@@ -486,9 +479,8 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamCtas) distill_stream_ke
                         finish(x);
                         if (word * N - w.lead < n) store_slot<T, N>(out, word * N - w.lead, n, x);
                     }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&empty[s]);
                 }
+                release_stage(&empty[s]);
             }
             if (!hold) at = again;
             named_arrive(3 + static_cast<int>(r & 1));

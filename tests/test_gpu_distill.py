@@ -209,3 +209,16 @@ def test_no_vocabulary_and_no_positions():
     assert (loss == 0).all() and (stats[:, 0] == -math.inf).all() and (stats[:, 1] == 0).all()
     loss, _ = bz.distill(torch.empty(0, 9, device="cuda"), torch.zeros(0, 2, device="cuda"), torch.zeros(0, 2, dtype=torch.int32, device="cuda"))
     assert loss.numel() == 0
+
+
+@pytest.mark.parametrize("dtype,v,grad", [(torch.float16, 50003, False), (torch.bfloat16, 32128, False), (torch.bfloat16, 40000, True), (torch.float32, 9001, True)])
+def test_ring_gives_the_same_bits_over_many_calls(dtype, v, grad):
+    """Rows enough to go round the ring several times a CTA, read once and read twice."""
+    logits, teacher, index, dloss = make(900, v, 16, dtype, seed=v)
+    how = {"dloss": dloss, "dlogits": torch.empty_like(logits)} if grad else {}
+    loss, stats = (t.clone() for t in bz.distill(logits, teacher, index, 2.0, **how)[:2])
+    differs = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(500):
+        again = bz.distill(logits, teacher, index, 2.0, **how)
+        differs += (again[0] != loss).any() | (again[1] != stats).any()
+    assert int(differs) == 0

@@ -19,7 +19,7 @@ def test_the_release_fences_first():
     assert steps == sorted(steps)
 
 
-@pytest.mark.parametrize("name", ["glu_few.cuh"])
+@pytest.mark.parametrize("name", ["glu_few.cuh", "distill.cu"])
 def test_readers_release_through_it(name):
     code = _code(name)
     assert "mbar_arrive(&empty" not in code and "release_stage(&empty" in code
