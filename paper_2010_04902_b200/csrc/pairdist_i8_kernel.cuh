@@ -479,12 +479,10 @@ __global__ void __launch_bounds__(I8Shape<F, W, R, FC, NS, TS>::kThreads, 1)
                                 val[sub][i] = make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
                             }
                         }
-                        // The box is in registers: hand it back.  The arrival is a release (the loads above are
-                        // ordered before the producer's next write into the box), so it comes BEFORE this tile's
-                        // global stores: a release waits for the stores its thread has in flight, and stores
+                        // The box is in registers: hand it back.  The arrival is a release, so it comes BEFORE this
+                        // tile's global stores: a release waits for the stores its thread has in flight, and stores
                         // issued after it have the whole conversion to drain before the step's next arrival.
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&in_empty[s]);
+                        release_stage(&in_empty[s]);
                         if constexpr (R > 1) {
 #pragma unroll
                             for (int i = 0; i < RWC; ++i) {

@@ -119,8 +119,7 @@ __global__ void __launch_bounds__(kRingConsumers + 32)
                 acc.z ^= x.z;
                 acc.w ^= x.w;
             }
-            __syncwarp();
-            if ((tid & 31) == 0) mbar_arrive(&empty[s]);
+            release_stage(&empty[s]);
         }
         if (!alive && (tid & 31) == 0) atomicAdd(&g_probe_timeouts, 1u);
         unsigned long long w = (static_cast<unsigned long long>(acc.y ^ acc.w) << 32) | (acc.x ^ acc.z);

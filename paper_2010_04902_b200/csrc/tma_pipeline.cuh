@@ -41,6 +41,19 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
     return false;
 }
 
+// Orders this thread's ordinary accesses to shared memory before accesses by the asynchronous proxy (bulk copies, the
+// tensor core's reads) that follow.
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// The warp's arrival for a stage that it has read with ordinary loads and that a bulk copy will refill.  The copy writes by
+// the asynchronous proxy, and an arrival alone does not hold it back behind loads that are still on their way: shared loads
+// queue behind misses of global ones, and one call of a million (24 rows of 2048, 5461 units) multiplied pieces of a
+// later group's weights.  So each lane fences first; times are the same (20 us from memory).
+__device__ __forceinline__ void release_stage(uint64_t* empty) {
+    fence_async_smem();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(empty);
+}
+
 __device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"

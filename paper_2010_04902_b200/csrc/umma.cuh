@@ -18,8 +18,6 @@ __device__ __forceinline__ void tmem_dealloc(uint32_t base, uint32_t n_cols) {
 }
 __device__ __forceinline__ void tc_fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// Writes made with ordinary stores become visible to the tensor core's reads of shared memory.
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // ---- descriptors ---------------------------------------------------------------------------------
 // Operand tile in shared memory, K-major, 128-byte swizzle: rows of 128 bytes, groups of 8 rows

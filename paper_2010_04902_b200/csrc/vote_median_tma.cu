@@ -129,8 +129,8 @@ __global__ void __launch_bounds__(kThreads)
                         }
                     }
                 }
-                __syncwarp();
                 if constexpr (VOTE_ONLY) {
+                    __syncwarp();
                     if (wide_out) {
                         // the warp's 32 columns of the FC winner rows leave as 128-bit stores: lane -> (row, four columns)
                         const int warp = tid >> 5, lane = tid & 31;
@@ -143,13 +143,9 @@ __global__ void __launch_bounds__(kThreads)
                                 __stcs(reinterpret_cast<float4*>(out + (chunk * FC + row) * ld_out + j4 + c4), w);
                             }
                         }
-                        // this thread wrote the stage through the generic proxy; the bulk copy that refills it
-                        // writes through the asynchronous one
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
                     }
                 }
-                if ((tid & 31) == 0) mbar_arrive(&empty[s]);  // this warp is done reading the stage
+                release_stage(&empty[s]);
             }
             if constexpr (!VOTE_ONLY) {
                 if (alive && j < d) {

@@ -172,8 +172,7 @@ __global__ void __launch_bounds__(Fused<R, F, T, G, FC, STAGES>::kThreads, Fused
                     }
                 }
             }
-            __syncwarp();
-            if ((tid & 31) == 0) mbar_arrive(&empty[s]);  // this warp is done with the box (or has given up on it)
+            release_stage(&empty[s]);  // this warp is done with the box (or has given up on it)
         }
         if (compute_any<NTP>(failed)) {  // also publishes the tile to every warp
             failed = true;

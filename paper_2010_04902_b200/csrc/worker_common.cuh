@@ -4,7 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "umma.cuh"
+#include "bz_common.cuh"
 
 namespace bz {
 
@@ -160,16 +160,6 @@ template <int STAGES> struct RingAt {
         if (++stage == STAGES) stage = 0, parity ^= 1;
     }
 };
-
-// The warp's arrival for a stage that it has read with ordinary loads and that a bulk copy will refill.  The copy writes by
-// the asynchronous proxy, and an arrival alone does not hold it back behind loads that are still on their way: shared loads
-// queue behind misses of global ones, and one call of a million (24 rows of 2048, 5461 units) multiplied pieces of a
-// later group's weights.  So each lane fences first; times are the same (20 us from memory).
-__device__ __forceinline__ void release_stage(uint64_t* empty) {
-    fence_async_smem();
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) mbar_arrive(empty);
-}
 
 // ---- loads that stay in flight -------------------------------------------------------------------
 
