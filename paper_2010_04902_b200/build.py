@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libbz.so")
 
 
 def _headers():
-    return (sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + sorted(glob.glob(os.path.join(CSRC, "*.inc")))
+    return (sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + sorted(glob.glob(os.path.join(CSRC, "*.inc"))) + sorted(glob.glob(os.path.join(CSRC, "*.h")))
             + [os.path.join(ROOT, "include", "bz.h")])
 
 

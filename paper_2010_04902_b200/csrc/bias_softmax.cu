@@ -14,6 +14,7 @@
 // of diagonals: a row meets each diagonal once, so its lanes add without conflict, row after row, in a fixed order;
 // the far sums stay in registers.  CTAs leave one value a bucket and a last kernel adds those in order.  Three transfers an
 // element; 176 us at 8 x 16 x 1024 x 1024 (70 % of the copy's rate): 22 instructions an element are what is left to cut.
+#include "bucket_rule.h"
 #include "worker_common.cuh"
 
 namespace bz {
@@ -544,16 +545,6 @@ __global__ void __launch_bounds__(256) bias_table_kernel(const float* __restrict
 
 // ---- host side ----------------------------------------------------------------------------------
 
-// Boundaries of the logarithmic buckets: the smallest n >= e*(d/e)^(t/steps); a bound that is a whole number counts as
-// reached (it differs from the rounded products by far less than one part in 10^9).
-void fill_starts(BiasForm& f) {
-    const int steps = f.nb - f.exact;
-    const double ratio = pow(static_cast<double>(f.distance) / f.exact, 1.0 / steps);
-    double x = f.exact;
-    f.starts[0] = static_cast<uint16_t>(f.exact);
-    for (int t = 1; t < steps; ++t) f.starts[t] = static_cast<uint16_t>(ceil((x *= ratio) * (1.0 - 1e-9)));
-}
-
 // Query rows a CTA takes.  Building the window (and leaving the buckets) costs a CTA what some rows do, so it takes up to
 // `most` of them; `resident` CTAs run at a time, and of the counts that fill whole rounds of those the smallest one is taken
 // (a part-filled last round leaves the GPU idle).  Small problems spread over one round.
@@ -603,7 +594,7 @@ BiasForm make_form(int64_t h, int64_t tq, int64_t tk, const float* table, int bu
     f.table = table, f.k_len = k_len, f.q_start = q_start, f.scale = scale;
     f.buckets = buckets, f.nb = bidirectional ? buckets / 2 : buckets, f.exact = f.nb / 2, f.distance = max_distance;
     f.bidirectional = bidirectional != 0, f.causal = causal != 0, f.h = static_cast<int>(h), f.tq = tq, f.tk = tk;
-    fill_starts(f);
+    bucket_starts(f.nb, f.distance, f.starts);
     return f;
 }
 

@@ -268,3 +268,13 @@ def test_only_what_is_asked_for():
     assert bz.lib().bz_bias_softmax_backward(*common, None, None, dt2.data_ptr(), ws.data_ptr(), ws.numel(), None) == bz.OK
     torch.cuda.synchronize()
     assert torch.equal(ds, ds2) and torch.equal(dt, dt2)
+
+
+@pytest.mark.parametrize("both,buckets,distance,at", [(False, 73, 905, 347), (False, 109, 1549, 183), (True, 218, 1549, 183), (False, 187, 1839, 96), (False, 226, 188, 157)])
+def test_distances_next_to_a_bound_just_above_them(both, buckets, distance, at):
+    """The bound of a bucket lies a billionth above the distance `at`, which still belongs to the bucket before."""
+    shape = (1, 2, 3, 9)
+    scores = make(*shape, torch.float32, seed=at)
+    table = torch.randn(buckets, 2, generator=torch.Generator().manual_seed(at)).cuda()
+    check_forward(scores, table, distance, both, q_start=[at + 1])
+    check_backward(scores, table, distance, both, q_start=[at + 1], dprobs=make(*shape, torch.float32, seed=1 + at, sigma=1.0))
