@@ -598,10 +598,22 @@ BiasForm make_form(int64_t h, int64_t tq, int64_t tk, const float* table, int bu
     return f;
 }
 
-template <typename K> int allow_smem(K kern, size_t bytes) {
+// The limit belongs to the kernel and not to the call, so every call sets the same one, the most that the kernel can need:
+// a smaller one would make another thread's launch fail.
+template <typename K> int allow_smem(K kern, size_t bytes, size_t most) {
     if (bytes <= 48 * 1024) return BZ_OK;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
     return e == cudaSuccess ? BZ_OK : cuda_failed(e);
+}
+
+// The wide kernels keep eight (or four) copies of the window in shared memory, the backward ones a set for each warp too, so
+// there is a distance beyond which one element at a time is faster.  4 x 8 x 1024 x 1024 bfloat16, wide against narrow:
+// forward 40 against 86 us at distance 512; backward 87 against 145 at 300, 156 against 152 at 400 (one CTA an SM from 337 on).
+constexpr int kWideForward = 512, kWideBackward = 336;
+
+template <int VEC> size_t backward_smem(int distance, int warps, bool table) {
+    const Window<VEC> w(distance);
+    return (w.floats() * (1 + (table ? warps : 0)) + w.values()) * sizeof(float);
 }
 
 template <typename T> Rows4<T> rows4(T* p, const int64_t* s, int64_t b, const BiasForm& f) {
@@ -652,17 +664,17 @@ template <typename T, int VEC, int G, int SLOTS>
 int launch_backward(BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& in, const Rows4<const T>& up, const Rows4<T>& out, const MaxSum* stats,
                     float* partial, cudaStream_t s) {
     f.rows_per_cta = rows_for(b * f.h, f.tq, 512 / Cta<G>::kThreads * kNumSMs, Cta<G>::kRows, kBackwardMost);
-    const Window<VEC> w(f.distance);
-    const size_t smem = (w.floats() * (1 + (partial != nullptr ? Cta<G>::kThreads / 32 : 0)) + w.values()) * sizeof(float);
+    const int warps = Cta<G>::kThreads / 32;
+    const size_t smem = backward_smem<VEC>(f.distance, warps, partial != nullptr), most = backward_smem<VEC>(VEC > 1 ? kWideBackward : BZ_MAX_DISTANCE, warps, true);
     const dim3 grid(static_cast<unsigned>((f.tq + f.rows_per_cta - 1) / f.rows_per_cta), f.h, static_cast<unsigned>(b));
     int st;
     if constexpr (SLOTS == 0) {
-        if ((st = allow_smem(bias_softmax_backward_long_kernel<T, VEC>, smem)) != BZ_OK) return st;
+        if ((st = allow_smem(bias_softmax_backward_long_kernel<T, VEC>, smem, most)) != BZ_OK) return st;
         bias_softmax_backward_long_kernel<T, VEC><<<grid, 256, smem, s>>>(f, in, up, out, stats, partial);
     } else {
         auto kern = VEC > 1 && whole_rows<T, VEC, G, SLOTS>(f, n) ? bias_softmax_backward_kernel<T, VEC, G, SLOTS, (VEC > 1)>
                                                                   : bias_softmax_backward_kernel<T, VEC, G, SLOTS, false>;
-        if ((st = allow_smem(kern, smem)) != BZ_OK) return st;
+        if ((st = allow_smem(kern, smem, most)) != BZ_OK) return st;
         kern<<<grid, Cta<G>::kThreads, smem, s>>>(f, in, up, out, stats, partial);
     }
     note_launch();
@@ -680,11 +692,6 @@ int dispatch_backward(BiasForm& f, int64_t n, int64_t b, const Rows4<const T>& i
     if (n <= kMost * 256) return launch_backward<T, VEC, 256, kFull>(f, n, b, in, up, out, stats, partial, s);
     return launch_backward<T, VEC, 256, 0>(f, n, b, in, up, out, stats, partial, s);
 }
-
-// The wide kernels keep eight (or four) copies of the window in shared memory, the backward ones a set for each warp too, so
-// there is a distance beyond which one element at a time is faster.  4 x 8 x 1024 x 1024 bfloat16, wide against narrow:
-// forward 40 against 86 us at distance 512; backward 87 against 145 at 300, 156 against 152 at 400 (one CTA an SM from 337 on).
-constexpr int kWideForward = 512, kWideBackward = 336;
 
 // Elements a row takes up from its first slot on: none before it if every row begins on a 16-byte boundary.
 int64_t row_span(const void* p, const int64_t* strides, int64_t b, int64_t h, int64_t tq, int64_t tk, int bytes) {

@@ -585,9 +585,11 @@ template <typename T, int VEC> int launch(const DistillArgs& a, int64_t m, const
 constexpr int64_t kStreamRows = kNumSMs, kStreamBytes = 16384;
 
 template <typename T> int stream(const DistillArgs& a, int64_t m, const T* logits, T* dlogits, cudaStream_t s) {
-    const int smem = kRing * kChunkBytes + 2 * kRing * 8 + 4 * 32 * static_cast<int>(sizeof(MaxSum)) + kTeachers * 16 * a.t;
+    constexpr int kRingSmem = kRing * kChunkBytes + 2 * kRing * 8 + 4 * 32 * static_cast<int>(sizeof(MaxSum)), kEach = kTeachers * 16;
+    const int smem = kRingSmem + kEach * a.t;
     auto kern = distill_stream_kernel<T>;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    // the limit belongs to the kernel and not to the call: the same one each time, or another thread's launch could fail
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingSmem + kEach * BZ_MAX_TOP);
     if (e != cudaSuccess) return cuda_failed(e);
     const int hold = a.v + 2 * (Word<T>::kN - 1) <= static_cast<int64_t>(kHoldChunks) * kChunkWords * Word<T>::kN;
     kern<<<static_cast<unsigned>(m < kStreamCtas * kNumSMs ? m : kStreamCtas * kNumSMs), kStreamThreads, smem, s>>>(a, m, logits, dlogits, hold);
