@@ -67,7 +67,20 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+// The encoder needs the device's context to be current, which it is not yet in a thread that has made no call of the
+// runtime; choosing the device that is chosen already makes it so.
+inline void bind_context() {
+    static thread_local bool bound = false;
+    int device;
+    if (bound) return;
+    if (cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess)
+        bound = true;
+    else
+        (void)cudaGetLastError();
+}
+
 inline EncodeTiledFn encode_tiled() {
+    bind_context();
     static EncodeTiledFn fn = nullptr;
     static bool tried = false;
     if (!tried) {

@@ -36,6 +36,11 @@ extern "C" int bias_twice(const Bias* p, int n, int64_t heads, int64_t tq, int64
                                         c.dprobs, strides, c.dscores, strides, c.dtable, c.ws, c.bytes, c.stream);
     });
 }
+extern "C" int glu_in_a_new_thread(const void* x, const void* w, void* h) {
+    int st = 1;
+    std::thread([&] { st = bz_glu(x, 64, w, w, 64, 64, 32, 64, BZ_BF16, BZ_ACT_SILU, h, 32, nullptr, nullptr, 0, nullptr); }).join();
+    return st;
+}
 extern "C" int distill_twice(const Distill* p, int n, int64_t m, int64_t v) {
     return both(n, [&](int k) {
         const Distill& c = p[k];
@@ -103,3 +108,13 @@ def test_teachers_of_different_size(threads):
     torch.cuda.synchronize()
     for (_, _, _, loss, stats, _), (loss0, stats0) in zip(held, want):
         assert torch.equal(loss, loss0) and torch.equal(stats, stats0)
+
+
+def test_first_call_of_a_thread(threads):
+    """Nothing has made the device's context current in a new thread before the call."""
+    x, w = torch.randn(64, 64, device="cuda").to(torch.bfloat16), torch.randn(32, 64, device="cuda").to(torch.bfloat16)
+    want, h = bz.glu(x, w, w), torch.zeros(64, 32, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    assert threads.glu_in_a_new_thread(P(x.data_ptr()), P(w.data_ptr()), P(h.data_ptr())) == bz.OK
+    torch.cuda.synchronize()
+    assert torch.equal(h, want)
