@@ -3,6 +3,7 @@ other one asked for.  The threads are native, so that nothing makes them take tu
 import ctypes
 import os
 import subprocess
+import sys
 
 import pytest
 import torch
@@ -36,6 +37,9 @@ extern "C" int bias_twice(const Bias* p, int n, int64_t heads, int64_t tq, int64
                                         c.dprobs, strides, c.dscores, strides, c.dtable, c.ws, c.bytes, c.stream);
     });
 }
+extern "C" int glu_twice(const void* x, const void* w, void* h0, void* h1) {
+    return both(1, [&](int k) { return bz_glu(x, 64, w, w, 64, 64, 32, 64, BZ_BF16, BZ_ACT_SILU, k ? h1 : h0, 32, nullptr, nullptr, 0, nullptr); });
+}
 extern "C" int glu_in_a_new_thread(const void* x, const void* w, void* h) {
     int st = 1;
     std::thread([&] { st = bz_glu(x, 64, w, w, 64, 64, 32, 64, BZ_BF16, BZ_ACT_SILU, h, 32, nullptr, nullptr, 0, nullptr); }).join();
@@ -47,6 +51,19 @@ extern "C" int distill_twice(const Distill* p, int n, int64_t m, int64_t v) {
         return bz_distill(c.logits, v, BZ_BF16, m, v, c.teacher, c.index, c.t, 1.f, nullptr, c.loss, c.stats, nullptr, 0, c.stream);
     });
 }
+"""
+FIRST = r"""
+import ctypes, sys
+import torch
+from paper_2010_04902_b200 import binding as bz
+bz.lib()
+x, w = torch.ones(64, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(32, 64, dtype=torch.bfloat16, device="cuda")
+h = torch.zeros(2, 64, 32, dtype=torch.bfloat16, device="cuda")
+torch.cuda.synchronize()
+P = ctypes.c_void_p
+failed = ctypes.CDLL(sys.argv[1]).glu_twice(P(x.data_ptr()), P(w.data_ptr()), P(h[0].data_ptr()), P(h[1].data_ptr()))
+torch.cuda.synchronize()
+print("failed", failed, "same", torch.equal(h[0], h[1]))
 """
 P, I, SZ = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
 
@@ -118,3 +135,11 @@ def test_first_call_of_a_thread(threads):
     assert threads.glu_in_a_new_thread(P(x.data_ptr()), P(w.data_ptr()), P(h.data_ptr())) == bz.OK
     torch.cuda.synchronize()
     assert torch.equal(h, want)
+
+
+def test_first_calls_of_a_process(threads):
+    """Both threads need the driver's tensor-map encoder, which nobody has looked up yet."""
+    for _ in range(5):
+        r = subprocess.run([sys.executable, "-c", FIRST, threads._name], cwd=ROOT, capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stderr[-2000:]
+        assert r.stdout.strip() == "failed 0 same True"
