@@ -126,7 +126,8 @@ template <int ACT> __device__ __forceinline__ float act(float g) {
     if constexpr (ACT == BZ_ACT_SILU) return g * logistic(g);
     // (1 + tanh y)/2 = 1/(1 + exp(-2y))
     if constexpr (ACT == BZ_ACT_GELU_TANH) return g * logistic(1.5957691216f * (g + 0.044715f * g * g * g));
-    if constexpr (ACT == BZ_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678f));
+    // 1 + erf y = erfc(-y): the sum would lose every digit from g = -5.6 down, where bfloat16 still holds the product
+    if constexpr (ACT == BZ_ACT_GELU) return 0.5f * g * erfcf(g * -0.70710678f);
     return g > 0.f ? g : (g == g ? 0.f : g);
 }
 template <int ACT> __device__ __forceinline__ float act_slope(float g) {
@@ -138,7 +139,7 @@ template <int ACT> __device__ __forceinline__ float act_slope(float g) {
         const float s = logistic(1.5957691216f * (g + 0.044715f * g * g * g));
         return s + g * s * (1.f - s) * 1.5957691216f * (1.f + 0.134145f * g * g);
     }
-    if constexpr (ACT == BZ_ACT_GELU) return 0.5f * (1.f + erff(g * 0.70710678f)) + g * 0.39894228f * __expf(-0.5f * g * g);
+    if constexpr (ACT == BZ_ACT_GELU) return 0.5f * erfcf(g * -0.70710678f) + g * 0.39894228f * __expf(-0.5f * g * g);
     return g > 0.f ? 1.f : 0.f;
 }
 template <int ACT> __device__ __forceinline__ void gate(float (&g)[8], const float (&u)[8]) {

@@ -267,3 +267,24 @@ def test_stages_of_the_ring_are_not_refilled_under_their_readers():
         bz.glu(x, wg, wu, h=h, preact=preact)
         differs += (preact != want).any()
     assert int(differs) == 0
+
+
+@pytest.mark.parametrize("m", [8, 89])
+def test_gelu_far_below_zero(m):
+    """act(g) and its slope for g in [-10, 4.75], exact in bfloat16, relative to their own size: the erfc's argument is known
+    to 2^-23 relative, which its exponential makes g^2 2^-23 (1.2e-5 at -10), and the fast exponential of the slope adds
+    50 units of 2^-23 at most; then half a unit of the type.  Near its zero (g about -0.75) the slope is a difference
+    of terms of 0.2.  h = act * 1; dx's two columns are dg = dh * 1 * slope and du = dh * act."""
+    g = (torch.arange(m, device="cuda", dtype=torch.float64) / 6 - 10).to(torch.bfloat16)
+    x = torch.stack([g, torch.ones_like(g)], 1).contiguous()
+    wg, wu = torch.tensor([[1.0, 0.0]], device="cuda").to(torch.bfloat16), torch.tensor([[0.0, 1.0]], device="cuda").to(torch.bfloat16)
+    preact, dh = torch.empty(2, m, 1, device="cuda"), torch.ones(m, 1, dtype=torch.bfloat16, device="cuda")
+    h = bz.glu(x, wg, wu, "gelu", preact=preact)
+    dx, _, _ = bz.glu_backward(x, wg, wu, preact, dh, "gelu")
+    G = g.double()
+    phi, density = 0.5 * torch.special.erfc(-G / math.sqrt(2)), torch.exp(-G * G / 2) / math.sqrt(2 * math.pi)
+    want, slope = G * phi, phi + G * density
+    near = 2.0 ** -8 + 2e-5
+    assert ((h[:, 0].double() - want).abs() <= near * want.abs()).all()
+    assert ((dx[:, 1].double() - want).abs() <= near * want.abs()).all()
+    assert ((dx[:, 0].double() - slope).abs() <= 2.0 ** -8 * slope.abs() + 2e-5 * (phi + (G * density).abs())).all()
