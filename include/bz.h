@@ -557,7 +557,9 @@ size_t bz_glu_workspace_bytes(int64_t m, int64_t n, int64_t k, int dtype, int ba
  * where rel > 0; otherwise nb = buckets, n = max(-rel, 0).  Distances n < e = nb / 2 have a bucket each;
  * from there bucket e + t, t = 0 .. nb - e - 1, begins at the smallest n >= e * (max_distance / e)^(t / (nb - e)).
  *   scores, probs  device [b][h][tq][tk], unit stride along tk; strides of b, h, tq in elements in host
- *           arrays of three (any order, none negative; probs may be scores itself).  dtype: BZ_F32, _F16, _BF16.
+ *           arrays of three (any order, none negative; probs may be scores itself).  Scores may repeat rows (stride
+ *           0); no two rows of probs may overlap: taken by size, the strides of its dimensions longer than one each
+ *           reach over what the smaller ones span.  dtype: BZ_F32, _F16, _BF16.
  *   table   device binary32 [buckets][h], contiguous;  2 <= buckets <= 256 (4 <= buckets, even, when
  *           bidirectional), nb / 2 < max_distance <= BZ_MAX_DISTANCE.
  *   k_len   device int32 [b], values taken into [0, tk], or NULL: all tk.
@@ -576,7 +578,7 @@ int bz_bias_softmax(const void* scores, const int64_t* strides_scores, int dtype
  * Its gradient.  With p the probabilities (recomputed in binary32 from scores and stats), dp = dprobs and
  * D = sum over j of p dp:   dz = p (dp - D),  dscores = scale * dz,
  * dtable[c][h] = sum of dz over all b, i, j whose bucket is c.
- *   dprobs, dscores  like scores (dscores may be dprobs or scores itself), dscores may be NULL.
+ *   dprobs, dscores  like scores and probs (dscores may be dprobs or scores itself), dscores may be NULL.
  *   dtable  device binary32 [buckets][h], overwritten, or NULL.
  *   workspace  device, bz_bias_softmax_workspace_bytes(b, h, tq, tk, buckets) bytes, 256-byte aligned (needed
  *           with dtable only).

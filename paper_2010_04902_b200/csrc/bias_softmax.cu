@@ -14,6 +14,8 @@
 // of diagonals: a row meets each diagonal once, so its lanes add without conflict, row after row, in a fixed order;
 // the far sums stay in registers.  CTAs leave one value a bucket and a last kernel adds those in order.  Three transfers an
 // element; 176 us at 8 x 16 x 1024 x 1024 (70 % of the copy's rate): 22 instructions an element are what is left to cut.
+#include <algorithm>
+
 #include "bucket_rule.h"
 #include "worker_common.cuh"
 
@@ -579,6 +581,24 @@ int check_tensor(const void* p, const int64_t* strides, int dtype) {
     return strides[0] < 0 || strides[1] < 0 || strides[2] < 0 ? BZ_ERR_INVALID_ARG : BZ_OK;
 }
 
+// An output's: no two rows may share memory.  In order of the strides of the dimensions longer than one, each has to reach over
+// all that the ones before it span (so lie slices, permutations and gaps of any tensor).
+int check_output(const void* p, const int64_t* strides, int dtype, int64_t b, int64_t h, int64_t tq, int64_t tk) {
+    const int st = check_tensor(p, strides, dtype);
+    if (st != BZ_OK) return st;
+    struct Dim {
+        int64_t stride, n;
+    } d[3] = {{strides[0], b}, {strides[1], h}, {strides[2], tq}};
+    std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+    __int128 span = tk;
+    for (const Dim& x : d) {
+        if (x.n == 1) continue;
+        if (x.stride < span) return BZ_ERR_INVALID_ARG;
+        span += static_cast<__int128>(x.stride) * (x.n - 1);
+    }
+    return BZ_OK;
+}
+
 // Whether two tensors' rows all sit alike relative to 16-byte boundaries.
 bool alike(const void* p, const int64_t* sp, const void* q, const int64_t* sq, int64_t b, int64_t h, int64_t tq, int bytes) {
     if ((reinterpret_cast<uintptr_t>(p) - reinterpret_cast<uintptr_t>(q)) & 15) return false;
@@ -737,7 +757,7 @@ extern "C" int bz_bias_softmax(const void* scores, const int64_t* strides_scores
     int st = check_form(dtype, b, h, tq, tk, table, buckets, max_distance, bidirectional, scale);
     if (st != BZ_OK) return st;
     if (b == 0 || h == 0 || tq == 0 || tk == 0) return BZ_OK;
-    if ((st = check_tensor(scores, strides_scores, dtype)) != BZ_OK || (st = check_tensor(probs, strides_probs, dtype)) != BZ_OK) return st;
+    if ((st = check_tensor(scores, strides_scores, dtype)) != BZ_OK || (st = check_output(probs, strides_probs, dtype, b, h, tq, tk)) != BZ_OK) return st;
     if (!aligned8(stats)) return BZ_ERR_INVALID_ARG;
     BiasForm f = make_form(h, tq, tk, table, buckets, max_distance, bidirectional, causal, scale, k_len, q_start);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -762,7 +782,7 @@ extern "C" int bz_bias_softmax_backward(const void* scores, const int64_t* strid
     }
     if (stats == nullptr || !aligned8(stats)) return BZ_ERR_INVALID_ARG;
     if ((st = check_tensor(scores, strides_scores, dtype)) != BZ_OK || (st = check_tensor(dprobs, strides_dprobs, dtype)) != BZ_OK) return st;
-    if (dscores != nullptr && (st = check_tensor(dscores, strides_dscores, dtype)) != BZ_OK) return st;
+    if (dscores != nullptr && (st = check_output(dscores, strides_dscores, dtype, b, h, tq, tk)) != BZ_OK) return st;
     if (dtable != nullptr &&
         (workspace == nullptr || !aligned256(workspace) || workspace_bytes < bz_bias_softmax_workspace_bytes(b, h, tq, tk, buckets)))
         return BZ_ERR_WORKSPACE;

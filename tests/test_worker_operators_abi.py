@@ -119,3 +119,27 @@ def test_python_side():
         bz.bias_softmax(torch.zeros(2, 3, 4), torch.zeros(32, 3))
     with pytest.raises(TypeError):
         bz.distill(torch.zeros(3, 9), torch.zeros(3, 2), torch.zeros(3, 2, dtype=torch.int32))
+
+
+def test_bias_softmax_outputs_that_overlap(L):
+    """Expanded and interleaved outputs: rows would overwrite one another."""
+    three = lambda *s: (ctypes.c_int64 * 3)(*s)  # noqa: E731
+    S2 = three(80, 40, 10)
+
+    def both(out, b=2, h=2, tq=4, tk=10):
+        head = (F, S2, bz.F16, b, h, tq, tk, F, 32, 128, 1, 0, 1.0, None, None)
+        return (L.bz_bias_softmax(*head, F, out, None, None), L.bz_bias_softmax_backward(*head, F, F, S2, F, out, F, F, BIG, None))
+
+    n0 = bz.kernel_launch_count()
+    for out in (three(0, 40, 10), three(80, 0, 10), three(80, 40, 0), three(80, 40, 9), three(80, 39, 10), three(79, 40, 10), three(40, 40, 10),
+                three(10, 20, 30), three(1 << 62, 1 << 62, 10)):
+        assert both(out) == (bz.ERR_INVALID_ARG, bz.ERR_INVALID_ARG), list(out)
+    # rows apart in any order, gaps, dimensions of one with any stride: past this check, refused for the workspace
+    for out, n in ((three(80, 40, 10), {}), (three(40, 80, 10), {}), (three(10, 20, 40), {}), (three(1 << 62, 40, 10), {}), (three(100, 50, 11), {}),
+                   (three(0, 0, 0), dict(b=1, h=1, tq=1)), (three(3, 10, 0), dict(b=1, h=3, tq=1))):
+        assert both_backward(L, S2, out, **n) == bz.ERR_WORKSPACE, list(out)
+    assert bz.kernel_launch_count() == n0
+
+
+def both_backward(L, strides, out, b=2, h=2, tq=4, tk=10):
+    return L.bz_bias_softmax_backward(F, strides, bz.F16, b, h, tq, tk, F, 32, 128, 1, 0, 1.0, None, None, F, F, strides, F, out, F, None, 0, None)
