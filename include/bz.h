@@ -520,9 +520,9 @@ uint64_t bz_kernel_launch_count(void);
  *           call.  A caller short of memory passes NULL here and repeats the call with one shared buffer
  *           before the backward call.
  *   k == 0 gives h = 0 (empty sums); m == 0 or n == 0 is a successful no-op.
- *   workspace  device, bz_glu_workspace_bytes(m, n, k, dtype, 0) bytes, 256-byte aligned; the bytes are 0
- *           and NULL will do where x and the weights are 16-byte aligned with leading dimensions that are
- *           multiples of 8 (other operands are laid out there first), and up to 32 rows.
+ *   workspace  device, bz_glu_workspace_bytes(m, n, k, dtype, 0) bytes, 256-byte aligned.  NULL will do up to
+ *           32 rows (the bytes are 0), and where x and the weights are 16-byte aligned with leading dimensions
+ *           that are multiples of 8: other operands are laid out there first.
  * m, n, k up to 2^31 - 512 each, leading dimensions below 2^38; m * n below 2^39 in the backward call.  The tensor-core kernels bound every wait; one that runs out stops the
  * kernel early with incomplete outputs and counts in bz_pipeline_timeouts().
  */
@@ -544,7 +544,7 @@ int bz_glu_backward(const void* x, int64_t ld_x, const void* w_gate, const void*
                     void* dw_gate, void* dw_up, int64_t ld_dw, int grad_dtype, void* workspace, size_t workspace_bytes,
                     void* stream);
 
-/* Device scratch of bz_glu (backward == 0) or bz_glu_backward for any alignment; 0 for arguments they refuse. */
+/* Device scratch of bz_glu (backward == 0) or bz_glu_backward for any alignment; 0 for sizes and types they refuse. */
 size_t bz_glu_workspace_bytes(int64_t m, int64_t n, int64_t k, int dtype, int backward);
 
 /*

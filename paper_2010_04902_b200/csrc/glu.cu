@@ -322,10 +322,13 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
     return bn == 256 ? launch_product<T, kBackward, 256>(maps, p, s) : launch_product<T, kBackward, 128>(maps, p, s);
 }
 
+constexpr int64_t kMostExtent = (int64_t(1) << 31) - 512;  // tile coordinates are 32-bit
+// Whether a tensor map's stride cannot reach from dg to du.
+bool too_far_apart(int64_t m, int64_t n) { return m > 0 && static_cast<int64_t>(round_up(n, 8)) >= (int64_t(1) << 39) / m; }
+
 int check(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t ld_w, int64_t m, int64_t n, int64_t k, int dtype, int act) {
     if (m < 0 || n < 0 || k < 0 || element_bytes(dtype) == 0 || act < BZ_ACT_SILU || act > BZ_ACT_RELU) return BZ_ERR_INVALID_ARG;
-    const int64_t most = (int64_t(1) << 31) - 512;  // tile coordinates are 32-bit
-    if (m > most || n > most || k > most || dtype == BZ_F32 || ld_x >= int64_t(1) << 38 || ld_w >= int64_t(1) << 38) return BZ_ERR_UNSUPPORTED;
+    if (m > kMostExtent || n > kMostExtent || k > kMostExtent || dtype == BZ_F32 || ld_x >= int64_t(1) << 38 || ld_w >= int64_t(1) << 38) return BZ_ERR_UNSUPPORTED;
     if ((m > 1 && ld_x < k) || (n > 1 && ld_w < k)) return BZ_ERR_INVALID_ARG;
     if ((m > 0 && k > 0 && x == nullptr) || (n > 0 && k > 0 && (wg == nullptr || wu == nullptr))) return BZ_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(wg) | reinterpret_cast<uintptr_t>(wu)) & 1) return BZ_ERR_INVALID_ARG;
@@ -344,7 +347,8 @@ int glu_timeouts(unsigned int* count) {
 using namespace bz;
 
 extern "C" size_t bz_glu_workspace_bytes(int64_t m, int64_t n, int64_t k, int dtype, int backward) {
-    if (m < 0 || n < 0 || k < 0 || (dtype != BZ_F16 && dtype != BZ_BF16)) return 0;
+    if (m < 0 || n < 0 || k < 0 || m > kMostExtent || n > kMostExtent || k > kMostExtent || (dtype != BZ_F16 && dtype != BZ_BF16)) return 0;
+    if (backward ? too_far_apart(m, n) : m <= kFewMost) return 0;
     const size_t kp = round_up(k, 8), np = round_up(n, 8);
     const size_t operands = round_up(2 * m * kp, 256) + 2 * round_up(2 * n * kp, 256);
     return backward ? round_up(4 * m * np, 256) + kPartialBytes + operands : operands;
@@ -372,7 +376,7 @@ extern "C" int bz_glu_backward(const void* x, int64_t ld_x, const void* w_gate, 
     const int st = check(x, ld_x, w_gate, w_up, ld_w, m, n, k, dtype, act);
     if (st != BZ_OK) return st;
     if ((grad_dtype != dtype && grad_dtype != BZ_F32) || (dw_gate == nullptr) != (dw_up == nullptr)) return BZ_ERR_INVALID_ARG;
-    if (m > 0 && static_cast<int64_t>(round_up(n, 8)) >= (int64_t(1) << 39) / m) return BZ_ERR_UNSUPPORTED;  // a tensor map's stride from dg to du
+    if (too_far_apart(m, n)) return BZ_ERR_UNSUPPORTED;
     if (k == 0 || (m == 0 && n == 0)) return BZ_OK;
     const uintptr_t grads = reinterpret_cast<uintptr_t>(dw_gate) | reinterpret_cast<uintptr_t>(dw_up);
     if (dx == nullptr && dw_gate == nullptr) return BZ_ERR_INVALID_ARG;

@@ -143,3 +143,14 @@ def test_bias_softmax_outputs_that_overlap(L):
 
 def both_backward(L, strides, out, b=2, h=2, tq=4, tk=10):
     return L.bz_bias_softmax_backward(F, strides, bz.F16, b, h, tq, tk, F, 32, 128, 1, 0, 1.0, None, None, F, F, strides, F, out, F, None, 0, None)
+
+
+def test_glu_workspace_sizes(L):
+    size = L.bz_glu_workspace_bytes
+    assert size(1, 10922, 4096, bz.BF16, 0) == size(32, 7, 9, bz.F16, 0) == 0       # up to 32 rows nothing is laid out
+    assert size(33, 7, 9, bz.F16, 0) >= 2 * (33 + 2 * 7) * 9 and size(1, 7, 9, bz.F16, 1) > 0
+    most = (1 << 31) - 512
+    assert size(40, 8, most, bz.BF16, 0) > 0
+    for m, n, k in ((most + 1, 8, 8), (40, most + 1, 8), (40, 8, most + 1), (BIG, 8, 8)):
+        assert size(m, n, k, bz.BF16, 0) == size(m, n, k, bz.BF16, 1) == 0
+    assert size(1 << 20, 1 << 19, 8, bz.BF16, 1) == 0 and size(1 << 20, (1 << 19) - 8, 8, bz.BF16, 1) > 0
