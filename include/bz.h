@@ -589,6 +589,7 @@ int bz_bias_softmax_backward(const void* scores, const int64_t* strides_scores, 
                              const int64_t* strides_dprobs, void* dscores, const int64_t* strides_dscores, float* dtable,
                              void* workspace, size_t workspace_bytes, void* stream);
 
+/* 0 for sizes that the call refuses; the largest multiple of 256 where the bytes would not fit a size_t. */
 size_t bz_bias_softmax_workspace_bytes(int64_t b, int64_t h, int64_t tq, int64_t tk, int buckets);
 
 /*

@@ -549,14 +549,12 @@ __global__ void __launch_bounds__(256) bias_table_kernel(const float* __restrict
 
 // Query rows a CTA takes.  Building the window (and leaving the buckets) costs a CTA what some rows do, so it takes up to
 // `most` of them; `resident` CTAs run at a time, and of the counts that fill whole rounds of those the smallest one is taken
-// (a part-filled last round leaves the GPU idle).  Small problems spread over one round.
+// (a part-filled last round leaves the GPU idle).  Small problems spread over one round.  `most` is a multiple of at_a_time.
 int rows_for(int64_t heads, int64_t tq, int64_t resident, int at_a_time, int most) {
-    for (int64_t rounds = 1;; ++rounds) {
-        int64_t chunks = rounds * resident / heads;
-        if (chunks < 1) chunks = 1;
-        const int64_t rows = ((tq + chunks - 1) / chunks + at_a_time - 1) / at_a_time * at_a_time;
-        if (rows <= most) return static_cast<int>(rows);
-    }
+    const int64_t least = (tq + most - 1) / most;   // chunks a head that keep a CTA to `most` rows
+    const int64_t rounds = least < 2 ? 1 : (least * heads + resident - 1) / resident;
+    const int64_t chunks = std::max<int64_t>(1, rounds * resident / heads);
+    return static_cast<int>(((tq + chunks - 1) / chunks + at_a_time - 1) / at_a_time * at_a_time);
 }
 // The backward kernels run 512 threads an SM; the smallest groups (64 threads, one row) make the most CTAs.
 constexpr int kBackwardMost = 64;
@@ -746,8 +744,11 @@ int backward(BiasForm& f, int64_t b, const void* scores, const int64_t* ss, cons
 using namespace bz;
 
 extern "C" size_t bz_bias_softmax_workspace_bytes(int64_t b, int64_t h, int64_t tq, int64_t tk, int buckets) {
-    if (b < 1 || h < 1 || tq < 1 || tk < 1 || buckets < 2 || buckets > 256 || b > 65535 || h > 65535 || tq >= (int64_t(1) << 31)) return 0;
-    return round_up(static_cast<size_t>(b) * h * most_chunks(b * h, tq) * buckets * sizeof(float), 256);
+    if (b < 1 || h < 1 || tq < 1 || tk < 1 || buckets < 2 || buckets > 256 || b > 65535 || h > 65535) return 0;
+    if (tq >= (int64_t(1) << 31) || tk >= (int64_t(1) << 31)) return 0;
+    const size_t parts = static_cast<size_t>(b) * h * most_chunks(b * h, tq), each = buckets * sizeof(float);   // parts < 2^58
+    const size_t most = ~size_t(0) / 256 * 256;
+    return parts > most / each ? most : round_up(parts * each, 256);
 }
 
 extern "C" int bz_bias_softmax(const void* scores, const int64_t* strides_scores, int dtype, int64_t b, int64_t h, int64_t tq, int64_t tk,

@@ -1,5 +1,8 @@
 """Refusals of the worker's operators: every call here returns from the host's checks, before anything is launched."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -154,3 +157,14 @@ def test_glu_workspace_sizes(L):
     for m, n, k in ((most + 1, 8, 8), (40, most + 1, 8), (40, 8, most + 1), (BIG, 8, 8)):
         assert size(m, n, k, bz.BF16, 0) == size(m, n, k, bz.BF16, 1) == 0
     assert size(1 << 20, 1 << 19, 8, bz.BF16, 1) == 0 and size(1 << 20, (1 << 19) - 8, 8, bz.BF16, 1) > 0
+
+
+def test_bias_softmax_workspace_of_many_heads_and_queries(L):
+    """The size takes no longer for more heads and queries (it had counted rounds of CTAs one by one: hours at the limits),
+    and it does not wrap."""
+    ask = ("import sys; sys.path.insert(0, %r)\nfrom paper_2010_04902_b200 import binding as bz\nf = bz.lib().bz_bias_softmax_workspace_bytes\n"
+           "print(f(65535, 65535, 2 ** 31 - 1, 1, 256), f(512, 512, 512, 1, 32), f(1, 1, 1, 1 << 31, 32))" % os.path.dirname(os.path.dirname(__file__)))
+    r = subprocess.run([sys.executable, "-c", ask], capture_output=True, text=True, timeout=60)
+    largest, usual, refused = (int(v) for v in r.stdout.split())
+    assert largest == 2 ** 64 - 256 and refused == 0
+    assert 512 * 512 * 8 * 32 * 4 <= usual <= 2 * 512 * 512 * 8 * 32 * 4      # eight chunks of 64 queries a head
