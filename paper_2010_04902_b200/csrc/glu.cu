@@ -63,20 +63,25 @@ dim3 row_grid(int64_t rows, int64_t columns_of_threads) {
 // Whether a tensor map can describe rows like these.
 bool laid_out(const void* p, int64_t ld, int64_t rows) { return aligned16(p) && (rows <= 1 || ld % 8 == 0); }
 
+// An operand as the tensor maps describe it: itself, or a copy of it in the workspace that lay_out() makes.  The maps are made
+// first, so that nothing has been launched when one is refused.
 struct Operand {
     const void* p;
-    int64_t ld;
+    int64_t ld, rows, n;
+    const void* at;      // what the map describes
+    int64_t ld_at;
 };
-// The operand itself, or a copy of it in `room`.
-int lay_out(const void* p, int64_t ld, int64_t rows, int64_t n, char*& room, Operand& o, cudaStream_t s) {
-    const int64_t ld_to = (n + 7) / 8 * 8;
-    if (laid_out(p, ld, rows)) {
-        o = {p, rows > 1 ? ld : ld_to};
-        return BZ_OK;
-    }
-    o = {room, ld_to};
-    glu_lay_out_kernel<<<row_grid(rows, n), 256, 0, s>>>(static_cast<const uint16_t*>(p), ld, rows, n, reinterpret_cast<uint16_t*>(room), ld_to);
-    room += round_up(static_cast<size_t>(rows) * ld_to * 2, 256);
+Operand place_operand(const void* p, int64_t ld, int64_t rows, int64_t n, char*& room) {
+    const int64_t ld_at = (n + 7) / 8 * 8;
+    if (laid_out(p, ld, rows)) return {p, ld, rows, n, p, rows > 1 ? ld : ld_at};
+    const Operand o{p, ld, rows, n, room, ld_at};
+    room += round_up(static_cast<size_t>(rows) * ld_at * 2, 256);
+    return o;
+}
+int lay_out(const Operand& o, cudaStream_t s) {
+    if (o.at == o.p) return BZ_OK;
+    glu_lay_out_kernel<<<row_grid(o.rows, o.n), 256, 0, s>>>(static_cast<const uint16_t*>(o.p), o.ld, o.rows, o.n,
+                                                             static_cast<uint16_t*>(const_cast<void*>(o.at)), o.ld_at);
     note_launch();
     return check_launch();
 }
@@ -235,10 +240,7 @@ int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t
         const bool wide = laid_out(x, ld_x, m) && laid_out(wg, ld_w, n) && laid_out(wu, ld_w, n);
         return few<T>(p, wide, s);
     }
-    Operand ox, og, ou;
-    if ((st = lay_out(x, ld_x, m, k, ws, ox, s)) != BZ_OK || (st = lay_out(wg, ld_w, n, k, ws, og, s)) != BZ_OK ||
-        (st = lay_out(wu, ld_w, n, k, ws, ou, s)) != BZ_OK)
-        return st;
+    const Operand ox = place_operand(x, ld_x, m, k, ws), og = place_operand(wg, ld_w, n, k, ws), ou = place_operand(wu, ld_w, n, k, ws);
     ProductParams p{};
     ProductPart& o = p.part[0];
     o.rows = m, o.cols = n, o.blocks = ceil_div(k, kBlockK);
@@ -247,9 +249,10 @@ int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t
     o.out = h, o.ld_out = ld_h, o.wide = wide_rows(h, ld_h, m, 2), o.pairs = pair_rows(h, ld_h, m, 2);
     p.act = act, p.preact = preact, p.preact_wide = n % 4 == 0, p.preact_pairs = n % 2 == 0;
     ProductMaps maps;
-    if (!make_map<T>(&maps.map[0], ox.p, k, m, ox.ld, 128, 0) || !make_map<T>(&maps.map[1], og.p, k, n, og.ld, bn / 2, 0) ||
-        !make_map<T>(&maps.map[2], ou.p, k, n, ou.ld, bn / 2, 0))
+    if (!make_map<T>(&maps.map[0], ox.at, k, m, ox.ld_at, 128, 0) || !make_map<T>(&maps.map[1], og.at, k, n, og.ld_at, bn / 2, 0) ||
+        !make_map<T>(&maps.map[2], ou.at, k, n, ou.ld_at, bn / 2, 0))
         return BZ_ERR_UNSUPPORTED;
+    if ((st = lay_out(ox, s)) != BZ_OK || (st = lay_out(og, s)) != BZ_OK || (st = lay_out(ou, s)) != BZ_OK) return st;
     if (bn == 256) return launch_product<T, kForward, 256>(maps, p, s);
     return bn == 128 ? launch_product<T, kForward, 128>(maps, p, s) : launch_product<T, kForward, 64>(maps, p, s);
 }
@@ -279,6 +282,29 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
     T* dgu = reinterpret_cast<T*>(ws);
     float* partial = reinterpret_cast<float*>(ws + round_up(static_cast<size_t>(4) * m * ld, 256));
     char* room = reinterpret_cast<char*>(partial) + kPartialBytes;
+    ProductParams p{};
+    ProductMaps maps;
+    Operand og{}, ou{}, ox{};
+    if (dx != nullptr) {
+        og = place_operand(wg, ld_w, n, k, room), ou = place_operand(wu, ld_w, n, k, room);
+        ProductPart& o = p.part[kInput];
+        o.rows = m, o.cols = k, o.half_blocks = ceil_div(n, kBlockK), o.blocks = 2 * o.half_blocks;
+        o.out = dx, o.ld_out = ld_dx, o.wide = wide_rows(dx, ld_dx, m, 2), o.pairs = pair_rows(dx, ld_dx, m, 2);
+        if (!make_map<T>(&maps.map[0], dgu, n, m, ld, 128, m * ld) || !make_map<T>(&maps.map[1], og.at, k, n, og.ld_at, kBlockK, 0) ||
+            !make_map<T>(&maps.map[2], ou.at, k, n, ou.ld_at, kBlockK, 0))
+            return BZ_ERR_UNSUPPORTED;
+    }
+    if (dwg != nullptr) {
+        ox = place_operand(x, ld_x, m, k, room);
+        const int bytes = grad_f32 ? 4 : 2;
+        ProductPart& o = p.part[kWeight];
+        o.rows = n, o.cols = k, o.blocks = ceil_div(m, kBlockK);
+        o.out = dwg, o.out2 = dwu, o.ld_out = ld_dw, o.out_f32 = grad_f32;
+        o.wide = wide_rows(dwg, ld_dw, n, bytes) && aligned16(dwu);
+        o.pairs = pair_rows(dwg, ld_dw, n, bytes) && pair_rows(dwu, ld_dw, n, bytes);
+        if (!make_map<T>(&maps.map[3], dgu, n, m, ld, kBlockK, m * ld) || !make_map<T>(&maps.map[4], ox.at, k, m, ox.ld_at, kBlockK, 0))
+            return BZ_ERR_UNSUPPORTED;
+    }
     const T* d = static_cast<const T*>(dh);
     switch (act) {
         case BZ_ACT_SILU: st = launch_dgu<T, BZ_ACT_SILU>(preact, d, ld_dh, m, n, dgu, ld, s); break;
@@ -287,30 +313,7 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
         default: st = launch_dgu<T, BZ_ACT_RELU>(preact, d, ld_dh, m, n, dgu, ld, s); break;
     }
     if (st != BZ_OK) return st;
-    ProductParams p{};
-    ProductMaps maps;
-    if (dx != nullptr) {
-        Operand og, ou;
-        if ((st = lay_out(wg, ld_w, n, k, room, og, s)) != BZ_OK || (st = lay_out(wu, ld_w, n, k, room, ou, s)) != BZ_OK) return st;
-        ProductPart& o = p.part[kInput];
-        o.rows = m, o.cols = k, o.half_blocks = ceil_div(n, kBlockK), o.blocks = 2 * o.half_blocks;
-        o.out = dx, o.ld_out = ld_dx, o.wide = wide_rows(dx, ld_dx, m, 2), o.pairs = pair_rows(dx, ld_dx, m, 2);
-        if (!make_map<T>(&maps.map[0], dgu, n, m, ld, 128, m * ld) || !make_map<T>(&maps.map[1], og.p, k, n, og.ld, kBlockK, 0) ||
-            !make_map<T>(&maps.map[2], ou.p, k, n, ou.ld, kBlockK, 0))
-            return BZ_ERR_UNSUPPORTED;
-    }
-    if (dwg != nullptr) {
-        Operand ox;
-        if ((st = lay_out(x, ld_x, m, k, room, ox, s)) != BZ_OK) return st;
-        const int bytes = grad_f32 ? 4 : 2;
-        ProductPart& o = p.part[kWeight];
-        o.rows = n, o.cols = k, o.blocks = ceil_div(m, kBlockK);
-        o.out = dwg, o.out2 = dwu, o.ld_out = ld_dw, o.out_f32 = grad_f32;
-        o.wide = wide_rows(dwg, ld_dw, n, bytes) && aligned16(dwu);
-        o.pairs = pair_rows(dwg, ld_dw, n, bytes) && pair_rows(dwu, ld_dw, n, bytes);
-        if (!make_map<T>(&maps.map[3], dgu, n, m, ld, kBlockK, m * ld) || !make_map<T>(&maps.map[4], ox.p, k, m, ox.ld, kBlockK, 0))
-            return BZ_ERR_UNSUPPORTED;
-    }
+    if ((st = lay_out(og, s)) != BZ_OK || (st = lay_out(ou, s)) != BZ_OK || (st = lay_out(ox, s)) != BZ_OK) return st;
     if (dx == nullptr) maps.map[0] = maps.map[1] = maps.map[2] = maps.map[3];   // prefetched, not used
     if (dwg == nullptr) maps.map[3] = maps.map[4] = maps.map[0];
     const double narrow = plan_backward(p, 128);

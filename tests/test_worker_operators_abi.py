@@ -168,3 +168,24 @@ def test_bias_softmax_workspace_of_many_heads_and_queries(L):
     largest, usual, refused = (int(v) for v in r.stdout.split())
     assert largest == 2 ** 64 - 256 and refused == 0
     assert 512 * 512 * 8 * 32 * 4 <= usual <= 2 * 512 * 512 * 8 * 32 * 4      # eight chunks of 64 queries a head
+
+
+def test_glu_enqueues_nothing_when_a_tensor_map_cannot_be_made():
+    """Where there is no driver no map can be made: operands off the 16-byte grid (which are copied first) and the backward
+    call (whose first kernel comes before the products) must have launched nothing.  No device is visible to the process."""
+    try:
+        ctypes.CDLL("libcuda.so.1")
+        pytest.skip("there is a driver")
+    except OSError:
+        pass
+    ask = """if 1:
+        import sys; sys.path.insert(0, %r)
+        import ctypes
+        from paper_2010_04902_b200 import binding as bz
+        P = ctypes.c_void_p(256)
+        a = bz.lib().bz_glu(P, 9, P, P, 9, 40, 6, 9, bz.BF16, 0, P, 6, None, P, 1 << 40, None)
+        b = bz.lib().bz_glu_backward(P, 8, P, P, 8, P, P, 6, 40, 6, 8, bz.BF16, 0, P, 8, P, P, 8, bz.BF16, P, 1 << 40, None)
+        print(a, b, bz.kernel_launch_count())
+    """ % os.path.dirname(os.path.dirname(__file__))
+    r = subprocess.run([sys.executable, "-c", ask], capture_output=True, text=True, timeout=120, env={**os.environ, "CUDA_VISIBLE_DEVICES": ""})
+    assert r.stdout.split() == [str(bz.ERR_UNSUPPORTED)] * 2 + ["0"], r.stdout + r.stderr[-1000:]
