@@ -606,6 +606,9 @@ def vote_bulyan(replicas: torch.Tensor, c: int, voted: torch.Tensor | None = Non
 
 
 # ------------------------------------------------------------------------------------- a worker's step
+#
+# These calls record nothing for automatic differentiation: each has its gradient as a call of its own.  The forward calls
+# refuse tensors that require a gradient while gradients are recorded, whose gradient would be lost without a word.
 
 _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 _Strides = ctypes.c_int64 * 3
@@ -661,6 +664,13 @@ def _like_rows(t: torch.Tensor) -> torch.Tensor:
     return t.new_empty(t.shape[:-1] + (ld,))[..., :n]
 
 
+def _unrecorded(what: str, **tensors):
+    """Called with the tensors of a forward call of which one at least requires a gradient."""
+    if torch.is_grad_enabled():
+        raise ValueError("%s: %s requires a gradient, which this call does not record: call it under torch.no_grad() (or inside an "
+                         "autograd.Function) and %s_backward for the gradient" % (what, " and ".join(n for n, t in tensors.items() if t.requires_grad), what))
+
+
 def _act(name: str) -> int:
     try:
         return _ACTS[name]
@@ -697,6 +707,8 @@ def glu(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "s
         preact: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """bz_glu: act(x w_gate^T) * (x w_up^T) for x [m][k], weights [n][k] (float16 or bfloat16).  `preact`, binary32
     [2][m][n], receives both projections for glu_backward."""
+    if x.requires_grad or w_gate.requires_grad or w_up.requires_grad:
+        _unrecorded("glu", x=x, w_gate=w_gate, w_up=w_up)
     m, n, k, ld_x, ld_w = _glu_operands(x, w_gate, w_up)
     dt = _dtype(x, "x")
     if h is None:
@@ -788,6 +800,8 @@ def bias_softmax(scores: torch.Tensor, table: torch.Tensor, max_distance: int = 
                  q_start: torch.Tensor | None = None, probs: torch.Tensor | None = None, stats: torch.Tensor | None = None):
     """bz_bias_softmax: softmax over keys of scale * scores [b][h][tq][tk] + table[bucket(key - query)][h].  Returns
     (probs, stats)."""
+    if scores.requires_grad or table.requires_grad:
+        _unrecorded("bias_softmax", scores=scores, table=table)
     strides, form = _bias_form(scores, table, max_distance, bidirectional, causal, scale, k_len, q_start)
     probs, p_probs, s_probs = _rows_out(probs, scores, strides, "probs")
     if stats is None:
@@ -835,6 +849,8 @@ def distill(logits: torch.Tensor, teacher: torch.Tensor, index: torch.Tensor, te
             dlogits: torch.Tensor | None = None):
     """bz_distill: the loss of each position against the teacher's top logits.  Returns (loss, stats); with `dloss`
     (float32 [m]) or `dlogits` given also the gradient, from the same pass: (loss, stats, dlogits)."""
+    if logits.requires_grad:
+        _unrecorded("distill", logits=logits)
     m, v, ld = _matrix(logits, "logits")
     dt = _dtype(logits, "logits")
     p_teacher, p_index, top = _teacher(logits, teacher, index)

@@ -189,3 +189,17 @@ def test_glu_enqueues_nothing_when_a_tensor_map_cannot_be_made():
     """ % os.path.dirname(os.path.dirname(__file__))
     r = subprocess.run([sys.executable, "-c", ask], capture_output=True, text=True, timeout=120, env={**os.environ, "CUDA_VISIBLE_DEVICES": ""})
     assert r.stdout.split() == [str(bz.ERR_UNSUPPORTED)] * 2 + ["0"], r.stdout + r.stderr[-1000:]
+
+
+def test_tensors_that_require_a_gradient():
+    """Refused while gradients are recorded; otherwise the calls go on (here to the refusal of tensors that are not on a GPU)."""
+    x, w, table = torch.zeros(4, 8).half(), torch.zeros(3, 8).half(), torch.zeros(32, 2)
+    scores, teacher, index = torch.zeros(1, 2, 3, 4), torch.zeros(4, 2), torch.zeros(4, 2, dtype=torch.int32)
+    g = lambda t: t.clone().requires_grad_(True)  # noqa: E731
+    calls = [lambda: bz.glu(g(x), w, w), lambda: bz.glu(x, g(w), w), lambda: bz.glu(x, w, g(w)), lambda: bz.bias_softmax(g(scores), table),
+             lambda: bz.bias_softmax(scores, g(table)), lambda: bz.distill(g(x), teacher, index)]
+    for call in calls:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(TypeError):
+            call()
