@@ -182,6 +182,13 @@ def _dev(t: torch.Tensor, dtype, name: str) -> int:
     return t.data_ptr()
 
 
+def _room(workspace: torch.Tensor):
+    """(address, bytes) of a workspace: contiguous device memory of any type."""
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def _rows(t: torch.Tensor, name: str):
     """(f, d, ld) of a [f][d] tensor whose last dimension is contiguous."""
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
@@ -247,7 +254,7 @@ def worst_case(worker_mask, f: int, r: int, q: int, max_subsets: int = 0, worksp
     n = ctypes.c_uint64(0)
     arg = np.zeros(max(q, 1), np.int32)
     st = lib().bz_worst_case(mask.ctypes.data, K, f, r, q, max_subsets, ctypes.addressof(cmax), arg.ctypes.data,
-                             ctypes.addressof(n), ws.data_ptr(), ws.numel(), _stream())
+                             ctypes.addressof(n), *_room(ws), _stream())
     _check(st, "bz_worst_case(K=%d, q=%d)" % (K, q))
     return int(cmax.value), arg[:q].copy(), int(n.value)
 
@@ -263,7 +270,7 @@ def worst_case_part(worker_mask, f: int, r: int, q: int, part: int, parts: int, 
     n = ctypes.c_uint64(0)
     arg = np.zeros(max(q, 1), np.int32)
     st = lib().bz_worst_case_part(mask.ctypes.data, K, f, r, q, part, parts, max_subsets, ctypes.addressof(cmax),
-                                  arg.ctypes.data, ctypes.addressof(n), ws.data_ptr(), ws.numel(), _stream())
+                                  arg.ctypes.data, ctypes.addressof(n), *_room(ws), _stream())
     _check(st, "bz_worst_case_part(K=%d, q=%d, part %d of %d)" % (K, q, part, parts))
     return int(cmax.value), arg[:q].copy(), int(n.value)
 
@@ -276,7 +283,7 @@ def worst_case_mols(l: int, r: int, q: int, max_subsets: int = 0, workspace: tor
     n = ctypes.c_uint64(0)
     arg = np.zeros(max(q, 1), np.int32)
     st = lib().bz_worst_case_mols(l, r, q, max_subsets, ctypes.addressof(cmax), arg.ctypes.data, ctypes.addressof(n),
-                                  ws.data_ptr(), ws.numel(), _stream())
+                                  *_room(ws), _stream())
     _check(st, "bz_worst_case_mols(l=%d, r=%d, q=%d)" % (l, r, q))
     return int(cmax.value), arg[:q].copy(), int(n.value)
 
@@ -290,7 +297,7 @@ def worst_case_mols_part(l: int, r: int, q: int, part: int, parts: int, max_subs
     n = ctypes.c_uint64(0)
     arg = np.zeros(max(q, 1), np.int32)
     st = lib().bz_worst_case_mols_part(l, r, q, part, parts, max_subsets, ctypes.addressof(cmax), arg.ctypes.data,
-                                       ctypes.addressof(n), ws.data_ptr(), ws.numel(), _stream())
+                                       ctypes.addressof(n), *_room(ws), _stream())
     _check(st, "bz_worst_case_mols_part(l=%d, r=%d, q=%d, part %d of %d)" % (l, r, q, part, parts))
     return int(cmax.value), arg[:q].copy(), int(n.value)
 
@@ -368,7 +375,7 @@ def vote_vectorwise(replicas: torch.Tensor, voted: torch.Tensor | None = None, w
     ws = workspace if workspace is not None else alloc_workspace(OP_VOTE_VECTORWISE, r, f, d, device=replicas.device)
     winner = torch.empty(f, dtype=torch.int32, device=replicas.device)
     st = lib().bz_vote_vectorwise(_dev(replicas, torch.float32, "replicas"), r, f, d, ld_file, ld_rep,
-                                  _dev(voted, torch.float32, "voted"), ld_v, winner.data_ptr(), ws.data_ptr(), ws.numel(),
+                                  _dev(voted, torch.float32, "voted"), ld_v, winner.data_ptr(), *_room(ws),
                                   _stream())
     _check(st, "bz_vote_vectorwise")
     return voted, winner
@@ -386,8 +393,7 @@ def vote_clusters(replicas: torch.Tensor, abs_tol: float, rel_tol: float, voted:
     ws = workspace if workspace is not None else alloc_workspace(OP_VOTE_VECTORWISE, r, f, d, device=replicas.device)
     winner = torch.empty(f, dtype=torch.int32, device=replicas.device)
     st = lib().bz_vote_clusters(_dev(replicas, torch.float32, "replicas"), r, f, d, ld_file, ld_rep, float(abs_tol),
-                                float(rel_tol), _dev(voted, torch.float32, "voted"), ld_v, winner.data_ptr(), ws.data_ptr(),
-                                ws.numel(), _stream())
+                                float(rel_tol), _dev(voted, torch.float32, "voted"), ld_v, winner.data_ptr(), *_room(ws), _stream())
     _check(st, "bz_vote_clusters")
     return voted, winner
 
@@ -445,8 +451,7 @@ def vote_median_host(replicas_host: torch.Tensor, out_host: torch.Tensor, worksp
     if replicas_host.dtype != torch.float32 or out_host.dtype != torch.float32:
         raise TypeError("float32 expected")
     r, f, d = replicas_host.shape
-    st = lib().bz_vote_median_host(replicas_host.data_ptr(), r, f, d, out_host.data_ptr(), workspace.data_ptr(),
-                                   workspace.numel(), _stream())
+    st = lib().bz_vote_median_host(replicas_host.data_ptr(), r, f, d, out_host.data_ptr(), *_room(workspace), _stream())
     _check(st, "bz_vote_median_host")
     return out_host
 
@@ -457,7 +462,7 @@ def pairdist(voted: torch.Tensor, workspace: torch.Tensor | None = None, dist: t
     if dist is None:
         dist = torch.empty((f, f), dtype=torch.float64, device=voted.device)
     st = lib().bz_pairdist(_dev(voted, torch.float32, "voted"), f, d, ld, _dev(dist, torch.float64, "dist"),
-                           ws.data_ptr(), ws.numel(), _stream())
+                           *_room(ws), _stream())
     _check(st, "bz_pairdist")
     return dist
 
@@ -507,7 +512,7 @@ def multikrum(voted: torch.Tensor, c: int, m: int, workspace: torch.Tensor | Non
     sel = torch.empty(max(m, 1), dtype=torch.int32, device=voted.device)
     dist = torch.empty((f, f), dtype=torch.float64, device=voted.device) if want_dist else None
     st = lib().bz_multikrum(_dev(voted, torch.float32, "voted"), f, d, ld, c, m, _dev(out, torch.float32, "out"),
-                            sel.data_ptr(), dist.data_ptr() if dist is not None else None, ws.data_ptr(), ws.numel(),
+                            sel.data_ptr(), dist.data_ptr() if dist is not None else None, *_room(ws),
                             _stream())
     _check(st, "bz_multikrum")
     return (out, sel[:m], dist) if want_dist else (out, sel[:m])
@@ -541,7 +546,7 @@ def bulyan(voted: torch.Tensor, c: int, workspace: torch.Tensor | None = None, o
     theta = f - 2 * c
     sel = torch.empty(max(theta, 1), dtype=torch.int32, device=voted.device)
     st = lib().bz_bulyan(_dev(voted, torch.float32, "voted"), f, d, ld, c, _dev(out, torch.float32, "out"),
-                         sel.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+                         sel.data_ptr(), *_room(ws), _stream())
     _check(st, "bz_bulyan")
     return out, sel[:max(theta, 0)]
 
@@ -567,7 +572,7 @@ def vote_pairdist(replicas: torch.Tensor, voted: torch.Tensor | None = None, wor
         dist = torch.empty((f, f), dtype=torch.float64, device=replicas.device)
     st = lib().bz_vote_pairdist(_dev(replicas, torch.float32, "replicas"), r, f, d, ld_file, ld_rep,
                                 _dev(voted, torch.float32, "voted"), ld_v, _dev(dist, torch.float64, "dist"),
-                                ws.data_ptr(), ws.numel(), _stream())
+                                *_room(ws), _stream())
     _check(st, "bz_vote_pairdist")
     return voted, dist
 
@@ -584,7 +589,7 @@ def vote_multikrum(replicas: torch.Tensor, c: int, m: int, voted: torch.Tensor |
     st = lib().bz_vote_multikrum(_dev(replicas, torch.float32, "replicas"), r, f, d, ld_file, ld_rep, c, m,
                                  _dev(voted, torch.float32, "voted"), ld_v, _dev(out, torch.float32, "out"),
                                  sel.data_ptr(), None if dist is None else _dev(dist, torch.float64, "dist"),
-                                 ws.data_ptr(), ws.numel(), _stream())
+                                 *_room(ws), _stream())
     _check(st, "bz_vote_multikrum")
     return out, sel[:m], voted
 
@@ -600,7 +605,7 @@ def vote_bulyan(replicas: torch.Tensor, c: int, voted: torch.Tensor | None = Non
     sel = torch.empty(max(theta, 1), dtype=torch.int32, device=replicas.device)
     st = lib().bz_vote_bulyan(_dev(replicas, torch.float32, "replicas"), r, f, d, ld_file, ld_rep, c,
                               _dev(voted, torch.float32, "voted"), ld_v, _dev(out, torch.float32, "out"),
-                              sel.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+                              sel.data_ptr(), *_room(ws), _stream())
     _check(st, "bz_vote_bulyan")
     return out, sel[:max(theta, 0)], voted
 
@@ -719,7 +724,7 @@ def glu(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, act: str = "s
     px, pg, pu = x.data_ptr(), _dev(w_gate, x.dtype, "w_gate"), _dev(w_up, x.dtype, "w_up")
     ws, ws_bytes = None, 0
     if workspace is not None:
-        ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+        ws, ws_bytes = _room(workspace)
     elif m > GLU_FEW and ((ld_x | ld_w) & 7 or (px | pg | pu) & 15):
         workspace = torch.empty(max(256, lib().bz_glu_workspace_bytes(m, n, k, dt, 0)), dtype=torch.uint8, device=x.device)
         ws, ws_bytes = workspace.data_ptr(), workspace.numel()
@@ -758,7 +763,7 @@ def glu_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, prea
     st = lib().bz_glu_backward(_dev(x, x.dtype, "x"), ld_x, _dev(w_gate, x.dtype, "w_gate"), _dev(w_up, x.dtype, "w_up"), ld_w,
                                _packed(preact, (2, m, n), torch.float32, "preact"), _shaped(dh, (m, n), x.dtype, "dh"),
                                _matrix(dh, "dh")[2], m, n, k, dt, _act(act), p_dx, ld_dx, p_dg, p_du, ld_dw, grad,
-                               workspace.data_ptr(), workspace.numel(), _stream())
+                               *_room(workspace), _stream())
     if st:
         _check(st, "bz_glu_backward")
     return dx, dw_gate, dw_up
@@ -830,7 +835,7 @@ def bias_softmax_backward(scores: torch.Tensor, table: torch.Tensor, stats: torc
         workspace = torch.empty(max(256, size), dtype=torch.uint8, device=scores.device)
     st = lib().bz_bias_softmax_backward(*form, _packed(stats, (*scores.shape[:3], 2), torch.float32, "stats"),
                                         _shaped(dprobs, scores.shape, scores.dtype, "dprobs"), _strides(dprobs, "dprobs"), p_ds, s_ds,
-                                        _packed(dtable, table.shape, torch.float32, "dtable"), workspace.data_ptr(), workspace.numel(),
+                                        _packed(dtable, table.shape, torch.float32, "dtable"), *_room(workspace),
                                         _stream())
     if st:
         _check(st, "bz_bias_softmax_backward")

@@ -64,3 +64,27 @@ def test_it_learns(byzantine):
     losses = ws.train(20, byzantine, eta=2.0, same_bits=True)
     assert losses[-1] < 0.97 * losses[0]
     assert sum(losses[-5:]) < sum(losses[:5])
+
+
+def test_workspaces_are_checked():
+    """A workspace in host memory is refused before any launch; one of another type counts by its bytes."""
+    x, w = torch.randn(40, 9, device="cuda").to(torch.bfloat16), torch.randn(6, 9, device="cuda").to(torch.bfloat16)
+    dh, preact = torch.randn(40, 6, device="cuda").to(torch.bfloat16), torch.empty(2, 40, 6, device="cuda")
+    scores, table = torch.randn(1, 2, 3, 8, device="cuda"), torch.randn(32, 2, device="cuda")
+    _, stats = bz.bias_softmax(scores, table)
+    h = bz.glu(x, w, w, preact=preact)
+    calls = [(lambda ws: bz.glu(x, w, w, workspace=ws), bz.glu_workspace_bytes(40, 6, 9)),
+             (lambda ws: bz.glu_backward(x, w, w, preact, dh, workspace=ws), bz.glu_workspace_bytes(40, 6, 9, backward=True)),
+             (lambda ws: bz.bias_softmax_backward(scores, table, stats, scores, workspace=ws), bz.lib().bz_bias_softmax_workspace_bytes(1, 2, 3, 8, 32)),
+             (lambda ws: bz.pairdist(scores.view(6, 8), workspace=ws), bz.workspace_bytes(bz.OP_PAIRDIST, 0, 6, 8))]
+    for call, size in calls:
+        n0 = bz.kernel_launch_count()
+        with pytest.raises(TypeError, match="workspace"):
+            call(torch.empty(size, dtype=torch.uint8))
+        with pytest.raises(TypeError, match="workspace"):
+            call(torch.empty(2 * size, dtype=torch.uint8, device="cuda")[::2])
+        with pytest.raises(bz.BzError):
+            call(torch.empty(max(size - 256, 1) // 4, device="cuda"))
+        assert bz.kernel_launch_count() == n0
+        call(torch.empty((size + 3) // 4, device="cuda"))
+    assert torch.equal(bz.glu(x, w, w, workspace=torch.empty(4096, device="cuda")), h)
