@@ -567,7 +567,7 @@ size_t bz_glu_workspace_bytes(int64_t m, int64_t n, int64_t k, int dtype, int ba
  *   stats   device binary32 [b][h][tq][2] for the backward call, or NULL: the row's largest z (-inf for an
  *           empty row) and the sum of exp(z - that) (0).  Kept apart, since their logarithmic sum would lose
  *           the last digits where z is large.
- * b, h <= 65535, tq, tk < 2^31; any of them 0 is a successful no-op.
+ * b, h <= 65535, tq, tk < 2^31; any of them 0 is a successful no-op (tk == 0 writes no stats either).
  */
 #define BZ_MAX_DISTANCE 2048
 int bz_bias_softmax(const void* scores, const int64_t* strides_scores, int dtype, int64_t b, int64_t h, int64_t tq, int64_t tk,

@@ -8,6 +8,7 @@ Device arrays are torch CUDA tensors (torch is used for allocation and streams o
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import numpy as np
@@ -817,6 +818,8 @@ def bias_softmax(scores: torch.Tensor, table: torch.Tensor, max_distance: int = 
     st = lib().bz_bias_softmax(*form, p_probs, s_probs, p_stats, _stream())
     if st:
         _check(st, "bz_bias_softmax")
+    if not scores.shape[3]:      # no keys at all: the library has nothing to do, and every row is an empty one
+        stats[..., 0], stats[..., 1] = -math.inf, 0.0
     return probs, stats
 
 

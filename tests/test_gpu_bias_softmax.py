@@ -278,3 +278,12 @@ def test_distances_next_to_a_bound_just_above_them(both, buckets, distance, at):
     table = torch.randn(buckets, 2, generator=torch.Generator().manual_seed(at)).cuda()
     check_forward(scores, table, distance, both, q_start=[at + 1])
     check_backward(scores, table, distance, both, q_start=[at + 1], dprobs=make(*shape, torch.float32, seed=1 + at, sigma=1.0))
+
+
+def test_no_keys_at_all():
+    table = torch.randn(32, 2, device="cuda")
+    for given in (None, torch.full((1, 2, 3, 2), 5.0, device="cuda")):
+        probs, stats = bz.bias_softmax(torch.empty(1, 2, 3, 0, device="cuda"), table, stats=given)
+        assert probs.shape == (1, 2, 3, 0) and (stats[..., 0] == -math.inf).all() and (stats[..., 1] == 0).all()
+    ds, dt = bz.bias_softmax_backward(torch.empty(1, 2, 3, 0, device="cuda"), table, stats, torch.empty(1, 2, 3, 0, device="cuda"))
+    assert ds.shape == (1, 2, 3, 0) and (dt == 0).all()
