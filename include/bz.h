@@ -602,7 +602,8 @@ size_t bz_bias_softmax_workspace_bytes(int64_t b, int64_t h, int64_t tq, int64_t
  * vocabulary): q is 0 there, and a kept entry that names such a c makes the loss +inf; in a position whose
  * logits are all -inf every q counts as 0.
  *   logits  device [m][v] with ld, dtype BZ_F32, _F16, _BF16;  teacher device binary32 [m][t], index device
- *           int32 [m][t], both contiguous, 1 <= t <= BZ_MAX_TOP;  temperature > 0, finite.
+ *           int32 [m][t], both contiguous, 1 <= t <= BZ_MAX_TOP;  temperature > 0, finite, and so is log2(e) / temperature
+ *           (from 4.3e-39 on).
  *   loss    device binary32 [m];  stats  device binary32 [m][2]: the row's largest logit and the sum of
  *           exp((logits - that) / T), for the backward call; either may be NULL.
  *   dloss   device binary32 [m], the upstream gradient of each position's loss, or NULL: all 1.

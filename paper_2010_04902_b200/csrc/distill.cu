@@ -620,7 +620,7 @@ template <typename T> int dispatch(const DistillArgs& a, int64_t m, const void* 
 int check(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const float* teacher, const int32_t* index, int t,
           float temperature, const void* dlogits, int64_t ld_d) {
     const int bytes = element_bytes(dtype);
-    if (bytes == 0 || m < 0 || v < 0 || t < 1 || !(temperature > 0.f) || temperature > 3.4e38f) return BZ_ERR_INVALID_ARG;
+    if (bytes == 0 || m < 0 || v < 0 || t < 1 || !(temperature > 0.f) || isinf(temperature) || isinf(kLog2e / temperature)) return BZ_ERR_INVALID_ARG;
     if (v >= (int64_t(1) << 31) || t > BZ_MAX_TOP) return BZ_ERR_UNSUPPORTED;
     if (m == 0) return BZ_OK;
     if (teacher == nullptr || index == nullptr) return BZ_ERR_INVALID_ARG;

@@ -222,3 +222,18 @@ def test_ring_gives_the_same_bits_over_many_calls(dtype, v, grad):
         again = bz.distill(logits, teacher, index, 2.0, **how)
         differs += (again[0] != loss).any() | (again[1] != stats).any()
     assert int(differs) == 0
+
+
+@pytest.mark.parametrize("T", [5e-39, 1e-30, 1e-3])
+def test_smallest_temperatures(T):
+    """q is all on the largest logit; the teacher names it alone, or another one."""
+    logits = torch.randn(2, 50, generator=torch.Generator().manual_seed(1)).cuda()
+    top = logits.argmax(1).to(torch.int32)
+    loss, _, d = bz.distill(logits, torch.zeros(2, 1, device="cuda"), top[:, None].contiguous(), T, dloss=torch.ones(2, device="cuda"))
+    assert (loss == 0).all() and (d == 0).all()
+    other = ((top + 1) % 50).to(torch.int32)
+    _, _, d = bz.distill(logits, torch.zeros(2, 1, device="cuda"), other[:, None].contiguous(), T, dloss=torch.ones(2, device="cuda"))
+    want = torch.zeros(2, 50)     # set on the host: an addition on the GPU by atomics would flush the smallest T
+    for i in range(2):
+        want[i, int(top[i])], want[i, int(other[i])] = T, -T
+    assert torch.equal(d.cpu(), want)

@@ -203,3 +203,16 @@ def test_tensors_that_require_a_gradient():
             call()
         with torch.no_grad(), pytest.raises(TypeError):
             call()
+
+
+def test_distill_temperatures_without_an_inverse(L):
+    """Below 4.3e-39 logits / T cannot be formed in binary32: every loss would be NaN."""
+    S1 = (F, 10, bz.F16, 4, 10, F, F, 3)
+    n0 = bz.kernel_launch_count()
+    for T in (1e-39, 4.2e-39, 2.0 ** -149):
+        assert L.bz_distill(*S1, T, None, F, F, F, 10, None) == bz.ERR_INVALID_ARG
+        assert L.bz_distill_backward(*S1, T, F, None, F, 10, None) == bz.ERR_INVALID_ARG
+    for T in (4.3e-39, 3.4028235e38):     # past this check: the loss and its gradient have nowhere to go
+        assert L.bz_distill(*S1, T, None, None, None, None, 10, None) == bz.ERR_INVALID_ARG
+        assert L.bz_distill(F, 9, bz.F16, 0, 10, F, F, 3, T, None, F, F, F, 10, None) == bz.OK
+    assert bz.kernel_launch_count() == n0
