@@ -458,9 +458,11 @@ int bz_stream_probe(const void* buf, size_t bytes, int staged, uint64_t* checksu
 /*
  * Testing aid for the recovery described at bz_pairdist: while `on` is not 0, the loader threads of
  * the tensor-core distance kernels (given rows and vote in front) issue no loads, so that every
- * CTA's first bounded wait runs out after about a second and the call takes its repair path.
+ * CTA's first bounded wait runs out after about a second and the call takes its repair path.  In the
+ * tensor-core kernels of bz_glu and its gradient one CTA of each pair stops loading after two blocks of the
+ * contraction (on == 2: the pair's second CTA, otherwise its first), and the outputs are incomplete.
  * Nothing faults or hangs.  Off when the library is loaded; a per-device switch (the current
- * device's is set); not for production use.  Synchronous.
+ * device's is set; bz_glu's is the process's); not for production use.  Synchronous.
  */
 int bz_debug_stall_pipeline(int on);
 

@@ -162,9 +162,9 @@ def pairdist_status(workspace: torch.Tensor, f: int) -> int:
     return int(st.value)
 
 
-def debug_stall_pipeline(on: bool) -> None:
-    """Testing aid: make the tensor-core distance kernels' bounded waits run out (see bz.h)."""
-    _check(lib().bz_debug_stall_pipeline(1 if on else 0), "bz_debug_stall_pipeline")
+def debug_stall_pipeline(on: int) -> None:
+    """Testing aid: make the bounded waits of the tensor-core kernels (distances, gated block) run out (see bz.h)."""
+    _check(lib().bz_debug_stall_pipeline(int(on)), "bz_debug_stall_pipeline")
 
 
 def _check(status: int, what: str):

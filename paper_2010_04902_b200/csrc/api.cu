@@ -18,6 +18,7 @@ int pairdist_i8_timeouts(unsigned int* count);    // pairdist_i8.cu
 int pairdist_i8_stall(int on);
 int probe_timeouts(unsigned int* count);          // probe.cu
 int glu_timeouts(unsigned int* count);            // glu.cu
+void glu_stall(int on);
 int distill_timeouts(unsigned int* count);        // distill.cu
 int* pairdist_status_words(void* ws, int f);      // pairdist.cu
 
@@ -270,7 +271,10 @@ extern "C" int bz_pairdist_status(const void* workspace, int f, int32_t* status,
     return BZ_OK;
 }
 
-extern "C" int bz_debug_stall_pipeline(int on) { return pairdist_i8_stall(on); }
+extern "C" int bz_debug_stall_pipeline(int on) {
+    glu_stall(on);
+    return pairdist_i8_stall(on);
+}
 
 extern "C" int bz_last_path(void) { return g_last_path; }
 

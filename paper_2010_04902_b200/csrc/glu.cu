@@ -8,6 +8,8 @@ namespace bz {
 
 namespace {
 
+std::atomic<int> g_glu_stall{0};   // bz_debug_stall_pipeline
+
 constexpr int kClusters = kNumSMs / 2;
 constexpr size_t kPartialBytes = static_cast<size_t>(2 * kClusters) * kRowTile * 256 * sizeof(float);  // see plan_backward()
 
@@ -242,6 +244,7 @@ int forward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t
     }
     const Operand ox = place_operand(x, ld_x, m, k, ws), og = place_operand(wg, ld_w, n, k, ws), ou = place_operand(wu, ld_w, n, k, ws);
     ProductParams p{};
+    p.stall = g_glu_stall.load(std::memory_order_relaxed);
     ProductPart& o = p.part[0];
     o.rows = m, o.cols = n, o.blocks = ceil_div(k, kBlockK);
     const int bn = plan_forward(m, n, o.blocks);
@@ -283,6 +286,7 @@ int backward(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_
     float* partial = reinterpret_cast<float*>(ws + round_up(static_cast<size_t>(4) * m * ld, 256));
     char* room = reinterpret_cast<char*>(partial) + kPartialBytes;
     ProductParams p{};
+    p.stall = g_glu_stall.load(std::memory_order_relaxed);
     ProductMaps maps;
     Operand og{}, ou{}, ox{};
     if (dx != nullptr) {
@@ -339,6 +343,8 @@ int check(const void* x, int64_t ld_x, const void* wg, const void* wu, int64_t l
 }
 
 }  // namespace
+
+void glu_stall(int on) { g_glu_stall.store(on == 2 ? 2 : on != 0, std::memory_order_relaxed); }
 
 int glu_timeouts(unsigned int* count) {
     const cudaError_t e = cudaMemcpyFromSymbol(count, g_glu_timeouts, sizeof(unsigned int));

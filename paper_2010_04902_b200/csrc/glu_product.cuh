@@ -22,8 +22,9 @@
 // fewer of them than clusters; each share then leaves binary32 sums in the workspace and a last kernel adds the shares in
 // order.
 //
-// Every wait is bounded: a thread whose wait runs out sets its CTA's `dead` word, all roles leave their loops, the leader
-// waits (bounded again) for the loads in flight, and both CTAs meet at the cluster barrier before tensor memory is freed.
+// Every wait is bounded: a thread whose wait runs out sets its CTA's
+// `dead` word, all roles leave their loops, and both CTAs wait (bounded again) for the MMAs and the loads in flight, which
+// use either one's shared memory, before tensor memory is freed (drain()).
 #pragma once
 
 #include "umma_pair.cuh"
@@ -37,6 +38,7 @@ enum GluProduct { kForward, kBackward };
 enum GluKind { kInput, kWeight };
 
 constexpr int kRowTile = 256, kBlockK = 64, kEpilogueWarps = 8, kProductThreads = 128 + 32 * kEpilogueWarps;
+constexpr uint32_t kStallBlocks = 2;
 
 // One result: h, or dx, or both weights' gradients.
 struct ProductPart {
@@ -56,6 +58,7 @@ struct ProductParams {
     ProductPart part[2];         // kForward: the first; kBackward: by GluKind
     int weight_first;            // the order of the two in the list of tiles: longer contractions first
     int act;
+    int stall;                   // 1 + the rank whose loads stop after kStallBlocks, for tests of expired waits; 0: none
     float* preact;               // kForward: [2][rows][cols] or null
     int preact_wide, preact_pairs;
 };
@@ -116,7 +119,7 @@ __device__ __forceinline__ void turn_out(const float* turn, E* out, int64_t ld, 
 template <int BN> struct ProductShape {
     static constexpr int kABytes = 128 * kBlockK * 2, kBBytes = BN / 2 * kBlockK * 2, kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = BN == 256 ? 5 : (BN == 128 ? 7 : 9);
-    static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpilogueWarps * kTurnBytes + (2 * kStages + 4) * 8 + 16;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpilogueWarps * kTurnBytes + (2 * kStages + 5) * 8 + 16;
 };
 
 // ---- activations --------------------------------------------------------------------------------
@@ -177,6 +180,37 @@ template <GluProduct P> __device__ __forceinline__ ProductTile tile_at(const Pro
     return t;
 }
 
+// Up to an eighth of a second.
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity) {
+    volatile int expired = 0;   // mbar_wait_live() tells through it; nobody else does
+    mbar_wait_live(bar, parity, &expired, 2000, 1u << 16);
+}
+// After an expired wait, by both CTAs: waits for all MMAs and loads issued.  The loads of a block report to the leader's
+// barrier, which expects both CTAs' bytes from when the leader issued its own; a CTA that stopped earlier than the other leaves
+// some of the last blocks half announced or half loaded, which the leader makes up for.  `blocks`: room for both CTAs'
+// counts; `drained`: a barrier of one arrival, not used before.
+template <typename S>
+__device__ __forceinline__ void drain(uint32_t rank, uint32_t issued, volatile uint32_t* blocks, uint64_t* full, uint64_t* drained) {
+    if (threadIdx.x == 0) store_cluster(const_cast<uint32_t*>(blocks + rank), 0, issued);
+    __syncwarp();
+    cluster_sync();
+    if (threadIdx.x == 32) {   // the thread that issued the MMAs
+        if (rank == 0) mma_commit_pair(drained);
+        drain_wait(drained, 0);
+    }
+    if (threadIdx.x == 0 && rank == 0) {
+        const uint32_t own = blocks[0], other = blocks[1], most = max(own, other);
+        for (uint32_t j = most > S::kStages ? most - S::kStages : 0; j < most; ++j) {
+            uint64_t* bar = &full[j % S::kStages];
+            if (j >= own) mbar_expect_tx(bar, S::kStageBytes);
+            if (j >= other) mbar_complete_tx(bar, S::kStageBytes);
+            drain_wait(bar, j / S::kStages & 1);
+        }
+    }
+    __syncwarp();
+    cluster_sync();
+}
+
 template <typename T, GluProduct P, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     glu_product_kernel(const __grid_constant__ ProductMaps maps, const __grid_constant__ ProductParams p) {
@@ -190,8 +224,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     uint64_t* empty = full + S::kStages;
     uint64_t* acc_full = empty + S::kStages;   // [2]
     uint64_t* acc_empty = acc_full + 2;        // [2], the leader's are used
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+    uint64_t* drained = acc_empty + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
     volatile int* dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    uint32_t* blocks_issued = tmem_slot + 2;   // [2]
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -201,6 +237,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
         for (int s = 0; s < 2; ++s) mbar_init(&acc_full[s], 1), mbar_init(&acc_empty[s], 2 * kEpilogueWarps);
+        mbar_init(drained, 1);
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -211,7 +248,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
     RingAt<S::kStages> at;          // of the loads (thread 0), of the MMAs (the issuing thread)
-    int filled = 0;                 // stages that have been loaded at least once (thread 0)
+    uint32_t issued = 0;            // blocks loaded (thread 0)
 
     if (warp == 0 && lane == 0) {
         // ---------------------------------------------------------------- loads
@@ -225,14 +262,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
             const int weight_half = t.row >= half_tiles, weight_x = static_cast<int>((t.row - weight_half * half_tiles) * 256 + rank * 128);
             for (int kb = static_cast<int>(t.from); kb < static_cast<int>(t.to); ++kb, at.next()) {
                 const int s = at.stage;
-                if (filled == S::kStages) {
+                if (issued >= S::kStages) {
                     if (!mbar_wait_live(&empty[s], at.parity ^ 1, dead)) {
                         alive = false;
                         break;
                     }
-                } else {
-                    ++filled;
+                } else if (issued == kStallBlocks && p.stall == static_cast<int>(rank) + 1) {
+                    alive = false;
+                    break;
                 }
+                ++issued;
                 const uint32_t bar = leader_full + s * 8;
                 if (rank == 0) mbar_expect_tx(&full[s], 2 * S::kStageBytes);
                 const uint32_t a = smem_addr + s * S::kStageBytes, b = a + S::kABytes;
@@ -390,12 +429,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
     __syncthreads();
     if (threadIdx.x == 0 && *dead) {
         atomicAdd(&g_glu_timeouts, 1u);
-        if (rank == 0)  // shared memory has to outlive the loads in flight, the other CTA's among them
-            for (int j = 0; j < filled; ++j, at.next()) mbar_wait(&full[filled < S::kStages ? j : at.stage], filled < S::kStages ? 0 : at.parity ^ 1);
+        store_cluster(const_cast<int*>(dead), rank ^ 1, 1);
     }
+    __syncwarp();
     tc_fence_before_sync();
     cluster_sync();
     tc_fence_after_sync();
+    if (*dead) drain<S>(rank, issued, blocks_issued, full, drained);   // both CTAs or neither: each one's is the other's too
     if (warp == 2) tmem_dealloc_pair(tmem, 512);
 }
 
