@@ -22,7 +22,8 @@
 // fewer of them than clusters; each share then leaves binary32 sums in the workspace and a last kernel adds the shares in
 // order.
 //
-// Every wait is bounded: a thread whose wait runs out sets its CTA's
+// Every wait is bounded (about a second; the epilogue's wait for a tile by two microseconds more for each block of its
+// contraction): a thread whose wait runs out sets its CTA's
 // `dead` word, all roles leave their loops, and both CTAs wait (bounded again) for the MMAs and the loads in flight, which
 // use either one's shared memory, before tensor memory is freed (drain()).
 #pragma once
@@ -38,7 +39,7 @@ enum GluProduct { kForward, kBackward };
 enum GluKind { kInput, kWeight };
 
 constexpr int kRowTile = 256, kBlockK = 64, kEpilogueWarps = 8, kProductThreads = 128 + 32 * kEpilogueWarps;
-constexpr uint32_t kStallBlocks = 2;
+constexpr uint32_t kWaitProbes = 1u << 19, kStallBlocks = 2;   // probes of two microseconds at most
 
 // One result: h, or dx, or both weights' gradients.
 struct ProductPart {
@@ -341,7 +342,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
             const ProductTile t = tile_at<P>(p, i);
             const ProductPart& o = p.part[t.kind];
             const int acc = static_cast<int>(n & 1);
-            if (!__all_sync(~0u, mbar_wait_live(&acc_full[acc], static_cast<uint32_t>(n >> 1) & 1, dead))) break;  // a warp leaves as one
+            if (!__all_sync(~0u, mbar_wait_live(&acc_full[acc], static_cast<uint32_t>(n >> 1) & 1, dead, 2000, kWaitProbes + static_cast<uint32_t>(t.to - t.from)))) break;  // a warp leaves as one
             tc_fence_after_sync();
             const uint32_t base = tmem + acc * 256 + (static_cast<uint32_t>(quarter * 32) << 16);
             const int in_tile = static_cast<int>(rank) * 128 + quarter * 32;   // first row of this warp

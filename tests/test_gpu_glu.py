@@ -288,3 +288,17 @@ def test_gelu_far_below_zero(m):
     assert ((h[:, 0].double() - want).abs() <= near * want.abs()).all()
     assert ((dx[:, 1].double() - want).abs() <= near * want.abs()).all()
     assert ((dx[:, 0].double() - slope).abs() <= 2.0 ** -8 * slope.abs() + 2e-5 * (phi + (G * density).abs())).all()
+
+
+def test_longest_contraction():
+    """One tile whose contraction alone takes longer than a second (2^28 elements, 19 GB): nothing may run out meanwhile."""
+    m, n, k = 33, 1, 1 << 28
+    x = torch.zeros(m, k, dtype=torch.bfloat16, device="cuda")
+    wg, wu = torch.zeros(n, k, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, k, dtype=torch.bfloat16, device="cuda")
+    for at, (a, b) in {0: (1.0, 3.0), 12345677: (2.0, 5.0), k - 1: (4.0, 7.0)}.items():
+        x[:, at] = torch.arange(m, device="cuda") + 1
+        wg[:, at], wu[:, at] = a, b
+    preact = torch.empty(2, m, n, device="cuda")
+    h = bz.glu(x, wg, wu, "relu", preact=preact)
+    row = (torch.arange(m, device="cuda") + 1).float()[:, None]
+    assert torch.equal(preact, torch.stack([7 * row, 15 * row])) and torch.equal(h, (105 * row * row).to(torch.bfloat16))
