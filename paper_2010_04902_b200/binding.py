@@ -684,17 +684,6 @@ def _act(name: str) -> int:
         raise ValueError("act must be one of %s" % ", ".join(sorted(_ACTS))) from None
 
 
-def _like_matrix(t: torch.Tensor) -> torch.Tensor:
-    """A new tensor of t's shape whose rows are as far apart as t's: the kernels' wide loads and stores need rows that
-    sit alike relative to 16-byte boundaries."""
-    if t.is_contiguous():
-        return torch.empty_like(t)
-    n, ld = t.shape[-1], t.stride(-2)
-    if t.shape[-2] <= 1 or ld <= n or ld > 2 * n:
-        return t.new_empty(t.shape)
-    return t.new_empty(t.shape[:-1] + (ld,))[..., :n]
-
-
 def _glu_operands(x, w_gate, w_up):
     m, k, ld_x = _matrix(x, "x")
     n, k2, ld_w = _matrix(w_gate, "w_gate")

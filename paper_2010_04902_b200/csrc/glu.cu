@@ -214,9 +214,10 @@ template <typename T, int NT> int launch_few(const FewParams& p, bool wide, cuda
         note_launch();
         return check_launch();
     }
+    static_assert(kFewStreamRows == 9, "wide operands of more than one group of eight rows take the ring");
     const unsigned grid = static_cast<unsigned>(ceil_div(p.n, kFewUnits));
-    if (wide)
-        glu_few_kernel<T, NT, true><<<grid, 32 * kFewWarps, 0, s>>>(p);
+    if (NT == 1 && wide)
+        glu_few_kernel<T, NT, NT == 1><<<grid, 32 * kFewWarps, 0, s>>>(p);
     else
         glu_few_kernel<T, NT, false><<<grid, 32 * kFewWarps, 0, s>>>(p);
     note_launch();

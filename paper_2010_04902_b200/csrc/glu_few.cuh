@@ -1,7 +1,7 @@
 // Gated feed-forward block for few rows (tokens): bound by reading both weights once.
 //
 // A CTA takes eight hidden units; its eight warps take 32-wide steps of k in turn, so the units' weights stream through
-// registers by 16-byte loads that a quad of lanes makes contiguous (64 bytes of each of 8 rows at a time, four or eight steps in
+// registers by 16-byte loads that a quad of lanes makes contiguous (64 bytes of each of 8 rows at a time, four steps in
 // flight).  The products run on mma.sync (m16n8k16: the eight gate rows above the eight up rows, times 8 tokens), so one
 // thread ends with g and u of its unit: at one to 32 tokens the arithmetic is far below either tensor path's rate, and this
 // one takes its operands from the registers the loads end in.  The order of k inside an MMA is free as long as weights and
@@ -65,10 +65,11 @@ __device__ __forceinline__ float few_gate(int which, float g) {
     }
 }
 
-// NT: groups of eight tokens.
+// NT: groups of eight tokens.  WIDE: whole steps by 16-byte loads (up to eight rows; more take the ring below).
 template <typename T, int NT, bool WIDE>
 __global__ void __launch_bounds__(32 * kFewWarps) glu_few_kernel(const __grid_constant__ FewParams p) {
-    constexpr int kUnroll = NT == 1 ? 4 : 8;   // 24 tokens, 5461 units of 2048: 14.8 us against 16.9 with four
+    static_assert(!WIDE || NT == 1, "no call takes it");
+    constexpr int kUnroll = 4;   // steps in flight
     __shared__ float part[kFewWarps][2][kFewUnits][8 * NT + 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int64_t unit = static_cast<int64_t>(blockIdx.x) * kFewUnits;
