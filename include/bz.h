@@ -502,7 +502,9 @@ uint64_t bz_kernel_launch_count(void);
  * statistics and losses are binary32; a result is rounded once, to its own type, when it is stored.
  * Any base alignment and leading dimension that the element type allows is accepted; rows whose addresses
  * are equal modulo 16 in every tensor of a call (for bz_glu: bases and leading dimensions that are
- * multiples of 16 bytes) take the wide loads, the others a slower path with the same results.
+ * multiples of 16 bytes) take the wide loads, the others a slower path.  The two add in different orders, so
+ * their results agree within rounding only: workers whose copies of a gradient are to be voted on lay their
+ * tensors out alike.
  */
 #define BZ_F32 0
 #define BZ_F16 1
@@ -535,6 +537,9 @@ int bz_glu(const void* x, int64_t ld_x, const void* w_gate, const void* w_up, in
  * Its gradient, with preact as bz_glu left it: dg = dh * u * act'(g) and du = dh * act(g), rounded to
  * dtype (the operands of the products below are 16-bit), then
  *   dx = dg w_gate + du w_up,   dw_gate = dg^T x,   dw_up = du^T x.
+ * The rounding of dg and du makes the gradients' error about 1.4 times that of one rounding at the end.  In
+ * binary16 dg and du beyond 65 504 become infinite and those below 2^-24 vanish, where 32 bits would keep them:
+ * scale dh accordingly.
  *   dh device [m][n] with ld_dh;  dx device [m][k] with ld_dx, or NULL;  dw_gate, dw_up device [n][k], both
  *   with ld_dw, or both NULL.  grad_dtype is the type of dw_gate and dw_up: dtype, or BZ_F32 to keep the
  *   32-bit sums - then they may lie in a binary32 gradient row as the aggregation calls read it.

@@ -2,10 +2,11 @@
 //
 // Forward: z = scale*s + bias[bucket(j - p)], P = e^(z - M) / S.  One read of the scores, one write of P: bound by memory
 // (8 x 16 x 1024 x 1024 bfloat16 in 87 us, 94 % of the copy's rate; causal 2 x 16 x 4096 x 4096 in 380, bound by issue).
-// A row lies in the registers of G threads (a warp up to 1024 keys, a CTA of 128 or 512 beyond; 32 elements each), the
-// next row's loads are on their way while this one is worked on, and a warp takes its exponentials relative to its own
-// maximum, so that one exchange of (maximum, sum) pairs a row is all that a CTA's warps need.  Rows beyond 16 384 keys
-// are read twice.
+// A row lies in the registers of G threads (a warp, then 64 to 512 threads; 32 16-bit elements each, 16 of binary32 or where
+// rows are taken element by element), the next row's loads are on their way while this one is worked on, and a warp takes
+// its exponentials relative to its own maximum, so that one exchange of (maximum, sum) pairs a row is all that a CTA's
+// warps need.  Rows of more than 16 384 keys (8192 at 16 elements a thread; the gradient's kernels, up to 256 threads: 8192
+// and 4096) are read twice.
 // The bias depends on j - p alone and is constant from max_distance on, so a CTA keeps the head's values for the
 // 2*max_distance + 1 distances in shared memory, in copies that make a slot's values whole words (struct Window).
 //

@@ -3,7 +3,7 @@
 // q = softmax(s/T) runs over the whole vocabulary, the teacher's p over t entries.  Loss and gradient need the same
 // maximum and sum of a row, so the fused call reads the row once, keeps its exponentials in registers (32 elements a
 // thread) and writes the gradient from there: two transfers a logit (4096 x 32128 bfloat16 in 130 us, 62 % of the copy's rate;
-// the loss alone of 2048 x 100003 binary16 in 86 us, 73 %: the exponentials' unit is at 51 and 58 %).  A row that one CTA cannot hold
+// the loss alone of 2048 x 100003 binary16 in 87 us, 72 %: the exponentials' unit is at 51 and 58 %).  A row that one CTA cannot hold
 // is split over a cluster of up to eight; the CTAs exchange their (maximum, sum) pair through distributed shared
 // memory, one barrier a row.  Beyond that (more than 131 072 logits) the cluster reads the row twice.
 // The t entries: one warp forms p while the row's loads are in flight; after the dense part dlogits = dloss*T*q is

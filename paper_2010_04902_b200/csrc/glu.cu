@@ -196,7 +196,7 @@ bool pair_rows(const void* p, int64_t ld, int64_t rows, int bytes) { return rein
 bool wide_rows(const void* p, int64_t ld, int64_t rows, int bytes) { return aligned16(p) && (rows <= 1 || ld * bytes % 16 == 0); }
 
 // The ring pays from nine rows on, and for eight and fewer from 16 MB of weights on (out of memory, ring against registers:
-// 24 rows, 512 x 2048 4.7 against 5.7 us; one row, 1024 x 2816 7.1 against 5.9; one row, 2048 x 5461 14.2 against 17.6;
+// 24 rows, 512 x 2048 4.9 against 5.7 us; one row, 1024 x 2816 7.1 against 5.9; one row, 2048 x 5461 14.2 against 17.6;
 // one row, 4096 x 10922 42 against 53; 32 rows of that 70 against 90: there the rows' own traffic out of the L2 is the bound).
 constexpr int64_t kFewStreamRows = 9, kFewStreamBytes = int64_t(16) << 20;
 

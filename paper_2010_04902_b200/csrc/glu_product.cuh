@@ -13,14 +13,15 @@
 // MMA reads the block across rows.  For the forward product CTA 0 brings gate columns and CTA 1 up columns of the same
 // BN/2 hidden units, so g and u of a unit meet in one thread of the epilogue and h = act(g)*u leaves without another pass.
 // Accumulators: two sets of BN tensor-memory columns in turn, so a tile's epilogue runs under the next tile's MMAs.
-// (Tiles of 512 columns over both sets, one ahead of the other, were tried: 842 us against 725 below.)
+// (Tiles of 512 columns over both sets, one ahead of the other, were tried: 842 us against 725 at 8192 x 4096 x 8192 forward.)
 // Eight epilogue warps: two to each quarter of the lanes, steps of columns in turn.
 //
 // Persistent: at most one cluster per pair of SMs; tiles in groups of sixteen row tiles, columns inside a group in turn, so
 // that the operands of the tiles in flight stay in the L2 (8192 x 4096 x 8192 forward: 934 us with groups of four, 900
-// with eight, 880 with sixteen, sustained, before the issue loop counted its stages; 800 since: 1374 TFLOP/s).  Tiles of the backward products may be cut along the contraction when there are
-// fewer of them than clusters; each share then leaves binary32 sums in the workspace and a last kernel adds the shares in
-// order.
+// with eight, 880 with sixteen, sustained, before the issue loop counted its stages; 800 since).  8192 x 4096 x 10922
+// forward: 1127 us, 1300 TFLOP/s at the power limit.  Tiles of the backward products may be cut along the contraction when there
+// are fewer of them than clusters; each share then leaves binary32 sums in the workspace and a last kernel adds the shares
+// in order.
 //
 // Every wait is bounded (about a second; the epilogue's wait for a tile by two microseconds more for each block of its
 // contraction): a thread whose wait runs out sets its CTA's
