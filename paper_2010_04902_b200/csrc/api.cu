@@ -272,8 +272,9 @@ extern "C" int bz_pairdist_status(const void* workspace, int f, int32_t* status,
 }
 
 extern "C" int bz_debug_stall_pipeline(int on) {
-    glu_stall(on);
-    return pairdist_i8_stall(on);
+    const int st = pairdist_i8_stall(on);
+    if (st == BZ_OK) glu_stall(on);
+    return st;
 }
 
 extern "C" int bz_last_path(void) { return g_last_path; }

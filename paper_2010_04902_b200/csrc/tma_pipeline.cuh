@@ -67,29 +67,29 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// The encoder needs the device's context to be current, which it is not yet in a thread that has made no call of the
-// runtime; choosing the device that is chosen already makes it so.
+template <typename F> F driver_entry(const char* name) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint(name, &p, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess)
+        return reinterpret_cast<F>(p);
+    (void)cudaGetLastError();
+    return nullptr;
+}
+
+// The encoder needs a current context, and a thread that has made no call of the runtime has none yet: choosing the
+// device that is chosen already makes its context current.  A context that the caller has made current stays.
 inline void bind_context() {
-    static thread_local bool bound = false;
+    static const auto current = driver_entry<CUresult (*)(CUcontext*)>("cuCtxGetCurrent");
+    CUcontext context = nullptr;
     int device;
-    if (bound) return;
-    if (cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess)
-        bound = true;
-    else
-        (void)cudaGetLastError();
+    if (current == nullptr || current(&context) != CUDA_SUCCESS || context != nullptr) return;
+    if (cudaGetDevice(&device) != cudaSuccess || cudaSetDevice(device) != cudaSuccess) (void)cudaGetLastError();
 }
 
 // Looked up once; a second thread's first call waits for it.
 inline EncodeTiledFn encode_tiled() {
-    bind_context();
-    static const EncodeTiledFn fn = []() -> EncodeTiledFn {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<EncodeTiledFn>(p);
-        (void)cudaGetLastError();
-        return nullptr;
-    }();
+    static const EncodeTiledFn fn = driver_entry<EncodeTiledFn>("cuTensorMapEncodeTiled");
+    if (fn != nullptr) bind_context();
     return fn;
 }
 
