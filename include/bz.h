@@ -627,6 +627,134 @@ int bz_distill(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, 
 int bz_distill_backward(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const float* teacher, const int32_t* index,
                         int t, float temperature, const float* stats, const float* dloss, void* dlogits, int64_t ld_d, void* stream);
 
+/*
+ * ---- Fine-tuning losses --------------------------------------------------------------------------
+ * Both losses below look at one token a position: with z = logits / T and a = index, the token's log-probability is
+ *   lp = z[a] - log(sum over c of exp z[c]).
+ * A position whose index lies outside [0, v) has no token (a prompt's or a padded one): its lp, loss and gradient are 0, and
+ * its logits count for nothing (they may be NaN).  Logits may be -inf (a masked vocabulary); a token whose own logit is
+ * -inf has lp = -inf and takes no gradient.  Row scalars (lp, ratios, sums over a sequence) are formed in binary64
+ * from a binary32 maximum and sum, and rounded once when they are stored.
+ *   logits   device [m][v] with ld, dtype BZ_F32, _F16, _BF16;  index device int32 [m];  temperature > 0, finite, and so is
+ *            log2(e) / temperature.
+ *   logp     device binary32 [m], or NULL: receives lp.
+ *   stats    device binary32 [m][4], 16-byte aligned, for the backward call: the row's largest logit, the sum of
+ *            exp((logits - that) / T), the slope d loss / d lp, and (an int32's bits) the place of the row's upstream gradient
+ *            in dloss.
+ *   dlogits  device [m][v] with ld_d, dtype's elements, or NULL: the loss alone.  It may be logits itself (ld_d == ld).
+ *            dlogits[c] = dloss * slope / T * ([c == a] - softmax(z)[c]).
+ * v < 2^31; m == 0 is a successful no-op; v == 0 counts as rows without a token.
+ */
+
+/*
+ * Clipped policy loss with a KL term, a position at a time:
+ *   r = exp(lp - old_logp),   d = ref_logp - lp,
+ *   loss = -min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A) + kl (exp(d) - d - 1).
+ * Where the clipped product is the smaller one the policy term has no slope; at the border itself it has the unclipped one.
+ * A = 0 has no policy term, kl = 0 no KL term, whatever the ratios.
+ *   old_logp   device binary32 [m], or NULL: lp itself (r = 1, on policy; the slope is still -A).
+ *   ref_logp   device binary32 [m]; may be NULL if kl == 0.
+ *   advantage  device binary32 [m];  clip_low in [0, 1], clip_high >= 0 (may be infinite: no clip);  kl >= 0, finite.
+ *   dloss      device binary32 [m], or NULL: all 1.   loss device binary32 [m], or NULL.   stats may be NULL.
+ * With dlogits the logits are read once for loss and gradient together.
+ */
+int bz_policy(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const int32_t* index, const float* old_logp,
+              const float* ref_logp, const float* advantage, float temperature, float clip_low, float clip_high, float kl,
+              const float* dloss, float* loss, float* logp, float* stats, void* dlogits, int64_t ld_d, void* stream);
+
+/*
+ * Paired preference loss.  Sequence n is rows starts[n] .. starts[n + 1] - 1; sequences 0 .. pairs - 1 are the chosen
+ * answers, pairs .. 2 pairs - 1 the rejected ones.
+ *   reward[n] = beta * sum over the sequence's tokens of (lp - ref_logp)     (mean != 0: their mean; no token: 0)
+ *   h = reward[p] - reward[pairs + p] - margin,
+ *   loss[p] = -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h).
+ * Rows of no sequence (before the first, behind the last) get lp, but slope and gradient 0.
+ *   starts     device int32 [2 pairs + 1], not decreasing; values are taken into [0, m].  A sequence may be empty.
+ *   ref_logp   device binary32 [m], or NULL: no reference (0).
+ *   beta finite, smoothing in [0, 1], margin finite.   pairs up to 2^30 - 1; 0 means that no row is of a sequence.
+ *   loss       device binary32 [pairs], or NULL;  reward device binary32 [2 pairs], or NULL;  stats must be given.
+ *   dloss      device binary32 [pairs], or NULL: all 1.
+ * A row's slope depends on the whole pair, so the logits are read again for the gradient, the last rows first: what the L2 still
+ * holds of them is not read from memory again.
+ */
+int bz_preference(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const int32_t* index, const float* ref_logp,
+                  const int32_t* starts, int64_t pairs, float temperature, float beta, float margin, float smoothing, int mean,
+                  const float* dloss, float* loss, float* reward, float* logp, float* stats, void* dlogits, int64_t ld_d,
+                  void* stream);
+
+/* The gradient alone of either loss, with stats as bz_policy or bz_preference left them, for a dloss that is known only after
+ * the loss: [m] for the first, [pairs] for the second, or NULL: all 1.  dlogits may be logits itself. */
+int bz_token_loss_backward(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const int32_t* index, float temperature,
+                           const float* stats, const float* dloss, void* dlogits, int64_t ld_d, void* stream);
+
+/*
+ * ---- Dropout -------------------------------------------------------------------------------------
+ * The mask is a function of a seed, an offset and the element's number, and never stored: the r workers that hold a file
+ * drop the same elements, and the backward pass is the same call on the gradient.
+ * Element e = i n + j of an [m][n] tensor (its place in row-major order, whatever the strides) has the 16 random bits
+ * number e mod 8 (the lowest first) of the 128 bits that Philox4x32-10 (Salmon et al., 2011) makes of the counter
+ * (floor(e / 8), offset), two 64-bit halves, lower word first, under the key seed.  With t = rate * 65536 rounded to a whole number,
+ * an element stays if its bits are at least t: the rate is t / 65536, and what stays is multiplied by 65536 / (65536 - t)
+ * (rounded to binary32).  What is dropped becomes 0, whatever it was.
+ */
+
+/*
+ *   x, out  device [m][n] with ld_x, ld_out, dtype BZ_F32, _F16, _BF16; out may be x itself (ld_out == ld_x).
+ *   rng     device uint64 [2], 8-byte aligned: seed, offset.  Read by the kernel, so a captured call takes new ones at each replay.
+ *   rate    in [0, 1), and so is its rounded value: up to 65535.5 / 65536.
+ * m, n < 2^40, m * n < 2^50; either 0 is a successful no-op.
+ */
+int bz_dropout(const void* x, int64_t ld_x, int dtype, int64_t m, int64_t n, double rate, const uint64_t* rng, void* out,
+               int64_t ld_out, void* stream);
+
+/*
+ * ---- Joining a block to its residual stream ------------------------------------------------------
+ * From the residual stream x and a block's output y to the new stream s and the next block's input z, row by row:
+ *   a = norm(y) * w_post                      (w_post NULL: a = y)
+ *   s = residual_scale * x + branch_scale * gate * drop(a)
+ *   z = norm(s) * w_pre                       (w_pre NULL: no z)
+ * norm is BZ_NORM_RMS: v / sqrt(mean of v^2 + eps), or BZ_NORM_LAYER: the same of v less its mean.  Statistics are taken of
+ * binary32 values, those of z from s before it is rounded.  drop is bz_dropout of the [m][n] tensor.
+ *   x, y, s, z  device [m][n] with ld_x, ld_y, ld_s, ld_z, one dtype: BZ_F32, _F16, _BF16.  y may be NULL: no branch (w_post and
+ *           gate NULL, rate 0), z = norm(residual_scale * x), the norm alone.  s or z may be NULL.  s may be x itself, z may be y (equal
+ *           leading dimensions).
+ *   w_post, w_pre  device binary32 [n], or NULL.
+ *   gate    device binary32 [groups][n], or NULL (1 everywhere; groups 0): rows i m/groups .. (i + 1) m/groups - 1 take
+ *           gate row i; m is a multiple of groups.  One group: a gate for each channel; m groups: for each element.
+ *   rate, rng   as in bz_dropout; rate 0 needs no rng.
+ *   stats   device binary32 [m][4], 16-byte aligned, for the backward call, or NULL: mean and 1 / deviation of the norm of y, then of s
+ *           (0 and 1 where there is no norm; RMS has mean 0). eps = 0 makes a row of zeros (for
+ *           LAYER: a constant one) NaN.
+ * n <= BZ_MAX_WIDTH; m < 2^31; either 0 is a successful no-op.  eps >= 0, scales finite.
+ */
+#define BZ_NORM_RMS 0
+#define BZ_NORM_LAYER 1
+#define BZ_MAX_WIDTH 16384
+int bz_join(const void* x, int64_t ld_x, const void* y, int64_t ld_y, int dtype, int64_t m, int64_t n, int norm, float eps,
+            const float* w_post, const float* gate, int64_t groups, float residual_scale, float branch_scale, double rate,
+            const uint64_t* rng, const float* w_pre, void* s, int64_t ld_s, void* z, int64_t ld_z, float* stats, void* stream);
+
+/*
+ * Its gradient, from the stream's ds (NULL: 0) and the next block's dz (NULL: 0), with x, y and stats as bz_join had and left
+ * them; s is formed anew, in binary32 (x is read where there are dz and w_pre only).  A forward call that wrote s over x or z over y
+ * has no backward call.
+ *   g = ds + the norm's gradient of dz * w_pre at s,   dx = residual_scale * g,
+ *   u = branch_scale * drop'(g),  dgate = sum over a group's rows of u * a,   dy = the norm's gradient of u * gate * w_post at y,
+ *   dw_post = sum over rows of u * gate * norm(y),   dw_pre = sum over rows of dz * norm(s).
+ *   dx, dy  device [m][n] with ld_dx, ld_dy, or NULL.  Each may be x, y, ds or dz itself (equal leading dimensions).
+ *   dw_post, dgate, dw_pre  device binary32 [n], [groups][n], [n], overwritten, or NULL.
+ *   workspace  device, bz_join_workspace_bytes(m, n, groups) bytes, 256-byte aligned (needed with dw_post, dgate or dw_pre only).
+ * m == 0 writes dw_post = dw_pre = 0 (dgate has no rows then, or one: 0).
+ */
+int bz_join_backward(const void* x, int64_t ld_x, const void* y, int64_t ld_y, int dtype, int64_t m, int64_t n, int norm,
+                     const float* w_post, const float* gate, int64_t groups, float residual_scale, float branch_scale, double rate,
+                     const uint64_t* rng, const float* w_pre, const float* stats, const void* ds, int64_t ld_ds, const void* dz,
+                     int64_t ld_dz, void* dx, int64_t ld_dx, void* dy, int64_t ld_dy, float* dw_post, float* dgate, float* dw_pre,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* 0 for sizes that the call refuses. */
+size_t bz_join_workspace_bytes(int64_t m, int64_t n, int64_t groups);
+
 #ifdef __cplusplus
 }
 #endif

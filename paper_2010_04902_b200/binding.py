@@ -25,6 +25,8 @@ STATUS_RECOMPUTED, STATUS_STOPPED_EARLY = 1, 2
 F32, F16, BF16 = 0, 1, 2
 ACT_SILU, ACT_GELU_TANH, ACT_GELU, ACT_RELU = range(4)
 MAX_DISTANCE, MAX_TOP = 2048, 1024
+NORM_RMS, NORM_LAYER = 0, 1
+MAX_WIDTH = 16384
 GLU_FEW = 32                # up to so many rows bz_glu needs no workspace
 PATH_NONE, PATH_STAGED, PATH_REGISTERS, PATH_GENERIC, PATH_TENSOR, PATH_FP32, PATH_FP32_FUSED, PATH_FP64 = range(8)
 
@@ -41,7 +43,7 @@ class BzError(RuntimeError):
 _lib = None
 
 _c_int, _c_i64, _c_sz, _c_vp, _c_u64 = ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_uint64
-_c_f = ctypes.c_float
+_c_f, _c_d = ctypes.c_float, ctypes.c_double
 
 _SIGNATURES = {
     "bz_assign_mols": (_c_int, [_c_int, _c_int, _c_vp, _c_vp, _c_vp]),
@@ -97,6 +99,18 @@ _SIGNATURES = {
     "bz_bias_softmax_workspace_bytes": (_c_sz, [_c_i64, _c_i64, _c_i64, _c_i64, _c_int]),
     "bz_distill": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_vp, _c_int, _c_f, _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]),
     "bz_distill_backward": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_vp, _c_int, _c_f, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]),
+    "bz_policy": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_vp, _c_vp, _c_vp, _c_f, _c_f, _c_f, _c_f, _c_vp, _c_vp, _c_vp, _c_vp,
+                           _c_vp, _c_i64, _c_vp]),
+    "bz_preference": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_vp, _c_vp, _c_i64, _c_f, _c_f, _c_f, _c_f, _c_int, _c_vp, _c_vp,
+                               _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]),
+    "bz_token_loss_backward": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_f, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]),
+    "bz_dropout": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_d, _c_vp, _c_vp, _c_i64, _c_vp]),
+    "bz_join": (_c_int, [_c_vp, _c_i64, _c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_int, _c_f, _c_vp, _c_vp, _c_i64, _c_f, _c_f, _c_d, _c_vp, _c_vp,
+                         _c_vp, _c_i64, _c_vp, _c_i64, _c_vp, _c_vp]),
+    "bz_join_backward": (_c_int, [_c_vp, _c_i64, _c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_int, _c_vp, _c_vp, _c_i64, _c_f, _c_f, _c_d, _c_vp,
+                                  _c_vp, _c_vp, _c_vp, _c_i64, _c_vp, _c_i64, _c_vp, _c_i64, _c_vp, _c_i64, _c_vp, _c_vp, _c_vp, _c_vp, _c_sz,
+                                  _c_vp]),
+    "bz_join_workspace_bytes": (_c_sz, [_c_i64, _c_i64, _c_i64]),
 }
 
 EXPORTS = sorted(_SIGNATURES)
@@ -885,3 +899,245 @@ def distill_backward(logits: torch.Tensor, teacher: torch.Tensor, index: torch.T
     if st:
         _check(st, "bz_distill_backward")
     return dlogits
+
+
+# ------------------------------------------------------------------------- losses on one token a position
+
+def _here(t: torch.Tensor, name: str):
+    """The calls below launch on the current device's current stream: their tensors have to live there."""
+    if t.is_cuda and t.device.index != torch._C._cuda_getDevice():
+        raise ValueError("%s is on %s, the current device is cuda:%d: call under torch.cuda.device(%s.device)"
+                         % (name, t.device, torch._C._cuda_getDevice(), name))
+
+
+def _token_operands(logits, index, dloss, dlogits):
+    """(m, v, arguments from logits to index, whether a gradient is wanted, dlogits, its address and leading dimension)."""
+    m, v, ld = _matrix(logits, "logits")
+    head = (logits.data_ptr(), ld, _dtype(logits, "logits"), m, v, _packed(index, (m,), torch.int32, "index"))
+    _here(logits, "logits")
+    if dlogits is None:
+        if dloss is None:
+            return m, v, head, False, None, None, 0
+        dlogits = _like_rows(logits)
+        return m, v, head, True, dlogits, dlogits.data_ptr(), dlogits.stride(0) if m > 1 else v
+    return m, v, head, True, dlogits, _shaped(dlogits, (m, v), logits.dtype, "dlogits"), _matrix(dlogits, "dlogits")[2]
+
+
+def _made(t, like, shape, name):
+    """(tensor, address) of a binary32 output; a new one if t is None."""
+    if t is None:
+        t = torch.empty(shape, dtype=torch.float32, device=like.device)
+        return t, t.data_ptr()
+    return t, _packed(t, shape, torch.float32, name)
+
+
+def policy(logits: torch.Tensor, index: torch.Tensor, advantage: torch.Tensor, old_logp: torch.Tensor | None = None,
+           ref_logp: torch.Tensor | None = None, kl: float = 0.0, clip_low: float = 0.2, clip_high: float = 0.2, temperature: float = 1.0,
+           dloss: torch.Tensor | None = None, loss: torch.Tensor | None = None, logp: torch.Tensor | None = None,
+           stats: torch.Tensor | None = None, dlogits: torch.Tensor | None = None):
+    """bz_policy: the clipped policy loss of each position, with a KL term.  Returns (loss, logp, stats); with `dloss`
+    (float32 [m]) or `dlogits` given also the gradient, from the same pass: (loss, logp, stats, dlogits)."""
+    if logits.requires_grad:
+        _unrecorded("policy", logits=logits)
+    m, v, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
+    loss, p_loss = _made(loss, logits, (m,), "loss")
+    logp, p_logp = _made(logp, logits, (m,), "logp")
+    stats, p_stats = _made(stats, logits, (m, 4), "stats")
+    st = lib().bz_policy(*head, _packed(old_logp, (m,), torch.float32, "old_logp"), _packed(ref_logp, (m,), torch.float32, "ref_logp"),
+                         _packed(advantage, (m,), torch.float32, "advantage"), temperature, clip_low, clip_high, kl,
+                         _packed(dloss, (m,), torch.float32, "dloss"), p_loss, p_logp, p_stats, p_d, ld_d, _stream())
+    if st:
+        _check(st, "bz_policy")
+    return (loss, logp, stats, dlogits) if grad else (loss, logp, stats)
+
+
+def preference(logits: torch.Tensor, index: torch.Tensor, starts: torch.Tensor, ref_logp: torch.Tensor | None = None, beta: float = 0.1,
+               margin: float = 0.0, smoothing: float = 0.0, mean: bool = False, temperature: float = 1.0,
+               dloss: torch.Tensor | None = None, loss: torch.Tensor | None = None, reward: torch.Tensor | None = None,
+               logp: torch.Tensor | None = None, stats: torch.Tensor | None = None, dlogits: torch.Tensor | None = None):
+    """bz_preference: the paired preference loss of the sequences that `starts` (int32 [2 pairs + 1]) cuts the rows into, chosen
+    ones first.  Returns (loss, reward, logp, stats); with `dloss` (float32 [pairs]) or `dlogits` given also the gradient:
+    (loss, reward, logp, stats, dlogits)."""
+    if logits.requires_grad:
+        _unrecorded("preference", logits=logits)
+    m, v, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
+    if starts.dim() != 1 or starts.shape[0] % 2 != 1:
+        raise ValueError("starts must be [2 pairs + 1]")
+    pairs = starts.shape[0] // 2
+    loss, p_loss = _made(loss, logits, (pairs,), "loss")
+    reward, p_reward = _made(reward, logits, (2 * pairs,), "reward")
+    logp, p_logp = _made(logp, logits, (m,), "logp")
+    stats, p_stats = _made(stats, logits, (m, 4), "stats")
+    st = lib().bz_preference(*head, _packed(ref_logp, (m,), torch.float32, "ref_logp"), _packed(starts, starts.shape, torch.int32, "starts"), pairs,
+                             temperature, beta, margin, smoothing, 1 if mean else 0, _packed(dloss, (pairs,), torch.float32, "dloss"), p_loss, p_reward,
+                             p_logp, p_stats, p_d, ld_d, _stream())
+    if st:
+        _check(st, "bz_preference")
+    return (loss, reward, logp, stats, dlogits) if grad else (loss, reward, logp, stats)
+
+
+def token_loss_backward(logits: torch.Tensor, index: torch.Tensor, stats: torch.Tensor, dloss: torch.Tensor | None = None,
+                        temperature: float = 1.0, dlogits: torch.Tensor | None = None) -> torch.Tensor:
+    """bz_token_loss_backward: the gradient alone, with stats as policy() or preference() returned them; dloss as there."""
+    if dlogits is None:
+        dlogits = _like_rows(logits)
+    m, v, head, _, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
+    if dloss is not None and dloss.dim() != 1:
+        raise ValueError("dloss must be [m] or [pairs]")
+    st = lib().bz_token_loss_backward(*head, temperature, _packed(stats, (m, 4), torch.float32, "stats"),
+                                      None if dloss is None else _packed(dloss, dloss.shape, torch.float32, "dloss"), p_d, ld_d, _stream())
+    if st:
+        _check(st, "bz_token_loss_backward")
+    return dlogits
+
+
+# ------------------------------------------------------------------------- dropout, joins of blocks
+
+def _collapsed(t: torch.Tensor, name: str):
+    """(m, n, ld): the tensor as rows of one distance, in row-major order."""
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    dims = []      # from the last to the first: [size, stride]
+    for size, stride in zip(reversed(t.shape), reversed(t.stride())):
+        if size == 1:
+            continue
+        if dims and stride == dims[-1][0] * dims[-1][1]:
+            dims[-1][0] *= size
+        else:
+            dims.append([size, stride])
+    if dims[0][1] != 1:
+        dims.insert(0, [1, 1])
+    if len(dims) > 2 or (len(dims) == 2 and dims[1][1] < dims[0][0]):
+        raise ValueError("%s must be rows of unit stride, one distance apart: make it contiguous" % name)
+    (n, _), (m, ld) = dims if len(dims) == 2 else (dims[0], (1, dims[0][0]))
+    return m, n, ld
+
+
+def dropout(x: torch.Tensor, rate: float, rng: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
+    """bz_dropout: x with the elements dropped that seed and offset in `rng` (int64 [2] on the device) name, the others scaled.  The
+    gradient is the same call on the gradient.  `out` may be x itself."""
+    if x.requires_grad:
+        if torch.is_grad_enabled():
+            raise ValueError("dropout: x requires a gradient, which this call does not record: call it under torch.no_grad() (or inside an "
+                             "autograd.Function), and again on the gradient")
+    dt = _dtype(x, "x")
+    _here(x, "x")
+    m, n, ld = _collapsed(x, "x")
+    if out is None:
+        out = torch.empty_like(x) if m == 1 else x.new_empty(m, ld).as_strided(x.shape, x.stride()) if ld <= 2 * n else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if out.shape != x.shape or out.dtype != x.dtype or not out.is_cuda:
+        raise ValueError("out must be a CUDA tensor like x")
+    m2, n2, ld2 = _collapsed(out, "out")
+    if m == 1 and m2 > 1:
+        m, n, ld = m2, n2, n2
+    elif m2 == 1:
+        m2, n2, ld2 = m, n, n
+    if n2 != n:
+        raise ValueError("x and out must be cut into rows alike: make one of them contiguous")
+    st = lib().bz_dropout(x.data_ptr(), ld, dt, m, n, rate, _packed(rng, (2,), torch.int64, "rng"), out.data_ptr(), ld2, _stream())
+    if st:
+        _check(st, "bz_dropout")
+    return out
+
+
+_NORMS = {"rms": NORM_RMS, "layer": NORM_LAYER}
+
+
+def _norm(name: str) -> int:
+    try:
+        return _NORMS[name]
+    except KeyError:
+        raise ValueError("norm must be rms or layer") from None
+
+
+def _join_form(n, w_post, gate, w_pre, rate, rng):
+    """Addresses of w_post, gate, its rows, rng, w_pre."""
+    if gate is not None and (gate.dim() != 2 or gate.shape[1] != n):
+        raise ValueError("gate must be [groups][%d]" % n)
+    return (_packed(w_post, (n,), torch.float32, "w_post"), None if gate is None else _packed(gate, gate.shape, torch.float32, "gate"),
+            0 if gate is None else gate.shape[0], _packed(rng, (2,), torch.int64, "rng"), _packed(w_pre, (n,), torch.float32, "w_pre"))
+
+
+def _row_tensor(t, like, name):
+    """(address, leading dimension) of a matrix shaped like `like`, or of None."""
+    if t is None:
+        return None, 0
+    return _shaped(t, like.shape, like.dtype, name), _matrix(t, name)[2]
+
+
+def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+         w_pre: torch.Tensor | None = None, norm: str = "rms", eps: float = 1e-6, residual_scale: float = 1.0, branch_scale: float = 1.0,
+         rate: float = 0.0, rng: torch.Tensor | None = None, s: torch.Tensor | None = None, z: torch.Tensor | None = None,
+         stats: torch.Tensor | None = None):
+    """bz_join: s = residual_scale x + branch_scale gate drop(norm(y) w_post), z = norm(s) w_pre, for rows x, y [m][n] and weights
+    float32 [n], gate float32 [groups][n].  Returns (s, z, stats); z is None without w_pre.  Without y: the norm alone, and s is
+    written only if it is given (or residual_scale is not 1; otherwise the s that comes back is x)."""
+    if x.requires_grad or (y is not None and y.requires_grad):
+        _unrecorded("join", x=x, y=y if y is not None else x)
+    for name, w in (("w_post", w_post), ("gate", gate), ("w_pre", w_pre)):
+        if w is not None and w.requires_grad:
+            _unrecorded("join", **{name: w})
+    m, n, ld_x = _matrix(x, "x")
+    dt = _dtype(x, "x")
+    _here(x, "x")
+    p_post, p_gate, groups, p_rng, p_pre = _join_form(n, w_post, gate, w_pre, rate, rng)
+    p_y, ld_y = _row_tensor(y, x, "y")
+    keep = s is None and y is None and residual_scale == 1.0 and w_pre is not None
+    if s is None and not keep:
+        s = _like_rows(x)
+    p_s, ld_s = _row_tensor(s, x, "s")
+    if z is None and w_pre is not None:
+        z = _like_rows(x)
+    p_z, ld_z = _row_tensor(z, x, "z")
+    stats, p_stats = _made(stats, x, (m, 4), "stats")
+    st = lib().bz_join(x.data_ptr(), ld_x, p_y, ld_y, dt, m, n, _norm(norm), eps, p_post, p_gate, groups, residual_scale, branch_scale, rate, p_rng,
+                       p_pre, p_s, ld_s, p_z, ld_z, p_stats, _stream())
+    if st:
+        _check(st, "bz_join")
+    return x if keep else s, z, stats
+
+
+def join_workspace_bytes(m: int, n: int, groups: int = 0) -> int:
+    return int(lib().bz_join_workspace_bytes(m, n, groups))
+
+
+def join_backward(x: torch.Tensor, y: torch.Tensor | None, stats: torch.Tensor, ds: torch.Tensor | None = None,
+                  dz: torch.Tensor | None = None, w_post: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                  w_pre: torch.Tensor | None = None, norm: str = "rms", residual_scale: float = 1.0, branch_scale: float = 1.0,
+                  rate: float = 0.0, rng: torch.Tensor | None = None, dx: torch.Tensor | None = None, dy: torch.Tensor | None = None,
+                  dw_post: torch.Tensor | None = None, dgate: torch.Tensor | None = None, dw_pre: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None):
+    """bz_join_backward, with x, y and stats as join() had and returned them: returns (dx, dy, dw_post, dgate, dw_pre), None for what the call has no operand of.  dw_post, dgate and
+    dw_pre may be views of a gradient row."""
+    m, n, ld = _matrix(x, "x")
+    dt = _dtype(x, "x")
+    _here(x, "x")
+    p_post, p_gate, groups, p_rng, p_pre = _join_form(n, w_post, gate, w_pre, rate, rng)
+    p_y, ld_y = _row_tensor(y, x, "y")
+    p_ds, ld_ds = _row_tensor(ds, x, "ds")
+    p_dz, ld_dz = _row_tensor(dz, x, "dz")
+    if dx is None:
+        dx = _like_rows(x)
+    p_dx, ld_dx = _row_tensor(dx, x, "dx")
+    if dy is None and y is not None:
+        dy = _like_rows(y)
+    p_dy, ld_dy = _row_tensor(dy, x, "dy")
+    p_dpost = p_dgate = p_dpre = None
+    if w_post is not None:
+        dw_post, p_dpost = _made(dw_post, x, (n,), "dw_post")
+    if gate is not None:
+        dgate, p_dgate = _made(dgate, x, gate.shape, "dgate")
+    if w_pre is not None:
+        dw_pre, p_dpre = _made(dw_pre, x, (n,), "dw_pre")
+    room = (None, 0)
+    if workspace is not None:
+        room = _room(workspace)
+    elif w_post is not None or gate is not None or w_pre is not None:
+        workspace = torch.empty(max(256, lib().bz_join_workspace_bytes(m, n, groups)), dtype=torch.uint8, device=x.device)
+        room = workspace.data_ptr(), workspace.numel()
+    st = lib().bz_join_backward(x.data_ptr(), ld, p_y, ld_y, dt, m, n, _norm(norm), p_post, p_gate, groups, residual_scale, branch_scale, rate, p_rng,
+                                p_pre, _packed(stats, (m, 4), torch.float32, "stats"), p_ds, ld_ds, p_dz, ld_dz, p_dx, ld_dx, p_dy, ld_dy,
+                                p_dpost, p_dgate, p_dpre, *room, _stream())
+    if st:
+        _check(st, "bz_join_backward")
+    return dx, dy, dw_post, dgate, dw_pre

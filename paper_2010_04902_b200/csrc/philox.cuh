@@ -1,0 +1,50 @@
+// Random bits by counter: Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3, SC 2011).
+#pragma once
+
+#include <stdint.h>
+
+namespace bz {
+
+// Ten rounds, as the paper's default: 20 wide products and 40 logic operations for eight elements' bits.
+__device__ __forceinline__ uint4 philox(uint4 c, uint32_t k0, uint32_t k1) {
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p = static_cast<uint64_t>(c.x) * 0xD2511F53u, q = static_cast<uint64_t>(c.z) * 0xCD9E8D57u;
+        c = make_uint4(static_cast<uint32_t>(q >> 32) ^ c.y ^ k0, static_cast<uint32_t>(q), static_cast<uint32_t>(p >> 32) ^ c.w ^ k1, static_cast<uint32_t>(p));
+        k0 += 0x9E3779B9u, k1 += 0xBB67AE85u;
+    }
+    return c;
+}
+
+// Which elements stay, 16 bits an element.
+struct Dropout {
+    const uint64_t* rng;   // seed, offset
+    uint32_t least;        // an element stays if its bits are at least this
+    float scale;           // of what stays
+};
+struct Keep {
+    uint32_t k0, k1, o0, o1, least;
+    __device__ __forceinline__ explicit Keep(const Dropout& d) : least(d.least) {
+        uint64_t seed = 0, offset = 0;
+        if (d.rng != nullptr) seed = d.rng[0], offset = d.rng[1];
+        k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32), o0 = static_cast<uint32_t>(offset), o1 = static_cast<uint32_t>(offset >> 32);
+    }
+    // bit i: element 8 * group + i stays
+    __device__ __forceinline__ uint32_t group(uint64_t number) const {
+        const uint4 w = philox(make_uint4(static_cast<uint32_t>(number), static_cast<uint32_t>(number >> 32), o0, o1), k0, k1);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        uint32_t bits = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits |= ((u[i] & 0xffffu) >= least ? 1u << (2 * i) : 0u) | ((u[i] >> 16) >= least ? 2u << (2 * i) : 0u);
+        return bits;
+    }
+    // bit i, i < N <= 8: element first + i stays
+    template <int N> __device__ __forceinline__ uint32_t elements(uint64_t first) const {
+        const int at = static_cast<int>(first & 7);
+        uint32_t bits = group(first >> 3) >> at;
+        if (at + N > 8) bits |= group((first >> 3) + 1) << (8 - at);
+        return bits & ((1u << N) - 1u);
+    }
+};
+
+}  // namespace bz
