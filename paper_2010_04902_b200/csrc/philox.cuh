@@ -29,14 +29,31 @@ struct Keep {
         if (d.rng != nullptr) seed = d.rng[0], offset = d.rng[1];
         k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32), o0 = static_cast<uint32_t>(offset), o1 = static_cast<uint32_t>(offset >> 32);
     }
-    // bit i: element 8 * group + i stays
+    // the 128 bits of elements 8 * number ... 8 * number + 7
+    __device__ __forceinline__ uint4 words(uint64_t number) const {
+        return philox(make_uint4(static_cast<uint32_t>(number), static_cast<uint32_t>(number >> 32), o0, o1), k0, k1);
+    }
+    // whether the element of the lower, the upper 16 bits of a word stays
+    __device__ __forceinline__ bool lower(uint32_t w) const { return w << 16 >= least << 16; }
+    __device__ __forceinline__ bool upper(uint32_t w) const { return w >= least << 16; }
+    // bit i: element 8 * number + i stays
     __device__ __forceinline__ uint32_t group(uint64_t number) const {
-        const uint4 w = philox(make_uint4(static_cast<uint32_t>(number), static_cast<uint32_t>(number >> 32), o0, o1), k0, k1);
+        const uint4 w = words(number);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
         uint32_t bits = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) bits |= ((u[i] & 0xffffu) >= least ? 1u << (2 * i) : 0u) | ((u[i] >> 16) >= least ? 2u << (2 * i) : 0u);
+        for (int i = 0; i < 4; ++i) bits |= (lower(u[i]) ? 1u << (2 * i) : 0u) | (upper(u[i]) ? 2u << (2 * i) : 0u);
         return bits;
+    }
+    // x[i] = element 8 * number + i, scaled or 0
+    __device__ __forceinline__ void apply(uint64_t number, float scale, float (&x)[8]) const {
+        const uint4 w = words(number);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = lower(u[i]) ? x[2 * i] * scale : 0.f;
+            x[2 * i + 1] = upper(u[i]) ? x[2 * i + 1] * scale : 0.f;
+        }
     }
     // bit i, i < N <= 8: element first + i stays
     template <int N> __device__ __forceinline__ uint32_t elements(uint64_t first) const {
