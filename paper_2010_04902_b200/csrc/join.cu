@@ -1,5 +1,20 @@
 // The join of a block to its residual stream: norm of the block's output, gate, dropout, residual scale, norm for the next
 // block - and its gradient.
+//
+// With h = norm(y) (h = y without that norm), w = scale * gate * w_post by column (scale: the branch's times dropout's) and [.] the mask:
+//   s = residual * x + [h w],  z = norm(s) w_pre;
+//   g = ds + norm'(dz w_pre),  dx = residual * g,  e = [g] w,  dy = norm'(e),
+//   P = sum over a group's rows of [g] h:  dgate = scale * w_post * P,  dw_post = sum over the groups of scale * gate * P,
+//   dw_pre = sum over rows of dz norm(s).
+// One read of x, y and one write of s, z forward; one read of x, y, ds, dz and one write of dx, dy backward.
+//
+// A thread owns the same columns of every row: COLS of them, in 16-byte words where every tensor's rows begin on 16-byte
+// boundaries, else single elements a CTA's width apart.  So what belongs to a column (w and w_pre in shared memory, the column sums in
+// registers) needs no exchange.  A CTA of up to 512 threads holds a row, a cluster of two or four a wider one; the row's
+// sums cost one barrier each.  The next row's words come by cp.async while a row is worked on: a thread copies what it reads
+// itself, and waits for nobody.
+#include <cooperative_groups.h>
+
 #include <cmath>
 
 #include "dropout_rule.h"
@@ -10,8 +25,10 @@ namespace bz {
 
 namespace {
 
-constexpr int kWide = 1024;                       // threads of the kernels for any width
-constexpr int kWideColumns = BZ_MAX_WIDTH / kWide;
+namespace cg = cooperative_groups;
+
+constexpr int kTeam = 512;       // threads of a CTA at most
+constexpr int kMostRanks = 4;    // CTAs of a cluster
 
 struct JoinArgs {
     int64_t m;
@@ -19,7 +36,7 @@ struct JoinArgs {
     float eps;
     const float *w_post, *gate, *w_pre;
     int64_t group_rows;          // rows that share a gate row
-    float residual, scale;       // of the branch: its own times dropout's
+    float residual, scale;       // scale of the branch: its own times dropout's
     int drop;                    // whether there is dropout
     Dropout dropout;
     float4* stats;
@@ -30,559 +47,486 @@ template <typename T> struct JoinRows {
     __device__ __forceinline__ T* row(int64_t i) const { return p + i * ld; }
 };
 
-// Sum over the CTA; every thread gets it.
-__device__ __forceinline__ float cta_sum(float v, float* part) {
-    v = warp_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    return warp_sum(lane < (blockDim.x >> 5) ? part[lane] : 0.f);
+// ---- pairs of elements ---------------------------------------------------------------------------
+
+__device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
+template <typename T> __device__ __forceinline__ float2 word_pair(const uint4& w, int k) {   // elements 2k, 2k + 1 of a word
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    if constexpr (sizeof(T) == 4)
+        return make_float2(__uint_as_float(u[2 * k]), __uint_as_float(u[2 * k + 1]));
+    else
+        return unpack2(T(), u[k]);
 }
 
-// Mean and 1 / deviation of a row held in `value(column)`.
-template <typename F> __device__ __forceinline__ float2 row_norm(const JoinArgs& a, float* part, F value) {
-    float mean = 0.f, sum = 0.f;
-    if (a.layer) {
-        for (int c = threadIdx.x; c < a.n; c += blockDim.x) sum += value(c);
-        mean = cta_sum(sum, part) / static_cast<float>(a.n);
-        sum = 0.f;
-    }
-    for (int c = threadIdx.x; c < a.n; c += blockDim.x) {
-        const float d = value(c) - mean;
-        sum = fmaf(d, d, sum);
-    }
-    return {mean, 1.f / sqrtf(cta_sum(sum, part) / static_cast<float>(a.n) + a.eps)};
-}
-
-// One CTA a row, any width; the row of s in shared memory.
-template <typename T> __global__ void __launch_bounds__(kWide) join_wide_kernel(const __grid_constant__ JoinArgs a, JoinRows<const T> x, JoinRows<const T> y, JoinRows<T> s, JoinRows<T> z) {
-    extern __shared__ float held[];
-    __shared__ float part[32];
-    const Keep keep(a.dropout);
-    for (int64_t i = blockIdx.x; i < a.m; i += gridDim.x) {
-        const T* in = x.row(i);
-        const T* block = y.p != nullptr ? y.row(i) : nullptr;
-        const float* gate = a.gate != nullptr ? a.gate + i / a.group_rows * a.n : nullptr;
-        float2 post = make_float2(0.f, 1.f), pre = make_float2(0.f, 1.f);
-        if (a.w_post != nullptr) post = row_norm(a, part, [&](int c) { return to_f32(block[c]); });
-        for (int c = threadIdx.x; c < a.n; c += kWide) {
-            float v = a.residual * to_f32(in[c]);
-            if (block != nullptr) {
-                float b = to_f32(block[c]);
-                if (a.w_post != nullptr) b = (b - post.x) * post.y * a.w_post[c];
-                const float f = gate != nullptr ? a.scale * gate[c] : a.scale;
-                if (!a.drop || keep.elements<1>(static_cast<uint64_t>(i) * a.n + c)) v = fmaf(f, b, v);
-            }
-            held[c] = v;
-        }
-        if (a.w_pre != nullptr) pre = row_norm(a, part, [&](int c) { return held[c]; });
-        for (int c = threadIdx.x; c < a.n; c += kWide) {
-            if (s.p != nullptr) s.row(i)[c] = from_f32<T>(held[c]);
-            if (z.p != nullptr) z.row(i)[c] = from_f32<T>((held[c] - pre.x) * pre.y * a.w_pre[c]);
-        }
-        if (a.stats != nullptr && threadIdx.x == 0) a.stats[i] = make_float4(post.x, post.y, pre.x, pre.y);
-    }
-}
-
-// ---- rows of up to 8192 columns ------------------------------------------------------------------
-//
-// A thread owns the same columns of every row, SL slots of VEC (a 16-byte word where every tensor's rows begin on 16-byte boundaries, else
-// single elements), so what belongs to a column - weights in shared memory, column sums in registers - needs no exchange.  The next
-// row's words come by cp.async while a row is worked on; each thread copies what it reads itself, and waits for nobody.
-
-constexpr int kTeam = 512;   // threads of a CTA at most
-
-// Two rows of NT tensors in shared memory, or (VEC = 1) one row in registers.
-template <typename T, int VEC, int SL, int NT> struct Staged {
-    uint4* room;
-    __device__ __forceinline__ explicit Staged(void* smem) : room(static_cast<uint4*>(smem) + threadIdx.x) {}
-    __device__ __forceinline__ void fetch(int t, int which, const T* row, int n) {
-#pragma unroll
-        for (int q = 0; q < SL; ++q) {
-            const int c = (q * blockDim.x + threadIdx.x) * VEC;
-            const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(room + ((which * NT + t) * SL + q) * blockDim.x));
-            const int left = (n - c) * static_cast<int>(sizeof(T)), bytes = left < 16 ? left : 16;
-            if (left > 0) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row + c), "r"(bytes) : "memory");
-        }
-    }
-    __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-    __device__ __forceinline__ static void arrived() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }   // all but the last group
-    __device__ __forceinline__ void get(int t, int which, int q, float (&x)[VEC]) const { Word<T>::unpack(room[((which * NT + t) * SL + q) * blockDim.x], x); }
+// Where a thread's columns lie: element e of COLS.
+template <int VEC> struct Columns {
+    int first;   // of the CTA
+    __device__ __forceinline__ int of(int e) const { return first + (e / VEC * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * VEC + e % VEC; }
 };
-template <typename T, int SL, int NT> struct Staged<T, 1, SL, NT> {
-    float r[NT][SL];
-    __device__ __forceinline__ explicit Staged(void*) {}
-    __device__ __forceinline__ void fetch(int t, int, const T* row, int n) {
+
+// NT tensors' elements of a row, as they were loaded.  VEC > 1: the next row's are on their way to the other half of the room meanwhile; a
+// half is filled again only a whole row after it was read.
+template <typename T, int VEC, int COLS, int NT> struct Held {
+    static constexpr int kWords = COLS / VEC;
+    uint4* room;
+    int half = 0;
+    uint4 w[NT][kWords];
+    __device__ __forceinline__ explicit Held(void* smem) : room(static_cast<uint4*>(smem) + threadIdx.x) {}
+    __device__ __forceinline__ uint4* place(int which, int t, int q) const { return room + ((which * NT + t) * kWords + q) * blockDim.x; }
+    // words behind the last column are never copied, and stay zero
+    __device__ __forceinline__ void clear(int n, const Columns<VEC>& at) {
 #pragma unroll
-        for (int q = 0; q < SL; ++q) {
-            const int c = q * blockDim.x + threadIdx.x;
-            r[t][q] = c < n ? to_f32(row[c]) : 0.f;
+        for (int q = 0; q < kWords; ++q)
+            if (at.of(q * VEC) >= n) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) *place(0, t, q) = *place(1, t, q) = make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int q = 0; q < kWords; ++q) w[t][q] = make_uint4(0, 0, 0, 0);
+    }
+    // the next row's: fetches, then commit
+    __device__ __forceinline__ void fetch(int t, const T* row, int n, const Columns<VEC>& at) {
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) {
+            const int c = at.of(q * VEC);
+            const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(place(half, t, q)));
+            const int left = (n - c) * static_cast<int>(sizeof(T));   // what reaches over the row's end is filled with zeros
+            if (left > 0) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row + c), "r"(min(left, 16)) : "memory");
+        }
+    }
+    __device__ __forceinline__ void commit() {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        half ^= 1;
+    }
+    __device__ __forceinline__ static void arrived() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }   // all but the last commit
+    __device__ __forceinline__ void take(int t) {   // this row's: the half that the next commit will fill
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) w[t][q] = *place(half, t, q);
+    }
+    __device__ __forceinline__ float2 get(int t, int p) const { return word_pair<T>(w[t][p / (VEC / 2)], p % (VEC / 2)); }
+};
+template <typename T, int COLS, int NT> struct Held<T, 1, COLS, NT> {
+    float2 v[NT][COLS / 2];
+    __device__ __forceinline__ explicit Held(void*) {}
+    __device__ __forceinline__ void clear(int, const Columns<1>&) {
+#pragma unroll
+        for (int k = 0; k < NT * COLS / 2; ++k) v[k / (COLS / 2)][k % (COLS / 2)] = pair(0.f);
+    }
+    __device__ __forceinline__ void fetch(int t, const T* row, int n, const Columns<1>& at) {
+#pragma unroll
+        for (int p = 0; p < COLS / 2; ++p) {
+            const int c = at.of(2 * p), d = at.of(2 * p + 1);
+            v[t][p] = make_float2(c < n ? to_f32(row[c]) : 0.f, d < n ? to_f32(row[d]) : 0.f);
         }
     }
     __device__ __forceinline__ static void commit() {}
     __device__ __forceinline__ static void arrived() {}
-    __device__ __forceinline__ void get(int t, int, int q, float (&x)[1]) const { x[0] = r[t][q]; }
+    __device__ __forceinline__ void take(int) {}
+    __device__ __forceinline__ float2 get(int t, int p) const { return v[t][p]; }
 };
 
-// A vector of weights in shared memory, a thread's columns where only it looks.
-template <int VEC, int SL> struct Weights {
-    static constexpr int kPiece = VEC == 1 ? 1 : 4;
-    float* room;
-    __device__ __forceinline__ void load(const float* w, int n) const {
+template <typename T, int VEC, int COLS> __device__ __forceinline__ void put(T* row, int n, const Columns<VEC>& at, const float2 (&v)[COLS / 2]) {
+    if constexpr (VEC == 1) {
 #pragma unroll
-        for (int q = 0; q < SL; ++q)
+        for (int p = 0; p < COLS / 2; ++p) {
+            if (at.of(2 * p) < n) row[at.of(2 * p)] = from_f32<T>(v[p].x);
+            if (at.of(2 * p + 1) < n) row[at.of(2 * p + 1)] = from_f32<T>(v[p].y);
+        }
+    } else {
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const int c = (q * blockDim.x + threadIdx.x) * VEC + k;
-                room[((q * (VEC / kPiece) + k / kPiece) * blockDim.x + threadIdx.x) * kPiece + k % kPiece] = c < n ? __ldg(w + c) : 0.f;
-            }
-    }
-    __device__ __forceinline__ void get(int q, float (&x)[VEC]) const {
-        if constexpr (VEC == 1) {
-            x[0] = room[q * blockDim.x + threadIdx.x];
-        } else {
+        for (int q = 0; q < COLS / VEC; ++q) {
+            const int c = at.of(q * VEC);
+            float x[VEC];
 #pragma unroll
-            for (int k = 0; k < VEC / 4; ++k) {
-                const float4 w = reinterpret_cast<const float4*>(room)[(q * (VEC / 4) + k) * blockDim.x + threadIdx.x];
-                x[4 * k] = w.x, x[4 * k + 1] = w.y, x[4 * k + 2] = w.z, x[4 * k + 3] = w.w;
+            for (int k = 0; k < VEC; ++k) x[k] = k & 1 ? v[(q * VEC + k) / 2].y : v[(q * VEC + k) / 2].x;
+            if (c + VEC <= n) {
+                *reinterpret_cast<uint4*>(row + c) = Word<T>::pack(x);
+            } else if (c < n) {
+                rare();
+#pragma unroll
+                for (int k = 0; k < VEC; ++k)
+                    if (c + k < n) row[c + k] = from_f32<T>(x[k]);
             }
         }
     }
-};
-inline __host__ __device__ int weight_floats(int threads, int columns) { return threads * columns; }
+}
 
-// Sums over the CTA, one barrier each: two sets of partial sums in turn.
+// A number for each column in shared memory, where only its thread looks; 0 behind the last column.
+template <int VEC, int COLS> struct ByColumn {
+    float4* room;
+    template <typename F> __device__ __forceinline__ void set(int n, const Columns<VEC>& at, F value) const {
+#pragma unroll
+        for (int k = 0; k < COLS / 4; ++k) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = at.of(4 * k + e) < n ? value(at.of(4 * k + e)) : 0.f;
+            room[k * blockDim.x + threadIdx.x] = make_float4(x[0], x[1], x[2], x[3]);
+        }
+    }
+    __device__ __forceinline__ void get(int k, float2 (&w)[2]) const {   // pairs 2k, 2k + 1
+        const float4 f = room[k * blockDim.x + threadIdx.x];
+        w[0] = make_float2(f.x, f.y), w[1] = make_float2(f.z, f.w);
+    }
+};
+
+// Sums over the row's threads, one barrier each; two sets of partial sums in turn.
 struct Exchange {
-    float (*part)[2][16];
-    int turn = 0;
-    __device__ __forceinline__ explicit Exchange(float (*p)[2][16]) : part(p) {
-        if (threadIdx.x < 64) p[threadIdx.x / 32][threadIdx.x / 16 % 2][threadIdx.x % 16] = 0.f;
-        if (blockDim.x < 64) p[1][threadIdx.x / 16][threadIdx.x % 16] = 0.f;
-        __syncthreads();
+    struct Room {
+        float warp[2][2][16];
+        float rank[2][2][kMostRanks];
+    };
+    Room* room;
+    int ranks, turn = 0;
+    __device__ __forceinline__ Exchange(Room* r, int ranks_) : room(r), ranks(ranks_) {
+        for (int k = threadIdx.x; k < 64; k += blockDim.x) (&r->warp[0][0][0])[k] = 0.f;
+        if (ranks > 1)
+            cg::this_cluster().sync();
+        else
+            __syncthreads();
     }
     template <int K> __device__ __forceinline__ void sum(float (&v)[K]) {
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
         const int warps = blockDim.x >> 5;
-        if (warps == 1) return;
-        if ((threadIdx.x & 31) == 0) {
+        if (warps > 1) {
+            if ((threadIdx.x & 31) == 0) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) part[turn][k][threadIdx.x >> 5] = v[k];
+                for (int k = 0; k < K; ++k) room->warp[turn][k][threadIdx.x >> 5] = v[k];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                v[k] = 0.f;
+                for (int w = 0; w < warps; w += 4) {
+                    const float4 p = *reinterpret_cast<const float4*>(&room->warp[turn][k][w]);
+                    v[k] += (p.x + p.y) + (p.z + p.w);
+                }
+            }
         }
-        __syncthreads();
+        if (ranks > 1) {
+            cg::cluster_group cluster = cg::this_cluster();
+            if (threadIdx.x < ranks) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            v[k] = 0.f;
-            for (int w = 0; w < warps; w += 4) {
-                const float4 p = *reinterpret_cast<const float4*>(&part[turn][k][w]);
-                v[k] += (p.x + p.y) + (p.z + p.w);
+                for (int k = 0; k < K; ++k) cluster.map_shared_rank(room, threadIdx.x)->rank[turn][k][cluster.block_rank()] = v[k];
+            }
+            cluster.sync();
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                v[k] = 0.f;
+                for (int r = 0; r < ranks; ++r) v[k] += room->rank[turn][k][r];
             }
         }
         turn ^= 1;
     }
 };
 
-// Mean and 1 / deviation of what the CTA's threads hold.
-template <int VEC, int SL> __device__ __forceinline__ float2 held_norm(const JoinArgs& a, Exchange& ex, const float (&v)[SL][VEC], float inv_n) {
-    float mean = 0.f, t[1] = {0.f};
-    if (a.layer) {
+// The bits of a row's elements, two halves of a word a pair.  Where the thread's words are whole groups of the generator it makes
+// its own; else the CTA makes each group once and leaves the 16-bit numbers in shared memory, two rows' in turn.
+template <int VEC, int COLS> struct Mask {
+    uint16_t* room;      // [2][width + 16]
+    int width, turn = 0;
+    bool own;
+    __device__ __forceinline__ static int halves(int width) { return width + 16; }
+    __device__ __forceinline__ void make(const JoinArgs& a, const Keep& keep, int64_t i, const Columns<VEC>& at, uint32_t (&r)[COLS / 2]) {
+        const uint64_t first = static_cast<uint64_t>(i) * a.n;
+        if constexpr (VEC == 8) {
+            if (own) {
 #pragma unroll
-        for (int q = 0; q < SL; ++q)
+                for (int q = 0; q < COLS / 8; ++q) {
+                    const uint4 w = keep.words((first + at.of(q * 8)) >> 3);
+                    r[4 * q] = w.x, r[4 * q + 1] = w.y, r[4 * q + 2] = w.z, r[4 * q + 3] = w.w;
+                }
+                return;
+            }
+        }
+        const uint64_t begin = first + at.first;
+        const int lead = static_cast<int>(begin & 7), used = min(width, a.n - at.first);
+        uint16_t* to = room + turn * halves(width);
+        for (int g = threadIdx.x; g * 8 < lead + used; g += blockDim.x) reinterpret_cast<uint4*>(to)[g] = keep.words((begin >> 3) + g);
+        __syncthreads();
+        turn ^= 1;
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) t[0] += v[q][k];   // 0 behind the last column
-        ex.sum(t);
-        mean = t[0] * inv_n;
-        t[0] = 0.f;
-    }
-#pragma unroll
-    for (int q = 0; q < SL; ++q) {
-        const int c = (q * blockDim.x + threadIdx.x) * VEC;
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            const float d = c + k < a.n ? v[q][k] - mean : 0.f;
-            t[0] = fmaf(d, d, t[0]);
+        for (int p = 0; p < COLS / 2; ++p) {
+            // numbers behind the last column are whatever lies there
+            const int c = at.of(2 * p) - at.first + lead, d = at.of(2 * p + 1) - at.first + lead;
+            r[p] = static_cast<uint32_t>(to[c]) | static_cast<uint32_t>(to[d]) << 16;
         }
     }
+    __device__ __forceinline__ static float2 apply(const Keep& keep, uint32_t r, float2 v) { return make_float2(keep.lower(r) ? v.x : 0.f, keep.upper(r) ? v.y : 0.f); }
+};
+
+// Mean and 1 / deviation of what the row's threads hold.
+template <int VEC, int COLS> __device__ __forceinline__ float2 held_norm(const JoinArgs& a, Exchange& ex, const Columns<VEC>& at, const float2 (&v)[COLS / 2], float inv_n) {
+    float mean = 0.f, t[1];
+    float2 sum = pair(0.f);
+    if (a.layer) {
+#pragma unroll
+        for (int p = 0; p < COLS / 2; ++p) sum = __fadd2_rn(sum, v[p]);   // 0 behind the last column
+        t[0] = sum.x + sum.y;
+        ex.sum(t);
+        mean = t[0] * inv_n;
+        sum = pair(0.f);
+    }
+    if (mean == 0.f || at.of(COLS - 1) < a.n) {
+#pragma unroll
+        for (int p = 0; p < COLS / 2; ++p) {
+            const float2 d = __fadd2_rn(v[p], pair(-mean));
+            sum = __ffma2_rn(d, d, sum);
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < COLS / 2; ++p) {
+            const float x = at.of(2 * p) < a.n ? v[p].x - mean : 0.f, y = at.of(2 * p + 1) < a.n ? v[p].y - mean : 0.f;
+            sum.x = fmaf(x, x, sum.x), sum.y = fmaf(y, y, sum.y);
+        }
+    }
+    t[0] = sum.x + sum.y;
     ex.sum(t);
     return {mean, 1.f / sqrtf(t[0] * inv_n + a.eps)};
 }
 
-// Which of a slot's elements stay.
-template <int VEC> __device__ __forceinline__ uint32_t staying(const JoinArgs& a, const Keep& keep, int64_t i, int c) {
-    return a.drop && c < a.n ? keep.elements<VEC>(static_cast<uint64_t>(i) * a.n + c) : 0xffffffffu;
-}
-
-template <typename T, int VEC> __device__ __forceinline__ void put_slot(T* row, int c, int n, const float (&x)[VEC]) {
-    if (c + VEC <= n) {
-        store_whole<T, VEC>(row + c, x);
+// v[p] = s of the pair.
+template <int VEC, int COLS, typename In>
+__device__ __forceinline__ void joined(const JoinArgs& a, const Keep& keep, bool branch, const In& in, const float2 (&h)[COLS / 2], const uint32_t (&r)[COLS / 2], const ByColumn<VEC, COLS>& weight,
+                                       float2 (&v)[COLS / 2]) {
+    if (branch) {
+#pragma unroll
+        for (int k = 0; k < COLS / 4; ++k) {
+            float2 w[2];
+            weight.get(k, w);
+            v[2 * k] = __fmul2_rn(h[2 * k], w[0]), v[2 * k + 1] = __fmul2_rn(h[2 * k + 1], w[1]);
+        }
+        if (a.drop) {
+#pragma unroll
+            for (int p = 0; p < COLS / 2; ++p) v[p] = Mask<VEC, COLS>::apply(keep, r[p], v[p]);
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < VEC; ++k)
-            if (c + k < n) row[c + k] = from_f32<T>(x[k]);
+        for (int p = 0; p < COLS / 2; ++p) v[p] = pair(0.f);
     }
-}
-
-// s of a slot from x, the block's output (normalised if it is) and their factors.
-template <int VEC> __device__ __forceinline__ void joined(const JoinArgs& a, bool branch, uint32_t stays, const float (&w_post)[VEC], const float (&gate)[VEC], const float (&b)[VEC], float (&x)[VEC]) {
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-        x[k] *= a.residual;
-        if (branch && (stays >> k & 1)) {
-            const float v = a.w_post != nullptr ? b[k] * w_post[k] : b[k];
-            x[k] = fmaf(a.gate != nullptr ? a.scale * gate[k] : a.scale, v, x[k]);
-        }
-    }
+    for (int p = 0; p < COLS / 2; ++p) v[p] = __ffma2_rn(in.get(0, p), pair(a.residual), v[p]);
 }
 
-template <typename T, int VEC, int SL>
-__global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ JoinArgs a, JoinRows<const T> x, JoinRows<const T> y, JoinRows<T> s, JoinRows<T> z) {
-    extern __shared__ __align__(16) float smem[];
-    __shared__ __align__(16) float part[2][2][16];
-    Exchange ex(part);
-    const Keep keep(a.dropout);
-    const bool branch = y.p != nullptr, post = a.w_post != nullptr;
-    const int floats = weight_floats(blockDim.x, VEC * SL);
-    float* room = smem;
-    Weights<VEC, SL> w_post{room}, gate{room += post ? floats : 0}, w_pre{room += a.gate != nullptr ? floats : 0};
-    Staged<T, VEC, SL, 2> in(room + (a.w_pre != nullptr ? floats : 0));
+// The weight of a column of the branch.
+__device__ __forceinline__ float branch_weight(const JoinArgs& a, int64_t group, int c) {
+    const float w = a.gate != nullptr ? a.scale * a.gate[group * a.n + c] : a.scale;
+    return a.w_post != nullptr ? w * a.w_post[c] : w;
+}
+
+template <typename T, int VEC, int COLS>
+__global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ JoinArgs a, int ranks, JoinRows<const T> x, JoinRows<const T> y, JoinRows<T> s, JoinRows<T> z) {
+    extern __shared__ __align__(16) float4 smem[];
+    __shared__ __align__(16) Exchange::Room room;
+    const int width = blockDim.x * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks, teams = gridDim.x / ranks;
+    const Columns<VEC> at{rank * width};
+    const ByColumn<VEC, COLS> weight{smem}, w_pre{smem + width / 4};
+    Held<T, VEC, COLS, 2> in(smem + width / 2);
+    Mask<VEC, COLS> mask{reinterpret_cast<uint16_t*>(smem + width / 2 + (VEC > 1 ? 2 * 2 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
+    const bool branch = y.p != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr;
     const float inv_n = 1.f / static_cast<float>(a.n);
-    int64_t i = a.m * blockIdx.x / gridDim.x, group = -1;
-    const int64_t last = a.m * (blockIdx.x + 1) / gridDim.x;
-    auto fetch = [&](int64_t row, int which) {
-        if (row < last) {
-            in.fetch(0, which, x.row(row), a.n);
-            if (branch) in.fetch(1, which, y.row(row), a.n);
-        }
-        in.commit();
+    int64_t i = a.m * team / teams, change = i;   // change: the row at which the next gate row begins
+    const int64_t last = a.m * (team + 1) / teams;
+    auto fetch = [&](int64_t row) {
+        in.fetch(0, x.row(row), a.n, at);
+        if (branch) in.fetch(1, y.row(row), a.n, at);
     };
-    if (VEC > 1) fetch(i, 0);
-    if (post) w_post.load(a.w_post, a.n);
-    if (a.w_pre != nullptr) w_pre.load(a.w_pre, a.n);
-    for (int which = 0; i < last; ++i, which ^= 1) {
-        if (a.gate != nullptr && i / a.group_rows != group) group = i / a.group_rows, gate.load(a.gate + group * a.n, a.n);
-        fetch(VEC > 1 ? i + 1 : i, which ^ 1);
+    in.clear(a.n, at);
+    if (VEC > 1) {
+        if (i < last) fetch(i);
+        in.commit();
+    }
+    const Keep keep(a.dropout);
+    if (pre) w_pre.set(a.n, at, [&](int c) { return __ldg(a.w_pre + c); });
+    Exchange ex(&room, ranks);
+    for (; i < last; ++i) {
+        if (branch && i == change) {
+            const int64_t group = i / a.group_rows;
+            change = (group + 1) * a.group_rows;
+            weight.set(a.n, at, [&](int c) { return branch_weight(a, group, c); });
+        }
+        if (VEC == 1 || i + 1 < last) fetch(VEC == 1 ? i : i + 1);
+        in.commit();
         in.arrived();
-        float v[SL][VEC];
-        float2 st = make_float2(0.f, 1.f), pre = make_float2(0.f, 1.f);
-        if (post) {
+        in.take(0);
+        if (branch) in.take(1);
+        uint32_t r[COLS / 2];
+        if (a.drop) mask.make(a, keep, i, at, r);
+        float2 h[COLS / 2], v[COLS / 2], st = make_float2(0.f, 1.f), to = make_float2(0.f, 1.f);
+        if (branch) {
 #pragma unroll
-            for (int q = 0; q < SL; ++q) {
+            for (int p = 0; p < COLS / 2; ++p) h[p] = in.get(1, p);
+            if (post) {
+                st = held_norm<VEC, COLS>(a, ex, at, h, inv_n);
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) v[q][k] = 0.f;
-                if ((q * blockDim.x + threadIdx.x) * VEC < a.n) in.get(1, which, q, v[q]);
-            }
-            st = held_norm(a, ex, v, inv_n);
-        }
-#pragma unroll
-        for (int q = 0; q < SL; ++q) {
-            const int c = (q * blockDim.x + threadIdx.x) * VEC;
-            float b[VEC], wp[VEC], g[VEC];
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) b[k] = wp[k] = g[k] = 0.f;
-            if (c < a.n) {
-                if (post) {
-                    w_post.get(q, wp);
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) b[k] = (v[q][k] - st.x) * st.y;
-                } else if (branch) {
-                    in.get(1, which, q, b);
-                }
-                if (a.gate != nullptr) gate.get(q, g);
-                in.get(0, which, q, v[q]);
-                joined(a, branch, staying<VEC>(a, keep, i, c), wp, g, b, v[q]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) v[q][k] = 0.f;
+                for (int p = 0; p < COLS / 2; ++p) h[p] = __fmul2_rn(__fadd2_rn(h[p], pair(-st.x)), pair(st.y));
             }
         }
-        if (s.p != nullptr) {
+        joined<VEC, COLS>(a, keep, branch, in, h, r, weight, v);
+        if (s.p != nullptr) put<T, VEC, COLS>(s.row(i), a.n, at, v);
+        if (pre) {
+            to = held_norm<VEC, COLS>(a, ex, at, v, inv_n);
 #pragma unroll
-            for (int q = 0; q < SL; ++q) put_slot(s.row(i), (q * blockDim.x + threadIdx.x) * VEC, a.n, v[q]);
-        }
-        if (a.w_pre != nullptr) {
-            pre = held_norm(a, ex, v, inv_n);
+            for (int k = 0; k < COLS / 4; ++k) {
+                float2 w[2];
+                w_pre.get(k, w);
 #pragma unroll
-            for (int q = 0; q < SL; ++q) {
-                const int c = (q * blockDim.x + threadIdx.x) * VEC;
-                if (c >= a.n) continue;
-                float w[VEC];
-                w_pre.get(q, w);
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) v[q][k] = (v[q][k] - pre.x) * pre.y * w[k];
-                put_slot(z.row(i), c, a.n, v[q]);
+                for (int e = 0; e < 2; ++e) v[2 * k + e] = __fmul2_rn(__fmul2_rn(__fadd2_rn(v[2 * k + e], pair(-to.x)), pair(to.y)), w[e]);
             }
+            put<T, VEC, COLS>(z.row(i), a.n, at, v);
         }
-        if (a.stats != nullptr && threadIdx.x == 0) a.stats[i] = make_float4(st.x, st.y, pre.x, pre.y);
+        if (a.stats != nullptr && threadIdx.x == 0 && rank == 0) a.stats[i] = make_float4(st.x, st.y, to.x, to.y);
     }
 }
 
 // ---- gradient -----------------------------------------------------------------------------------
 //
-// The rows are cut into parts that lie within a gate's group each; a CTA takes a run of parts and keeps the column sums of
+// The rows are cut into parts that lie within a gate's group each; a CTA (cluster) takes a run of parts and keeps the column sums of
 // dw_post and dw_pre over all of them, that of dgate over a part.  The sums of the CTAs and parts go to the workspace and are
 // added up in their order by a second kernel.
 
 struct Parts {
-    int64_t groups, rows, per_group, count, ctas;   // rows of a group; parts of a group, of all
+    int64_t groups, rows, per_group, count, teams;   // rows of a group; parts of a group, of all
 };
 struct Sums {
-    float *post, *gate, *pre;   // [ctas][n], [count][n], [ctas][n]; nullptr: not wanted
+    float *post, *gate, *pre;   // [teams][n], [count][n], [teams][n]; nullptr: not wanted
 };
 
 __device__ __forceinline__ int64_t part_begin(const Parts& p, int64_t k) { return k / p.per_group * p.rows + k % p.per_group * p.rows / p.per_group; }
 __device__ __forceinline__ int64_t part_end(const Parts& p, int64_t k) { return k / p.per_group * p.rows + (k % p.per_group + 1) * p.rows / p.per_group; }
 
-// Any width: column sums in shared memory, what a row's passes share in registers.
-template <typename T>
-__global__ void __launch_bounds__(kWide) join_wide_backward_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ Parts parts, const __grid_constant__ Sums out,
-                                                                   JoinRows<const T> x, JoinRows<const T> y, JoinRows<const T> ds, JoinRows<const T> dz, JoinRows<T> dx, JoinRows<T> dy) {
-    extern __shared__ float sums[];
-    __shared__ float part[32];
-    float *sum_post = sums, *sum_gate = sums + a.n, *sum_pre = sums + 2 * a.n;
-    const Keep keep(a.dropout);
-    const bool pre = a.w_pre != nullptr && dz.p != nullptr, post = a.w_post != nullptr, branch = y.p != nullptr;
+template <typename T, int VEC, int COLS>
+__global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ Parts parts, const __grid_constant__ Sums out, int ranks,
+                                                              JoinRows<const T> x, JoinRows<const T> y, JoinRows<const T> ds, JoinRows<const T> dz, JoinRows<T> dx, JoinRows<T> dy) {
+    extern __shared__ __align__(16) float4 smem[];
+    __shared__ __align__(16) Exchange::Room room;
+    const int width = blockDim.x * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks;
+    const Columns<VEC> at{rank * width};
+    const ByColumn<VEC, COLS> weight{smem}, w_pre{smem + width / 4};
+    Held<T, VEC, COLS, 4> in(smem + width / 2);
+    Mask<VEC, COLS> mask{reinterpret_cast<uint16_t*>(smem + width / 2 + (VEC > 1 ? 2 * 4 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
+    const bool branch = y.p != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr && dz.p != nullptr, stream = ds.p != nullptr;
     const float inv_n = 1.f / static_cast<float>(a.n);
-    for (int c = threadIdx.x; c < 3 * a.n; c += kWide) sums[c] = 0.f;
-    __syncthreads();
-    const int64_t last = parts.count * (blockIdx.x + 1) / parts.ctas;
-    for (int64_t k = parts.count * blockIdx.x / parts.ctas; k < last; ++k) {
-        for (int64_t i = part_begin(parts, k); i < part_end(parts, k); ++i) {
-            const float4 st = a.stats != nullptr ? a.stats[i] : make_float4(0.f, 1.f, 0.f, 1.f);
-            const float* gate = a.gate != nullptr ? a.gate + i / a.group_rows * a.n : nullptr;
-            uint32_t stays = 0xffffffffu;   // bit q: column q of this thread is not dropped
-            float hat[kWideColumns], c0 = 0.f, c1 = 0.f;
+    float2 sum_branch[COLS / 2], sum_pre[COLS / 2], sum_post[COLS / 2];
 #pragma unroll
-            for (int q = 0; q < kWideColumns; ++q) {
-                const int c = q * kWide + threadIdx.x;
-                hat[q] = 0.f;
-                if (c >= a.n) continue;
-                if (a.drop && !keep.elements<1>(static_cast<uint64_t>(i) * a.n + c)) stays &= ~(1u << q);
-                if (!pre) continue;
-                float v = a.residual * to_f32(x.row(i)[c]);
-                if (branch && (stays >> q & 1)) {
-                    float b = to_f32(y.row(i)[c]);
-                    if (post) b = (b - st.x) * st.y * a.w_post[c];
-                    v = fmaf(gate != nullptr ? a.scale * gate[c] : a.scale, b, v);
-                }
-                hat[q] = (v - st.z) * st.w;
-                const float d = to_f32(dz.row(i)[c]);
-                sum_pre[c] = fmaf(d, hat[q], sum_pre[c]);
-                c0 = fmaf(d, a.w_pre[c], c0), c1 = fmaf(d * a.w_pre[c], hat[q], c1);
-            }
-            if (pre) {
-                c0 = a.layer ? cta_sum(c0, part) * inv_n : 0.f;
-                c1 = cta_sum(c1, part) * inv_n;
-            }
-            float k0 = 0.f, k1 = 0.f;
-            // from here on hat[] is what the block's norm gets; dx is written last, so that it may lie over any input
-            float g[kWideColumns];
-#pragma unroll
-            for (int q = 0; q < kWideColumns; ++q) {
-                const int c = q * kWide + threadIdx.x;
-                g[q] = 0.f;
-                if (c >= a.n) continue;
-                g[q] = ds.p != nullptr ? to_f32(ds.row(i)[c]) : 0.f;
-                if (pre) g[q] += st.w * (to_f32(dz.row(i)[c]) * a.w_pre[c] - c0 - hat[q] * c1);
-                if (!branch) continue;
-                float u = stays >> q & 1 ? a.scale * g[q] : 0.f;
-                float h = to_f32(y.row(i)[c]);
-                if (post) h = (h - st.x) * st.y;
-                sum_gate[c] = fmaf(u, post ? h * a.w_post[c] : h, sum_gate[c]);
-                if (gate != nullptr) u *= gate[c];
-                if (post) {
-                    sum_post[c] = fmaf(u, h, sum_post[c]);
-                    u *= a.w_post[c];
-                    k0 += u, k1 = fmaf(u, h, k1);
-                }
-                hat[q] = u;
-            }
-            if (post) {
-                k0 = a.layer ? cta_sum(k0, part) * inv_n : 0.f;
-                k1 = cta_sum(k1, part) * inv_n;
-            }
-#pragma unroll
-            for (int q = 0; q < kWideColumns; ++q) {
-                const int c = q * kWide + threadIdx.x;
-                if (c >= a.n) continue;
-                const float h = post ? (to_f32(y.row(i)[c]) - st.x) * st.y : 0.f;
-                if (dy.p != nullptr) dy.row(i)[c] = from_f32<T>(post ? st.y * (hat[q] - k0 - h * k1) : hat[q]);
-                if (dx.p != nullptr) dx.row(i)[c] = from_f32<T>(a.residual * g[q]);
-            }
-        }
-        if (out.gate != nullptr)
-            for (int c = threadIdx.x; c < a.n; c += kWide) out.gate[k * a.n + c] = sum_gate[c], sum_gate[c] = 0.f;
-    }
-    for (int c = threadIdx.x; c < a.n; c += kWide) {
-        if (out.post != nullptr) out.post[static_cast<int64_t>(blockIdx.x) * a.n + c] = sum_post[c];
-        if (out.pre != nullptr) out.pre[static_cast<int64_t>(blockIdx.x) * a.n + c] = sum_pre[c];
-    }
-}
-
-// Column sums in registers.
-template <typename T, int VEC, int SL>
-__global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ Parts parts, const __grid_constant__ Sums out, JoinRows<const T> x,
-                                                              JoinRows<const T> y, JoinRows<const T> ds, JoinRows<const T> dz, JoinRows<T> dx, JoinRows<T> dy) {
-    extern __shared__ __align__(16) float smem[];
-    __shared__ __align__(16) float part[2][2][16];
-    Exchange ex(part);
-    const Keep keep(a.dropout);
-    const bool branch = y.p != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr && dz.p != nullptr;
-    const int floats = weight_floats(blockDim.x, VEC * SL);
-    float* room = smem;
-    Weights<VEC, SL> w_post{room}, gate{room += post ? floats : 0}, w_pre{room += a.gate != nullptr ? floats : 0};
-    Staged<T, VEC, SL, 4> in(room + (pre ? floats : 0));
-    const float inv_n = 1.f / static_cast<float>(a.n);
-    float sum_post[SL][VEC], sum_gate[SL][VEC], sum_pre[SL][VEC];
-#pragma unroll
-    for (int q = 0; q < SL; ++q)
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) sum_post[q][k] = sum_gate[q][k] = sum_pre[q][k] = 0.f;
-    if (post) w_post.load(a.w_post, a.n);
-    if (pre) w_pre.load(a.w_pre, a.n);
+    for (int p = 0; p < COLS / 2; ++p) sum_branch[p] = sum_pre[p] = sum_post[p] = pair(0.f);
     // the CTA's rows, part after part: parts that follow one another hold rows that do
-    int64_t k = parts.count * blockIdx.x / parts.ctas, group = -1;
-    const int64_t last_part = parts.count * (blockIdx.x + 1) / parts.ctas, last = part_end(parts, last_part - 1);
+    int64_t k = parts.count * team / parts.teams;
+    const int64_t last_part = parts.count * (team + 1) / parts.teams, last = part_end(parts, last_part - 1);
     int64_t i = part_begin(parts, k), end = part_end(parts, k);
-    auto fetch = [&](int64_t row, int which) {
-        if (row < last) {
-            if (pre) in.fetch(0, which, x.row(row), a.n), in.fetch(3, which, dz.row(row), a.n);
-            if (branch) in.fetch(1, which, y.row(row), a.n);
-            if (ds.p != nullptr) in.fetch(2, which, ds.row(row), a.n);
-        }
-        in.commit();
+    auto fetch = [&](int64_t row) {
+        if (pre) in.fetch(0, x.row(row), a.n, at), in.fetch(3, dz.row(row), a.n, at);
+        if (branch) in.fetch(1, y.row(row), a.n, at);
+        if (stream) in.fetch(2, ds.row(row), a.n, at);
     };
-    if (VEC > 1) fetch(i, 0);
-    int which = 0;
+    in.clear(a.n, at);
+    if (VEC > 1) {
+        if (i < last) fetch(i);
+        in.commit();
+    }
+    const Keep keep(a.dropout);
+    if (pre) w_pre.set(a.n, at, [&](int c) { return __ldg(a.w_pre + c); });
+    Exchange ex(&room, ranks);
     for (; k < last_part; ++k, end = part_end(parts, k)) {
-        for (; i < end; ++i, which ^= 1) {
-            if (a.gate != nullptr && i / a.group_rows != group) group = i / a.group_rows, gate.load(a.gate + group * a.n, a.n);
+        const int64_t group = k / parts.per_group;
+        if (branch && i < end) weight.set(a.n, at, [&](int c) { return branch_weight(a, group, c); });
+        for (; i < end; ++i) {
             const float4 st = a.stats != nullptr ? a.stats[i] : make_float4(0.f, 1.f, 0.f, 1.f);
-            fetch(VEC > 1 ? i + 1 : i, which ^ 1);
+            if (VEC == 1 || i + 1 < last) fetch(VEC == 1 ? i : i + 1);
+            in.commit();
             in.arrived();
-            uint32_t stays[SL];
-            float v[SL][VEC], c01[2] = {0.f, 0.f};
+            if (pre) in.take(0), in.take(3);
+            if (branch) in.take(1);
+            if (stream) in.take(2);
+            uint32_t r[COLS / 2];
+            if (a.drop) mask.make(a, keep, i, at, r);
+            float2 h[COLS / 2], v[COLS / 2], g[COLS / 2];
+            if (branch) {
 #pragma unroll
-            for (int q = 0; q < SL; ++q) {
-                const int c = (q * blockDim.x + threadIdx.x) * VEC;
-                stays[q] = staying<VEC>(a, keep, i, c);
-                if (!pre || c >= a.n) continue;
-                float b[VEC], wp[VEC], g[VEC], d[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) b[e] = wp[e] = g[e] = 0.f;
-                if (branch) {
-                    in.get(1, which, q, b);
-                    if (post) {
-                        w_post.get(q, wp);
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) b[e] = (b[e] - st.x) * st.y;
-                    }
-                    if (a.gate != nullptr) gate.get(q, g);
-                }
-                in.get(0, which, q, v[q]);
-                joined(a, branch, stays[q], wp, g, b, v[q]);
-                in.get(3, which, q, d);
-                w_pre.get(q, wp);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    v[q][e] = c + e < a.n ? (v[q][e] - st.z) * st.w : 0.f;
-                    sum_pre[q][e] = fmaf(d[e], v[q][e], sum_pre[q][e]);
-                    d[e] *= wp[e];   // 0 behind the last column
-                    c01[0] += d[e], c01[1] = fmaf(d[e], v[q][e], c01[1]);
-                }
+                for (int p = 0; p < COLS / 2; ++p) h[p] = __fmul2_rn(__fadd2_rn(in.get(1, p), pair(-st.x)), pair(st.y));   // no norm: mean 0, deviation 1
             }
+            float c01[2] = {0.f, 0.f}, k01[2] = {0.f, 0.f};
+#pragma unroll
+            for (int p = 0; p < COLS / 2; ++p) g[p] = stream ? in.get(2, p) : pair(0.f);
             if (pre) {
-                ex.sum(c01);
-                c01[0] = a.layer ? c01[0] * inv_n : 0.f, c01[1] *= inv_n;
-            }
-            float k01[2] = {0.f, 0.f};
+                joined<VEC, COLS>(a, keep, branch, in, h, r, weight, v);
+                float2 c0 = pair(0.f), c1 = pair(0.f);
+                float2 d[COLS / 2];
 #pragma unroll
-            for (int q = 0; q < SL; ++q) {
-                const int c = (q * blockDim.x + threadIdx.x) * VEC;
-                if (c >= a.n) continue;
-                float g[VEC], d[VEC], w[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) g[e] = 0.f;
-                if (ds.p != nullptr) in.get(2, which, q, g);
-                if (pre) {
-                    in.get(3, which, q, d);
+                for (int q = 0; q < COLS / 4; ++q) {
+                    float2 w[2];
                     w_pre.get(q, w);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) g[e] = fmaf(st.w, fmaf(-v[q][e], c01[1], fmaf(d[e], w[e], -c01[0])), g[e]);
-                }
-                float h[VEC];
-                if (branch) in.get(1, which, q, h);
-                if (dx.p != nullptr) {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) d[e] = a.residual * g[e];
-                    put_slot(dx.row(i), c, a.n, d);
-                }
-                if (!branch) continue;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    g[e] = (stays[q] >> e & 1) && c + e < a.n ? a.scale * g[e] : 0.f;
-                    if (post) h[e] = (h[e] - st.x) * st.y;
-                }
-                if (a.gate != nullptr) {
-                    float wp[VEC];
-                    if (post) w_post.get(q, wp);
-                    gate.get(q, w);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        sum_gate[q][e] = fmaf(g[e], post ? h[e] * wp[e] : h[e], sum_gate[q][e]);
-                        g[e] *= w[e];
+                    for (int e = 0; e < 2; ++e) {
+                        const int p = 2 * q + e;
+                        const float2 z = in.get(3, p);
+                        v[p] = __fmul2_rn(__fadd2_rn(v[p], pair(-st.z)), pair(st.w));
+                        sum_pre[p] = __ffma2_rn(z, v[p], sum_pre[p]);
+                        d[p] = __fmul2_rn(z, w[e]);
+                        c0 = __fadd2_rn(c0, d[p]), c1 = __ffma2_rn(d[p], v[p], c1);
                     }
                 }
-                if (post) {
-                    w_post.get(q, w);
+                c01[0] = c0.x + c0.y, c01[1] = c1.x + c1.y;
+                ex.sum(c01);
+                const float2 k0 = pair(a.layer ? -st.w * c01[0] * inv_n : 0.f), k1 = pair(-st.w * c01[1] * inv_n);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        sum_post[q][e] = fmaf(g[e], h[e], sum_post[q][e]);
-                        g[e] *= w[e];
-                        k01[0] += g[e], k01[1] = fmaf(g[e], h[e], k01[1]);
-                    }
+                for (int p = 0; p < COLS / 2; ++p) g[p] = __ffma2_rn(v[p], k1, __ffma2_rn(d[p], pair(st.w), __fadd2_rn(g[p], k0)));
+            }
+            if (dx.p != nullptr) {
+#pragma unroll
+                for (int p = 0; p < COLS / 2; ++p) v[p] = __fmul2_rn(g[p], pair(a.residual));
+                put<T, VEC, COLS>(dx.row(i), a.n, at, v);
+            }
+            if (!branch) continue;
+            if (a.drop) {
+#pragma unroll
+                for (int p = 0; p < COLS / 2; ++p) g[p] = Mask<VEC, COLS>::apply(keep, r[p], g[p]);
+            }
+            float2 c0 = pair(0.f), c1 = pair(0.f);
+#pragma unroll
+            for (int q = 0; q < COLS / 4; ++q) {
+                float2 w[2];
+                weight.get(q, w);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int p = 2 * q + e;
+                    sum_branch[p] = __ffma2_rn(g[p], h[p], sum_branch[p]);
+                    g[p] = __fmul2_rn(g[p], w[e]);
+                    c0 = __fadd2_rn(c0, g[p]), c1 = __ffma2_rn(g[p], h[p], c1);
                 }
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) v[q][e] = g[e];
             }
             if (dy.p == nullptr) continue;
             if (post) {
+                k01[0] = c0.x + c0.y, k01[1] = c1.x + c1.y;
                 ex.sum(k01);
-                k01[0] = a.layer ? k01[0] * inv_n : 0.f, k01[1] *= inv_n;
-            }
+                const float2 k0 = pair(a.layer ? -k01[0] * inv_n : 0.f), k1 = pair(-k01[1] * inv_n);
 #pragma unroll
-            for (int q = 0; q < SL; ++q) {
-                const int c = (q * blockDim.x + threadIdx.x) * VEC;
-                if (c >= a.n) continue;
-                if (post) {
-                    float h[VEC];
-                    in.get(1, which, q, h);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) v[q][e] = st.y * fmaf(-(h[e] - st.x) * st.y, k01[1], v[q][e] - k01[0]);
-                }
-                put_slot(dy.row(i), c, a.n, v[q]);
+                for (int p = 0; p < COLS / 2; ++p) g[p] = __fmul2_rn(__ffma2_rn(h[p], k1, __fadd2_rn(g[p], k0)), pair(st.y));
             }
+            put<T, VEC, COLS>(dy.row(i), a.n, at, g);
         }
-        if (out.gate != nullptr) {
+        if (out.gate != nullptr || out.post != nullptr) {
 #pragma unroll
-            for (int q = 0; q < SL; ++q) {
-                const int c = (q * blockDim.x + threadIdx.x) * VEC;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    if (c + e < a.n) out.gate[k * a.n + c + e] = sum_gate[q][e];
-                    sum_gate[q][e] = 0.f;
+            for (int e = 0; e < COLS; ++e) {
+                const int c = at.of(e);
+                const float sum = a.scale * (e & 1 ? sum_branch[e / 2].y : sum_branch[e / 2].x);
+                if (c < a.n) {
+                    if (out.gate != nullptr) out.gate[k * a.n + c] = post ? a.w_post[c] * sum : sum;
+                    float& to = e & 1 ? sum_post[e / 2].y : sum_post[e / 2].x;
+                    if (post) to = a.gate != nullptr ? fmaf(a.gate[group * a.n + c], sum, to) : to + sum;
                 }
             }
+#pragma unroll
+            for (int p = 0; p < COLS / 2; ++p) sum_branch[p] = pair(0.f);
         }
     }
 #pragma unroll
-    for (int q = 0; q < SL; ++q) {
-        const int c = (q * blockDim.x + threadIdx.x) * VEC;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            if (out.post != nullptr && c + e < a.n) out.post[static_cast<int64_t>(blockIdx.x) * a.n + c + e] = sum_post[q][e];
-            if (out.pre != nullptr && c + e < a.n) out.pre[static_cast<int64_t>(blockIdx.x) * a.n + c + e] = sum_pre[q][e];
-        }
+    for (int e = 0; e < COLS; ++e) {
+        const int c = at.of(e);
+        if (out.post != nullptr && c < a.n) out.post[static_cast<int64_t>(team) * a.n + c] = e & 1 ? sum_post[e / 2].y : sum_post[e / 2].x;
+        if (out.pre != nullptr && c < a.n) out.pre[static_cast<int64_t>(team) * a.n + c] = e & 1 ? sum_pre[e / 2].y : sum_pre[e / 2].x;
     }
 }
 
@@ -620,21 +564,21 @@ Parts parts_of(int64_t m, int64_t n, int64_t groups) {
     Parts p;
     p.groups = groups > 0 ? groups : 1;
     p.rows = m / p.groups;
-    // CTAs that share an SM, as many as have 32 rows each: fewer would have the column sums' traffic show
+    // As many as run at a time, but none of fewer than 32 rows: their sums' traffic would show.
     int64_t per_sm = n <= 8 * kTeam ? 8 * kTeam / (n > 256 ? n : 256) : 1;
     if (per_sm > 1 && m < per_sm * kNumSMs * 32) per_sm = m / (kNumSMs * 32) > 1 ? m / (kNumSMs * 32) : 1;
-    p.ctas = per_sm * kNumSMs;
+    p.teams = n <= 16 * kTeam ? per_sm * kNumSMs : kNumSMs / 2;   // wider rows take a cluster
     // one group: a part for each CTA; more: four rounds of parts, so that the last round is short
-    int64_t per = p.groups == 1 ? p.ctas : (4 * p.ctas + p.groups - 1) / p.groups;
+    int64_t per = p.groups == 1 ? p.teams : (4 * p.teams + p.groups - 1) / p.groups;
     p.per_group = per < p.rows ? per : (p.rows > 0 ? p.rows : 1);
     p.count = p.groups * p.per_group;
-    if (p.ctas > p.count) p.ctas = p.count;
+    if (p.teams > p.count) p.teams = p.count;
     return p;
 }
 size_t gate_sums(const Parts& p, int64_t n) { return p.per_group > 1 ? static_cast<size_t>(p.count) * n : 0; }
 size_t workspace_of(int64_t m, int64_t n, int64_t groups) {
     const Parts p = parts_of(m, n, groups);
-    return round_up((gate_sums(p, n) + 2 * static_cast<size_t>(p.ctas) * n) * sizeof(float), 256);
+    return round_up((gate_sums(p, n) + 2 * static_cast<size_t>(p.teams) * n) * sizeof(float), 256);
 }
 
 struct JoinTensors {
@@ -652,70 +596,66 @@ bool in_words(const JoinTensors& t, int64_t m, int bytes) {
         if (p[k] != nullptr && (!aligned16(p[k]) || (m > 1 && ld[k] * bytes % 16 != 0))) return false;
     return true;
 }
-int threads_for(int64_t n, int columns) {
-    int t = 32;
-    while (t < kTeam && static_cast<int64_t>(t) * columns < n) t *= 2;
-    return t;
+
+struct Shape {
+    int threads, ranks, smem;
+};
+template <typename T, int VEC, int COLS> Shape shape_of(int n, int tensors, bool drop) {
+    Shape s{32, 1, 0};
+    while (s.threads < kTeam && s.threads * COLS < n) s.threads *= 2;
+    while (s.threads * COLS * s.ranks < n) s.ranks *= 2;
+    const int width = s.threads * COLS;
+    s.smem = width * (8 + (VEC > 1 ? 2 * tensors * static_cast<int>(sizeof(T)) : 0)) + (drop && !(VEC == 8 && n % 8 == 0) ? 2 * 2 * (width + 16) : 0);
+    return s;
 }
-
-constexpr int kSharedPerSm = 220 * 1024;   // leaves room for the static arrays and what the system takes of each CTA
-
-template <typename T, int VEC, int SL> int forward_fast(const JoinArgs& a, const JoinTensors& t, cudaStream_t s) {
-    const int threads = threads_for(a.n, VEC * SL), weights = (a.w_post != nullptr) + (a.gate != nullptr) + (a.w_pre != nullptr);
-    const int smem = threads * VEC * SL * (4 * weights + (VEC > 1 ? 2 * 2 * static_cast<int>(sizeof(T)) : 0));
-    auto kern = join_kernel<T, VEC, SL>;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTeam * VEC * SL * (12 + (VEC > 1 ? 4 * static_cast<int>(sizeof(T)) : 0)));
+// teams: clusters of s.ranks CTAs
+template <typename K, typename... A> int start(K kern, const Shape& s, int64_t teams, int most_smem, cudaStream_t stream, A... args) {
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem);
     if (e != cudaSuccess) return cuda_failed(e);
-    int per_sm = 1024 / threads;
-    if (per_sm * (smem + 1280) > kSharedPerSm) per_sm = kSharedPerSm / (smem + 1280);
-    if (per_sm < 1) per_sm = 1;
-    const int64_t grid = a.m < static_cast<int64_t>(per_sm) * kNumSMs ? a.m : static_cast<int64_t>(per_sm) * kNumSMs;
-    kern<<<static_cast<unsigned>(grid), threads, smem, s>>>(a, {static_cast<const T*>(t.a), t.ld_a}, {static_cast<const T*>(t.b), t.ld_b}, {static_cast<T*>(t.e), t.ld_e},
-                                                            {static_cast<T*>(t.f), t.ld_f});
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(teams * s.ranks));
+    cfg.blockDim = dim3(static_cast<unsigned>(s.threads));
+    cfg.dynamicSmemBytes = static_cast<size_t>(s.smem);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {static_cast<unsigned>(s.ranks), 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = s.ranks > 1 ? 1 : 0;
+    e = cudaLaunchKernelEx(&cfg, kern, args...);
+    if (e != cudaSuccess) return cuda_failed(e);
     note_launch();
     return check_launch();
+}
+template <typename T, int VEC, int COLS> int most_smem(int tensors) { return kTeam * COLS * (8 + (VEC > 1 ? 2 * tensors * static_cast<int>(sizeof(T)) : 0)) + 2 * 2 * (kTeam * COLS + 16); }
+
+template <typename T, int VEC, int COLS> int forward_as(const JoinArgs& a, const JoinTensors& t, cudaStream_t s) {
+    const Shape shape = shape_of<T, VEC, COLS>(a.n, 2, a.drop != 0);
+    // as many as fit an SM
+    int per_sm = 1024 / shape.threads;
+    if (per_sm * (shape.smem + 2048) > 220 * 1024) per_sm = 220 * 1024 / (shape.smem + 2048);
+    const int64_t most = static_cast<int64_t>(per_sm > 1 ? per_sm : 1) * kNumSMs / shape.ranks;
+    return start(join_kernel<T, VEC, COLS>, shape, a.m < most ? a.m : most, most_smem<T, VEC, COLS>(2), s, a, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
+                 JoinRows<const T>{static_cast<const T*>(t.b), t.ld_b}, JoinRows<T>{static_cast<T*>(t.e), t.ld_e}, JoinRows<T>{static_cast<T*>(t.f), t.ld_f});
+}
+template <typename T, int VEC, int COLS> int backward_as(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, cudaStream_t s) {
+    const Shape shape = shape_of<T, VEC, COLS>(a.n, 4, a.drop != 0);
+    return start(join_backward_kernel<T, VEC, COLS>, shape, p.teams, most_smem<T, VEC, COLS>(4), s, a, p, sums, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
+                 JoinRows<const T>{static_cast<const T*>(t.b), t.ld_b}, JoinRows<const T>{static_cast<const T*>(t.c), t.ld_c}, JoinRows<const T>{static_cast<const T*>(t.d), t.ld_d},
+                 JoinRows<T>{static_cast<T*>(t.e), t.ld_e}, JoinRows<T>{static_cast<T*>(t.f), t.ld_f});
 }
 
 template <typename T> int forward(const JoinArgs& a, const JoinTensors& t, cudaStream_t s) {
     constexpr int N = Word<T>::kN;
-    const bool words = in_words(t, a.m, sizeof(T));
-    if (a.n <= 8 * 32) return words ? forward_fast<T, N, 8 / N>(a, t, s) : forward_fast<T, 1, 8>(a, t, s);
-    if (a.n <= 16 * kTeam) return words ? forward_fast<T, N, 16 / N>(a, t, s) : forward_fast<T, 1, 16>(a, t, s);
-    auto kern = join_wide_kernel<T>;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, BZ_MAX_WIDTH * sizeof(float));
-    if (e != cudaSuccess) return cuda_failed(e);
-    kern<<<static_cast<unsigned>(a.m < 2 * kNumSMs ? a.m : 2 * kNumSMs), kWide, static_cast<size_t>(a.n) * sizeof(float), s>>>(
-        a, {static_cast<const T*>(t.a), t.ld_a}, {static_cast<const T*>(t.b), t.ld_b}, {static_cast<T*>(t.e), t.ld_e}, {static_cast<T*>(t.f), t.ld_f});
-    note_launch();
-    return check_launch();
+    if (!in_words(t, a.m, sizeof(T))) return forward_as<T, 1, 8>(a, t, s);
+    return a.n <= 8 * 256 ? forward_as<T, N, 8>(a, t, s) : forward_as<T, N, 16>(a, t, s);
 }
-
-template <typename T, int VEC, int SL> int backward_fast(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, cudaStream_t s) {
-    const int threads = threads_for(a.n, VEC * SL), weights = (a.w_post != nullptr) + (a.gate != nullptr) + (a.w_pre != nullptr && t.d != nullptr);
-    const int smem = threads * VEC * SL * (4 * weights + (VEC > 1 ? 4 * 2 * static_cast<int>(sizeof(T)) : 0));
-    auto kern = join_backward_kernel<T, VEC, SL>;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTeam * VEC * SL * (12 + (VEC > 1 ? 8 * static_cast<int>(sizeof(T)) : 0)));
-    if (e != cudaSuccess) return cuda_failed(e);
-    kern<<<static_cast<unsigned>(p.ctas), threads, smem, s>>>(a, p, sums, {static_cast<const T*>(t.a), t.ld_a}, {static_cast<const T*>(t.b), t.ld_b}, {static_cast<const T*>(t.c), t.ld_c},
-                                                              {static_cast<const T*>(t.d), t.ld_d}, {static_cast<T*>(t.e), t.ld_e}, {static_cast<T*>(t.f), t.ld_f});
-    note_launch();
-    return check_launch();
-}
-
 template <typename T> int backward(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, cudaStream_t s) {
     constexpr int N = Word<T>::kN;
-    const bool words = in_words(t, a.m, sizeof(T));
-    if (a.n <= 8 * kTeam) return words ? backward_fast<T, N, 8 / N>(a, t, p, sums, s) : backward_fast<T, 1, 8>(a, t, p, sums, s);
+    if (!in_words(t, a.m, sizeof(T))) return backward_as<T, 1, 8>(a, t, p, sums, s);
     if constexpr (sizeof(T) == 2)
-        if (a.n <= 16 * kTeam && words) return backward_fast<T, N, 16 / N>(a, t, p, sums, s);
-    auto kern = join_wide_backward_kernel<T>;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * BZ_MAX_WIDTH * sizeof(float));
-    if (e != cudaSuccess) return cuda_failed(e);
-    kern<<<static_cast<unsigned>(p.ctas), kWide, 3 * static_cast<size_t>(a.n) * sizeof(float), s>>>(
-        a, p, sums, {static_cast<const T*>(t.a), t.ld_a}, {static_cast<const T*>(t.b), t.ld_b}, {static_cast<const T*>(t.c), t.ld_c}, {static_cast<const T*>(t.d), t.ld_d},
-        {static_cast<T*>(t.e), t.ld_e}, {static_cast<T*>(t.f), t.ld_f});
-    note_launch();
-    return check_launch();
+        if (a.n > 8 * kTeam) return backward_as<T, N, 16>(a, t, p, sums, s);
+    return backward_as<T, N, 8>(a, t, p, sums, s);
 }
 
 // A row tensor: rows that do not overlap, elements on their type's boundary.
@@ -816,8 +756,8 @@ extern "C" int bz_join_backward(const void* x, int64_t ld_x, const void* y, int6
         folds.f[count++] = {from, to, rows, per};
         return from;
     };
-    if (dw_post != nullptr) partial.post = fold(dw_post, 1, p.ctas);
-    if (dw_pre != nullptr) partial.pre = fold(dw_pre, 1, p.ctas);
+    if (dw_post != nullptr) partial.post = fold(dw_post, 1, p.teams);
+    if (dw_pre != nullptr) partial.pre = fold(dw_pre, 1, p.teams);
     if (dgate != nullptr) partial.gate = p.per_group > 1 ? fold(dgate, p.groups, p.per_group) : dgate;
     const JoinArgs a = join_args(m, n, norm, 0.f, w_post, gate, groups, residual_scale, branch_scale, least, rng, w_pre, stats);
     cudaStream_t stream_ = static_cast<cudaStream_t>(stream);
