@@ -70,30 +70,24 @@ template <typename T, int VEC, int COLS, int NT> struct Held {
     static constexpr int kWords = COLS / VEC;
     uint4* room;
     int half = 0;
-    uint4 w[NT][kWords];
-    __device__ __forceinline__ explicit Held(void* smem) : room(static_cast<uint4*>(smem) + threadIdx.x) {}
-    __device__ __forceinline__ uint4* place(int which, int t, int q) const { return room + ((which * NT + t) * kWords + q) * blockDim.x; }
-    // words behind the last column are never copied, and stay zero
-    __device__ __forceinline__ void clear(int n, const Columns<VEC>& at) {
+    int bytes[kWords];   // of the row in each word
+    __device__ __forceinline__ Held(void* smem, int n, const Columns<VEC>& at) : room(static_cast<uint4*>(smem) + threadIdx.x) {
 #pragma unroll
-        for (int q = 0; q < kWords; ++q)
-            if (at.of(q * VEC) >= n) {
+        for (int q = 0; q < kWords; ++q) {
+            bytes[q] = min(max((n - at.of(q * VEC)) * static_cast<int>(sizeof(T)), 0), 16);
+            if (bytes[q] == 0) {   // never copied, and stays zero
 #pragma unroll
                 for (int t = 0; t < NT; ++t) *place(0, t, q) = *place(1, t, q) = make_uint4(0, 0, 0, 0);
             }
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int q = 0; q < kWords; ++q) w[t][q] = make_uint4(0, 0, 0, 0);
+        }
     }
-    // the next row's: fetches, then commit
-    __device__ __forceinline__ void fetch(int t, const T* row, int n, const Columns<VEC>& at) {
+    __device__ __forceinline__ uint4* place(int which, int t, int q) const { return room + ((which * NT + t) * kWords + q) * blockDim.x; }
+    // the next row's: fetches, then commit; what a word has behind the row's end is filled with zeros
+    __device__ __forceinline__ void fetch(int t, const T* row, int, const Columns<VEC>& at) {
 #pragma unroll
         for (int q = 0; q < kWords; ++q) {
-            const int c = at.of(q * VEC);
             const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(place(half, t, q)));
-            const int left = (n - c) * static_cast<int>(sizeof(T));   // what reaches over the row's end is filled with zeros
-            if (left > 0) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row + c), "r"(min(left, 16)) : "memory");
+            if (bytes[q] > 0) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row + at.of(q * VEC)), "r"(bytes[q]) : "memory");
         }
     }
     __device__ __forceinline__ void commit() {
@@ -101,19 +95,35 @@ template <typename T, int VEC, int COLS, int NT> struct Held {
         half ^= 1;
     }
     __device__ __forceinline__ static void arrived() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }   // all but the last commit
-    __device__ __forceinline__ void take(int t) {   // this row's: the half that the next commit will fill
+    __device__ __forceinline__ void get(int t, float2 (&v)[COLS / 2]) const {   // this row's: the half that the next commit will fill
 #pragma unroll
-        for (int q = 0; q < kWords; ++q) w[t][q] = *place(half, t, q);
+        for (int q = 0; q < kWords; ++q) {
+            const uint4 w = *place(half, t, q);
+#pragma unroll
+            for (int p = 0; p < VEC / 2; ++p) v[q * (VEC / 2) + p] = word_pair<T>(w, p);
+        }
     }
-    __device__ __forceinline__ float2 get(int t, int p) const { return word_pair<T>(w[t][p / (VEC / 2)], p % (VEC / 2)); }
+    __device__ __forceinline__ void put(T* row, int n, const Columns<VEC>& at, const float2 (&v)[COLS / 2]) const {
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) {
+            const int c = at.of(q * VEC);
+            float x[VEC];
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) x[k] = k & 1 ? v[(q * VEC + k) / 2].y : v[(q * VEC + k) / 2].x;
+            if (bytes[q] == 16) {
+                *reinterpret_cast<uint4*>(row + c) = Word<T>::pack(x);
+            } else if (bytes[q] > 0) {
+                rare();
+#pragma unroll
+                for (int k = 0; k < VEC; ++k)
+                    if (c + k < n) row[c + k] = from_f32<T>(x[k]);
+            }
+        }
+    }
 };
 template <typename T, int COLS, int NT> struct Held<T, 1, COLS, NT> {
     float2 v[NT][COLS / 2];
-    __device__ __forceinline__ explicit Held(void*) {}
-    __device__ __forceinline__ void clear(int, const Columns<1>&) {
-#pragma unroll
-        for (int k = 0; k < NT * COLS / 2; ++k) v[k / (COLS / 2)][k % (COLS / 2)] = pair(0.f);
-    }
+    __device__ __forceinline__ Held(void*, int, const Columns<1>&) {}
     __device__ __forceinline__ void fetch(int t, const T* row, int n, const Columns<1>& at) {
 #pragma unroll
         for (int p = 0; p < COLS / 2; ++p) {
@@ -123,35 +133,18 @@ template <typename T, int COLS, int NT> struct Held<T, 1, COLS, NT> {
     }
     __device__ __forceinline__ static void commit() {}
     __device__ __forceinline__ static void arrived() {}
-    __device__ __forceinline__ void take(int) {}
-    __device__ __forceinline__ float2 get(int t, int p) const { return v[t][p]; }
-};
-
-template <typename T, int VEC, int COLS> __device__ __forceinline__ void put(T* row, int n, const Columns<VEC>& at, const float2 (&v)[COLS / 2]) {
-    if constexpr (VEC == 1) {
+    __device__ __forceinline__ void get(int t, float2 (&x)[COLS / 2]) const {
+#pragma unroll
+        for (int p = 0; p < COLS / 2; ++p) x[p] = v[t][p];
+    }
+    __device__ __forceinline__ void put(T* row, int n, const Columns<1>& at, const float2 (&x)[COLS / 2]) const {
 #pragma unroll
         for (int p = 0; p < COLS / 2; ++p) {
-            if (at.of(2 * p) < n) row[at.of(2 * p)] = from_f32<T>(v[p].x);
-            if (at.of(2 * p + 1) < n) row[at.of(2 * p + 1)] = from_f32<T>(v[p].y);
-        }
-    } else {
-#pragma unroll
-        for (int q = 0; q < COLS / VEC; ++q) {
-            const int c = at.of(q * VEC);
-            float x[VEC];
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) x[k] = k & 1 ? v[(q * VEC + k) / 2].y : v[(q * VEC + k) / 2].x;
-            if (c + VEC <= n) {
-                *reinterpret_cast<uint4*>(row + c) = Word<T>::pack(x);
-            } else if (c < n) {
-                rare();
-#pragma unroll
-                for (int k = 0; k < VEC; ++k)
-                    if (c + k < n) row[c + k] = from_f32<T>(x[k]);
-            }
+            if (at.of(2 * p) < n) row[at.of(2 * p)] = from_f32<T>(x[p].x);
+            if (at.of(2 * p + 1) < n) row[at.of(2 * p + 1)] = from_f32<T>(x[p].y);
         }
     }
-}
+};
 
 // A number for each column in shared memory, where only its thread looks; 0 behind the last column.
 template <int VEC, int COLS> struct ByColumn {
@@ -287,27 +280,27 @@ template <int VEC, int COLS> __device__ __forceinline__ float2 held_norm(const J
     return {mean, 1.f / sqrtf(t[0] * inv_n + a.eps)};
 }
 
-// v[p] = s of the pair.
-template <int VEC, int COLS, typename In>
-__device__ __forceinline__ void joined(const JoinArgs& a, const Keep& keep, bool branch, const In& in, const float2 (&h)[COLS / 2], const uint32_t (&r)[COLS / 2], const ByColumn<VEC, COLS>& weight,
+// v[p] = s of the pair, from x[p].
+template <int VEC, int COLS>
+__device__ __forceinline__ void joined(const JoinArgs& a, const Keep& keep, bool branch, const float2 (&h)[COLS / 2], const uint32_t (&r)[COLS / 2], const ByColumn<VEC, COLS>& weight,
                                        float2 (&v)[COLS / 2]) {
     if (branch) {
 #pragma unroll
         for (int k = 0; k < COLS / 4; ++k) {
             float2 w[2];
             weight.get(k, w);
-            v[2 * k] = __fmul2_rn(h[2 * k], w[0]), v[2 * k + 1] = __fmul2_rn(h[2 * k + 1], w[1]);
-        }
-        if (a.drop) {
 #pragma unroll
-            for (int p = 0; p < COLS / 2; ++p) v[p] = Mask<VEC, COLS>::apply(keep, r[p], v[p]);
+            for (int e = 0; e < 2; ++e) {
+                const int p = 2 * k + e;
+                float2 b = __fmul2_rn(h[p], w[e]);
+                if (a.drop) b = Mask<VEC, COLS>::apply(keep, r[p], b);
+                v[p] = __ffma2_rn(v[p], pair(a.residual), b);
+            }
         }
     } else {
 #pragma unroll
-        for (int p = 0; p < COLS / 2; ++p) v[p] = pair(0.f);
+        for (int p = 0; p < COLS / 2; ++p) v[p] = __fmul2_rn(v[p], pair(a.residual));
     }
-#pragma unroll
-    for (int p = 0; p < COLS / 2; ++p) v[p] = __ffma2_rn(in.get(0, p), pair(a.residual), v[p]);
 }
 
 // The weight of a column of the branch.
@@ -323,7 +316,7 @@ __global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ Joi
     const int width = blockDim.x * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks, teams = gridDim.x / ranks;
     const Columns<VEC> at{rank * width};
     const ByColumn<VEC, COLS> weight{smem}, w_pre{smem + width / 4};
-    Held<T, VEC, COLS, 2> in(smem + width / 2);
+    Held<T, VEC, COLS, 2> in(smem + width / 2, a.n, at);
     Mask<VEC, COLS> mask{reinterpret_cast<uint16_t*>(smem + width / 2 + (VEC > 1 ? 2 * 2 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
     const bool branch = y.p != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr;
     const float inv_n = 1.f / static_cast<float>(a.n);
@@ -333,7 +326,6 @@ __global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ Joi
         in.fetch(0, x.row(row), a.n, at);
         if (branch) in.fetch(1, y.row(row), a.n, at);
     };
-    in.clear(a.n, at);
     if (VEC > 1) {
         if (i < last) fetch(i);
         in.commit();
@@ -350,22 +342,20 @@ __global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ Joi
         if (VEC == 1 || i + 1 < last) fetch(VEC == 1 ? i : i + 1);
         in.commit();
         in.arrived();
-        in.take(0);
-        if (branch) in.take(1);
         uint32_t r[COLS / 2];
         if (a.drop) mask.make(a, keep, i, at, r);
         float2 h[COLS / 2], v[COLS / 2], st = make_float2(0.f, 1.f), to = make_float2(0.f, 1.f);
         if (branch) {
-#pragma unroll
-            for (int p = 0; p < COLS / 2; ++p) h[p] = in.get(1, p);
+            in.get(1, h);
             if (post) {
                 st = held_norm<VEC, COLS>(a, ex, at, h, inv_n);
 #pragma unroll
                 for (int p = 0; p < COLS / 2; ++p) h[p] = __fmul2_rn(__fadd2_rn(h[p], pair(-st.x)), pair(st.y));
             }
         }
-        joined<VEC, COLS>(a, keep, branch, in, h, r, weight, v);
-        if (s.p != nullptr) put<T, VEC, COLS>(s.row(i), a.n, at, v);
+        in.get(0, v);
+        joined<VEC, COLS>(a, keep, branch, h, r, weight, v);
+        if (s.p != nullptr) in.put(s.row(i), a.n, at, v);
         if (pre) {
             to = held_norm<VEC, COLS>(a, ex, at, v, inv_n);
 #pragma unroll
@@ -375,7 +365,7 @@ __global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ Joi
 #pragma unroll
                 for (int e = 0; e < 2; ++e) v[2 * k + e] = __fmul2_rn(__fmul2_rn(__fadd2_rn(v[2 * k + e], pair(-to.x)), pair(to.y)), w[e]);
             }
-            put<T, VEC, COLS>(z.row(i), a.n, at, v);
+            in.put(z.row(i), a.n, at, v);
         }
         if (a.stats != nullptr && threadIdx.x == 0 && rank == 0) a.stats[i] = make_float4(st.x, st.y, to.x, to.y);
     }
@@ -386,6 +376,18 @@ __global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ Joi
 // The rows are cut into parts that lie within a gate's group each; a CTA (cluster) takes a run of parts and keeps the column sums of
 // dw_post and dw_pre over all of them, that of dgate over a part.  The sums of the CTAs and parts go to the workspace and are
 // added up in their order by a second kernel.
+
+// Sums over the row of c0 (0 but for LAYER) and c1.
+__device__ __forceinline__ float2 row_sums(const JoinArgs& a, Exchange& ex, float2 c0, float2 c1) {
+    if (a.layer) {
+        float t[2] = {c0.x + c0.y, c1.x + c1.y};
+        ex.sum(t);
+        return make_float2(t[0], t[1]);
+    }
+    float t[1] = {c1.x + c1.y};
+    ex.sum(t);
+    return make_float2(0.f, t[0]);
+}
 
 struct Parts {
     int64_t groups, rows, per_group, count, teams;   // rows of a group; parts of a group, of all
@@ -405,13 +407,15 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
     const int width = blockDim.x * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks;
     const Columns<VEC> at{rank * width};
     const ByColumn<VEC, COLS> weight{smem}, w_pre{smem + width / 4};
-    Held<T, VEC, COLS, 4> in(smem + width / 2);
-    Mask<VEC, COLS> mask{reinterpret_cast<uint16_t*>(smem + width / 2 + (VEC > 1 ? 2 * 4 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
+    const ByColumn<VEC, COLS> sum_post{smem + width / 2};
+    Held<T, VEC, COLS, 4> in(smem + 3 * width / 4, a.n, at);
+    Mask<VEC, COLS> mask{reinterpret_cast<uint16_t*>(smem + 3 * width / 4 + (VEC > 1 ? 2 * 4 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
     const bool branch = y.p != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr && dz.p != nullptr, stream = ds.p != nullptr;
     const float inv_n = 1.f / static_cast<float>(a.n);
-    float2 sum_branch[COLS / 2], sum_pre[COLS / 2], sum_post[COLS / 2];
+    float2 sum_branch[COLS / 2], sum_pre[COLS / 2];
 #pragma unroll
-    for (int p = 0; p < COLS / 2; ++p) sum_branch[p] = sum_pre[p] = sum_post[p] = pair(0.f);
+    for (int p = 0; p < COLS / 2; ++p) sum_branch[p] = sum_pre[p] = pair(0.f);
+    if (post) sum_post.set(a.n, at, [](int) { return 0.f; });
     // the CTA's rows, part after part: parts that follow one another hold rows that do
     int64_t k = parts.count * team / parts.teams;
     const int64_t last_part = parts.count * (team + 1) / parts.teams, last = part_end(parts, last_part - 1);
@@ -421,7 +425,6 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
         if (branch) in.fetch(1, y.row(row), a.n, at);
         if (stream) in.fetch(2, ds.row(row), a.n, at);
     };
-    in.clear(a.n, at);
     if (VEC > 1) {
         if (i < last) fetch(i);
         in.commit();
@@ -437,23 +440,21 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
             if (VEC == 1 || i + 1 < last) fetch(VEC == 1 ? i : i + 1);
             in.commit();
             in.arrived();
-            if (pre) in.take(0), in.take(3);
-            if (branch) in.take(1);
-            if (stream) in.take(2);
             uint32_t r[COLS / 2];
             if (a.drop) mask.make(a, keep, i, at, r);
-            float2 h[COLS / 2], v[COLS / 2], g[COLS / 2];
+            float2 h[COLS / 2], g[COLS / 2];
             if (branch) {
+                in.get(1, h);
+                if (post) {
 #pragma unroll
-                for (int p = 0; p < COLS / 2; ++p) h[p] = __fmul2_rn(__fadd2_rn(in.get(1, p), pair(-st.x)), pair(st.y));   // no norm: mean 0, deviation 1
+                    for (int p = 0; p < COLS / 2; ++p) h[p] = __fmul2_rn(__fadd2_rn(h[p], pair(-st.x)), pair(st.y));
+                }
             }
-            float c01[2] = {0.f, 0.f}, k01[2] = {0.f, 0.f};
-#pragma unroll
-            for (int p = 0; p < COLS / 2; ++p) g[p] = stream ? in.get(2, p) : pair(0.f);
             if (pre) {
-                joined<VEC, COLS>(a, keep, branch, in, h, r, weight, v);
-                float2 c0 = pair(0.f), c1 = pair(0.f);
-                float2 d[COLS / 2];
+                float2 v[COLS / 2], d[COLS / 2], c0 = pair(0.f), c1 = pair(0.f);
+                in.get(0, v);
+                joined<VEC, COLS>(a, keep, branch, h, r, weight, v);
+                in.get(3, d);
 #pragma unroll
                 for (int q = 0; q < COLS / 4; ++q) {
                     float2 w[2];
@@ -461,29 +462,43 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int p = 2 * q + e;
-                        const float2 z = in.get(3, p);
                         v[p] = __fmul2_rn(__fadd2_rn(v[p], pair(-st.z)), pair(st.w));
-                        sum_pre[p] = __ffma2_rn(z, v[p], sum_pre[p]);
-                        d[p] = __fmul2_rn(z, w[e]);
-                        c0 = __fadd2_rn(c0, d[p]), c1 = __ffma2_rn(d[p], v[p], c1);
+                        sum_pre[p] = __ffma2_rn(d[p], v[p], sum_pre[p]);
+                        d[p] = __fmul2_rn(d[p], w[e]);
+                        c1 = __ffma2_rn(d[p], v[p], c1);
                     }
                 }
-                c01[0] = c0.x + c0.y, c01[1] = c1.x + c1.y;
-                ex.sum(c01);
-                const float2 k0 = pair(a.layer ? -st.w * c01[0] * inv_n : 0.f), k1 = pair(-st.w * c01[1] * inv_n);
+                if (a.layer) {
 #pragma unroll
-                for (int p = 0; p < COLS / 2; ++p) g[p] = __ffma2_rn(v[p], k1, __ffma2_rn(d[p], pair(st.w), __fadd2_rn(g[p], k0)));
+                    for (int p = 0; p < COLS / 2; ++p) c0 = __fadd2_rn(c0, d[p]);
+                }
+                const float2 k01 = row_sums(a, ex, c0, c1);
+                const float2 k0 = pair(-st.w * k01.x * inv_n), k1 = pair(-st.w * k01.y * inv_n);
+                if (stream) {
+                    in.get(2, g);
+                } else {
+#pragma unroll
+                    for (int p = 0; p < COLS / 2; ++p) g[p] = pair(0.f);
+                }
+                if (a.layer) {
+#pragma unroll
+                    for (int p = 0; p < COLS / 2; ++p) g[p] = __fadd2_rn(g[p], k0);
+                }
+#pragma unroll
+                for (int p = 0; p < COLS / 2; ++p) g[p] = __ffma2_rn(v[p], k1, __ffma2_rn(d[p], pair(st.w), g[p]));
+            } else if (stream) {
+                in.get(2, g);
+            } else {
+#pragma unroll
+                for (int p = 0; p < COLS / 2; ++p) g[p] = pair(0.f);
             }
             if (dx.p != nullptr) {
+                float2 v[COLS / 2];
 #pragma unroll
                 for (int p = 0; p < COLS / 2; ++p) v[p] = __fmul2_rn(g[p], pair(a.residual));
-                put<T, VEC, COLS>(dx.row(i), a.n, at, v);
+                in.put(dx.row(i), a.n, at, v);
             }
             if (!branch) continue;
-            if (a.drop) {
-#pragma unroll
-                for (int p = 0; p < COLS / 2; ++p) g[p] = Mask<VEC, COLS>::apply(keep, r[p], g[p]);
-            }
             float2 c0 = pair(0.f), c1 = pair(0.f);
 #pragma unroll
             for (int q = 0; q < COLS / 4; ++q) {
@@ -492,41 +507,61 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int p = 2 * q + e;
+                    if (a.drop) g[p] = Mask<VEC, COLS>::apply(keep, r[p], g[p]);
                     sum_branch[p] = __ffma2_rn(g[p], h[p], sum_branch[p]);
                     g[p] = __fmul2_rn(g[p], w[e]);
-                    c0 = __fadd2_rn(c0, g[p]), c1 = __ffma2_rn(g[p], h[p], c1);
+                    c1 = __ffma2_rn(g[p], h[p], c1);
                 }
             }
             if (dy.p == nullptr) continue;
             if (post) {
-                k01[0] = c0.x + c0.y, k01[1] = c1.x + c1.y;
-                ex.sum(k01);
-                const float2 k0 = pair(a.layer ? -k01[0] * inv_n : 0.f), k1 = pair(-k01[1] * inv_n);
+                if (a.layer) {
 #pragma unroll
-                for (int p = 0; p < COLS / 2; ++p) g[p] = __fmul2_rn(__ffma2_rn(h[p], k1, __fadd2_rn(g[p], k0)), pair(st.y));
+                    for (int p = 0; p < COLS / 2; ++p) c0 = __fadd2_rn(c0, g[p]);
+                }
+                const float2 k01 = row_sums(a, ex, c0, c1);
+                const float2 k0 = pair(-k01.x * inv_n), k1 = pair(-k01.y * inv_n);
+                if (a.layer) {
+#pragma unroll
+                    for (int p = 0; p < COLS / 2; ++p) g[p] = __fadd2_rn(g[p], k0);
+                }
+#pragma unroll
+                for (int p = 0; p < COLS / 2; ++p) g[p] = __fmul2_rn(__ffma2_rn(h[p], k1, g[p]), pair(st.y));
             }
-            put<T, VEC, COLS>(dy.row(i), a.n, at, g);
+            in.put(dy.row(i), a.n, at, g);
         }
         if (out.gate != nullptr || out.post != nullptr) {
 #pragma unroll
-            for (int e = 0; e < COLS; ++e) {
-                const int c = at.of(e);
-                const float sum = a.scale * (e & 1 ? sum_branch[e / 2].y : sum_branch[e / 2].x);
-                if (c < a.n) {
+            for (int q = 0; q < COLS / 4; ++q) {
+                float total[4];
+                float2 before[2];
+                if (post) sum_post.get(q, before);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int c = at.of(4 * q + e), p = 2 * q + e / 2;
+                    const float sum = a.scale * (e & 1 ? sum_branch[p].y : sum_branch[p].x);
+                    total[e] = e & 1 ? before[e / 2].y : before[e / 2].x;
+                    if (c >= a.n) continue;
                     if (out.gate != nullptr) out.gate[k * a.n + c] = post ? a.w_post[c] * sum : sum;
-                    float& to = e & 1 ? sum_post[e / 2].y : sum_post[e / 2].x;
-                    if (post) to = a.gate != nullptr ? fmaf(a.gate[group * a.n + c], sum, to) : to + sum;
+                    total[e] = a.gate != nullptr ? fmaf(a.gate[group * a.n + c], sum, total[e]) : total[e] + sum;
                 }
+                if (post) sum_post.room[q * blockDim.x + threadIdx.x] = make_float4(total[0], total[1], total[2], total[3]);
             }
 #pragma unroll
             for (int p = 0; p < COLS / 2; ++p) sum_branch[p] = pair(0.f);
         }
     }
 #pragma unroll
-    for (int e = 0; e < COLS; ++e) {
-        const int c = at.of(e);
-        if (out.post != nullptr && c < a.n) out.post[static_cast<int64_t>(team) * a.n + c] = e & 1 ? sum_post[e / 2].y : sum_post[e / 2].x;
-        if (out.pre != nullptr && c < a.n) out.pre[static_cast<int64_t>(team) * a.n + c] = e & 1 ? sum_pre[e / 2].y : sum_pre[e / 2].x;
+    for (int q = 0; q < COLS / 4; ++q) {
+        float2 total[2];
+        if (out.post != nullptr) sum_post.get(q, total);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = at.of(4 * q + e), p = 2 * q + e / 2;
+            if (c >= a.n) continue;
+            if (out.post != nullptr) out.post[static_cast<int64_t>(team) * a.n + c] = e & 1 ? total[e / 2].y : total[e / 2].x;
+            if (out.pre != nullptr) out.pre[static_cast<int64_t>(team) * a.n + c] = e & 1 ? sum_pre[p].y : sum_pre[p].x;
+        }
     }
 }
 
@@ -560,14 +595,16 @@ __global__ void __launch_bounds__(256) fold_kernel(const __grid_constant__ Folds
 
 // ---- host side ----------------------------------------------------------------------------------
 
-Parts parts_of(int64_t m, int64_t n, int64_t groups) {
+// columns: how many a thread of the backward kernel has (16: 16-bit rows in words)
+Parts parts_of(int64_t m, int64_t n, int64_t groups, int columns) {
     Parts p;
     p.groups = groups > 0 ? groups : 1;
     p.rows = m / p.groups;
-    // As many as run at a time, but none of fewer than 32 rows: their sums' traffic would show.
-    int64_t per_sm = n <= 8 * kTeam ? 8 * kTeam / (n > 256 ? n : 256) : 1;
-    if (per_sm > 1 && m < per_sm * kNumSMs * 32) per_sm = m / (kNumSMs * 32) > 1 ? m / (kNumSMs * 32) : 1;
-    p.teams = n <= 16 * kTeam ? per_sm * kNumSMs : kNumSMs / 2;   // wider rows take a cluster
+    // As many CTAs as an SM holds (512 threads by their registers, and a little less by the shared memory of small ones), but none of fewer
+    // than 16 rows: their sums' traffic would show.  Wider rows take a cluster.
+    int64_t per_sm = columns * kTeam / (n > 512 ? n : columns == 16 ? 683 : 512);
+    if (per_sm > 1 && m < per_sm * kNumSMs * 16) per_sm = m / (kNumSMs * 16);
+    p.teams = per_sm > 1 ? per_sm * kNumSMs : n <= 16 * kTeam ? kNumSMs : kNumSMs / 2;
     // one group: a part for each CTA; more: four rounds of parts, so that the last round is short
     int64_t per = p.groups == 1 ? p.teams : (4 * p.teams + p.groups - 1) / p.groups;
     p.per_group = per < p.rows ? per : (p.rows > 0 ? p.rows : 1);
@@ -577,8 +614,13 @@ Parts parts_of(int64_t m, int64_t n, int64_t groups) {
 }
 size_t gate_sums(const Parts& p, int64_t n) { return p.per_group > 1 ? static_cast<size_t>(p.count) * n : 0; }
 size_t workspace_of(int64_t m, int64_t n, int64_t groups) {
-    const Parts p = parts_of(m, n, groups);
-    return round_up((gate_sums(p, n) + 2 * static_cast<size_t>(p.teams) * n) * sizeof(float), 256);
+    size_t most = 0;
+    for (int columns : {8, 16}) {
+        const Parts p = parts_of(m, n, groups, columns);
+        const size_t bytes = (gate_sums(p, n) + 2 * static_cast<size_t>(p.teams) * n) * sizeof(float);
+        if (bytes > most) most = bytes;
+    }
+    return round_up(most, 256);
 }
 
 struct JoinTensors {
@@ -600,12 +642,12 @@ bool in_words(const JoinTensors& t, int64_t m, int bytes) {
 struct Shape {
     int threads, ranks, smem;
 };
-template <typename T, int VEC, int COLS> Shape shape_of(int n, int tensors, bool drop) {
+template <typename T, int VEC, int COLS> Shape shape_of(int n, int vectors, int tensors, bool drop) {
     Shape s{32, 1, 0};
     while (s.threads < kTeam && s.threads * COLS < n) s.threads *= 2;
     while (s.threads * COLS * s.ranks < n) s.ranks *= 2;
     const int width = s.threads * COLS;
-    s.smem = width * (8 + (VEC > 1 ? 2 * tensors * static_cast<int>(sizeof(T)) : 0)) + (drop && !(VEC == 8 && n % 8 == 0) ? 2 * 2 * (width + 16) : 0);
+    s.smem = width * (4 * vectors + (VEC > 1 ? 2 * tensors * static_cast<int>(sizeof(T)) : 0)) + (drop && !(VEC == 8 && n % 8 == 0) ? 2 * 2 * (width + 16) : 0);
     return s;
 }
 // teams: clusters of s.ranks CTAs
@@ -627,20 +669,23 @@ template <typename K, typename... A> int start(K kern, const Shape& s, int64_t t
     note_launch();
     return check_launch();
 }
-template <typename T, int VEC, int COLS> int most_smem(int tensors) { return kTeam * COLS * (8 + (VEC > 1 ? 2 * tensors * static_cast<int>(sizeof(T)) : 0)) + 2 * 2 * (kTeam * COLS + 16); }
+template <typename T, int VEC, int COLS> int most_smem(int vectors, int tensors) {
+    const int all = kTeam * COLS * (4 * vectors + (VEC > 1 ? 2 * tensors * static_cast<int>(sizeof(T)) : 0)) + 2 * 2 * (kTeam * COLS + 16), limit = 227 * 1024 - 1024;
+    return all < limit ? all : limit;
+}
 
 template <typename T, int VEC, int COLS> int forward_as(const JoinArgs& a, const JoinTensors& t, cudaStream_t s) {
-    const Shape shape = shape_of<T, VEC, COLS>(a.n, 2, a.drop != 0);
-    // as many as fit an SM
-    int per_sm = 1024 / shape.threads;
+    const Shape shape = shape_of<T, VEC, COLS>(a.n, 2, 2, a.drop != 0);
+    // as many as an SM holds, by their registers and by their shared memory
+    int per_sm = (COLS == 8 && VEC == 8 ? 768 : 512) / shape.threads;
     if (per_sm * (shape.smem + 2048) > 220 * 1024) per_sm = 220 * 1024 / (shape.smem + 2048);
     const int64_t most = static_cast<int64_t>(per_sm > 1 ? per_sm : 1) * kNumSMs / shape.ranks;
-    return start(join_kernel<T, VEC, COLS>, shape, a.m < most ? a.m : most, most_smem<T, VEC, COLS>(2), s, a, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
+    return start(join_kernel<T, VEC, COLS>, shape, a.m < most ? a.m : most, most_smem<T, VEC, COLS>(2, 2), s, a, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
                  JoinRows<const T>{static_cast<const T*>(t.b), t.ld_b}, JoinRows<T>{static_cast<T*>(t.e), t.ld_e}, JoinRows<T>{static_cast<T*>(t.f), t.ld_f});
 }
 template <typename T, int VEC, int COLS> int backward_as(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, cudaStream_t s) {
-    const Shape shape = shape_of<T, VEC, COLS>(a.n, 4, a.drop != 0);
-    return start(join_backward_kernel<T, VEC, COLS>, shape, p.teams, most_smem<T, VEC, COLS>(4), s, a, p, sums, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
+    const Shape shape = shape_of<T, VEC, COLS>(a.n, 3, 4, a.drop != 0);
+    return start(join_backward_kernel<T, VEC, COLS>, shape, p.teams, most_smem<T, VEC, COLS>(3, 4), s, a, p, sums, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
                  JoinRows<const T>{static_cast<const T*>(t.b), t.ld_b}, JoinRows<const T>{static_cast<const T*>(t.c), t.ld_c}, JoinRows<const T>{static_cast<const T*>(t.d), t.ld_d},
                  JoinRows<T>{static_cast<T*>(t.e), t.ld_e}, JoinRows<T>{static_cast<T*>(t.f), t.ld_f});
 }
@@ -650,11 +695,14 @@ template <typename T> int forward(const JoinArgs& a, const JoinTensors& t, cudaS
     if (!in_words(t, a.m, sizeof(T))) return forward_as<T, 1, 8>(a, t, s);
     return a.n <= 8 * 256 ? forward_as<T, N, 8>(a, t, s) : forward_as<T, N, 16>(a, t, s);
 }
-template <typename T> int backward(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, cudaStream_t s) {
+// Columns of a thread of the backward kernel.  Sixteen keep two CTAs on an SM at 4096 columns; with random numbers of odd rows beside them
+// their shared memory ends at 4096.
+int backward_columns(int64_t n, int bytes, bool words, bool drop) { return bytes == 2 && words && n > 256 && (n <= 8 * kTeam || n % 8 == 0 || !drop) ? 16 : 8; }
+template <typename T> int backward(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, bool words, int columns, cudaStream_t s) {
     constexpr int N = Word<T>::kN;
-    if (!in_words(t, a.m, sizeof(T))) return backward_as<T, 1, 8>(a, t, p, sums, s);
+    if (!words) return backward_as<T, 1, 8>(a, t, p, sums, s);
     if constexpr (sizeof(T) == 2)
-        if (a.n > 8 * kTeam) return backward_as<T, N, 16>(a, t, p, sums, s);
+        if (columns == 16) return backward_as<T, N, 16>(a, t, p, sums, s);
     return backward_as<T, N, 8>(a, t, p, sums, s);
 }
 
@@ -666,13 +714,13 @@ bool far_apart(const JoinTensors& t) {
     const int64_t lim = int64_t(1) << 31;
     return t.ld_a >= lim || t.ld_b >= lim || t.ld_c >= lim || t.ld_d >= lim || t.ld_e >= lim || t.ld_f >= lim;
 }
-bool words(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+bool on_float(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // What both calls check of sizes and form; `least` gets the dropout threshold.
 int check(int dtype, int64_t m, int64_t n, int norm, float eps, const void* y, const float* w_post, const float* gate, int64_t groups, float residual,
           float branch, double rate, const uint64_t* rng, const float* w_pre, const void* stats, uint32_t* least) {
     if (element_bytes(dtype) == 0 || m < 0 || n < 0 || (norm != BZ_NORM_RMS && norm != BZ_NORM_LAYER) || groups < 0 || !isfinite(residual) || !isfinite(branch) ||
-        !(eps >= 0.f) || isinf(eps) || !drop_threshold(rate, least) || !aligned16(stats) || !aligned8(rng) || !words(w_post) || !words(gate) || !words(w_pre))
+        !(eps >= 0.f) || isinf(eps) || !drop_threshold(rate, least) || !aligned16(stats) || !aligned8(rng) || !on_float(w_post) || !on_float(gate) || !on_float(w_pre))
         return BZ_ERR_INVALID_ARG;
     if (m >= (int64_t(1) << 31) || n > BZ_MAX_WIDTH || groups >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
     if ((gate != nullptr) != (groups > 0) || (groups > 0 && m % groups != 0)) return BZ_ERR_INVALID_ARG;
@@ -733,8 +781,8 @@ extern "C" int bz_join_backward(const void* x, int64_t ld_x, const void* y, int6
     const int bytes = element_bytes(dtype);
     JoinTensors t{x, y, ds, dz, ld_x, ld_y, ld_ds, ld_dz, dx, dy, ld_dx, ld_dy};
     const bool pre = dz != nullptr && w_pre != nullptr, sums = dw_post != nullptr || dgate != nullptr || dw_pre != nullptr;
-    if ((dw_post != nullptr && w_post == nullptr) || (dgate != nullptr && gate == nullptr) || (dw_pre != nullptr && w_pre == nullptr) || !words(dw_post) || !words(dgate) ||
-        !words(dw_pre))
+    if ((dw_post != nullptr && w_post == nullptr) || (dgate != nullptr && gate == nullptr) || (dw_pre != nullptr && w_pre == nullptr) || !on_float(dw_post) || !on_float(dgate) ||
+        !on_float(dw_pre))
         return BZ_ERR_INVALID_ARG;
     if (n == 0) return BZ_OK;
     if (dx == nullptr && dy == nullptr && !sums) return m == 0 ? BZ_OK : BZ_ERR_INVALID_ARG;
@@ -744,7 +792,9 @@ extern "C" int bz_join_backward(const void* x, int64_t ld_x, const void* y, int6
                   !good(dx, ld_dx, m, n, bytes) || !good(dy, ld_dy, m, n, bytes)))
         return BZ_ERR_INVALID_ARG;
     if (m > 1 && far_apart(t)) return BZ_ERR_UNSUPPORTED;
-    const Parts p = parts_of(m, n, groups);
+    const bool words = in_words(t, m, bytes);
+    const int columns = backward_columns(n, bytes, words, least != 0);
+    const Parts p = parts_of(m, n, groups, columns);
     if (sums && (workspace == nullptr || !aligned256(workspace) || workspace_bytes < workspace_of(m, n, groups))) return BZ_ERR_WORKSPACE;
     float* room = static_cast<float*>(workspace);
     Sums partial{};
@@ -761,8 +811,8 @@ extern "C" int bz_join_backward(const void* x, int64_t ld_x, const void* y, int6
     if (dgate != nullptr) partial.gate = p.per_group > 1 ? fold(dgate, p.groups, p.per_group) : dgate;
     const JoinArgs a = join_args(m, n, norm, 0.f, w_post, gate, groups, residual_scale, branch_scale, least, rng, w_pre, stats);
     cudaStream_t stream_ = static_cast<cudaStream_t>(stream);
-    const int done = dtype == BZ_F32 ? backward<float>(a, t, p, partial, stream_) : dtype == BZ_F16 ? backward<__half>(a, t, p, partial, stream_)
-                                                                                              : backward<__nv_bfloat16>(a, t, p, partial, stream_);
+    const int done = dtype == BZ_F32 ? backward<float>(a, t, p, partial, words, columns, stream_) : dtype == BZ_F16 ? backward<__half>(a, t, p, partial, words, columns, stream_)
+                                                                                              : backward<__nv_bfloat16>(a, t, p, partial, words, columns, stream_);
     if (done != BZ_OK || count == 0) return done;
     int64_t rows = 1;
     for (int k = 0; k < count; ++k) rows = rows > folds.f[k].rows ? rows : folds.f[k].rows;

@@ -146,7 +146,7 @@ def test_tensors_that_require_a_gradient():
 
 
 def test_workspace_of_many_groups(L):
-    """A part each once there are many groups: dgate needs no sums then."""
-    some = L.bz_join_workspace_bytes(1 << 20, 1024, 1 << 20)
-    assert some == 2 * 148 * 1024 * 4
-    assert L.bz_join_workspace_bytes(1 << 20, 1024, 0) == 3 * 148 * 1024 * 4
+    """A part each once there are many groups: dgate needs no sums then, and the bytes do not grow with them."""
+    size = L.bz_join_workspace_bytes
+    assert 0 < size(1 << 20, 1024, 1 << 20) < size(1 << 20, 1024, 1) == size(1 << 20, 1024, 0)
+    assert size(1 << 20, 1024, 1 << 19) == size(1 << 20, 1024, 1 << 20)
