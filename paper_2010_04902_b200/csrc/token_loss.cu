@@ -2,17 +2,29 @@
 //
 // Both rest on lp = z[a] - log(sum of exp z), z = logits / T, and on one number a row, the slope d loss / d lp:
 // dlogits = dloss * slope / T * ([c == a] - softmax(z)[c]).
+//
+// Exponents.  A sum over a sequence adds up the errors of its lp, and a factor log2(e)/T rounded to binary32 is wrong to the same
+// side in all of them; so exponents are (s - m) c + (s - m) c_low with the rounding's rest c_low, relative to an m that is subtracted exactly.
+#include <cooperative_groups.h>
+
 #include "worker_common.cuh"
 
 namespace bz {
 
 namespace {
 
+namespace cg = cooperative_groups;
+
+constexpr int kTeam = 512;      // threads of a CTA at most
+constexpr int kMostRanks = 8;   // CTAs of a cluster: the portable size
+
 struct TokenArgs {
-    int64_t ld, v, ld_d;
+    int64_t m, ld, v, ld_d;
     const int32_t* index;
+    Extent extent;            // of the logits
     double inv_t;             // 1 / T
-    float temperature, c;     // c = log2(e) / T
+    float temperature;
+    float c, c_low;           // log2(e) / T = c + c_low, c_low > 0: what is infinite stays so
     const float *old_logp, *ref_logp, *advantage;
     float clip_low, clip_high, kl;
     const float* dloss;
@@ -20,117 +32,362 @@ struct TokenArgs {
     float4* stats;            // largest logit, sum of e^((s - that)/T), slope, place in dloss
 };
 
+__device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
+// 2^(exponent of d = s - reference)
+__device__ __forceinline__ float power(const TokenArgs& a, float d) { return exp2_fast(fmaf(d, a.c, d * a.c_low)); }
+__device__ __forceinline__ float2 powers(const TokenArgs& a, float2 s, float reference) {
+    const float2 d = __fadd2_rn(s, pair(-reference)), y = __ffma2_rn(d, pair(a.c), __fmul2_rn(d, pair(a.c_low)));
+    return make_float2(exp2_fast(y.x), exp2_fast(y.y));
+}
+// What exponents are relative to: the largest, but 0 where everything is -inf.
+__device__ __forceinline__ float reference_of(float largest) { return largest == -INFINITY ? 0.f : largest; }
+// The parts of a warp's lanes as one.
+__device__ __forceinline__ MaxSum joined(const TokenArgs& a, const MaxSum& v) {
+    const float m = warp_max(v.m);
+    return {m, warp_sum(v.s == 0.f ? 0.f : v.s * power(a, v.m - reference_of(m)))};
+}
+
 // lp of a logit in a row of maximum m and sum s.
 __device__ __forceinline__ double log_probability(float logit, float m, float s, double inv_t) {
     if (logit == -INFINITY) return -INFINITY;
     return (static_cast<double>(logit) - static_cast<double>(m)) * inv_t - log(static_cast<double>(s));
 }
 
+struct RowInputs {   // loaded a row ahead
+    float old_logp, ref_logp, advantage, dloss;
+};
 struct PolicyRow {
     float loss, slope;
 };
-__device__ __forceinline__ PolicyRow policy_row(const TokenArgs& a, int64_t i, double lp) {
+__device__ __forceinline__ PolicyRow policy_row(const TokenArgs& a, const RowInputs& in, double lp) {
     double loss = 0.0, slope = 0.0;
-    const double adv = a.advantage[i];
+    const double adv = in.advantage;
     if (adv != 0.0) {   // a NaN goes on
-        const double r = a.old_logp != nullptr ? exp(lp - static_cast<double>(a.old_logp[i])) : 1.0;
+        const double r = a.old_logp != nullptr ? exp(lp - static_cast<double>(in.old_logp)) : 1.0;
         const double lo = 1.0 - static_cast<double>(a.clip_low), hi = 1.0 + static_cast<double>(a.clip_high);
         const bool held = adv > 0.0 ? r > hi : adv < 0.0 && r < lo;
         loss = -(held ? (adv > 0.0 ? hi : lo) : r) * adv;
         slope = held ? 0.0 : -r * adv;
     }
     if (a.kl != 0.f) {
-        const double d = static_cast<double>(a.ref_logp[i]) - lp, e = expm1(d), k = a.kl;
+        const double d = static_cast<double>(in.ref_logp) - lp, e = expm1(d), k = a.kl;
         loss += k * (isinf(e) ? e : e - d);
         slope -= k * e;
     }
     return {static_cast<float>(loss), lp == -INFINITY ? 0.f : static_cast<float>(slope)};
 }
 
-// The largest of a row and its sum of exponentials, over the CTA.
-template <typename T, int VEC> __device__ __forceinline__ MaxSum row_statistics(const T* row, int64_t v, float c, MaxSum* part) {
-    MaxSum mine{-INFINITY, 0.f};
-    float x[VEC];
-    for (int64_t j0 = static_cast<int64_t>(threadIdx.x) * VEC - row_lead<T, VEC>(row); j0 < v; j0 += blockDim.x * VEC) {
-        load_slot<T, VEC>(row, j0, v, -INFINITY, x);
-        const float m = largest(mine.m, x);
-        const Reference r(m, c);
-        if (mine.s != 0.f) mine.s *= exp2_fast(r.of_part(mine.m, c));
-        mine.m = m;
-        exponentials(x, r, c);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) mine.s += x[k];
+__device__ __forceinline__ bool has_token(const TokenArgs& a, int at) { return at >= 0 && at < a.v; }
+
+// What one thread does of a row with a token: its scalars, and the factor of the gradient (0: none).
+template <bool POLICY> __device__ __forceinline__ RowInputs row_inputs(const TokenArgs& a, int64_t i) {
+    RowInputs r{0.f, 0.f, 0.f, 1.f};
+    if (POLICY) {
+        if (a.old_logp != nullptr) r.old_logp = __ldg(a.old_logp + i);
+        if (a.ref_logp != nullptr) r.ref_logp = __ldg(a.ref_logp + i);
+        r.advantage = __ldg(a.advantage + i);
+        if (a.dloss != nullptr) r.dloss = __ldg(a.dloss + i);
     }
-    mine = warp_join(mine, c);
+    return r;
+}
+template <bool POLICY> __device__ __forceinline__ float finish_row(const TokenArgs& a, int64_t i, const RowInputs& in, float logit, const MaxSum& all, bool write) {
+    const double lp = log_probability(logit, all.m, all.s, a.inv_t);
+    PolicyRow p{0.f, 0.f};
+    if (POLICY) p = policy_row(a, in, lp);
+    if (write) {
+        if (a.logp != nullptr) a.logp[i] = static_cast<float>(lp);
+        if (POLICY && a.loss != nullptr) a.loss[i] = p.loss;
+        if (a.stats != nullptr) a.stats[i] = make_float4(all.m, all.s, p.slope, __int_as_float(static_cast<int>(i)));
+    }
+    return p.slope == 0.f ? 0.f : p.slope * in.dloss / a.temperature;
+}
+__device__ __forceinline__ void finish_without(const TokenArgs& a, int64_t i, bool policy) {
+    if (a.logp != nullptr) a.logp[i] = 0.f;
+    if (policy && a.loss != nullptr) a.loss[i] = 0.f;
+    if (a.stats != nullptr) a.stats[i] = make_float4(-INFINITY, 0.f, 0.f, __int_as_float(static_cast<int>(i)));
+}
+
+// ---- a row in a CTA's or a cluster's shared memory -----------------------------------------------
+//
+// A thread copies its own 16-byte words of the row (cp.async, four groups), takes each group into its largest logit and sum as it
+// arrives, and with a gradient passes over them again out of shared memory: the row comes from memory once.  The row's maximum and
+// sum cost one exchange, the scalars of its loss one thread in binary64.  Nothing of a row overlaps inside its CTA but the loads; three CTAs or
+// more on an SM, each at another point of its row, do that.  (Rows kept as exponentials in registers with the next one on its way,
+// two CTAs an SM: 148 us at 4096 x 32128 bfloat16 with the gradient.  Rows through a ring with warps for each part of the work: 170 us, most of
+// it bookkeeping of sixteen warps for rows of four chunks.)
+
+constexpr int kQuarters = 4;     // groups of copies
+constexpr int kBatch = 4;        // words a thread works on at a time
+constexpr int kMostWords = 227 * 1024 / 16 - 64;   // of a CTA
+
+struct RowShare {
+    int ranks, words;   // CTAs of a row; words of a CTA at most
+};
+
+template <typename T, bool POLICY, bool GRADIENT>
+__global__ void __launch_bounds__(kTeam) token_shared_kernel(const __grid_constant__ TokenArgs a, const RowShare share, const T* logits, T* dlogits) {
+    constexpr int N = Word<T>::kN;
+    extern __shared__ __align__(16) uint4 held[];
+    __shared__ MaxSum part[16], peers[kMostRanks];
+    __shared__ float3 outcome;   // the row's largest, the exponentials' factor, the gradient's
+    const int threads = blockDim.x, t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const int64_t i = blockIdx.x / share.ranks;
+    const int rank = static_cast<int>(blockIdx.x - i * share.ranks);
+    if (share.ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // every CTA of the cluster has started
+    const int at = __ldg(a.index + i);
+    const T* row = logits + i * a.ld;
+    const int n = static_cast<int>(a.v), lead = row_lead<T, N>(row);
+    // this CTA's words [begin, end) of the row's, counted from the 16-byte boundary at or before it
+    const int all = (lead + n + N - 1) / N, begin = rank * share.words, end = min(begin + share.words, all);
+    const int mine = max((end - begin - t + threads - 1) / threads, 0);   // words begin + t + q threads, q < mine
+    const int first_word = begin + t, last_word = begin + t + (mine - 1) * threads;
+    // words over an end of the row: this thread's first, its last
+    const bool over_first = mine > 0 && first_word == 0 && lead != 0, over_last = mine > 0 && last_word == all - 1 && (lead + n) % N != 0;
+    const bool there = has_token(a, at);
+    T* out = GRADIENT ? dlogits + i * a.ld_d : nullptr;
+    float g = 0.f, f = 0.f, ref = 0.f;
+    RowInputs in{};
+    float logit = 0.f;
+    if (there) {
+        const uint4* from = reinterpret_cast<const uint4*>(row - lead) + first_word;
+        const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(held + t));
+        const int quarter = (mine + kQuarters - 1) / kQuarters;
+#pragma unroll
+        for (int k = 0; k < kQuarters; ++k) {
+            for (int q = k * quarter; q < min((k + 1) * quarter, mine); ++q)
+                if (!(over_first && q == 0) && !(over_last && q == mine - 1))
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + q * threads * 16), "l"(from + static_cast<int64_t>(q) * threads) : "memory");
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        if (t == 0) in = row_inputs<POLICY>(a, i), logit = to_f32(row[at]);
+        if (over_first || over_last) {   // element by element, -inf in the place of what is not the row's
+            rare();
+            float x[N];
+            if (over_first) {
+                load_slot<T, N>(row, -lead, n, -INFINITY, x);
+                held[t] = Word<T>::pack(x);
+            }
+            if (over_last) {
+                load_slot<T, N>(row, static_cast<int64_t>(all - 1) * N - lead, n, -INFINITY, x);
+                held[t + (mine - 1) * threads] = Word<T>::pack(x);
+            }
+        }
+        MaxSum sum{-INFINITY, 0.f};
+        auto absorb = [&](auto& x) {
+            float top = sum.m;
+            for (auto& w : x) top = largest(top, w);
+            const float r = reference_of(top);
+            float2 s0 = make_float2(sum.s == 0.f ? 0.f : sum.s * power(a, sum.m - r), 0.f), s1 = pair(0.f);
+            for (auto& w : x) {
+#pragma unroll
+                for (int e = 0; e < N; e += 4) {
+                    s0 = __fadd2_rn(s0, powers(a, make_float2(w[e], w[e + 1]), r));
+                    s1 = __fadd2_rn(s1, powers(a, make_float2(w[e + 2], w[e + 3]), r));
+                }
+            }
+            s0 = __fadd2_rn(s0, s1);
+            sum = {top, s0.x + s0.y};
+        };
+#pragma unroll
+        for (int k = 0; k < kQuarters; ++k) {
+            if (k == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
+            if (k == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
+            if (k == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            if (k == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
+            const int to_q = min((k + 1) * quarter, mine);
+            int q = k * quarter;
+#pragma unroll 1
+            for (; q + kBatch <= to_q; q += kBatch) {
+                float x[kBatch][N];
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) Word<T>::unpack(held[t + (q + j) * threads], x[j]);
+                absorb(x);
+            }
+#pragma unroll 1
+            for (; q < to_q; ++q) {
+                float x[1][N];
+                Word<T>::unpack(held[t + q * threads], x[0]);
+                absorb(x);
+            }
+        }
+        sum = joined(a, sum);
+        if (lane == 0) part[warp] = sum;
+        __syncthreads();
+        if (share.ranks > 1) {
+            cg::cluster_group cluster = cg::this_cluster();
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if (warp == 0) {
+                sum = joined(a, lane < (threads >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f});
+                if (lane < share.ranks) *cluster.map_shared_rank(&peers[rank], lane) = sum;
+            }
+            cluster.sync();
+        }
+        if (warp == 0) {
+            sum = joined(a, share.ranks > 1 ? (lane < share.ranks ? peers[lane] : MaxSum{-INFINITY, 0.f}) : (lane < (threads >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f}));
+            if (lane == 0) {
+                const float got = finish_row<POLICY>(a, i, in, logit, sum, rank == 0);
+                outcome = make_float3(sum.m, got == 0.f ? 0.f : -got / sum.s, got);
+            }
+        }
+        if (!GRADIENT) return;
+        __syncthreads();
+        ref = reference_of(outcome.x), f = outcome.y, g = outcome.z;
+    } else {
+        if (share.ranks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (t == 0 && rank == 0) finish_without(a, i, POLICY);
+        if (!GRADIENT) return;
+    }
+    uint4* to = reinterpret_cast<uint4*>(out - lead) + first_word;
+    const int from_q = over_first ? 1 : 0, to_q = over_last ? mine - 1 : mine;
+    if (g == 0.f) {
+        for (int q = from_q; q < to_q; ++q) to[static_cast<int64_t>(q) * threads] = make_uint4(0, 0, 0, 0);
+    } else {
+        auto finish = [&](float (&x)[N]) {
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const float2 y = __fmul2_rn(powers(a, make_float2(x[e], x[e + 1]), ref), pair(f));
+                x[e] = y.x, x[e + 1] = y.y;
+            }
+        };
+        int q = from_q;
+#pragma unroll 1
+        for (; q + kBatch <= to_q; q += kBatch) {
+            float x[kBatch][N];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) Word<T>::unpack(held[t + (q + j) * threads], x[j]);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) finish(x[j]), to[static_cast<int64_t>(q + j) * threads] = Word<T>::pack(x[j]);
+        }
+#pragma unroll 1
+        for (; q < to_q; ++q) {
+            float x[N];
+            Word<T>::unpack(held[t + q * threads], x);
+            finish(x), to[static_cast<int64_t>(q) * threads] = Word<T>::pack(x);
+        }
+    }
+    if (over_first || over_last) {
+        rare();
+        for (int which = 0; which < 2; ++which) {
+            if (which == 0 ? !over_first : !over_last || (over_first && mine == 1)) continue;
+            const int word = which == 0 ? first_word : last_word;
+            float x[N];
+            Word<T>::unpack(held[word - begin], x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[e] = g == 0.f ? 0.f : power(a, x[e] - ref) * f;
+            store_slot<T, N>(out, static_cast<int64_t>(word) * N - lead, n, x);
+        }
+    }
+    if (g != 0.f) {   // the token's place, once more, by the thread that has just written it
+        const int word = (at + lead) / N - begin;
+        if (word >= 0 && word < end - begin && word % threads == t) {
+            const int e = (at + lead) % N;
+            out[at] = from_f32<T>(fmaf(power(a, to_f32(reinterpret_cast<const T*>(held + word)[e]) - ref), f, g));
+        }
+    }
+}
+
+// ---- any length and layout: the row is read twice -----------------------------------------------------------
+
+// The largest of a row and its sum of exponentials, over the CTA.
+template <typename T, int VEC> __device__ __forceinline__ MaxSum row_statistics(const TokenArgs& a, const T* row, MaxSum* part) {
+    MaxSum mine{-INFINITY, 0.f};
+    for (int64_t j0 = static_cast<int64_t>(threadIdx.x) * VEC - row_lead<T, VEC>(row); j0 < a.v; j0 += blockDim.x * VEC) {
+        float x[VEC];
+        load_slot<T, VEC>(row, j0, a.v, -INFINITY, x);
+        const float m = largest(mine.m, x), ref = reference_of(m);
+        if (mine.s != 0.f) mine.s *= power(a, mine.m - ref);
+        mine.m = m;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) mine.s += power(a, x[k] - ref);
+    }
+    mine = joined(a, mine);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = mine;
     __syncthreads();
     const int lane = threadIdx.x & 31;
-    return warp_join(lane < (blockDim.x >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f}, c);
-}
-
-// g ([c == a] - softmax); g == 0: zeros, whatever the logits.
-template <typename T, int VEC> __device__ __forceinline__ void row_gradient(const T* row, T* out, int64_t v, int a, float c, MaxSum all, float g) {
-    const Reference r(all.m, c);
-    const float factor = g == 0.f ? 0.f : -g / all.s;
-    for (int64_t j0 = static_cast<int64_t>(threadIdx.x) * VEC - row_lead<T, VEC>(row); j0 < v; j0 += blockDim.x * VEC) {
-        float x[VEC];
-        if (g == 0.f) {
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) x[k] = 0.f;
-        } else {
-            load_slot<T, VEC>(row, j0, v, -INFINITY, x);
-            exponentials(x, r, c);
-            multiply(x, factor);
-#pragma unroll
-            for (int k = 0; k < VEC; ++k)
-                if (j0 + k == a) x[k] += g;
-        }
-        store_slot<T, VEC>(out, j0, v, x);
-    }
+    return joined(a, lane < (blockDim.x >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f});
 }
 
 // One CTA a row.  POLICY: the loss too, and the gradient if it is wanted; otherwise lp and stats alone.
-template <typename T, int VEC, bool POLICY> __global__ void __launch_bounds__(512) token_rows_kernel(const __grid_constant__ TokenArgs a, const T* logits, T* dlogits) {
+template <typename T, int VEC, bool POLICY> __global__ void __launch_bounds__(kTeam) token_rows_kernel(const __grid_constant__ TokenArgs a, const T* logits, T* dlogits) {
     __shared__ MaxSum part[32];
-    __shared__ float slope;
+    __shared__ float factor;
     const int64_t i = blockIdx.x;
     const T* row = logits + i * a.ld;
     const int at = a.index[i];
-    const bool there = at >= 0 && at < a.v;
+    const bool there = has_token(a, at);
     MaxSum all{-INFINITY, 0.f};
-    if (there) all = row_statistics<T, VEC>(row, a.v, a.c, part);
+    if (there) all = row_statistics<T, VEC>(a, row, part);
     if (threadIdx.x == 0) {
-        float4 st = make_float4(-INFINITY, 0.f, 0.f, __int_as_float(static_cast<int>(i)));
-        float lp = 0.f, loss = 0.f;
-        if (there) {
-            st.x = all.m, st.y = all.s / Reference(all.m, a.c).left_out(a.c);
-            const double precise = log_probability(to_f32(row[at]), st.x, st.y, a.inv_t);
-            lp = static_cast<float>(precise);
-            if (POLICY) {
-                const PolicyRow p = policy_row(a, i, precise);
-                loss = p.loss, st.z = p.slope;
-            }
-        }
-        if (a.logp != nullptr) a.logp[i] = lp;
-        if (POLICY && a.loss != nullptr) a.loss[i] = loss;
-        if (a.stats != nullptr) a.stats[i] = st;
-        slope = st.z;
+        factor = 0.f;
+        if (there)
+            factor = finish_row<POLICY>(a, i, row_inputs<POLICY>(a, i), to_f32(row[at]), all, true);
+        else
+            finish_without(a, i, POLICY);
     }
     if (!POLICY || dlogits == nullptr) return;
     __syncthreads();
-    const float g = slope == 0.f ? 0.f : slope * (a.dloss != nullptr ? a.dloss[i] : 1.f) / a.temperature;
-    row_gradient<T, VEC>(row, dlogits + i * a.ld_d, a.v, at, a.c, all, g);
+    const float g = factor, f = g == 0.f ? 0.f : -g / all.s, ref = reference_of(all.m);
+    T* out = dlogits + i * a.ld_d;
+    for (int64_t j0 = static_cast<int64_t>(threadIdx.x) * VEC - row_lead<T, VEC>(row); j0 < a.v; j0 += blockDim.x * VEC) {
+        float x[VEC];
+        load_slot<T, VEC>(row, j0, a.v, -INFINITY, x);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) x[k] = g == 0.f ? 0.f : power(a, x[k] - ref) * f + (j0 + k == at ? g : 0.f);
+        store_slot<T, VEC>(out, j0, a.v, x);
+    }
 }
 
-// The gradient from given stats.
-template <typename T, int VEC> __global__ void __launch_bounds__(512) token_gradient_kernel(const __grid_constant__ TokenArgs a, const T* logits, T* dlogits) {
-    const int64_t i = gridDim.x - 1 - blockIdx.x;
+// ---- the gradient from given stats ---------------------------------------------------------------
+
+// CTA (row, share): shares of kShare elements; the last rows first, as far as the L2 still holds them.
+constexpr int kGradientThreads = 256, kGradientColumns = 32, kShare = kGradientThreads * kGradientColumns;
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const __grid_constant__ TokenArgs a, const T* logits, T* dlogits, int shares) {
+    constexpr int kSlots = kGradientColumns / VEC;
+    const int64_t k = gridDim.x - 1 - blockIdx.x, i = k / shares;
     const T* row = logits + i * a.ld;
+    T* out = dlogits + i * a.ld_d;
+    const int64_t base = k % shares * kShare - row_lead<T, VEC>(row);
+    auto first = [&](int q) { return base + (q * kGradientThreads + static_cast<int64_t>(threadIdx.x)) * VEC; };
+    Raw<T, VEC> raw[kSlots];
+    const bool safe = a.extent.around(row, a.v);
+    auto whole = [&](int64_t j0) { return j0 < a.v && (safe || (j0 >= 0 && j0 + VEC <= a.v)); };
+#pragma unroll
+    for (int q = 0; q < kSlots; ++q) raw[q].fetch(row + first(q), whole(first(q)));
     const float4 st = a.stats[i];
     const int at = a.index[i];
-    const bool there = at >= 0 && at < a.v;
-    const float g = st.z == 0.f || !there ? 0.f : st.z * (a.dloss != nullptr ? a.dloss[__float_as_int(st.w)] : 1.f) / a.temperature;
-    row_gradient<T, VEC>(row, dlogits + i * a.ld_d, a.v, at, a.c, {st.x, st.y * Reference(st.x, a.c).left_out(a.c)}, g);
+    const float g = st.z == 0.f || !has_token(a, at) ? 0.f : st.z * (a.dloss != nullptr ? a.dloss[__float_as_int(st.w)] : 1.f) / a.temperature;
+    const float f = g == 0.f ? 0.f : -g / st.y, ref = reference_of(st.x);
+#pragma unroll
+    for (int q = 0; q < kSlots; ++q) {
+        const int64_t j0 = first(q);
+        if (j0 >= a.v) continue;
+        float x[VEC];
+        raw[q].get(x);
+        if (!whole(j0)) read_apart<T, VEC>(row, j0, a.v, x);
+        if constexpr (VEC == 1) {
+            x[0] = power(a, x[0] - ref);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2) {
+                const float2 y = powers(a, make_float2(x[e], x[e + 1]), ref);
+                x[e] = y.x, x[e + 1] = y.y;
+            }
+        }
+        multiply(x, f);
+        if (g == 0.f) {
+            rare();
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[e] = 0.f;
+        }
+        if (static_cast<uint64_t>(at - j0) < static_cast<uint64_t>(VEC)) {
+            rare();
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (j0 + e == at) x[e] += g;
+        }
+        store_slot<T, VEC>(out, j0, a.v, x);
+    }
 }
 
 struct PairArgs {
@@ -214,14 +471,57 @@ __global__ void token_empty_kernel(int64_t m, float* loss, float* logp, float4* 
 
 enum What { kPolicy, kScore, kGradient };
 
-template <typename T, int VEC> int launch(const TokenArgs& a, int64_t m, const T* logits, T* dlogits, What what, cudaStream_t s) {
-    const unsigned rows = static_cast<unsigned>(m);
-    if (what == kPolicy)
-        token_rows_kernel<T, VEC, true><<<rows, 512, 0, s>>>(a, logits, dlogits);
-    else if (what == kScore)
-        token_rows_kernel<T, VEC, false><<<rows, 512, 0, s>>>(a, logits, dlogits);
-    else
-        token_gradient_kernel<T, VEC><<<rows, 512, 0, s>>>(a, logits, dlogits);
+template <typename T, bool POLICY, bool GRADIENT> int shared(const TokenArgs& a, const T* logits, T* dlogits, int64_t words, int ranks, cudaStream_t s) {
+    RowShare share{ranks, static_cast<int>((words + ranks - 1) / ranks)};
+    // up to sixteen words a thread; where few rows leave SMs idle, four
+    const int each = a.m * ranks <= kNumSMs ? 4 : 16;
+    int threads = (share.words + each * 32 - 1) / (each * 32) * 32;
+    const int most = a.m * ranks <= kNumSMs ? kTeam : 256;
+    if (threads > most) threads = most;
+    auto kern = token_shared_kernel<T, POLICY, GRADIENT>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostWords * 16);
+    if (e != cudaSuccess) return cuda_failed(e);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.m * ranks));
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = static_cast<size_t>(share.words) * 16;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {static_cast<unsigned>(ranks), 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = ranks > 1 ? 1 : 0;
+    e = cudaLaunchKernelEx(&cfg, kern, a, share, logits, dlogits);
+    if (e != cudaSuccess) return cuda_failed(e);
+    note_launch();
+    return check_launch();
+}
+
+template <typename T, int VEC, bool POLICY> int rows(const TokenArgs& a, const T* logits, T* dlogits, cudaStream_t s) {
+    if constexpr (VEC > 1) {
+        const int64_t words = (a.v + 2 * (VEC - 1)) / VEC;   // of a row, at most
+        // three CTAs an SM; a cluster's CTAs hold what they can of the longest rows
+        int64_t ranks = (words + 4607) / 4608;
+        if (ranks > kMostRanks) ranks = kMostRanks;
+        while (ranks < kMostRanks && a.m * ranks * 2 <= kNumSMs && words > ranks * 256) ranks *= 2;   // few rows: on more SMs
+        if (ranks > kMostRanks) ranks = kMostRanks;
+        if ((words + ranks - 1) / ranks <= kMostWords && a.m * ranks < (int64_t(1) << 31)) {
+            if constexpr (POLICY)
+                if (dlogits != nullptr) return shared<T, true, true>(a, logits, dlogits, words, static_cast<int>(ranks), s);
+            return shared<T, POLICY, false>(a, logits, dlogits, words, static_cast<int>(ranks), s);
+        }
+    }
+    token_rows_kernel<T, VEC, POLICY><<<static_cast<unsigned>(a.m), kTeam, 0, s>>>(a, logits, dlogits);
+    note_launch();
+    return check_launch();
+}
+
+template <typename T, int VEC> int launch(const TokenArgs& a, const T* logits, T* dlogits, What what, cudaStream_t s) {
+    if (what == kPolicy) return rows<T, VEC, true>(a, logits, dlogits, s);
+    if (what == kScore) return rows<T, VEC, false>(a, logits, dlogits, s);
+    const int64_t shares = (a.v + (VEC - 1) + kShare - 1) / kShare;
+    if (a.m * shares >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
+    token_gradient_kernel<T, VEC><<<static_cast<unsigned>(a.m * shares), kGradientThreads, 0, s>>>(a, logits, dlogits, static_cast<int>(shares));
     note_launch();
     return check_launch();
 }
@@ -231,7 +531,7 @@ template <typename T> int dispatch(const TokenArgs& a, int64_t m, const void* lo
     T* out = static_cast<T*>(dlogits);
     const uintptr_t apart = reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(dlogits);
     const bool alike = out == nullptr || ((apart & 15) == 0 && (m == 1 || ((a.ld - a.ld_d) * static_cast<int64_t>(sizeof(T))) % 16 == 0));
-    return alike ? launch<T, Word<T>::kN>(a, m, in, out, what, s) : launch<T, 1>(a, m, in, out, what, s);
+    return alike ? launch<T, Word<T>::kN>(a, in, out, what, s) : launch<T, 1>(a, in, out, what, s);
 }
 
 int dispatch(const TokenArgs& a, int dtype, int64_t m, const void* logits, void* dlogits, What what, cudaStream_t s) {
@@ -253,9 +553,17 @@ int check(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const
     return BZ_OK;
 }
 
-TokenArgs token_args(int64_t ld, int64_t v, int64_t ld_d, const int32_t* index, float temperature, const float* dloss, float* logp, float* stats) {
+TokenArgs token_args(const void* logits, int dtype, int64_t m, int64_t ld, int64_t v, int64_t ld_d, const int32_t* index, float temperature, const float* dloss, float* logp, float* stats) {
     TokenArgs a{};
-    a.ld = ld, a.v = v, a.ld_d = ld_d, a.index = index, a.inv_t = 1.0 / static_cast<double>(temperature), a.temperature = temperature, a.c = kLog2e / temperature;
+    a.ld = ld, a.v = v, a.ld_d = ld_d, a.index = index, a.inv_t = 1.0 / static_cast<double>(temperature), a.temperature = temperature;
+    a.m = m;
+    const char* p = static_cast<const char*>(logits);
+    a.extent = {p, p + ((m - 1) * ld + v) * element_bytes(dtype)};
+    const double c = 1.4426950408889634 / static_cast<double>(temperature);
+    a.c = static_cast<float>(c);
+    if (static_cast<double>(a.c) > c) a.c = nextafterf(a.c, 0.f);
+    a.c_low = static_cast<float>(c - static_cast<double>(a.c));
+    if (a.c_low < 1e-37f) a.c_low = 1e-37f;
     a.dloss = dloss, a.logp = logp, a.stats = reinterpret_cast<float4*>(stats);
     return a;
 }
@@ -275,7 +583,7 @@ extern "C" int bz_policy(const void* logits, int64_t ld, int dtype, int64_t m, i
     if (advantage == nullptr || (kl != 0.f && ref_logp == nullptr) || (loss == nullptr && logp == nullptr && stats == nullptr && dlogits == nullptr))
         return BZ_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    TokenArgs a = token_args(ld, v, ld_d, index, temperature, dloss, logp, stats);
+    TokenArgs a = token_args(logits, dtype, m, ld, v, ld_d, index, temperature, dloss, logp, stats);
     a.old_logp = old_logp, a.ref_logp = ref_logp, a.advantage = advantage, a.clip_low = clip_low, a.clip_high = clip_high, a.kl = kl, a.loss = loss;
     if (v == 0) {
         token_empty_kernel<<<kNumSMs, 256, 0, s>>>(m, loss, logp, a.stats);
@@ -294,7 +602,7 @@ extern "C" int bz_preference(const void* logits, int64_t ld, int dtype, int64_t 
     if (st != BZ_OK) return st;
     if ((pairs > 0 && starts == nullptr) || (m > 0 && stats == nullptr)) return BZ_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    TokenArgs a = token_args(ld, v, ld_d, index, temperature, dloss, logp, stats);
+    TokenArgs a = token_args(logits, dtype, m, ld, v, ld_d, index, temperature, dloss, logp, stats);
     a.ref_logp = ref_logp;
     if (m > 0 && v == 0) {
         token_empty_kernel<<<kNumSMs, 256, 0, s>>>(m, nullptr, logp, a.stats);
@@ -319,6 +627,6 @@ extern "C" int bz_token_loss_backward(const void* logits, int64_t ld, int dtype,
     const int st = check(logits, ld, dtype, m, v, index, temperature, stats, dlogits, ld_d);
     if (st != BZ_OK || m == 0 || v == 0) return st;
     if (stats == nullptr || dlogits == nullptr) return BZ_ERR_INVALID_ARG;
-    return dispatch(token_args(ld, v, ld_d, index, temperature, dloss, nullptr, const_cast<float*>(stats)), dtype, m, logits, dlogits, kGradient,
+    return dispatch(token_args(logits, dtype, m, ld, v, ld_d, index, temperature, dloss, nullptr, const_cast<float*>(stats)), dtype, m, logits, dlogits, kGradient,
                     static_cast<cudaStream_t>(stream));
 }
