@@ -3,8 +3,10 @@
 // Both rest on lp = z[a] - log(sum of exp z), z = logits / T, and on one number a row, the slope d loss / d lp:
 // dlogits = dloss * slope / T * ([c == a] - softmax(z)[c]).
 //
-// Exponents.  A sum over a sequence adds up the errors of its lp, and a factor log2(e)/T rounded to binary32 is wrong to the same
-// side in all of them; so exponents are (s - m) c + (s - m) c_low with the rounding's rest c_low, relative to an m that is subtracted exactly.
+// Exponents are s c - R, one multiply-add: c = log2(e)/T rounded to binary32 and R the whole number next to the largest s c, so that the
+// multiply-add's rounding is the only one, and joining two parts of a row is exact.  The rounding of c is a temperature that differs by 2^-25 at
+// most; the token's own logit goes by the same c, or the error would have one sign in all lp and a sum over a sequence would collect it.
+// Where s c is beyond 2^100 (rows of a type's lowest value) exponents are (s - largest) c.
 #include <cooperative_groups.h>
 
 #include "worker_common.cuh"
@@ -22,9 +24,7 @@ struct TokenArgs {
     int64_t m, ld, v, ld_d;
     const int32_t* index;
     Extent extent;            // of the logits
-    double inv_t;             // 1 / T
-    float temperature;
-    float c, c_low;           // log2(e) / T = c + c_low, c_low > 0: what is infinite stays so
+    float temperature, c;     // c = log2(e) / T
     const float *old_logp, *ref_logp, *advantage;
     float clip_low, clip_high, kl;
     const float* dloss;
@@ -33,55 +33,100 @@ struct TokenArgs {
 };
 
 __device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
-// 2^(exponent of d = s - reference)
-__device__ __forceinline__ float power(const TokenArgs& a, float d) { return exp2_fast(fmaf(d, a.c, d * a.c_low)); }
-__device__ __forceinline__ float2 powers(const TokenArgs& a, float2 s, float reference) {
-    const float2 d = __fadd2_rn(s, pair(-reference)), y = __ffma2_rn(d, pair(a.c), __fmul2_rn(d, pair(a.c_low)));
+// What the exponents of a row, or a part of it, are relative to.  A MaxSum here is the largest s and the sum of 2^(s c - R).
+struct Base {
+    float r, m;     // R; apart: the largest
+    bool apart;
+    __device__ __forceinline__ Base(const TokenArgs& a, float largest) {
+        const float y = largest * a.c;
+        m = largest, apart = !(fabsf(y) < 0x1p100f) && largest != -INFINITY;
+        r = apart || largest == -INFINITY ? 0.f : rintf(y);
+    }
+    __device__ __forceinline__ float exponent(const TokenArgs& a, float s) const { return apart ? (s - m) * a.c : fmaf(s, a.c, -r); }
+    // of a part's base, relative to this one, which has the larger s
+    __device__ __forceinline__ float of(const TokenArgs& a, const Base& part) const { return !apart && !part.apart ? part.r - r : apart && part.apart ? (part.m - m) * a.c : -INFINITY; }
+    // log2 of what the sum is relative to the largest itself
+    __device__ __forceinline__ float rest(const TokenArgs& a) const { return apart || m == -INFINITY ? 0.f : fmaf(m, a.c, -r); }
+};
+__device__ __forceinline__ float2 powers(const TokenArgs& a, float2 s, float2 minus_r) {
+    const float2 y = __ffma2_rn(s, pair(a.c), minus_r);
     return make_float2(exp2_fast(y.x), exp2_fast(y.y));
 }
-// What exponents are relative to: the largest, but 0 where everything is -inf.
-__device__ __forceinline__ float reference_of(float largest) { return largest == -INFINITY ? 0.f : largest; }
 // The parts of a warp's lanes as one.
 __device__ __forceinline__ MaxSum joined(const TokenArgs& a, const MaxSum& v) {
     const float m = warp_max(v.m);
-    return {m, warp_sum(v.s == 0.f ? 0.f : v.s * power(a, v.m - reference_of(m)))};
+    return {m, warp_sum(v.s == 0.f ? 0.f : v.s * exp2_fast(Base(a, m).of(a, Base(a, v.m))))};
+}
+// sum and the elements of x as one.
+template <int K, int N> __device__ __forceinline__ void absorb(const TokenArgs& a, MaxSum& sum, const float (&x)[K][N]) {
+    float top = sum.m;
+#pragma unroll
+    for (int j = 0; j < K; ++j) top = largest(top, x[j]);
+    const Base base(a, top);
+    float2 s0 = make_float2(sum.s == 0.f ? 0.f : sum.s * exp2_fast(base.of(a, Base(a, sum.m))), 0.f), s1 = pair(0.f);
+    if (base.apart) {
+        rare();
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int e = 0; e < N; ++e) s0.x += exp2_fast(base.exponent(a, x[j][e]));
+    } else {
+        const float2 minus_r = pair(-base.r);
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if constexpr (N == 1) {
+                s0.x += exp2_fast(base.exponent(a, x[j][0]));
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; e += 4) {
+                    s0 = __fadd2_rn(s0, powers(a, make_float2(x[j][e], x[j][e + 1]), minus_r));
+                    s1 = __fadd2_rn(s1, powers(a, make_float2(x[j][e + 2], x[j][e + 3]), minus_r));
+                }
+            }
+        }
+    }
+    s0 = __fadd2_rn(s0, s1);
+    sum = {top, s0.x + s0.y};
+}
+// x = f 2^(exponents of x)
+template <int N> __device__ __forceinline__ void scaled_powers(const TokenArgs& a, const Base& base, float f, float (&x)[N]) {
+    if (base.apart) {
+        rare();
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = f * exp2_fast(base.exponent(a, x[e]));
+    } else if constexpr (N == 1) {
+        x[0] = f * exp2_fast(base.exponent(a, x[0]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+            const float2 y = __fmul2_rn(powers(a, make_float2(x[e], x[e + 1]), pair(-base.r)), pair(f));
+            x[e] = y.x, x[e + 1] = y.y;
+        }
+    }
 }
 
-// lp of a logit in a row of maximum m and sum s.
-__device__ __forceinline__ double log_probability(float logit, float m, float s, double inv_t) {
+// ex2.approx returns 2.2e-8 too little on average (measured over rows of normal logits: 1.9 to 2.5e-8), which a sum over a sequence would
+// collect.
+constexpr double kPowers = 1.0 + 2.2e-8;
+
+// lp of a logit in a row of largest m, where the sum relative to 2^(m c + rest) is s.
+__device__ __forceinline__ double log_probability(const TokenArgs& a, float logit, float m, double rest, double s) {
     if (logit == -INFINITY) return -INFINITY;
-    return (static_cast<double>(logit) - static_cast<double>(m)) * inv_t - log(static_cast<double>(s));
+    return (static_cast<double>(logit) - static_cast<double>(m)) * static_cast<double>(a.c) * 0.6931471805599453094 + rest * 0.6931471805599453094 - log(s);
 }
-
-struct RowInputs {   // loaded a row ahead
-    float old_logp, ref_logp, advantage, dloss;
-};
-struct PolicyRow {
-    float loss, slope;
-};
-__device__ __forceinline__ PolicyRow policy_row(const TokenArgs& a, const RowInputs& in, double lp) {
-    double loss = 0.0, slope = 0.0;
-    const double adv = in.advantage;
-    if (adv != 0.0) {   // a NaN goes on
-        const double r = a.old_logp != nullptr ? exp(lp - static_cast<double>(in.old_logp)) : 1.0;
-        const double lo = 1.0 - static_cast<double>(a.clip_low), hi = 1.0 + static_cast<double>(a.clip_high);
-        const bool held = adv > 0.0 ? r > hi : adv < 0.0 && r < lo;
-        loss = -(held ? (adv > 0.0 ? hi : lo) : r) * adv;
-        slope = held ? 0.0 : -r * adv;
-    }
-    if (a.kl != 0.f) {
-        const double d = static_cast<double>(in.ref_logp) - lp, e = expm1(d), k = a.kl;
-        loss += k * (isinf(e) ? e : e - d);
-        slope -= k * e;
-    }
-    return {static_cast<float>(loss), lp == -INFINITY ? 0.f : static_cast<float>(slope)};
+// Of a sum relative to R: s c - R = (s - m) c + (m c - R).
+__device__ __forceinline__ double exact_rest(const TokenArgs& a, const Base& base) {
+    return base.apart || base.m == -INFINITY ? 0.0 : static_cast<double>(base.m) * static_cast<double>(a.c) - static_cast<double>(base.r);
 }
 
 __device__ __forceinline__ bool has_token(const TokenArgs& a, int at) { return at >= 0 && at < a.v; }
 
-// What one thread does of a row with a token: its scalars, and the factor of the gradient (0: none).
-template <bool POLICY> __device__ __forceinline__ RowInputs row_inputs(const TokenArgs& a, int64_t i) {
-    RowInputs r{0.f, 0.f, 0.f, 1.f};
+// What one warp does of a row with a token, all lanes alike: its scalars.
+struct RowInputs {
+    float logit, old_logp, ref_logp, advantage, dloss;
+};
+template <bool POLICY> __device__ __forceinline__ RowInputs row_inputs(const TokenArgs& a, int64_t i, float logit) {
+    RowInputs r{logit, 0.f, 0.f, 0.f, 1.f};
     if (POLICY) {
         if (a.old_logp != nullptr) r.old_logp = __ldg(a.old_logp + i);
         if (a.ref_logp != nullptr) r.ref_logp = __ldg(a.ref_logp + i);
@@ -90,16 +135,41 @@ template <bool POLICY> __device__ __forceinline__ RowInputs row_inputs(const Tok
     }
     return r;
 }
-template <bool POLICY> __device__ __forceinline__ float finish_row(const TokenArgs& a, int64_t i, const RowInputs& in, float logit, const MaxSum& all, bool write) {
-    const double lp = log_probability(logit, all.m, all.s, a.inv_t);
-    PolicyRow p{0.f, 0.f};
-    if (POLICY) p = policy_row(a, in, lp);
-    if (write) {
-        if (a.logp != nullptr) a.logp[i] = static_cast<float>(lp);
-        if (POLICY && a.loss != nullptr) a.loss[i] = p.loss;
-        if (a.stats != nullptr) a.stats[i] = make_float4(all.m, all.s, p.slope, __int_as_float(static_cast<int>(i)));
+struct RowScalars {
+    double lp, sum, rest;
+    float loss, slope;
+    // of the gradient: g times (indicator of the token less softmax)
+    __device__ __forceinline__ float factor(const TokenArgs& a, const RowInputs& in) const { return slope == 0.f ? 0.f : slope * in.dloss / a.temperature; }
+};
+template <bool POLICY> __device__ __forceinline__ RowScalars row_scalars(const TokenArgs& a, const RowInputs& in, const MaxSum& all) {
+    RowScalars s{0.0, static_cast<double>(all.s) * kPowers, exact_rest(a, Base(a, all.m)), 0.f, 0.f};
+    s.lp = log_probability(a, in.logit, all.m, s.rest, s.sum);
+    if (POLICY) {
+        // both exponentials at once: the ratio's on the even lanes, the KL term's on the odd ones
+        const double shift = threadIdx.x & 1 ? static_cast<double>(in.ref_logp) - s.lp : s.lp - static_cast<double>(in.old_logp), e = expm1(shift);
+        const double ratio = __shfl_sync(~0u, e, 0) + 1.0, back = __shfl_sync(~0u, shift, 1), grown = __shfl_sync(~0u, e, 1);
+        const double adv = in.advantage, k = a.kl;
+        double loss = 0.0, slope = 0.0;
+        if (adv != 0.0) {   // a NaN goes on
+            const double r = a.old_logp != nullptr ? ratio : 1.0;
+            const double lo = 1.0 - static_cast<double>(a.clip_low), hi = 1.0 + static_cast<double>(a.clip_high);
+            const bool held = adv > 0.0 ? r > hi : adv < 0.0 && r < lo;
+            loss = -(held ? (adv > 0.0 ? hi : lo) : r) * adv;
+            slope = held ? 0.0 : -r * adv;
+        }
+        if (k != 0.0) {
+            loss += k * (isinf(grown) ? grown : grown - back);
+            slope -= k * grown;
+        }
+        s.loss = static_cast<float>(loss), s.slope = s.lp == -INFINITY ? 0.f : static_cast<float>(slope);
     }
-    return p.slope == 0.f ? 0.f : p.slope * in.dloss / a.temperature;
+    return s;
+}
+// One thread.
+__device__ __forceinline__ void write_row(const TokenArgs& a, int64_t i, const MaxSum& all, const RowScalars& s, bool policy) {
+    if (a.logp != nullptr) a.logp[i] = static_cast<float>(s.lp);
+    if (policy && a.loss != nullptr) a.loss[i] = s.loss;
+    if (a.stats != nullptr) a.stats[i] = make_float4(all.m, static_cast<float>(s.sum * exp2(-s.rest)), s.slope, __int_as_float(static_cast<int>(i)));
 }
 __device__ __forceinline__ void finish_without(const TokenArgs& a, int64_t i, bool policy) {
     if (a.logp != nullptr) a.logp[i] = 0.f;
@@ -109,106 +179,94 @@ __device__ __forceinline__ void finish_without(const TokenArgs& a, int64_t i, bo
 
 // ---- a row in a CTA's or a cluster's shared memory -----------------------------------------------
 //
-// A thread copies its own 16-byte words of the row (cp.async, four groups), takes each group into its largest logit and sum as it
+// A thread copies its own 16-byte words of the row (cp.async, up to four groups), takes each group into its largest logit and sum as it
 // arrives, and with a gradient passes over them again out of shared memory: the row comes from memory once.  The row's maximum and
 // sum cost one exchange, the scalars of its loss one thread in binary64.  Nothing of a row overlaps inside its CTA but the loads; three CTAs or
 // more on an SM, each at another point of its row, do that.  (Rows kept as exponentials in registers with the next one on its way,
 // two CTAs an SM: 148 us at 4096 x 32128 bfloat16 with the gradient.  Rows through a ring with warps for each part of the work: 170 us, most of
 // it bookkeeping of sixteen warps for rows of four chunks.)
 
-constexpr int kQuarters = 4;     // groups of copies
+constexpr int kShared = 256;     // threads of a CTA at most
 constexpr int kBatch = 4;        // words a thread works on at a time
 constexpr int kMostWords = 227 * 1024 / 16 - 64;   // of a CTA
 
+// All but the last LEFT groups of copies have arrived.
+template <int LEFT> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+__device__ __forceinline__ void copy_word(uint32_t to, const char* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+
 struct RowShare {
-    int ranks, words;   // CTAs of a row; words of a CTA at most
+    int ranks, words, batches;   // CTAs of a row; words of a CTA at most; batches of a thread
 };
 
-template <typename T, bool POLICY, bool GRADIENT>
-__global__ void __launch_bounds__(kTeam) token_shared_kernel(const __grid_constant__ TokenArgs a, const RowShare share, const T* logits, T* dlogits) {
+// THREADS: of the CTA, or 0 for whatever it is launched with (the distances of a thread's words are constants in the long rows).
+template <typename T, bool POLICY, bool GRADIENT, int THREADS>
+__global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_constant__ TokenArgs a, const RowShare share, const T* logits, T* dlogits) {
     constexpr int N = Word<T>::kN;
     extern __shared__ __align__(16) uint4 held[];
     __shared__ MaxSum part[16], peers[kMostRanks];
     __shared__ float3 outcome;   // the row's largest, the exponentials' factor, the gradient's
-    const int threads = blockDim.x, t = threadIdx.x, warp = t >> 5, lane = t & 31;
-    const int64_t i = blockIdx.x / share.ranks;
-    const int rank = static_cast<int>(blockIdx.x - i * share.ranks);
+    const int threads = THREADS ? THREADS : blockDim.x, t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const unsigned r = share.ranks == 1 ? blockIdx.x : blockIdx.x / static_cast<unsigned>(share.ranks);
+    const int rank = static_cast<int>(blockIdx.x - r * share.ranks);
+    const int64_t i = r;
     if (share.ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // every CTA of the cluster has started
     const int at = __ldg(a.index + i);
     const T* row = logits + i * a.ld;
     const int n = static_cast<int>(a.v), lead = row_lead<T, N>(row);
-    // this CTA's words [begin, end) of the row's, counted from the 16-byte boundary at or before it
-    const int all = (lead + n + N - 1) / N, begin = rank * share.words, end = min(begin + share.words, all);
-    const int mine = max((end - begin - t + threads - 1) / threads, 0);   // words begin + t + q threads, q < mine
-    const int first_word = begin + t, last_word = begin + t + (mine - 1) * threads;
-    // words over an end of the row: this thread's first, its last
-    const bool over_first = mine > 0 && first_word == 0 && lead != 0, over_last = mine > 0 && last_word == all - 1 && (lead + n) % N != 0;
+    // this CTA's words [begin, begin + count) of the row's, counted from the 16-byte boundary at or before it; this thread's: t, t + threads, ...
+    const int all = (lead + n + N - 1) / N, begin = rank * share.words, count = min(share.words, all - begin);
+    // words over an end of the row: places in the CTA, -1: elsewhere
+    const int head = lead != 0 && begin == 0 ? 0 : -1, tail = (lead + n) % N != 0 && begin + count == all ? count - 1 : -1;
+    // batches without any of these, and without words behind the last
+    const int stride = threads * 16, plain_from = head >= 0, plain_to = (count - (tail >= 0)) / (kBatch * threads);
     const bool there = has_token(a, at);
-    T* out = GRADIENT ? dlogits + i * a.ld_d : nullptr;
-    float g = 0.f, f = 0.f, ref = 0.f;
-    RowInputs in{};
-    float logit = 0.f;
+    float g = 0.f, f = 0.f, top = 0.f;
     if (there) {
-        const uint4* from = reinterpret_cast<const uint4*>(row - lead) + first_word;
-        const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(held + t));
-        const int quarter = (mine + kQuarters - 1) / kQuarters;
+        const char* from = reinterpret_cast<const char*>(row - lead) + (begin + t) * int64_t(16);
+        uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(held + t));
+        for (int b = 0, w = t; b < share.batches; ++b, w += kBatch * threads, from += kBatch * stride, to += kBatch * stride) {
+            if (b >= plain_from && b < plain_to) {
 #pragma unroll
-        for (int k = 0; k < kQuarters; ++k) {
-            for (int q = k * quarter; q < min((k + 1) * quarter, mine); ++q)
-                if (!(over_first && q == 0) && !(over_last && q == mine - 1))
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + q * threads * 16), "l"(from + static_cast<int64_t>(q) * threads) : "memory");
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        }
-        if (t == 0) in = row_inputs<POLICY>(a, i), logit = to_f32(row[at]);
-        if (over_first || over_last) {   // element by element, -inf in the place of what is not the row's
-            rare();
-            float x[N];
-            if (over_first) {
-                load_slot<T, N>(row, -lead, n, -INFINITY, x);
-                held[t] = Word<T>::pack(x);
+                for (int j = 0; j < kBatch; ++j) copy_word(to + j * stride, from + j * stride);
+            } else {
+                rare();
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j)
+                    if (const int v = w + j * threads; v < count && v != head && v != tail) copy_word(to + j * stride, from + j * stride);
             }
-            if (over_last) {
-                load_slot<T, N>(row, static_cast<int64_t>(all - 1) * N - lead, n, -INFINITY, x);
-                held[t + (mine - 1) * threads] = Word<T>::pack(x);
+            if (b < 3 || b + 1 == share.batches) asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        RowInputs in{};
+        if (warp == 0) in = row_inputs<POLICY>(a, i, to_f32(row[at]));
+        // -inf in what was not copied: words behind the CTA's last, elements that are not the row's
+        for (int b = 0; b < share.batches; ++b) {
+            if (b >= plain_from && b < plain_to) continue;
+            for (int w = b * kBatch * threads + t, j = 0; j < kBatch; ++j, w += threads) {
+                if (w < count && w != head && w != tail) continue;
+                float x[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) x[e] = -INFINITY;
+                if (w < count) load_slot<T, N>(row, static_cast<int64_t>(begin + w) * N - lead, n, -INFINITY, x);
+                held[w] = Word<T>::pack(x);
             }
         }
         MaxSum sum{-INFINITY, 0.f};
-        auto absorb = [&](auto& x) {
-            float top = sum.m;
-            for (auto& w : x) top = largest(top, w);
-            const float r = reference_of(top);
-            float2 s0 = make_float2(sum.s == 0.f ? 0.f : sum.s * power(a, sum.m - r), 0.f), s1 = pair(0.f);
-            for (auto& w : x) {
-#pragma unroll
-                for (int e = 0; e < N; e += 4) {
-                    s0 = __fadd2_rn(s0, powers(a, make_float2(w[e], w[e + 1]), r));
-                    s1 = __fadd2_rn(s1, powers(a, make_float2(w[e + 2], w[e + 3]), r));
-                }
-            }
-            s0 = __fadd2_rn(s0, s1);
-            sum = {top, s0.x + s0.y};
-        };
-#pragma unroll
-        for (int k = 0; k < kQuarters; ++k) {
-            if (k == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
-            if (k == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
-            if (k == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-            if (k == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
-            const int to_q = min((k + 1) * quarter, mine);
-            int q = k * quarter;
+        const char* word = reinterpret_cast<const char*>(held + t);
 #pragma unroll 1
-            for (; q + kBatch <= to_q; q += kBatch) {
-                float x[kBatch][N];
+        for (int b = 0; b < share.batches; ++b) {
+            // groups: a batch each, the fourth all that are left
+            switch (min(share.batches, 4) - 1 - b) {
+                case 3: wait_copies<3>(); break;
+                case 2: wait_copies<2>(); break;
+                case 1: wait_copies<1>(); break;
+                default: wait_copies<0>();
+            }
+            float x[kBatch][N];
 #pragma unroll
-                for (int j = 0; j < kBatch; ++j) Word<T>::unpack(held[t + (q + j) * threads], x[j]);
-                absorb(x);
-            }
-#pragma unroll 1
-            for (; q < to_q; ++q) {
-                float x[1][N];
-                Word<T>::unpack(held[t + q * threads], x[0]);
-                absorb(x);
-            }
+            for (int j = 0; j < kBatch; ++j) Word<T>::unpack(*reinterpret_cast<const uint4*>(word + j * stride), x[j]);
+            word += kBatch * stride;
+            absorb(a, sum, x);
         }
         sum = joined(a, sum);
         if (lane == 0) part[warp] = sum;
@@ -224,64 +282,63 @@ __global__ void __launch_bounds__(kTeam) token_shared_kernel(const __grid_consta
         }
         if (warp == 0) {
             sum = joined(a, share.ranks > 1 ? (lane < share.ranks ? peers[lane] : MaxSum{-INFINITY, 0.f}) : (lane < (threads >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f}));
-            if (lane == 0) {
-                const float got = finish_row<POLICY>(a, i, in, logit, sum, rank == 0);
-                outcome = make_float3(sum.m, got == 0.f ? 0.f : -got / sum.s, got);
+            const RowScalars scalars = row_scalars<POLICY>(a, in, sum);
+            if (GRADIENT) {
+                const float got = scalars.factor(a, in);
+                if (lane == 0) outcome = make_float3(sum.m, got == 0.f ? 0.f : -got / sum.s, got);
+                __syncthreads();
             }
+            if (lane == 0 && rank == 0) write_row(a, i, sum, scalars, POLICY);
+        } else if (GRADIENT) {
+            __syncthreads();
         }
         if (!GRADIENT) return;
-        __syncthreads();
-        ref = reference_of(outcome.x), f = outcome.y, g = outcome.z;
+        top = outcome.x, f = outcome.y, g = outcome.z;
     } else {
         if (share.ranks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (t == 0 && rank == 0) finish_without(a, i, POLICY);
         if (!GRADIENT) return;
     }
-    uint4* to = reinterpret_cast<uint4*>(out - lead) + first_word;
-    const int from_q = over_first ? 1 : 0, to_q = over_last ? mine - 1 : mine;
+    const Base base(a, top);
+    T* out = dlogits + i * a.ld_d;
+    char* to = reinterpret_cast<char*>(out - lead) + (begin + t) * int64_t(16);
+    const char* word = reinterpret_cast<const char*>(held + t);
     if (g == 0.f) {
-        for (int q = from_q; q < to_q; ++q) to[static_cast<int64_t>(q) * threads] = make_uint4(0, 0, 0, 0);
+        for (int w = t; w < count; w += threads, to += stride)
+            if (w != head && w != tail) *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
     } else {
-        auto finish = [&](float (&x)[N]) {
-#pragma unroll
-            for (int e = 0; e < N; e += 2) {
-                const float2 y = __fmul2_rn(powers(a, make_float2(x[e], x[e + 1]), ref), pair(f));
-                x[e] = y.x, x[e + 1] = y.y;
-            }
-        };
-        int q = from_q;
 #pragma unroll 1
-        for (; q + kBatch <= to_q; q += kBatch) {
+        for (int b = 0, w = t; b < share.batches; ++b, w += kBatch * threads, word += kBatch * stride, to += kBatch * stride) {
             float x[kBatch][N];
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) Word<T>::unpack(held[t + (q + j) * threads], x[j]);
+            for (int j = 0; j < kBatch; ++j) Word<T>::unpack(*reinterpret_cast<const uint4*>(word + j * stride), x[j]);
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) finish(x[j]), to[static_cast<int64_t>(q + j) * threads] = Word<T>::pack(x[j]);
-        }
-#pragma unroll 1
-        for (; q < to_q; ++q) {
-            float x[N];
-            Word<T>::unpack(held[t + q * threads], x);
-            finish(x), to[static_cast<int64_t>(q) * threads] = Word<T>::pack(x);
+            for (int j = 0; j < kBatch; ++j) scaled_powers(a, base, f, x[j]);
+            if (b >= plain_from && b < plain_to) {
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) *reinterpret_cast<uint4*>(to + j * stride) = Word<T>::pack(x[j]);
+            } else {
+                rare();
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j)
+                    if (const int v = w + j * threads; v < count && v != head && v != tail) *reinterpret_cast<uint4*>(to + j * stride) = Word<T>::pack(x[j]);
+            }
         }
     }
-    if (over_first || over_last) {
-        rare();
-        for (int which = 0; which < 2; ++which) {
-            if (which == 0 ? !over_first : !over_last || (over_first && mine == 1)) continue;
-            const int word = which == 0 ? first_word : last_word;
-            float x[N];
-            Word<T>::unpack(held[word - begin], x);
+    for (int which = 0; which < 2; ++which) {
+        const int w = which == 0 ? head : tail == head ? -1 : tail;
+        if (w < 0 || w % threads != t) continue;
+        float x[N];
+        Word<T>::unpack(held[w], x);
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = g == 0.f ? 0.f : power(a, x[e] - ref) * f;
-            store_slot<T, N>(out, static_cast<int64_t>(word) * N - lead, n, x);
-        }
+        for (int e = 0; e < N; ++e) x[e] = g == 0.f ? 0.f : exp2_fast(base.exponent(a, x[e])) * f;
+        store_slot<T, N>(out, static_cast<int64_t>(begin + w) * N - lead, n, x);
     }
     if (g != 0.f) {   // the token's place, once more, by the thread that has just written it
-        const int word = (at + lead) / N - begin;
-        if (word >= 0 && word < end - begin && word % threads == t) {
+        const int w = (at + lead) / N - begin;
+        if (w >= 0 && w < count && w % threads == t) {
             const int e = (at + lead) % N;
-            out[at] = from_f32<T>(fmaf(power(a, to_f32(reinterpret_cast<const T*>(held + word)[e]) - ref), f, g));
+            out[at] = from_f32<T>(fmaf(exp2_fast(base.exponent(a, to_f32(reinterpret_cast<const T*>(held + w)[e]))), f, g));
         }
     }
 }
@@ -292,13 +349,9 @@ __global__ void __launch_bounds__(kTeam) token_shared_kernel(const __grid_consta
 template <typename T, int VEC> __device__ __forceinline__ MaxSum row_statistics(const TokenArgs& a, const T* row, MaxSum* part) {
     MaxSum mine{-INFINITY, 0.f};
     for (int64_t j0 = static_cast<int64_t>(threadIdx.x) * VEC - row_lead<T, VEC>(row); j0 < a.v; j0 += blockDim.x * VEC) {
-        float x[VEC];
-        load_slot<T, VEC>(row, j0, a.v, -INFINITY, x);
-        const float m = largest(mine.m, x), ref = reference_of(m);
-        if (mine.s != 0.f) mine.s *= power(a, mine.m - ref);
-        mine.m = m;
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) mine.s += power(a, x[k] - ref);
+        float x[1][VEC];
+        load_slot<T, VEC>(row, j0, a.v, -INFINITY, x[0]);
+        absorb(a, mine, x);
     }
     mine = joined(a, mine);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = mine;
@@ -317,22 +370,28 @@ template <typename T, int VEC, bool POLICY> __global__ void __launch_bounds__(kT
     const bool there = has_token(a, at);
     MaxSum all{-INFINITY, 0.f};
     if (there) all = row_statistics<T, VEC>(a, row, part);
-    if (threadIdx.x == 0) {
-        factor = 0.f;
-        if (there)
-            factor = finish_row<POLICY>(a, i, row_inputs<POLICY>(a, i), to_f32(row[at]), all, true);
-        else
+    if (threadIdx.x < 32) {
+        float g = 0.f;
+        if (there) {
+            const RowInputs in = row_inputs<POLICY>(a, i, to_f32(row[at]));
+            const RowScalars scalars = row_scalars<POLICY>(a, in, all);
+            g = scalars.factor(a, in);
+            if (threadIdx.x == 0) write_row(a, i, all, scalars, POLICY);
+        } else if (threadIdx.x == 0) {
             finish_without(a, i, POLICY);
+        }
+        if (threadIdx.x == 0) factor = g;
     }
     if (!POLICY || dlogits == nullptr) return;
     __syncthreads();
-    const float g = factor, f = g == 0.f ? 0.f : -g / all.s, ref = reference_of(all.m);
+    const float g = factor, f = g == 0.f ? 0.f : -g / all.s;
+    const Base base(a, all.m);
     T* out = dlogits + i * a.ld_d;
     for (int64_t j0 = static_cast<int64_t>(threadIdx.x) * VEC - row_lead<T, VEC>(row); j0 < a.v; j0 += blockDim.x * VEC) {
         float x[VEC];
         load_slot<T, VEC>(row, j0, a.v, -INFINITY, x);
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) x[k] = g == 0.f ? 0.f : power(a, x[k] - ref) * f + (j0 + k == at ? g : 0.f);
+        for (int k = 0; k < VEC; ++k) x[k] = g == 0.f ? 0.f : exp2_fast(base.exponent(a, x[k])) * f + (j0 + k == at ? g : 0.f);
         store_slot<T, VEC>(out, j0, a.v, x);
     }
 }
@@ -357,7 +416,8 @@ __global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const 
     const float4 st = a.stats[i];
     const int at = a.index[i];
     const float g = st.z == 0.f || !has_token(a, at) ? 0.f : st.z * (a.dloss != nullptr ? a.dloss[__float_as_int(st.w)] : 1.f) / a.temperature;
-    const float f = g == 0.f ? 0.f : -g / st.y, ref = reference_of(st.x);
+    const Base reference(a, st.x);
+    const float f = g == 0.f ? 0.f : -g / st.y * exp2_fast(-reference.rest(a));
 #pragma unroll
     for (int q = 0; q < kSlots; ++q) {
         const int64_t j0 = first(q);
@@ -365,16 +425,7 @@ __global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const 
         float x[VEC];
         raw[q].get(x);
         if (!whole(j0)) read_apart<T, VEC>(row, j0, a.v, x);
-        if constexpr (VEC == 1) {
-            x[0] = power(a, x[0] - ref);
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; e += 2) {
-                const float2 y = powers(a, make_float2(x[e], x[e + 1]), ref);
-                x[e] = y.x, x[e + 1] = y.y;
-            }
-        }
-        multiply(x, f);
+        scaled_powers(a, reference, f, x);
         if (g == 0.f) {
             rare();
 #pragma unroll
@@ -418,7 +469,7 @@ __global__ void __launch_bounds__(256) pair_kernel(const __grid_constant__ Token
             const float logit = dtype == BZ_F32 ? static_cast<const float*>(logits)[k] : dtype == BZ_F16 ? to_f32(static_cast<const __half*>(logits)[k])
                                                                                                           : to_f32(static_cast<const __nv_bfloat16*>(logits)[k]);
             const float4 st = a.stats[i];
-            sum += log_probability(logit, st.x, st.y, a.inv_t) - (a.ref_logp != nullptr ? static_cast<double>(a.ref_logp[i]) : 0.0);
+            sum += log_probability(a, logit, st.x, 0.0, st.y) - (a.ref_logp != nullptr ? static_cast<double>(a.ref_logp[i]) : 0.0);
             ++count;
         }
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), count += __shfl_xor_sync(~0u, count, o);
@@ -472,19 +523,20 @@ __global__ void token_empty_kernel(int64_t m, float* loss, float* logp, float4* 
 enum What { kPolicy, kScore, kGradient };
 
 template <typename T, bool POLICY, bool GRADIENT> int shared(const TokenArgs& a, const T* logits, T* dlogits, int64_t words, int ranks, cudaStream_t s) {
-    RowShare share{ranks, static_cast<int>((words + ranks - 1) / ranks)};
+    RowShare share{ranks, static_cast<int>((words + ranks - 1) / ranks), 0};
     // up to sixteen words a thread; where few rows leave SMs idle, four
     const int each = a.m * ranks <= kNumSMs ? 4 : 16;
     int threads = (share.words + each * 32 - 1) / (each * 32) * 32;
-    const int most = a.m * ranks <= kNumSMs ? kTeam : 256;
-    if (threads > most) threads = most;
-    auto kern = token_shared_kernel<T, POLICY, GRADIENT>;
+    if (threads > 64 && each == 16) threads = threads > 128 ? 256 : 128;
+    if (threads > kShared) threads = kShared;
+    share.batches = (share.words + threads * kBatch - 1) / (threads * kBatch);
+    auto kern = threads == 256 ? token_shared_kernel<T, POLICY, GRADIENT, 256> : threads == 128 ? token_shared_kernel<T, POLICY, GRADIENT, 128> : token_shared_kernel<T, POLICY, GRADIENT, 0>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostWords * 16);
     if (e != cudaSuccess) return cuda_failed(e);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(a.m * ranks));
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
-    cfg.dynamicSmemBytes = static_cast<size_t>(share.words) * 16;
+    cfg.dynamicSmemBytes = static_cast<size_t>(share.batches) * kBatch * threads * 16;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -501,11 +553,11 @@ template <typename T, int VEC, bool POLICY> int rows(const TokenArgs& a, const T
     if constexpr (VEC > 1) {
         const int64_t words = (a.v + 2 * (VEC - 1)) / VEC;   // of a row, at most
         // three CTAs an SM; a cluster's CTAs hold what they can of the longest rows
-        int64_t ranks = (words + 4607) / 4608;
+        int64_t ranks = words <= 4096 ? 1 : (words + 2047) / 2048;
         if (ranks > kMostRanks) ranks = kMostRanks;
         while (ranks < kMostRanks && a.m * ranks * 2 <= kNumSMs && words > ranks * 256) ranks *= 2;   // few rows: on more SMs
         if (ranks > kMostRanks) ranks = kMostRanks;
-        if ((words + ranks - 1) / ranks <= kMostWords && a.m * ranks < (int64_t(1) << 31)) {
+        if ((words + ranks - 1) / ranks + kBatch * kShared <= kMostWords && a.m * ranks < (int64_t(1) << 31)) {
             if constexpr (POLICY)
                 if (dlogits != nullptr) return shared<T, true, true>(a, logits, dlogits, words, static_cast<int>(ranks), s);
             return shared<T, POLICY, false>(a, logits, dlogits, words, static_cast<int>(ranks), s);
@@ -555,15 +607,11 @@ int check(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const
 
 TokenArgs token_args(const void* logits, int dtype, int64_t m, int64_t ld, int64_t v, int64_t ld_d, const int32_t* index, float temperature, const float* dloss, float* logp, float* stats) {
     TokenArgs a{};
-    a.ld = ld, a.v = v, a.ld_d = ld_d, a.index = index, a.inv_t = 1.0 / static_cast<double>(temperature), a.temperature = temperature;
+    a.ld = ld, a.v = v, a.ld_d = ld_d, a.index = index, a.temperature = temperature;
     a.m = m;
     const char* p = static_cast<const char*>(logits);
     a.extent = {p, p + ((m - 1) * ld + v) * element_bytes(dtype)};
-    const double c = 1.4426950408889634 / static_cast<double>(temperature);
-    a.c = static_cast<float>(c);
-    if (static_cast<double>(a.c) > c) a.c = nextafterf(a.c, 0.f);
-    a.c_low = static_cast<float>(c - static_cast<double>(a.c));
-    if (a.c_low < 1e-37f) a.c_low = 1e-37f;
+    a.c = static_cast<float>(1.4426950408889634 / static_cast<double>(temperature));
     a.dloss = dloss, a.logp = logp, a.stats = reinterpret_cast<float4*>(stats);
     return a;
 }

@@ -112,7 +112,7 @@ def test_policy_matches(m, v, T, kl, dtype):
 
 
 @pytest.mark.parametrize("dtype,m,v,pad", [(torch.bfloat16, 500, 8200, 0), (torch.bfloat16, 700, 8201, 0), (torch.float32, 400, 4111, 1), (torch.float16, 300, 49153, 3),
-                                           (torch.float32, 300, 30011, 0), (torch.bfloat16, 300, 150001, 0), (torch.float16, 200, 113000, 0), (torch.float16, 3000, 513, 1)])
+                                           (torch.float32, 300, 30011, 0), (torch.bfloat16, 300, 150001, 0), (torch.bfloat16, 600, 35001, 0), (torch.float32, 543, 117813, 0), (torch.float16, 200, 113000, 0), (torch.float16, 3000, 513, 1)])
 def test_policy_many_rows(dtype, m, v, pad):
     x = make(m, v, dtype, v, pad)
     x["index"][3] = -1
