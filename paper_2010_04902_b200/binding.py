@@ -905,28 +905,35 @@ def distill_backward(logits: torch.Tensor, teacher: torch.Tensor, index: torch.T
 
 def _here(t: torch.Tensor, name: str):
     """The calls below launch on the current device's current stream: their tensors have to live there."""
-    if t.is_cuda and t.device.index != torch._C._cuda_getDevice():
+    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
         raise ValueError("%s is on %s, the current device is cuda:%d: call under torch.cuda.device(%s.device)"
                          % (name, t.device, torch._C._cuda_getDevice(), name))
 
 
+def _row_tensor(t, shape, dtype, name: str):
+    """(address, leading dimension) of a matrix of this shape and type."""
+    if t.is_contiguous() and t.shape == shape and t.dtype is dtype and t.is_cuda:
+        return t.data_ptr(), shape[1]
+    return _shaped(t, shape, dtype, name), _matrix(t, name)[2]
+
+
 def _token_operands(logits, index, dloss, dlogits):
-    """(m, v, arguments from logits to index, whether a gradient is wanted, dlogits, its address and leading dimension)."""
+    """(m, arguments from logits to index, whether a gradient is wanted, dlogits, its address and leading dimension)."""
     m, v, ld = _matrix(logits, "logits")
     head = (logits.data_ptr(), ld, _dtype(logits, "logits"), m, v, _packed(index, (m,), torch.int32, "index"))
     _here(logits, "logits")
     if dlogits is None:
         if dloss is None:
-            return m, v, head, False, None, None, 0
+            return m, head, False, None, None, 0
         dlogits = _like_rows(logits)
-        return m, v, head, True, dlogits, dlogits.data_ptr(), dlogits.stride(0) if m > 1 else v
-    return m, v, head, True, dlogits, _shaped(dlogits, (m, v), logits.dtype, "dlogits"), _matrix(dlogits, "dlogits")[2]
+        return m, head, True, dlogits, dlogits.data_ptr(), dlogits.stride(0) if m > 1 else v
+    return m, head, True, dlogits, *_row_tensor(dlogits, logits.shape, logits.dtype, "dlogits")
 
 
 def _made(t, like, shape, name):
     """(tensor, address) of a binary32 output; a new one if t is None."""
     if t is None:
-        t = torch.empty(shape, dtype=torch.float32, device=like.device)
+        t = like.new_empty(shape, dtype=torch.float32)
         return t, t.data_ptr()
     return t, _packed(t, shape, torch.float32, name)
 
@@ -939,7 +946,7 @@ def policy(logits: torch.Tensor, index: torch.Tensor, advantage: torch.Tensor, o
     (float32 [m]) or `dlogits` given also the gradient, from the same pass: (loss, logp, stats, dlogits)."""
     if logits.requires_grad:
         _unrecorded("policy", logits=logits)
-    m, v, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
+    m, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
     loss, p_loss = _made(loss, logits, (m,), "loss")
     logp, p_logp = _made(logp, logits, (m,), "logp")
     stats, p_stats = _made(stats, logits, (m, 4), "stats")
@@ -960,7 +967,7 @@ def preference(logits: torch.Tensor, index: torch.Tensor, starts: torch.Tensor, 
     (loss, reward, logp, stats, dlogits)."""
     if logits.requires_grad:
         _unrecorded("preference", logits=logits)
-    m, v, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
+    m, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
     if starts.dim() != 1 or starts.shape[0] % 2 != 1:
         raise ValueError("starts must be [2 pairs + 1]")
     pairs = starts.shape[0] // 2
@@ -981,7 +988,7 @@ def token_loss_backward(logits: torch.Tensor, index: torch.Tensor, stats: torch.
     """bz_token_loss_backward: the gradient alone, with stats as policy() or preference() returned them; dloss as there."""
     if dlogits is None:
         dlogits = _like_rows(logits)
-    m, v, head, _, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
+    m, head, _, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
     if dloss is not None and dloss.dim() != 1:
         raise ValueError("dloss must be [m] or [pairs]")
     st = lib().bz_token_loss_backward(*head, temperature, _packed(stats, (m, 4), torch.float32, "stats"),
@@ -1058,13 +1065,6 @@ def _join_form(n, w_post, gate, w_pre, rate, rng):
             0 if gate is None else gate.shape[0], _packed(rng, (2,), torch.int64, "rng"), _packed(w_pre, (n,), torch.float32, "w_pre"))
 
 
-def _row_tensor(t, like, name):
-    """(address, leading dimension) of a matrix shaped like `like`, or of None."""
-    if t is None:
-        return None, 0
-    return _shaped(t, like.shape, like.dtype, name), _matrix(t, name)[2]
-
-
 def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | None = None, gate: torch.Tensor | None = None,
          w_pre: torch.Tensor | None = None, norm: str = "rms", eps: float = 1e-6, residual_scale: float = 1.0, branch_scale: float = 1.0,
          rate: float = 0.0, rng: torch.Tensor | None = None, s: torch.Tensor | None = None, z: torch.Tensor | None = None,
@@ -1081,14 +1081,14 @@ def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | 
     dt = _dtype(x, "x")
     _here(x, "x")
     p_post, p_gate, groups, p_rng, p_pre = _join_form(n, w_post, gate, w_pre, rate, rng)
-    p_y, ld_y = _row_tensor(y, x, "y")
+    p_y, ld_y = (None, 0) if y is None else _row_tensor(y, x.shape, x.dtype, "y")
     keep = s is None and y is None and residual_scale == 1.0 and w_pre is not None
     if s is None and not keep:
         s = _like_rows(x)
-    p_s, ld_s = _row_tensor(s, x, "s")
+    p_s, ld_s = (None, 0) if s is None else _row_tensor(s, x.shape, x.dtype, "s")
     if z is None and w_pre is not None:
         z = _like_rows(x)
-    p_z, ld_z = _row_tensor(z, x, "z")
+    p_z, ld_z = (None, 0) if z is None else _row_tensor(z, x.shape, x.dtype, "z")
     stats, p_stats = _made(stats, x, (m, 4), "stats")
     st = lib().bz_join(x.data_ptr(), ld_x, p_y, ld_y, dt, m, n, _norm(norm), eps, p_post, p_gate, groups, residual_scale, branch_scale, rate, p_rng,
                        p_pre, p_s, ld_s, p_z, ld_z, p_stats, _stream())
@@ -1113,15 +1113,16 @@ def join_backward(x: torch.Tensor, y: torch.Tensor | None, stats: torch.Tensor, 
     dt = _dtype(x, "x")
     _here(x, "x")
     p_post, p_gate, groups, p_rng, p_pre = _join_form(n, w_post, gate, w_pre, rate, rng)
-    p_y, ld_y = _row_tensor(y, x, "y")
-    p_ds, ld_ds = _row_tensor(ds, x, "ds")
-    p_dz, ld_dz = _row_tensor(dz, x, "dz")
+    like = x.shape, x.dtype
+    p_y, ld_y = (None, 0) if y is None else _row_tensor(y, *like, "y")
+    p_ds, ld_ds = (None, 0) if ds is None else _row_tensor(ds, *like, "ds")
+    p_dz, ld_dz = (None, 0) if dz is None else _row_tensor(dz, *like, "dz")
     if dx is None:
         dx = _like_rows(x)
-    p_dx, ld_dx = _row_tensor(dx, x, "dx")
+    p_dx, ld_dx = _row_tensor(dx, *like, "dx")
     if dy is None and y is not None:
         dy = _like_rows(y)
-    p_dy, ld_dy = _row_tensor(dy, x, "dy")
+    p_dy, ld_dy = (None, 0) if dy is None else _row_tensor(dy, *like, "dy")
     p_dpost = p_dgate = p_dpre = None
     if w_post is not None:
         dw_post, p_dpost = _made(dw_post, x, (n,), "dw_post")
@@ -1133,8 +1134,9 @@ def join_backward(x: torch.Tensor, y: torch.Tensor | None, stats: torch.Tensor, 
     if workspace is not None:
         room = _room(workspace)
     elif w_post is not None or gate is not None or w_pre is not None:
-        workspace = torch.empty(max(256, lib().bz_join_workspace_bytes(m, n, groups)), dtype=torch.uint8, device=x.device)
-        room = workspace.data_ptr(), workspace.numel()
+        size = max(256, lib().bz_join_workspace_bytes(m, n, groups))
+        workspace = x.new_empty(size, dtype=torch.uint8)
+        room = workspace.data_ptr(), size
     st = lib().bz_join_backward(x.data_ptr(), ld, p_y, ld_y, dt, m, n, _norm(norm), p_post, p_gate, groups, residual_scale, branch_scale, rate, p_rng,
                                 p_pre, _packed(stats, (m, 4), torch.float32, "stats"), p_ds, ld_ds, p_dz, ld_dz, p_dx, ld_dx, p_dy, ld_dy,
                                 p_dpost, p_dgate, p_dpre, *room, _stream())

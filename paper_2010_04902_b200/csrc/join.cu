@@ -652,7 +652,9 @@ template <typename T, int VEC, int COLS> Shape shape_of(int n, int vectors, int 
 }
 // teams: clusters of s.ranks CTAs
 template <typename K, typename... A> int start(K kern, const Shape& s, int64_t teams, int most_smem, cudaStream_t stream, A... args) {
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem);
+    cudaError_t e = cudaSuccess;
+    // up to 48 KB need no leave; beyond, the limit belongs to the kernel and not to the call: the same one each time
+    if (s.smem > 48 * 1024 - 2048) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem);
     if (e != cudaSuccess) return cuda_failed(e);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(teams * s.ranks));

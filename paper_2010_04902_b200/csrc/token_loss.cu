@@ -398,19 +398,22 @@ template <typename T, int VEC, bool POLICY> __global__ void __launch_bounds__(kT
 
 // ---- the gradient from given stats ---------------------------------------------------------------
 
-// CTA (row, share): shares of kShare elements; the last rows first, as far as the L2 still holds them.
-constexpr int kGradientThreads = 256, kGradientColumns = 32, kShare = kGradientThreads * kGradientColumns;
+// CTA (row, share): shares of kGradientColumns elements a thread; the last rows first, as far as the L2 still holds them.
+constexpr int kGradientThreads = 256, kGradientColumns = 32;
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const __grid_constant__ TokenArgs a, const T* logits, T* dlogits, int shares) {
     constexpr int kSlots = kGradientColumns / VEC;
-    const int64_t k = gridDim.x - 1 - blockIdx.x, i = k / shares;
+    const unsigned k = gridDim.x - 1 - blockIdx.x, r = shares == 1 ? k : k / static_cast<unsigned>(shares);
+    const int64_t i = r;
     const T* row = logits + i * a.ld;
     T* out = dlogits + i * a.ld_d;
-    const int64_t base = k % shares * kShare - row_lead<T, VEC>(row);
-    auto first = [&](int q) { return base + (q * kGradientThreads + static_cast<int64_t>(threadIdx.x)) * VEC; };
+    const int n = static_cast<int>(a.v);
+    // places of this thread's first elements: below 2^31, as v and a share more are
+    const int base = static_cast<int>((k - r * shares) * (blockDim.x * kGradientColumns)) + static_cast<int>(threadIdx.x) * VEC - row_lead<T, VEC>(row);
+    auto first = [&](int q) { return base + q * static_cast<int>(blockDim.x) * VEC; };
     Raw<T, VEC> raw[kSlots];
     const bool safe = a.extent.around(row, a.v);
-    auto whole = [&](int64_t j0) { return j0 < a.v && (safe || (j0 >= 0 && j0 + VEC <= a.v)); };
+    auto whole = [&](int j0) { return j0 < n && (safe || (j0 >= 0 && j0 + VEC <= n)); };
 #pragma unroll
     for (int q = 0; q < kSlots; ++q) raw[q].fetch(row + first(q), whole(first(q)));
     const float4 st = a.stats[i];
@@ -420,24 +423,24 @@ __global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const 
     const float f = g == 0.f ? 0.f : -g / st.y * exp2_fast(-reference.rest(a));
 #pragma unroll
     for (int q = 0; q < kSlots; ++q) {
-        const int64_t j0 = first(q);
-        if (j0 >= a.v) continue;
+        const int j0 = first(q);
+        if (j0 >= n) continue;
         float x[VEC];
         raw[q].get(x);
-        if (!whole(j0)) read_apart<T, VEC>(row, j0, a.v, x);
+        if (!whole(j0)) read_apart<T, VEC>(row, j0, n, x);
         scaled_powers(a, reference, f, x);
         if (g == 0.f) {
             rare();
 #pragma unroll
             for (int e = 0; e < VEC; ++e) x[e] = 0.f;
         }
-        if (static_cast<uint64_t>(at - j0) < static_cast<uint64_t>(VEC)) {
+        if (static_cast<unsigned>(at - j0) < static_cast<unsigned>(VEC)) {
             rare();
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
                 if (j0 + e == at) x[e] += g;
         }
-        store_slot<T, VEC>(out, j0, a.v, x);
+        store_slot<T, VEC>(out, j0, n, x);
     }
 }
 
@@ -527,16 +530,19 @@ template <typename T, bool POLICY, bool GRADIENT> int shared(const TokenArgs& a,
     // up to sixteen words a thread; where few rows leave SMs idle, four
     const int each = a.m * ranks <= kNumSMs ? 4 : 16;
     int threads = (share.words + each * 32 - 1) / (each * 32) * 32;
-    if (threads > 64 && each == 16) threads = threads > 128 ? 256 : 128;
+    if (each == 16 && share.words > 640) threads = share.words > 2048 ? 256 : 128;
     if (threads > kShared) threads = kShared;
     share.batches = (share.words + threads * kBatch - 1) / (threads * kBatch);
     auto kern = threads == 256 ? token_shared_kernel<T, POLICY, GRADIENT, 256> : threads == 128 ? token_shared_kernel<T, POLICY, GRADIENT, 128> : token_shared_kernel<T, POLICY, GRADIENT, 0>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostWords * 16);
+    const int smem = share.batches * kBatch * threads * 16;
+    cudaError_t e = cudaSuccess;
+    // up to 48 KB need no leave; beyond, the limit belongs to the kernel and not to the call: the same one each time
+    if (smem > 48 * 1024 - 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostWords * 16);
     if (e != cudaSuccess) return cuda_failed(e);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(a.m * ranks));
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
-    cfg.dynamicSmemBytes = static_cast<size_t>(share.batches) * kBatch * threads * 16;
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -571,9 +577,12 @@ template <typename T, int VEC, bool POLICY> int rows(const TokenArgs& a, const T
 template <typename T, int VEC> int launch(const TokenArgs& a, const T* logits, T* dlogits, What what, cudaStream_t s) {
     if (what == kPolicy) return rows<T, VEC, true>(a, logits, dlogits, s);
     if (what == kScore) return rows<T, VEC, false>(a, logits, dlogits, s);
-    const int64_t shares = (a.v + (VEC - 1) + kShare - 1) / kShare;
+    if (a.v >= (int64_t(1) << 31) - kGradientThreads * kGradientColumns - 16) return BZ_ERR_UNSUPPORTED;
+    const int64_t each = (a.v + (VEC - 1) + kGradientColumns - 1) / kGradientColumns;   // threads for a row
+    const int threads = static_cast<int>(each < kGradientThreads ? (each + 31) / 32 * 32 : kGradientThreads);
+    const int64_t shares = (each + threads - 1) / threads;
     if (a.m * shares >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
-    token_gradient_kernel<T, VEC><<<static_cast<unsigned>(a.m * shares), kGradientThreads, 0, s>>>(a, logits, dlogits, static_cast<int>(shares));
+    token_gradient_kernel<T, VEC><<<static_cast<unsigned>(a.m * shares), threads, 0, s>>>(a, logits, dlogits, static_cast<int>(shares));
     note_launch();
     return check_launch();
 }
