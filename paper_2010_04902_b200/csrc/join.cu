@@ -58,20 +58,23 @@ template <typename T> __device__ __forceinline__ float2 word_pair(const uint4& w
         return unpack2(T(), u[k]);
 }
 
+// Threads of the CTA: known beforehand for wide rows (the distances of a thread's words are constants then), or 0.
+template <int THREADS> __device__ __forceinline__ int team_threads() { return THREADS ? THREADS : static_cast<int>(blockDim.x); }
+
 // Where a thread's columns lie: element e of COLS.
-template <int VEC> struct Columns {
+template <int VEC, int THREADS> struct Columns {
     int first;   // of the CTA
-    __device__ __forceinline__ int of(int e) const { return first + (e / VEC * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * VEC + e % VEC; }
+    __device__ __forceinline__ int of(int e) const { return first + static_cast<int>(threadIdx.x) * VEC + e / VEC * team_threads<THREADS>() * VEC + e % VEC; }
 };
 
 // NT tensors' elements of a row, as they were loaded.  VEC > 1: the next row's are on their way to the other half of the room meanwhile; a
 // half is filled again only a whole row after it was read.
-template <typename T, int VEC, int COLS, int NT> struct Held {
+template <typename T, int VEC, int COLS, int NT, int THREADS> struct Held {
     static constexpr int kWords = COLS / VEC;
     uint4* room;
     int half = 0;
     int bytes[kWords];   // of the row in each word
-    __device__ __forceinline__ Held(void* smem, int n, const Columns<VEC>& at) : room(static_cast<uint4*>(smem) + threadIdx.x) {
+    __device__ __forceinline__ Held(void* smem, int n, const Columns<VEC, THREADS>& at) : room(static_cast<uint4*>(smem) + threadIdx.x) {
 #pragma unroll
         for (int q = 0; q < kWords; ++q) {
             bytes[q] = min(max((n - at.of(q * VEC)) * static_cast<int>(sizeof(T)), 0), 16);
@@ -81,9 +84,9 @@ template <typename T, int VEC, int COLS, int NT> struct Held {
             }
         }
     }
-    __device__ __forceinline__ uint4* place(int which, int t, int q) const { return room + ((which * NT + t) * kWords + q) * blockDim.x; }
+    __device__ __forceinline__ uint4* place(int which, int t, int q) const { return room + which * (NT * kWords * team_threads<THREADS>()) + (t * kWords + q) * team_threads<THREADS>(); }
     // the next row's: fetches, then commit; what a word has behind the row's end is filled with zeros
-    __device__ __forceinline__ void fetch(int t, const T* row, int, const Columns<VEC>& at) {
+    __device__ __forceinline__ void fetch(int t, const T* row, int, const Columns<VEC, THREADS>& at) {
 #pragma unroll
         for (int q = 0; q < kWords; ++q) {
             const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(place(half, t, q)));
@@ -103,7 +106,7 @@ template <typename T, int VEC, int COLS, int NT> struct Held {
             for (int p = 0; p < VEC / 2; ++p) v[q * (VEC / 2) + p] = word_pair<T>(w, p);
         }
     }
-    __device__ __forceinline__ void put(T* row, int n, const Columns<VEC>& at, const float2 (&v)[COLS / 2]) const {
+    __device__ __forceinline__ void put(T* row, int n, const Columns<VEC, THREADS>& at, const float2 (&v)[COLS / 2]) const {
 #pragma unroll
         for (int q = 0; q < kWords; ++q) {
             const int c = at.of(q * VEC);
@@ -121,10 +124,10 @@ template <typename T, int VEC, int COLS, int NT> struct Held {
         }
     }
 };
-template <typename T, int COLS, int NT> struct Held<T, 1, COLS, NT> {
+template <typename T, int COLS, int NT, int THREADS> struct Held<T, 1, COLS, NT, THREADS> {
     float2 v[NT][COLS / 2];
-    __device__ __forceinline__ Held(void*, int, const Columns<1>&) {}
-    __device__ __forceinline__ void fetch(int t, const T* row, int n, const Columns<1>& at) {
+    __device__ __forceinline__ Held(void*, int, const Columns<1, THREADS>&) {}
+    __device__ __forceinline__ void fetch(int t, const T* row, int n, const Columns<1, THREADS>& at) {
 #pragma unroll
         for (int p = 0; p < COLS / 2; ++p) {
             const int c = at.of(2 * p), d = at.of(2 * p + 1);
@@ -137,7 +140,7 @@ template <typename T, int COLS, int NT> struct Held<T, 1, COLS, NT> {
 #pragma unroll
         for (int p = 0; p < COLS / 2; ++p) x[p] = v[t][p];
     }
-    __device__ __forceinline__ void put(T* row, int n, const Columns<1>& at, const float2 (&x)[COLS / 2]) const {
+    __device__ __forceinline__ void put(T* row, int n, const Columns<1, THREADS>& at, const float2 (&x)[COLS / 2]) const {
 #pragma unroll
         for (int p = 0; p < COLS / 2; ++p) {
             if (at.of(2 * p) < n) row[at.of(2 * p)] = from_f32<T>(x[p].x);
@@ -147,33 +150,34 @@ template <typename T, int COLS, int NT> struct Held<T, 1, COLS, NT> {
 };
 
 // A number for each column in shared memory, where only its thread looks; 0 behind the last column.
-template <int VEC, int COLS> struct ByColumn {
+template <int VEC, int COLS, int THREADS> struct ByColumn {
     float4* room;
-    template <typename F> __device__ __forceinline__ void set(int n, const Columns<VEC>& at, F value) const {
+    template <typename F> __device__ __forceinline__ void set(int n, const Columns<VEC, THREADS>& at, F value) const {
 #pragma unroll
         for (int k = 0; k < COLS / 4; ++k) {
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = at.of(4 * k + e) < n ? value(at.of(4 * k + e)) : 0.f;
-            room[k * blockDim.x + threadIdx.x] = make_float4(x[0], x[1], x[2], x[3]);
+            room[k * team_threads<THREADS>() + threadIdx.x] = make_float4(x[0], x[1], x[2], x[3]);
         }
     }
     __device__ __forceinline__ void get(int k, float2 (&w)[2]) const {   // pairs 2k, 2k + 1
-        const float4 f = room[k * blockDim.x + threadIdx.x];
+        const float4 f = room[k * team_threads<THREADS>() + threadIdx.x];
         w[0] = make_float2(f.x, f.y), w[1] = make_float2(f.z, f.w);
     }
 };
 
 // Sums over the row's threads, one barrier each; two sets of partial sums in turn.
-struct Exchange {
-    struct Room {
-        float warp[2][2][16];
-        float rank[2][2][kMostRanks];
-    };
+struct ExchangeRoom {
+    float warp[2][2][16];
+    float rank[2][2][kMostRanks];
+};
+template <int THREADS> struct Exchange {
+    using Room = ExchangeRoom;
     Room* room;
     int ranks, turn = 0;
     __device__ __forceinline__ Exchange(Room* r, int ranks_) : room(r), ranks(ranks_) {
-        for (int k = threadIdx.x; k < 64; k += blockDim.x) (&r->warp[0][0][0])[k] = 0.f;
+        for (int k = threadIdx.x; k < 64; k += team_threads<THREADS>()) (&r->warp[0][0][0])[k] = 0.f;
         if (ranks > 1)
             cg::this_cluster().sync();
         else
@@ -182,7 +186,7 @@ struct Exchange {
     template <int K> __device__ __forceinline__ void sum(float (&v)[K]) {
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
-        const int warps = blockDim.x >> 5;
+        const int warps = team_threads<THREADS>() >> 5;
         if (warps > 1) {
             if ((threadIdx.x & 31) == 0) {
 #pragma unroll
@@ -192,7 +196,9 @@ struct Exchange {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 v[k] = 0.f;
-                for (int w = 0; w < warps; w += 4) {
+#pragma unroll
+                for (int w = 0; w < 16; w += 4) {
+                    if (w >= warps) break;
                     const float4 p = *reinterpret_cast<const float4*>(&room->warp[turn][k][w]);
                     v[k] += (p.x + p.y) + (p.z + p.w);
                 }
@@ -217,12 +223,12 @@ struct Exchange {
 
 // The bits of a row's elements, two halves of a word a pair.  Where the thread's words are whole groups of the generator it makes
 // its own; else the CTA makes each group once and leaves the 16-bit numbers in shared memory, two rows' in turn.
-template <int VEC, int COLS> struct Mask {
+template <int VEC, int COLS, int THREADS> struct Mask {
     uint16_t* room;      // [2][width + 16]
     int width, turn = 0;
     bool own;
     __device__ __forceinline__ static int halves(int width) { return width + 16; }
-    __device__ __forceinline__ void make(const JoinArgs& a, const Keep& keep, int64_t i, const Columns<VEC>& at, uint32_t (&r)[COLS / 2]) {
+    __device__ __forceinline__ void make(const JoinArgs& a, const Keep& keep, int64_t i, const Columns<VEC, THREADS>& at, uint32_t (&r)[COLS / 2]) {
         const uint64_t first = static_cast<uint64_t>(i) * a.n;
         if constexpr (VEC == 8) {
             if (own) {
@@ -237,7 +243,7 @@ template <int VEC, int COLS> struct Mask {
         const uint64_t begin = first + at.first;
         const int lead = static_cast<int>(begin & 7), used = min(width, a.n - at.first);
         uint16_t* to = room + turn * halves(width);
-        for (int g = threadIdx.x; g * 8 < lead + used; g += blockDim.x) reinterpret_cast<uint4*>(to)[g] = keep.words((begin >> 3) + g);
+        for (int g = threadIdx.x; g * 8 < lead + used; g += team_threads<THREADS>()) reinterpret_cast<uint4*>(to)[g] = keep.words((begin >> 3) + g);
         __syncthreads();
         turn ^= 1;
 #pragma unroll
@@ -251,7 +257,7 @@ template <int VEC, int COLS> struct Mask {
 };
 
 // Mean and 1 / deviation of what the row's threads hold.
-template <int VEC, int COLS> __device__ __forceinline__ float2 held_norm(const JoinArgs& a, Exchange& ex, const Columns<VEC>& at, const float2 (&v)[COLS / 2], float inv_n) {
+template <int VEC, int COLS, int THREADS> __device__ __forceinline__ float2 held_norm(const JoinArgs& a, Exchange<THREADS>& ex, const Columns<VEC, THREADS>& at, const float2 (&v)[COLS / 2], float inv_n) {
     float mean = 0.f, t[1];
     float2 sum = pair(0.f);
     if (a.layer) {
@@ -281,8 +287,8 @@ template <int VEC, int COLS> __device__ __forceinline__ float2 held_norm(const J
 }
 
 // v[p] = s of the pair, from x[p].
-template <int VEC, int COLS>
-__device__ __forceinline__ void joined(const JoinArgs& a, const Keep& keep, bool branch, const float2 (&h)[COLS / 2], const uint32_t (&r)[COLS / 2], const ByColumn<VEC, COLS>& weight,
+template <int VEC, int COLS, int THREADS>
+__device__ __forceinline__ void joined(const JoinArgs& a, const Keep& keep, bool branch, const float2 (&h)[COLS / 2], const uint32_t (&r)[COLS / 2], const ByColumn<VEC, COLS, THREADS>& weight,
                                        float2 (&v)[COLS / 2]) {
     if (branch) {
 #pragma unroll
@@ -293,7 +299,7 @@ __device__ __forceinline__ void joined(const JoinArgs& a, const Keep& keep, bool
             for (int e = 0; e < 2; ++e) {
                 const int p = 2 * k + e;
                 float2 b = __fmul2_rn(h[p], w[e]);
-                if (a.drop) b = Mask<VEC, COLS>::apply(keep, r[p], b);
+                if (a.drop) b = Mask<VEC, COLS, THREADS>::apply(keep, r[p], b);
                 v[p] = __ffma2_rn(v[p], pair(a.residual), b);
             }
         }
@@ -309,15 +315,15 @@ __device__ __forceinline__ float branch_weight(const JoinArgs& a, int64_t group,
     return a.w_post != nullptr ? w * a.w_post[c] : w;
 }
 
-template <typename T, int VEC, int COLS>
-__global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ JoinArgs a, int ranks, JoinRows<const T> x, JoinRows<const T> y, JoinRows<T> s, JoinRows<T> z) {
+template <typename T, int VEC, int COLS, int THREADS>
+__global__ void __launch_bounds__(THREADS ? THREADS : VEC > 1 ? 256 : kTeam, VEC == 8 && COLS == 8 ? 3 : THREADS == 512 || VEC == 1 ? 1 : 2) join_kernel(const __grid_constant__ JoinArgs a, int ranks, JoinRows<const T> x, JoinRows<const T> y, JoinRows<T> s, JoinRows<T> z) {
     extern __shared__ __align__(16) float4 smem[];
-    __shared__ __align__(16) Exchange::Room room;
-    const int width = blockDim.x * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks, teams = gridDim.x / ranks;
-    const Columns<VEC> at{rank * width};
-    const ByColumn<VEC, COLS> weight{smem}, w_pre{smem + width / 4};
-    Held<T, VEC, COLS, 2> in(smem + width / 2, a.n, at);
-    Mask<VEC, COLS> mask{reinterpret_cast<uint16_t*>(smem + width / 2 + (VEC > 1 ? 2 * 2 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
+    __shared__ __align__(16) ExchangeRoom room;
+    const int width = team_threads<THREADS>() * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks, teams = gridDim.x / ranks;
+    const Columns<VEC, THREADS> at{rank * width};
+    const ByColumn<VEC, COLS, THREADS> weight{smem}, w_pre{smem + width / 4};
+    Held<T, VEC, COLS, 2, THREADS> in(smem + width / 2, a.n, at);
+    Mask<VEC, COLS, THREADS> mask{reinterpret_cast<uint16_t*>(smem + width / 2 + (VEC > 1 ? 2 * 2 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
     const bool branch = y.p != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr;
     const float inv_n = 1.f / static_cast<float>(a.n);
     int64_t i = a.m * team / teams, change = i;   // change: the row at which the next gate row begins
@@ -332,7 +338,7 @@ __global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ Joi
     }
     const Keep keep(a.dropout);
     if (pre) w_pre.set(a.n, at, [&](int c) { return __ldg(a.w_pre + c); });
-    Exchange ex(&room, ranks);
+    Exchange<THREADS> ex(&room, ranks);
     for (; i < last; ++i) {
         if (branch && i == change) {
             const int64_t group = i / a.group_rows;
@@ -348,16 +354,16 @@ __global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ Joi
         if (branch) {
             in.get(1, h);
             if (post) {
-                st = held_norm<VEC, COLS>(a, ex, at, h, inv_n);
+                st = held_norm<VEC, COLS, THREADS>(a, ex, at, h, inv_n);
 #pragma unroll
                 for (int p = 0; p < COLS / 2; ++p) h[p] = __fmul2_rn(__fadd2_rn(h[p], pair(-st.x)), pair(st.y));
             }
         }
         in.get(0, v);
-        joined<VEC, COLS>(a, keep, branch, h, r, weight, v);
+        joined<VEC, COLS, THREADS>(a, keep, branch, h, r, weight, v);
         if (s.p != nullptr) in.put(s.row(i), a.n, at, v);
         if (pre) {
-            to = held_norm<VEC, COLS>(a, ex, at, v, inv_n);
+            to = held_norm<VEC, COLS, THREADS>(a, ex, at, v, inv_n);
 #pragma unroll
             for (int k = 0; k < COLS / 4; ++k) {
                 float2 w[2];
@@ -378,7 +384,7 @@ __global__ void __launch_bounds__(kTeam) join_kernel(const __grid_constant__ Joi
 // added up in their order by a second kernel.
 
 // Sums over the row of c0 (0 but for LAYER) and c1.
-__device__ __forceinline__ float2 row_sums(const JoinArgs& a, Exchange& ex, float2 c0, float2 c1) {
+template <int THREADS> __device__ __forceinline__ float2 row_sums(const JoinArgs& a, Exchange<THREADS>& ex, float2 c0, float2 c1) {
     if (a.layer) {
         float t[2] = {c0.x + c0.y, c1.x + c1.y};
         ex.sum(t);
@@ -399,17 +405,17 @@ struct Sums {
 __device__ __forceinline__ int64_t part_begin(const Parts& p, int64_t k) { return k / p.per_group * p.rows + k % p.per_group * p.rows / p.per_group; }
 __device__ __forceinline__ int64_t part_end(const Parts& p, int64_t k) { return k / p.per_group * p.rows + (k % p.per_group + 1) * p.rows / p.per_group; }
 
-template <typename T, int VEC, int COLS>
-__global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ Parts parts, const __grid_constant__ Sums out, int ranks,
+template <typename T, int VEC, int COLS, int THREADS>
+__global__ void __launch_bounds__(THREADS ? THREADS : kTeam, THREADS == 256 ? 2 : 1) join_backward_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ Parts parts, const __grid_constant__ Sums out, int ranks,
                                                               JoinRows<const T> x, JoinRows<const T> y, JoinRows<const T> ds, JoinRows<const T> dz, JoinRows<T> dx, JoinRows<T> dy) {
     extern __shared__ __align__(16) float4 smem[];
-    __shared__ __align__(16) Exchange::Room room;
-    const int width = blockDim.x * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks;
-    const Columns<VEC> at{rank * width};
-    const ByColumn<VEC, COLS> weight{smem}, w_pre{smem + width / 4};
-    const ByColumn<VEC, COLS> sum_post{smem + width / 2};
-    Held<T, VEC, COLS, 4> in(smem + 3 * width / 4, a.n, at);
-    Mask<VEC, COLS> mask{reinterpret_cast<uint16_t*>(smem + 3 * width / 4 + (VEC > 1 ? 2 * 4 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
+    __shared__ __align__(16) ExchangeRoom room;
+    const int width = team_threads<THREADS>() * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks;
+    const Columns<VEC, THREADS> at{rank * width};
+    const ByColumn<VEC, COLS, THREADS> weight{smem}, w_pre{smem + width / 4};
+    const ByColumn<VEC, COLS, THREADS> sum_post{smem + width / 2};
+    Held<T, VEC, COLS, 4, THREADS> in(smem + 3 * width / 4, a.n, at);
+    Mask<VEC, COLS, THREADS> mask{reinterpret_cast<uint16_t*>(smem + 3 * width / 4 + (VEC > 1 ? 2 * 4 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
     const bool branch = y.p != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr && dz.p != nullptr, stream = ds.p != nullptr;
     const float inv_n = 1.f / static_cast<float>(a.n);
     float2 sum_branch[COLS / 2], sum_pre[COLS / 2];
@@ -431,7 +437,7 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
     }
     const Keep keep(a.dropout);
     if (pre) w_pre.set(a.n, at, [&](int c) { return __ldg(a.w_pre + c); });
-    Exchange ex(&room, ranks);
+    Exchange<THREADS> ex(&room, ranks);
     for (; k < last_part; ++k, end = part_end(parts, k)) {
         const int64_t group = k / parts.per_group;
         if (branch && i < end) weight.set(a.n, at, [&](int c) { return branch_weight(a, group, c); });
@@ -453,7 +459,7 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
             if (pre) {
                 float2 v[COLS / 2], d[COLS / 2], c0 = pair(0.f), c1 = pair(0.f);
                 in.get(0, v);
-                joined<VEC, COLS>(a, keep, branch, h, r, weight, v);
+                joined<VEC, COLS, THREADS>(a, keep, branch, h, r, weight, v);
                 in.get(3, d);
 #pragma unroll
                 for (int q = 0; q < COLS / 4; ++q) {
@@ -507,7 +513,7 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int p = 2 * q + e;
-                    if (a.drop) g[p] = Mask<VEC, COLS>::apply(keep, r[p], g[p]);
+                    if (a.drop) g[p] = Mask<VEC, COLS, THREADS>::apply(keep, r[p], g[p]);
                     sum_branch[p] = __ffma2_rn(g[p], h[p], sum_branch[p]);
                     g[p] = __fmul2_rn(g[p], w[e]);
                     c1 = __ffma2_rn(g[p], h[p], c1);
@@ -545,7 +551,7 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
                     if (out.gate != nullptr) out.gate[k * a.n + c] = post ? a.w_post[c] * sum : sum;
                     total[e] = a.gate != nullptr ? fmaf(a.gate[group * a.n + c], sum, total[e]) : total[e] + sum;
                 }
-                if (post) sum_post.room[q * blockDim.x + threadIdx.x] = make_float4(total[0], total[1], total[2], total[3]);
+                if (post) sum_post.room[q * team_threads<THREADS>() + threadIdx.x] = make_float4(total[0], total[1], total[2], total[3]);
             }
 #pragma unroll
             for (int p = 0; p < COLS / 2; ++p) sum_branch[p] = pair(0.f);
@@ -565,7 +571,7 @@ __global__ void __launch_bounds__(kTeam) join_backward_kernel(const __grid_const
     }
 }
 
-// to[g][c] = from[g * per][c] + ... + from[g * per + per - 1][c], in that order within eight interleaved sums.
+// to[g][c] = sum of from[g * per + k][c] over k < per: 32 interleaved sums a column, then their sum, in an order fixed by `per`.
 struct Fold {
     const float* from;
     float* to;
@@ -574,21 +580,23 @@ struct Fold {
 struct Folds {
     Fold f[3];
 };
-__global__ void __launch_bounds__(256) fold_kernel(const __grid_constant__ Folds folds, int n) {
-    __shared__ float part[8][32];
+constexpr int kFoldRows = 32;
+__global__ void __launch_bounds__(32 * kFoldRows) fold_kernel(const __grid_constant__ Folds folds, int n) {
+    __shared__ float part[kFoldRows][33];
     const Fold f = folds.f[blockIdx.z];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), which = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, which = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     for (int64_t g = blockIdx.y; g < f.rows; g += gridDim.y) {
         float sum = 0.f;
-        if (c < n)
-            for (int64_t k = which; k < f.per; k += 8) sum += f.from[(g * f.per + k) * n + c];
-        part[which][threadIdx.x & 31] = sum;
-        __syncthreads();
-        if (which == 0 && c < n) {
-#pragma unroll
-            for (int w = 1; w < 8; ++w) sum += part[w][threadIdx.x];
-            f.to[g * n + c] = sum;
+        if (c < n) {
+            const float* from = f.from + g * f.per * n + c;
+#pragma unroll 8
+            for (int64_t k = which; k < f.per; k += kFoldRows) sum += from[k * n];
         }
+        part[which][lane] = sum;
+        __syncthreads();
+        sum = warp_sum(part[lane][which]);   // of column `which`
+        const int column = blockIdx.x * 32 + which;
+        if (lane == 0 && column < n) f.to[g * n + column] = sum;
         __syncthreads();
     }
 }
@@ -601,9 +609,10 @@ Parts parts_of(int64_t m, int64_t n, int64_t groups, int columns) {
     p.groups = groups > 0 ? groups : 1;
     p.rows = m / p.groups;
     // As many CTAs as an SM holds (512 threads by their registers, and a little less by the shared memory of small ones), but none of fewer
-    // than 16 rows: their sums' traffic would show.  Wider rows take a cluster.
+    // than 16 rows: their sums' traffic would show (few rows take the time of one after the other: two then).  Wider rows take a cluster.
     int64_t per_sm = columns * kTeam / (n > 512 ? n : columns == 16 ? 683 : 512);
-    if (per_sm > 1 && m < per_sm * kNumSMs * 16) per_sm = m / (kNumSMs * 16);
+    const int64_t least = m * n >= (int64_t(1) << 23) ? 16 : 2;
+    if (per_sm > 1 && m < per_sm * kNumSMs * least) per_sm = m / (kNumSMs * least);
     p.teams = per_sm > 1 ? per_sm * kNumSMs : n <= 16 * kTeam ? kNumSMs : kNumSMs / 2;
     // one group: a part for each CTA; more: four rounds of parts, so that the last round is short
     int64_t per = p.groups == 1 ? p.teams : (4 * p.teams + p.groups - 1) / p.groups;
@@ -682,12 +691,22 @@ template <typename T, int VEC, int COLS> int forward_as(const JoinArgs& a, const
     int per_sm = (COLS == 8 && VEC == 8 ? 768 : 512) / shape.threads;
     if (per_sm * (shape.smem + 2048) > 220 * 1024) per_sm = 220 * 1024 / (shape.smem + 2048);
     const int64_t most = static_cast<int64_t>(per_sm > 1 ? per_sm : 1) * kNumSMs / shape.ranks;
-    return start(join_kernel<T, VEC, COLS>, shape, a.m < most ? a.m : most, most_smem<T, VEC, COLS>(2, 2), s, a, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
+    // with words, eight columns a thread go up to 256 threads and sixteen begin there
+    auto kern = join_kernel<T, VEC, COLS, COLS == 16 ? 512 : 0>;
+    if constexpr (VEC > 1)
+        if (shape.threads == 256) kern = join_kernel<T, VEC, COLS, 256>;
+    return start(kern, shape, a.m < most ? a.m : most, most_smem<T, VEC, COLS>(2, 2), s, a, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
                  JoinRows<const T>{static_cast<const T*>(t.b), t.ld_b}, JoinRows<T>{static_cast<T*>(t.e), t.ld_e}, JoinRows<T>{static_cast<T*>(t.f), t.ld_f});
 }
 template <typename T, int VEC, int COLS> int backward_as(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, cudaStream_t s) {
     const Shape shape = shape_of<T, VEC, COLS>(a.n, 3, 4, a.drop != 0);
-    return start(join_backward_kernel<T, VEC, COLS>, shape, p.teams, most_smem<T, VEC, COLS>(3, 4), s, a, p, sums, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
+    auto kern = join_backward_kernel<T, VEC, COLS, 0>;
+    if constexpr (VEC > 1) {
+        if (shape.threads == 512) kern = join_backward_kernel<T, VEC, COLS, 512>;
+        if constexpr (VEC != 8 || COLS != 8)   // 16-bit words by eight columns: up to 256 columns, or from 4096 on
+            if (shape.threads == 256) kern = join_backward_kernel<T, VEC, COLS, 256>;
+    }
+    return start(kern, shape, p.teams, most_smem<T, VEC, COLS>(3, 4), s, a, p, sums, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
                  JoinRows<const T>{static_cast<const T*>(t.b), t.ld_b}, JoinRows<const T>{static_cast<const T*>(t.c), t.ld_c}, JoinRows<const T>{static_cast<const T*>(t.d), t.ld_d},
                  JoinRows<T>{static_cast<T*>(t.e), t.ld_e}, JoinRows<T>{static_cast<T*>(t.f), t.ld_f});
 }
@@ -818,7 +837,7 @@ extern "C" int bz_join_backward(const void* x, int64_t ld_x, const void* y, int6
     if (done != BZ_OK || count == 0) return done;
     int64_t rows = 1;
     for (int k = 0; k < count; ++k) rows = rows > folds.f[k].rows ? rows : folds.f[k].rows;
-    fold_kernel<<<dim3(static_cast<unsigned>((n + 31) / 32), static_cast<unsigned>(rows < 1024 ? rows : 1024), count), 256, 0, stream_>>>(folds, static_cast<int>(n));
+    fold_kernel<<<dim3(static_cast<unsigned>((n + 31) / 32), static_cast<unsigned>(rows < 1024 ? rows : 1024), count), 32 * kFoldRows, 0, stream_>>>(folds, static_cast<int>(n));
     note_launch();
     return check_launch();
 }
