@@ -44,6 +44,7 @@ struct JoinArgs {
 template <typename T> struct JoinRows {
     T* p;
     int64_t ld;
+    T* end;   // behind the tensor's last element
     __device__ __forceinline__ T* row(int64_t i) const { return p + i * ld; }
 };
 
@@ -67,30 +68,32 @@ template <int VEC, int THREADS> struct Columns {
     __device__ __forceinline__ int of(int e) const { return first + static_cast<int>(threadIdx.x) * VEC + e / VEC * team_threads<THREADS>() * VEC + e % VEC; }
 };
 
-// NT tensors' elements of a row, as they were loaded.  VEC > 1: the next row's are on their way to the other half of the room meanwhile; a
-// half is filled again only a whole row after it was read.
-template <typename T, int VEC, int COLS, int NT, int THREADS> struct Held {
-    static constexpr int kWords = COLS / VEC;
+// NT tensors' elements of a row, as they were loaded.  The next row's are on their way to the other half of the room meanwhile; a half is
+// filled again only a whole row after it was read.  SHIFT: rows that do not all begin on 16-byte boundaries.
+template <typename T, int COLS, int NT, int THREADS, bool SHIFT> struct Held {
+    static constexpr int VEC = Word<T>::kN, kWords = COLS / VEC;
     uint4* room;
     int half = 0;
-    int bytes[kWords];   // of the row in each word
+    int filled[kWords];   // bytes of the row in each word
     __device__ __forceinline__ Held(void* smem, int n, const Columns<VEC, THREADS>& at) : room(static_cast<uint4*>(smem) + threadIdx.x) {
 #pragma unroll
         for (int q = 0; q < kWords; ++q) {
-            bytes[q] = min(max((n - at.of(q * VEC)) * static_cast<int>(sizeof(T)), 0), 16);
-            if (bytes[q] == 0) {   // never copied, and stays zero
+            filled[q] = min(max((n - at.of(q * VEC)) * static_cast<int>(sizeof(T)), 0), 16);
+            if (filled[q] == 0) {   // never copied, and stays zero
 #pragma unroll
                 for (int t = 0; t < NT; ++t) *place(0, t, q) = *place(1, t, q) = make_uint4(0, 0, 0, 0);
             }
         }
     }
     __device__ __forceinline__ uint4* place(int which, int t, int q) const { return room + which * (NT * kWords * team_threads<THREADS>()) + (t * kWords + q) * team_threads<THREADS>(); }
+    __host__ __device__ static int bytes(int threads, int) { return 2 * NT * kWords * threads * 16; }
     // the next row's: fetches, then commit; what a word has behind the row's end is filled with zeros
-    __device__ __forceinline__ void fetch(int t, const T* row, int, const Columns<VEC, THREADS>& at) {
+    __device__ __forceinline__ void fetch(int t, const JoinRows<const T>& from, int64_t i, const Columns<VEC, THREADS>& at) {
+        const T* row = from.row(i);
 #pragma unroll
         for (int q = 0; q < kWords; ++q) {
             const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(place(half, t, q)));
-            if (bytes[q] > 0) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row + at.of(q * VEC)), "r"(bytes[q]) : "memory");
+            if (filled[q] > 0) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(row + at.of(q * VEC)), "r"(filled[q]) : "memory");
         }
     }
     __device__ __forceinline__ void commit() {
@@ -98,7 +101,7 @@ template <typename T, int VEC, int COLS, int NT, int THREADS> struct Held {
         half ^= 1;
     }
     __device__ __forceinline__ static void arrived() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }   // all but the last commit
-    __device__ __forceinline__ void get(int t, float2 (&v)[COLS / 2]) const {   // this row's: the half that the next commit will fill
+    __device__ __forceinline__ void get(int t, float2 (&v)[COLS / 2], const Columns<VEC, THREADS>&) const {   // this row's: the half that the next commit will fill
 #pragma unroll
         for (int q = 0; q < kWords; ++q) {
             const uint4 w = *place(half, t, q);
@@ -106,46 +109,141 @@ template <typename T, int VEC, int COLS, int NT, int THREADS> struct Held {
             for (int p = 0; p < VEC / 2; ++p) v[q * (VEC / 2) + p] = word_pair<T>(w, p);
         }
     }
-    __device__ __forceinline__ void put(T* row, int n, const Columns<VEC, THREADS>& at, const float2 (&v)[COLS / 2]) const {
+    __device__ __forceinline__ void put(int, T* row, const Columns<VEC, THREADS>& at, const float2 (&v)[COLS / 2]) const {
 #pragma unroll
         for (int q = 0; q < kWords; ++q) {
             const int c = at.of(q * VEC);
             float x[VEC];
 #pragma unroll
             for (int k = 0; k < VEC; ++k) x[k] = k & 1 ? v[(q * VEC + k) / 2].y : v[(q * VEC + k) / 2].x;
-            if (bytes[q] == 16) {
+            if (filled[q] == 16) {
                 *reinterpret_cast<uint4*>(row + c) = Word<T>::pack(x);
-            } else if (bytes[q] > 0) {
+            } else if (filled[q] > 0) {
                 rare();
 #pragma unroll
                 for (int k = 0; k < VEC; ++k)
-                    if (c + k < n) row[c + k] = from_f32<T>(x[k]);
+                    if ((k + 1) * static_cast<int>(sizeof(T)) <= filled[q]) row[c + k] = from_f32<T>(x[k]);
             }
         }
     }
 };
-template <typename T, int COLS, int NT, int THREADS> struct Held<T, 1, COLS, NT, THREADS> {
-    float2 v[NT][COLS / 2];
-    __device__ __forceinline__ Held(void*, int, const Columns<1, THREADS>&) {}
-    __device__ __forceinline__ void fetch(int t, const T* row, int n, const Columns<1, THREADS>& at) {
+// Rows that do not all begin on 16-byte boundaries.  Whole words are copied, from the boundary at or before the row on, and a thread's elements lie in two
+// of them: its own copy and its neighbour's, so a row begins with a barrier.  Outputs go through shared memory in the same way.
+template <typename T, int COLS, int NT, int THREADS> struct Held<T, COLS, NT, THREADS, true> {
+    static constexpr int N = Word<T>::kN, kWords = COLS / N;
+    uint4 *room, *out;
+    int half = 0, lead[NT];   // of this row's tensors; the next row's are found anew
+    int n, left[NT];
+    __device__ __forceinline__ Held(void* smem, int n_, const Columns<N, THREADS>&) : room(static_cast<uint4*>(smem)), n(n_) { out = room + 2 * NT * words(); }
+    __device__ __forceinline__ static int words() { return kWords * team_threads<THREADS>() + 1; }
+    __host__ __device__ static int bytes(int threads, int outputs) { return (2 * NT + outputs) * (kWords * threads + 1) * 16; }
+    __device__ __forceinline__ void fetch(int t, const JoinRows<const T>& from, int64_t i, const Columns<N, THREADS>& at) {
+        const T* row = from.row(i);
+        left[t] = row_lead<T, N>(row);
+        const T* begin = row - left[t] + at.first;
+        uint4* to = room + (half * NT + t) * words();
+        auto copy = [&](int w) {
+            const T* p = begin + w * N;
+            if (p >= row + n) return;   // behind the row: its columns are masked
+            if (p < from.p) {           // before the tensor: element by element
+                rare();
+                for (int e = 0; e < N; ++e)
+                    if (p + e >= from.p && p + e < from.end) reinterpret_cast<T*>(to + w)[e] = p[e];
+                return;
+            }
+            const int64_t room_left = (from.end - p) * static_cast<int64_t>(sizeof(T));
+            const int size = room_left < 16 ? static_cast<int>(room_left) : 16;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to + w))), "l"(p), "r"(size) : "memory");
+        };
 #pragma unroll
-        for (int p = 0; p < COLS / 2; ++p) {
-            const int c = at.of(2 * p), d = at.of(2 * p + 1);
-            v[t][p] = make_float2(c < n ? to_f32(row[c]) : 0.f, d < n ? to_f32(row[d]) : 0.f);
+        for (int q = 0; q < kWords; ++q) copy(q * team_threads<THREADS>() + threadIdx.x);
+        if (threadIdx.x == 0) copy(kWords * team_threads<THREADS>());
+    }
+    __device__ __forceinline__ void commit() {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        half ^= 1;
+    }
+    // this row's words, everyone's
+    __device__ __forceinline__ void arrived() {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) lead[t] = left[t];
+    }
+    // the four registers from element `by` on of two words
+    __device__ __forceinline__ static uint4 shifted(const uint4& a, const uint4& b, int by) {
+        uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        const int words = by * static_cast<int>(sizeof(T)) / 4;
+        if (words & 2) {
+#pragma unroll
+            for (int k = 0; k < 6; ++k) u[k] = u[k + 2];
+        }
+        if (words & 1) {
+#pragma unroll
+            for (int k = 0; k < 5; ++k) u[k] = u[k + 1];
+        }
+        if (sizeof(T) == 2 && (by & 1)) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = __funnelshift_r(u[k], u[k + 1], 16);
+        }
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    // `fetched`: the next row's fetches have been made, and its half is the other one
+    __device__ __forceinline__ void get(int t, float2 (&v)[COLS / 2], const Columns<N, THREADS>& at) const {
+        const uint4* from = room + (half * NT + t) * words();
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) {
+            const int w = q * team_threads<THREADS>() + threadIdx.x;
+            const uint4 u = shifted(from[w], from[w + 1], lead[t]);
+#pragma unroll
+            for (int p = 0; p < N / 2; ++p) v[q * (N / 2) + p] = word_pair<T>(u, p);
+            const int c = at.of(q * N);
+            if (c + N > n) {
+                rare();
+#pragma unroll
+                for (int p = 0; p < N / 2; ++p) {
+                    if (c + 2 * p >= n) v[q * (N / 2) + p].x = 0.f;
+                    if (c + 2 * p + 1 >= n) v[q * (N / 2) + p].y = 0.f;
+                }
+            }
         }
     }
-    __device__ __forceinline__ static void commit() {}
-    __device__ __forceinline__ static void arrived() {}
-    __device__ __forceinline__ void get(int t, float2 (&x)[COLS / 2]) const {
+    // which: 0 or 1, the output's room; ends behind a barrier
+    __device__ __forceinline__ void put(int which, T* row, const Columns<N, THREADS>& at, const float2 (&v)[COLS / 2]) const {
+        uint4* mine = out + which * words();
 #pragma unroll
-        for (int p = 0; p < COLS / 2; ++p) x[p] = v[t][p];
-    }
-    __device__ __forceinline__ void put(T* row, int n, const Columns<1, THREADS>& at, const float2 (&x)[COLS / 2]) const {
+        for (int q = 0; q < kWords; ++q) {
+            float x[N];
 #pragma unroll
-        for (int p = 0; p < COLS / 2; ++p) {
-            if (at.of(2 * p) < n) row[at.of(2 * p)] = from_f32<T>(x[p].x);
-            if (at.of(2 * p + 1) < n) row[at.of(2 * p + 1)] = from_f32<T>(x[p].y);
+            for (int k = 0; k < N; ++k) x[k] = k & 1 ? v[(q * N + k) / 2].y : v[(q * N + k) / 2].x;
+            mine[q * team_threads<THREADS>() + threadIdx.x] = Word<T>::pack(x);
         }
+        __syncthreads();
+        const int shift = row_lead<T, N>(row), all = kWords * team_threads<THREADS>(), width = all * N;
+        T* to = row - shift + at.first;
+        auto store = [&](int w) {   // columns w N - shift ... of the CTA's
+            const int c = w * N - shift;
+            if (c >= width || at.first + c >= n) return;
+            const uint4 zero = make_uint4(0, 0, 0, 0);
+            const uint4 u = shift == 0 ? mine[w] : shifted(w > 0 ? mine[w - 1] : zero, w < all ? mine[w] : zero, N - shift);
+            if (c >= 0 && c + N <= width && at.first + c + N <= n) {
+                *reinterpret_cast<uint4*>(to + w * N) = u;
+            } else {
+                rare();
+                const uint32_t r[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (c + e >= 0 && c + e < width && at.first + c + e < n) {
+                        if constexpr (sizeof(T) == 4)
+                            to[w * N + e] = __uint_as_float(r[e]);
+                        else
+                            reinterpret_cast<uint16_t*>(to)[w * N + e] = static_cast<uint16_t>(r[e / 2] >> (e & 1 ? 16 : 0));
+                    }
+            }
+        };
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) store(q * team_threads<THREADS>() + threadIdx.x);
+        if (threadIdx.x == 0) store(all);
     }
 };
 
@@ -315,27 +413,26 @@ __device__ __forceinline__ float branch_weight(const JoinArgs& a, int64_t group,
     return a.w_post != nullptr ? w * a.w_post[c] : w;
 }
 
-template <typename T, int VEC, int COLS, int THREADS>
-__global__ void __launch_bounds__(THREADS ? THREADS : VEC > 1 ? 256 : kTeam, VEC == 8 && COLS == 8 ? 3 : THREADS == 512 || VEC == 1 ? 1 : 2) join_kernel(const __grid_constant__ JoinArgs a, int ranks, JoinRows<const T> x, JoinRows<const T> y, JoinRows<T> s, JoinRows<T> z) {
+template <typename T, int COLS, int THREADS, bool SHIFT>
+__global__ void __launch_bounds__(THREADS ? THREADS : 128, (sizeof(T) == 2 && COLS == 8 && !SHIFT ? 768 : 512) / (THREADS ? THREADS : 128)) join_kernel(const __grid_constant__ JoinArgs a, int ranks, JoinRows<const T> x, JoinRows<const T> y, JoinRows<T> s, JoinRows<T> z) {
+    constexpr int VEC = Word<T>::kN;
     extern __shared__ __align__(16) float4 smem[];
     __shared__ __align__(16) ExchangeRoom room;
     const int width = team_threads<THREADS>() * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks, teams = gridDim.x / ranks;
     const Columns<VEC, THREADS> at{rank * width};
     const ByColumn<VEC, COLS, THREADS> weight{smem}, w_pre{smem + width / 4};
-    Held<T, VEC, COLS, 2, THREADS> in(smem + width / 2, a.n, at);
-    Mask<VEC, COLS, THREADS> mask{reinterpret_cast<uint16_t*>(smem + width / 2 + (VEC > 1 ? 2 * 2 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
+    Held<T, COLS, 2, THREADS, SHIFT> in(smem + width / 2, a.n, at);
+    Mask<VEC, COLS, THREADS> mask{reinterpret_cast<uint16_t*>(smem + width / 2 + Held<T, COLS, 2, THREADS, SHIFT>::bytes(team_threads<THREADS>(), 2) / 16), width, 0, VEC == 8 && a.n % 8 == 0};
     const bool branch = y.p != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr;
     const float inv_n = 1.f / static_cast<float>(a.n);
     int64_t i = a.m * team / teams, change = i;   // change: the row at which the next gate row begins
     const int64_t last = a.m * (team + 1) / teams;
     auto fetch = [&](int64_t row) {
-        in.fetch(0, x.row(row), a.n, at);
-        if (branch) in.fetch(1, y.row(row), a.n, at);
+        in.fetch(0, x, row, at);
+        if (branch) in.fetch(1, y, row, at);
     };
-    if (VEC > 1) {
-        if (i < last) fetch(i);
-        in.commit();
-    }
+    if (i < last) fetch(i);
+    in.commit();
     const Keep keep(a.dropout);
     if (pre) w_pre.set(a.n, at, [&](int c) { return __ldg(a.w_pre + c); });
     Exchange<THREADS> ex(&room, ranks);
@@ -345,23 +442,24 @@ __global__ void __launch_bounds__(THREADS ? THREADS : VEC > 1 ? 256 : kTeam, VEC
             change = (group + 1) * a.group_rows;
             weight.set(a.n, at, [&](int c) { return branch_weight(a, group, c); });
         }
-        if (VEC == 1 || i + 1 < last) fetch(VEC == 1 ? i : i + 1);
+        if (SHIFT) in.arrived();
+        if (i + 1 < last) fetch(i + 1);
         in.commit();
-        in.arrived();
+        if (!SHIFT) in.arrived();
         uint32_t r[COLS / 2];
         if (a.drop) mask.make(a, keep, i, at, r);
         float2 h[COLS / 2], v[COLS / 2], st = make_float2(0.f, 1.f), to = make_float2(0.f, 1.f);
         if (branch) {
-            in.get(1, h);
+            in.get(1, h, at);
             if (post) {
                 st = held_norm<VEC, COLS, THREADS>(a, ex, at, h, inv_n);
 #pragma unroll
                 for (int p = 0; p < COLS / 2; ++p) h[p] = __fmul2_rn(__fadd2_rn(h[p], pair(-st.x)), pair(st.y));
             }
         }
-        in.get(0, v);
+        in.get(0, v, at);
         joined<VEC, COLS, THREADS>(a, keep, branch, h, r, weight, v);
-        if (s.p != nullptr) in.put(s.row(i), a.n, at, v);
+        if (s.p != nullptr) in.put(0, s.row(i), at, v);
         if (pre) {
             to = held_norm<VEC, COLS, THREADS>(a, ex, at, v, inv_n);
 #pragma unroll
@@ -371,7 +469,7 @@ __global__ void __launch_bounds__(THREADS ? THREADS : VEC > 1 ? 256 : kTeam, VEC
 #pragma unroll
                 for (int e = 0; e < 2; ++e) v[2 * k + e] = __fmul2_rn(__fmul2_rn(__fadd2_rn(v[2 * k + e], pair(-to.x)), pair(to.y)), w[e]);
             }
-            in.put(z.row(i), a.n, at, v);
+            in.put(1, z.row(i), at, v);
         }
         if (a.stats != nullptr && threadIdx.x == 0 && rank == 0) a.stats[i] = make_float4(st.x, st.y, to.x, to.y);
     }
@@ -405,17 +503,18 @@ struct Sums {
 __device__ __forceinline__ int64_t part_begin(const Parts& p, int64_t k) { return k / p.per_group * p.rows + k % p.per_group * p.rows / p.per_group; }
 __device__ __forceinline__ int64_t part_end(const Parts& p, int64_t k) { return k / p.per_group * p.rows + (k % p.per_group + 1) * p.rows / p.per_group; }
 
-template <typename T, int VEC, int COLS, int THREADS>
-__global__ void __launch_bounds__(THREADS ? THREADS : kTeam, THREADS == 256 ? 2 : 1) join_backward_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ Parts parts, const __grid_constant__ Sums out, int ranks,
+template <typename T, int COLS, int THREADS, bool SHIFT>
+__global__ void __launch_bounds__(THREADS ? THREADS : 128, 512 / (THREADS ? THREADS : 128)) join_backward_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ Parts parts, const __grid_constant__ Sums out, int ranks,
                                                               JoinRows<const T> x, JoinRows<const T> y, JoinRows<const T> ds, JoinRows<const T> dz, JoinRows<T> dx, JoinRows<T> dy) {
+    constexpr int VEC = Word<T>::kN;
     extern __shared__ __align__(16) float4 smem[];
     __shared__ __align__(16) ExchangeRoom room;
     const int width = team_threads<THREADS>() * COLS, rank = blockIdx.x % ranks, team = blockIdx.x / ranks;
     const Columns<VEC, THREADS> at{rank * width};
     const ByColumn<VEC, COLS, THREADS> weight{smem}, w_pre{smem + width / 4};
     const ByColumn<VEC, COLS, THREADS> sum_post{smem + width / 2};
-    Held<T, VEC, COLS, 4, THREADS> in(smem + 3 * width / 4, a.n, at);
-    Mask<VEC, COLS, THREADS> mask{reinterpret_cast<uint16_t*>(smem + 3 * width / 4 + (VEC > 1 ? 2 * 4 * width / VEC : 0)), width, 0, VEC == 8 && a.n % 8 == 0};
+    Held<T, COLS, 4, THREADS, SHIFT> in(smem + 3 * width / 4, a.n, at);
+    Mask<VEC, COLS, THREADS> mask{reinterpret_cast<uint16_t*>(smem + 3 * width / 4 + Held<T, COLS, 4, THREADS, SHIFT>::bytes(team_threads<THREADS>(), 2) / 16), width, 0, VEC == 8 && a.n % 8 == 0};
     const bool branch = y.p != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr && dz.p != nullptr, stream = ds.p != nullptr;
     const float inv_n = 1.f / static_cast<float>(a.n);
     float2 sum_branch[COLS / 2], sum_pre[COLS / 2];
@@ -427,14 +526,12 @@ __global__ void __launch_bounds__(THREADS ? THREADS : kTeam, THREADS == 256 ? 2 
     const int64_t last_part = parts.count * (team + 1) / parts.teams, last = part_end(parts, last_part - 1);
     int64_t i = part_begin(parts, k), end = part_end(parts, k);
     auto fetch = [&](int64_t row) {
-        if (pre) in.fetch(0, x.row(row), a.n, at), in.fetch(3, dz.row(row), a.n, at);
-        if (branch) in.fetch(1, y.row(row), a.n, at);
-        if (stream) in.fetch(2, ds.row(row), a.n, at);
+        if (pre) in.fetch(0, x, row, at), in.fetch(3, dz, row, at);
+        if (branch) in.fetch(1, y, row, at);
+        if (stream) in.fetch(2, ds, row, at);
     };
-    if (VEC > 1) {
-        if (i < last) fetch(i);
-        in.commit();
-    }
+    if (i < last) fetch(i);
+    in.commit();
     const Keep keep(a.dropout);
     if (pre) w_pre.set(a.n, at, [&](int c) { return __ldg(a.w_pre + c); });
     Exchange<THREADS> ex(&room, ranks);
@@ -443,14 +540,15 @@ __global__ void __launch_bounds__(THREADS ? THREADS : kTeam, THREADS == 256 ? 2 
         if (branch && i < end) weight.set(a.n, at, [&](int c) { return branch_weight(a, group, c); });
         for (; i < end; ++i) {
             const float4 st = a.stats != nullptr ? a.stats[i] : make_float4(0.f, 1.f, 0.f, 1.f);
-            if (VEC == 1 || i + 1 < last) fetch(VEC == 1 ? i : i + 1);
+            if (SHIFT) in.arrived();
+        if (i + 1 < last) fetch(i + 1);
             in.commit();
-            in.arrived();
+            if (!SHIFT) in.arrived();
             uint32_t r[COLS / 2];
             if (a.drop) mask.make(a, keep, i, at, r);
             float2 h[COLS / 2], g[COLS / 2];
             if (branch) {
-                in.get(1, h);
+                in.get(1, h, at);
                 if (post) {
 #pragma unroll
                     for (int p = 0; p < COLS / 2; ++p) h[p] = __fmul2_rn(__fadd2_rn(h[p], pair(-st.x)), pair(st.y));
@@ -458,9 +556,9 @@ __global__ void __launch_bounds__(THREADS ? THREADS : kTeam, THREADS == 256 ? 2 
             }
             if (pre) {
                 float2 v[COLS / 2], d[COLS / 2], c0 = pair(0.f), c1 = pair(0.f);
-                in.get(0, v);
+                in.get(0, v, at);
                 joined<VEC, COLS, THREADS>(a, keep, branch, h, r, weight, v);
-                in.get(3, d);
+                in.get(3, d, at);
 #pragma unroll
                 for (int q = 0; q < COLS / 4; ++q) {
                     float2 w[2];
@@ -481,7 +579,7 @@ __global__ void __launch_bounds__(THREADS ? THREADS : kTeam, THREADS == 256 ? 2 
                 const float2 k01 = row_sums(a, ex, c0, c1);
                 const float2 k0 = pair(-st.w * k01.x * inv_n), k1 = pair(-st.w * k01.y * inv_n);
                 if (stream) {
-                    in.get(2, g);
+                    in.get(2, g, at);
                 } else {
 #pragma unroll
                     for (int p = 0; p < COLS / 2; ++p) g[p] = pair(0.f);
@@ -493,7 +591,7 @@ __global__ void __launch_bounds__(THREADS ? THREADS : kTeam, THREADS == 256 ? 2 
 #pragma unroll
                 for (int p = 0; p < COLS / 2; ++p) g[p] = __ffma2_rn(v[p], k1, __ffma2_rn(d[p], pair(st.w), g[p]));
             } else if (stream) {
-                in.get(2, g);
+                in.get(2, g, at);
             } else {
 #pragma unroll
                 for (int p = 0; p < COLS / 2; ++p) g[p] = pair(0.f);
@@ -502,7 +600,7 @@ __global__ void __launch_bounds__(THREADS ? THREADS : kTeam, THREADS == 256 ? 2 
                 float2 v[COLS / 2];
 #pragma unroll
                 for (int p = 0; p < COLS / 2; ++p) v[p] = __fmul2_rn(g[p], pair(a.residual));
-                in.put(dx.row(i), a.n, at, v);
+                in.put(0, dx.row(i), at, v);
             }
             if (!branch) continue;
             float2 c0 = pair(0.f), c1 = pair(0.f);
@@ -534,7 +632,7 @@ __global__ void __launch_bounds__(THREADS ? THREADS : kTeam, THREADS == 256 ? 2 
 #pragma unroll
                 for (int p = 0; p < COLS / 2; ++p) g[p] = __fmul2_rn(__ffma2_rn(h[p], k1, g[p]), pair(st.y));
             }
-            in.put(dy.row(i), a.n, at, g);
+            in.put(1, dy.row(i), at, g);
         }
         if (out.gate != nullptr || out.post != nullptr) {
 #pragma unroll
@@ -651,12 +749,16 @@ bool in_words(const JoinTensors& t, int64_t m, int bytes) {
 struct Shape {
     int threads, ranks, smem;
 };
-template <typename T, int VEC, int COLS> Shape shape_of(int n, int vectors, int tensors, bool drop) {
+// vectors: weights and sums by column in shared memory
+template <typename T, int COLS, int NT, bool SHIFT> int smem_of(int threads, int vectors, bool numbers) {
+    return threads * COLS * 4 * vectors + Held<T, COLS, NT, 0, SHIFT>::bytes(threads, 2) + (numbers ? 2 * 2 * (threads * COLS + 16) : 0);
+}
+template <typename T, int COLS, int NT, bool SHIFT> Shape shape_of(int n, int vectors, bool drop) {
     Shape s{32, 1, 0};
-    while (s.threads < kTeam && s.threads * COLS < n) s.threads *= 2;
+    const int most = sizeof(T) == 4 && COLS == 16 && SHIFT ? kTeam / 2 : kTeam;   // what shared memory holds
+    while (s.threads < most && s.threads * COLS < n) s.threads *= 2;
     while (s.threads * COLS * s.ranks < n) s.ranks *= 2;
-    const int width = s.threads * COLS;
-    s.smem = width * (4 * vectors + (VEC > 1 ? 2 * tensors * static_cast<int>(sizeof(T)) : 0)) + (drop && !(VEC == 8 && n % 8 == 0) ? 2 * 2 * (width + 16) : 0);
+    s.smem = smem_of<T, COLS, NT, SHIFT>(s.threads, vectors, drop && !(sizeof(T) == 2 && n % 8 == 0));
     return s;
 }
 // teams: clusters of s.ranks CTAs
@@ -680,51 +782,51 @@ template <typename K, typename... A> int start(K kern, const Shape& s, int64_t t
     note_launch();
     return check_launch();
 }
-template <typename T, int VEC, int COLS> int most_smem(int vectors, int tensors) {
-    const int all = kTeam * COLS * (4 * vectors + (VEC > 1 ? 2 * tensors * static_cast<int>(sizeof(T)) : 0)) + 2 * 2 * (kTeam * COLS + 16), limit = 227 * 1024 - 1024;
+template <typename T, int COLS, int NT, bool SHIFT> int most_smem(int vectors) {
+    const int all = smem_of<T, COLS, NT, SHIFT>(kTeam, vectors, true), limit = 227 * 1024 - 1024;
     return all < limit ? all : limit;
 }
+template <typename T> JoinRows<const T> input(const void* p, int64_t ld, const JoinArgs& a) {
+    const T* t = static_cast<const T*>(p);
+    return {t, ld, t == nullptr ? t : t + (a.m - 1) * ld + a.n};
+}
+template <typename T> JoinRows<T> output(void* p, int64_t ld) { return {static_cast<T*>(p), ld, nullptr}; }
 
-template <typename T, int VEC, int COLS> int forward_as(const JoinArgs& a, const JoinTensors& t, cudaStream_t s) {
-    const Shape shape = shape_of<T, VEC, COLS>(a.n, 2, 2, a.drop != 0);
+template <typename T, int COLS, bool SHIFT> int forward_as(const JoinArgs& a, const JoinTensors& t, cudaStream_t s) {
+    const Shape shape = shape_of<T, COLS, 2, SHIFT>(a.n, 2, a.drop != 0);
     // as many as an SM holds, by their registers and by their shared memory
-    int per_sm = (COLS == 8 && VEC == 8 ? 768 : 512) / shape.threads;
+    int per_sm = (COLS == 8 && sizeof(T) == 2 && !SHIFT ? 768 : 512) / shape.threads;
     if (per_sm * (shape.smem + 2048) > 220 * 1024) per_sm = 220 * 1024 / (shape.smem + 2048);
     const int64_t most = static_cast<int64_t>(per_sm > 1 ? per_sm : 1) * kNumSMs / shape.ranks;
-    // with words, eight columns a thread go up to 256 threads and sixteen begin there
-    auto kern = join_kernel<T, VEC, COLS, COLS == 16 ? 512 : 0>;
-    if constexpr (VEC > 1)
-        if (shape.threads == 256) kern = join_kernel<T, VEC, COLS, 256>;
-    return start(kern, shape, a.m < most ? a.m : most, most_smem<T, VEC, COLS>(2, 2), s, a, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
-                 JoinRows<const T>{static_cast<const T*>(t.b), t.ld_b}, JoinRows<T>{static_cast<T*>(t.e), t.ld_e}, JoinRows<T>{static_cast<T*>(t.f), t.ld_f});
+    // sixteen columns a thread begin at 256 threads, eight end there
+    constexpr int kOther = COLS == 8 ? 0 : sizeof(T) == 4 && SHIFT ? 256 : 512;
+    auto kern = join_kernel<T, COLS, kOther, SHIFT>;
+    if (shape.threads == 256) kern = join_kernel<T, COLS, 256, SHIFT>;
+    return start(kern, shape, a.m < most ? a.m : most, most_smem<T, COLS, 2, SHIFT>(2), s, a, shape.ranks, input<T>(t.a, t.ld_a, a), input<T>(t.b, t.ld_b, a), output<T>(t.e, t.ld_e),
+                 output<T>(t.f, t.ld_f));
 }
-template <typename T, int VEC, int COLS> int backward_as(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, cudaStream_t s) {
-    const Shape shape = shape_of<T, VEC, COLS>(a.n, 3, 4, a.drop != 0);
-    auto kern = join_backward_kernel<T, VEC, COLS, 0>;
-    if constexpr (VEC > 1) {
-        if (shape.threads == 512) kern = join_backward_kernel<T, VEC, COLS, 512>;
-        if constexpr (VEC != 8 || COLS != 8)   // 16-bit words by eight columns: up to 256 columns, or from 4096 on
-            if (shape.threads == 256) kern = join_backward_kernel<T, VEC, COLS, 256>;
-    }
-    return start(kern, shape, p.teams, most_smem<T, VEC, COLS>(3, 4), s, a, p, sums, shape.ranks, JoinRows<const T>{static_cast<const T*>(t.a), t.ld_a},
-                 JoinRows<const T>{static_cast<const T*>(t.b), t.ld_b}, JoinRows<const T>{static_cast<const T*>(t.c), t.ld_c}, JoinRows<const T>{static_cast<const T*>(t.d), t.ld_d},
-                 JoinRows<T>{static_cast<T*>(t.e), t.ld_e}, JoinRows<T>{static_cast<T*>(t.f), t.ld_f});
+template <typename T, int COLS, bool SHIFT> int backward_as(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, cudaStream_t s) {
+    const Shape shape = shape_of<T, COLS, 4, SHIFT>(a.n, 3, a.drop != 0);
+    auto kern = join_backward_kernel<T, COLS, 0, SHIFT>;
+    if (shape.threads == 512) kern = join_backward_kernel<T, COLS, 512, SHIFT>;
+    if constexpr (sizeof(T) == 4 || COLS == 16 || SHIFT)   // 16-bit words by eight columns: up to 256 columns, or from 4096 on
+        if (shape.threads == 256) kern = join_backward_kernel<T, COLS, 256, SHIFT>;
+    return start(kern, shape, p.teams, most_smem<T, COLS, 4, SHIFT>(3), s, a, p, sums, shape.ranks, input<T>(t.a, t.ld_a, a), input<T>(t.b, t.ld_b, a), input<T>(t.c, t.ld_c, a),
+                 input<T>(t.d, t.ld_d, a), output<T>(t.e, t.ld_e), output<T>(t.f, t.ld_f));
 }
 
 template <typename T> int forward(const JoinArgs& a, const JoinTensors& t, cudaStream_t s) {
-    constexpr int N = Word<T>::kN;
-    if (!in_words(t, a.m, sizeof(T))) return forward_as<T, 1, 8>(a, t, s);
-    return a.n <= 8 * 256 ? forward_as<T, N, 8>(a, t, s) : forward_as<T, N, 16>(a, t, s);
+    if (!in_words(t, a.m, sizeof(T))) return a.n <= 8 * 256 ? forward_as<T, 8, true>(a, t, s) : forward_as<T, 16, true>(a, t, s);
+    return a.n <= 8 * 256 ? forward_as<T, 8, false>(a, t, s) : forward_as<T, 16, false>(a, t, s);
 }
 // Columns of a thread of the backward kernel.  Sixteen keep two CTAs on an SM at 4096 columns; with random numbers of odd rows beside them
 // their shared memory ends at 4096.
 int backward_columns(int64_t n, int bytes, bool words, bool drop) { return bytes == 2 && words && n > 256 && (n <= 8 * kTeam || n % 8 == 0 || !drop) ? 16 : 8; }
 template <typename T> int backward(const JoinArgs& a, const JoinTensors& t, const Parts& p, const Sums& sums, bool words, int columns, cudaStream_t s) {
-    constexpr int N = Word<T>::kN;
-    if (!words) return backward_as<T, 1, 8>(a, t, p, sums, s);
+    if (!words) return backward_as<T, 8, true>(a, t, p, sums, s);
     if constexpr (sizeof(T) == 2)
-        if (columns == 16) return backward_as<T, N, 16>(a, t, p, sums, s);
-    return backward_as<T, N, 8>(a, t, p, sums, s);
+        if (columns == 16) return backward_as<T, 16, false>(a, t, p, sums, s);
+    return backward_as<T, 8, false>(a, t, p, sums, s);
 }
 
 // A row tensor: rows that do not overlap, elements on their type's boundary.
