@@ -343,6 +343,71 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
     }
 }
 
+// ---- the loss alone, many rows: one CTA a row, words from memory into registers ------------------
+//
+// Nothing of the row has to stay, so a row of any length takes one CTA and four of them an SM; a thread has its next four words on their
+// way while it takes four in.
+
+constexpr int kScoreThreads = 256;
+template <typename T, bool POLICY> __global__ void __launch_bounds__(kScoreThreads, 3) token_score_kernel(const __grid_constant__ TokenArgs a, const T* logits) {
+    constexpr int N = Word<T>::kN;
+    __shared__ MaxSum part[kScoreThreads / 32];
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    const int64_t i = blockIdx.x;
+    const int at = __ldg(a.index + i);
+    if (!has_token(a, at)) {
+        if (t == 0) finish_without(a, i, POLICY);
+        return;
+    }
+    const T* row = logits + i * a.ld;
+    const int n = static_cast<int>(a.v), lead = row_lead<T, N>(row), all = (lead + n + N - 1) / N;
+    const int head = lead != 0 ? 0 : -1, tail = (lead + n) % N != 0 ? all - 1 : -1;   // words over an end of the row
+    const int batches = (all + kBatch * kScoreThreads - 1) / (kBatch * kScoreThreads);
+    const uint4* from = reinterpret_cast<const uint4*>(row - lead) + t;
+    auto plain = [&](int b) { return (b > 0 || head < 0) && (b + 1) * kBatch * kScoreThreads <= all - (tail >= 0); };
+    uint4 next[kBatch];
+    auto fetch = [&](int b) {
+        if (plain(b)) {
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) next[j] = __ldg(from + (b * kBatch + j) * kScoreThreads);
+        } else {
+            rare();
+            float x[N];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const int w = (b * kBatch + j) * kScoreThreads + t;
+                if (w < all && w != head && w != tail) {
+                    next[j] = __ldg(from + (b * kBatch + j) * kScoreThreads);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[e] = -INFINITY;
+                    if (w < all) load_slot<T, N>(row, static_cast<int64_t>(w) * N - lead, n, -INFINITY, x);
+                    next[j] = Word<T>::pack(x);
+                }
+            }
+        }
+    };
+    fetch(0);
+    RowInputs in{};
+    if (warp == 0) in = row_inputs<POLICY>(a, i, to_f32(row[at]));
+    MaxSum sum{-INFINITY, 0.f};
+#pragma unroll 1
+    for (int b = 0; b < batches; ++b) {
+        float x[kBatch][N];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) Word<T>::unpack(next[j], x[j]);
+        if (b + 1 < batches) fetch(b + 1);
+        absorb(a, sum, x);
+    }
+    sum = joined(a, sum);
+    if (lane == 0) part[warp] = sum;
+    __syncthreads();
+    if (warp != 0) return;
+    sum = joined(a, lane < kScoreThreads / 32 ? part[lane] : MaxSum{-INFINITY, 0.f});
+    const RowScalars scalars = row_scalars<POLICY>(a, in, sum);
+    if (lane == 0) write_row(a, i, sum, scalars, POLICY);
+}
+
 // ---- any length and layout: the row is read twice -----------------------------------------------------------
 
 // The largest of a row and its sum of exponentials, over the CTA.
@@ -555,9 +620,13 @@ template <typename T, bool POLICY, bool GRADIENT> int shared(const TokenArgs& a,
     return check_launch();
 }
 
+// Rows, and words of a row, from which the loss alone takes its own kernel.
+constexpr int64_t kScoreRows = 2 * kNumSMs, kScoreWords = 4096;
+
 template <typename T, int VEC, bool POLICY> int rows(const TokenArgs& a, const T* logits, T* dlogits, cudaStream_t s) {
     if constexpr (VEC > 1) {
         const int64_t words = (a.v + 2 * (VEC - 1)) / VEC;   // of a row, at most
+        const bool score = dlogits == nullptr && a.m >= kScoreRows && words > kScoreWords;
         // three CTAs an SM; a cluster's CTAs hold what they can of the longest rows
         int64_t ranks = words <= 4096 ? 1 : (words + 2047) / 2048;
         if (ranks > kMostRanks) ranks = kMostRanks;
@@ -566,6 +635,11 @@ template <typename T, int VEC, bool POLICY> int rows(const TokenArgs& a, const T
         if ((words + ranks - 1) / ranks + kBatch * kShared <= kMostWords && a.m * ranks < (int64_t(1) << 31)) {
             if constexpr (POLICY)
                 if (dlogits != nullptr) return shared<T, true, true>(a, logits, dlogits, words, static_cast<int>(ranks), s);
+            if (score) {
+                token_score_kernel<T, POLICY><<<static_cast<unsigned>(a.m), kScoreThreads, 0, s>>>(a, logits);
+                note_launch();
+                return check_launch();
+            }
             return shared<T, POLICY, false>(a, logits, dlogits, words, static_cast<int>(ranks), s);
         }
     }
