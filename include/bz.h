@@ -636,14 +636,15 @@ int bz_distill_backward(const void* logits, int64_t ld, int dtype, int64_t m, in
  * -inf has lp = -inf and takes no gradient.  Row scalars (lp, ratios, sums over a sequence) are formed in binary64
  * from a binary32 maximum and sum, and rounded once when they are stored.
  *   logits   device [m][v] with ld, dtype BZ_F32, _F16, _BF16;  index device int32 [m];  temperature > 0, finite, and so is
- *            log2(e) / temperature.
+ *            log2(e) / temperature (from 4.3e-39 on).
  *   logp     device binary32 [m], or NULL: receives lp.
  *   stats    device binary32 [m][4], 16-byte aligned, for the backward call: the row's largest logit, the sum of
  *            exp((logits - that) / T), the slope d loss / d lp, and (an int32's bits) the place of the row's upstream gradient
  *            in dloss.
- *   dlogits  device [m][v] with ld_d, dtype's elements, or NULL: the loss alone.  It may be logits itself (ld_d == ld).
+ *   dlogits  device [m][v] with ld_d, dtype's elements, or NULL: the loss alone.  It may be logits itself (ld_d == ld), or else memory apart.
  *            dlogits[c] = dloss * slope / T * ([c == a] - softmax(z)[c]).
- * v < 2^31; m == 0 is a successful no-op; v == 0 counts as rows without a token.
+ * m < 2^31, v up to 2^31 - 16384, leading dimensions below 2^31; m == 0 is a successful no-op; v == 0 counts as rows without a
+ * token.  T is taken as log2(e) / c with c rounded to binary32: it differs from the given one by 2^-24 at most, relatively.
  */
 
 /*

@@ -651,7 +651,6 @@ template <typename T, int VEC, bool POLICY> int rows(const TokenArgs& a, const T
 template <typename T, int VEC> int launch(const TokenArgs& a, const T* logits, T* dlogits, What what, cudaStream_t s) {
     if (what == kPolicy) return rows<T, VEC, true>(a, logits, dlogits, s);
     if (what == kScore) return rows<T, VEC, false>(a, logits, dlogits, s);
-    if (a.v >= (int64_t(1) << 31) - kGradientThreads * kGradientColumns - 16) return BZ_ERR_UNSUPPORTED;
     const int64_t each = (a.v + (VEC - 1) + kGradientColumns - 1) / kGradientColumns;   // threads for a row
     const int threads = static_cast<int>(each < kGradientThreads ? (each + 31) / 32 * 32 : kGradientThreads);
     const int64_t shares = (each + threads - 1) / threads;
@@ -675,10 +674,13 @@ int dispatch(const TokenArgs& a, int dtype, int64_t m, const void* logits, void*
     return dispatch<__nv_bfloat16>(a, m, logits, dlogits, what, s);
 }
 
+// binary32 and int32 arrays lie on their type's boundary
+template <typename... P> bool on_boundary(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3u) == 0; }
+
 int check(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const int32_t* index, float temperature, const void* stats, const void* dlogits, int64_t ld_d) {
     const int bytes = element_bytes(dtype);
     if (bytes == 0 || m < 0 || v < 0 || !(temperature > 0.f) || isinf(temperature) || isinf(kLog2e / temperature) || !aligned16(stats)) return BZ_ERR_INVALID_ARG;
-    if (v >= (int64_t(1) << 31) || m >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
+    if (v > (int64_t(1) << 31) - 16384 || m >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
     if (m == 0) return BZ_OK;
     if (index == nullptr) return BZ_ERR_INVALID_ARG;
     if (v == 0) return BZ_OK;
@@ -708,7 +710,7 @@ using namespace bz;
 extern "C" int bz_policy(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const int32_t* index, const float* old_logp,
                          const float* ref_logp, const float* advantage, float temperature, float clip_low, float clip_high, float kl,
                          const float* dloss, float* loss, float* logp, float* stats, void* dlogits, int64_t ld_d, void* stream) {
-    if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f) || !(kl >= 0.f) || isinf(kl)) return BZ_ERR_INVALID_ARG;
+    if (!on_boundary(index, old_logp, ref_logp, advantage, dloss, loss, logp) || !(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f) || !(kl >= 0.f) || isinf(kl)) return BZ_ERR_INVALID_ARG;
     const int st = check(logits, ld, dtype, m, v, index, temperature, stats, dlogits, ld_d);
     if (st != BZ_OK || m == 0) return st;
     if (advantage == nullptr || (kl != 0.f && ref_logp == nullptr) || (loss == nullptr && logp == nullptr && stats == nullptr && dlogits == nullptr))
@@ -727,7 +729,7 @@ extern "C" int bz_policy(const void* logits, int64_t ld, int dtype, int64_t m, i
 extern "C" int bz_preference(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const int32_t* index, const float* ref_logp,
                              const int32_t* starts, int64_t pairs, float temperature, float beta, float margin, float smoothing, int mean,
                              const float* dloss, float* loss, float* reward, float* logp, float* stats, void* dlogits, int64_t ld_d, void* stream) {
-    if (pairs < 0 || !isfinite(beta) || !isfinite(margin) || !(smoothing >= 0.f && smoothing <= 1.f)) return BZ_ERR_INVALID_ARG;
+    if (!on_boundary(index, ref_logp, starts, dloss, loss, reward, logp) || pairs < 0 || !isfinite(beta) || !isfinite(margin) || !(smoothing >= 0.f && smoothing <= 1.f)) return BZ_ERR_INVALID_ARG;
     if (pairs >= (int64_t(1) << 30)) return BZ_ERR_UNSUPPORTED;
     int st = check(logits, ld, dtype, m, v, index, temperature, stats, dlogits, ld_d);
     if (st != BZ_OK) return st;
@@ -755,6 +757,7 @@ extern "C" int bz_preference(const void* logits, int64_t ld, int dtype, int64_t 
 
 extern "C" int bz_token_loss_backward(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const int32_t* index, float temperature,
                                       const float* stats, const float* dloss, void* dlogits, int64_t ld_d, void* stream) {
+    if (!on_boundary(index, dloss)) return BZ_ERR_INVALID_ARG;
     const int st = check(logits, ld, dtype, m, v, index, temperature, stats, dlogits, ld_d);
     if (st != BZ_OK || m == 0 || v == 0) return st;
     if (stats == nullptr || dlogits == nullptr) return BZ_ERR_INVALID_ARG;

@@ -26,6 +26,9 @@ def tokens(logits, index, T):
     v = z.shape[1]
     there = (index.cpu() >= 0) & (index.cpu() < v)
     at = torch.where(there, index.cpu().long(), torch.zeros(1, dtype=torch.long))
+    # the largest goes first: beside a type's lowest value 64 bits would not hold the logarithm
+    top = z.amax(1, keepdim=True)
+    z = z - torch.where(top == -math.inf, torch.zeros_like(top), top)
     lse = torch.logsumexp(z, 1)
     log_q = torch.where(lse[:, None] == -math.inf, torch.full_like(z, -math.inf), z - lse[:, None])
     lp = torch.where(there, log_q[torch.arange(len(at)), at], torch.zeros(1, dtype=torch.float64))
@@ -329,3 +332,51 @@ def test_no_vocabulary_and_no_positions():
     x = make(4, 30, torch.float32, 0)
     loss, reward, logp, stats, d = bz.preference(x["logits"], x["index"], torch.zeros(1, dtype=torch.int32, device="cuda"), dloss=torch.empty(0, device="cuda"))
     assert loss.numel() == 0 and (d == 0).all() and near(logp, tokens(x["logits"], x["index"], 1.0)[0], 2 * TOL)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,v", [(9, 500), (400, 9001), (300, 70001)])
+def test_rows_far_from_zero(dtype, m, v):
+    """Rows of the type's lowest value alone (every token is as likely), lowest values beside ordinary ones, logits around a large number."""
+    x = make(m, v, dtype, 11)
+    low = torch.finfo(dtype).min
+    x["index"] = torch.full((m,), 3, dtype=torch.int32, device="cuda")
+    x["logits"][0] = low
+    x["logits"][1] = low
+    x["logits"][1, 3] = 1.0
+    x["logits"][2, ::2] = low
+    x["logits"][3] = 30000.0
+    x["logits"][3, 3] += 32.0
+    x["logits"][4] = -30000.0
+    loss, logp, stats, d = bz.policy(x["logits"], x["index"], torch.ones(m, device="cuda"), dloss=torch.ones(m, device="cuda"))
+    lp, q, there, at = tokens(x["logits"][:6], x["index"][:6], 1.0)
+    assert near(logp[:6], lp, TOL + F32 * lp.abs())
+    want, bound = gradient(q, there, at, -torch.ones(6, dtype=torch.float64), torch.ones(6, dtype=torch.float64), torch.ones(6, dtype=torch.float64), 1.0)
+    assert near(d[:6], want, bound + HALF_UNIT[dtype] * want.abs() + TINY[dtype])
+    assert near(bz.token_loss_backward(x["logits"], x["index"], stats)[:6], want, bound + HALF_UNIT[dtype] * want.abs() + TINY[dtype])
+
+
+def test_two_threads_with_different_sizes():
+    """Each call's launch is its own: rows of 70 KB of shared memory beside short ones, from two host threads on two streams."""
+    import threading
+    jobs = [make(300, 35001, torch.bfloat16, 1), make(300, 900, torch.bfloat16, 2)]
+    want = [bz.policy(x["logits"], x["index"], x["adv"], dloss=x["dloss"])[3] for x in jobs]
+    torch.cuda.synchronize()
+    failed = []
+
+    def run(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(100):
+                    got = bz.policy(jobs[k]["logits"], jobs[k]["index"], jobs[k]["adv"], dloss=jobs[k]["dloss"])[3]
+                torch.cuda.current_stream().synchronize()
+                failed.append(not torch.equal(got, want[k]))
+        except Exception as e:      # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=run, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert failed == [False, False]

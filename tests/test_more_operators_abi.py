@@ -30,9 +30,10 @@ def test_policy(L):
     n0 = bz.kernel_launch_count()
     for bad in (dict(logits=None), dict(ld=9), dict(dtype=3), dict(m=-1), dict(v=-1), dict(index=None), dict(adv=None), dict(ref=None), dict(T=0.0), dict(T=-1.0),
                 dict(T=INF), dict(T=NAN), dict(T=4.2e-39), dict(lo=-0.1), dict(lo=1.1), dict(lo=NAN), dict(hi=-0.1), dict(hi=NAN), dict(kl=-0.1), dict(kl=INF),
-                dict(kl=NAN), dict(ld_d=9), dict(logits=ODD), dict(d=ODD), dict(stats=EIGHT), dict(loss=None, logp=None, stats=None, d=None)):
+                dict(kl=NAN), dict(ld_d=9), dict(logits=ODD), dict(d=ODD), dict(stats=EIGHT), dict(loss=None, logp=None, stats=None, d=None),
+                dict(index=ODD), dict(old=ODD), dict(ref=ODD), dict(adv=ODD), dict(dloss=ODD), dict(loss=ODD), dict(logp=ODD)):
         assert call(**bad) == bz.ERR_INVALID_ARG, bad
-    for bad in (dict(v=1 << 31, ld=1 << 31, ld_d=1 << 31), dict(m=1 << 31), dict(ld=1 << 31), dict(ld_d=1 << 31)):
+    for bad in (dict(v=1 << 31, ld=1 << 31, ld_d=1 << 31), dict(v=(1 << 31) - 16383, ld=1 << 33, ld_d=1 << 33), dict(m=1 << 31), dict(ld=1 << 31), dict(ld_d=1 << 31)):
         assert call(**bad) == bz.ERR_UNSUPPORTED, bad
     assert call(m=0, index=None, adv=None, ref=None) == bz.OK
     assert bz.kernel_launch_count() == n0
@@ -46,9 +47,9 @@ def test_preference(L):
     n0 = bz.kernel_launch_count()
     for bad in (dict(logits=None), dict(ld=9), dict(dtype=-1), dict(m=-1), dict(v=-1), dict(index=None), dict(starts=None), dict(pairs=-1), dict(T=0.0), dict(T=NAN),
                 dict(beta=NAN), dict(beta=INF), dict(margin=INF), dict(margin=NAN), dict(eps=-0.1), dict(eps=1.1), dict(eps=NAN), dict(stats=None), dict(stats=EIGHT),
-                dict(ld_d=9), dict(d=ODD), dict(logits=ODD)):
+                dict(ld_d=9), dict(d=ODD), dict(logits=ODD), dict(index=ODD), dict(starts=ODD), dict(ref=ODD), dict(dloss=ODD), dict(loss=ODD), dict(reward=ODD), dict(logp=ODD)):
         assert call(**bad) == bz.ERR_INVALID_ARG, bad
-    for bad in (dict(v=1 << 31, ld=1 << 31, ld_d=1 << 31), dict(m=1 << 31), dict(pairs=1 << 30)):
+    for bad in (dict(v=1 << 31, ld=1 << 31, ld_d=1 << 31), dict(v=(1 << 31) - 16383, ld=1 << 33, ld_d=1 << 33), dict(m=1 << 31), dict(pairs=1 << 30)):
         assert call(**bad) == bz.ERR_UNSUPPORTED, bad
     assert call(m=0, pairs=0, starts=None, stats=None) == bz.OK
     assert bz.kernel_launch_count() == n0
@@ -60,7 +61,7 @@ def test_token_loss_backward(L):
 
     n0 = bz.kernel_launch_count()
     for bad in (dict(logits=None), dict(ld=9), dict(dtype=9), dict(m=-1), dict(index=None), dict(T=0.0), dict(stats=None), dict(stats=EIGHT), dict(d=None), dict(ld_d=9),
-                dict(logits=ODD), dict(d=ODD)):
+                dict(logits=ODD), dict(d=ODD), dict(index=ODD), dict(dloss=ODD)):
         assert call(**bad) == bz.ERR_INVALID_ARG, bad
     assert call(m=1 << 31) == bz.ERR_UNSUPPORTED
     assert call(m=0) == bz.OK and call(v=0) == bz.OK
