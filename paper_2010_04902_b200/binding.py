@@ -925,7 +925,7 @@ def _token_operands(logits, index, dloss, dlogits):
     if dlogits is None:
         if dloss is None:
             return m, head, False, None, None, 0
-        dlogits = _like_rows(logits)
+        dlogits = _alike(logits)
         return m, head, True, dlogits, dlogits.data_ptr(), dlogits.stride(0) if m > 1 else v
     return m, head, True, dlogits, *_row_tensor(dlogits, logits.shape, logits.dtype, "dlogits")
 
@@ -933,9 +933,18 @@ def _token_operands(logits, index, dloss, dlogits):
 def _made(t, like, shape, name):
     """(tensor, address) of a binary32 output; a new one if t is None."""
     if t is None:
-        t = like.new_empty(shape, dtype=torch.float32)
+        t = like.new_empty(shape) if like.dtype is torch.float32 else like.new_empty(shape, dtype=torch.float32)
         return t, t.data_ptr()
     return t, _packed(t, shape, torch.float32, name)
+
+
+def _alike(t: torch.Tensor) -> torch.Tensor:
+    """_like_rows() of a matrix, in one step where its rows are apart."""
+    if t.is_contiguous():
+        return torch.empty_like(t)
+    m, n = t.shape
+    ld = t.stride(0)
+    return torch.empty_strided((m, n), (ld, 1), dtype=t.dtype, device=t.device) if m > 1 and n < ld <= 2 * n else t.new_empty((m, n))
 
 
 def policy(logits: torch.Tensor, index: torch.Tensor, advantage: torch.Tensor, old_logp: torch.Tensor | None = None,
@@ -947,11 +956,12 @@ def policy(logits: torch.Tensor, index: torch.Tensor, advantage: torch.Tensor, o
     if logits.requires_grad:
         _unrecorded("policy", logits=logits)
     m, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
-    loss, p_loss = _made(loss, logits, (m,), "loss")
-    logp, p_logp = _made(logp, logits, (m,), "logp")
-    stats, p_stats = _made(stats, logits, (m, 4), "stats")
+    p_advantage = _packed(advantage, (m,), torch.float32, "advantage")
+    loss, p_loss = _made(loss, advantage, (m,), "loss")
+    logp, p_logp = _made(logp, advantage, (m,), "logp")
+    stats, p_stats = _made(stats, advantage, (m, 4), "stats")
     st = lib().bz_policy(*head, _packed(old_logp, (m,), torch.float32, "old_logp"), _packed(ref_logp, (m,), torch.float32, "ref_logp"),
-                         _packed(advantage, (m,), torch.float32, "advantage"), temperature, clip_low, clip_high, kl,
+                         p_advantage, temperature, clip_low, clip_high, kl,
                          _packed(dloss, (m,), torch.float32, "dloss"), p_loss, p_logp, p_stats, p_d, ld_d, _stream())
     if st:
         _check(st, "bz_policy")
@@ -987,7 +997,7 @@ def token_loss_backward(logits: torch.Tensor, index: torch.Tensor, stats: torch.
                         temperature: float = 1.0, dlogits: torch.Tensor | None = None) -> torch.Tensor:
     """bz_token_loss_backward: the gradient alone, with stats as policy() or preference() returned them; dloss as there."""
     if dlogits is None:
-        dlogits = _like_rows(logits)
+        dlogits = _alike(logits)
     m, head, _, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
     if dloss is not None and dloss.dim() != 1:
         raise ValueError("dloss must be [m] or [pairs]")
@@ -1084,10 +1094,10 @@ def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | 
     p_y, ld_y = (None, 0) if y is None else _row_tensor(y, x.shape, x.dtype, "y")
     keep = s is None and y is None and residual_scale == 1.0 and w_pre is not None
     if s is None and not keep:
-        s = _like_rows(x)
+        s = _alike(x)
     p_s, ld_s = (None, 0) if s is None else _row_tensor(s, x.shape, x.dtype, "s")
     if z is None and w_pre is not None:
-        z = _like_rows(x)
+        z = _alike(x)
     p_z, ld_z = (None, 0) if z is None else _row_tensor(z, x.shape, x.dtype, "z")
     stats, p_stats = _made(stats, x, (m, 4), "stats")
     st = lib().bz_join(x.data_ptr(), ld_x, p_y, ld_y, dt, m, n, _norm(norm), eps, p_post, p_gate, groups, residual_scale, branch_scale, rate, p_rng,
@@ -1118,10 +1128,10 @@ def join_backward(x: torch.Tensor, y: torch.Tensor | None, stats: torch.Tensor, 
     p_ds, ld_ds = (None, 0) if ds is None else _row_tensor(ds, *like, "ds")
     p_dz, ld_dz = (None, 0) if dz is None else _row_tensor(dz, *like, "dz")
     if dx is None:
-        dx = _like_rows(x)
+        dx = _alike(x)
     p_dx, ld_dx = _row_tensor(dx, *like, "dx")
     if dy is None and y is not None:
-        dy = _like_rows(y)
+        dy = _alike(y)
     p_dy, ld_dy = (None, 0) if dy is None else _row_tensor(dy, *like, "dy")
     p_dpost = p_dgate = p_dpre = None
     if w_post is not None:
