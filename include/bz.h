@@ -673,7 +673,7 @@ int bz_policy(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, c
  *   starts     device int32 [2 pairs + 1], not decreasing; values are taken into [0, m].  A sequence may be empty.
  *   ref_logp   device binary32 [m], or NULL: no reference (0).
  *   beta finite, smoothing in [0, 1], margin finite.   pairs up to 2^30 - 1; 0 means that no row is of a sequence.
- *   loss       device binary32 [pairs], or NULL;  reward device binary32 [2 pairs], or NULL;  stats must be given.
+ *   loss       device binary32 [pairs], or NULL;  reward device binary32 [2 pairs], or NULL;  stats and logp must be given.
  *   dloss      device binary32 [pairs], or NULL: all 1.
  * A row's slope depends on the whole pair, so the logits are read again for the gradient, the last rows first: what the L2 still
  * holds of them is not read from memory again.

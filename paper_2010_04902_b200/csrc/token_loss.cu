@@ -165,16 +165,20 @@ template <bool POLICY> __device__ __forceinline__ RowScalars row_scalars(const T
     }
     return s;
 }
+// In the place of that rest: a row without a token.
+constexpr float kNoToken = INFINITY;
 // One thread.
 __device__ __forceinline__ void write_row(const TokenArgs& a, int64_t i, const MaxSum& all, const RowScalars& s, bool policy) {
     if (a.logp != nullptr) a.logp[i] = static_cast<float>(s.lp);
     if (policy && a.loss != nullptr) a.loss[i] = s.loss;
-    if (a.stats != nullptr) a.stats[i] = make_float4(all.m, static_cast<float>(s.sum * exp2(-s.rest)), s.slope, __int_as_float(static_cast<int>(i)));
+    // until a pair's slopes are known the last place holds what lp has beyond binary32
+    const float rest = s.lp == -INFINITY ? 0.f : static_cast<float>(s.lp - static_cast<double>(static_cast<float>(s.lp)));
+    if (a.stats != nullptr) a.stats[i] = make_float4(all.m, static_cast<float>(s.sum * exp2(-s.rest)), s.slope, policy ? __int_as_float(static_cast<int>(i)) : rest);
 }
 __device__ __forceinline__ void finish_without(const TokenArgs& a, int64_t i, bool policy) {
     if (a.logp != nullptr) a.logp[i] = 0.f;
     if (policy && a.loss != nullptr) a.loss[i] = 0.f;
-    if (a.stats != nullptr) a.stats[i] = make_float4(-INFINITY, 0.f, 0.f, __int_as_float(static_cast<int>(i)));
+    if (a.stats != nullptr) a.stats[i] = make_float4(-INFINITY, 0.f, 0.f, policy ? __int_as_float(static_cast<int>(i)) : kNoToken);
 }
 
 // ---- a row in a CTA's or a cluster's shared memory -----------------------------------------------
@@ -511,78 +515,67 @@ __global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const 
 
 struct PairArgs {
     const int32_t* starts;
-    int64_t m, v, pairs;
+    int64_t m, pairs;
     float beta, margin, smoothing;
     int mean;
     float *loss, *reward;
 };
 
-// One CTA a pair: the sequences' sums, the loss and each row's slope.
-__global__ void __launch_bounds__(256) pair_kernel(const __grid_constant__ TokenArgs a, const __grid_constant__ PairArgs p, const void* logits, int dtype) {
-    __shared__ double sums[2][8];
-    __shared__ int counts[2][8];
+// One CTA a pair, a half of it each sequence: the sums, the loss and each row's slope.
+constexpr int kPairThreads = 1024, kHalf = kPairThreads / 2;
+__global__ void __launch_bounds__(kPairThreads) pair_kernel(const __grid_constant__ TokenArgs a, const __grid_constant__ PairArgs p) {
+    __shared__ double sums[2][kHalf / 32];
+    __shared__ int counts[2][kHalf / 32];
     const int64_t pair = blockIdx.x;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t from[2], to[2];
-    for (int side = 0; side < 2; ++side) {
-        const int64_t n = pair + side * p.pairs;
-        from[side] = min(max(static_cast<int64_t>(p.starts[n]), int64_t(0)), p.m);
-        to[side] = max(from[side], min(static_cast<int64_t>(p.starts[n + 1]), p.m));
-        double sum = 0.0;
-        int count = 0;
-        for (int64_t i = from[side] + threadIdx.x; i < to[side]; i += blockDim.x) {
-            const int at = a.index[i];
-            if (at < 0 || at >= p.v) continue;
-            const int64_t k = i * a.ld + at;
-            const float logit = dtype == BZ_F32 ? static_cast<const float*>(logits)[k] : dtype == BZ_F16 ? to_f32(static_cast<const __half*>(logits)[k])
-                                                                                                          : to_f32(static_cast<const __nv_bfloat16*>(logits)[k]);
-            const float4 st = a.stats[i];
-            sum += log_probability(a, logit, st.x, 0.0, st.y) - (a.ref_logp != nullptr ? static_cast<double>(a.ref_logp[i]) : 0.0);
-            ++count;
-        }
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), count += __shfl_xor_sync(~0u, count, o);
-        if (lane == 0) sums[side][warp] = sum, counts[side][warp] = count;
+    const int side = threadIdx.x / kHalf, t = threadIdx.x % kHalf, lane = t & 31, warp = t >> 5;
+    const int64_t n = pair + side * p.pairs;
+    const int64_t from = min(max(static_cast<int64_t>(p.starts[n]), int64_t(0)), p.m), to = max(from, min(static_cast<int64_t>(p.starts[n + 1]), p.m));
+    double sum = 0.0;
+    int count = 0;
+#pragma unroll 4
+    for (int64_t i = from + t; i < to; i += kHalf) {
+        const float rest = a.stats[i].w, lp = a.logp[i], ref = a.ref_logp != nullptr ? a.ref_logp[i] : 0.f;
+        if (rest != kNoToken) sum += static_cast<double>(lp) + static_cast<double>(rest) - static_cast<double>(ref), ++count;
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o), count += __shfl_xor_sync(~0u, count, o);
+    if (lane == 0) sums[side][warp] = sum, counts[side][warp] = count;
     __syncthreads();
     double reward[2], share[2];
-    for (int side = 0; side < 2; ++side) {
-        double sum = 0.0;
-        int count = 0;
-        for (int w = 0; w < 8; ++w) sum += sums[side][w], count += counts[side][w];
-        share[side] = static_cast<double>(p.beta) / (p.mean ? max(count, 1) : 1);
-        reward[side] = share[side] * sum;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        sum = 0.0, count = 0;
+#pragma unroll
+        for (int w = 0; w < kHalf / 32; ++w) sum += sums[k][w], count += counts[k][w];
+        share[k] = static_cast<double>(p.beta) / (p.mean ? max(count, 1) : 1);
+        reward[k] = share[k] * sum;
     }
     const double h = reward[0] - reward[1] - static_cast<double>(p.margin), eps = p.smoothing;
-    const double tail = log1p(exp(-fabs(h)));   // -log sigmoid(|h|)
+    const double e = exp(-fabs(h));
+    // d loss / d h = sigmoid(h) - (1 - eps); sigmoid(h) = 1 - sigmoid(-h) for the digits of the smaller one
+    const double small = e / (1.0 + e);
+    const double dh = h >= 0.0 ? eps - small : h < 0.0 ? small - (1.0 - eps) : NAN;
+    const float slope = static_cast<float>(side == 0 ? dh * share[0] : -dh * share[1]);
+    for (int64_t i = from + t; i < to; i += kHalf) {
+        float4* st = a.stats + i;
+        const bool takes = st->w != kNoToken && a.logp[i] != -INFINITY;
+        reinterpret_cast<float2*>(st)[1] = make_float2(takes ? slope : 0.f, __int_as_float(static_cast<int>(pair)));
+    }
     if (threadIdx.x == 0) {
+        const double tail = log1p(e);   // -log sigmoid(|h|)
         // a weight of 0 has no term, whatever its logarithm
         const double up = tail + fmax(-h, 0.0), down = tail + fmax(h, 0.0);
         if (p.loss != nullptr) p.loss[pair] = isnan(h) ? NAN : static_cast<float>((eps != 1.0 ? (1.0 - eps) * up : 0.0) + (eps != 0.0 ? eps * down : 0.0));
         if (p.reward != nullptr) p.reward[pair] = static_cast<float>(reward[0]), p.reward[pair + p.pairs] = static_cast<float>(reward[1]);
     }
-    // d loss / d h = sigmoid(h) - (1 - eps); sigmoid(h) = 1 - sigmoid(-h) for the digits of the smaller one
-    const double small = exp(-fabs(h)) / (1.0 + exp(-fabs(h)));
-    const double dh = h >= 0.0 ? eps - small : h < 0.0 ? small - (1.0 - eps) : NAN;
-    for (int side = 0; side < 2; ++side) {
-        const float slope = static_cast<float>(side == 0 ? dh * share[0] : -dh * share[1]);
-        for (int64_t i = from[side] + threadIdx.x; i < to[side]; i += blockDim.x) {
-            const int at = a.index[i];
-            float4 st = a.stats[i];
-            const float logit = at < 0 || at >= p.v ? -INFINITY : dtype == BZ_F32 ? static_cast<const float*>(logits)[i * a.ld + at]
-                                : dtype == BZ_F16 ? to_f32(static_cast<const __half*>(logits)[i * a.ld + at]) : to_f32(static_cast<const __nv_bfloat16*>(logits)[i * a.ld + at]);
-            st.z = logit == -INFINITY ? 0.f : slope;
-            st.w = __int_as_float(static_cast<int>(pair));
-            a.stats[i] = st;
-        }
-    }
 }
 
 // v == 0: rows without a token.
-__global__ void token_empty_kernel(int64_t m, float* loss, float* logp, float4* stats) {
+__global__ void token_empty_kernel(int64_t m, float* loss, float* logp, float4* stats, bool policy) {
     for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < m; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
         if (loss != nullptr) loss[i] = 0.f;
         if (logp != nullptr) logp[i] = 0.f;
-        if (stats != nullptr) stats[i] = make_float4(-INFINITY, 0.f, 0.f, __int_as_float(static_cast<int>(i)));
+        if (stats != nullptr) stats[i] = make_float4(-INFINITY, 0.f, 0.f, policy ? __int_as_float(static_cast<int>(i)) : kNoToken);
     }
 }
 
@@ -719,7 +712,7 @@ extern "C" int bz_policy(const void* logits, int64_t ld, int dtype, int64_t m, i
     TokenArgs a = token_args(logits, dtype, m, ld, v, ld_d, index, temperature, dloss, logp, stats);
     a.old_logp = old_logp, a.ref_logp = ref_logp, a.advantage = advantage, a.clip_low = clip_low, a.clip_high = clip_high, a.kl = kl, a.loss = loss;
     if (v == 0) {
-        token_empty_kernel<<<kNumSMs, 256, 0, s>>>(m, loss, logp, a.stats);
+        token_empty_kernel<<<kNumSMs, 256, 0, s>>>(m, loss, logp, a.stats, true);
         note_launch();
         return check_launch();
     }
@@ -733,12 +726,12 @@ extern "C" int bz_preference(const void* logits, int64_t ld, int dtype, int64_t 
     if (pairs >= (int64_t(1) << 30)) return BZ_ERR_UNSUPPORTED;
     int st = check(logits, ld, dtype, m, v, index, temperature, stats, dlogits, ld_d);
     if (st != BZ_OK) return st;
-    if ((pairs > 0 && starts == nullptr) || (m > 0 && stats == nullptr)) return BZ_ERR_INVALID_ARG;
+    if ((pairs > 0 && starts == nullptr) || (m > 0 && (stats == nullptr || logp == nullptr))) return BZ_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TokenArgs a = token_args(logits, dtype, m, ld, v, ld_d, index, temperature, dloss, logp, stats);
     a.ref_logp = ref_logp;
     if (m > 0 && v == 0) {
-        token_empty_kernel<<<kNumSMs, 256, 0, s>>>(m, nullptr, logp, a.stats);
+        token_empty_kernel<<<kNumSMs, 256, 0, s>>>(m, nullptr, logp, a.stats, false);
         note_launch();
         st = check_launch();
     } else if (m > 0) {
@@ -746,8 +739,8 @@ extern "C" int bz_preference(const void* logits, int64_t ld, int dtype, int64_t 
     }
     if (st != BZ_OK) return st;
     if (pairs > 0) {
-        const PairArgs p{starts, m, v, pairs, beta, margin, smoothing, mean, loss, reward};
-        pair_kernel<<<static_cast<unsigned>(pairs), 256, 0, s>>>(a, p, logits, dtype);
+        const PairArgs p{starts, m, pairs, beta, margin, smoothing, mean, loss, reward};
+        pair_kernel<<<static_cast<unsigned>(pairs), kPairThreads, 0, s>>>(a, p);
         note_launch();
         st = check_launch();
         if (st != BZ_OK) return st;

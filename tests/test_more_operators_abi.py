@@ -46,7 +46,7 @@ def test_preference(L):
 
     n0 = bz.kernel_launch_count()
     for bad in (dict(logits=None), dict(ld=9), dict(dtype=-1), dict(m=-1), dict(v=-1), dict(index=None), dict(starts=None), dict(pairs=-1), dict(T=0.0), dict(T=NAN),
-                dict(beta=NAN), dict(beta=INF), dict(margin=INF), dict(margin=NAN), dict(eps=-0.1), dict(eps=1.1), dict(eps=NAN), dict(stats=None), dict(stats=EIGHT),
+                dict(beta=NAN), dict(beta=INF), dict(margin=INF), dict(margin=NAN), dict(eps=-0.1), dict(eps=1.1), dict(eps=NAN), dict(stats=None), dict(logp=None), dict(stats=EIGHT),
                 dict(ld_d=9), dict(d=ODD), dict(logits=ODD), dict(index=ODD), dict(starts=ODD), dict(ref=ODD), dict(dloss=ODD), dict(loss=ODD), dict(reward=ODD), dict(logp=ODD)):
         assert call(**bad) == bz.ERR_INVALID_ARG, bad
     for bad in (dict(v=1 << 31, ld=1 << 31, ld_d=1 << 31), dict(v=(1 << 31) - 16383, ld=1 << 33, ld_d=1 << 33), dict(m=1 << 31), dict(pairs=1 << 30)):
