@@ -469,17 +469,18 @@ template <typename T, int VEC, bool POLICY> __global__ void __launch_bounds__(kT
 
 // CTA (row, share): shares of kGradientColumns elements a thread; the last rows first, as far as the L2 still holds them.
 constexpr int kGradientThreads = 256, kGradientColumns = 32;
-template <typename T, int VEC>
+template <typename T, int VEC, int THREADS>
 __global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const __grid_constant__ TokenArgs a, const T* logits, T* dlogits, int shares) {
     constexpr int kSlots = kGradientColumns / VEC;
+    const int threads = THREADS ? THREADS : blockDim.x;
     const unsigned k = gridDim.x - 1 - blockIdx.x, r = shares == 1 ? k : k / static_cast<unsigned>(shares);
     const int64_t i = r;
     const T* row = logits + i * a.ld;
     T* out = dlogits + i * a.ld_d;
     const int n = static_cast<int>(a.v);
     // places of this thread's first elements: below 2^31, as v and a share more are
-    const int base = static_cast<int>((k - r * shares) * (blockDim.x * kGradientColumns)) + static_cast<int>(threadIdx.x) * VEC - row_lead<T, VEC>(row);
-    auto first = [&](int q) { return base + q * static_cast<int>(blockDim.x) * VEC; };
+    const int base = static_cast<int>((k - r * shares) * (threads * kGradientColumns)) + static_cast<int>(threadIdx.x) * VEC - row_lead<T, VEC>(row);
+    auto first = [&](int q) { return base + q * threads * VEC; };
     Raw<T, VEC> raw[kSlots];
     const bool safe = a.extent.around(row, a.v);
     auto whole = [&](int j0) { return j0 < n && (safe || (j0 >= 0 && j0 + VEC <= n)); };
@@ -648,7 +649,8 @@ template <typename T, int VEC> int launch(const TokenArgs& a, const T* logits, T
     const int threads = static_cast<int>(each < kGradientThreads ? (each + 31) / 32 * 32 : kGradientThreads);
     const int64_t shares = (each + threads - 1) / threads;
     if (a.m * shares >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
-    token_gradient_kernel<T, VEC><<<static_cast<unsigned>(a.m * shares), threads, 0, s>>>(a, logits, dlogits, static_cast<int>(shares));
+    auto kern = threads == kGradientThreads ? token_gradient_kernel<T, VEC, kGradientThreads> : token_gradient_kernel<T, VEC, 0>;
+    kern<<<static_cast<unsigned>(a.m * shares), threads, 0, s>>>(a, logits, dlogits, static_cast<int>(shares));
     note_launch();
     return check_launch();
 }
