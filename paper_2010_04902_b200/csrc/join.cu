@@ -13,6 +13,12 @@
 // registers) needs no exchange.  A CTA of up to 512 threads holds a row, a cluster of two or four a wider one; the row's
 // sums cost one barrier each.  The next row's words come by cp.async while a row is worked on: a thread copies what it reads
 // itself, and waits for nobody.
+//
+// 8192 x 4096 bfloat16 with both norms, a gate and dropout: forward 70 us (42 at the copy's rate; 49 with the second norm alone), backward
+// 114 (62; 82).  Bound by instructions and their latencies: 40 and 57 an element (the generator 8 of them each time), issue slots 55 and
+// 51 % with 16 warps an SM, which wait for two sums a row.  Sixteen columns a thread carry the bookkeeping of a row better
+// than eight (backward 156 us); what takes part in a call known beforehand made the forward call 2 % faster and the backward call
+// 4 % slower (registers spilled).
 #include <cooperative_groups.h>
 
 #include <cmath>

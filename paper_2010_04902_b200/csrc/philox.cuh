@@ -51,8 +51,9 @@ struct Keep {
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[2 * i] = lower(u[i]) ? x[2 * i] * scale : 0.f;
-            x[2 * i + 1] = upper(u[i]) ? x[2 * i + 1] * scale : 0.f;
+            const float2 y = __fmul2_rn(make_float2(x[2 * i], x[2 * i + 1]), make_float2(scale, scale));
+            x[2 * i] = lower(u[i]) ? y.x : 0.f;
+            x[2 * i + 1] = upper(u[i]) ? y.y : 0.f;
         }
     }
     // bit i, i < N <= 8: element first + i stays
