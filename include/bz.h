@@ -675,6 +675,7 @@ int bz_policy(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, c
  *   beta finite, smoothing in [0, 1], margin finite.   pairs up to 2^30 - 1; 0 means that no row is of a sequence.
  *   loss       device binary32 [pairs], or NULL;  reward device binary32 [2 pairs], or NULL;  stats and logp must be given.
  *   dloss      device binary32 [pairs], or NULL: all 1.
+ * An lp below binary32's range counts as -inf here, as it is stored.
  * A row's slope depends on the whole pair, so the logits are read again for the gradient, the last rows first: what the L2 still
  * holds of them is not read from memory again.
  */
@@ -743,7 +744,7 @@ int bz_join(const void* x, int64_t ld_x, const void* y, int64_t ld_y, int dtype,
  *   u = branch_scale * drop'(g),  dgate = sum over a group's rows of u * a,   dy = the norm's gradient of u * gate * w_post at y,
  *   dw_post = sum over rows of u * gate * norm(y),   dw_pre = sum over rows of dz * norm(s).
  *   dx, dy  device [m][n] with ld_dx, ld_dy, or NULL.  Each may be x, y, ds or dz itself (equal leading dimensions).
- *   dw_post, dgate, dw_pre  device binary32 [n], [groups][n], [n], overwritten, or NULL.
+ *   dw_post, dgate, dw_pre  device binary32 [n], [groups][n], [n], overwritten, or NULL; apart from the weights and the gate.
  *   workspace  device, bz_join_workspace_bytes(m, n, groups) bytes, 256-byte aligned (needed with dw_post, dgate or dw_pre only).
  * m == 0 writes dw_post = dw_pre = 0 (dgate has no rows then, or one: 0).
  */

@@ -169,10 +169,10 @@ template <bool POLICY> __device__ __forceinline__ RowScalars row_scalars(const T
 constexpr float kNoToken = INFINITY;
 // One thread.
 __device__ __forceinline__ void write_row(const TokenArgs& a, int64_t i, const MaxSum& all, const RowScalars& s, bool policy) {
-    if (a.logp != nullptr) a.logp[i] = static_cast<float>(s.lp);
     if (policy && a.loss != nullptr) a.loss[i] = s.loss;
     // until a pair's slopes are known the last place holds what lp has beyond binary32
-    const float rest = s.lp == -INFINITY ? 0.f : static_cast<float>(s.lp - static_cast<double>(static_cast<float>(s.lp)));
+    const float lp = static_cast<float>(s.lp), rest = isfinite(lp) ? static_cast<float>(s.lp - static_cast<double>(lp)) : 0.f;
+    if (a.logp != nullptr) a.logp[i] = lp;
     if (a.stats != nullptr) a.stats[i] = make_float4(all.m, static_cast<float>(s.sum * exp2(-s.rest)), s.slope, policy ? __int_as_float(static_cast<int>(i)) : rest);
 }
 __device__ __forceinline__ void finish_without(const TokenArgs& a, int64_t i, bool policy) {

@@ -259,6 +259,30 @@ def test_preference_far_apart():
     check_preference(x, [0, 10, 20, 30, 40], beta=-20.0, smoothing=0.2)
 
 
+@pytest.mark.parametrize("low, peak", [(-math.inf, 0.0), (torch.finfo(torch.float32).min, 0.0), (torch.finfo(torch.float32).min, 1e38)])
+def test_preference_with_tokens_of_no_probability(low, peak):
+    """A chosen token whose logit is -inf, or whose logarithm is as low as binary32 goes or, counted as -inf, lower: reward and loss are the
+    formula's rounded to binary32 (half the lowest value where the logarithm still is one), the other rows' slopes those of a lost pair, and
+    the token takes a gradient where its logarithm is finite."""
+    x = make(8, 40, torch.float32, 2)
+    x["index"] = torch.arange(8, dtype=torch.int32, device="cuda")
+    x["logits"][1, 1] = low
+    x["logits"][1, 2] += peak
+    loss, reward, logp, _, d = bz.preference(x["logits"], x["index"], torch.tensor([0, 4, 8], dtype=torch.int32, device="cuda"), ref_logp=x["ref"], beta=0.5,
+                                             dloss=torch.ones(1, device="cuda"))
+    lp = torch.log_softmax(x["logits"].double(), 1)[torch.arange(8), torch.arange(8)]
+    lp[1] = float(lp[1].float())
+    assert float(logp[1]) == float(lp[1])
+    chosen, rejected = (0.5 * (lp - x["ref"].double())).view(2, 4).sum(1)
+    assert float(reward[0]) == float(chosen.float()) and torch.isfinite(reward[1]) and float(loss) == float((rejected - chosen).float())
+    p = torch.softmax(x["logits"].double(), 1)
+    want = -0.5 * (torch.eye(8, 40, dtype=torch.float64, device="cuda") - p)
+    want[4:] *= -1
+    if float(lp[1]) == -math.inf:
+        want[1] = 0
+    assert (d.double() - want).abs().max() < 1e-6
+
+
 def test_preference_many_pairs():
     m, pairs = 4000, 1000
     x = make(m, 50, torch.bfloat16, 3)
