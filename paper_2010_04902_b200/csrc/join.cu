@@ -194,7 +194,7 @@ template <typename T, int COLS, int NT, int THREADS> struct Held<T, COLS, NT, TH
         }
         return make_uint4(u[0], u[1], u[2], u[3]);
     }
-    // `fetched`: the next row's fetches have been made, and its half is the other one
+    // after the next row's commit: this row's half is the one that the commit after it will fill
     __device__ __forceinline__ void get(int t, float2 (&v)[COLS / 2], const Columns<N, THREADS>& at) const {
         const uint4* from = room + (half * NT + t) * words();
 #pragma unroll
@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(THREADS ? THREADS : 128, 512 / (THREADS ? THRE
         for (; i < end; ++i) {
             const float4 st = a.stats != nullptr ? a.stats[i] : make_float4(0.f, 1.f, 0.f, 1.f);
             if (SHIFT) in.arrived();
-        if (i + 1 < last) fetch(i + 1);
+            if (i + 1 < last) fetch(i + 1);
             in.commit();
             if (!SHIFT) in.arrived();
             uint32_t r[COLS / 2];
