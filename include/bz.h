@@ -685,9 +685,10 @@ int bz_preference(const void* logits, int64_t ld, int dtype, int64_t m, int64_t 
                   void* stream);
 
 /* The gradient alone of either loss, with stats as bz_policy or bz_preference left them, for a dloss that is known only after
- * the loss: [m] for the first, [pairs] for the second, or NULL: all 1.  dlogits may be logits itself. */
+ * the loss: [places], m for the first, pairs for the second, or NULL: all 1 (places is not looked at then).  A row with a slope
+ * whose place in dloss (both of its stats) is not below places gets a gradient of NaN.  dlogits may be logits itself. */
 int bz_token_loss_backward(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const int32_t* index, float temperature,
-                           const float* stats, const float* dloss, void* dlogits, int64_t ld_d, void* stream);
+                           const float* stats, const float* dloss, int64_t places, void* dlogits, int64_t ld_d, void* stream);
 
 /*
  * ---- Dropout -------------------------------------------------------------------------------------

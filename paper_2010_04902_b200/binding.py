@@ -103,7 +103,7 @@ _SIGNATURES = {
                            _c_vp, _c_i64, _c_vp]),
     "bz_preference": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_vp, _c_vp, _c_i64, _c_f, _c_f, _c_f, _c_f, _c_int, _c_vp, _c_vp,
                                _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]),
-    "bz_token_loss_backward": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_f, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]),
+    "bz_token_loss_backward": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_vp, _c_f, _c_vp, _c_vp, _c_i64, _c_vp, _c_i64, _c_vp]),
     "bz_dropout": (_c_int, [_c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_d, _c_vp, _c_vp, _c_i64, _c_vp]),
     "bz_join": (_c_int, [_c_vp, _c_i64, _c_vp, _c_i64, _c_int, _c_i64, _c_i64, _c_int, _c_f, _c_vp, _c_vp, _c_i64, _c_f, _c_f, _c_d, _c_vp, _c_vp,
                          _c_vp, _c_i64, _c_vp, _c_i64, _c_vp, _c_vp]),
@@ -995,14 +995,19 @@ def preference(logits: torch.Tensor, index: torch.Tensor, starts: torch.Tensor, 
 
 def token_loss_backward(logits: torch.Tensor, index: torch.Tensor, stats: torch.Tensor, dloss: torch.Tensor | None = None,
                         temperature: float = 1.0, dlogits: torch.Tensor | None = None) -> torch.Tensor:
-    """bz_token_loss_backward: the gradient alone, with stats as policy() or preference() returned them; dloss as there."""
+    """bz_token_loss_backward: the gradient alone, with stats as policy() or preference() returned them; dloss as there (rows whose
+    loss it does not hold get NaN)."""
     if dlogits is None:
         dlogits = _alike(logits)
     m, head, _, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
     if dloss is not None and dloss.dim() != 1:
         raise ValueError("dloss must be [m] or [pairs]")
-    st = lib().bz_token_loss_backward(*head, temperature, _packed(stats, (m, 4), torch.float32, "stats"),
-                                      None if dloss is None else _packed(dloss, dloss.shape, torch.float32, "dloss"), p_d, ld_d, _stream())
+    p_stats = _packed(stats, (m, 4), torch.float32, "stats")
+    p_dloss, places = None, 0
+    if dloss is not None:
+        # a tensor without elements has no address, which would stand for ones
+        p_dloss, places = _packed(dloss, dloss.shape, torch.float32, "dloss") or p_stats, dloss.shape[0]
+    st = lib().bz_token_loss_backward(*head, temperature, p_stats, p_dloss, places, p_d, ld_d, _stream())
     if st:
         _check(st, "bz_token_loss_backward")
     return dlogits

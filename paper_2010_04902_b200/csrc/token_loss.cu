@@ -28,6 +28,7 @@ struct TokenArgs {
     const float *old_logp, *ref_logp, *advantage;
     float clip_low, clip_high, kl;
     const float* dloss;
+    uint32_t places;          // of dloss, for the gradient alone
     float *loss, *logp;
     float4* stats;            // largest logit, sum of e^((s - that)/T), slope, place in dloss
 };
@@ -469,6 +470,12 @@ template <typename T, int VEC, bool POLICY> __global__ void __launch_bounds__(kT
 
 // ---- the gradient from given stats ---------------------------------------------------------------
 
+// What comes from above for a row whose place in dloss is `place`.
+__device__ __forceinline__ float upstream(const TokenArgs& a, float place) {
+    const uint32_t k = __float_as_uint(place);
+    return a.dloss == nullptr ? 1.f : k < a.places ? a.dloss[k] : NAN;
+}
+
 // CTA (row, share): shares of kGradientColumns elements a thread; the last rows first, as far as the L2 still holds them.  4096 x 32128
 // bfloat16: 85 us, 96 % of the copy's rate.  (Stores that leave the L2 first, to keep more of the logits there: 95 us.)
 constexpr int kGradientThreads = 256, kGradientColumns = 32;
@@ -491,7 +498,7 @@ __global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const 
     for (int q = 0; q < kSlots; ++q) raw[q].fetch(row + first(q), whole(first(q)));
     const float4 st = a.stats[i];
     const int at = a.index[i];
-    const float g = st.z == 0.f || !has_token(a, at) ? 0.f : st.z * (a.dloss != nullptr ? a.dloss[__float_as_int(st.w)] : 1.f) / a.temperature;
+    const float g = st.z == 0.f || !has_token(a, at) ? 0.f : st.z * upstream(a, st.w) / a.temperature;
     const Base reference(a, st.x);
     const float f = g == 0.f ? 0.f : -g / st.y * exp2_fast(-reference.rest(a));
 #pragma unroll
@@ -735,7 +742,7 @@ extern "C" int bz_preference(const void* logits, int64_t ld, int dtype, int64_t 
     if ((pairs > 0 && starts == nullptr) || (m > 0 && (stats == nullptr || logp == nullptr))) return BZ_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     TokenArgs a = token_args(logits, dtype, m, ld, v, ld_d, index, temperature, dloss, logp, stats);
-    a.ref_logp = ref_logp;
+    a.ref_logp = ref_logp, a.places = static_cast<uint32_t>(pairs);
     if (m > 0 && v == 0) {
         token_empty_kernel<<<kNumSMs, 256, 0, s>>>(m, nullptr, logp, a.stats, false);
         note_launch();
@@ -755,11 +762,12 @@ extern "C" int bz_preference(const void* logits, int64_t ld, int dtype, int64_t 
 }
 
 extern "C" int bz_token_loss_backward(const void* logits, int64_t ld, int dtype, int64_t m, int64_t v, const int32_t* index, float temperature,
-                                      const float* stats, const float* dloss, void* dlogits, int64_t ld_d, void* stream) {
-    if (!on_boundary(index, dloss)) return BZ_ERR_INVALID_ARG;
+                                      const float* stats, const float* dloss, int64_t places, void* dlogits, int64_t ld_d, void* stream) {
+    if (!on_boundary(index, dloss) || (dloss != nullptr && places < 0)) return BZ_ERR_INVALID_ARG;
     const int st = check(logits, ld, dtype, m, v, index, temperature, stats, dlogits, ld_d);
     if (st != BZ_OK || m == 0 || v == 0) return st;
     if (stats == nullptr || dlogits == nullptr) return BZ_ERR_INVALID_ARG;
-    return dispatch(token_args(logits, dtype, m, ld, v, ld_d, index, temperature, dloss, nullptr, const_cast<float*>(stats)), dtype, m, logits, dlogits, kGradient,
-                    static_cast<cudaStream_t>(stream));
+    TokenArgs a = token_args(logits, dtype, m, ld, v, ld_d, index, temperature, dloss, nullptr, const_cast<float*>(stats));
+    a.places = static_cast<uint32_t>(places < (int64_t(1) << 31) ? places : int64_t(1) << 31);
+    return dispatch(a, dtype, m, logits, dlogits, kGradient, static_cast<cudaStream_t>(stream));
 }

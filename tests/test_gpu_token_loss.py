@@ -283,6 +283,24 @@ def test_preference_with_tokens_of_no_probability(low, peak):
     assert (d.double() - want).abs().max() < 1e-6
 
 
+def test_gradient_of_losses_that_dloss_does_not_hold():
+    """Stats of one loss with an upstream gradient of another length: rows whose place it has not get NaN, rows without a slope 0."""
+    for dtype in DTYPES:
+        x = make(12, 70, dtype, 3)
+        x["index"] = torch.arange(12, dtype=torch.int32, device="cuda")
+        x["index"][[2, 9]] = -1
+        _, _, stats, want = bz.policy(x["logits"], x["index"], x["adv"], clip_low=1.0, clip_high=math.inf, dloss=x["dloss"])
+        got = bz.token_loss_backward(x["logits"], x["index"], stats, x["dloss"][:5].clone())
+        want, size = want[:5].cpu().double(), (x["adv"] * x["dloss"])[:5, None].cpu().double().abs()
+        # two computations of slope times (indicator less softmax), each within 3 TOL of its terms, and their roundings
+        assert near(got[:5], want, 2 * (3 * TOL * 2 * size + HALF_UNIT[dtype] * (want.abs() + 6 * TOL * size) + TINY[dtype]))
+        assert got[9].eq(0).all() and got[[5, 6, 7, 8, 10, 11]].isnan().all()
+        assert bz.token_loss_backward(x["logits"], x["index"], stats, x["dloss"][:0].clone())[[0, 11]].isnan().all()
+        stats = bz.preference(x["logits"], x["index"], torch.tensor([0, 3, 6, 9, 12], dtype=torch.int32, device="cuda"), dloss=x["dloss"][:2].clone())[3]
+        got = bz.token_loss_backward(x["logits"], x["index"], stats, x["dloss"][:1].clone())
+        assert got[[2, 9]].eq(0).all() and got[[3, 4, 5, 10, 11]].isnan().all() and got[[0, 1, 6, 7, 8]].isfinite().all()
+
+
 def test_preference_many_pairs():
     m, pairs = 4000, 1000
     x = make(m, 50, torch.bfloat16, 3)

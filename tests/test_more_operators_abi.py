@@ -56,12 +56,12 @@ def test_preference(L):
 
 
 def test_token_loss_backward(L):
-    def call(logits=F, ld=10, dtype=bz.F32, m=4, v=10, index=F, T=1.0, stats=F, dloss=None, d=F, ld_d=10):
-        return L.bz_token_loss_backward(logits, ld, dtype, m, v, index, T, stats, dloss, d, ld_d, None)
+    def call(logits=F, ld=10, dtype=bz.F32, m=4, v=10, index=F, T=1.0, stats=F, dloss=None, places=0, d=F, ld_d=10):
+        return L.bz_token_loss_backward(logits, ld, dtype, m, v, index, T, stats, dloss, places, d, ld_d, None)
 
     n0 = bz.kernel_launch_count()
     for bad in (dict(logits=None), dict(ld=9), dict(dtype=9), dict(m=-1), dict(index=None), dict(T=0.0), dict(stats=None), dict(stats=EIGHT), dict(d=None), dict(ld_d=9),
-                dict(logits=ODD), dict(d=ODD), dict(index=ODD), dict(dloss=ODD)):
+                dict(logits=ODD), dict(d=ODD), dict(index=ODD), dict(dloss=ODD), dict(dloss=F, places=-1)):
         assert call(**bad) == bz.ERR_INVALID_ARG, bad
     assert call(m=1 << 31) == bz.ERR_UNSUPPORTED
     assert call(m=0) == bz.OK and call(v=0) == bz.OK
