@@ -202,7 +202,7 @@ template <int LEFT> __device__ __forceinline__ void wait_copies() { asm volatile
 __device__ __forceinline__ void copy_word(uint32_t to, const char* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
 
 struct RowShare {
-    int ranks, words, batches;   // CTAs of a row; words of a CTA at most; batches of a thread
+    int ranks, words;   // CTAs of a row; words of a CTA at most
 };
 
 // THREADS: of the CTA, or 0 for whatever it is launched with (the distances of a thread's words are constants in the long rows).
@@ -224,14 +224,14 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
     const int all = (lead + n + N - 1) / N, begin = rank * share.words, count = min(share.words, all - begin);
     // words over an end of the row: places in the CTA, -1: elsewhere
     const int head = lead != 0 && begin == 0 ? 0 : -1, tail = (lead + n) % N != 0 && begin + count == all ? count - 1 : -1;
-    // batches without any of these, and without words behind the last
-    const int stride = threads * 16, plain_from = head >= 0, plain_to = (count - (tail >= 0)) / (kBatch * threads);
+    // batches, and those without any of these and without words behind the last
+    const int batches = (count + kBatch * threads - 1) / (kBatch * threads), stride = threads * 16, plain_from = head >= 0, plain_to = (count - (tail >= 0)) / (kBatch * threads);
     const bool there = has_token(a, at);
     float g = 0.f, f = 0.f, top = 0.f;
     if (there) {
         const char* from = reinterpret_cast<const char*>(row - lead) + (begin + t) * int64_t(16);
         uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(held + t));
-        for (int b = 0, w = t; b < share.batches; ++b, w += kBatch * threads, from += kBatch * stride, to += kBatch * stride) {
+        for (int b = 0, w = t; b < batches; ++b, w += kBatch * threads, from += kBatch * stride, to += kBatch * stride) {
             if (b >= plain_from && b < plain_to) {
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) copy_word(to + j * stride, from + j * stride);
@@ -241,12 +241,12 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
                 for (int j = 0; j < kBatch; ++j)
                     if (const int v = w + j * threads; v < count && v != head && v != tail) copy_word(to + j * stride, from + j * stride);
             }
-            if (b < 3 || b + 1 == share.batches) asm volatile("cp.async.commit_group;" ::: "memory");
+            if (b < 3 || b + 1 == batches) asm volatile("cp.async.commit_group;" ::: "memory");
         }
         RowInputs in{};
         if (warp == 0) in = row_inputs<POLICY>(a, i, to_f32(row[at]));
         // -inf in what was not copied: words behind the CTA's last, elements that are not the row's
-        for (int b = 0; b < share.batches; ++b) {
+        for (int b = 0; b < batches; ++b) {
             if (b >= plain_from && b < plain_to) continue;
             for (int w = b * kBatch * threads + t, j = 0; j < kBatch; ++j, w += threads) {
                 if (w < count && w != head && w != tail) continue;
@@ -260,9 +260,9 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
         MaxSum sum{-INFINITY, 0.f};
         const char* word = reinterpret_cast<const char*>(held + t);
 #pragma unroll 1
-        for (int b = 0; b < share.batches; ++b) {
+        for (int b = 0; b < batches; ++b) {
             // groups: a batch each, the fourth all that are left
-            switch (min(share.batches, 4) - 1 - b) {
+            switch (min(batches, 4) - 1 - b) {
                 case 3: wait_copies<3>(); break;
                 case 2: wait_copies<2>(); break;
                 case 1: wait_copies<1>(); break;
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
             if (w != head && w != tail) *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
     } else {
 #pragma unroll 1
-        for (int b = 0, w = t; b < share.batches; ++b, w += kBatch * threads, word += kBatch * stride, to += kBatch * stride) {
+        for (int b = 0, w = t; b < batches; ++b, w += kBatch * threads, word += kBatch * stride, to += kBatch * stride) {
             float x[kBatch][N];
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) Word<T>::unpack(*reinterpret_cast<const uint4*>(word + j * stride), x[j]);
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
 // ---- the loss alone, many rows: one CTA a row, words from memory into registers ------------------
 //
 // Nothing of the row has to stay, so a row of any length takes one CTA and three of them an SM; a thread has its next four words on their
-// way while it takes four in.  1531 x 65537 binary16: 47 us (31 at the copy's rate), 66 through shared memory and clusters; rows of 64 KB and
+// way while it takes four in.  1531 x 65537 binary16: 47 us (31 at the copy's rate), 60 through shared memory and clusters; rows of 64 KB and
 // less are as fast there (57 us at 4096 x 32128) or faster (8192 x 8000: 33 against 57).
 
 constexpr int kScoreThreads = 256;
@@ -595,16 +595,36 @@ __global__ void token_empty_kernel(int64_t m, float* loss, float* logp, float4* 
 
 enum What { kPolicy, kScore, kGradient };
 
+// Threads for a CTA's words: a warp up to 640, 128 threads up to 2048, else 256; where few rows leave SMs idle, four words each.  (Policy
+// loss with its gradient, bfloat16: 8192 rows of 2000 with a warp 22.6 us, with two 26.9; of 4096 42, 49; 8192 x 8000 with 128 threads 57, with two
+// warps 66, with 256 threads 80.)
+int threads_for(int words, bool few) {
+    const int quarter = (words + 127) / 128 * 32;
+    if (few) return quarter < kShared ? quarter : kShared;
+    return words <= 640 ? 32 : words <= 2048 ? 128 : 256;
+}
+// Words that they take in, those behind the last ones among them.
+int in_batches(int words, int threads) { return (words + threads * kBatch - 1) / (threads * kBatch) * (threads * kBatch); }
+// CTAs of a long row, parts of 1024 to 2048 words where it has them: what leaves the fewest words behind the last ones, and the more CTAs
+// of two like that.  2048 x 50257 bfloat16 in 5 parts of 1257 words 106 us, in 4 of 1571 (2048 with the empty ones) 115, in 7 of 898 113.
+int ranks_for(int64_t words) {
+    const int64_t most = words <= 2048 * kMostRanks ? 2048 : 4096;
+    int best = kMostRanks;
+    int64_t least = INT64_MAX;
+    for (int r = 2; r <= kMostRanks; ++r) {
+        const int64_t part = (words + r - 1) / r;
+        if (part < 1024 || part > most) continue;
+        const int64_t all = static_cast<int64_t>(r) * in_batches(static_cast<int>(part), threads_for(static_cast<int>(part), false));
+        if (all <= least) least = all, best = r;
+    }
+    return best;
+}
+
 template <typename T, bool POLICY, bool GRADIENT> int shared(const TokenArgs& a, const T* logits, T* dlogits, int64_t words, int ranks, cudaStream_t s) {
-    RowShare share{ranks, static_cast<int>((words + ranks - 1) / ranks), 0};
-    // up to sixteen words a thread; where few rows leave SMs idle, four
-    const int each = a.m * ranks <= kNumSMs ? 4 : 16;
-    int threads = (share.words + each * 32 - 1) / (each * 32) * 32;
-    if (each == 16 && share.words > 640) threads = share.words > 2048 ? 256 : 128;
-    if (threads > kShared) threads = kShared;
-    share.batches = (share.words + threads * kBatch - 1) / (threads * kBatch);
+    const RowShare share{ranks, static_cast<int>((words + ranks - 1) / ranks)};
+    const int threads = threads_for(share.words, a.m * ranks <= kNumSMs);
     auto kern = threads == 256 ? token_shared_kernel<T, POLICY, GRADIENT, 256> : threads == 128 ? token_shared_kernel<T, POLICY, GRADIENT, 128> : token_shared_kernel<T, POLICY, GRADIENT, 0>;
-    const int smem = share.batches * kBatch * threads * 16;
+    const int smem = in_batches(share.words, threads) * 16;
     cudaError_t e = cudaSuccess;
     // up to 48 KB need no leave; beyond, the limit belongs to the kernel and not to the call: the same one each time
     if (smem > 48 * 1024 - 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostWords * 16);
@@ -632,9 +652,8 @@ template <typename T, int VEC, bool POLICY> int rows(const TokenArgs& a, const T
     if constexpr (VEC > 1) {
         const int64_t words = (a.v + 2 * (VEC - 1)) / VEC;   // of a row, at most
         const bool score = dlogits == nullptr && a.m >= kScoreRows && words > kScoreWords;
-        // three CTAs an SM; a cluster's CTAs hold what they can of the longest rows
-        int64_t ranks = words <= 4096 ? 1 : (words + 2047) / 2048;
-        if (ranks > kMostRanks) ranks = kMostRanks;
+        // a cluster's CTAs hold what they can of the longest rows
+        int64_t ranks = words <= 4096 ? 1 : ranks_for(words);
         while (ranks < kMostRanks && a.m * ranks * 2 <= kNumSMs && words > ranks * 256) ranks *= 2;   // few rows: on more SMs
         if (ranks > kMostRanks) ranks = kMostRanks;
         if ((words + ranks - 1) / ranks + kBatch * kShared <= kMostWords && a.m * ranks < (int64_t(1) << 31)) {

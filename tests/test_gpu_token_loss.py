@@ -283,6 +283,15 @@ def test_preference_with_tokens_of_no_probability(low, peak):
     assert (d.double() - want).abs().max() < 1e-6
 
 
+@pytest.mark.parametrize("dtype,m,v,pad", [(torch.bfloat16, 300, 4100, 0), (torch.bfloat16, 300, 5113, 0), (torch.float32, 300, 2551, 1), (torch.bfloat16, 200, 40001, 0),
+                                           (torch.float16, 160, 50257, 0), (torch.float16, 160, 65537, 5), (torch.float32, 100, 65531, 0), (torch.bfloat16, 100, 160001, 0)])
+def test_policy_lengths_between_batches(dtype, m, v, pad):
+    """Rows whose words leave a CTA, or the last of a row's, batches that are not full: one warp's, and those of three to eight CTAs."""
+    x = make(m, v, dtype, v, pad)
+    x["index"][:4] = torch.tensor([0, v - 1, -1, v], dtype=torch.int32)
+    check_policy(x, 1.0, 0.05)
+
+
 def test_gradient_of_losses_that_dloss_does_not_hold():
     """Stats of one loss with an upstream gradient of another length: rows whose place it has not get NaN, rows without a slope 0."""
     for dtype in DTYPES:
