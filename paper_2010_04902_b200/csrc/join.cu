@@ -273,7 +273,7 @@ template <int VEC, int COLS, int THREADS> struct ByColumn {
 
 // Sums over the row's threads, one barrier each; two sets of partial sums in turn.
 struct ExchangeRoom {
-    float warp[2][2][16];
+    float warp[2][2][kTeam / 32];
     float rank[2][2][kMostRanks];
 };
 template <int THREADS> struct Exchange {
@@ -281,7 +281,7 @@ template <int THREADS> struct Exchange {
     Room* room;
     int ranks, turn = 0;
     __device__ __forceinline__ Exchange(Room* r, int ranks_) : room(r), ranks(ranks_) {
-        for (int k = threadIdx.x; k < 64; k += team_threads<THREADS>()) (&r->warp[0][0][0])[k] = 0.f;
+        for (int k = threadIdx.x; k < kTeam / 8; k += team_threads<THREADS>()) (&r->warp[0][0][0])[k] = 0.f;
         if (ranks > 1)
             cg::this_cluster().sync();
         else
@@ -301,7 +301,7 @@ template <int THREADS> struct Exchange {
             for (int k = 0; k < K; ++k) {
                 v[k] = 0.f;
 #pragma unroll
-                for (int w = 0; w < 16; w += 4) {
+                for (int w = 0; w < kTeam / 32; w += 4) {
                     if (w >= warps) break;
                     const float4 p = *reinterpret_cast<const float4*>(&room->warp[turn][k][w]);
                     v[k] += (p.x + p.y) + (p.z + p.w);
@@ -419,8 +419,16 @@ __device__ __forceinline__ float branch_weight(const JoinArgs& a, int64_t group,
     return a.w_post != nullptr ? w * a.w_post[c] : w;
 }
 
+// Threads that an SM holds of the kernel, by its registers; of a CTA without a constant number.
+template <typename T, int COLS, bool SHIFT> constexpr int held_threads() { return sizeof(T) == 2 && COLS == 8 && !SHIFT ? 768 : kTeam; }
+template <int COLS> constexpr int most_threads() { return COLS == 8 ? 256 : kTeam; }
+// 16-bit rows in words of 4096 to 6144 columns (of a CTA): a row's time is its own chain of barriers, 2.3 us, and an SM holds two CTAs of 320
+// (96 registers a thread) or 384 (80) threads.  Bfloat16 with both norms and dropout: 8192 x 5120 87 us, one CTA an SM 128; x 6144 101, 131; 4096 x 12288
+// in pairs of CTAs 132, 202.  (Three CTAs of 256 threads, for up to 4096 columns: 8192 rows 70 us, as with two; 1024 rows 18.5 for 16.6.)
+template <typename T, int COLS, bool SHIFT> constexpr bool two_wide() { return COLS == 16 && sizeof(T) == 2 && !SHIFT; }
+
 template <typename T, int COLS, int THREADS, bool SHIFT>
-__global__ void __launch_bounds__(THREADS ? THREADS : 128, (sizeof(T) == 2 && COLS == 8 && !SHIFT ? 768 : 512) / (THREADS ? THREADS : 128)) join_kernel(const __grid_constant__ JoinArgs a, int ranks, JoinRows<const T> x, JoinRows<const T> y, JoinRows<T> s, JoinRows<T> z) {
+__global__ void __launch_bounds__(THREADS ? THREADS : most_threads<COLS>(), THREADS == 320 || THREADS == 384 ? 2 : held_threads<T, COLS, SHIFT>() / (THREADS ? THREADS : most_threads<COLS>())) join_kernel(const __grid_constant__ JoinArgs a, int ranks, JoinRows<const T> x, JoinRows<const T> y, JoinRows<T> s, JoinRows<T> z) {
     constexpr int VEC = Word<T>::kN;
     extern __shared__ __align__(16) float4 smem[];
     __shared__ __align__(16) ExchangeRoom room;
@@ -510,7 +518,7 @@ __device__ __forceinline__ int64_t part_begin(const Parts& p, int64_t k) { retur
 __device__ __forceinline__ int64_t part_end(const Parts& p, int64_t k) { return k / p.per_group * p.rows + (k % p.per_group + 1) * p.rows / p.per_group; }
 
 template <typename T, int COLS, int THREADS, bool SHIFT>
-__global__ void __launch_bounds__(THREADS ? THREADS : 128, 512 / (THREADS ? THREADS : 128)) join_backward_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ Parts parts, const __grid_constant__ Sums out, int ranks,
+__global__ void __launch_bounds__(THREADS ? THREADS : kTeam, 512 / (THREADS ? THREADS : kTeam)) join_backward_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ Parts parts, const __grid_constant__ Sums out, int ranks,
                                                               JoinRows<const T> x, JoinRows<const T> y, JoinRows<const T> ds, JoinRows<const T> dz, JoinRows<T> dx, JoinRows<T> dy) {
     constexpr int VEC = Word<T>::kN;
     extern __shared__ __align__(16) float4 smem[];
@@ -707,6 +715,17 @@ __global__ void __launch_bounds__(32 * kFoldRows) fold_kernel(const __grid_const
 
 // ---- host side ----------------------------------------------------------------------------------
 
+// Threads for so many columns, a multiple of 32.  A power of two, whose distances are constants for 256 and 512 threads, but what the row
+// needs where an SM, which holds `held` threads, then has another CTA (8192 x 2560 bfloat16, 160 threads for 256: 56 us forward and 89 backward,
+// 68 and 121; x 3584, two CTAs either way: 76 and 119 against 68 and 109) and, if `wide`, beyond 256: backward 4096 x 5120 binary32 242 -> 218 us
+// (forward 89 -> 94).
+int threads_of(int columns, int each, int held, bool wide) {
+    int threads = 32;
+    while (threads * each < columns) threads *= 2;
+    const int needed = (columns + 32 * each - 1) / (32 * each) * 32;
+    return (needed > 256 ? wide : held / needed > held / threads) ? needed : threads;
+}
+
 // columns: how many a thread of the backward kernel has (16: 16-bit rows in words)
 Parts parts_of(int64_t m, int64_t n, int64_t groups, int columns) {
     Parts p;
@@ -715,6 +734,10 @@ Parts parts_of(int64_t m, int64_t n, int64_t groups, int columns) {
     // As many CTAs as an SM holds (512 threads by their registers, and a little less by the shared memory of small ones), but none of fewer
     // than 16 rows: their sums' traffic would show (few rows take the time of one after the other: two then).  Wider rows take a cluster.
     int64_t per_sm = columns * kTeam / (n > 512 ? n : columns == 16 ? 683 : 512);
+    if (n <= 512 * columns) {
+        const int fit = kTeam / threads_of(static_cast<int>(n), columns, kTeam, true);
+        if (per_sm > fit) per_sm = fit;
+    }
     const int64_t least = m * n >= (int64_t(1) << 23) ? 16 : 2;
     if (per_sm > 1 && m < per_sm * kNumSMs * least) per_sm = m / (kNumSMs * least);
     p.teams = per_sm > 1 ? per_sm * kNumSMs : n <= 16 * kTeam ? kNumSMs : kNumSMs / 2;
@@ -761,9 +784,12 @@ template <typename T, int COLS, int NT, bool SHIFT> int smem_of(int threads, int
 }
 template <typename T, int COLS, int NT, bool SHIFT> Shape shape_of(int n, int vectors, bool drop) {
     Shape s{32, 1, 0};
-    const int most = sizeof(T) == 4 && COLS == 16 && SHIFT ? kTeam / 2 : kTeam;   // what shared memory holds
-    while (s.threads < most && s.threads * COLS < n) s.threads *= 2;
-    while (s.threads * COLS * s.ranks < n) s.ranks *= 2;
+    const int held = NT == 2 ? held_threads<T, COLS, SHIFT>() : kTeam;            // by an SM
+    const int most = sizeof(T) == 4 && COLS == 16 && SHIFT ? kTeam / 2 : kTeam;   // what shared memory holds of the widest
+    while (most * COLS * s.ranks < n) s.ranks *= 2;
+    const int part = (n + s.ranks - 1) / s.ranks;   // columns of a CTA
+    s.threads = threads_of(part, COLS, held, NT == 4);
+    if (NT == 2 && two_wide<T, COLS, SHIFT>() && s.threads == 512 && part <= 384 * COLS) s.threads = part <= 320 * COLS ? 320 : 384;
     s.smem = smem_of<T, COLS, NT, SHIFT>(s.threads, vectors, drop && !(sizeof(T) == 2 && n % 8 == 0));
     return s;
 }
@@ -801,13 +827,18 @@ template <typename T> JoinRows<T> output(void* p, int64_t ld) { return {static_c
 template <typename T, int COLS, bool SHIFT> int forward_as(const JoinArgs& a, const JoinTensors& t, cudaStream_t s) {
     const Shape shape = shape_of<T, COLS, 2, SHIFT>(a.n, 2, a.drop != 0);
     // as many as an SM holds, by their registers and by their shared memory
-    int per_sm = (COLS == 8 && sizeof(T) == 2 && !SHIFT ? 768 : 512) / shape.threads;
+    int per_sm = held_threads<T, COLS, SHIFT>() / shape.threads;
+    if (two_wide<T, COLS, SHIFT>() && shape.threads > 256 && shape.threads <= 384) per_sm = 2;
     if (per_sm * (shape.smem + 2048) > 220 * 1024) per_sm = 220 * 1024 / (shape.smem + 2048);
     const int64_t most = static_cast<int64_t>(per_sm > 1 ? per_sm : 1) * kNumSMs / shape.ranks;
-    // sixteen columns a thread begin at 256 threads, eight end there
-    constexpr int kOther = COLS == 8 ? 0 : sizeof(T) == 4 && SHIFT ? 256 : 512;
-    auto kern = join_kernel<T, COLS, kOther, SHIFT>;
+    auto kern = join_kernel<T, COLS, 0, SHIFT>;
     if (shape.threads == 256) kern = join_kernel<T, COLS, 256, SHIFT>;
+    if constexpr (two_wide<T, COLS, SHIFT>()) {
+        if (shape.threads == 320) kern = join_kernel<T, COLS, 320, SHIFT>;
+        if (shape.threads == 384) kern = join_kernel<T, COLS, 384, SHIFT>;
+    }
+    if constexpr (COLS == 16 && !(sizeof(T) == 4 && SHIFT))   // eight columns a thread end at 256 threads, and what shared memory holds of these
+        if (shape.threads == 512) kern = join_kernel<T, COLS, 512, SHIFT>;
     return start(kern, shape, a.m < most ? a.m : most, most_smem<T, COLS, 2, SHIFT>(2), s, a, shape.ranks, input<T>(t.a, t.ld_a, a), input<T>(t.b, t.ld_b, a), output<T>(t.e, t.ld_e),
                  output<T>(t.f, t.ld_f));
 }

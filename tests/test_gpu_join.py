@@ -167,6 +167,14 @@ def test_forms(change, n, dtype):
     check(*make(6, n, dtype, seed=1, **change))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,n,pad", [(1900, 600, 0), (1900, 768, 0), (1300, 1536, 0), (600, 2304, 8), (600, 2560, 0), (600, 2561, 0), (400, 4600, 8), (400, 5120, 0), (400, 5128, 0),
+                                     (310, 6144, 8), (310, 6143, 2), (310, 6152, 0), (300, 7000, 0), (160, 9600, 0), (160, 12288, 0), (160, 13000, 0), (150, 12281, 0)])
+def test_widths_between_powers_of_two(m, n, pad, dtype):
+    """A CTA's threads are what such a row needs, or more; several of them share an SM and take some rows one after the other."""
+    check(*make(m, n, dtype, seed=n, pad=pad, norm="layer" if m % 100 else "rms"))
+
+
 @pytest.mark.parametrize("which", ["ds", "dz"])
 def test_one_gradient_alone(which):
     t, form = make(10, 300, torch.bfloat16, seed=2)
