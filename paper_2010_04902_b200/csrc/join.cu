@@ -8,8 +8,8 @@
 //   dw_pre = sum over rows of dz norm(s).
 // One read of x, y and one write of s, z forward; one read of x, y, ds, dz and one write of dx, dy backward.
 //
-// A thread owns the same columns of every row: COLS of them, in 16-byte words where every tensor's rows begin on 16-byte
-// boundaries, else single elements a CTA's width apart.  So what belongs to a column (w and w_pre in shared memory, the column sums in
+// A thread owns the same columns of every row: COLS of them, in 16-byte words (rows that do not begin on 16-byte boundaries are
+// copied in whole words and shifted in shared memory).  So what belongs to a column (w and w_pre in shared memory, the column sums in
 // registers) needs no exchange.  A CTA of up to 512 threads holds a row, a cluster of two or four a wider one; the row's
 // sums cost one barrier each.  The next row's words come by cp.async while a row is worked on: a thread copies what it reads
 // itself, and waits for nobody.
