@@ -739,8 +739,9 @@ int bz_join(const void* x, int64_t ld_x, const void* y, int64_t ld_y, int dtype,
 
 /*
  * Its gradient, from the stream's ds (NULL: 0) and the next block's dz (NULL: 0), with x, y and stats as bz_join had and left
- * them; s is formed anew, in binary32 (x is read where there are dz and w_pre only).  A forward call that wrote s over x or z over y
- * has no backward call.
+ * them; s is formed anew, in binary32 (x is read where there are dz and w_pre only).  x is the stream that went in: the s that
+ * bz_join wrote is rounded, has the same form, and in x's place gives wrong numbers.  A forward call that wrote s over x or z over y has no
+ * backward call.
  *   g = ds + the norm's gradient of dz * w_pre at s,   dx = residual_scale * g,
  *   u = branch_scale * drop'(g),  dgate = sum over a group's rows of u * a,   dy = the norm's gradient of u * gate * w_post at y,
  *   dw_post = sum over rows of u * gate * norm(y),   dw_pre = sum over rows of dz * norm(s).

@@ -1045,6 +1045,7 @@ def dropout(x: torch.Tensor, rate: float, rng: torch.Tensor, out: torch.Tensor |
     dt = _dtype(x, "x")
     _here(x, "x")
     m, n, ld = _collapsed(x, "x")
+    given = out
     if out is None:
         out = torch.empty_like(x) if m == 1 else x.new_empty(m, ld).as_strided(x.shape, x.stride()) if ld <= 2 * n else torch.empty(x.shape, dtype=x.dtype, device=x.device)
     if out.shape != x.shape or out.dtype != x.dtype or not out.is_cuda:
@@ -1059,7 +1060,15 @@ def dropout(x: torch.Tensor, rate: float, rng: torch.Tensor, out: torch.Tensor |
     st = lib().bz_dropout(x.data_ptr(), ld, dt, m, n, rate, _packed(rng, (2,), torch.int64, "rng"), out.data_ptr(), ld2, _stream())
     if st:
         _check(st, "bz_dropout")
+    _written(given)
     return out
+
+
+def _written(*given):
+    """The caller's tensors that a call has written, for who keeps one of them: torch counts only its own writes."""
+    for t in given:
+        if t is not None:
+            torch._C._increment_version((t,))
 
 
 _NORMS = {"rms": NORM_RMS, "layer": NORM_LAYER}
@@ -1086,7 +1095,8 @@ def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | 
          stats: torch.Tensor | None = None):
     """bz_join: s = residual_scale x + branch_scale gate drop(norm(y) w_post), z = norm(s) w_pre, for rows x, y [m][n] and weights
     float32 [n], gate float32 [groups][n].  Returns (s, z, stats); z is None without w_pre.  Without y: the norm alone, and s is
-    written only if it is given (or residual_scale is not 1; otherwise the s that comes back is x)."""
+    written only if it is given (or residual_scale is not 1; otherwise the s that comes back is x).  For join_backward() stats keep x
+    alive (itself, no copy of it), as automatic differentiation keeps what a backward pass reads."""
     if x.requires_grad or (y is not None and y.requires_grad):
         _unrecorded("join", x=x, y=y if y is not None else x)
     for name, w in (("w_post", w_post), ("gate", gate), ("w_pre", w_pre)):
@@ -1098,6 +1108,7 @@ def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | 
     p_post, p_gate, groups, p_rng, p_pre = _join_form(n, w_post, gate, w_pre, rate, rng)
     p_y, ld_y = (None, 0) if y is None else _row_tensor(y, x.shape, x.dtype, "y")
     keep = s is None and y is None and residual_scale == 1.0 and w_pre is not None
+    given = s, z
     if s is None and not keep:
         s = _alike(x)
     p_s, ld_s = (None, 0) if s is None else _row_tensor(s, x.shape, x.dtype, "s")
@@ -1109,26 +1120,51 @@ def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | 
                        p_pre, p_s, ld_s, p_z, ld_z, p_stats, _stream())
     if st:
         _check(st, "bz_join")
+    _written(*given)
+    stats._stream_in = x, None if x.is_inference() else x._version, m * n > 0 and any(t is not None and t.data_ptr() == x.data_ptr() for t in given)
     return x if keep else s, z, stats
+
+
+def _stream_in(stream: torch.Tensor, stats: torch.Tensor) -> torch.Tensor:
+    """The x of the join() call that stats come from, where they keep it; `stream` may be that x or the s of the call."""
+    x, version, over = getattr(stats, "_stream_in", (stream, None, False))
+    if x is stream and not over:
+        return x
+    if stream.shape != x.shape or stream.dtype is not x.dtype or stream.device != x.device:
+        raise ValueError("join_backward: the stream must be like the x that join() had")
+    there = stream.data_ptr() == x.data_ptr()
+    if over and there:
+        raise ValueError("join_backward: join() has written over its x, which the gradient needs: keep a copy and give it as x=")
+    if over or there:
+        return stream
+    if version is not None and x._version != version:
+        raise ValueError("join_backward: the x that join() had was written since: give the stream as it went in as x=")
+    return x
 
 
 def join_workspace_bytes(m: int, n: int, groups: int = 0) -> int:
     return int(lib().bz_join_workspace_bytes(m, n, groups))
 
 
-def join_backward(x: torch.Tensor, y: torch.Tensor | None, stats: torch.Tensor, ds: torch.Tensor | None = None,
+def join_backward(stream: torch.Tensor | None = None, y: torch.Tensor | None = None, stats: torch.Tensor | None = None, ds: torch.Tensor | None = None,
                   dz: torch.Tensor | None = None, w_post: torch.Tensor | None = None, gate: torch.Tensor | None = None,
                   w_pre: torch.Tensor | None = None, norm: str = "rms", residual_scale: float = 1.0, branch_scale: float = 1.0,
                   rate: float = 0.0, rng: torch.Tensor | None = None, dx: torch.Tensor | None = None, dy: torch.Tensor | None = None,
                   dw_post: torch.Tensor | None = None, dgate: torch.Tensor | None = None, dw_pre: torch.Tensor | None = None,
-                  workspace: torch.Tensor | None = None):
-    """bz_join_backward, with x, y and stats as join() had and returned them: returns (dx, dy, dw_post, dgate, dw_pre), None for what the call has no operand of.  dw_post, dgate and
-    dw_pre may be views of a gradient row."""
+                  workspace: torch.Tensor | None = None, x: torch.Tensor | None = None):
+    """bz_join_backward, with y and stats as join() had and returned them: returns (dx, dy, dw_post, dgate, dw_pre), None for what the call has
+    no operand of.  `stream` is the x that went into join() or the s that came out: the gradient is formed from x, which stats keep.  A copy of
+    stats keeps none, and `stream` is x then; x=... is taken as it is.  dw_post, dgate and dw_pre may be views of a gradient row."""
+    if stats is None or (x is None) == (stream is None):
+        raise TypeError("join_backward needs stats and either a stream or x")
+    if x is None:
+        x = _stream_in(stream, stats)
     m, n, ld = _matrix(x, "x")
     dt = _dtype(x, "x")
     _here(x, "x")
     p_post, p_gate, groups, p_rng, p_pre = _join_form(n, w_post, gate, w_pre, rate, rng)
     like = x.shape, x.dtype
+    given = dx, dy
     p_y, ld_y = (None, 0) if y is None else _row_tensor(y, *like, "y")
     p_ds, ld_ds = (None, 0) if ds is None else _row_tensor(ds, *like, "ds")
     p_dz, ld_dz = (None, 0) if dz is None else _row_tensor(dz, *like, "dz")
@@ -1157,4 +1193,5 @@ def join_backward(x: torch.Tensor, y: torch.Tensor | None, stats: torch.Tensor, 
                                 p_dpost, p_dgate, p_dpre, *room, _stream())
     if st:
         _check(st, "bz_join_backward")
+    _written(*given)
     return dx, dy, dw_post, dgate, dw_pre
