@@ -342,7 +342,7 @@ def run(state):
         s, z, stats = bz.join(state["x"], state["y"], **form)
         out = {"s": s, "z": z}
         if train:
-            back = bz.join_backward(state["x"], state["y"], stats, ds=state["ds"], dz=state["dz"], **form)
+            back = bz.join_backward(s, state["y"], stats, ds=state["ds"], dz=state["dz"], **form)
             out.update({name: t for name, t in zip(("dx", "dy", "dw_post", "dgate", "dw_pre"), back) if t is not None})
         return out
     else:
