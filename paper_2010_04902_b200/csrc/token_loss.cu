@@ -3,10 +3,11 @@
 // Both rest on lp = z[a] - log(sum of exp z), z = logits / T, and on one number a row, the slope d loss / d lp:
 // dlogits = dloss * slope / T * ([c == a] - softmax(z)[c]).
 //
-// Exponents are s c - R, one multiply-add: c = log2(e)/T rounded to binary32 and R the whole number next to the largest s c, so that the
-// multiply-add's rounding is the only one, and joining two parts of a row is exact.  The rounding of c is a temperature that differs by 2^-25 at
+// Exponents are s c - R, one multiply-add: c = log2(e)/T rounded to binary32 and R the largest s c, rounded to binary32 and to a whole number, so that
+// the multiply-add's rounding is the only one, and joining two parts of a row is exact.  The rounding of c is a temperature that differs by 2^-24 at
 // most; the token's own logit goes by the same c, or the error would have one sign in all lp and a sum over a sequence would collect it.
-// Where s c is beyond 2^100 (rows of a type's lowest value) exponents are (s - largest) c.
+// The largest's own exponent is what the rounding of R left: half a unit of the largest s c beyond 2^24.  So from 2^30 on (a row of a mask's
+// fill, a peak) exponents are (s - largest) c; below, that exponent is 32 at most, and a sum of 2^31 terms fits.
 #include <cooperative_groups.h>
 
 #include "worker_common.cuh"
@@ -40,11 +41,12 @@ struct Base {
     bool apart;
     __device__ __forceinline__ Base(const TokenArgs& a, float largest) {
         const float y = largest * a.c;
-        m = largest, apart = !(fabsf(y) < 0x1p100f) && largest != -INFINITY;
+        m = largest, apart = !(fabsf(y) < 0x1p30f) && largest != -INFINITY;
         r = apart || largest == -INFINITY ? 0.f : rintf(y);
     }
     __device__ __forceinline__ float exponent(const TokenArgs& a, float s) const { return apart ? (s - m) * a.c : fmaf(s, a.c, -r); }
-    // of a part's base, relative to this one, which has the larger s
+    // of a part's base, relative to this one, which has the larger s.  Where one of the two is apart and the other is not, they are a unit of a
+    // number of 2^30 from one another at least, 2^6, and what the part adds is below 2^-64 of the sum.
     __device__ __forceinline__ float of(const TokenArgs& a, const Base& part) const { return !apart && !part.apart ? part.r - r : apart && part.apart ? (part.m - m) * a.c : -INFINITY; }
     // log2 of what the sum is relative to the largest itself
     __device__ __forceinline__ float rest(const TokenArgs& a) const { return apart || m == -INFINITY ? 0.f : fmaf(m, a.c, -r); }
