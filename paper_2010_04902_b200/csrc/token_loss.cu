@@ -145,8 +145,16 @@ struct RowScalars {
     __device__ __forceinline__ float factor(const TokenArgs& a, const RowInputs& in) const { return slope == 0.f ? 0.f : slope * in.dloss / a.temperature; }
 };
 template <bool POLICY> __device__ __forceinline__ RowScalars row_scalars(const TokenArgs& a, const RowInputs& in, const MaxSum& all) {
-    RowScalars s{0.0, static_cast<double>(all.s) * kPowers, exact_rest(a, Base(a, all.m)), 0.f, 0.f};
-    s.lp = log_probability(a, in.logit, all.m, s.rest, s.sum);
+    const Base base(a, all.m);
+    RowScalars s{0.0, static_cast<double>(all.s) * kPowers, exact_rest(a, base), 0.f, 0.f};
+    // A token that has most of the row goes by its own exponential, which is a term of the sum bit for bit (it is the largest, and its thread's
+    // whole number was the row's): sums only grow, so lp is at most 0, and 0 where the others vanish beside it.  The correction is a mean over
+    // many terms and has no place there.
+    const float own = in.logit == all.m ? exp2_fast(base.exponent(a, in.logit)) : 0.f;
+    if (own > 0.5f * all.s)
+        s.lp = 0.0 - log1p((static_cast<double>(all.s) - static_cast<double>(own)) / static_cast<double>(own));
+    else
+        s.lp = log_probability(a, in.logit, all.m, s.rest, s.sum);
     if (POLICY) {
         // both exponentials at once: the ratio's on the even lanes, the KL term's on the odd ones
         const double shift = threadIdx.x & 1 ? static_cast<double>(in.ref_logp) - s.lp : s.lp - static_cast<double>(in.old_logp), e = expm1(shift);
