@@ -750,6 +750,7 @@ Parts parts_of(int64_t m, int64_t n, int64_t groups, int columns) {
 }
 size_t gate_sums(const Parts& p, int64_t n) { return p.per_group > 1 ? static_cast<size_t>(p.count) * n : 0; }
 size_t workspace_of(int64_t m, int64_t n, int64_t groups) {
+    if (n == 0) return 256;   // no columns to cut: nothing is kept, and 0 would be a refusal
     size_t most = 0;
     for (int columns : {8, 16}) {
         const Parts p = parts_of(m, n, groups, columns);
