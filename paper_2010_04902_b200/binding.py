@@ -1081,10 +1081,10 @@ def _norm(name: str) -> int:
         raise ValueError("norm must be rms or layer") from None
 
 
-def _join_form(n, w_post, gate, w_pre, rate, rng):
+def _join_form(m, n, w_post, gate, w_pre, rate, rng):
     """Addresses of w_post, gate, its rows, rng, w_pre."""
-    if gate is not None and (gate.dim() != 2 or gate.shape[1] != n):
-        raise ValueError("gate must be [groups][%d]" % n)
+    if gate is not None and (gate.dim() != 2 or gate.shape[1] != n or (m > 0 and gate.shape[0] == 0)):
+        raise ValueError("gate must be [groups][%d], of one group at least" % n)
     return (_packed(w_post, (n,), torch.float32, "w_post"), None if gate is None else _packed(gate, gate.shape, torch.float32, "gate"),
             0 if gate is None else gate.shape[0], _packed(rng, (2,), torch.int64, "rng"), _packed(w_pre, (n,), torch.float32, "w_pre"))
 
@@ -1105,7 +1105,7 @@ def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | 
     m, n, ld_x = _matrix(x, "x")
     dt = _dtype(x, "x")
     _here(x, "x")
-    p_post, p_gate, groups, p_rng, p_pre = _join_form(n, w_post, gate, w_pre, rate, rng)
+    p_post, p_gate, groups, p_rng, p_pre = _join_form(m, n, w_post, gate, w_pre, rate, rng)
     p_y, ld_y = (None, 0) if y is None else _row_tensor(y, x.shape, x.dtype, "y")
     keep = s is None and y is None and residual_scale == 1.0 and w_pre is not None
     given = s, z
@@ -1162,7 +1162,7 @@ def join_backward(stream: torch.Tensor | None = None, y: torch.Tensor | None = N
     m, n, ld = _matrix(x, "x")
     dt = _dtype(x, "x")
     _here(x, "x")
-    p_post, p_gate, groups, p_rng, p_pre = _join_form(n, w_post, gate, w_pre, rate, rng)
+    p_post, p_gate, groups, p_rng, p_pre = _join_form(m, n, w_post, gate, w_pre, rate, rng)
     like = x.shape, x.dtype
     given = dx, dy
     p_y, ld_y = (None, 0) if y is None else _row_tensor(y, *like, "y")
