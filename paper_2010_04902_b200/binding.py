@@ -1085,6 +1085,8 @@ def _join_form(m, n, w_post, gate, w_pre, rate, rng):
     """Addresses of w_post, gate, its rows, rng, w_pre."""
     if gate is not None and (gate.dim() != 2 or gate.shape[1] != n or (m > 0 and gate.shape[0] == 0)):
         raise ValueError("gate must be [groups][%d], of one group at least" % n)
+    if n == 0:
+        gate = None      # it has no address, and rows without one are refused
     return (_packed(w_post, (n,), torch.float32, "w_post"), None if gate is None else _packed(gate, gate.shape, torch.float32, "gate"),
             0 if gate is None else gate.shape[0], _packed(rng, (2,), torch.int64, "rng"), _packed(w_pre, (n,), torch.float32, "w_pre"))
 

@@ -885,7 +885,7 @@ int check(int dtype, int64_t m, int64_t n, int norm, float eps, const void* y, c
         return BZ_ERR_INVALID_ARG;
     if (m >= (int64_t(1) << 31) || n > BZ_MAX_WIDTH || groups >= (int64_t(1) << 31)) return BZ_ERR_UNSUPPORTED;
     if ((gate != nullptr) != (groups > 0) || (groups > 0 && m % groups != 0)) return BZ_ERR_INVALID_ARG;
-    if (m > 0 && y == nullptr && (w_post != nullptr || gate != nullptr || *least != 0)) return BZ_ERR_INVALID_ARG;
+    if (m > 0 && n > 0 && y == nullptr && (w_post != nullptr || gate != nullptr || *least != 0)) return BZ_ERR_INVALID_ARG;
     if (*least != 0 && rng == nullptr) return BZ_ERR_INVALID_ARG;
     return BZ_OK;
 }
