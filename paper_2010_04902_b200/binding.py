@@ -903,11 +903,16 @@ def distill_backward(logits: torch.Tensor, teacher: torch.Tensor, index: torch.T
 
 # ------------------------------------------------------------------------- losses on one token a position
 
-def _here(t: torch.Tensor, name: str):
-    """The calls below launch on the current device's current stream: their tensors have to live there."""
-    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError("%s is on %s, the current device is cuda:%d: call under torch.cuda.device(%s.device)"
-                         % (name, t.device, torch._C._cuda_getDevice(), name))
+def _here(t: torch.Tensor, name: str, others=()):
+    """The calls below launch on the current device's current stream: their tensors have to live there, `others` (None among them) too."""
+    if not t.is_cuda:
+        return
+    here = torch._C._cuda_getDevice()
+    if t.get_device() != here:
+        raise ValueError("%s is on %s, the current device is cuda:%d: call under torch.cuda.device(%s.device)" % (name, t.device, here, name))
+    for other in others:
+        if other is not None and other.get_device() != here and other.is_cuda:
+            raise ValueError("%s is on %s, another tensor of the call on %s" % (name, t.device, other.device))
 
 
 def _row_tensor(t, shape, dtype, name: str):
@@ -917,11 +922,11 @@ def _row_tensor(t, shape, dtype, name: str):
     return _shaped(t, shape, dtype, name), _matrix(t, name)[2]
 
 
-def _token_operands(logits, index, dloss, dlogits):
+def _token_operands(logits, index, dloss, dlogits, *others):
     """(m, arguments from logits to index, whether a gradient is wanted, dlogits, its address and leading dimension)."""
     m, v, ld = _matrix(logits, "logits")
     head = (logits.data_ptr(), ld, _dtype(logits, "logits"), m, v, _packed(index, (m,), torch.int32, "index"))
-    _here(logits, "logits")
+    _here(logits, "logits", (index, dloss, dlogits, *others))
     if dlogits is None:
         if dloss is None:
             return m, head, False, None, None, 0
@@ -955,7 +960,7 @@ def policy(logits: torch.Tensor, index: torch.Tensor, advantage: torch.Tensor, o
     (float32 [m]) or `dlogits` given also the gradient, from the same pass: (loss, logp, stats, dlogits)."""
     if logits.requires_grad:
         _unrecorded("policy", logits=logits)
-    m, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
+    m, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits, advantage, old_logp, ref_logp, loss, logp, stats)
     p_advantage = _packed(advantage, (m,), torch.float32, "advantage")
     loss, p_loss = _made(loss, advantage, (m,), "loss")
     logp, p_logp = _made(logp, advantage, (m,), "logp")
@@ -977,7 +982,7 @@ def preference(logits: torch.Tensor, index: torch.Tensor, starts: torch.Tensor, 
     (loss, reward, logp, stats, dlogits)."""
     if logits.requires_grad:
         _unrecorded("preference", logits=logits)
-    m, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
+    m, head, grad, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits, starts, ref_logp, loss, reward, logp, stats)
     if starts.dim() != 1 or starts.shape[0] % 2 != 1:
         raise ValueError("starts must be [2 pairs + 1]")
     pairs = starts.shape[0] // 2
@@ -999,7 +1004,7 @@ def token_loss_backward(logits: torch.Tensor, index: torch.Tensor, stats: torch.
     loss it does not hold get NaN)."""
     if dlogits is None:
         dlogits = _alike(logits)
-    m, head, _, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits)
+    m, head, _, dlogits, p_d, ld_d = _token_operands(logits, index, dloss, dlogits, stats)
     if dloss is not None and dloss.dim() != 1:
         raise ValueError("dloss must be [m] or [pairs]")
     p_stats = _packed(stats, (m, 4), torch.float32, "stats")
@@ -1043,7 +1048,7 @@ def dropout(x: torch.Tensor, rate: float, rng: torch.Tensor, out: torch.Tensor |
             raise ValueError("dropout: x requires a gradient, which this call does not record: call it under torch.no_grad() (or inside an "
                              "autograd.Function), and again on the gradient")
     dt = _dtype(x, "x")
-    _here(x, "x")
+    _here(x, "x", (rng, out))
     m, n, ld = _collapsed(x, "x")
     given = out
     if out is None:
@@ -1106,7 +1111,7 @@ def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | 
             _unrecorded("join", **{name: w})
     m, n, ld_x = _matrix(x, "x")
     dt = _dtype(x, "x")
-    _here(x, "x")
+    _here(x, "x", (y, w_post, gate, w_pre, rng, s, z, stats))
     p_post, p_gate, groups, p_rng, p_pre = _join_form(m, n, w_post, gate, w_pre, rate, rng)
     p_y, ld_y = (None, 0) if y is None else _row_tensor(y, x.shape, x.dtype, "y")
     keep = s is None and y is None and residual_scale == 1.0 and w_pre is not None
@@ -1163,7 +1168,7 @@ def join_backward(stream: torch.Tensor | None = None, y: torch.Tensor | None = N
         x = _stream_in(stream, stats)
     m, n, ld = _matrix(x, "x")
     dt = _dtype(x, "x")
-    _here(x, "x")
+    _here(x, "x", (y, stats, ds, dz, w_post, gate, w_pre, rng, dx, dy, dw_post, dgate, dw_pre, workspace))
     p_post, p_gate, groups, p_rng, p_pre = _join_form(m, n, w_post, gate, w_pre, rate, rng)
     like = x.shape, x.dtype
     given = dx, dy
