@@ -296,18 +296,17 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
             }
             cluster.sync();
         }
+        RowScalars scalars{};
         if (warp == 0) {
             sum = joined(a, share.ranks > 1 ? (lane < share.ranks ? peers[lane] : MaxSum{-INFINITY, 0.f}) : (lane < (threads >> 5) ? part[lane] : MaxSum{-INFINITY, 0.f}));
-            const RowScalars scalars = row_scalars<POLICY>(a, in, sum);
+            scalars = row_scalars<POLICY>(a, in, sum);
             if (GRADIENT) {
                 const float got = scalars.factor(a, in);
                 if (lane == 0) outcome = make_float3(sum.m, got == 0.f ? 0.f : -got / sum.s, got);
-                __syncthreads();
             }
-            if (lane == 0 && rank == 0) write_row(a, i, sum, scalars, POLICY);
-        } else if (GRADIENT) {
-            __syncthreads();
         }
+        if (GRADIENT) __syncthreads();
+        if (t == 0 && rank == 0) write_row(a, i, sum, scalars, POLICY);
         if (!GRADIENT) return;
         top = outcome.x, f = outcome.y, g = outcome.z;
     } else {
