@@ -1128,7 +1128,12 @@ def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | 
     if st:
         _check(st, "bz_join")
     _written(*given)
-    stats._stream_in = x, None if x.is_inference() else x._version, m * n > 0 and any(t is not None and t.data_ptr() == x.data_ptr() for t in given)
+    p_x = x.data_ptr()
+    try:
+        version = x._version
+    except RuntimeError:      # a tensor of inference mode counts no writes
+        version = None
+    stats._stream_in = x, version, p_x != 0 and (p_s == p_x or p_z == p_x)
     return x if keep else s, z, stats
 
 

@@ -87,3 +87,14 @@ def test_captured_and_replayed():
     graph.replay()
     _, _, stats = bz.join(t["x"], t["y"], **form, eps=EPS)
     assert all_equal(back, bz.join_backward(t["x"], t["y"], stats, ds=t["ds"], dz=t["dz"], **form))
+
+
+def test_tensors_of_inference_mode():
+    """They count no writes."""
+    t, form = make(20, 128, torch.bfloat16, seed=1)
+    _, _, stats = bz.join(t["x"], t["y"], **form)
+    want = bz.join_backward(t["x"], t["y"], stats, ds=t["ds"], dz=t["dz"], **form)
+    with torch.inference_mode():
+        x = t["x"].clone()
+        s, _, stats = bz.join(x, t["y"], **form)
+        assert all_equal(bz.join_backward(s, t["y"], stats, ds=t["ds"], dz=t["dz"], **form), want)
