@@ -56,13 +56,6 @@ struct Keep {
             x[2 * i + 1] = upper(u[i]) ? y.y : 0.f;
         }
     }
-    // bit i, i < N <= 8: element first + i stays
-    template <int N> __device__ __forceinline__ uint32_t elements(uint64_t first) const {
-        const int at = static_cast<int>(first & 7);
-        uint32_t bits = group(first >> 3) >> at;
-        if (at + N > 8) bits |= group((first >> 3) + 1) << (8 - at);
-        return bits & ((1u << N) - 1u);
-    }
 };
 
 }  // namespace bz
