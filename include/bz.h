@@ -645,7 +645,8 @@ int bz_distill_backward(const void* logits, int64_t ld, int dtype, int64_t m, in
  *   dlogits  device [m][v] with ld_d, dtype's elements, or NULL: the loss alone.  It may be logits itself (ld_d == ld), or else memory apart.
  *            dlogits[c] = dloss * slope / T * ([c == a] - softmax(z)[c]).
  * m < 2^31, v up to 2^31 - 16384, leading dimensions below 2^31; m == 0 is a successful no-op; v == 0 counts as rows without a
- * token.  T is taken as log2(e) / c with c rounded to binary32: it differs from the given one by 2^-24 at most, relatively.
+ * token.  T is taken as log2(e) / c with c rounded to binary32: it differs from the given one by 2^-24 at most, relatively (beyond 1.2e38,
+ * where c has fewer bits, by 2^-22).
  */
 
 /*
