@@ -952,6 +952,12 @@ def _alike(t: torch.Tensor) -> torch.Tensor:
     return torch.empty_strided((m, n), (ld, 1), dtype=t.dtype, device=t.device) if m > 1 and n < ld <= 2 * n else t.new_empty((m, n))
 
 
+def _new_rows(t: torch.Tensor, m: int, n: int):
+    """(tensor, address, leading dimension): a new one like the matrix t, [m][n]."""
+    new = _alike(t)
+    return new, new.data_ptr(), new.stride(0) if m > 1 else n
+
+
 def policy(logits: torch.Tensor, index: torch.Tensor, advantage: torch.Tensor, old_logp: torch.Tensor | None = None,
            ref_logp: torch.Tensor | None = None, kl: float = 0.0, clip_low: float = 0.2, clip_high: float = 0.2, temperature: float = 1.0,
            dloss: torch.Tensor | None = None, loss: torch.Tensor | None = None, logp: torch.Tensor | None = None,
@@ -1116,12 +1122,15 @@ def join(x: torch.Tensor, y: torch.Tensor | None = None, w_post: torch.Tensor | 
     p_y, ld_y = (None, 0) if y is None else _row_tensor(y, x.shape, x.dtype, "y")
     keep = s is None and y is None and residual_scale == 1.0 and w_pre is not None
     given = s, z
-    if s is None and not keep:
-        s = _alike(x)
-    p_s, ld_s = (None, 0) if s is None else _row_tensor(s, x.shape, x.dtype, "s")
-    if z is None and w_pre is not None:
-        z = _alike(x)
-    p_z, ld_z = (None, 0) if z is None else _row_tensor(z, x.shape, x.dtype, "z")
+    p_s, ld_s, p_z, ld_z = None, 0, None, 0
+    if s is not None:
+        p_s, ld_s = _row_tensor(s, x.shape, x.dtype, "s")
+    elif not keep:
+        s, p_s, ld_s = _new_rows(x, m, n)
+    if z is not None:
+        p_z, ld_z = _row_tensor(z, x.shape, x.dtype, "z")
+    elif w_pre is not None:
+        z, p_z, ld_z = _new_rows(x, m, n)
     stats, p_stats = _made(stats, x, (m, 4), "stats")
     st = lib().bz_join(x.data_ptr(), ld_x, p_y, ld_y, dt, m, n, _norm(norm), eps, p_post, p_gate, groups, residual_scale, branch_scale, rate, p_rng,
                        p_pre, p_s, ld_s, p_z, ld_z, p_stats, _stream())
@@ -1180,12 +1189,12 @@ def join_backward(stream: torch.Tensor | None = None, y: torch.Tensor | None = N
     p_y, ld_y = (None, 0) if y is None else _row_tensor(y, *like, "y")
     p_ds, ld_ds = (None, 0) if ds is None else _row_tensor(ds, *like, "ds")
     p_dz, ld_dz = (None, 0) if dz is None else _row_tensor(dz, *like, "dz")
-    if dx is None:
-        dx = _alike(x)
-    p_dx, ld_dx = _row_tensor(dx, *like, "dx")
-    if dy is None and y is not None:
-        dy = _alike(y)
-    p_dy, ld_dy = (None, 0) if dy is None else _row_tensor(dy, *like, "dy")
+    dx, p_dx, ld_dx = (dx, *_row_tensor(dx, *like, "dx")) if dx is not None else _new_rows(x, m, n)
+    p_dy, ld_dy = None, 0
+    if dy is not None:
+        p_dy, ld_dy = _row_tensor(dy, *like, "dy")
+    elif y is not None:
+        dy, p_dy, ld_dy = _new_rows(y, m, n)
     p_dpost = p_dgate = p_dpre = None
     if w_post is not None:
         dw_post, p_dpost = _made(dw_post, x, (n,), "dw_post")
