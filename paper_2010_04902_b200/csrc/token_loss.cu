@@ -197,8 +197,8 @@ __device__ __forceinline__ void finish_without(const TokenArgs& a, int64_t i, bo
 // A thread copies its own 16-byte words of the row (cp.async, up to four groups), takes each group into its largest logit and sum as it
 // arrives, and with a gradient passes over them again out of shared memory: the row comes from memory once.  The row's maximum and
 // sum cost one exchange, the scalars of its loss one warp in binary64.  Nothing of a row overlaps inside its CTA but the loads; three CTAs or
-// more on an SM, each at another point of its row, do that.  4096 x 32128 bfloat16 with the gradient: 106 us, 81 at the copy's rate;
-// issue slots 52 %, exponentials 59 %, two an element.  Of other forms, rows kept as exponentials in registers with the next one on its way (two
+// more on an SM, each at another point of its row, do that.  4096 x 32128 bfloat16 with the gradient: 108 us, 81 at the copy's rate;
+// issue slots 52 %, exponentials 61 %, two an element.  Of other forms, rows kept as exponentials in registers with the next one on its way (two
 // CTAs an SM) took 148 us, rows through a ring with warps for each part of the work 170 (most of it bookkeeping of sixteen
 // warps for rows of four chunks), the row read again out of the L2 129.
 
