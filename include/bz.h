@@ -640,8 +640,8 @@ int bz_distill_backward(const void* logits, int64_t ld, int dtype, int64_t m, in
  *   logp     device binary32 [m], or NULL: receives lp.  It is at most 0, and 0 where the other tokens vanish beside the row's own.  Beside its
  *            rounding it is off by that of the row's sum in binary32: 1.1e-6 at most over rows of 300 to 70001 normal logits.
  *   stats    device binary32 [m][4], 16-byte aligned, for the backward call: the row's largest logit, the sum of
- *            exp((logits - that) / T), the slope d loss / d lp, and (an int32's bits) the place of the row's upstream gradient
- *            in dloss.
+ *            exp((logits - that) / T) (negative where the token has more than half of it), the slope d loss / d lp, and (an int32's
+ *            bits) the place of the row's upstream gradient in dloss.
  *   dlogits  device [m][v] with ld_d, dtype's elements, or NULL: the loss alone.  It may be logits itself (ld_d == ld), or else memory apart.
  *            dlogits[c] = dloss * slope / T * ([c == a] - softmax(z)[c]).
  * m < 2^31, v up to 2^31 - 16384, leading dimensions below 2^31; m == 0 is a successful no-op; v == 0 counts as rows without a

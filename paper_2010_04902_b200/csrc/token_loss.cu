@@ -31,7 +31,7 @@ struct TokenArgs {
     const float* dloss;
     uint32_t places;          // of dloss, for the gradient alone
     float *loss, *logp;
-    float4* stats;            // largest logit, sum of e^((s - that)/T), slope, place in dloss
+    float4* stats;            // largest logit, sum of e^((s - that)/T) (negative: the token is likely), slope, place in dloss
 };
 
 __device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
@@ -141,18 +141,22 @@ template <bool POLICY> __device__ __forceinline__ RowInputs row_inputs(const Tok
 struct RowScalars {
     double lp, sum, rest;
     float loss, slope;
+    float own;      // the token's exponential
+    bool likely;    // more than half of the sum
     // of the gradient: g times (indicator of the token less softmax)
     __device__ __forceinline__ float factor(const TokenArgs& a, const RowInputs& in) const { return slope == 0.f ? 0.f : slope * in.dloss / a.temperature; }
+    // at the token: g (1 - p) by what the sum has beside it, or a rounded p would leave its rounding
+    __device__ __forceinline__ float at_token(float g, float sum_) const { return g == 0.f ? 0.f : g * ((sum_ - own) / sum_); }
 };
 template <bool POLICY> __device__ __forceinline__ RowScalars row_scalars(const TokenArgs& a, const RowInputs& in, const MaxSum& all) {
     const Base base(a, all.m);
-    RowScalars s{0.0, static_cast<double>(all.s) * kPowers, exact_rest(a, base), 0.f, 0.f};
+    RowScalars s{0.0, static_cast<double>(all.s) * kPowers, exact_rest(a, base), 0.f, 0.f, exp2_fast(base.exponent(a, in.logit)), false};
     // A token that has most of the row goes by its own exponential, which is a term of the sum bit for bit (it is the largest, and its thread's
     // whole number was the row's): sums only grow, so lp is at most 0, and 0 where the others vanish beside it.  The correction is a mean over
     // many terms and has no place there.
-    const float own = in.logit == all.m ? exp2_fast(base.exponent(a, in.logit)) : 0.f;
-    if (own > 0.5f * all.s)
-        s.lp = 0.0 - log1p((static_cast<double>(all.s) - static_cast<double>(own)) / static_cast<double>(own));
+    s.likely = in.logit == all.m && s.own > 0.5f * all.s;
+    if (s.likely)
+        s.lp = 0.0 - log1p((static_cast<double>(all.s) - static_cast<double>(s.own)) / static_cast<double>(s.own));
     else
         s.lp = log_probability(a, in.logit, all.m, s.rest, s.sum);
     if (POLICY) {
@@ -184,7 +188,9 @@ __device__ __forceinline__ void write_row(const TokenArgs& a, int64_t i, const M
     // until a pair's slopes are known the last place holds what lp has beyond binary32
     const float lp = static_cast<float>(s.lp), rest = isfinite(lp) ? static_cast<float>(s.lp - static_cast<double>(lp)) : 0.f;
     if (a.logp != nullptr) a.logp[i] = lp;
-    if (a.stats != nullptr) a.stats[i] = make_float4(all.m, static_cast<float>(s.sum * exp2(-s.rest)), s.slope, policy ? __int_as_float(static_cast<int>(i)) : rest);
+    // a likely token is the largest itself; the sign tells the gradient's call
+    const float sum = s.likely ? -all.s / s.own : static_cast<float>(s.sum * exp2(-s.rest));
+    if (a.stats != nullptr) a.stats[i] = make_float4(all.m, sum, s.slope, policy ? __int_as_float(static_cast<int>(i)) : rest);
 }
 __device__ __forceinline__ void finish_without(const TokenArgs& a, int64_t i, bool policy) {
     if (a.logp != nullptr) a.logp[i] = 0.f;
@@ -221,7 +227,7 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
     constexpr int N = Word<T>::kN;
     extern __shared__ __align__(16) uint4 held[];
     __shared__ MaxSum part[16], peers[kMostRanks];
-    __shared__ float3 outcome;   // the row's largest, the exponentials' factor, the gradient's
+    __shared__ float4 outcome;   // the row's largest, the exponentials' factor, the gradient's, its entry at the token
     const int threads = THREADS ? THREADS : blockDim.x, t = threadIdx.x, warp = t >> 5, lane = t & 31;
     const unsigned r = share.ranks == 1 ? blockIdx.x : blockIdx.x / static_cast<unsigned>(share.ranks);
     const int rank = static_cast<int>(blockIdx.x - r * share.ranks);
@@ -237,7 +243,7 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
     // batches, and those without any of these and without words behind the last
     const int batches = (count + kBatch * threads - 1) / (kBatch * threads), stride = threads * 16, plain_from = head >= 0, plain_to = (count - (tail >= 0)) / (kBatch * threads);
     const bool there = has_token(a, at);
-    float g = 0.f, f = 0.f, top = 0.f;
+    float g = 0.f, f = 0.f, top = 0.f, hot = 0.f;
     if (there) {
         const char* from = reinterpret_cast<const char*>(row - lead) + (begin + t) * int64_t(16);
         uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(held + t));
@@ -302,13 +308,13 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
             scalars = row_scalars<POLICY>(a, in, sum);
             if (GRADIENT) {
                 const float got = scalars.factor(a, in);
-                if (lane == 0) outcome = make_float3(sum.m, got == 0.f ? 0.f : -got / sum.s, got);
+                if (lane == 0) outcome = make_float4(sum.m, got == 0.f ? 0.f : -got / sum.s, got, scalars.at_token(got, sum.s));
             }
         }
         if (GRADIENT) __syncthreads();
         if (t == 0 && rank == 0) write_row(a, i, sum, scalars, POLICY);
         if (!GRADIENT) return;
-        top = outcome.x, f = outcome.y, g = outcome.z;
+        top = outcome.x, f = outcome.y, g = outcome.z, hot = outcome.w;
     } else {
         if (share.ranks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (t == 0 && rank == 0) finish_without(a, i, POLICY);
@@ -351,10 +357,7 @@ __global__ void __launch_bounds__(kShared, 4) token_shared_kernel(const __grid_c
     }
     if (g != 0.f) {   // the token's place, once more, by the thread that has just written it
         const int w = (at + lead) / N - begin;
-        if (w >= 0 && w < count && w % threads == t) {
-            const int e = (at + lead) % N;
-            out[at] = from_f32<T>(fmaf(exp2_fast(base.exponent(a, to_f32(reinterpret_cast<const T*>(held + w)[e]))), f, g));
-        }
+        if (w >= 0 && w < count && w % threads == t) out[at] = from_f32<T>(hot);
     }
 }
 
@@ -444,7 +447,7 @@ template <typename T, int VEC> __device__ __forceinline__ MaxSum row_statistics(
 // One CTA a row.  POLICY: the loss too, and the gradient if it is wanted; otherwise lp and stats alone.
 template <typename T, int VEC, bool POLICY> __global__ void __launch_bounds__(kTeam) token_rows_kernel(const __grid_constant__ TokenArgs a, const T* logits, T* dlogits) {
     __shared__ MaxSum part[32];
-    __shared__ float factor;
+    __shared__ float2 factor;   // of the gradient, its entry at the token
     const int64_t i = blockIdx.x;
     const T* row = logits + i * a.ld;
     const int at = a.index[i];
@@ -452,11 +455,11 @@ template <typename T, int VEC, bool POLICY> __global__ void __launch_bounds__(kT
     MaxSum all{-INFINITY, 0.f};
     if (there) all = row_statistics<T, VEC>(a, row, part);
     if (threadIdx.x < 32) {
-        float g = 0.f;
+        float2 g = pair(0.f);
         if (there) {
             const RowInputs in = row_inputs<POLICY>(a, i, to_f32(row[at]));
             const RowScalars scalars = row_scalars<POLICY>(a, in, all);
-            g = scalars.factor(a, in);
+            g.x = scalars.factor(a, in), g.y = scalars.at_token(g.x, all.s);
             if (threadIdx.x == 0) write_row(a, i, all, scalars, POLICY);
         } else if (threadIdx.x == 0) {
             finish_without(a, i, POLICY);
@@ -465,14 +468,14 @@ template <typename T, int VEC, bool POLICY> __global__ void __launch_bounds__(kT
     }
     if (!POLICY || dlogits == nullptr) return;
     __syncthreads();
-    const float g = factor, f = g == 0.f ? 0.f : -g / all.s;
+    const float g = factor.x, hot = factor.y, f = g == 0.f ? 0.f : -g / all.s;
     const Base base(a, all.m);
     T* out = dlogits + i * a.ld_d;
     for (int64_t j0 = static_cast<int64_t>(threadIdx.x) * VEC - row_lead<T, VEC>(row); j0 < a.v; j0 += blockDim.x * VEC) {
         float x[VEC];
         load_slot<T, VEC>(row, j0, a.v, -INFINITY, x);
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) x[k] = g == 0.f ? 0.f : exp2_fast(base.exponent(a, x[k])) * f + (j0 + k == at ? g : 0.f);
+        for (int k = 0; k < VEC; ++k) x[k] = g == 0.f ? 0.f : j0 + k == at ? hot : exp2_fast(base.exponent(a, x[k])) * f;
         store_slot<T, VEC>(out, j0, a.v, x);
     }
 }
@@ -507,9 +510,9 @@ __global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const 
     for (int q = 0; q < kSlots; ++q) raw[q].fetch(row + first(q), whole(first(q)));
     const float4 st = a.stats[i];
     const int at = a.index[i];
-    const float g = st.z == 0.f || !has_token(a, at) ? 0.f : st.z * upstream(a, st.w) / a.temperature;
+    const float g = st.z == 0.f || !has_token(a, at) ? 0.f : st.z * upstream(a, st.w) / a.temperature, sum = fabsf(st.y);
     const Base reference(a, st.x);
-    const float f = g == 0.f ? 0.f : -g / st.y * exp2_fast(-reference.rest(a));
+    const float f = g == 0.f ? 0.f : -g / sum * exp2_fast(-reference.rest(a));
 #pragma unroll
     for (int q = 0; q < kSlots; ++q) {
         const int j0 = first(q);
@@ -530,6 +533,11 @@ __global__ void __launch_bounds__(kGradientThreads) token_gradient_kernel(const 
                 if (j0 + e == at) x[e] += g;
         }
         store_slot<T, VEC>(out, j0, n, x);
+    }
+    if (st.y < 0.f && g != 0.f) {   // a likely token's entry once more, by the thread that has just written it
+        rare();
+        const unsigned from = static_cast<unsigned>(at - base), slot = static_cast<unsigned>(threads * VEC);
+        if (from / slot < kSlots && from % slot < VEC) out[at] = from_f32<T>(g * ((sum - 1.f) / sum));
     }
 }
 
