@@ -106,3 +106,25 @@ def test_neighbours_far_from_zero(fill, T):
     # a probability's exponent is off by the temperature's 2^-24 too
     bound = bound + 3 * F32 * ((q.clamp(min=1e-300).log().abs() + 3) * q / T) + F32 * want.abs() + TINY[torch.float32]
     assert near(d, want, bound) and near(bz.token_loss_backward(x["logits"], x["index"], stats, None, T), want, bound)
+
+
+@pytest.mark.parametrize("T", [1e-3, 1e-6, 1e-9, 1e-30])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("m,v", SIZES)
+def test_low_temperatures(m, v, dtype, T):
+    """Ordinary logits, whose exponents a low temperature takes as far: nearly all of a row is its largest token's.  The temperature reaches the
+    kernel as a binary32 number, and exponentials below 2^-126 become 0."""
+    T = float(torch.tensor(T))
+    x = make(m, v, dtype, 9, T=T)
+    x["index"][::2] = x["logits"][::2].float().argmax(1).int()
+    ones = torch.ones(m, device="cuda")
+    _, logp, stats, d = bz.policy(x["logits"], x["index"], ones, temperature=T, dloss=ones)
+    lp, q, there, at = tokens(x["logits"], x["index"], T)
+    assert near(logp, lp, TOL + 3 * F32 * lp.abs()) and (logp <= 0).all()
+    one = torch.ones(m, dtype=torch.float64)
+    want, bound = gradient(q, there, at, -one, one, one, T)
+    # a probability's exponent is off by the temperature's 2^-24 too
+    bound = bound + 3 * F32 * q.clamp(min=1e-300).log().abs() * q / T + HALF_UNIT[dtype] * want.abs() + TINY[dtype] + 2.0 ** -125 / T
+    most = torch.finfo(dtype).max * (1 + HALF_UNIT[dtype])      # beyond it the rounded value is an infinity
+    want = torch.where(want.abs() > most, want.sign() * float("inf"), want)
+    assert near(d, want, bound) and near(bz.token_loss_backward(x["logits"], x["index"], stats, None, T), want, bound)
